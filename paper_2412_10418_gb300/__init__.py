@@ -17,7 +17,7 @@ from typing import List, Optional, Sequence
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libcdsl_gb300.so")
 
-DTYPE_F32, DTYPE_BF16 = 0, 1
+DTYPE_F32, DTYPE_BF16, DTYPE_F8E4M3 = 0, 1, 2   # (e4m3: of a KvCache)
 STATUS = {0: "CDSL_OK", 1: "CDSL_EINVAL", 2: "CDSL_ENOMEM", 3: "CDSL_ECUDA", 4: "CDSL_ETIMEOUT",
           5: "CDSL_ENONFINITE", 6: "CDSL_ESTATE", 7: "CDSL_ERANGE"}
 (CDSL_OK, CDSL_EINVAL, CDSL_ENOMEM, CDSL_ECUDA, CDSL_ETIMEOUT, CDSL_ENONFINITE, CDSL_ESTATE,
@@ -71,6 +71,15 @@ EXPORTS = {
     "cdsl_get_profile_launches": (_I, [_P, ctypes.POINTER(ctypes.c_double), _I]),
     "cdsl_gemv_noalloc": (_I, [_P, _I, _I, _P, _I, _P, _P]),
     "cdsl_set_wait_limit": (_I, [_P, ctypes.c_uint64]),
+    "cdsl_kv_write": (_I, [_P, _I, _P, _P, _I, _I, _P, _P, _P, _P, _P]),
+    "cdsl_kv_read": (_I, [_P, _I, _I, _P, _P, _I, _I, _P, _P, _P, _P]),
+    "cdsl_kv_commit": (_I, [_P, _P, _P, _P, _I, _P, _P, _P]),
+    "cdsl_tree_mask": (_I, [_P, _I, _P, _P]),
+    "cdsl_tree_attention_workspace": (_I, [_P, _I, _I, _P]),
+    "cdsl_tree_attention": (_I, [_P, _I, _P, _I, _I, _I, _P, _P, _P, _P, ctypes.c_float, _I, _P, _P, _P,
+                                 ctypes.c_size_t, _P, _P]),
+    "cdsl_tree_verify": (_I, [_I, _I, _I, _P, _P, _I, _P, _P, _P, _P, _P, _P, ctypes.c_float, _P, _P, _P,
+                              _P, _P]),
     "cdsl_last_error": (ctypes.c_char_p, [_P]),
     "cdsl_destroy": (None, [_P]),
 }
@@ -268,6 +277,237 @@ def cdsl_last_error(ctx=None) -> str:
 
 def cdsl_destroy(ctx):
     lib().cdsl_destroy(ctx)
+
+
+# ------------------------------------------------------------------------------ tree speculation
+# The C ABI sees pointers, sizes and strides; types, shapes, layouts and devices are checked here, and
+# anything the calls cannot take raises CdslError(CDSL_EINVAL) before a call. `stream` is a cudaStream_t
+# as an integer, None the current torch stream. Semantics: include/cdsl_tree.h.
+
+class _KvCacheC(ctypes.Structure):
+    _fields_ = [("d_pool", _P), ("d_scale", _P), ("d_page_table", _P), ("n_layers", _I), ("n_pages", _I),
+                ("n_kv_heads", _I), ("page_size", _I), ("head_dim", _I), ("dtype", _I), ("batch", _I),
+                ("max_pages", _I)]
+
+
+class _Types:
+    """torch and its types that the bindings compare with (torch is imported on first use)."""
+
+    def __init__(self):
+        import torch
+
+        self.torch = torch
+        self.i32, self.f32, self.bf16, self.u8 = torch.int32, torch.float32, torch.bfloat16, torch.uint8
+        self.values = {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16}
+        self.caches = {torch.float8_e4m3fn: DTYPE_F8E4M3, torch.bfloat16: DTYPE_BF16}
+
+
+_types: Optional[_Types] = None
+
+
+def _torch() -> _Types:
+    global _types
+    if _types is None:
+        _types = _Types()
+    return _types
+
+
+def _bad(fn: str, why: str):
+    raise CdslError(CDSL_EINVAL, f"{fn}: {why}")
+
+
+def _ints(fn: str, name: str, t, shape, device, dtype=None):
+    """A contiguous int32 (or `dtype`) tensor of this shape on this device: its pointer."""
+    if t.dtype is not (dtype or _types.i32) or t.shape != shape or not t.is_contiguous() or t.device != device:
+        _bad(fn, f"{name} must be a contiguous {dtype or _types.i32} tensor {tuple(shape)} on {device}, got "
+                 f"{t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def _optional(fn, name, t, shape, device, dtype=None):
+    return None if t is None else _ints(fn, name, t, shape, device, dtype)
+
+
+def _stream(stream, device):
+    if stream is None:
+        return _types.torch.cuda.current_stream(device).cuda_stream
+    return stream
+
+
+class KvCache:
+    """A paged K/V cache in e4m3 or bfloat16: ``pool`` [layers, pages, 2, kv_heads, page_size, head_dim] of
+    torch.float8_e4m3fn or torch.bfloat16, ``scale`` [layers, pages, 2, kv_heads, page_size] uint8 (a row's
+    values are code * 2^(byte - 127)) and ``page_table`` [batch, max_pages] int32, all contiguous on one CUDA
+    device. The tensors are the caller's; the object keeps them referenced. ``cache.at(page_table)`` is
+    the same pool under another table (another set of sequences)."""
+
+    def __init__(self, pool, scale, page_table):
+        ty = _torch()
+        if not pool.is_cuda:
+            _bad("KvCache", "pool must be on a CUDA device")
+        if pool.dim() != 6 or pool.shape[2] != 2 or not pool.is_contiguous() or pool.dtype not in ty.caches:
+            _bad("KvCache", "pool must be a contiguous float8_e4m3fn or bfloat16 tensor [layers, pages, 2, "
+                            "kv_heads, page_size, head_dim]")
+        L, N, _, H, P, D = pool.shape
+        _ints("KvCache", "scale", scale, pool.shape[:5], pool.device, ty.u8)
+        if page_table.dim() != 2:
+            _bad("KvCache", "page_table must be [batch, max_pages]")
+        _ints("KvCache", "page_table", page_table, page_table.shape, pool.device)
+        self.pool, self.scale, self.page_table, self.device = pool, scale, page_table, pool.device
+        self.batch, self.n_layers, self.n_kv_heads, self.head_dim = page_table.shape[0], L, H, D
+        self._c = _KvCacheC(pool.data_ptr(), scale.data_ptr(), page_table.data_ptr(), L, N, H, P, D,
+                            ty.caches[pool.dtype], page_table.shape[0], page_table.shape[1])
+        self._ref = ctypes.addressof(self._c)
+        self._one = ty.torch.Size((self.batch,))
+
+    @classmethod
+    def empty(cls, n_layers, n_pages, n_kv_heads, page_size, head_dim, page_table, dtype=None):
+        """A cache with memory of its own (dtype: torch.float8_e4m3fn, the default, or torch.bfloat16)."""
+        t = _torch().torch
+        pool = t.empty((n_layers, n_pages, 2, n_kv_heads, page_size, head_dim), dtype=dtype or t.float8_e4m3fn,
+                       device=page_table.device)
+        return cls(pool, t.empty(pool.shape[:5], dtype=t.uint8, device=page_table.device), page_table)
+
+    def at(self, page_table):
+        return KvCache(self.pool, self.scale, page_table)
+
+
+def _rows(fn, cache, name, x, heads, T=None):
+    """[batch, T, heads, head_dim] with a contiguous last dimension: (type code, T)."""
+    code = _types.values.get(x.dtype)
+    s = x.shape
+    if (code is None or len(s) != 4 or s[0] != cache.batch or s[2] != heads or s[3] != cache.head_dim
+            or (T is not None and s[1] != T) or x.device != cache.device or (x.stride(3) != 1)):
+        _bad(fn, f"{name} must be a float32 or bfloat16 tensor [{cache.batch}, {'T' if T is None else T}, {heads}, "
+                 f"{cache.head_dim}] on {cache.device} with a contiguous last dimension, got {x.dtype} {tuple(s)} "
+                 f"{tuple(x.stride())} on {x.device}")
+    return code, s[1]
+
+
+_Strides6 = ctypes.c_int64 * 6
+_Strides4 = ctypes.c_int64 * 4
+
+
+def cdsl_kv_write(cache: KvCache, layer: int, k, v, start, count=None, status=None, stream=None):
+    """Rows k, v [batch, T, kv_heads, head_dim] (float32 or bfloat16, any strides but the last) into slots
+    start[b] + i of the layer, i < count[b] (None: all)."""
+    fn = "cdsl_kv_write"
+    code, T = _rows(fn, cache, "k", k, cache.n_kv_heads)
+    if v.dtype is not k.dtype:
+        _bad(fn, "k and v must have one type")
+    _rows(fn, cache, "v", v, cache.n_kv_heads, T)
+    st = _Strides6(*k.stride()[:3], *v.stride()[:3])
+    _check(lib().cdsl_kv_write(cache._ref, layer, k.data_ptr(), v.data_ptr(), code, T, st,
+                               _ints(fn, "start", start, cache._one, cache.device),
+                               _optional(fn, "count", count, cache._one, cache.device),
+                               _optional(fn, "status", status, (1,), cache.device),
+                               _stream(stream, cache.device)))
+
+
+def cdsl_kv_read(cache: KvCache, layer: int, start, k, v, count=None, status=None, stream=None):
+    """Slots start[b] + i of layers layer .. layer + n - 1 back as values into k, v [n, batch, T, kv_heads,
+    head_dim] (contiguous, float32 or bfloat16); rows i >= count[b] become zeros."""
+    fn = "cdsl_kv_read"
+    code = _types.values.get(k.dtype)
+    s = k.shape
+    if (code is None or len(s) != 5 or s[1] != cache.batch or s[3] != cache.n_kv_heads or s[4] != cache.head_dim
+            or v.shape != s or v.dtype is not k.dtype or not k.is_contiguous() or not v.is_contiguous()
+            or k.device != cache.device or v.device != cache.device):
+        _bad(fn, f"k and v must be contiguous float32 or bfloat16 tensors [n_layers, {cache.batch}, T, "
+                 f"{cache.n_kv_heads}, {cache.head_dim}] on {cache.device}")
+    _check(lib().cdsl_kv_read(cache._ref, layer, s[0], k.data_ptr(), v.data_ptr(), code, s[2],
+                              _ints(fn, "start", start, cache._one, cache.device),
+                              _optional(fn, "count", count, cache._one, cache.device),
+                              _optional(fn, "status", status, (1,), cache.device),
+                              _stream(stream, cache.device)))
+
+
+def cdsl_kv_commit(cache: KvCache, lens, path, n_path, new_lens=None, status=None, stream=None):
+    """The taken paths' rows of every layer to their places: slot lens[b] + path[b, i] to lens[b] + i; new_lens
+    [batch] becomes lens + n_path."""
+    fn = "cdsl_kv_commit"
+    if path.dim() != 2:
+        _bad(fn, "path must be [batch, T]")
+    T = path.shape[1]
+    _check(lib().cdsl_kv_commit(cache._ref, _ints(fn, "lens", lens, cache._one, cache.device),
+                                _ints(fn, "path", path, (cache.batch, T), cache.device),
+                                _ints(fn, "n_path", n_path, cache._one, cache.device), T,
+                                _optional(fn, "new_lens", new_lens, cache._one, cache.device),
+                                _optional(fn, "status", status, (1,), cache.device),
+                                _stream(stream, cache.device)))
+
+
+def cdsl_tree_mask(parents: Sequence[int]):
+    """(mask, depth) of a tree on the host: mask a CPU int32 tensor [T, (T + 31) // 32] of ancestor bits,
+    depth [T] each node's number of ancestors. parents[i] < i; parents[0] is ignored."""
+    t = _torch().torch
+    T = len(parents)
+    p = (ctypes.c_int32 * T)(*[int(x) for x in parents])
+    mask = t.zeros((T, (T + 31) // 32), dtype=t.int32)
+    depth = t.zeros(T, dtype=t.int32)
+    _check(lib().cdsl_tree_mask(p, T, mask.data_ptr(), depth.data_ptr()))
+    return mask, depth
+
+
+def cdsl_tree_attention_workspace(cache: KvCache, T: int, n_heads: int) -> int:
+    """Bytes of workspace that cdsl_tree_attention needs for trees of up to T nodes."""
+    n = ctypes.c_size_t(0)
+    _check(lib().cdsl_tree_attention_workspace(cache._ref, n_heads, T, ctypes.byref(n)))
+    return n.value
+
+
+def cdsl_tree_attention(cache: KvCache, layer: int, q, lens, mask, out, workspace, *, scale: float, max_len: int,
+                        nodes=None, lse=None, status=None, stream=None):
+    """Attention of each sequence's tree of T nodes, q and out [batch, T, n_heads, head_dim] (one type, any
+    strides but the last), over its lens[b] cached slots and the tree's own after them, by the ancestor bits of
+    mask [batch, T, (T + 31) // 32]."""
+    fn = "cdsl_tree_attention"
+    if q.dim() != 4:
+        _bad(fn, "q must be [batch, T, n_heads, head_dim]")
+    H = q.shape[2]
+    code, T = _rows(fn, cache, "q", q, H)
+    if out.dtype is not q.dtype:
+        _bad(fn, "out must have q's type")
+    _rows(fn, cache, "out", out, H, T)
+    dev = cache.device
+    if workspace.dtype is not _types.u8 or not workspace.is_contiguous() or workspace.device != dev:
+        _bad(fn, f"workspace must be a contiguous uint8 tensor on {dev}")
+    st = _Strides6(*q.stride()[:3], *out.stride()[:3])
+    _check(lib().cdsl_tree_attention(
+        cache._ref, layer, q.data_ptr(), code, H, T, st, _ints(fn, "lens", lens, cache._one, dev),
+        _optional(fn, "nodes", nodes, cache._one, dev),
+        _ints(fn, "mask", mask, (cache.batch, T, (T + 31) // 32), dev), scale, max_len, out.data_ptr(),
+        _optional(fn, "lse", lse, (cache.batch, T, H), dev, _types.f32), workspace.data_ptr(), workspace.numel(),
+        _optional(fn, "status", status, (1,), dev), _stream(stream, dev)))
+
+
+def cdsl_tree_verify(logits, tokens, parents, u, u_last, path, n_path, emitted, *, draft_logits=None,
+                     temperature: float = 1.0, nodes=None, status=None, stream=None):
+    """Which path of each sequence's tree the target takes, and the next token: logits (and draft_logits)
+    [batch, T, vocab] float32 or bfloat16 with a contiguous last dimension; tokens, parents, path, emitted
+    [batch, T] and n_path, nodes [batch] int32; u [batch, T] and u_last [batch] float32 in [0, 1)."""
+    ty = _torch()
+    fn = "cdsl_tree_verify"
+    code = ty.values.get(logits.dtype)
+    if code is None or logits.dim() != 3 or not logits.is_cuda or logits.stride(2) != 1:
+        _bad(fn, "logits must be a CUDA float32 or bfloat16 tensor [batch, T, vocab] with a contiguous last dimension")
+    B, T, V = logits.shape
+    dev = logits.device
+    st = logits.stride()
+    sd = st
+    if draft_logits is not None:
+        sd = draft_logits.stride()
+        if (draft_logits.dtype is not logits.dtype or draft_logits.shape != logits.shape or sd[2] != 1
+                or draft_logits.device != dev):
+            _bad(fn, "draft_logits must be like logits")
+    one, all_ = (B,), (B, T)
+    _check(lib().cdsl_tree_verify(
+        B, T, V, logits.data_ptr(), _ptr(draft_logits), code, _Strides4(st[0], st[1], sd[0], sd[1]),
+        _ints(fn, "tokens", tokens, all_, dev), _ints(fn, "parents", parents, all_, dev),
+        _optional(fn, "nodes", nodes, one, dev), _ints(fn, "u", u, all_, dev, ty.f32),
+        _ints(fn, "u_last", u_last, one, dev, ty.f32), temperature, _ints(fn, "path", path, all_, dev),
+        _ints(fn, "n_path", n_path, one, dev), _ints(fn, "emitted", emitted, all_, dev),
+        _optional(fn, "status", status, (1,), dev), _stream(stream, dev)))
 
 
 # ------------------------------------------------------------------------------ Engine
