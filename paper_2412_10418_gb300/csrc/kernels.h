@@ -172,6 +172,9 @@ bool tc_supported(const GemmArgs& a);
 TcPlan plan_tc(int K, int n_virtual, int R, int n_sm, int force_per_sm = 0, int max_split = 0,
                int cluster = -1);
 size_t tc_scratch_floats(const TcPlan& p);
+// (encode_map: any element type and swizzle.)
+int encode_map(CUtensorMap* m, CUtensorMapDataType type, int elem_bytes, const void* base, uint64_t inner,
+               uint64_t outer, uint32_t box_inner, uint32_t box_outer, CUtensorMapSwizzle swizzle);
 int encode_bf16_map(CUtensorMap* m, const void* base, uint64_t inner, uint64_t outer,
                     uint32_t box_inner, uint32_t box_outer);
 int configure_gemm_tc();

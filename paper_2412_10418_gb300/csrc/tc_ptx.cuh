@@ -244,6 +244,16 @@ __device__ __forceinline__ uint64_t desc_sw128_mn(uint32_t saddr, uint32_t block
   return d | (uint64_t)(block >> 4) << 16;    // leading byte offset: between blocks along M / N
 }
 
+// Descriptor of an operand tile whose rows are `row` bytes (32, 64 or 128, which is also the swizzle's
+// span): K-major rows of `row` bytes of K, or MN-major rows of one K value; 8-row groups 8 * row bytes
+// apart. The tile base must be aligned to 8 * row bytes. block: MN-major, bytes to the next `row` bytes along M
+// or N (not used where one row holds all).
+__device__ __forceinline__ uint64_t desc_rows(uint32_t saddr, uint32_t row, uint32_t block) {
+  const uint64_t swizzle = row == 128 ? 2 : row == 64 ? 4 : 6;
+  return (uint64_t)((saddr & 0x3FFFFu) >> 4) | (uint64_t)(block >> 4) << 16 |
+         (uint64_t)(8 * row >> 4) << 32 | (uint64_t)1 << 46 | swizzle << 61;
+}
+
 // Instruction descriptor of kind::f16 with bf16 A and B (K-major; b_mn: B MN-major), fp32
 // accumulator.
 __host__ __device__ constexpr uint32_t idesc_bf16_f32(int M, int N, bool b_mn = false) {
@@ -261,6 +271,16 @@ __device__ __forceinline__ void umma_bf16(uint32_t tmem_d, uint64_t adesc, uint6
       "{\n\t.reg .pred p;\n\t"
       "setp.ne.b32 p, %4, 0;\n\t"
       "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(tmem_d),
+      "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+// The same of e4m3 A and B (kind::f8f6f4, K = 32 a step; the descriptor's formats are 0).
+__device__ __forceinline__ void umma_f8(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc,
+                                        uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(tmem_d),
       "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
       : "memory");
 }
@@ -356,6 +376,13 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const float (&v)[16]) 
       "r"(__float_as_uint(v[15]))
       : "memory");
   asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+}
+
+// Byte offset of 16-byte chunk `ch` of row `r` in an operand tile of desc_rows (the swizzle of spans
+// of `row` bytes exchanges 16-byte chunks by the address bits above 128).
+__device__ __forceinline__ uint32_t row_offset(int r, int ch, int row) {
+  const uint32_t x = row == 128 ? r & 7 : row == 64 ? (r >> 1) & 3 : (r >> 2) & 1;
+  return (uint32_t)(r * row) + ((uint32_t)(ch ^ x) << 4);
 }
 
 // Byte offset of 16-byte chunk `ch` (0..7) of row `r` in a K-major operand tile of 128-byte

@@ -263,18 +263,16 @@ struct Sizes {
 };
 constexpr int kSimtPerSM = 4;                  // resident k_tree_simt blocks per SM
 
-int sizes_of(const Cache& c, int dtype_bf16, int H, int T, Sizes* z) {
+void sizes_of(const Cache& c, bool tc, int H, int T, Sizes* z) {
   const int vectors = T * (H / c.kvh);
-  z->NQ = SQ;
+  z->NQ = tc ? tc_query_block(vectors) : SQ;
   z->QB = (vectors + z->NQ - 1) / z->NQ;
-  z->blocks = kPlanSMs * kSimtPerSM;
-  (void)dtype_bf16;
+  z->blocks = kPlanSMs * (tc ? tc_blocks_per_sm(c, z->NQ) : kSimtPerSM);
   const size_t slots = (size_t)z->blocks * 2 * z->NQ;
   auto up = [](size_t n) { return (n + 255) / 256 * 256; };
   z->ml_off = up((c.batch + 1) * sizeof(int32_t));
   z->o_off = up(z->ml_off + slots * 2 * sizeof(float));
   z->bytes = up(z->o_off + slots * c.hd * sizeof(float));
-  return 0;
 }
 
 template <typename T, int HD>
@@ -288,13 +286,15 @@ cudaError_t launch_simt(const TreeArgs& a, cudaStream_t s) {
   return launch_pdl(k_tree_simt<T, HD, F8>, dim3(a.blocks), dim3(kThreads), (a.c.batch + 1) * 4, s, a);
 }
 
-template <typename T>
-cudaError_t launch_pass(const TreeArgs& a, bool split, cudaStream_t s) {
+cudaError_t launch_pass(const TreeArgs& a, bool tc, bool split, cudaStream_t s) {
+  const bool d128 = a.c.hd == 128, f8 = a.c.eb == 1;
   cudaError_t e;
-  if (a.c.hd == 128) e = a.c.eb == 1 ? launch_simt<T, 128, true>(a, s) : launch_simt<T, 128, false>(a, s);
-  else e = a.c.eb == 1 ? launch_simt<T, 64, true>(a, s) : launch_simt<T, 64, false>(a, s);
+  if (tc) e = launch_tree_tc(a, s);
+  else if (d128) e = f8 ? launch_simt<float, 128, true>(a, s) : launch_simt<float, 128, false>(a, s);
+  else e = f8 ? launch_simt<float, 64, true>(a, s) : launch_simt<float, 64, false>(a, s);
   if (e != cudaSuccess || !split) return e;
-  return a.c.hd == 128 ? launch_combine<T, 128>(a, s) : launch_combine<T, 64>(a, s);
+  if (tc) return d128 ? launch_combine<__nv_bfloat16, 128>(a, s) : launch_combine<__nv_bfloat16, 64>(a, s);
+  return d128 ? launch_combine<float, 128>(a, s) : launch_combine<float, 64>(a, s);
 }
 
 bool heads_ok(const Check& ck, const Cache& c, int n_heads) {
@@ -333,8 +333,8 @@ extern "C" int32_t cdsl_tree_attention_workspace(const cdsl_kv_cache* cache, int
   if (!ck.cache(cache, &c, false) || !ck.nodes(c, T) || !heads_ok(ck, c, n_heads)) return CDSL_EINVAL;
   if (!bytes) return ck.fail("bytes is NULL");
   Sizes z[2];
-  sizes_of(c, 0, n_heads, T, &z[0]);
-  sizes_of(c, 1, n_heads, T, &z[1]);
+  sizes_of(c, false, n_heads, T, &z[0]);
+  sizes_of(c, true, n_heads, T, &z[1]);
   *bytes = std::max(z[0].bytes, z[1].bytes);
   return CDSL_OK;
 }
@@ -357,8 +357,9 @@ extern "C" int32_t cdsl_tree_attention(const cdsl_kv_cache* cache, int32_t layer
     return ck.fail("max_len must be 0 .. max_pages * page_size - T");
   const int eb = dtype == CDSL_DTYPE_BF16 ? 2 : 4;
   if (!ck.aligned(d_q, eb) || !ck.aligned(d_out, eb)) return ck.fail("q and out must be aligned to their type");
+  const bool tc = dtype == CDSL_DTYPE_BF16;
   Sizes z;
-  sizes_of(c, dtype == CDSL_DTYPE_BF16, n_heads, T, &z);
+  sizes_of(c, tc, n_heads, T, &z);
   if (!ck.aligned(d_workspace, 256) || workspace_bytes < z.bytes)
     return ck.fail("the workspace must be 256-byte aligned and hold cdsl_tree_attention_workspace bytes",
                    workspace_bytes < z.bytes ? CDSL_ENOMEM : CDSL_EINVAL);
@@ -382,6 +383,5 @@ extern "C" int32_t cdsl_tree_attention(const cdsl_kv_cache* cache, int32_t layer
   a.status = d_status;
   const bool split = chunks > 1;               // one chunk: every item is whole
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  return ck.launched(dtype == CDSL_DTYPE_BF16 ? launch_pass<__nv_bfloat16>(a, split, s)
-                                              : launch_pass<float>(a, split, s));
+  return ck.launched(launch_pass(a, tc, split, s));
 }

@@ -155,7 +155,7 @@ __device__ __forceinline__ void check_lens(const TreeArgs& a) {
 
 // The tensor-core kernels (tree_attention_tc.cu).
 int tc_query_block(int vectors);               // query vectors per block
-int tc_blocks(const Cache& c, int NQ);         // resident blocks, < 0: a CUDA error
+int tc_blocks_per_sm(const Cache& c, int NQ);
 cudaError_t launch_tree_tc(const TreeArgs& a, cudaStream_t s);
 
 }  // namespace tree
