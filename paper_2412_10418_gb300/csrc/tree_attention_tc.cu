@@ -94,13 +94,6 @@ __device__ __forceinline__ __half2 f8x2_half(uint32_t two) {
   asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((uint16_t)two));
   return *reinterpret_cast<__half2*>(&r);
 }
-__device__ __forceinline__ void tmem_ld16_raw(uint32_t taddr, float (&v)[16]) {
-  uint32_t r[16];
-  tc::tmem_ld16_nowait(taddr, r);
-#pragma unroll
-  for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
-}
-
 template <int HD, int NQ, bool F8>
 __global__ void __launch_bounds__(kThreads, Cfg<HD, NQ, F8>::CTAS)
     k_tree_tc(TreeArgs a, const __grid_constant__ CUtensorMap map) {
@@ -114,9 +107,11 @@ __global__ void __launch_bounds__(kThreads, Cfg<HD, NQ, F8>::CTAS)
   __shared__ uint32_t s_tmem;
   // per query vector: score factor (softmax scale and the row's own), reference in raw scores, what raises
   // it, reference in base 2; factors of a raise
-  __shared__ __align__(16) float s_qs[NQ], s_mq[NQ], s_alpha[NQ], s_beta[NQ];
-  __shared__ float s_ref[NQ], s_lim[NQ], s_wmax[4][NQ], s_l[4][NQ];
-  __shared__ uint32_t s_mask[NQ][kWords];
+  __shared__ __align__(16) float s_qs[NQ], s_mq[NQ], s_lim[NQ], s_alpha[NQ], s_beta[NQ], s_inv[NQ];
+  __shared__ float s_ref[NQ], s_wmax[4][NQ], s_l[4][NQ];
+  __shared__ int s_bad[NQ];                    // the query is not finite
+  __shared__ long long s_out[NQ];              // where its output begins
+  __shared__ uint32_t s_mask[NQ + 1][kWords];  // of the block's nodes
   __shared__ int s_vref, s_wv[4];
   const Cache& c = a.c;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -207,56 +202,65 @@ __global__ void __launch_bounds__(kThreads, Cfg<HD, NQ, F8>::CTAS)
         if constexpr (F8) tc::umma_f8(d, x, y, id, add);
         else tc::umma_bf16(d, x, y, id, add);
       };
+      // (a descriptor's low bits are its tile's address / 16: steps add to them)
+      constexpr uint32_t next = C::NB > 1 ? C::BLOCK : 8 * C::BW;   // of V along M; head_dim 64: what the
+                                               // second half of the M = 128 lanes reads and sums is not used
+      const uint64_t desc_k = tc::desc_rows(sbase + C::KV_OFF, C::BW, 16);
+      const uint64_t desc_q = tc::desc_rows(sbase + C::Q_OFF, C::BW, 16);
+      const uint64_t desc_v = tc::desc_rows(sbase + C::KV_OFF + C::TILE, C::BW, next);
+      const uint64_t desc_p = tc::desc_rows(sbase + C::P_OFF, C::RB, 16);
+      auto s_mma = [&](int i) {                // S of chunk i
+        const uint64_t k = desc_k + (uint32_t)(i % NST) * (2 * C::TILE / 16);
+        const uint32_t d = tmem + (i & 1) * NQ;
+#pragma unroll 1
+        for (int p = C::QP - 1; p >= 0; --p)
+#pragma unroll 1
+          for (int nb = 0; nb < C::NB; ++nb)
+#pragma unroll
+            for (int x = 0; x < C::BW / 32; ++x)
+              mma(d, k + (nb * C::BLOCK / 16 + 2 * x),
+                  desc_q + ((uint32_t)(p * C::Q_PLANE + nb * NQ * C::BW) / 16 + 2 * x), idesc_s,
+                  p < C::QP - 1 || nb + x > 0);
+        tc::umma_commit(&s_full[i & 1]);
+        tc::umma_commit(&k_empty[i % NST]);
+      };
       auto pv = [&](int i, bool add) {         // the P V of chunk i
         if (!tc::mbar_wait(&p_full, i & 1, a.status) ||
             !tc::mbar_wait(&v_full[i % NST], parity(i, NST), a.status))
           return false;
         tc::tc_fence_after();
-        const uint32_t v = sbase + C::KV_OFF + ((i % NST) * 2 + 1) * C::TILE;
-        // (head_dim 64: what the second half of the M = 128 lanes reads and sums is not used)
-        constexpr uint32_t next = C::NB > 1 ? C::BLOCK : 8 * C::BW;
-#pragma unroll
-        for (int k = 0; k < kKeys / STEP; ++k)
-#pragma unroll
-          for (int p = C::PP - 1; p >= 0; --p)
-            mma(t_o, tc::desc_rows(v + k * STEP * C::BW, C::BW, next),
-                tc::desc_rows(sbase + C::P_OFF + p * C::P_TILE + k * STEP * C::RB, C::RB, 16), idesc_o,
+        const uint64_t v = desc_v + (uint32_t)(i % NST) * (2 * C::TILE / 16);
+#pragma unroll 1
+        for (int p = C::PP - 1; p >= 0; --p)
+#pragma unroll 4
+          for (int k = 0; k < kKeys / STEP; ++k)
+            mma(t_o, v + k * (STEP * C::BW / 16), desc_p + (p * C::P_TILE / 16 + k * (STEP * C::RB / 16)), idesc_o,
                 add || k > 0 || p < C::PP - 1);
         tc::umma_commit(&p_empty);
         tc::umma_commit(&v_empty[i % NST]);
         return true;
       };
+      // chunk i's S goes before chunk i - 1's P V, except that a new item's queries are staged only after
+      // the last one's P V
       int it = 0, seg = 0;
       bool ok = true, add = false;             // add: chunk it - 1 is not its segment's first
       for (int unit = begin; unit < end && ok; ++seg) {
         const Segment s = segment_at(a, s_first, unit, end);
-        for (int ch = s.c0; ch < s.c1; ++ch, ++it) {
-          const bool first = ch == s.c0;
-          // a new item's queries are staged only after the last one's P V
-          if (first && it > 0 && !(ok = pv(it - 1, add))) break;
-          if (first && !(ok = tc::mbar_wait(&q_full, seg & 1, a.status))) break;
-          if (!(ok = tc::mbar_wait(&s_empty[it & 1], parity(it, 2) ^ 1, a.status) &&
-                     tc::mbar_wait(&k_full[it % NST], parity(it, NST), a.status)))
-            break;
-          tc::tc_fence_after();
-          const uint32_t k = sbase + C::KV_OFF + (it % NST) * 2 * C::TILE;
-#pragma unroll
-          for (int p = C::QP - 1; p >= 0; --p)
-#pragma unroll
-            for (int x = 0; x < C::KROW / 32; ++x) {
-              const int nb = x * 32 / C::BW, off = x * 32 % C::BW;
-              mma(tmem + (it & 1) * NQ, tc::desc_rows(k + nb * C::BLOCK + off, C::BW, 16),
-                  tc::desc_rows(sbase + C::Q_OFF + p * C::Q_PLANE + nb * NQ * C::BW + off, C::BW, 16),
-                  idesc_s, p < C::QP - 1 || x > 0);
-            }
-          tc::umma_commit(&s_full[it & 1]);
-          tc::umma_commit(&k_empty[it % NST]);
-          if (!first && !(ok = pv(it - 1, add))) break;
-          add = !first;
+        for (int ch = s.c0; ch <= s.c1; ++ch) {   // (one round more: the last chunk's P V)
+          if (ch < s.c1) {
+            ok = (ch > s.c0 || tc::mbar_wait(&q_full, seg & 1, a.status)) &&
+                 tc::mbar_wait(&s_empty[it & 1], parity(it, 2) ^ 1, a.status) &&
+                 tc::mbar_wait(&k_full[it % NST], parity(it, NST), a.status);
+            if (!ok) break;
+            tc::tc_fence_after();
+            s_mma(it);
+          }
+          if (ch > s.c0 && !(ok = pv(it - 1, add))) break;
+          add = ch > s.c0;
+          if (ch < s.c1) ++it;
         }
         unit += s.c1 - s.c0;
       }
-      if (ok && it > 0) pv(it - 1, add);
       // what was issued completes before the block's memory goes
       tc::umma_commit(&done);
       tc::mbar_wait(&done, 0, a.status);
@@ -293,14 +297,14 @@ __global__ void __launch_bounds__(kThreads, Cfg<HD, NQ, F8>::CTAS)
       // ---- queries: eight threads a vector, HD / 8 values each
       sync();                                  // the item before is done with the statistics
       constexpr int QE = HD / 8;
-#pragma unroll
+#pragma unroll 1
       for (int v0 = 0; v0 < NQ; v0 += kSoft / 8) {
         const int v = v0 + r / 8, part = r % 8;
+        const Vec x = vector_of(a, s.h, s.qb, v);
         uint32_t w[QE / 2];
 #pragma unroll
         for (int i = 0; i < QE / 2; ++i) w[i] = 0u;
         if (v < s.nq) {
-          const Vec x = vector_of(a, s.h, s.qb, v);
           const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(a.q) + s.b * a.sq[0] + x.t * a.sq[1] +
                                    x.h * a.sq[2] + part * QE;
           if (q_aligned) {
@@ -362,16 +366,17 @@ __global__ void __launch_bounds__(kThreads, Cfg<HD, NQ, F8>::CTAS)
           }
         }
         if (part == 0) {
-          // a query that is not finite sees NaN scores
-          s_qs[v] = v < s.nq ? (bad ? __uint_as_float(0x7fc00000u) : qs) : 0.f;
+          s_qs[v] = v < s.nq ? qs : 0.f;
           s_ref[v] = s_lim[v] = -INFINITY;
           s_mq[v] = 0.f;
+          s_bad[v] = v < s.nq && bad;
+          s_out[v] = s.b * a.so[0] + x.t * a.so[1] + x.h * a.so[2];
         }
       }
-      for (int i = r; i < NQ * kWords; i += kSoft) {
-        const int v = i / kWords, w = i % kWords;
-        s_mask[v][w] = v < s.nq && w < a.W
-                           ? __ldg(a.mask + ((size_t)s.b * a.T + vector_of(a, s.h, s.qb, v).t) * a.W + w) : 0u;
+      const int t0 = s.qb * NQ / a.G;          // the block's first node
+      for (int i = r; i < (NQ + 1) * kWords; i += kSoft) {
+        const int t = t0 + i / kWords, w = i % kWords;
+        s_mask[i / kWords][w] = t < s.nodes && w < a.W ? __ldg(a.mask + ((size_t)s.b * a.T + t) * a.W + w) : 0u;
       }
       if (r == 0) s_vref = F8 ? -1 : 127;
       tc::fence_proxy_async();
@@ -390,42 +395,48 @@ __global__ void __launch_bounds__(kThreads, Cfg<HD, NQ, F8>::CTAS)
         const int node = ch * kKeys + r - s.len;
         if (!valid && ch * kKeys + r < s.keys) set_status(a.status, CDSL_ERANGE);
         const float ks = scale_value(cur.ks);
-        // any slot here that is not seen by all? (a warp's branch)
-        const bool masked = __any_sync(0xffffffffu, !valid || node >= 0);
-        auto seen = [&](int v) {
-          return valid && (node < 0 || (s_mask[v][node >> 5] >> (node & 31) & 1));
-        };
         if (!__all_sync(0xffffffffu, tc::mbar_wait(&s_full[it & 1], parity(it, 2), a.status))) failed = true;
         tc::tc_fence_after();
-        // ---- scores and their maxima over the warp's slots: lane v % 32 has column v's
+        // which vectors see this slot: bit v. Only chunks with slots of the tree or past the item's ask
+        // (a warp's branch).
+        const bool masked = __any_sync(0xffffffffu, !valid || node >= 0);
+        uint64_t vis = ~0ull;
+        if (masked && (!valid || node >= 0)) {
+          vis = 0;
+          const uint64_t group = a.G < 64 ? (1ull << a.G) - 1 : ~0ull;
+          if (valid)
+#pragma unroll 4
+            for (int t = t0, v = t0 * a.G - s.qb * NQ; v < s.nq; ++t, v += a.G)
+              if (s_mask[t - t0][node >> 5] >> (node & 31) & 1) vis |= v < 0 ? group >> -v : group << v;
+        }
+        // ---- scores; does any pass its column's limit?
         constexpr bool kKeep = NQ <= 32;       // scores stay in registers
-        float t[kKeep ? NQ : 16], wm[(NQ + 31) / 32];
-#pragma unroll
-        for (int v = 0; v < (NQ + 31) / 32; ++v) wm[v] = -INFINITY;
+        float t[kKeep ? NQ : 16];
         auto scores = [&](int g, float (&x)[16]) {
           tc::tmem_ld16(t_s + g, x);
 #pragma unroll
           for (int e = 0; e < 16; ++e) x[e] *= ks;
           if (masked) {
+            const uint32_t bits = (uint32_t)(vis >> g);
 #pragma unroll
             for (int e = 0; e < 16; ++e)
-              if (!seen(g + e)) x[e] = -INFINITY;
+              if (!(bits >> e & 1)) x[e] = -INFINITY;
           }
         };
+        bool raise = F8 && valid && cur.vs != 255 && (int)cur.vs > s_vref;
 #pragma unroll
         for (int g = 0; g < NQ; g += 16) {
           float x[16];
           scores(g, x);
 #pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const float top = warp_fmax(x[e]);
-            if (lane == ((g + e) & 31)) wm[(g + e) / 32] = top;
-            if (kKeep) t[(kKeep ? g : 0) + e] = x[e];
+          for (int e = 0; e < 16; e += 4) {
+            const float4 lim = *reinterpret_cast<const float4*>(&s_lim[g + e]);
+            raise = raise || x[e] > lim.x || x[e + 1] > lim.y || x[e + 2] > lim.z || x[e + 3] > lim.w;
           }
-        }
-        bool raise = F8 && valid && cur.vs != 255 && (int)cur.vs > s_vref;
 #pragma unroll
-        for (int v = lane; v < NQ; v += 32) raise = raise || wm[v / 32] > s_lim[v];
+          for (int e = 0; e < 16; ++e)
+            if (kKeep) t[(kKeep ? g : 0) + e] = x[e];
+        }
         bool waited = false;                   // for the chunk before's P V
         auto wait_pv = [&] {
           if (it > 0 && !waited &&
@@ -439,8 +450,17 @@ __global__ void __launch_bounds__(kThreads, Cfg<HD, NQ, F8>::CTAS)
             break;
           }
           // ---- raise every reference to its column's maximum so far
+#pragma unroll 1
+          for (int g = 0; g < NQ; g += 16) {
+            float x[16], wm = 0.f;
+            scores(g, x);
 #pragma unroll
-          for (int v = lane; v < NQ; v += 32) s_wmax[warp][v] = wm[v / 32];
+            for (int e = 0; e < 16; ++e) {
+              const float top = warp_fmax(x[e]);
+              if (lane == e) wm = top;
+            }
+            if (lane < 16) s_wmax[warp][g + lane] = wm;
+          }
           const int wv = __reduce_max_sync(0xffffffffu, valid && cur.vs != 255 ? (int)cur.vs : -1);
           if (lane == 0) s_wv[warp] = wv;
           sync();
@@ -498,19 +518,14 @@ __global__ void __launch_bounds__(kThreads, Cfg<HD, NQ, F8>::CTAS)
             x[e + 2] = ex2(fmaf(x[e + 2], qs.z, -mq.z));
             x[e + 3] = ex2(fmaf(x[e + 3], qs.w, -mq.w));
           }
-          if (masked) {                        // (0 * qs of a vector past the block's is no score)
-#pragma unroll
-            for (int e = 0; e < 16; ++e)
-              if (!seen(g + e)) x[e] = 0.f;
-          }
 #pragma unroll
           for (int e = 0; e < 16; ++e) l[g + e] += x[e];
-          if (masked) {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) x[e] = seen(g + e) ? x[e] * vf : 0.f;
-          } else {
+          for (int e = 0; e < 16; ++e) x[e] *= vf;
+          if (__any_sync(0xffffffffu, cur.vs == 255)) {   // a V that is not finite: NaN where it is seen
 #pragma unroll
-            for (int e = 0; e < 16; ++e) x[e] *= vf;
+            for (int e = 0; e < 16; ++e)
+              if (cur.vs == 255) x[e] = (uint32_t)(vis >> (g + e)) & 1 ? vf : 0.f;
           }
           uint8_t* const p = sm + C::P_OFF;
           if constexpr (F8) {
@@ -581,14 +596,30 @@ __global__ void __launch_bounds__(kThreads, Cfg<HD, NQ, F8>::CTAS)
         if ((lane & 1) == 0) s_l[warp][g + (lane >> 1)] = x[0];
       }
       sync();
+      // ---- a thread per vector: its sum (0: it saw nothing; of a query that is not finite: NaN)
       const bool whole = s.c0 == 0 && s.c1 == s.units;
       const size_t slot = (size_t)blockIdx.x * 2 + (s.c0 == 0);
       const int live = min(NQ, a.T * a.G - s.qb * NQ);
+      for (int v = r; v < live; v += kSoft) {
+        float sum = 0.f;
+        if (v < s.nq && s.keys > 0) sum = s_l[0][v] + s_l[1][v] + s_l[2][v] + s_l[3][v];
+        const float m = sum == 0.f ? -INFINITY : s_mq[v];
+        if (sum != 0.f && s_bad[v]) sum = __uint_as_float(0x7fc00000u);
+        if (whole) {
+          s_inv[v] = sum == 0.f ? 0.f : 1.f / sum;
+          store_lse(a, s.b, vector_of(a, s.h, s.qb, v), m, sum);
+        } else {
+          s_inv[v] = sum == 0.f ? 0.f : 1.f;
+          a.part_ml[(slot * 2) * NQ + v] = m;
+          a.part_ml[(slot * 2 + 1) * NQ + v] = sum;
+        }
+      }
+      sync();
       // O^T holds sums of p * 2^(V's scale - s_vref + kPShift)
       const float unscale = F8 ? ex2((float)(s_vref - 127)) : 1.f;
-      if (r < (HD + 31) / 32 * 32) {           // whole warps
+      if (r < HD) {                            // (whole warps)
 #pragma unroll 1
-        for (int g = 0; g < NQ; g += 16) {
+        for (int g = 0; g < live; g += 16) {
           float o[16];
           tc::tmem_ld16(t_o + lane_base + g, o);
           if constexpr (F8) {
@@ -599,22 +630,10 @@ __global__ void __launch_bounds__(kThreads, Cfg<HD, NQ, F8>::CTAS)
           }
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
-            const int v = g + e;
-            if (v >= live) break;
-            const bool has = v < s.nq && s.keys > 0;
-            const float sum = has ? s_l[0][v] + s_l[1][v] + s_l[2][v] + s_l[3][v] : 0.f;
-            const bool any = !(sum == 0.f);
-            if (whole) {
-              const Vec x = vector_of(a, s.h, s.qb, v);
-              store_out<__nv_bfloat16>(a, s.b, x, r, any ? o[e] / sum : 0.f);
-              if (r == 0) store_lse(a, s.b, x, s_mq[v], sum);
-            } else {
-              a.part_o[(slot * NQ + v) * HD + r] = any ? o[e] : 0.f;
-              if (r == 0) {
-                a.part_ml[(slot * 2) * NQ + v] = any ? s_mq[v] : -INFINITY;
-                a.part_ml[(slot * 2 + 1) * NQ + v] = sum;
-              }
-            }
+            if (g + e >= live) break;
+            const float inv = s_inv[g + e], x = inv == 0.f ? 0.f : o[e] * inv;
+            if (whole) static_cast<__nv_bfloat16*>(a.out)[s_out[g + e] + r] = __float2bfloat16_rn(x);
+            else a.part_o[(slot * NQ + g + e) * HD + r] = x;
           }
         }
       }
