@@ -4,7 +4,7 @@
 // N (16, 32 or 64: a tree has few of them, and as M they would be padded to 128), so that the work
 // follows the number of queries:
 //   S^T = K Q^T   M = 128 slots, N = NQ vectors, K = head_dim      K tile K-major, as TMA lands it
-//   O^T += V^T P^T  M = head_dim, N = NQ (x planes), K = 128 slots   V tile MN-major, as TMA lands it
+//   O^T = V^T P^T  M = head_dim, N = NQ (x planes), K = 128 slots   V tile MN-major, as TMA lands it
 // An e4m3 cache takes kind::f8f6f4, twice the rate and half the shared memory of bf16 and no
 // conversion of K and V at all. What is not e4m3 is split into e4m3 planes instead: a query row, scaled
 // by a power of two to at most 448, is hi + lo, each to 4 bits, together bf16's 8 (to 2^-18 of the row's
@@ -13,12 +13,17 @@
 // The rows' power-of-two scales never touch the codes: K's multiplies the thread's scores, V's the
 // thread's probabilities (relative to the largest V scale so far, so that they use e4m3's range).
 //
-// Six warps. Warp 4 loads K and V chunks by TMA into a ring, a box per page piece; warp 5 issues
-// the MMAs, the next chunk's S while this one's softmax runs (S has two buffers in TMEM). Warps 0-3 do the
-// softmax: a thread owns a slot (a TMEM lane) and walks the query vectors (columns). Column maxima
-// come from redux.sync over a warp; the running reference is raised only when some column's maximum passes
-// it by more than kMargin (p <= 6.7: e4m3's 448 holds 64 p), which after the first chunk is rare, so a
-// chunk costs one barrier among the four warps. Each thread keeps its own slots' share of the sums l.
+// Every chunk's P is relative to that chunk's own column maxima and largest V scale, and its O^T starts
+// anew in TMEM and is added to fp32 sums in registers with the factor that this takes, so that small
+// probabilities keep their bits beside one large one chunks away, and no sum is a chain of the tensor
+// core's truncating additions. The sums' own reference is raised only when a maximum passes it by
+// more than 2^kMargin.
+//
+// Warps: one loads the chunks by TMA into a ring (a box per page piece, the scale bytes with V), one issues
+// the MMAs, the next chunk's S while this one's softmax runs (S has two buffers in TMEM), and four, or
+// eight at NQ = 64 (half of the columns each), do the softmax: a thread owns a slot (a TMEM lane) of the chunk and
+// walks the query vectors (columns), and later one dimension of O^T. Column maxima come from redux.sync over
+// a warp and shared memory over the warps. Each thread keeps its own slots' share of the sums l.
 //
 // Waits are bounded (tc::kWaitLimitNs): on expiry CDSL_ETIMEOUT is latched, the role winds down and
 // the block frees its TMEM and exits.
@@ -34,16 +39,16 @@ namespace cdsl {
 namespace tree {
 namespace {
 
-constexpr int kSoft = 128;                     // softmax threads: one per slot of a chunk
-constexpr int kThreads = kSoft + 64;
-constexpr int kProducer = 4, kIssuer = 5;      // warps
-constexpr float kMargin = 2.75f;               // base 2: 2^2.75 * 64 < 448
-constexpr int kPShift = 6;                     // probabilities are stored times 2^kPShift
-constexpr float kLoScale = 32.f;               // of the second e4m3 plane
+constexpr float kMargin = 8.f;                 // base 2
+constexpr int kPShift = 8;                     // e4m3 probabilities are stored times 2^kPShift <= 448
+constexpr float kLoScale = 32.f;               // of their second plane
 
 template <int HD, int NQ, bool F8>
 struct Cfg {
   static constexpr int EB = F8 ? 1 : 2;
+  static constexpr int CQ = NQ < 32 ? NQ : 32;             // columns of a softmax thread
+  static constexpr int SOFT = kKeys * (NQ / CQ);           // softmax threads
+  static constexpr int THREADS = SOFT + 64;                // and warps SOFT / 32 (loads), SOFT / 32 + 1 (MMAs)
   static constexpr int KROW = HD * EB;                     // bytes of a K or V row
   static constexpr int BW = KROW < 128 ? KROW : 128;       // of it per tile block
   static constexpr int NB = KROW / BW;                     // blocks
@@ -55,16 +60,17 @@ struct Cfg {
   static constexpr int PP = F8 ? 1 : 2;                    // P tiles
   static constexpr uint32_t P_TILE = kKeys * RB;
   static constexpr uint32_t FIXED = QP * Q_PLANE + PP * P_TILE;
-  // two blocks per SM where two stages fit, else one
-  static constexpr uint32_t LIMIT2 = 110 * 1024, LIMIT1 = 220 * 1024;
-  static constexpr int CTAS = FIXED + 4 * TILE <= LIMIT2 ? 2 : 1;
+  // two blocks per SM where two stages and the registers of one group of softmax warps fit, else one
+  static constexpr uint32_t LIMIT2 = 109 * 1024, LIMIT1 = 216 * 1024;
+  static constexpr int CTAS = SOFT == kKeys && FIXED + 4 * TILE <= LIMIT2 ? 2 : 1;
   static constexpr int FIT = ((CTAS == 2 ? LIMIT2 : LIMIT1) - FIXED) / (2 * TILE);
   static constexpr int NST = FIT > 4 ? 4 : FIT;            // ring stages of K and V
   static_assert(NST >= 2, "stages");
   static constexpr uint32_t Q_OFF = 0;
   static constexpr uint32_t P_OFF = Q_OFF + QP * Q_PLANE;
   static constexpr uint32_t KV_OFF = (P_OFF + PP * P_TILE + 1023) / 1024 * 1024;
-  static constexpr uint32_t PLAN_OFF = KV_OFF + NST * 2 * TILE;
+  static constexpr uint32_t SCALE_OFF = KV_OFF + NST * 2 * TILE;   // a byte per slot, K and V
+  static constexpr uint32_t PLAN_OFF = SCALE_OFF + NST * 2 * kKeys;
   static constexpr int OC = F8 ? 2 * NQ : NQ;              // TMEM columns of O^T
   static constexpr uint32_t TMEM = 4 * NQ;                 // S twice, O
   static constexpr size_t smem(int batch) { return 1024 + PLAN_OFF + (batch + 1) * 4; }
@@ -95,24 +101,25 @@ __device__ __forceinline__ __half2 f8x2_half(uint32_t two) {
   return *reinterpret_cast<__half2*>(&r);
 }
 template <int HD, int NQ, bool F8>
-__global__ void __launch_bounds__(kThreads, Cfg<HD, NQ, F8>::CTAS)
+__global__ void __launch_bounds__(Cfg<HD, NQ, F8>::THREADS, Cfg<HD, NQ, F8>::CTAS)
     k_tree_tc(TreeArgs a, const __grid_constant__ CUtensorMap map) {
   using C = Cfg<HD, NQ, F8>;
-  constexpr int NST = C::NST;
+  constexpr int NST = C::NST, kSoft = C::SOFT, kProducer = kSoft / 32, kIssuer = kProducer + 1;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* const sm = smem_raw + ((1024 - (tc::smem_u32(smem_raw) & 1023)) & 1023);
   int* const s_first = reinterpret_cast<int*>(sm + C::PLAN_OFF);
   __shared__ __align__(8) uint64_t k_full[NST], v_full[NST], k_empty[NST], v_empty[NST];
   __shared__ __align__(8) uint64_t s_full[2], s_empty[2], p_full, p_empty, q_full, done;
   __shared__ uint32_t s_tmem;
-  // per query vector: score factor (softmax scale and the row's own), reference in raw scores, what raises
-  // it, reference in base 2; factors of a raise
-  __shared__ __align__(16) float s_qs[NQ], s_mq[NQ], s_lim[NQ], s_alpha[NQ], s_beta[NQ], s_inv[NQ];
+  // per query vector: score factor (softmax scale and the row's own), the chunk's maximum in base 2, its
+  // factors to the sums (of l, and of O^T with V's scale: two chunks' in turn), the sums' reference, factor of a raise
+  __shared__ __align__(16) float s_qs[NQ], s_mq[NQ], s_b[NQ], s_bo[2][NQ], s_f[NQ], s_inv[NQ];
   __shared__ float s_ref[NQ], s_wmax[4][NQ], s_l[4][NQ];
   __shared__ int s_bad[NQ];                    // the query is not finite
   __shared__ long long s_out[NQ];              // where its output begins
   __shared__ uint32_t s_mask[NQ + 1][kWords];  // of the block's nodes
-  __shared__ int s_vref, s_wv[4];
+  __shared__ uint32_t s_pieces[NST];           // pieces of a stage's chunk that hold slots, as bits
+  __shared__ int s_wv[4];
   const Cache& c = a.c;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
@@ -144,7 +151,7 @@ __global__ void __launch_bounds__(kThreads, Cfg<HD, NQ, F8>::CTAS)
   const uint32_t sbase = tc::smem_u32(sm);
   if (blockIdx.x == 0) {
     check_lens(a);
-    for (int b = threadIdx.x; b <= c.batch; b += kThreads) a.plan[b] = s_first[b];
+    for (int b = threadIdx.x; b <= c.batch; b += C::THREADS) a.plan[b] = s_first[b];
   }
   const int total = s_first[c.batch], runs = runs_of(a, total);
   const int begin = (int)blockIdx.x < runs ? run_begin(blockIdx.x, total, runs) : 0;
@@ -163,17 +170,27 @@ __global__ void __launch_bounds__(kThreads, Cfg<HD, NQ, F8>::CTAS)
         const int slot = ch * kKeys + lane * rows;
         int page = -1;
         if (lane < pieces && slot < s.keys) page = page_of(c, s.b, slot);
-        const uint32_t bytes = __popc(__ballot_sync(0xffffffffu, page >= 0)) * rows * C::KROW;
+        const uint32_t live = __ballot_sync(0xffffffffu, page >= 0), n = __popc(live) * rows;
+        if (slot < s.keys && lane < pieces && page < 0) set_status(a.status, CDSL_ERANGE);
 #pragma unroll
         for (int kv = 0; kv < 2; ++kv) {
           uint64_t* full = kv ? &v_full[st] : &k_full[st];
           ok = ok && __all_sync(0xffffffffu, tc::mbar_wait(kv ? &v_empty[st] : &k_empty[st],
                                                            parity(it, NST) ^ 1, a.status));
           if (!ok) break;
-          if (lane == 0) tc::mbar_expect_tx(full, bytes);
+          if (lane == 0) {
+            if (kv) s_pieces[st] = live;
+            tc::mbar_expect_tx(full, n * (C::KROW + 2 * kv));
+          }
           __syncwarp();
           if (page >= 0) {
             const int y = (int)row_of(c, 0, page, kv, s.h, slot & (P - 1));
+            if (kv) {                          // with V: both scale bytes
+              const uint8_t* from = c.scale + row_of(c, a.layer, page, 0, s.h, slot & (P - 1));
+              uint8_t* to = sm + C::SCALE_OFF + st * 2 * kKeys + lane * rows;
+              tc::bulk_load(to, from, rows, full);
+              tc::bulk_load(to + kKeys, from + ((size_t)c.kvh << c.page_shift), rows, full);
+            }
             uint8_t* dst = sm + C::KV_OFF + (st * 2 + kv) * C::TILE + lane * rows * C::BW;
 #pragma unroll
             for (int nb = 0; nb < C::NB; ++nb)
@@ -224,7 +241,7 @@ __global__ void __launch_bounds__(kThreads, Cfg<HD, NQ, F8>::CTAS)
         tc::umma_commit(&s_full[i & 1]);
         tc::umma_commit(&k_empty[i % NST]);
       };
-      auto pv = [&](int i, bool add) {         // the P V of chunk i
+      auto pv = [&](int i) {                   // the P V of chunk i
         if (!tc::mbar_wait(&p_full, i & 1, a.status) ||
             !tc::mbar_wait(&v_full[i % NST], parity(i, NST), a.status))
           return false;
@@ -235,7 +252,7 @@ __global__ void __launch_bounds__(kThreads, Cfg<HD, NQ, F8>::CTAS)
 #pragma unroll 4
           for (int k = 0; k < kKeys / STEP; ++k)
             mma(t_o, v + k * (STEP * C::BW / 16), desc_p + (p * C::P_TILE / 16 + k * (STEP * C::RB / 16)), idesc_o,
-                add || k > 0 || p < C::PP - 1);
+                k > 0 || p < C::PP - 1);
         tc::umma_commit(&p_empty);
         tc::umma_commit(&v_empty[i % NST]);
         return true;
@@ -243,7 +260,7 @@ __global__ void __launch_bounds__(kThreads, Cfg<HD, NQ, F8>::CTAS)
       // chunk i's S goes before chunk i - 1's P V, except that a new item's queries are staged only after
       // the last one's P V
       int it = 0, seg = 0;
-      bool ok = true, add = false;             // add: chunk it - 1 is not its segment's first
+      bool ok = true;
       for (int unit = begin; unit < end && ok; ++seg) {
         const Segment s = segment_at(a, s_first, unit, end);
         for (int ch = s.c0; ch <= s.c1; ++ch) {   // (one round more: the last chunk's P V)
@@ -255,8 +272,7 @@ __global__ void __launch_bounds__(kThreads, Cfg<HD, NQ, F8>::CTAS)
             tc::tc_fence_after();
             s_mma(it);
           }
-          if (ch > s.c0 && !(ok = pv(it - 1, add))) break;
-          add = ch > s.c0;
+          if (ch > s.c0 && !(ok = pv(it - 1))) break;
           if (ch < s.c1) ++it;
         }
         unit += s.c1 - s.c0;
@@ -268,38 +284,23 @@ __global__ void __launch_bounds__(kThreads, Cfg<HD, NQ, F8>::CTAS)
     __syncwarp();
   } else {
     // ------------------------------------------------------------------------- softmax
-    const int r = threadIdx.x;                 // slot of the chunk = TMEM lane; dimension of O^T
-    const uint32_t lane_base = (uint32_t)(warp * 32) << 16;
+    constexpr int CQ = C::CQ;
+    const int tid = threadIdx.x;
+    const int r = tid % kKeys;                 // slot of the chunk = TMEM lane; dimension of O^T
+    const int c0 = tid / kKeys * CQ;           // this group's columns: c0 .. c0 + CQ - 1
+    const int w4 = warp & 3;
+    const uint32_t lane_base = (uint32_t)(w4 * 32) << 16;
     auto sync = [] { tc::named_barrier(1, kSoft); };
     const bool q_aligned = (reinterpret_cast<uintptr_t>(a.q) | (a.sq[0] | a.sq[1] | a.sq[2]) * 2) % 16 == 0;
     int it = 0;
     bool failed = false, gone = false;
     for (int unit = begin; unit < end && !gone;) {
       const Segment s = segment_at(a, s_first, unit, end);
-      // ---- scale bytes of the slots, loaded a chunk ahead and their page ids two
-      auto page_at = [&](int ch) {
-        const int slot = ch * kKeys + r;
-        return ch < s.c1 && slot < s.keys ? page_of(c, s.b, slot) : -1;
-      };
-      struct Slot { int page; uint32_t ks, vs; };   // page -1: nothing to see
-      auto slot_at = [&](int ch, int page) {
-        Slot x = {page, 127, 127};
-        if (page >= 0) {
-          const size_t row = row_of(c, a.layer, page, 0, s.h, (ch * kKeys + r) & (P - 1));
-          x.ks = __ldg(c.scale + row);
-          x.vs = __ldg(c.scale + row + ((size_t)c.kvh << c.page_shift));
-        }
-        return x;
-      };
-      const int page0 = page_at(s.c0);
-      int page_next = page_at(s.c0 + 1);
-      Slot cur = slot_at(s.c0, page0);
       // ---- queries: eight threads a vector, HD / 8 values each
-      sync();                                  // the item before is done with the statistics
       constexpr int QE = HD / 8;
 #pragma unroll 1
       for (int v0 = 0; v0 < NQ; v0 += kSoft / 8) {
-        const int v = v0 + r / 8, part = r % 8;
+        const int v = v0 + tid / 8, part = tid % 8;
         const Vec x = vector_of(a, s.h, s.qb, v);
         uint32_t w[QE / 2];
 #pragma unroll
@@ -334,15 +335,15 @@ __global__ void __launch_bounds__(kThreads, Cfg<HD, NQ, F8>::CTAS)
           uint32_t hi[QE / 4], lo[QE / 4];
 #pragma unroll
           for (int i = 0; i < QE / 4; ++i) {
-            float x[4] = {__uint_as_float(w[2 * i] << 16), __uint_as_float(w[2 * i] & 0xffff0000u),
-                          __uint_as_float(w[2 * i + 1] << 16), __uint_as_float(w[2 * i + 1] & 0xffff0000u)};
+            const float y[4] = {__uint_as_float(w[2 * i] << 16), __uint_as_float(w[2 * i] & 0xffff0000u),
+                                __uint_as_float(w[2 * i + 1] << 16), __uint_as_float(w[2 * i + 1] & 0xffff0000u)};
             uint32_t hl[2], ll[2];
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-              const float2 y = make_float2(x[2 * j] * inv, x[2 * j + 1] * inv);
-              hl[j] = __nv_cvt_float2_to_fp8x2(y, __NV_SATFINITE, __NV_E4M3);
+              const float2 u = make_float2(y[2 * j] * inv, y[2 * j + 1] * inv);
+              hl[j] = __nv_cvt_float2_to_fp8x2(u, __NV_SATFINITE, __NV_E4M3);
               const float2 z = f8x2_to_f32(hl[j]);
-              ll[j] = __nv_cvt_float2_to_fp8x2(make_float2(y.x - z.x, y.y - z.y), __NV_SATFINITE, __NV_E4M3);
+              ll[j] = __nv_cvt_float2_to_fp8x2(make_float2(u.x - z.x, u.y - z.y), __NV_SATFINITE, __NV_E4M3);
             }
             hi[i] = bad ? 0u : hl[0] | hl[1] << 16;
             lo[i] = bad ? 0u : ll[0] | ll[1] << 16;
@@ -367,167 +368,173 @@ __global__ void __launch_bounds__(kThreads, Cfg<HD, NQ, F8>::CTAS)
         }
         if (part == 0) {
           s_qs[v] = v < s.nq ? qs : 0.f;
-          s_ref[v] = s_lim[v] = -INFINITY;
-          s_mq[v] = 0.f;
+          s_ref[v] = -INFINITY;
           s_bad[v] = v < s.nq && bad;
           s_out[v] = s.b * a.so[0] + x.t * a.so[1] + x.h * a.so[2];
         }
       }
       const int t0 = s.qb * NQ / a.G;          // the block's first node
-      for (int i = r; i < (NQ + 1) * kWords; i += kSoft) {
+      for (int i = tid; i < (NQ + 1) * kWords; i += kSoft) {
         const int t = t0 + i / kWords, w = i % kWords;
         s_mask[i / kWords][w] = t < s.nodes && w < a.W ? __ldg(a.mask + ((size_t)s.b * a.T + t) * a.W + w) : 0u;
       }
-      if (r == 0) s_vref = F8 ? -1 : 127;
       tc::fence_proxy_async();
       tc::mbar_arrive(&q_full);
       sync();
-      float l[NQ];
+      float l[CQ], o[CQ];
 #pragma unroll
-      for (int v = 0; v < NQ; ++v) l[v] = 0.f;
+      for (int v = 0; v < CQ; ++v) l[v] = o[v] = 0.f;
+      // a chunk's O^T (its P V complete) to the sums, with its factors
+      auto add_o = [&](int i) {
+        tc::tc_fence_after();
+        if (r < HD) {                          // (whole warps)
+#pragma unroll
+          for (int g = 0; g < CQ; g += 16) {
+            if (c0 + g >= s.nq) break;
+            uint32_t x[16], y[16];
+            tc::tmem_ld16_nowait(t_o + lane_base + c0 + g, x);
+            if constexpr (F8) tc::tmem_ld16_nowait(t_o + lane_base + NQ + c0 + g, y);
+            tc::tmem_wait_ld();
+#pragma unroll
+            for (int e = 0; e < 16; e += 4) {
+              const float4 b = *reinterpret_cast<const float4*>(&s_bo[i & 1][c0 + g + e]);
+              const float f[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                float z = __uint_as_float(x[e + j]);
+                if constexpr (F8) z = fmaf(__uint_as_float(y[e + j]), 1.f / kLoScale, z);
+                o[g + e + j] = fmaf(z, f[j], o[g + e + j]);
+              }
+            }
+          }
+        }
+        tc::tc_fence_before();
+      };
 
       for (int ch = s.c0; ch < s.c1; ++ch, ++it) {
         const bool first = ch == s.c0;
-        const uint32_t t_s = tmem + (it & 1) * NQ + lane_base;
-        const Slot ahead = slot_at(ch + 1, page_next);
-        page_next = page_at(ch + 2);
-        const bool valid = cur.page >= 0;
-        const int node = ch * kKeys + r - s.len;
-        if (!valid && ch * kKeys + r < s.keys) set_status(a.status, CDSL_ERANGE);
-        const float ks = scale_value(cur.ks);
-        if (!__all_sync(0xffffffffu, tc::mbar_wait(&s_full[it & 1], parity(it, 2), a.status))) failed = true;
-        tc::tc_fence_after();
-        // which vectors see this slot: bit v. Only chunks with slots of the tree or past the item's ask
-        // (a warp's branch).
+        const int st = it % NST;
+        // ---- this thread's slot: the scales, and which vectors see it (bit v of vis). Only chunks with slots
+        //      of the tree or past the item's ask (a warp's branch).
+        bool ok = tc::mbar_wait(&v_full[st], parity(it, NST), a.status);
+        const int slot = ch * kKeys + r, node = slot - s.len;
+        const bool valid = slot < s.keys && s_pieces[st] >> (r >> min(c.page_shift, 7)) & 1;
+        const uint32_t kb = valid ? sm[C::SCALE_OFF + st * 2 * kKeys + r] : 127u;
+        const uint32_t vb = valid ? sm[C::SCALE_OFF + (st * 2 + 1) * kKeys + r] : 0u;
+        const float ks = scale_value(kb);
         const bool masked = __any_sync(0xffffffffu, !valid || node >= 0);
-        uint64_t vis = ~0ull;
+        uint32_t vis = ~0u;
         if (masked && (!valid || node >= 0)) {
           vis = 0;
-          const uint64_t group = a.G < 64 ? (1ull << a.G) - 1 : ~0ull;
-          if (valid)
-#pragma unroll 4
-            for (int t = t0, v = t0 * a.G - s.qb * NQ; v < s.nq; ++t, v += a.G)
-              if (s_mask[t - t0][node >> 5] >> (node & 31) & 1) vis |= v < 0 ? group >> -v : group << v;
+          if (valid) {
+            const uint64_t group = a.G < 64 ? (1ull << a.G) - 1 : ~0ull;
+            const int first_t = (s.qb * NQ + c0) / a.G;
+#pragma unroll 2
+            for (int t = first_t, v = t * a.G - s.qb * NQ - c0; v < min(CQ, s.nq - c0); ++t, v += a.G)
+              if (s_mask[t - t0][node >> 5] >> (node & 31) & 1)
+                vis |= (uint32_t)(v < 0 ? group >> -v : group << v);
+          }
         }
-        // ---- scores; does any pass its column's limit?
-        constexpr bool kKeep = NQ <= 32;       // scores stay in registers
-        float t[kKeep ? NQ : 16];
-        auto scores = [&](int g, float (&x)[16]) {
-          tc::tmem_ld16(t_s + g, x);
+        // ---- scores, and their maxima over the warp's slots: lane v has column c0 + v's
+        ok = ok && tc::mbar_wait(&s_full[it & 1], parity(it, 2), a.status);
+        if (!__all_sync(0xffffffffu, ok)) failed = true;
+        tc::tc_fence_after();
+        float t[CQ], wm = -INFINITY;
 #pragma unroll
-          for (int e = 0; e < 16; ++e) x[e] *= ks;
+        for (int g = 0; g < CQ; g += 16) {
+          if (c0 + g >= s.nq) break;
+          uint32_t x[16];
+          tc::tmem_ld16_nowait(tmem + (it & 1) * NQ + lane_base + c0 + g, x);
+          tc::tmem_wait_ld();
+#pragma unroll
+          for (int e = 0; e < 16; ++e) t[g + e] = __uint_as_float(x[e]) * ks;
           if (masked) {
-            const uint32_t bits = (uint32_t)(vis >> g);
 #pragma unroll
             for (int e = 0; e < 16; ++e)
-              if (!(bits >> e & 1)) x[e] = -INFINITY;
+              if (!(vis >> (g + e) & 1)) t[g + e] = -INFINITY;
           }
-        };
-        bool raise = F8 && valid && cur.vs != 255 && (int)cur.vs > s_vref;
 #pragma unroll
-        for (int g = 0; g < NQ; g += 16) {
+          for (int e = 0; e < 16; ++e) {
+            const float top = warp_fmax(t[g + e]);
+            if (lane == g + e) wm = top;
+          }
+        }
+        tc::tc_fence_before();
+        tc::mbar_arrive(&s_empty[it & 1]);
+        if (lane < CQ) s_wmax[w4][c0 + lane] = wm;
+        if (F8 && c0 == 0) {
+          const int wv = __reduce_max_sync(0xffffffffu, vb == 255 ? 0 : (int)vb);
+          if (lane == 0) s_wv[w4] = wv;
+        }
+        if (tc::named_barrier_or(1, kSoft, failed)) {
+          gone = true;
+          break;
+        }
+        // ---- the chunk's references: a thread per vector
+        const int vref = F8 ? max(max(s_wv[0], s_wv[1]), max(s_wv[2], s_wv[3])) : 127;
+        bool raise = false;
+        if (tid < NQ) {
+          const int v = tid;
+          const float top = fmaxf(fmaxf(s_wmax[0][v], s_wmax[1][v]), fmaxf(s_wmax[2][v], s_wmax[3][v]));
+          const float mq = top == -INFINITY ? 0.f : top * s_qs[v];
+          float ref = s_ref[v], f = 1.f;
+          if (top > -INFINITY && !(mq - ref <= kMargin)) {
+            raise = ref > -INFINITY;
+            f = raise ? ex2(ref - mq) : 1.f;   // (no reference: nothing seen so far, the sums are 0)
+            s_ref[v] = ref = mq;
+          }
+          const float b = top == -INFINITY ? 0.f : ex2(mq - ref);
+          s_mq[v] = mq;
+          s_b[v] = b;
+          s_f[v] = f;
+          s_bo[it & 1][v] = F8 ? b * (1.f / (1 << kPShift)) * ex2((float)(vref - 127)) : b;
+        }
+        raise = tc::named_barrier_or(1, kSoft, raise);
+        // ---- the chunk before's O^T; its P may be overwritten
+        if (it > 0) {
+          if (!__all_sync(0xffffffffu, tc::mbar_wait(&p_empty, (it - 1) & 1, a.status))) failed = true;
+          else if (!first) add_o(it - 1);
+        }
+        if (raise) {
+#pragma unroll
+          for (int v = 0; v < CQ; ++v) {
+            const float f = s_f[c0 + v];
+            l[v] *= f;
+            o[v] *= f;
+          }
+        }
+        // ---- probabilities, their sums, V's scale on them
+        const int ve = F8 ? (int)vb - vref + kPShift : 0;
+        const float vf = !valid ? 0.f : ve < -126 ? 0.f : __uint_as_float((uint32_t)(ve + 127) << 23);
+        const bool bad_v = __any_sync(0xffffffffu, vb == 255);
+        uint8_t* const p = sm + C::P_OFF;
+#pragma unroll
+        for (int g = 0; g < CQ; g += 16) {
+          if (c0 + g >= s.nq) break;
           float x[16];
-          scores(g, x);
 #pragma unroll
           for (int e = 0; e < 16; e += 4) {
-            const float4 lim = *reinterpret_cast<const float4*>(&s_lim[g + e]);
-            raise = raise || x[e] > lim.x || x[e + 1] > lim.y || x[e + 2] > lim.z || x[e + 3] > lim.w;
+            const float4 qs = *reinterpret_cast<const float4*>(&s_qs[c0 + g + e]);
+            const float4 mq = *reinterpret_cast<const float4*>(&s_mq[c0 + g + e]);
+            const float4 b = *reinterpret_cast<const float4*>(&s_b[c0 + g + e]);
+            x[e] = ex2(fmaf(t[g + e], qs.x, -mq.x));
+            x[e + 1] = ex2(fmaf(t[g + e + 1], qs.y, -mq.y));
+            x[e + 2] = ex2(fmaf(t[g + e + 2], qs.z, -mq.z));
+            x[e + 3] = ex2(fmaf(t[g + e + 3], qs.w, -mq.w));
+            l[g + e] = fmaf(x[e], b.x, l[g + e]);
+            l[g + e + 1] = fmaf(x[e + 1], b.y, l[g + e + 1]);
+            l[g + e + 2] = fmaf(x[e + 2], b.z, l[g + e + 2]);
+            l[g + e + 3] = fmaf(x[e + 3], b.w, l[g + e + 3]);
           }
+          if constexpr (F8) {
 #pragma unroll
-          for (int e = 0; e < 16; ++e)
-            if (kKeep) t[(kKeep ? g : 0) + e] = x[e];
-        }
-        bool waited = false;                   // for the chunk before's P V
-        auto wait_pv = [&] {
-          if (it > 0 && !waited &&
-              !__all_sync(0xffffffffu, tc::mbar_wait(&p_empty, (it - 1) & 1, a.status)))
-            failed = true;
-          waited = true;
-        };
-        if (tc::named_barrier_or(1, kSoft, raise || failed)) {
-          if (tc::named_barrier_or(1, kSoft, failed)) {
-            gone = true;
-            break;
+            for (int e = 0; e < 16; ++e) x[e] *= vf;
           }
-          // ---- raise every reference to its column's maximum so far
-#pragma unroll 1
-          for (int g = 0; g < NQ; g += 16) {
-            float x[16], wm = 0.f;
-            scores(g, x);
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              const float top = warp_fmax(x[e]);
-              if (lane == e) wm = top;
-            }
-            if (lane < 16) s_wmax[warp][g + lane] = wm;
-          }
-          const int wv = __reduce_max_sync(0xffffffffu, valid && cur.vs != 255 ? (int)cur.vs : -1);
-          if (lane == 0) s_wv[warp] = wv;
-          sync();
-          const int v_old = s_vref;
-          const int v_new = F8 ? max(max(v_old, max(s_wv[0], s_wv[1])), max(s_wv[2], s_wv[3])) : 127;
-          for (int v = r; v < NQ; v += kSoft) {
-            const float old = s_ref[v];
-            const float top = fmaxf(fmaxf(s_wmax[0][v], s_wmax[1][v]), fmaxf(s_wmax[2][v], s_wmax[3][v]));
-            const float now = fmaxf(old, top), qs = s_qs[v];
-            const float alpha = old == -INFINITY ? (now == -INFINITY ? 1.f : 0.f) : ex2((old - now) * qs);
-            s_alpha[v] = alpha;
-            s_beta[v] = alpha * ex2((float)(v_old - v_new));
-            s_ref[v] = now;
-            s_lim[v] = now + kMargin / qs;
-            s_mq[v] = now == -INFINITY ? 0.f : now * qs;
-          }
-          sync();
-          if (r == 0) s_vref = v_new;          // (read again after the next chunk's barrier)
-#pragma unroll
-          for (int v = 0; v < NQ; ++v) l[v] *= s_alpha[v];
-          if (!first) {
-            wait_pv();
-            tc::tc_fence_after();
-#pragma unroll 1
-            for (int g = 0; g < C::OC; g += 16) {
-              float o[16];
-              tc::tmem_ld16(t_o + lane_base + g, o);
-#pragma unroll
-              for (int e = 0; e < 16; ++e) o[e] *= s_beta[(g + e) % NQ];
-              tc::tmem_st16(t_o + lane_base + g, o);
-            }
-          }
-          sync();                              // s_vref, and the factors are read
-        }
-        // ---- probabilities, their sums, and V's scale on them
-        const int ve = F8 ? (int)cur.vs - s_vref + kPShift : 0;
-        const float vf = cur.vs == 255 ? __uint_as_float(0x7fc00000u)
-                                       : ve < -126 ? 0.f : __uint_as_float((uint32_t)(ve + 127) << 23);
-        wait_pv();
-#pragma unroll
-        for (int g = 0; g < NQ; g += 16) {
-          float x[16];
-          if constexpr (kKeep) {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) x[e] = t[g + e];
-          } else {
-            scores(g, x);
-          }
-#pragma unroll
-          for (int e = 0; e < 16; e += 4) {
-            const float4 qs = *reinterpret_cast<const float4*>(&s_qs[g + e]);
-            const float4 mq = *reinterpret_cast<const float4*>(&s_mq[g + e]);
-            x[e] = ex2(fmaf(x[e], qs.x, -mq.x));
-            x[e + 1] = ex2(fmaf(x[e + 1], qs.y, -mq.y));
-            x[e + 2] = ex2(fmaf(x[e + 2], qs.z, -mq.z));
-            x[e + 3] = ex2(fmaf(x[e + 3], qs.w, -mq.w));
-          }
-#pragma unroll
-          for (int e = 0; e < 16; ++e) l[g + e] += x[e];
-#pragma unroll
-          for (int e = 0; e < 16; ++e) x[e] *= vf;
-          if (__any_sync(0xffffffffu, cur.vs == 255)) {   // a V that is not finite: NaN where it is seen
+          if (bad_v) {                         // a V that is not finite: NaN where it is seen
 #pragma unroll
             for (int e = 0; e < 16; ++e)
-              if (cur.vs == 255) x[e] = (uint32_t)(vis >> (g + e)) & 1 ? vf : 0.f;
+              if (vb == 255) x[e] = vis >> (g + e) & 1 ? __uint_as_float(0x7fc00000u) : 0.f;
           }
-          uint8_t* const p = sm + C::P_OFF;
           if constexpr (F8) {
             uint32_t hi[4], lo[4];
 #pragma unroll
@@ -542,8 +549,9 @@ __global__ void __launch_bounds__(kThreads, Cfg<HD, NQ, F8>::CTAS)
                 lo[i] |= f8x2(rest) << (16 * j);
               }
             }
-            *reinterpret_cast<uint4*>(p + tc::row_offset(r, g / 16, C::RB)) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-            *reinterpret_cast<uint4*>(p + tc::row_offset(r, (NQ + g) / 16, C::RB)) =
+            *reinterpret_cast<uint4*>(p + tc::row_offset(r, (c0 + g) / 16, C::RB)) =
+                make_uint4(hi[0], hi[1], hi[2], hi[3]);
+            *reinterpret_cast<uint4*>(p + tc::row_offset(r, (NQ + c0 + g) / 16, C::RB)) =
                 make_uint4(lo[0], lo[1], lo[2], lo[3]);
           } else {
 #pragma unroll
@@ -557,15 +565,13 @@ __global__ void __launch_bounds__(kThreads, Cfg<HD, NQ, F8>::CTAS)
                 hi[i] = *reinterpret_cast<const uint32_t*>(&h);
                 lo[i] = *reinterpret_cast<const uint32_t*>(&z);
               }
-              const uint32_t off = tc::row_offset(r, g / 8 + half, C::RB);
+              const uint32_t off = tc::row_offset(r, (c0 + g) / 8 + half, C::RB);
               *reinterpret_cast<uint4*>(p + off) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
               *reinterpret_cast<uint4*>(p + C::P_TILE + off) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
             }
           }
         }
-        if (!valid) {                          // nothing of its V row (page garbage, no copy) may reach the sums
-          const int st = it % NST;
-          if (!tc::mbar_wait(&v_full[st], parity(it, NST), a.status)) failed = true;
+        if (!valid && c0 == 0) {               // nothing of its V row (page garbage, no copy) may reach the sums
           uint8_t* v = sm + C::KV_OFF + (st * 2 + 1) * C::TILE + r * C::BW;
 #pragma unroll
           for (int nb = 0; nb < C::NB; ++nb)
@@ -575,69 +581,55 @@ __global__ void __launch_bounds__(kThreads, Cfg<HD, NQ, F8>::CTAS)
         }
         tc::fence_proxy_async();
         tc::tc_fence_before();
-        tc::mbar_arrive(&s_empty[it & 1]);
         tc::mbar_arrive(&p_full);
-        cur = ahead;
       }
       if (gone) break;
-      // ---- the item's (or its part's) sums and output
+      // ---- the last chunk's O^T, and the item's (or its part's) sums
       if (!__all_sync(0xffffffffu, tc::mbar_wait(&p_empty, (it - 1) & 1, a.status))) failed = true;
       if (tc::named_barrier_or(1, kSoft, failed)) {
         gone = true;
         break;
       }
-      tc::tc_fence_after();
+      add_o(it - 1);
 #pragma unroll
-      for (int g = 0; g < NQ; g += 16) {
+      for (int g = 0; g < CQ; g += 16) {
         float x[16];
 #pragma unroll
         for (int e = 0; e < 16; ++e) x[e] = l[g + e];
         warp_sums<16>(x);
-        if ((lane & 1) == 0) s_l[warp][g + (lane >> 1)] = x[0];
+        if ((lane & 1) == 0) s_l[w4][c0 + g + (lane >> 1)] = x[0];
       }
       sync();
       // ---- a thread per vector: its sum (0: it saw nothing; of a query that is not finite: NaN)
       const bool whole = s.c0 == 0 && s.c1 == s.units;
-      const size_t slot = (size_t)blockIdx.x * 2 + (s.c0 == 0);
+      const size_t part = (size_t)blockIdx.x * 2 + (s.c0 == 0);
       const int live = min(NQ, a.T * a.G - s.qb * NQ);
-      for (int v = r; v < live; v += kSoft) {
+      if (tid < live) {
+        const int v = tid;
         float sum = 0.f;
         if (v < s.nq && s.keys > 0) sum = s_l[0][v] + s_l[1][v] + s_l[2][v] + s_l[3][v];
-        const float m = sum == 0.f ? -INFINITY : s_mq[v];
+        const float m = sum == 0.f ? -INFINITY : s_ref[v] == -INFINITY ? 0.f : s_ref[v];   // (NaN scores: no maximum)
         if (sum != 0.f && s_bad[v]) sum = __uint_as_float(0x7fc00000u);
         if (whole) {
           s_inv[v] = sum == 0.f ? 0.f : 1.f / sum;
           store_lse(a, s.b, vector_of(a, s.h, s.qb, v), m, sum);
         } else {
           s_inv[v] = sum == 0.f ? 0.f : 1.f;
-          a.part_ml[(slot * 2) * NQ + v] = m;
-          a.part_ml[(slot * 2 + 1) * NQ + v] = sum;
+          a.part_ml[(part * 2) * NQ + v] = m;
+          a.part_ml[(part * 2 + 1) * NQ + v] = sum;
         }
       }
       sync();
-      // O^T holds sums of p * 2^(V's scale - s_vref + kPShift)
-      const float unscale = F8 ? ex2((float)(s_vref - 127)) : 1.f;
-      if (r < HD) {                            // (whole warps)
-#pragma unroll 1
-        for (int g = 0; g < live; g += 16) {
-          float o[16];
-          tc::tmem_ld16(t_o + lane_base + g, o);
-          if constexpr (F8) {
-            float o2[16];
-            tc::tmem_ld16(t_o + lane_base + NQ + g, o2);
+      if (r < HD) {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) o[e] = fmaf(o2[e], 1.f / kLoScale, o[e]) * (1.f / (1 << kPShift)) * unscale;
-          }
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            if (g + e >= live) break;
-            const float inv = s_inv[g + e], x = inv == 0.f ? 0.f : o[e] * inv;
-            if (whole) static_cast<__nv_bfloat16*>(a.out)[s_out[g + e] + r] = __float2bfloat16_rn(x);
-            else a.part_o[(slot * NQ + g + e) * HD + r] = x;
-          }
+        for (int v = 0; v < CQ; ++v) {
+          if (c0 + v >= live) break;
+          const float inv = s_inv[c0 + v], x = inv == 0.f ? 0.f : o[v] * inv;
+          if (whole) static_cast<__nv_bfloat16*>(a.out)[s_out[c0 + v] + r] = __float2bfloat16_rn(x);
+          else a.part_o[(part * NQ + c0 + v) * HD + r] = x;
         }
       }
-      tc::tc_fence_before();
+      sync();                                  // the statistics are read
       unit += s.c1 - s.c0;
     }
   }
@@ -661,7 +653,7 @@ cudaError_t launch(const TreeArgs& a, cudaStream_t s) {
   static const cudaError_t set =
       cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::smem(CDSL_TREE_MAX_BATCH));
   if (set != cudaSuccess) return set;
-  return launch_pdl(k, dim3(a.blocks), dim3(kThreads), C::smem(c.batch), s, a, map);
+  return launch_pdl(k, dim3(a.blocks), dim3(C::THREADS), C::smem(c.batch), s, a, map);
 }
 
 template <typename F>

@@ -35,7 +35,8 @@ struct Check {
   bool cache(const cdsl_kv_cache* k, Cache* c, bool pointers = true) const {
     if (!k) return no("cache is NULL");
     if (pointers && (!k->d_pool || !k->d_scale || !k->d_page_table)) return no("a cache pointer is NULL");
-    if (pointers && !aligned(k->d_pool, 16)) return no("the cache's pool must be 16-byte aligned");
+    if (pointers && (!aligned(k->d_pool, 16) || !aligned(k->d_scale, 16)))
+      return no("the cache's pool and scale must be 16-byte aligned");
     if (k->head_dim != 64 && k->head_dim != 128) return no("head_dim must be 64 or 128");
     if (k->page_size < 16 || k->page_size > 256 || (k->page_size & (k->page_size - 1)))
       return no("page_size must be a power of two, 16..256");
