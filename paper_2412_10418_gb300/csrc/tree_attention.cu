@@ -265,9 +265,9 @@ constexpr int kSimtPerSM = 4;                  // resident k_tree_simt blocks pe
 
 void sizes_of(const Cache& c, bool tc, int H, int T, Sizes* z) {
   const int vectors = T * (H / c.kvh);
-  z->NQ = tc ? tc_query_block(vectors) : SQ;
+  z->NQ = !tc ? SQ : vectors <= 16 ? 16 : vectors <= 32 ? 32 : kRowsBlock;
   z->QB = (vectors + z->NQ - 1) / z->NQ;
-  z->blocks = kPlanSMs * (tc ? tc_blocks_per_sm(c, z->NQ) : kSimtPerSM);
+  z->blocks = kPlanSMs * (!tc ? kSimtPerSM : z->NQ == kRowsBlock ? 1 : tc_blocks_per_sm(c, z->NQ));
   const size_t slots = (size_t)z->blocks * 2 * z->NQ;
   auto up = [](size_t n) { return (n + 255) / 256 * 256; };
   z->ml_off = up((c.batch + 1) * sizeof(int32_t));
@@ -289,7 +289,7 @@ cudaError_t launch_simt(const TreeArgs& a, cudaStream_t s) {
 cudaError_t launch_pass(const TreeArgs& a, bool tc, bool split, cudaStream_t s) {
   const bool d128 = a.c.hd == 128, f8 = a.c.eb == 1;
   cudaError_t e;
-  if (tc) e = launch_tree_tc(a, s);
+  if (tc) e = a.NQ == kRowsBlock ? launch_tree_rows(a, s) : launch_tree_tc(a, s);
   else if (d128) e = f8 ? launch_simt<float, 128, true>(a, s) : launch_simt<float, 128, false>(a, s);
   else e = f8 ? launch_simt<float, 64, true>(a, s) : launch_simt<float, 64, false>(a, s);
   if (e != cudaSuccess || !split) return e;

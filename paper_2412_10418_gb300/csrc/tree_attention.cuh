@@ -153,10 +153,12 @@ __device__ __forceinline__ void check_lens(const TreeArgs& a) {
     if (a.lens[b] < 0 || a.lens[b] > a.max_len) set_status(a.status, CDSL_ERANGE);
 }
 
-// The tensor-core kernels (tree_attention_tc.cu).
-int tc_query_block(int vectors);               // query vectors per block
+// The tensor-core kernels: slots as M, up to 32 query vectors per block (tree_attention_tc.cu), and vectors as
+// M, up to 128 (tree_attention_rows.cu).
+constexpr int kRowsBlock = 128;
 int tc_blocks_per_sm(const Cache& c, int NQ);
 cudaError_t launch_tree_tc(const TreeArgs& a, cudaStream_t s);
+cudaError_t launch_tree_rows(const TreeArgs& a, cudaStream_t s);
 
 }  // namespace tree
 }  // namespace cdsl

@@ -34,13 +34,12 @@
 #include "gemm.cuh"
 #include "kernels.h"
 #include "tree_attention.cuh"
+#include "tree_tc.cuh"
 
 namespace cdsl {
 namespace tree {
 namespace {
 
-constexpr float kMargin = 8.f;                 // base 2
-constexpr int kPShift = 8;                     // e4m3 probabilities are stored times 2^kPShift <= 448
 constexpr float kLoScale = 32.f;               // of their second plane
 
 template <int HD, int NQ, bool F8>
@@ -76,30 +75,6 @@ struct Cfg {
   static constexpr size_t smem(int batch) { return 1024 + PLAN_OFF + (batch + 1) * 4; }
 };
 
-// Position in a sequence of phases: index and parity of the `n`-th use of one of `of` barriers.
-__device__ __forceinline__ uint32_t parity(int n, int of) { return (n / of) & 1; }
-
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-__device__ __forceinline__ float warp_fmax(float x) {
-  float y;
-  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
-  return y;
-}
-// (a, b) to two e4m3 codes, a in the low byte, as a half2 (11 bits) would be rounded
-__device__ __forceinline__ uint32_t f8x2(__half2 h) {
-  uint16_t r;
-  asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(r) : "r"(*reinterpret_cast<uint32_t*>(&h)));
-  return r;
-}
-__device__ __forceinline__ __half2 f8x2_half(uint32_t two) {
-  uint32_t r;
-  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((uint16_t)two));
-  return *reinterpret_cast<__half2*>(&r);
-}
 template <int HD, int NQ, bool F8>
 __global__ void __launch_bounds__(Cfg<HD, NQ, F8>::THREADS, Cfg<HD, NQ, F8>::CTAS)
     k_tree_tc(TreeArgs a, const __grid_constant__ CUtensorMap map) {
@@ -156,57 +131,10 @@ __global__ void __launch_bounds__(Cfg<HD, NQ, F8>::THREADS, Cfg<HD, NQ, F8>::CTA
   const int total = s_first[c.batch], runs = runs_of(a, total);
   const int begin = (int)blockIdx.x < runs ? run_begin(blockIdx.x, total, runs) : 0;
   const int end = (int)blockIdx.x < runs ? run_begin(blockIdx.x + 1, total, runs) : 0;
-  const int P = 1 << c.page_shift;
 
   if (warp == kProducer) {
-    // ------------------------------------------------------------------------- K and V chunks
-    const int rows = min(P, kKeys), pieces = kKeys / rows;
-    int it = 0, issued[2] = {0, 0};            // chunks, and copies of K and of V
-    bool ok = true;
-    for (int unit = begin; unit < end && ok;) {
-      const Segment s = segment_at(a, s_first, unit, end);
-      for (int ch = s.c0; ch < s.c1 && ok; ++ch, ++it) {
-        const int st = it % NST;
-        const int slot = ch * kKeys + lane * rows;
-        int page = -1;
-        if (lane < pieces && slot < s.keys) page = page_of(c, s.b, slot);
-        const uint32_t live = __ballot_sync(0xffffffffu, page >= 0), n = __popc(live) * rows;
-        if (slot < s.keys && lane < pieces && page < 0) set_status(a.status, CDSL_ERANGE);
-#pragma unroll
-        for (int kv = 0; kv < 2; ++kv) {
-          uint64_t* full = kv ? &v_full[st] : &k_full[st];
-          ok = ok && __all_sync(0xffffffffu, tc::mbar_wait(kv ? &v_empty[st] : &k_empty[st],
-                                                           parity(it, NST) ^ 1, a.status));
-          if (!ok) break;
-          if (lane == 0) {
-            if (kv) s_pieces[st] = live;
-            tc::mbar_expect_tx(full, n * (C::KROW + 2 * kv));
-          }
-          __syncwarp();
-          if (page >= 0) {
-            const int y = (int)row_of(c, 0, page, kv, s.h, slot & (P - 1));
-            if (kv) {                          // with V: both scale bytes
-              const uint8_t* from = c.scale + row_of(c, a.layer, page, 0, s.h, slot & (P - 1));
-              uint8_t* to = sm + C::SCALE_OFF + st * 2 * kKeys + lane * rows;
-              tc::bulk_load(to, from, rows, full);
-              tc::bulk_load(to + kKeys, from + ((size_t)c.kvh << c.page_shift), rows, full);
-            }
-            uint8_t* dst = sm + C::KV_OFF + (st * 2 + kv) * C::TILE + lane * rows * C::BW;
-#pragma unroll
-            for (int nb = 0; nb < C::NB; ++nb)
-              tc::tma_load_2d(dst + nb * C::BLOCK, &map, nb * (C::BW / C::EB), y, full);
-          }
-          issued[kv] = it + 1;
-        }
-      }
-      unit += s.c1 - s.c0;
-    }
-    // the block leaves only with its copies landed (where a role gave up, nothing may have waited for them)
-    if (!ok)
-#pragma unroll
-      for (int kv = 0; kv < 2; ++kv)
-        for (int i = max(0, issued[kv] - NST); i < issued[kv]; ++i)
-          tc::mbar_wait(kv ? &v_full[i % NST] : &k_full[i % NST], parity(i, NST), a.status);
+    load_chunks<HD, F8, NST>(a, s_first, begin, end, map, sm + C::KV_OFF, sm + C::SCALE_OFF, s_pieces, k_full,
+                             v_full, k_empty, v_empty);
   } else if (warp == kIssuer) {
     // ------------------------------------------------------------------------- MMAs
     if (lane == 0) {
@@ -296,83 +224,12 @@ __global__ void __launch_bounds__(Cfg<HD, NQ, F8>::THREADS, Cfg<HD, NQ, F8>::CTA
     bool failed = false, gone = false;
     for (int unit = begin; unit < end && !gone;) {
       const Segment s = segment_at(a, s_first, unit, end);
-      // ---- queries: eight threads a vector, HD / 8 values each
-      constexpr int QE = HD / 8;
-#pragma unroll 1
-      for (int v0 = 0; v0 < NQ; v0 += kSoft / 8) {
-        const int v = v0 + tid / 8, part = tid % 8;
-        const Vec x = vector_of(a, s.h, s.qb, v);
-        uint32_t w[QE / 2];
-#pragma unroll
-        for (int i = 0; i < QE / 2; ++i) w[i] = 0u;
-        if (v < s.nq) {
-          const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(a.q) + s.b * a.sq[0] + x.t * a.sq[1] +
-                                   x.h * a.sq[2] + part * QE;
-          if (q_aligned) {
-#pragma unroll
-            for (int i = 0; i < QE / 8; ++i) {
-              const uint4 u = *reinterpret_cast<const uint4*>(q + 8 * i);
-              w[4 * i] = u.x; w[4 * i + 1] = u.y; w[4 * i + 2] = u.z; w[4 * i + 3] = u.w;
-            }
-          } else {
-#pragma unroll
-            for (int i = 0; i < QE; ++i)
-              w[i / 2] |= (uint32_t)__bfloat16_as_ushort(q[i]) << (i % 2 * 16);
-          }
-        }
-        uint32_t top = 0;                      // largest |x|, as bf16 bits
-#pragma unroll
-        for (int i = 0; i < QE / 2; ++i) top = max(top, max(w[i] & 0x7fffu, w[i] >> 16 & 0x7fffu));
-#pragma unroll
-        for (int o = 4; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-        const bool bad = top >= 0x7f80u;
-        float qs = a.scale;
-        if constexpr (F8) {
-          int e = (int)(top >> 7) - 127 - 8 + ((top & 0x7fu) > 0x60u);
-          e = top == 0 || bad ? 0 : max(e, -126);
-          const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
-          qs *= __uint_as_float((uint32_t)(127 + e) << 23);
-          uint32_t hi[QE / 4], lo[QE / 4];
-#pragma unroll
-          for (int i = 0; i < QE / 4; ++i) {
-            const float y[4] = {__uint_as_float(w[2 * i] << 16), __uint_as_float(w[2 * i] & 0xffff0000u),
-                                __uint_as_float(w[2 * i + 1] << 16), __uint_as_float(w[2 * i + 1] & 0xffff0000u)};
-            uint32_t hl[2], ll[2];
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-              const float2 u = make_float2(y[2 * j] * inv, y[2 * j + 1] * inv);
-              hl[j] = __nv_cvt_float2_to_fp8x2(u, __NV_SATFINITE, __NV_E4M3);
-              const float2 z = f8x2_to_f32(hl[j]);
-              ll[j] = __nv_cvt_float2_to_fp8x2(make_float2(u.x - z.x, u.y - z.y), __NV_SATFINITE, __NV_E4M3);
-            }
-            hi[i] = bad ? 0u : hl[0] | hl[1] << 16;
-            lo[i] = bad ? 0u : ll[0] | ll[1] << 16;
-          }
-          if constexpr (HD == 128) {
-            const uint32_t off = C::Q_OFF + tc::row_offset(v, part, C::BW);
-            *reinterpret_cast<uint4*>(sm + off) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-            *reinterpret_cast<uint4*>(sm + off + C::Q_PLANE) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-          } else {
-            const uint32_t off = C::Q_OFF + tc::row_offset(v, part / 2, C::BW) + part % 2 * 8;
-            *reinterpret_cast<uint2*>(sm + off) = make_uint2(hi[0], hi[1]);
-            *reinterpret_cast<uint2*>(sm + off + C::Q_PLANE) = make_uint2(lo[0], lo[1]);
-          }
-        } else {
-#pragma unroll
-          for (int i = 0; i < QE / 8; ++i) {
-            const int ch = part * (QE / 8) + i;   // 16-byte chunk of the row
-            const uint32_t off = C::Q_OFF + ch / 8 * NQ * C::BW + tc::row_offset(v, ch % 8, C::BW);
-            *reinterpret_cast<uint4*>(sm + off) =
-                bad ? make_uint4(0u, 0u, 0u, 0u) : make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
-          }
-        }
-        if (part == 0) {
-          s_qs[v] = v < s.nq ? qs : 0.f;
-          s_ref[v] = -INFINITY;
-          s_bad[v] = v < s.nq && bad;
-          s_out[v] = s.b * a.so[0] + x.t * a.so[1] + x.h * a.so[2];
-        }
-      }
+      stage_queries<HD, NQ, F8, kSoft>(a, s, tid, q_aligned, sm + C::Q_OFF, [&](int v, const Vec& x, float qs, bool bad) {
+        s_qs[v] = v < s.nq ? qs : 0.f;
+        s_ref[v] = -INFINITY;
+        s_bad[v] = bad;
+        s_out[v] = s.b * a.so[0] + x.t * a.so[1] + x.h * a.so[2];
+      });
       const int t0 = s.qb * NQ / a.G;          // the block's first node
       for (int i = tid; i < (NQ + 1) * kWords; i += kSoft) {
         const int t = t0 + i / kWords, w = i % kWords;
@@ -642,18 +499,12 @@ template <int HD, int NQ, bool F8>
 cudaError_t launch(const TreeArgs& a, cudaStream_t s) {
   using C = Cfg<HD, NQ, F8>;
   CUtensorMap map;
-  const Cache& c = a.c;
-  const size_t rows = (size_t)c.n_pages * 2 * c.kvh << c.page_shift;
-  const int e = encode_map(&map, F8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, C::EB,
-                           c.pool + (size_t)a.layer * rows * C::KROW, HD, rows, C::BW / C::EB,
-                           std::min(1 << c.page_shift, kKeys),
-                           C::BW == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B);
-  if (e) return cudaErrorInvalidValue;
+  if (encode_cache_map<HD, F8>(a, &map)) return cudaErrorInvalidValue;
   auto k = k_tree_tc<HD, NQ, F8>;
   static const cudaError_t set =
       cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::smem(CDSL_TREE_MAX_BATCH));
   if (set != cudaSuccess) return set;
-  return launch_pdl(k, dim3(a.blocks), dim3(C::THREADS), C::smem(c.batch), s, a, map);
+  return launch_pdl(k, dim3(a.blocks), dim3(C::THREADS), C::smem(a.c.batch), s, a, map);
 }
 
 template <typename F>
@@ -663,8 +514,6 @@ auto by_query_block(int NQ, F&& f) {
 }
 
 }  // namespace
-
-int tc_query_block(int vectors) { return vectors <= 16 ? 16 : vectors <= 32 ? 32 : 64; }
 
 int tc_blocks_per_sm(const Cache& c, int NQ) {
   return by_query_block(NQ, [&](auto n) {

@@ -1,0 +1,196 @@
+// tree_tc.cuh -- pieces that the tensor-core kernels of the tree attention share.
+#pragma once
+
+#include <algorithm>
+
+#include "kernels.h"
+#include "tree_attention.cuh"
+
+namespace cdsl {
+namespace tree {
+
+constexpr float kMargin = 8.f;                 // base 2: a sum's reference is raised past it
+constexpr int kPShift = 8;                     // e4m3 probabilities are stored times 2^kPShift <= 448
+
+// Position in a sequence of phases: index and parity of the `n`-th use of one of `of` barriers.
+__device__ __forceinline__ uint32_t parity(int n, int of) { return (n / of) & 1; }
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float warp_fmax(float x) {
+  float y;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
+  return y;
+}
+// (a, b) to two e4m3 codes, a in the low byte, as a half2 (11 bits) would be rounded
+__device__ __forceinline__ uint32_t f8x2(__half2 h) {
+  uint16_t r;
+  asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(r) : "r"(*reinterpret_cast<uint32_t*>(&h)));
+  return r;
+}
+__device__ __forceinline__ __half2 f8x2_half(uint32_t two) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((uint16_t)two));
+  return *reinterpret_cast<__half2*>(&r);
+}
+// Queries of a segment's block to shared memory, by NT threads, eight a vector: K-major tiles of NQ rows in
+// blocks of at most 128 bytes. F8: two e4m3 planes of q / 2^e, hi = e4m3(q / 2^e) and lo the rest, e the
+// smallest with which the row's largest value is at most 448; else bf16 as they are. A row that is not finite, and
+// rows past the block's, become zeros. put(v, where, factor of the scores, not finite) once per vector.
+template <int HD, int NQ, bool F8, int NT, typename F>
+__device__ __forceinline__ void stage_queries(const TreeArgs& a, const Segment& s, int tid, bool q_aligned,
+                                              uint8_t* q_smem, F&& put) {
+  constexpr int QE = HD / 8;                   // values per thread
+  constexpr int KROW = HD * (F8 ? 1 : 2), BW = KROW < 128 ? KROW : 128;
+  constexpr uint32_t PLANE = NQ * KROW;
+#pragma unroll 1
+  for (int v0 = 0; v0 < NQ; v0 += NT / 8) {
+    const int v = v0 + tid / 8, part = tid % 8;
+    const Vec x = vector_of(a, s.h, s.qb, v);
+    uint32_t w[QE / 2];
+#pragma unroll
+    for (int i = 0; i < QE / 2; ++i) w[i] = 0u;
+    if (v < s.nq) {
+      const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(a.q) + s.b * a.sq[0] + x.t * a.sq[1] +
+                               x.h * a.sq[2] + part * QE;
+      if (q_aligned) {
+#pragma unroll
+        for (int i = 0; i < QE / 8; ++i) {
+          const uint4 u = *reinterpret_cast<const uint4*>(q + 8 * i);
+          w[4 * i] = u.x; w[4 * i + 1] = u.y; w[4 * i + 2] = u.z; w[4 * i + 3] = u.w;
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < QE; ++i)
+          w[i / 2] |= (uint32_t)__bfloat16_as_ushort(q[i]) << (i % 2 * 16);
+      }
+    }
+    uint32_t top = 0;                      // largest |x|, as bf16 bits
+#pragma unroll
+    for (int i = 0; i < QE / 2; ++i) top = max(top, max(w[i] & 0x7fffu, w[i] >> 16 & 0x7fffu));
+#pragma unroll
+    for (int o = 4; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+    const bool bad = top >= 0x7f80u;
+    float qs = a.scale;
+    if constexpr (F8) {
+      int e = (int)(top >> 7) - 127 - 8 + ((top & 0x7fu) > 0x60u);
+      e = top == 0 || bad ? 0 : max(e, -126);
+      const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
+      qs *= __uint_as_float((uint32_t)(127 + e) << 23);
+      uint32_t hi[QE / 4], lo[QE / 4];
+#pragma unroll
+      for (int i = 0; i < QE / 4; ++i) {
+        const float y[4] = {__uint_as_float(w[2 * i] << 16), __uint_as_float(w[2 * i] & 0xffff0000u),
+                            __uint_as_float(w[2 * i + 1] << 16), __uint_as_float(w[2 * i + 1] & 0xffff0000u)};
+        uint32_t hl[2], ll[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const float2 u = make_float2(y[2 * j] * inv, y[2 * j + 1] * inv);
+          hl[j] = __nv_cvt_float2_to_fp8x2(u, __NV_SATFINITE, __NV_E4M3);
+          const float2 z = f8x2_to_f32(hl[j]);
+          ll[j] = __nv_cvt_float2_to_fp8x2(make_float2(u.x - z.x, u.y - z.y), __NV_SATFINITE, __NV_E4M3);
+        }
+        hi[i] = bad ? 0u : hl[0] | hl[1] << 16;
+        lo[i] = bad ? 0u : ll[0] | ll[1] << 16;
+      }
+      if constexpr (HD == 128) {
+        const uint32_t off = tc::row_offset(v, part, BW);
+        *reinterpret_cast<uint4*>(q_smem + off) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+        *reinterpret_cast<uint4*>(q_smem + off + PLANE) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+      } else {
+        const uint32_t off = tc::row_offset(v, part / 2, BW) + part % 2 * 8;
+        *reinterpret_cast<uint2*>(q_smem + off) = make_uint2(hi[0], hi[1]);
+        *reinterpret_cast<uint2*>(q_smem + off + PLANE) = make_uint2(lo[0], lo[1]);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < QE / 8; ++i) {
+        const int ch = part * (QE / 8) + i;   // 16-byte chunk of the row
+        const uint32_t off = ch / 8 * NQ * BW + tc::row_offset(v, ch % 8, BW);
+        *reinterpret_cast<uint4*>(q_smem + off) =
+            bad ? make_uint4(0u, 0u, 0u, 0u) : make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+      }
+    }
+    if (part == 0) put(v, x, qs, v < s.nq && bad);
+  }
+}
+
+// The loading warp: K and V chunks of a run's segments into a ring of NST stages (tiles of kKeys rows in blocks
+// of at most 128 bytes, swizzled as their rows are wide), a box per page piece, and with V the slots' scale
+// bytes and which pieces there are. Waits are bounded; on expiry it returns with its copies landed.
+template <int HD, bool F8, int NST>
+__device__ __forceinline__ void load_chunks(const TreeArgs& a, const int* first, int begin, int end,
+                                            const CUtensorMap& map, uint8_t* ring, uint8_t* scales,
+                                            uint32_t* s_pieces, uint64_t* k_full, uint64_t* v_full,
+                                            uint64_t* k_empty, uint64_t* v_empty) {
+  constexpr int EB = F8 ? 1 : 2, KROW = HD * EB, BW = KROW < 128 ? KROW : 128, NB = KROW / BW;
+  constexpr uint32_t BLOCK = kKeys * BW, TILE = NB * BLOCK;
+  const Cache& c = a.c;
+  const int lane = threadIdx.x & 31, P = 1 << c.page_shift;
+  const int rows = min(P, kKeys), pieces = kKeys / rows;
+  int it = 0, issued[2] = {0, 0};              // chunks, and copies of K and of V
+  bool ok = true;
+  for (int unit = begin; unit < end && ok;) {
+    const Segment s = segment_at(a, first, unit, end);
+    for (int ch = s.c0; ch < s.c1 && ok; ++ch, ++it) {
+      const int st = it % NST;
+      const int slot = ch * kKeys + lane * rows;
+      int page = -1;
+      if (lane < pieces && slot < s.keys) {
+        page = page_of(c, s.b, slot);
+        if (page < 0) set_status(a.status, CDSL_ERANGE);
+      }
+      const uint32_t live = __ballot_sync(0xffffffffu, page >= 0), n = __popc(live) * rows;
+#pragma unroll 1
+      for (int kv = 0; kv < 2; ++kv) {
+        uint64_t* full = kv ? &v_full[st] : &k_full[st];
+        ok = ok && __all_sync(0xffffffffu, tc::mbar_wait(kv ? &v_empty[st] : &k_empty[st], parity(it, NST) ^ 1,
+                                                         a.status));
+        if (!ok) break;
+        if (lane == 0) {
+          if (kv) s_pieces[st] = live;
+          tc::mbar_expect_tx(full, n * (KROW + 2 * kv));
+        }
+        __syncwarp();
+        if (page >= 0) {
+          const int y = (int)row_of(c, 0, page, kv, s.h, slot & (P - 1));
+          uint8_t* dst = ring + (st * 2 + kv) * TILE + lane * rows * BW;
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb) tc::tma_load_2d(dst + nb * BLOCK, &map, nb * (BW / EB), y, full);
+          if (kv) {                            // both scale bytes
+            const uint8_t* from = c.scale + row_of(c, a.layer, page, 0, s.h, slot & (P - 1));
+            uint8_t* to = scales + st * 2 * kKeys + lane * rows;
+            tc::bulk_load(to, from, rows, full);
+            tc::bulk_load(to + kKeys, from + ((size_t)c.kvh << c.page_shift), rows, full);
+          }
+        }
+        if (kv) issued[1] = it + 1;
+        else issued[0] = it + 1;
+      }
+    }
+    unit += s.c1 - s.c0;
+  }
+  // where a role gave up, nothing may have waited for the copies
+  if (!ok)
+#pragma unroll
+    for (int kv = 0; kv < 2; ++kv)
+      for (int i = max(0, issued[kv] - NST); i < issued[kv]; ++i)
+        tc::mbar_wait(kv ? &v_full[i % NST] : &k_full[i % NST], parity(i, NST), a.status);
+}
+
+// The tensor map of a layer's rows for load_chunks.
+template <int HD, bool F8>
+int encode_cache_map(const TreeArgs& a, CUtensorMap* map) {
+  constexpr int EB = F8 ? 1 : 2, KROW = HD * EB, BW = KROW < 128 ? KROW : 128;
+  const Cache& c = a.c;
+  const size_t rows = (size_t)c.n_pages * 2 * c.kvh << c.page_shift;
+  return encode_map(map, F8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, EB,
+                    c.pool + (size_t)a.layer * rows * KROW, HD, rows, BW / EB, std::min(1 << c.page_shift, kKeys),
+                    BW == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B);
+}
+
+}  // namespace tree
+}  // namespace cdsl
