@@ -5,17 +5,17 @@
 //   O = P V     M = 128 vectors, N = head_dim, K = 128 slots    P in TMEM over S, V tile MN-major as it lands
 //
 // Codes, planes and scales are as in tree_attention_tc.cu, and so are the warps that load chunks and issue
-// MMAs; another turns each chunk's scale bytes into factors. Eight softmax warps: a thread has a vector
-// (a TMEM lane) and half of the chunk's slots (columns), whose maxima the two halves of a row exchange through
-// shared memory, the one barrier of a chunk; its sum l and half of the row's O are its own, so that no other
-// value crosses lanes, whatever the number of vectors. What changes from slot to slot (scales, masks) is
-// read from shared memory. That costs the same for 33 vectors as for 128, and reads K and V once for all
-// of them.
+// MMAs; another turns each chunk's scale bytes into factors. A softmax thread has a vector (a TMEM lane) and
+// walks all the chunk's slots (columns): maximum, probabilities and their sum are its own, no value crosses
+// lanes and no barrier stands in a chunk, whatever the number of vectors. What changes from slot to slot (scales,
+// masks) is read from shared memory. That costs the same for 33 vectors as for 128, and reads K and V once
+// for all of them.
 //
-// Per chunk a thread reads its S twice (maximum, then probabilities), writes P over it, and adds its half
-// of the chunk before's O to fp32 sums in registers. S has two buffers in TMEM, the next chunk's MMAs run
-// during this one's softmax. Packed fp32 pairs (f32x2) halve the instructions of scaling, exponents'
-// arguments and sums; e4m3 planes cost five conversions a pair of probabilities. Bound by instruction issue.
+// Two groups of four softmax warps take alternate chunks, each with its own S (P over it) and O in TMEM, so
+// that one's conversions run beside the other's maxima; they keep nothing from chunk to chunk. Eight more warps
+// hold the rows' sums (half of a row's O each): they take a chunk's maximum and sum from shared memory and its
+// O, which starts anew, from TMEM. With all sixteen warps on one chunk, in the same phase behind a barrier, a
+// chunk took 4,500 to 5,000 cycles. Bound by instruction issue: about nine instructions a score.
 #include <cuda.h>
 
 #include <algorithm>
@@ -29,9 +29,12 @@ namespace tree {
 namespace {
 
 constexpr int kRows = 128;                     // query vectors per block
-constexpr int kSoft = 2 * kRows;
-constexpr int kThreads = kSoft + 96;
-constexpr int kProducer = kSoft / 32, kIssuer = kProducer + 1, kScaler = kProducer + 2;   // warps
+constexpr int kSoft = 2 * kRows;               // softmax threads: two groups
+constexpr int kSum = 2 * kRows;                // threads that hold the sums: two per row
+constexpr int kThreads = kSoft + kSum + 96;
+constexpr int kSumWarp = kSoft / 32, kProducer = kSumWarp + kSum / 32, kIssuer = kProducer + 1,
+              kScaler = kProducer + 2;         // warps
+constexpr int kFlags = 4;                      // segments whose flags are held: the sums lag by less than three
 
 template <int HD, bool F8>
 struct Cfg {
@@ -45,7 +48,7 @@ struct Cfg {
   static constexpr uint32_t Q_PLANE = kRows * KROW;
   static constexpr uint32_t KV_OFF = QP * Q_PLANE;
   static constexpr int FIT = (208 * 1024 - KV_OFF) / (2 * TILE);
-  static constexpr int NST = FIT > 6 ? 6 : FIT;
+  static constexpr int NST = FIT > 4 ? 4 : FIT;
   static_assert(NST >= 2, "stages");
   static constexpr uint32_t SCALE_OFF = KV_OFF + NST * 2 * TILE;
   // K's scale of each slot, and V's relative to the chunk's largest, times 2^kPShift
@@ -53,33 +56,6 @@ struct Cfg {
   static constexpr uint32_t PLAN_OFF = FACTOR_OFF + NST * 2 * kKeys * 4;
   static constexpr size_t smem(int batch) { return 1024 + PLAN_OFF + (batch + 1) * 4; }
 };
-
-// Pairs of fp32 values in a 64-bit register.
-__device__ __forceinline__ uint64_t pair(float a, float b) {
-  uint64_t r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
-  return r;
-}
-__device__ __forceinline__ float2 unpair(uint64_t x) {
-  float2 r;
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(x));
-  return r;
-}
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
-  uint64_t d;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
-  uint64_t d;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t d;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-  return d;
-}
 
 template <int HD, bool F8>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -90,12 +66,13 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint8_t* const sm = smem_raw + ((1024 - (tc::smem_u32(smem_raw) & 1023)) & 1023);
   int* const s_first = reinterpret_cast<int*>(sm + C::PLAN_OFF);
   __shared__ __align__(8) uint64_t k_full[NST], v_full[NST], k_empty[NST], v_empty[NST];
-  __shared__ __align__(8) uint64_t f_full[NST], s_full[2], p_full, o_full, q_full, done;
+  __shared__ __align__(8) uint64_t f_full[NST], s_full[2], p_full[2], o_full[2], o_empty[2], q_full, done;
   __shared__ uint32_t s_tmem;
-  __shared__ uint32_t s_valid[NST][4];         // slots that there are, as bits
+  __shared__ __align__(16) uint32_t s_valid[NST][4];   // slots that there are, as bits
   __shared__ float s_o[NST];                   // factor of the chunk's O
-  __shared__ float s_qs[kRows], s_max[2][2][kRows];   // score factors; the halves' maxima
-  __shared__ int s_bad[kRows];
+  __shared__ float s_qs[kRows];                // score factors
+  __shared__ float s_m[2][kRows], s_l[2][kRows], s_b[2];   // of a group's chunk: maxima, sums, factor of O
+  __shared__ uint8_t s_bad[kFlags][kRows];     // the query is not finite
   __shared__ uint32_t s_mask[kRows + 1][kWords];
   __shared__ uint32_t s_pieces[NST];
   const Cache& c = a.c;
@@ -109,9 +86,12 @@ __global__ void __launch_bounds__(kThreads, 1)
       tc::mbar_init(&v_empty[i], 1);
     }
     for (int i = 0; i < NST; ++i) tc::mbar_init(&f_full[i], 32);
-    for (int i = 0; i < 2; ++i) tc::mbar_init(&s_full[i], 1);
-    tc::mbar_init(&p_full, kSoft);
-    tc::mbar_init(&o_full, 1);
+    for (int i = 0; i < 2; ++i) {
+      tc::mbar_init(&s_full[i], 1);
+      tc::mbar_init(&p_full[i], kRows);
+      tc::mbar_init(&o_full[i], 1);
+      tc::mbar_init(&o_empty[i], kSum);
+    }
     tc::mbar_init(&q_full, kSoft);
     tc::mbar_init(&done, 1);
     tc::fence_mbar_init();
@@ -131,7 +111,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int total = s_first[c.batch], runs = runs_of(a, total);
   const int begin = (int)blockIdx.x < runs ? run_begin(blockIdx.x, total, runs) : 0;
   const int end = (int)blockIdx.x < runs ? run_begin(blockIdx.x + 1, total, runs) : 0;
-  const uint32_t t_o = tmem + 2 * kKeys;       // TMEM columns: S (then P) twice, O
+  const uint32_t t_o = tmem + 2 * kKeys;       // TMEM columns: S (then P) of both groups, O of both
 
   if (warp == kProducer) {
     load_chunks<HD, F8, NST>(a, s_first, begin, end, map, sm + C::KV_OFF, sm + C::SCALE_OFF, s_pieces, k_full,
@@ -167,24 +147,22 @@ __global__ void __launch_bounds__(kThreads, 1)
         return true;
       };
       auto pv = [&](int i) {                   // P V of chunk i
-        if (!tc::mbar_wait(&p_full, i & 1, a.status) ||
+        if (!tc::mbar_wait(&p_full[i & 1], parity(i, 2), a.status) ||
+            !tc::mbar_wait(&o_empty[i & 1], parity(i, 2) ^ 1, a.status) ||
             !tc::mbar_wait(&v_full[i % NST], parity(i, NST), a.status))
           return false;
         tc::tc_fence_after();
         const uint64_t v = desc_v + (uint32_t)(i % NST) * (2 * C::TILE / 16);
         constexpr int STEP = 32 / C::EB;       // slots of an MMA: 8 columns of P
-        // P of 32 slots: the planes side by side in the first 16 (e4m3) or all of the 32 columns that held their
-        // S, or of the 32 before (the same half's)
-        auto p_at = [](int k, int p) {
-          return F8 ? k / 2 * 64 + k % 2 * 16 + p * 8 : k / 2 * 32 + p * 16 + k % 2 * 8;
-        };
+        // P of 32 slots lies in the columns that held their S, hi then lo
+        auto p_at = [](int k, int p) { return F8 ? k * 32 + p * 8 : k / 2 * 32 + p * 16 + k % 2 * 8; };
 #pragma unroll 1
         for (int p = 1; p >= 0; --p)
 #pragma unroll
           for (int k = 0; k < kKeys / STEP; ++k)
-            tc::umma_tmem_a<F8>(t_o, tmem + (i & 1) * kKeys + p_at(k, p), v + k * (STEP * C::BW / 16), idesc_o,
+            tc::umma_tmem_a<F8>(t_o + (i & 1) * kKeys, tmem + (i & 1) * kKeys + p_at(k, p), v + k * (STEP * C::BW / 16), idesc_o,
                                 p < 1 || k > 0);
-        tc::umma_commit(&o_full);
+        tc::umma_commit(&o_full[i & 1]);
         tc::umma_commit(&v_empty[i % NST]);
         return true;
       };
@@ -194,10 +172,10 @@ __global__ void __launch_bounds__(kThreads, 1)
         const Segment s = segment_at(a, s_first, unit, end);
         const int n = s.c1 - s.c0;
         ok = tc::mbar_wait(&q_full, seg & 1, a.status);
-        // S a chunk ahead of P V; the S after that overwrites the P that this one reads, in order
-        for (int i = 0; i <= n && ok; ++i) {
-          if (i < n) ok = s_mma(it + i);
-          if (ok && i > 0) ok = pv(it + i - 1);
+        // S two chunks ahead; one that overwrites a P follows the P V that reads it, in order
+        for (int i = 0; i < n + 2 && ok; ++i) {
+          if (i >= 2) ok = pv(it + i - 2);
+          if (ok && i < n) ok = s_mma(it + i);
         }
         it += n;
         unit += n;
@@ -260,22 +238,19 @@ __global__ void __launch_bounds__(kThreads, 1)
       unit += s.c1 - s.c0;
     }
     __syncwarp();
-  } else {
+  } else if (warp < kSumWarp) {
     // ------------------------------------------------------------------------- softmax
-    const int tid = threadIdx.x, half = tid / kRows, r = tid % kRows, w4 = warp & 3;
-    const uint32_t lanes = (uint32_t)(w4 * 32) << 16;
-    constexpr int OD = HD / 2;                 // dimensions of O of a thread
-    const uint32_t my_o = t_o + lanes + half * OD;
+    const int tid = threadIdx.x, grp = tid / kRows, r = tid % kRows, w4 = warp & 3;
+    const uint32_t t_s = tmem + grp * kKeys + ((uint32_t)(w4 * 32) << 16);
     auto sync = [] { tc::named_barrier(1, kSoft); };
     const bool q_aligned = (reinterpret_cast<uintptr_t>(a.q) | (a.sq[0] | a.sq[1] | a.sq[2]) * 2) % 16 == 0;
-    const bool o_aligned = (reinterpret_cast<uintptr_t>(a.out) | (a.so[0] | a.so[1] | a.so[2]) * 2) % 16 == 0;
-    int it = 0;
-    bool failed = false, gone = false;
-    for (int unit = begin; unit < end && !gone;) {
+    int it0 = 0, seg = 0;
+    bool failed = false;
+    for (int unit = begin; unit < end; ++seg) {
       const Segment s = segment_at(a, s_first, unit, end);
       stage_queries<HD, kRows, F8, kSoft>(a, s, tid, q_aligned, sm, [&](int v, const Vec&, float qs, bool bad) {
         s_qs[v] = v < s.nq ? qs : 0.f;
-        s_bad[v] = bad;
+        s_bad[seg % kFlags][v] = bad;
       });
       const int t0 = s.qb * kRows / a.G;       // the block's first node
       for (int i = tid; i < (kRows + 1) * kWords; i += kSoft) {
@@ -288,190 +263,188 @@ __global__ void __launch_bounds__(kThreads, 1)
       const float qs = s_qs[r];
       const bool live = w4 * 32 < s.nq;        // (a warp's: its rows hold vectors)
       const uint32_t* const my_mask = s_mask[r < s.nq ? vector_of(a, s.h, s.qb, r).t - t0 : 0];
-      float ref = -INFINITY, l = 0.f, b_old = 0.f;
-      uint64_t o[OD / 2];
-#pragma unroll
-      for (int d = 0; d < OD / 2; ++d) o[d] = 0ull;
-      // the last P V's O to the sums
-      auto add_o = [&] {
-        tc::tc_fence_after();
-        if (live) {
-          const uint64_t f = pair(b_old, b_old);
-#pragma unroll
-          for (int d = 0; d < OD; d += 16) {
-            uint32_t x[16];
-            tc::tmem_ld16_nowait(my_o + d, x);
-            tc::tmem_wait_ld();
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-              o[d / 2 + e] = fma2(pair(__uint_as_float(x[2 * e]), __uint_as_float(x[2 * e + 1])), f, o[d / 2 + e]);
-          }
-        }
-        tc::tc_fence_before();
-      };
-
-      for (int ch = s.c0; ch < s.c1; ++ch, ++it) {
-        const int st = it % NST;
-        const uint32_t t_s = tmem + (it & 1) * kKeys + lanes + half * 64;   // this half's slots
-        const float* const kf = reinterpret_cast<const float*>(sm + C::FACTOR_OFF) + st * 2 * kKeys + half * 64;
+      const int n = s.c1 - s.c0;
+      for (int i = (it0 & 1) ^ grp; i < n && !failed; i += 2) {   // chunks it with it % 2 == grp
+        const int it = it0 + i, st = it % NST;
+        const float* const kf = reinterpret_cast<const float*>(sm + C::FACTOR_OFF) + st * 2 * kKeys;
         bool ok = tc::mbar_wait(&f_full[st], parity(it, NST), a.status);
-        ok = ok && tc::mbar_wait(&s_full[it & 1], parity(it, 2), a.status);
-        if (!__all_sync(0xffffffffu, ok)) failed = true;
+        ok = ok && tc::mbar_wait(&s_full[grp], parity(it, 2), a.status);
         tc::tc_fence_after();
         // a chunk with slots of the tree, past the item's, or without a page: each row has its mask
-        const int node0 = ch * kKeys - s.len;
-        const bool masked =
-            node0 > -kKeys || (s_valid[st][0] & s_valid[st][1] & s_valid[st][2] & s_valid[st][3]) != ~0u;
-        auto word = [&](int w) -> uint32_t {   // of the half's slots 32 w .. 32 w + 31
-          const int first = node0 + 64 * half + 32 * w;   // the tree's node in its first slot
+        const int node0 = (s.c0 + i) * kKeys - s.len;
+        const uint4 valid = *reinterpret_cast<const uint4*>(s_valid[st]);
+        const bool masked = node0 > -kKeys || (valid.x & valid.y & valid.z & valid.w) != ~0u;
+        auto word = [&](int w) -> uint32_t {   // slots 32 w .. 32 w + 31 that this row sees
+          const int first = node0 + 32 * w;    // the tree's node in the first of them
           uint32_t x;
           if (first <= -32) x = ~0u;
           else if (first < 0) x = ((1u << -first) - 1) | my_mask[0] << -first;
           else if (first >= 32 * kWords) x = 0u;
           else x = __funnelshift_r(my_mask[first >> 5], first >> 5 < kWords - 1 ? my_mask[(first >> 5) + 1] : 0u, first & 31);
-          return r < s.nq ? x & s_valid[st][2 * half + w] : 0u;
+          return r < s.nq ? x & s_valid[st][w] : 0u;
         };
-        // 16 slots from e0 on as scores times K's scale
-        auto scores = [&](int e0, uint64_t (&t)[8]) {
-          uint32_t x[16];
-          tc::tmem_ld16_nowait(t_s + e0, x);
-          tc::tmem_wait_ld();
-#pragma unroll
-          for (int e = 0; e < 8; e += 2) {
-            const float4 k = *reinterpret_cast<const float4*>(kf + e0 + 2 * e);
-            t[e] = mul2(pair(__uint_as_float(x[2 * e]), __uint_as_float(x[2 * e + 1])), pair(k.x, k.y));
-            t[e + 1] = mul2(pair(__uint_as_float(x[2 * e + 2]), __uint_as_float(x[2 * e + 3])), pair(k.z, k.w));
-          }
-          if (masked) {
-            const uint32_t m = word(e0 / 32) >> (e0 % 32);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const float2 y = unpair(t[e]);
-              t[e] = pair(m >> (2 * e) & 1 ? y.x : -INFINITY, m >> (2 * e + 1) & 1 ? y.y : -INFINITY);
-            }
-          }
-        };
-        // ---- the row's maximum
-        float top = -INFINITY;
+        float mq = -INFINITY, sum = 0.f;
         if (live) {
-#pragma unroll 2
-          for (int e0 = 0; e0 < 64; e0 += 16) {
-            uint64_t t[8];
-            scores(e0, t);
+          // slots 16 g .. as scores times K's scale
+          auto scores = [&](const uint32_t (&x)[16], int g, uint32_t seen, float (&t)[16]) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const float2 y = unpair(t[e]);
-              top = fmaxf(top, fmaxf(y.x, y.y));
+            for (int e = 0; e < 16; e += 4) {
+              const float4 k = *reinterpret_cast<const float4*>(kf + 16 * g + e);
+              t[e] = __uint_as_float(x[e]) * k.x;
+              t[e + 1] = __uint_as_float(x[e + 1]) * k.y;
+              t[e + 2] = __uint_as_float(x[e + 2]) * k.z;
+              t[e + 3] = __uint_as_float(x[e + 3]) * k.w;
             }
-          }
-        }
-        s_max[it & 1][half][r] = top;
-        if (tc::named_barrier_or(1, kSoft, failed)) {
-          gone = true;
-          break;
-        }
-        top = fmaxf(top, s_max[it & 1][1 - half][r]);
-        float b = 0.f, f = 1.f, mq = 0.f;      // the chunk's factor, the sums', the chunk's maximum
-        if (top > -INFINITY) {
-          mq = top * qs;
-          if (!(mq - ref <= kMargin)) {
-            f = ref == -INFINITY ? 1.f : ex2(ref - mq);   // (no reference: the sums are 0)
-            ref = mq;
-          }
-          b = ex2(mq - ref);
-        }
-        // ---- the chunk before's O
-        if (ch > s.c0) {
-          if (!__all_sync(0xffffffffu, tc::mbar_wait(&o_full, (it - 1) & 1, a.status))) failed = true;
-          else add_o();
-        }
-        if (live) {
-          if (__any_sync(0xffffffffu, f != 1.f)) {
-            l *= f;
-            const uint64_t ff = pair(f, f);
+            if (masked) {
 #pragma unroll
-            for (int d = 0; d < OD / 2; ++d) o[d] = mul2(o[d], ff);
-          }
-          // ---- probabilities, their sum, V's scale on them, P over S
-          const uint64_t qs2 = pair(qs, qs), mq2 = pair(-mq, -mq);
-          uint64_t sum = 0ull;
-#pragma unroll 1
-          for (int w = 0; w < 2; ++w) {
-            uint32_t p0[16], p1[16];           // e4m3: hi and lo words; bf16: hi pairs, lo pairs
+              for (int e = 0; e < 16; ++e)
+                if (!(seen >> e & 1)) t[e] = -INFINITY;
+            }
+          };
+          // ---- the row's maximum
+          float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            uint32_t x[2][16];
+            tc::tmem_ld16_nowait(t_s + 32 * w, x[0]);
+            tc::tmem_ld16_nowait(t_s + 32 * w + 16, x[1]);
+            const uint32_t seen = masked ? word(w) : ~0u;
+            tc::tmem_wait_ld();
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-              uint64_t t[8];
-              scores(32 * w + 16 * h, t);
+              float t[16];
+              scores(x[h], 2 * w + h, seen >> (16 * h), t);
 #pragma unroll
-              for (int e = 0; e < 8; e += 2) {
-                const float4 v = *reinterpret_cast<const float4*>(kf + kKeys + 32 * w + 16 * h + 2 * e);
+              for (int e = 0; e < 16; e += 2) m[e / 2 % 4] = fmaxf(fmaxf(t[e], t[e + 1]), m[e / 2 % 4]);
+            }
+          }
+          const float top = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
+          mq = top == -INFINITY ? -INFINITY : top * qs;
+          const float off = top == -INFINITY ? 0.f : mq;
+          // ---- probabilities, their sum, V's scale on them, P over S
+          float add[2] = {0.f, 0.f};
+#pragma unroll 1
+          for (int w = 0; w < 4; ++w) {
+            uint32_t x[2][16];
+            tc::tmem_ld16_nowait(t_s + 32 * w, x[0]);
+            tc::tmem_ld16_nowait(t_s + 32 * w + 16, x[1]);
+            const uint32_t seen = masked ? word(w) : ~0u;
+            tc::tmem_wait_ld();
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              float t[16];
+              scores(x[h], 2 * w + h, seen >> (16 * h), t);
+              constexpr int W = F8 ? 4 : 8;
+              uint32_t hi[W], lo[W];
+#pragma unroll
+              for (int e = 0; e < 16; e += 4) {
+                const float4 v = *reinterpret_cast<const float4*>(kf + kKeys + 32 * w + 16 * h + e);
                 float y[4];
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                  const float2 z = unpair(fma2(t[e + j], qs2, mq2));
-                  const uint64_t p = pair(ex2(z.x), ex2(z.y));
-                  sum = add2(sum, p);
-                  const float2 u = unpair(mul2(p, j ? pair(v.z, v.w) : pair(v.x, v.y)));
-                  y[2 * j] = u.x;
-                  y[2 * j + 1] = u.y;
+                for (int j = 0; j < 4; ++j) {
+                  y[j] = ex2(fmaf(t[e + j], qs, -off));
+                  add[j & 1] += y[j];
                 }
+                y[0] *= v.x;
+                y[1] *= v.y;
+                y[2] *= v.z;
+                y[3] *= v.w;
                 if (masked) {                  // (0 * NaN of a V that this row does not see)
-                  const uint32_t m = word(w) >> (16 * h + 2 * e);
 #pragma unroll
                   for (int j = 0; j < 4; ++j)
-                    if (!(m >> j & 1)) y[j] = 0.f;
+                    if (!(seen >> (16 * h + e + j) & 1)) y[j] = 0.f;
                 }
                 if constexpr (F8) {            // four slots: a word of each plane
-                  uint32_t hi[2], lo[2];
-#pragma unroll
-                  for (int j = 0; j < 2; ++j) {
-                    const __half2 z = __floats2half2_rn(y[2 * j], y[2 * j + 1]);
-                    hi[j] = f8x2(z);
-                    lo[j] = f8x2(__hsub2(z, f8x2_half(hi[j])));
-                  }
-                  p0[4 * h + e / 2] = hi[0] | hi[1] << 16;
-                  p0[8 + 4 * h + e / 2] = lo[0] | lo[1] << 16;
+                  const __half2 z0 = __floats2half2_rn(y[0], y[1]), z1 = __floats2half2_rn(y[2], y[3]);
+                  __half2 h0, h1;
+                  hi[e / 4] = f8x4(z0, z1);
+                  f8x4_half(hi[e / 4], &h0, &h1);
+                  lo[e / 4] = f8x4(__hsub2(z0, h0), __hsub2(z1, h1));
                 } else {
 #pragma unroll
                   for (int j = 0; j < 2; ++j) {
                     const __nv_bfloat162 z = __floats2bfloat162_rn(y[2 * j], y[2 * j + 1]);
                     const __nv_bfloat162 d = __floats2bfloat162_rn(y[2 * j] - __low2float(z), y[2 * j + 1] - __high2float(z));
-                    p0[8 * h + e + j] = *reinterpret_cast<const uint32_t*>(&z);
-                    p1[8 * h + e + j] = *reinterpret_cast<const uint32_t*>(&d);
+                    hi[e / 2 + j] = *reinterpret_cast<const uint32_t*>(&z);
+                    lo[e / 2 + j] = *reinterpret_cast<const uint32_t*>(&d);
                   }
                 }
               }
-            }
-            if constexpr (F8) {                // (into columns of this half that have been read)
-              tc::tmem_st16_nowait(t_s + 16 * w, p0);
-            } else {
-              tc::tmem_st16_nowait(t_s + 32 * w, p0);
-              tc::tmem_st16_nowait(t_s + 32 * w + 16, p1);
+              const uint32_t to = t_s + 32 * w + h * W;
+              tc::tmem_st_nowait(to, hi);
+              tc::tmem_st_nowait(to + 2 * W, lo);
             }
           }
-          const float2 two = unpair(sum);
-          l = fmaf(two.x + two.y, b, l);
-          b_old = b * s_o[st];
+          sum = add[0] + add[1];
           tc::tmem_wait_st();
         }
+        // ---- for the sums, which have taken this group's chunk before
+        ok = ok && tc::mbar_wait(&o_empty[grp], parity(it, 2) ^ 1, a.status);
+        failed = !__all_sync(0xffffffffu, ok);   // (a warp gives up as one)
+        s_m[grp][r] = mq;
+        s_l[grp][r] = sum;
+        if (r == 0) s_b[grp] = s_o[st];
         tc::tc_fence_before();
-        tc::mbar_arrive(&p_full);
+        tc::mbar_arrive(&p_full[grp]);
       }
-      // ---- the last O, the halves' sums, the output
-      if (!gone && !__all_sync(0xffffffffu, tc::mbar_wait(&o_full, (it - 1) & 1, a.status))) failed = true;
-      if (tc::named_barrier_or(1, kSoft, failed || gone)) {
-        gone = true;
-        break;
+      if (tc::named_barrier_or(1, kSoft, failed)) break;   // (and the queries and masks are free)
+      it0 += n;
+      unit += n;
+    }
+  } else {
+    // ------------------------------------------------------------------------- sums
+    const int tid = threadIdx.x - kSoft, half = tid / kRows, r = tid % kRows, w4 = warp & 3;
+    constexpr int OD = HD / 2;                 // dimensions of O of a thread
+    const uint32_t my_o = t_o + ((uint32_t)(w4 * 32) << 16) + half * OD;
+    const bool o_aligned = (reinterpret_cast<uintptr_t>(a.out) | (a.so[0] | a.so[1] | a.so[2]) * 2) % 16 == 0;
+    int it = 0, seg = 0;
+    bool failed = false;
+    for (int unit = begin; unit < end && !failed; ++seg) {
+      const Segment s = segment_at(a, s_first, unit, end);
+      const bool live = w4 * 32 < s.nq;
+      float ref = -INFINITY, l = 0.f, o[OD];
+#pragma unroll
+      for (int d = 0; d < OD; ++d) o[d] = 0.f;
+      for (int ch = s.c0; ch < s.c1 && !failed; ++ch, ++it) {
+        const int g = it & 1;
+        bool ok = tc::mbar_wait(&p_full[g], parity(it, 2), a.status);
+        const float mq = s_m[g][r], add = s_l[g][r], scale = s_b[g];
+        float f = 1.f;
+        if (mq > -INFINITY && !(mq - ref <= kMargin)) {
+          f = ref == -INFINITY ? 1.f : ex2(ref - mq);   // (no reference: the sums are 0)
+          ref = mq;
+        }
+        float b = mq == -INFINITY ? 0.f : ex2(mq - ref);
+        l = fmaf(l, f, add * b);
+        b *= scale;
+        if (__any_sync(0xffffffffu, f != 1.f)) {
+#pragma unroll
+          for (int d = 0; d < OD; ++d) o[d] *= f;
+        }
+        ok = ok && tc::mbar_wait(&o_full[g], parity(it, 2), a.status);
+        failed = !__all_sync(0xffffffffu, ok);
+        tc::tc_fence_after();
+        if (live) {
+#pragma unroll
+          for (int d = 0; d < OD; d += 32) {
+            uint32_t x[2][16];
+            tc::tmem_ld16_nowait(my_o + g * kKeys + d, x[0]);
+            if (OD > 16) tc::tmem_ld16_nowait(my_o + g * kKeys + d + 16, x[1]);
+            tc::tmem_wait_ld();
+#pragma unroll
+            for (int e = 0; e < 32; ++e)
+              if (d + e < OD) o[d + e] = fmaf(__uint_as_float(x[e / 16][e % 16]), b, o[d + e]);
+          }
+        }
+        tc::tc_fence_before();
+        tc::mbar_arrive(&o_empty[g]);
       }
-      add_o();
-      s_max[0][half][r] = l;                   // (no longer read as maxima)
-      sync();
-      l = s_max[0][0][r] + s_max[0][1][r];
+      if (failed) break;
       const int rows = min(kRows, a.T * a.G - s.qb * kRows);
       if (r < rows) {
         if (r >= s.nq || s.keys == 0) l = 0.f;
         const float m = l == 0.f ? -INFINITY : ref == -INFINITY ? 0.f : ref;   // (NaN scores: no maximum)
-        if (l != 0.f && s_bad[r]) l = __uint_as_float(0x7fc00000u);
+        if (l != 0.f && s_bad[seg % kFlags][r]) l = __uint_as_float(0x7fc00000u);
         const Vec x = vector_of(a, s.h, s.qb, r);
         if (s.c0 == 0 && s.c1 == s.units) {
           const float inv = l == 0.f ? 0.f : 1.f / l;
@@ -483,8 +456,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             uint32_t w[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              const float2 y = unpair(o[d / 2 + e]);
-              const __nv_bfloat162 z = __floats2bfloat162_rn(l == 0.f ? 0.f : y.x * inv, l == 0.f ? 0.f : y.y * inv);
+              const __nv_bfloat162 z =
+                  __floats2bfloat162_rn(l == 0.f ? 0.f : o[d + 2 * e] * inv, l == 0.f ? 0.f : o[d + 2 * e + 1] * inv);
               w[e] = *reinterpret_cast<const uint32_t*>(&z);
             }
             if (o_aligned) {
@@ -503,13 +476,10 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           float4* out = reinterpret_cast<float4*>(a.part_o + (part * kRows + r) * HD + half * OD);
 #pragma unroll
-          for (int d = 0; d < OD; d += 4) {
-            const float2 y = unpair(o[d / 2]), z = unpair(o[d / 2 + 1]);
-            out[d / 4] = l == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(y.x, y.y, z.x, z.y);
-          }
+          for (int d = 0; d < OD; d += 4)
+            out[d / 4] = l == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(o[d], o[d + 1], o[d + 2], o[d + 3]);
         }
       }
-      sync();                                  // queries, masks and statistics are free
       unit += s.c1 - s.c0;
     }
   }

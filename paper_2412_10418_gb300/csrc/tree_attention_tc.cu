@@ -40,7 +40,6 @@ namespace cdsl {
 namespace tree {
 namespace {
 
-constexpr float kLoScale = 32.f;               // of their second plane
 
 template <int HD, int NQ, bool F8>
 struct Cfg {
@@ -259,7 +258,7 @@ __global__ void __launch_bounds__(Cfg<HD, NQ, F8>::THREADS, Cfg<HD, NQ, F8>::CTA
 #pragma unroll
               for (int j = 0; j < 4; ++j) {
                 float z = __uint_as_float(x[e + j]);
-                if constexpr (F8) z = fmaf(__uint_as_float(y[e + j]), 1.f / kLoScale, z);
+                if constexpr (F8) z += __uint_as_float(y[e + j]);
                 o[g + e + j] = fmaf(z, f[j], o[g + e + j]);
               }
             }
@@ -396,15 +395,11 @@ __global__ void __launch_bounds__(Cfg<HD, NQ, F8>::THREADS, Cfg<HD, NQ, F8>::CTA
             uint32_t hi[4], lo[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              hi[i] = lo[i] = 0u;
-#pragma unroll
-              for (int j = 0; j < 2; ++j) {
-                const __half2 h = __floats2half2_rn(x[4 * i + 2 * j], x[4 * i + 2 * j + 1]);
-                const uint32_t y = f8x2(h);
-                const __half2 rest = __hmul2(__hsub2(h, f8x2_half(y)), __float2half2_rn(kLoScale));
-                hi[i] |= y << (16 * j);
-                lo[i] |= f8x2(rest) << (16 * j);
-              }
+              const __half2 z0 = __floats2half2_rn(x[4 * i], x[4 * i + 1]), z1 = __floats2half2_rn(x[4 * i + 2], x[4 * i + 3]);
+              __half2 h0, h1;
+              hi[i] = f8x4(z0, z1);
+              f8x4_half(hi[i], &h0, &h1);
+              lo[i] = f8x4(__hsub2(z0, h0), __hsub2(z1, h1));
             }
             *reinterpret_cast<uint4*>(p + tc::row_offset(r, (c0 + g) / 16, C::RB)) =
                 make_uint4(hi[0], hi[1], hi[2], hi[3]);

@@ -25,16 +25,25 @@ __device__ __forceinline__ float warp_fmax(float x) {
   asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
   return y;
 }
-// (a, b) to two e4m3 codes, a in the low byte, as a half2 (11 bits) would be rounded
-__device__ __forceinline__ uint32_t f8x2(__half2 h) {
-  uint16_t r;
-  asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(r) : "r"(*reinterpret_cast<uint32_t*>(&h)));
+// Four e4m3 codes, a's low half in the low byte; two codes to a half2 (exact).
+__device__ __forceinline__ uint32_t f8x4(__half2 a, __half2 b) {
+  uint32_t r;
+  asm("{\n\t.reg .b16 x, y;\n\t"
+      "cvt.rn.satfinite.e4m3x2.f16x2 x, %1;\n\t"
+      "cvt.rn.satfinite.e4m3x2.f16x2 y, %2;\n\t"
+      "mov.b32 %0, {x, y};\n\t}"
+      : "=r"(r)
+      : "r"(*reinterpret_cast<uint32_t*>(&a)), "r"(*reinterpret_cast<uint32_t*>(&b)));
   return r;
 }
-__device__ __forceinline__ __half2 f8x2_half(uint32_t two) {
-  uint32_t r;
-  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((uint16_t)two));
-  return *reinterpret_cast<__half2*>(&r);
+// The half2 pairs of four codes.
+__device__ __forceinline__ void f8x4_half(uint32_t four, __half2* a, __half2* b) {
+  asm("{\n\t.reg .b16 x, y;\n\t"
+      "mov.b32 {x, y}, %2;\n\t"
+      "cvt.rn.f16x2.e4m3x2 %0, x;\n\t"
+      "cvt.rn.f16x2.e4m3x2 %1, y;\n\t}"
+      : "=r"(*reinterpret_cast<uint32_t*>(a)), "=r"(*reinterpret_cast<uint32_t*>(b))
+      : "r"(four));
 }
 // Queries of a segment's block to shared memory, by NT threads, eight a vector: K-major tiles of NQ rows in
 // blocks of at most 128 bytes. F8: two e4m3 planes of q / 2^e, hi = e4m3(q / 2^e) and lo the rest, e the
