@@ -19,6 +19,7 @@
 #include <cuda.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "kernels.h"
 #include "tree_attention.cuh"
@@ -34,6 +35,7 @@ constexpr int kSum = 2 * kRows;                // threads that hold the sums: tw
 constexpr int kThreads = kSoft + kSum + 96;
 constexpr int kSumWarp = kSoft / 32, kProducer = kSumWarp + kSum / 32, kIssuer = kProducer + 1,
               kScaler = kProducer + 2;         // warps
+constexpr int kBuf = 3;                        // S (then P) buffers in TMEM; O has the rest
 constexpr int kFlags = 4;                      // segments whose flags are held: the sums lag by less than three
 
 template <int HD, bool F8>
@@ -66,7 +68,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint8_t* const sm = smem_raw + ((1024 - (tc::smem_u32(smem_raw) & 1023)) & 1023);
   int* const s_first = reinterpret_cast<int*>(sm + C::PLAN_OFF);
   __shared__ __align__(8) uint64_t k_full[NST], v_full[NST], k_empty[NST], v_empty[NST];
-  __shared__ __align__(8) uint64_t f_full[NST], s_full[2], p_full[2], o_full[2], o_empty[2], q_full, done;
+  __shared__ __align__(8) uint64_t f_full[NST], s_full[kBuf], p_full[2], m_empty[2], o_full, o_empty, q_full, done;
   __shared__ uint32_t s_tmem;
   __shared__ __align__(16) uint32_t s_valid[NST][4];   // slots that there are, as bits
   __shared__ float s_o[NST];                   // factor of the chunk's O
@@ -86,12 +88,13 @@ __global__ void __launch_bounds__(kThreads, 1)
       tc::mbar_init(&v_empty[i], 1);
     }
     for (int i = 0; i < NST; ++i) tc::mbar_init(&f_full[i], 32);
+    for (int i = 0; i < kBuf; ++i) tc::mbar_init(&s_full[i], 1);
     for (int i = 0; i < 2; ++i) {
-      tc::mbar_init(&s_full[i], 1);
       tc::mbar_init(&p_full[i], kRows);
-      tc::mbar_init(&o_full[i], 1);
-      tc::mbar_init(&o_empty[i], kSum);
+      tc::mbar_init(&m_empty[i], kSum);
     }
+    tc::mbar_init(&o_full, 1);
+    tc::mbar_init(&o_empty, kSum);
     tc::mbar_init(&q_full, kSoft);
     tc::mbar_init(&done, 1);
     tc::fence_mbar_init();
@@ -111,7 +114,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int total = s_first[c.batch], runs = runs_of(a, total);
   const int begin = (int)blockIdx.x < runs ? run_begin(blockIdx.x, total, runs) : 0;
   const int end = (int)blockIdx.x < runs ? run_begin(blockIdx.x + 1, total, runs) : 0;
-  const uint32_t t_o = tmem + 2 * kKeys;       // TMEM columns: S (then P) of both groups, O of both
+  const uint32_t t_o = tmem + kBuf * kKeys;
 
   if (warp == kProducer) {
     load_chunks<HD, F8, NST>(a, s_first, begin, end, map, sm + C::KV_OFF, sm + C::SCALE_OFF, s_pieces, k_full,
@@ -139,16 +142,16 @@ __global__ void __launch_bounds__(kThreads, 1)
               const uint64_t q = desc_q + ((uint32_t)(p * C::Q_PLANE + nb * kRows * C::BW) / 16 + 2 * x);
               const uint64_t kk = k + (nb * C::BLOCK / 16 + 2 * x);
               const bool add = p < C::QP - 1 || nb + x > 0;
-              if constexpr (F8) tc::umma_f8(tmem + (i & 1) * kKeys, q, kk, idesc_s, add);
-              else tc::umma_bf16(tmem + (i & 1) * kKeys, q, kk, idesc_s, add);
+              if constexpr (F8) tc::umma_f8(tmem + i % kBuf * kKeys, q, kk, idesc_s, add);
+              else tc::umma_bf16(tmem + i % kBuf * kKeys, q, kk, idesc_s, add);
             }
-        tc::umma_commit(&s_full[i & 1]);
+        tc::umma_commit(&s_full[i % kBuf]);
         tc::umma_commit(&k_empty[i % NST]);
         return true;
       };
       auto pv = [&](int i) {                   // P V of chunk i
         if (!tc::mbar_wait(&p_full[i & 1], parity(i, 2), a.status) ||
-            !tc::mbar_wait(&o_empty[i & 1], parity(i, 2) ^ 1, a.status) ||
+            !tc::mbar_wait(&o_empty, (i & 1) ^ 1, a.status) ||
             !tc::mbar_wait(&v_full[i % NST], parity(i, NST), a.status))
           return false;
         tc::tc_fence_after();
@@ -160,9 +163,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int p = 1; p >= 0; --p)
 #pragma unroll
           for (int k = 0; k < kKeys / STEP; ++k)
-            tc::umma_tmem_a<F8>(t_o + (i & 1) * kKeys, tmem + (i & 1) * kKeys + p_at(k, p), v + k * (STEP * C::BW / 16), idesc_o,
+            tc::umma_tmem_a<F8>(t_o, tmem + i % kBuf * kKeys + p_at(k, p), v + k * (STEP * C::BW / 16), idesc_o,
                                 p < 1 || k > 0);
-        tc::umma_commit(&o_full[i & 1]);
+        tc::umma_commit(&o_full);
         tc::umma_commit(&v_empty[i % NST]);
         return true;
       };
@@ -172,9 +175,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         const Segment s = segment_at(a, s_first, unit, end);
         const int n = s.c1 - s.c0;
         ok = tc::mbar_wait(&q_full, seg & 1, a.status);
-        // S two chunks ahead; one that overwrites a P follows the P V that reads it, in order
-        for (int i = 0; i < n + 2 && ok; ++i) {
-          if (i >= 2) ok = pv(it + i - 2);
+        // S as far ahead as it has buffers; one that overwrites a P follows the P V that reads it, in order
+        for (int i = 0; i < n + kBuf && ok; ++i) {
+          if (i >= kBuf) ok = pv(it + i - kBuf);
           if (ok && i < n) ok = s_mma(it + i);
         }
         it += n;
@@ -241,7 +244,6 @@ __global__ void __launch_bounds__(kThreads, 1)
   } else if (warp < kSumWarp) {
     // ------------------------------------------------------------------------- softmax
     const int tid = threadIdx.x, grp = tid / kRows, r = tid % kRows, w4 = warp & 3;
-    const uint32_t t_s = tmem + grp * kKeys + ((uint32_t)(w4 * 32) << 16);
     auto sync = [] { tc::named_barrier(1, kSoft); };
     const bool q_aligned = (reinterpret_cast<uintptr_t>(a.q) | (a.sq[0] | a.sq[1] | a.sq[2]) * 2) % 16 == 0;
     int it0 = 0, seg = 0;
@@ -266,9 +268,10 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int n = s.c1 - s.c0;
       for (int i = (it0 & 1) ^ grp; i < n && !failed; i += 2) {   // chunks it with it % 2 == grp
         const int it = it0 + i, st = it % NST;
+        const uint32_t t_s = tmem + it % kBuf * kKeys + ((uint32_t)(w4 * 32) << 16);
         const float* const kf = reinterpret_cast<const float*>(sm + C::FACTOR_OFF) + st * 2 * kKeys;
         bool ok = tc::mbar_wait(&f_full[st], parity(it, NST), a.status);
-        ok = ok && tc::mbar_wait(&s_full[grp], parity(it, 2), a.status);
+        ok = ok && tc::mbar_wait(&s_full[it % kBuf], parity(it, kBuf), a.status);
         tc::tc_fence_after();
         // a chunk with slots of the tree, past the item's, or without a page: each row has its mask
         const int node0 = (s.c0 + i) * kKeys - s.len;
@@ -284,7 +287,9 @@ __global__ void __launch_bounds__(kThreads, 1)
           return r < s.nq ? x & s_valid[st][w] : 0u;
         };
         float mq = -INFINITY, sum = 0.f;
-        if (live) {
+        // Code of its own for chunks with masks: as one, the compiler selects on every score, masked or not,
+        // which took twice the time.
+        auto softmax = [&](auto masked) {
           // slots 16 g .. as scores times K's scale
           auto scores = [&](const uint32_t (&x)[16], int g, uint32_t seen, float (&t)[16]) {
 #pragma unroll
@@ -295,7 +300,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               t[e + 2] = __uint_as_float(x[e + 2]) * k.z;
               t[e + 3] = __uint_as_float(x[e + 3]) * k.w;
             }
-            if (masked) {
+            if constexpr (masked) {
 #pragma unroll
               for (int e = 0; e < 16; ++e)
                 if (!(seen >> e & 1)) t[e] = -INFINITY;
@@ -349,7 +354,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 y[1] *= v.y;
                 y[2] *= v.z;
                 y[3] *= v.w;
-                if (masked) {                  // (0 * NaN of a V that this row does not see)
+                if constexpr (masked) {        // (0 * NaN of a V that this row does not see)
 #pragma unroll
                   for (int j = 0; j < 4; ++j)
                     if (!(seen >> (16 * h + e + j) & 1)) y[j] = 0.f;
@@ -377,9 +382,13 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           sum = add[0] + add[1];
           tc::tmem_wait_st();
+        };
+        if (live) {
+          if (masked) softmax(std::true_type());
+          else softmax(std::false_type());
         }
         // ---- for the sums, which have taken this group's chunk before
-        ok = ok && tc::mbar_wait(&o_empty[grp], parity(it, 2) ^ 1, a.status);
+        ok = ok && tc::mbar_wait(&m_empty[grp], parity(it, 2) ^ 1, a.status);
         failed = !__all_sync(0xffffffffu, ok);   // (a warp gives up as one)
         s_m[grp][r] = mq;
         s_l[grp][r] = sum;
@@ -409,6 +418,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int g = it & 1;
         bool ok = tc::mbar_wait(&p_full[g], parity(it, 2), a.status);
         const float mq = s_m[g][r], add = s_l[g][r], scale = s_b[g];
+        tc::mbar_arrive(&m_empty[g]);
         float f = 1.f;
         if (mq > -INFINITY && !(mq - ref <= kMargin)) {
           f = ref == -INFINITY ? 1.f : ex2(ref - mq);   // (no reference: the sums are 0)
@@ -421,15 +431,15 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
           for (int d = 0; d < OD; ++d) o[d] *= f;
         }
-        ok = ok && tc::mbar_wait(&o_full[g], parity(it, 2), a.status);
+        ok = ok && tc::mbar_wait(&o_full, it & 1, a.status);
         failed = !__all_sync(0xffffffffu, ok);
         tc::tc_fence_after();
         if (live) {
 #pragma unroll
           for (int d = 0; d < OD; d += 32) {
             uint32_t x[2][16];
-            tc::tmem_ld16_nowait(my_o + g * kKeys + d, x[0]);
-            if (OD > 16) tc::tmem_ld16_nowait(my_o + g * kKeys + d + 16, x[1]);
+            tc::tmem_ld16_nowait(my_o + d, x[0]);
+            if (OD > 16) tc::tmem_ld16_nowait(my_o + d + 16, x[1]);
             tc::tmem_wait_ld();
 #pragma unroll
             for (int e = 0; e < 32; ++e)
@@ -437,7 +447,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
         }
         tc::tc_fence_before();
-        tc::mbar_arrive(&o_empty[g]);
+        tc::mbar_arrive(&o_empty);
       }
       if (failed) break;
       const int rows = min(kRows, a.T * a.G - s.qb * kRows);
