@@ -290,20 +290,20 @@ __global__ void __launch_bounds__(kThreads, 1)
         // Code of its own for chunks with masks: as one, the compiler selects on every score, masked or not,
         // which took twice the time.
         auto softmax = [&](auto masked) {
-          // slots 16 g .. as scores times K's scale
-          auto scores = [&](const uint32_t (&x)[16], int g, uint32_t seen, float (&t)[16]) {
+          // slots 16 g .. as scores times K's scale, in pairs
+          auto scores = [&](const uint32_t (&x)[16], int g, uint32_t seen, uint64_t (&t)[8]) {
 #pragma unroll
-            for (int e = 0; e < 16; e += 4) {
-              const float4 k = *reinterpret_cast<const float4*>(kf + 16 * g + e);
-              t[e] = __uint_as_float(x[e]) * k.x;
-              t[e + 1] = __uint_as_float(x[e + 1]) * k.y;
-              t[e + 2] = __uint_as_float(x[e + 2]) * k.z;
-              t[e + 3] = __uint_as_float(x[e + 3]) * k.w;
+            for (int e = 0; e < 8; e += 2) {
+              const ulonglong2 k = *reinterpret_cast<const ulonglong2*>(kf + 16 * g + 2 * e);
+              t[e] = mul2(pair(x[2 * e], x[2 * e + 1]), k.x);
+              t[e + 1] = mul2(pair(x[2 * e + 2], x[2 * e + 3]), k.y);
             }
             if constexpr (masked) {
 #pragma unroll
-              for (int e = 0; e < 16; ++e)
-                if (!(seen >> e & 1)) t[e] = -INFINITY;
+              for (int e = 0; e < 8; ++e) {
+                const float2 y = unpair(t[e]);
+                t[e] = pair(seen >> (2 * e) & 1 ? y.x : -INFINITY, seen >> (2 * e + 1) & 1 ? y.y : -INFINITY);
+              }
             }
           };
           // ---- the row's maximum
@@ -317,17 +317,21 @@ __global__ void __launch_bounds__(kThreads, 1)
             tc::tmem_wait_ld();
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-              float t[16];
+              uint64_t t[8];
               scores(x[h], 2 * w + h, seen >> (16 * h), t);
 #pragma unroll
-              for (int e = 0; e < 16; e += 2) m[e / 2 % 4] = fmaxf(fmaxf(t[e], t[e + 1]), m[e / 2 % 4]);
+              for (int e = 0; e < 8; ++e) {
+                const float2 y = unpair(t[e]);
+                m[e % 4] = fmaxf(fmaxf(y.x, y.y), m[e % 4]);
+              }
             }
           }
           const float top = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
           mq = top == -INFINITY ? -INFINITY : top * qs;
           const float off = top == -INFINITY ? 0.f : mq;
           // ---- probabilities, their sum, V's scale on them, P over S
-          float add[2] = {0.f, 0.f};
+          uint64_t add = 0ull;
+          const uint64_t qs2 = pair(qs, qs), off2 = pair(-off, -off);
 #pragma unroll 1
           for (int w = 0; w < 4; ++w) {
             uint32_t x[2][16];
@@ -337,23 +341,23 @@ __global__ void __launch_bounds__(kThreads, 1)
             tc::tmem_wait_ld();
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-              float t[16];
+              uint64_t t[8];
               scores(x[h], 2 * w + h, seen >> (16 * h), t);
               constexpr int W = F8 ? 4 : 8;
               uint32_t hi[W], lo[W];
 #pragma unroll
               for (int e = 0; e < 16; e += 4) {
-                const float4 v = *reinterpret_cast<const float4*>(kf + kKeys + 32 * w + 16 * h + e);
+                const ulonglong2 v = *reinterpret_cast<const ulonglong2*>(kf + kKeys + 32 * w + 16 * h + e);
                 float y[4];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                  y[j] = ex2(fmaf(t[e + j], qs, -off));
-                  add[j & 1] += y[j];
+                for (int j = 0; j < 2; ++j) {
+                  const float2 z = unpair(fma2(t[e / 2 + j], qs2, off2));
+                  const uint64_t p = pair(ex2(z.x), ex2(z.y));
+                  add = add2(add, p);
+                  const float2 u = unpair(mul2(p, j ? v.y : v.x));
+                  y[2 * j] = u.x;
+                  y[2 * j + 1] = u.y;
                 }
-                y[0] *= v.x;
-                y[1] *= v.y;
-                y[2] *= v.z;
-                y[3] *= v.w;
                 if constexpr (masked) {        // (0 * NaN of a V that this row does not see)
 #pragma unroll
                   for (int j = 0; j < 4; ++j)
@@ -380,7 +384,8 @@ __global__ void __launch_bounds__(kThreads, 1)
               tc::tmem_st_nowait(to + 2 * W, lo);
             }
           }
-          sum = add[0] + add[1];
+          const float2 two = unpair(add);
+          sum = two.x + two.y;
           tc::tmem_wait_st();
         };
         if (live) {
@@ -411,9 +416,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (int unit = begin; unit < end && !failed; ++seg) {
       const Segment s = segment_at(a, s_first, unit, end);
       const bool live = w4 * 32 < s.nq;
-      float ref = -INFINITY, l = 0.f, o[OD];
+      float ref = -INFINITY, l = 0.f;
+      uint64_t o[OD / 2];                      // in pairs
 #pragma unroll
-      for (int d = 0; d < OD; ++d) o[d] = 0.f;
+      for (int d = 0; d < OD / 2; ++d) o[d] = 0ull;
       for (int ch = s.c0; ch < s.c1 && !failed; ++ch, ++it) {
         const int g = it & 1;
         bool ok = tc::mbar_wait(&p_full[g], parity(it, 2), a.status);
@@ -428,13 +434,15 @@ __global__ void __launch_bounds__(kThreads, 1)
         l = fmaf(l, f, add * b);
         b *= scale;
         if (__any_sync(0xffffffffu, f != 1.f)) {
+          const uint64_t ff = pair(f, f);
 #pragma unroll
-          for (int d = 0; d < OD; ++d) o[d] *= f;
+          for (int d = 0; d < OD / 2; ++d) o[d] = mul2(o[d], ff);
         }
         ok = ok && tc::mbar_wait(&o_full, it & 1, a.status);
         failed = !__all_sync(0xffffffffu, ok);
         tc::tc_fence_after();
         if (live) {
+          const uint64_t bb = pair(b, b);
 #pragma unroll
           for (int d = 0; d < OD; d += 32) {
             uint32_t x[2][16];
@@ -442,8 +450,9 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (OD > 16) tc::tmem_ld16_nowait(my_o + d + 16, x[1]);
             tc::tmem_wait_ld();
 #pragma unroll
-            for (int e = 0; e < 32; ++e)
-              if (d + e < OD) o[d + e] = fmaf(__uint_as_float(x[e / 16][e % 16]), b, o[d + e]);
+            for (int e = 0; e < 32; e += 2)
+              if (d + e < OD)
+                o[(d + e) / 2] = fma2(pair(x[e / 16][e % 16], x[e / 16][e % 16 + 1]), bb, o[(d + e) / 2]);
           }
         }
         tc::tc_fence_before();
@@ -466,8 +475,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             uint32_t w[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              const __nv_bfloat162 z =
-                  __floats2bfloat162_rn(l == 0.f ? 0.f : o[d + 2 * e] * inv, l == 0.f ? 0.f : o[d + 2 * e + 1] * inv);
+              const float2 y = unpair(o[d / 2 + e]);
+              const __nv_bfloat162 z = __floats2bfloat162_rn(l == 0.f ? 0.f : y.x * inv, l == 0.f ? 0.f : y.y * inv);
               w[e] = *reinterpret_cast<const uint32_t*>(&z);
             }
             if (o_aligned) {
@@ -486,8 +495,10 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           float4* out = reinterpret_cast<float4*>(a.part_o + (part * kRows + r) * HD + half * OD);
 #pragma unroll
-          for (int d = 0; d < OD; d += 4)
-            out[d / 4] = l == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(o[d], o[d + 1], o[d + 2], o[d + 3]);
+          for (int d = 0; d < OD; d += 4) {
+            const float2 y = unpair(o[d / 2]), z = unpair(o[d / 2 + 1]);
+            out[d / 4] = l == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(y.x, y.y, z.x, z.y);
+          }
         }
       }
       unit += s.c1 - s.c0;
