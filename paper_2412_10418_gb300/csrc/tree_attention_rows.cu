@@ -4,18 +4,25 @@
 //   S = Q K^T   M = 128 vectors, N = 128 slots, K = head_dim    Q and K tiles K-major in shared memory
 //   O = P V     M = 128 vectors, N = head_dim, K = 128 slots    P in TMEM over S, V tile MN-major as it lands
 //
-// Codes, planes and scales are as in tree_attention_tc.cu, and so are the warps that load chunks and issue
-// MMAs; another turns each chunk's scale bytes into factors. A softmax thread has a vector (a TMEM lane) and
-// walks all the chunk's slots (columns): maximum, probabilities and their sum are its own, no value crosses
-// lanes and no barrier stands in a chunk, whatever the number of vectors. What changes from slot to slot (scales,
-// masks) is read from shared memory. That costs the same for 33 vectors as for 128, and reads K and V once
-// for all of them.
+// S of an e4m3 cache is taken as in tree_attention_tc.cu, from the codes and two e4m3 planes of Q. P V is not:
+// turning a pair of probabilities into two e4m3 planes takes 14 cycles of a quarter of an SM (four
+// conversions at 2 or 4 and a difference, measured), 7 a score, where its exponential takes 4. Here the chunk's V is
+// turned into fp16 once for all rows instead, exactly, with its power-of-two scales multiplied in, and P into
+// fp16 by one conversion a pair: 2^-12 of itself, over 22 octaves below a row's reference. A bf16 cache has Q and V
+// as they are and P in two bf16 planes.
 //
-// Two groups of four softmax warps take alternate chunks, each with its own S (P over it) and O in TMEM, so
-// that one's conversions run beside the other's maxima; they keep nothing from chunk to chunk. Eight more warps
-// hold the rows' sums (half of a row's O each): they take a chunk's maximum and sum from shared memory and its
-// O, which starts anew, from TMEM. With all sixteen warps on one chunk, in the same phase behind a barrier, a
-// chunk took 4,500 to 5,000 cycles. Bound by instruction issue: about nine instructions a score.
+// A softmax thread has a vector (a TMEM lane) and walks all the chunk's slots (columns): maximum, reference,
+// probabilities and their sum are its own, no value crosses lanes and no barrier stands in a chunk, whatever
+// the number of vectors. What changes from slot to slot (K's scales, masks) is read from shared memory. That
+// costs the same for 33 vectors as for 128, and reads K and V once for all of them.
+//
+// Two groups of four softmax warps take alternate chunks, each with its own S (which P then overwrites) and O
+// in TMEM, so that one's exponentials run beside the other's maxima and MMAs; they are added up at the end of an
+// item. O is one chain over a group's chunks: fp16's range leaves P exact enough under a reference that is raised
+// only when a maximum passes it by more than 2^kMargin, which after the first chunk is rare, and then the thread
+// multiplies its O. (O started anew in every chunk and was added up in registers before: eight more warps, and a
+// chain of waits through them that held a chunk to 3,500 cycles.) Four warps convert V, one loads, one issues
+// MMAs, one turns scale bytes into factors.
 #include <cuda.h>
 
 #include <algorithm>
@@ -31,12 +38,13 @@ namespace {
 
 constexpr int kRows = 128;                     // query vectors per block
 constexpr int kSoft = 2 * kRows;               // softmax threads: two groups
-constexpr int kSum = 2 * kRows;                // threads that hold the sums: two per row
-constexpr int kThreads = kSoft + kSum + 96;
-constexpr int kSumWarp = kSoft / 32, kProducer = kSumWarp + kSum / 32, kIssuer = kProducer + 1,
+constexpr int kConv = 128;                     // threads that convert V
+constexpr int kThreads = kSoft + kConv + 96;
+constexpr int kConvWarp = kSoft / 32, kProducer = kConvWarp + kConv / 32, kIssuer = kProducer + 1,
               kScaler = kProducer + 2;         // warps
-constexpr int kBuf = 3;                        // S (then P) buffers in TMEM; O has the rest
-constexpr int kFlags = 4;                      // segments whose flags are held: the sums lag by less than three
+constexpr float kMargin = 7.f;                 // base 2: probabilities are at most 2^kMargin of a reference, and
+constexpr float kUp = 7.f;                     // stored times 2^kUp: below fp16's largest
+constexpr int kVRoom = 6;                      // octaves that V's scales may pass theirs by: 448 * 2^6 in fp16
 
 template <int HD, bool F8>
 struct Cfg {
@@ -48,12 +56,15 @@ struct Cfg {
   static constexpr uint32_t TILE = NB * BLOCK;             // K or V of a chunk
   static constexpr int QP = F8 ? 2 : 1;
   static constexpr uint32_t Q_PLANE = kRows * KROW;
-  static constexpr uint32_t KV_OFF = QP * Q_PLANE;
+  // e4m3: V of two chunks in fp16, in blocks of 64 dimensions
+  static constexpr uint32_t H_BLOCK = kKeys * 128, H_TILE = F8 ? HD / 64 * H_BLOCK : 0;
+  static constexpr uint32_t H_OFF = QP * Q_PLANE;
+  static constexpr uint32_t KV_OFF = H_OFF + 2 * H_TILE;
   static constexpr int FIT = (208 * 1024 - KV_OFF) / (2 * TILE);
   static constexpr int NST = FIT > 4 ? 4 : FIT;
   static_assert(NST >= 2, "stages");
   static constexpr uint32_t SCALE_OFF = KV_OFF + NST * 2 * TILE;
-  // K's scale of each slot, and V's relative to the chunk's largest, times 2^kPShift
+  // K's scale of each slot, and V's relative to its reference (0: nothing, or not finite)
   static constexpr uint32_t FACTOR_OFF = SCALE_OFF + NST * 2 * kKeys;
   static constexpr uint32_t PLAN_OFF = FACTOR_OFF + NST * 2 * kKeys * 4;
   static constexpr size_t smem(int batch) { return 1024 + PLAN_OFF + (batch + 1) * 4; }
@@ -68,13 +79,15 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint8_t* const sm = smem_raw + ((1024 - (tc::smem_u32(smem_raw) & 1023)) & 1023);
   int* const s_first = reinterpret_cast<int*>(sm + C::PLAN_OFF);
   __shared__ __align__(8) uint64_t k_full[NST], v_full[NST], k_empty[NST], v_empty[NST];
-  __shared__ __align__(8) uint64_t f_full[NST], s_full[kBuf], p_full[2], m_empty[2], o_full, o_empty, q_full, done;
+  __shared__ __align__(8) uint64_t f_full[NST], f_empty[NST], h_full[2];
+  __shared__ __align__(8) uint64_t s_full[2], p_full[2], pv_done[2], q_full, done;
   __shared__ uint32_t s_tmem;
-  __shared__ __align__(16) uint32_t s_valid[NST][4];   // slots that there are, as bits
-  __shared__ float s_o[NST];                   // factor of the chunk's O
+  __shared__ __align__(16) uint32_t s_valid[NST][4], s_nan[NST][4];   // slots that there are, whose V is not finite
+  __shared__ int s_vref[NST];                  // V's reference in the chunk
   __shared__ float s_qs[kRows];                // score factors
-  __shared__ float s_m[2][kRows], s_l[2][kRows], s_b[2];   // of a group's chunk: maxima, sums, factor of O
-  __shared__ uint8_t s_bad[kFlags][kRows];     // the query is not finite
+  __shared__ float s_m[2][kRows], s_l[2][kRows];   // the groups' references and sums
+  __shared__ int s_v[2];                       // and V references
+  __shared__ uint8_t s_bad[kRows];             // the query is not finite
   __shared__ uint32_t s_mask[kRows + 1][kWords];
   __shared__ uint32_t s_pieces[NST];
   const Cache& c = a.c;
@@ -85,16 +98,16 @@ __global__ void __launch_bounds__(kThreads, 1)
       tc::mbar_init(&k_full[i], 1);
       tc::mbar_init(&v_full[i], 1);
       tc::mbar_init(&k_empty[i], 1);
-      tc::mbar_init(&v_empty[i], 1);
+      tc::mbar_init(&v_empty[i], F8 ? kConv + 1 : 1);
+      tc::mbar_init(&f_full[i], 32);
+      tc::mbar_init(&f_empty[i], kRows);
     }
-    for (int i = 0; i < NST; ++i) tc::mbar_init(&f_full[i], 32);
-    for (int i = 0; i < kBuf; ++i) tc::mbar_init(&s_full[i], 1);
     for (int i = 0; i < 2; ++i) {
+      tc::mbar_init(&h_full[i], kConv);
+      tc::mbar_init(&s_full[i], 1);
       tc::mbar_init(&p_full[i], kRows);
-      tc::mbar_init(&m_empty[i], kSum);
+      tc::mbar_init(&pv_done[i], 1);
     }
-    tc::mbar_init(&o_full, 1);
-    tc::mbar_init(&o_empty, kSum);
     tc::mbar_init(&q_full, kSoft);
     tc::mbar_init(&done, 1);
     tc::fence_mbar_init();
@@ -114,7 +127,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int total = s_first[c.batch], runs = runs_of(a, total);
   const int begin = (int)blockIdx.x < runs ? run_begin(blockIdx.x, total, runs) : 0;
   const int end = (int)blockIdx.x < runs ? run_begin(blockIdx.x + 1, total, runs) : 0;
-  const uint32_t t_o = tmem + kBuf * kKeys;
+  const uint32_t t_o = tmem + 2 * kKeys;       // columns: S (then P) of both groups, O of both
 
   if (warp == kProducer) {
     load_chunks<HD, F8, NST>(a, s_first, begin, end, map, sm + C::KV_OFF, sm + C::SCALE_OFF, s_pieces, k_full,
@@ -124,11 +137,14 @@ __global__ void __launch_bounds__(kThreads, 1)
       constexpr uint32_t formats = F8 ? 0u : (1u << 7) | (1u << 10);
       constexpr uint32_t idesc = (1u << 4) | formats | (128u >> 4) << 24;
       constexpr uint32_t idesc_s = idesc | (uint32_t)(kKeys >> 3) << 17;
-      constexpr uint32_t idesc_o = idesc | (uint32_t)(HD >> 3) << 17 | 1u << 16;
+      // P V in 16 bits: fp16 (format 0) beside an e4m3 cache, else bf16
+      constexpr uint32_t idesc_o = (1u << 4) | (128u >> 4) << 24 | (F8 ? 0u : (1u << 7) | (1u << 10)) |
+                                   (uint32_t)(HD >> 3) << 17 | 1u << 16;
       const uint32_t sbase = tc::smem_u32(sm);
       const uint64_t desc_q = tc::desc_rows(sbase, C::BW, 16);
       const uint64_t desc_k = tc::desc_rows(sbase + C::KV_OFF, C::BW, 16);
-      const uint64_t desc_v = tc::desc_rows(sbase + C::KV_OFF + C::TILE, C::BW, C::BLOCK);
+      const uint64_t desc_v = F8 ? tc::desc_rows(sbase + C::H_OFF, 128, C::H_BLOCK)
+                                 : tc::desc_rows(sbase + C::KV_OFF + C::TILE, C::BW, C::BLOCK);
       auto s_mma = [&](int i) {                // S of chunk i
         if (!tc::mbar_wait(&k_full[i % NST], parity(i, NST), a.status)) return false;
         tc::tc_fence_after();
@@ -142,31 +158,30 @@ __global__ void __launch_bounds__(kThreads, 1)
               const uint64_t q = desc_q + ((uint32_t)(p * C::Q_PLANE + nb * kRows * C::BW) / 16 + 2 * x);
               const uint64_t kk = k + (nb * C::BLOCK / 16 + 2 * x);
               const bool add = p < C::QP - 1 || nb + x > 0;
-              if constexpr (F8) tc::umma_f8(tmem + i % kBuf * kKeys, q, kk, idesc_s, add);
-              else tc::umma_bf16(tmem + i % kBuf * kKeys, q, kk, idesc_s, add);
+              if constexpr (F8) tc::umma_f8(tmem + (i & 1) * kKeys, q, kk, idesc_s, add);
+              else tc::umma_bf16(tmem + (i & 1) * kKeys, q, kk, idesc_s, add);
             }
-        tc::umma_commit(&s_full[i % kBuf]);
+        tc::umma_commit(&s_full[i & 1]);
         tc::umma_commit(&k_empty[i % NST]);
         return true;
       };
-      auto pv = [&](int i) {                   // P V of chunk i
+      auto pv = [&](int i, bool add) {         // P V of chunk i
         if (!tc::mbar_wait(&p_full[i & 1], parity(i, 2), a.status) ||
-            !tc::mbar_wait(&o_empty, (i & 1) ^ 1, a.status) ||
-            !tc::mbar_wait(&v_full[i % NST], parity(i, NST), a.status))
+            !(F8 ? tc::mbar_wait(&h_full[i & 1], parity(i, 2), a.status)
+                 : tc::mbar_wait(&v_full[i % NST], parity(i, NST), a.status)))
           return false;
         tc::tc_fence_after();
-        const uint64_t v = desc_v + (uint32_t)(i % NST) * (2 * C::TILE / 16);
-        constexpr int STEP = 32 / C::EB;       // slots of an MMA: 8 columns of P
-        // P of 32 slots lies in the columns that held their S, hi then lo
-        auto p_at = [](int k, int p) { return F8 ? k * 32 + p * 8 : k / 2 * 32 + p * 16 + k % 2 * 8; };
+        const uint64_t v = desc_v + (F8 ? (uint32_t)(i & 1) * (C::H_TILE / 16) : (uint32_t)(i % NST) * (2 * C::TILE / 16));
+        // 16 slots an MMA: 8 columns of P, 16 rows of 128 bytes of V. P of 32 slots lies in the columns that held
+        // their S, bf16 hi then lo.
 #pragma unroll 1
-        for (int p = 1; p >= 0; --p)
+        for (int p = F8 ? 0 : 1; p >= 0; --p)
 #pragma unroll
-          for (int k = 0; k < kKeys / STEP; ++k)
-            tc::umma_tmem_a<F8>(t_o, tmem + i % kBuf * kKeys + p_at(k, p), v + k * (STEP * C::BW / 16), idesc_o,
-                                p < 1 || k > 0);
-        tc::umma_commit(&o_full);
-        tc::umma_commit(&v_empty[i % NST]);
+          for (int k = 0; k < kKeys / 16; ++k)
+            tc::umma_tmem_a(t_o + (i & 1) * kKeys, tmem + (i & 1) * kKeys + k / 2 * 32 + p * 16 + k % 2 * 8, v + k * (16 * 128 / 16), idesc_o,
+                            add || (!F8 && p < 1) || k > 0);
+        tc::umma_commit(&pv_done[i & 1]);
+        if (!F8) tc::umma_commit(&v_empty[i % NST]);
         return true;
       };
       bool ok = true;
@@ -175,9 +190,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         const Segment s = segment_at(a, s_first, unit, end);
         const int n = s.c1 - s.c0;
         ok = tc::mbar_wait(&q_full, seg & 1, a.status);
-        // S as far ahead as it has buffers; one that overwrites a P follows the P V that reads it, in order
-        for (int i = 0; i < n + kBuf && ok; ++i) {
-          if (i >= kBuf) ok = pv(it + i - kBuf);
+        // S two chunks ahead; it overwrites a P after the P V that reads it, in order
+        for (int i = 0; i < n + 2 && ok; ++i) {
+          if (i >= 2) ok = pv(it + i - 2, i >= 4);
           if (ok && i < n) ok = s_mma(it + i);
         }
         it += n;
@@ -193,9 +208,11 @@ __global__ void __launch_bounds__(kThreads, 1)
     bool ok = true;
     for (int unit = begin; unit < end && ok;) {
       const Segment s = segment_at(a, s_first, unit, end);
+      int vref = 0;
       for (int ch = s.c0; ch < s.c1 && ok; ++ch, ++it) {
         const int st = it % NST;
-        ok = __all_sync(0xffffffffu, tc::mbar_wait(&v_full[st], parity(it, NST), a.status));
+        ok = __all_sync(0xffffffffu, tc::mbar_wait(&v_full[st], parity(it, NST), a.status) &&
+                                         tc::mbar_wait(&f_empty[st], parity(it, NST) ^ 1, a.status));
         if (!ok) break;
         // a lane has slots 4 lane .. 4 lane + 3
         const uint8_t* from = sm + C::SCALE_OFF + st * 2 * kKeys + 4 * lane;
@@ -203,30 +220,43 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int slot = ch * kKeys + 4 * lane;
         const bool piece = s_pieces[st] >> (4 * lane >> min(c.page_shift, 7)) & 1;
         const int n = piece ? min(max(s.keys - slot, 0), 4) : 0;   // of them that there are
-        int vref = 0;
+        int vmax = 0;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int x = vb >> (8 * e) & 255;
-          if (e < n && x != 255) vref = max(vref, x);
+          if (e < n && x != 255) vmax = max(vmax, x);
         }
-        vref = __reduce_max_sync(0xffffffffu, vref);
+        vmax = __reduce_max_sync(0xffffffffu, vmax);
+        if (vref == 0 || vmax > vref + kVRoom) vref = vmax;
         float kf[4], vf[4];
+        uint32_t nan = 0;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const uint32_t k = kb >> (8 * e) & 255, v = vb >> (8 * e) & 255;
-          const int x = F8 ? (int)v - vref + kPShift + 127 : 127;
+          const int x = (int)v - vref + 127;
           kf[e] = e < n ? scale_value(k) : 1.f;
-          vf[e] = e >= n || x < 1 ? 0.f : v == 255 ? __uint_as_float(0x7fc00000u) : __uint_as_float((uint32_t)x << 23);
+          vf[e] = e >= n || v == 255 || x < 1 ? 0.f : __uint_as_float((uint32_t)x << 23);
+          nan |= (uint32_t)(e < n && v == 255) << e;
         }
         float* to = reinterpret_cast<float*>(sm + C::FACTOR_OFF) + st * 2 * kKeys + 4 * lane;
         *reinterpret_cast<float4*>(to) = make_float4(kf[0], kf[1], kf[2], kf[3]);
-        *reinterpret_cast<float4*>(to + kKeys) = make_float4(vf[0], vf[1], vf[2], vf[3]);
+        if (F8) *reinterpret_cast<float4*>(to + kKeys) = make_float4(vf[0], vf[1], vf[2], vf[3]);
         uint32_t valid = ((1u << n) - 1) << (4 * (lane & 7));       // eight lanes a word
+        nan <<= 4 * (lane & 7);
 #pragma unroll
-        for (int o = 1; o < 8; o <<= 1) valid |= __shfl_xor_sync(0xffffffffu, valid, o);
-        if ((lane & 7) == 0) s_valid[st][lane >> 3] = valid;
-        if (lane == 0) s_o[st] = F8 ? (1.f / (1 << kPShift)) * ex2((float)(vref - 127)) : 1.f;
-        if (n < 4) {                           // nothing of their V rows (page garbage, no copy) may reach the sums
+        for (int o = 1; o < 8; o <<= 1) {
+          valid |= __shfl_xor_sync(0xffffffffu, valid, o);
+          nan |= __shfl_xor_sync(0xffffffffu, nan, o);
+        }
+        if ((lane & 7) == 0) {
+          s_valid[st][lane >> 3] = valid;
+          s_nan[st][lane >> 3] = nan;
+        }
+        if (lane == 0) s_vref[st] = F8 ? vref : 127;
+        if (F8) {
+          __syncwarp();
+          if (lane == 0) tc::mbar_arrive(&v_empty[st]);             // (the scale bytes are read)
+        } else if (n < 4) {                    // nothing of their V rows (page garbage, no copy) may reach the sums
 #pragma unroll 1
           for (int e = n; e < 4; ++e) {
             uint8_t* v = sm + C::KV_OFF + (st * 2 + 1) * C::TILE + (4 * lane + e) * C::BW;
@@ -241,18 +271,20 @@ __global__ void __launch_bounds__(kThreads, 1)
       unit += s.c1 - s.c0;
     }
     __syncwarp();
-  } else if (warp < kSumWarp) {
+  } else if (warp < kConvWarp) {
     // ------------------------------------------------------------------------- softmax
     const int tid = threadIdx.x, grp = tid / kRows, r = tid % kRows, w4 = warp & 3;
     auto sync = [] { tc::named_barrier(1, kSoft); };
     const bool q_aligned = (reinterpret_cast<uintptr_t>(a.q) | (a.sq[0] | a.sq[1] | a.sq[2]) * 2) % 16 == 0;
-    int it0 = 0, seg = 0;
+    const bool o_aligned = (reinterpret_cast<uintptr_t>(a.out) | (a.so[0] | a.so[1] | a.so[2]) * 2) % 16 == 0;
+    const uint32_t lanes = (uint32_t)(w4 * 32) << 16, t_s = tmem + grp * kKeys + lanes;
+    int it0 = 0;
     bool failed = false;
-    for (int unit = begin; unit < end; ++seg) {
+    for (int unit = begin; unit < end;) {
       const Segment s = segment_at(a, s_first, unit, end);
       stage_queries<HD, kRows, F8, kSoft>(a, s, tid, q_aligned, sm, [&](int v, const Vec&, float qs, bool bad) {
         s_qs[v] = v < s.nq ? qs : 0.f;
-        s_bad[seg % kFlags][v] = bad;
+        s_bad[v] = bad;
       });
       const int t0 = s.qb * kRows / a.G;       // the block's first node
       for (int i = tid; i < (kRows + 1) * kWords; i += kSoft) {
@@ -266,17 +298,22 @@ __global__ void __launch_bounds__(kThreads, 1)
       const bool live = w4 * 32 < s.nq;        // (a warp's: its rows hold vectors)
       const uint32_t* const my_mask = s_mask[r < s.nq ? vector_of(a, s.h, s.qb, r).t - t0 : 0];
       const int n = s.c1 - s.c0;
+      float ref = -INFINITY, l = 0.f;
+      int vref = 0, last = -1;                 // V's reference in O, the group's last chunk
       for (int i = (it0 & 1) ^ grp; i < n && !failed; i += 2) {   // chunks it with it % 2 == grp
         const int it = it0 + i, st = it % NST;
-        const uint32_t t_s = tmem + it % kBuf * kKeys + ((uint32_t)(w4 * 32) << 16);
         const float* const kf = reinterpret_cast<const float*>(sm + C::FACTOR_OFF) + st * 2 * kKeys;
         bool ok = tc::mbar_wait(&f_full[st], parity(it, NST), a.status);
-        ok = ok && tc::mbar_wait(&s_full[it % kBuf], parity(it, kBuf), a.status);
+        ok = ok && tc::mbar_wait(&s_full[grp], parity(it, 2), a.status);
+        failed = !__all_sync(0xffffffffu, ok);   // (a warp gives up as one)
         tc::tc_fence_after();
-        // a chunk with slots of the tree, past the item's, or without a page: each row has its mask
+        // a chunk with slots of the tree, past the item's, without a page or with a V that is not finite: each row has
+        // its mask
         const int node0 = (s.c0 + i) * kKeys - s.len;
         const uint4 valid = *reinterpret_cast<const uint4*>(s_valid[st]);
-        const bool masked = node0 > -kKeys || (valid.x & valid.y & valid.z & valid.w) != ~0u;
+        const uint4 nan = *reinterpret_cast<const uint4*>(s_nan[st]);
+        const bool masked = node0 > -kKeys || (valid.x & valid.y & valid.z & valid.w) != ~0u ||
+                            (nan.x | nan.y | nan.z | nan.w) != 0u;
         auto word = [&](int w) -> uint32_t {   // slots 32 w .. 32 w + 31 that this row sees
           const int first = node0 + 32 * w;    // the tree's node in the first of them
           uint32_t x;
@@ -286,7 +323,6 @@ __global__ void __launch_bounds__(kThreads, 1)
           else x = __funnelshift_r(my_mask[first >> 5], first >> 5 < kWords - 1 ? my_mask[(first >> 5) + 1] : 0u, first & 31);
           return r < s.nq ? x & s_valid[st][w] : 0u;
         };
-        float mq = -INFINITY, sum = 0.f;
         // Code of its own for chunks with masks: as one, the compiler selects on every score, masked or not,
         // which took twice the time.
         auto softmax = [&](auto masked) {
@@ -327,9 +363,27 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
           }
           const float top = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
-          mq = top == -INFINITY ? -INFINITY : top * qs;
-          const float off = top == -INFINITY ? 0.f : mq;
-          // ---- probabilities, their sum, V's scale on them, P over S
+          // ---- the reference; the group's P V before is done (this S was issued after it)
+          float f = 1.f;
+          const float mq = top * qs;
+          if (top > -INFINITY && !(mq - ref <= kMargin)) {
+            f = ref == -INFINITY ? 1.f : ex2(ref - mq);   // (no reference: the sums are 0)
+            ref = mq;
+          }
+          l *= f;
+          if (F8 && last >= 0) f *= ex2((float)(vref - s_vref[st]));
+          if (last >= 0 && __any_sync(0xffffffffu, f != 1.f)) {
+#pragma unroll 1
+            for (int d = 0; d < HD; d += 16) {
+              float o[16];
+              tc::tmem_ld16(t_o + grp * kKeys + lanes + d, o);
+#pragma unroll
+              for (int e = 0; e < 16; ++e) o[e] *= f;
+              tc::tmem_st16(t_o + grp * kKeys + lanes + d, o);
+            }
+          }
+          const float off = ref == -INFINITY ? 0.f : ref - kUp;
+          // ---- probabilities, their sum, P over S
           uint64_t add = 0ull;
           const uint64_t qs2 = pair(qs, qs), off2 = pair(-off, -off);
 #pragma unroll 1
@@ -343,165 +397,168 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int h = 0; h < 2; ++h) {
               uint64_t t[8];
               scores(x[h], 2 * w + h, seen >> (16 * h), t);
-              constexpr int W = F8 ? 4 : 8;
-              uint32_t hi[W], lo[W];
+              uint32_t hi[8], lo[8];
 #pragma unroll
-              for (int e = 0; e < 16; e += 4) {
-                const ulonglong2 v = *reinterpret_cast<const ulonglong2*>(kf + kKeys + 32 * w + 16 * h + e);
-                float y[4];
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                  const float2 z = unpair(fma2(t[e / 2 + j], qs2, off2));
-                  const uint64_t p = pair(ex2(z.x), ex2(z.y));
-                  add = add2(add, p);
-                  const float2 u = unpair(mul2(p, j ? v.y : v.x));
-                  y[2 * j] = u.x;
-                  y[2 * j + 1] = u.y;
+              for (int e = 0; e < 8; ++e) {
+                const float2 z = unpair(fma2(t[e], qs2, off2));
+                float2 y = make_float2(ex2(z.x), ex2(z.y));
+                add = add2(add, pair(y.x, y.y));
+                if constexpr (masked) {        // a V that is not finite: NaN in the rows that see it
+                  const uint32_t m = (seen & s_nan[st][w]) >> (16 * h + 2 * e);
+                  if (m & 1) y.x = __uint_as_float(0x7fc00000u);
+                  if (m & 2) y.y = __uint_as_float(0x7fc00000u);
                 }
-                if constexpr (masked) {        // (0 * NaN of a V that this row does not see)
-#pragma unroll
-                  for (int j = 0; j < 4; ++j)
-                    if (!(seen >> (16 * h + e + j) & 1)) y[j] = 0.f;
-                }
-                if constexpr (F8) {            // four slots: a word of each plane
-                  const __half2 z0 = __floats2half2_rn(y[0], y[1]), z1 = __floats2half2_rn(y[2], y[3]);
-                  __half2 h0, h1;
-                  hi[e / 4] = f8x4(z0, z1);
-                  f8x4_half(hi[e / 4], &h0, &h1);
-                  lo[e / 4] = f8x4(__hsub2(z0, h0), __hsub2(z1, h1));
+                if constexpr (F8) {
+                  const __half2 p = __floats2half2_rn(y.x, y.y);
+                  hi[e] = *reinterpret_cast<const uint32_t*>(&p);
                 } else {
-#pragma unroll
-                  for (int j = 0; j < 2; ++j) {
-                    const __nv_bfloat162 z = __floats2bfloat162_rn(y[2 * j], y[2 * j + 1]);
-                    const __nv_bfloat162 d = __floats2bfloat162_rn(y[2 * j] - __low2float(z), y[2 * j + 1] - __high2float(z));
-                    hi[e / 2 + j] = *reinterpret_cast<const uint32_t*>(&z);
-                    lo[e / 2 + j] = *reinterpret_cast<const uint32_t*>(&d);
-                  }
+                  const __nv_bfloat162 p = __floats2bfloat162_rn(y.x, y.y);
+                  const __nv_bfloat162 d = __floats2bfloat162_rn(y.x - __low2float(p), y.y - __high2float(p));
+                  hi[e] = *reinterpret_cast<const uint32_t*>(&p);
+                  lo[e] = *reinterpret_cast<const uint32_t*>(&d);
                 }
               }
-              const uint32_t to = t_s + 32 * w + h * W;
+              const uint32_t to = t_s + 32 * w + h * 8;
               tc::tmem_st_nowait(to, hi);
-              tc::tmem_st_nowait(to + 2 * W, lo);
+              if (!F8) tc::tmem_st_nowait(to + 16, lo);
             }
           }
           const float2 two = unpair(add);
-          sum = two.x + two.y;
+          l += two.x + two.y;
           tc::tmem_wait_st();
         };
         if (live) {
           if (masked) softmax(std::true_type());
           else softmax(std::false_type());
         }
-        // ---- for the sums, which have taken this group's chunk before
-        ok = ok && tc::mbar_wait(&m_empty[grp], parity(it, 2) ^ 1, a.status);
-        failed = !__all_sync(0xffffffffu, ok);   // (a warp gives up as one)
-        s_m[grp][r] = mq;
-        s_l[grp][r] = sum;
-        if (r == 0) s_b[grp] = s_o[st];
+        vref = s_vref[st];
+        last = it;
         tc::tc_fence_before();
         tc::mbar_arrive(&p_full[grp]);
+        tc::mbar_arrive(&f_empty[st]);
       }
-      if (tc::named_barrier_or(1, kSoft, failed)) break;   // (and the queries and masks are free)
-      it0 += n;
-      unit += n;
-    }
-  } else {
-    // ------------------------------------------------------------------------- sums
-    const int tid = threadIdx.x - kSoft, half = tid / kRows, r = tid % kRows, w4 = warp & 3;
-    constexpr int OD = HD / 2;                 // dimensions of O of a thread
-    const uint32_t my_o = t_o + ((uint32_t)(w4 * 32) << 16) + half * OD;
-    const bool o_aligned = (reinterpret_cast<uintptr_t>(a.out) | (a.so[0] | a.so[1] | a.so[2]) * 2) % 16 == 0;
-    int it = 0, seg = 0;
-    bool failed = false;
-    for (int unit = begin; unit < end && !failed; ++seg) {
-      const Segment s = segment_at(a, s_first, unit, end);
-      const bool live = w4 * 32 < s.nq;
-      float ref = -INFINITY, l = 0.f;
-      uint64_t o[OD / 2];                      // in pairs
-#pragma unroll
-      for (int d = 0; d < OD / 2; ++d) o[d] = 0ull;
-      for (int ch = s.c0; ch < s.c1 && !failed; ++ch, ++it) {
-        const int g = it & 1;
-        bool ok = tc::mbar_wait(&p_full[g], parity(it, 2), a.status);
-        const float mq = s_m[g][r], add = s_l[g][r], scale = s_b[g];
-        tc::mbar_arrive(&m_empty[g]);
-        float f = 1.f;
-        if (mq > -INFINITY && !(mq - ref <= kMargin)) {
-          f = ref == -INFINITY ? 1.f : ex2(ref - mq);   // (no reference: the sums are 0)
-          ref = mq;
-        }
-        float b = mq == -INFINITY ? 0.f : ex2(mq - ref);
-        l = fmaf(l, f, add * b);
-        b *= scale;
-        if (__any_sync(0xffffffffu, f != 1.f)) {
-          const uint64_t ff = pair(f, f);
-#pragma unroll
-          for (int d = 0; d < OD / 2; ++d) o[d] = mul2(o[d], ff);
-        }
-        ok = ok && tc::mbar_wait(&o_full, it & 1, a.status);
-        failed = !__all_sync(0xffffffffu, ok);
-        tc::tc_fence_after();
-        if (live) {
-          const uint64_t bb = pair(b, b);
-#pragma unroll
-          for (int d = 0; d < OD; d += 32) {
-            uint32_t x[2][16];
-            tc::tmem_ld16_nowait(my_o + d, x[0]);
-            if (OD > 16) tc::tmem_ld16_nowait(my_o + d + 16, x[1]);
-            tc::tmem_wait_ld();
-#pragma unroll
-            for (int e = 0; e < 32; e += 2)
-              if (d + e < OD)
-                o[(d + e) / 2] = fma2(pair(x[e / 16][e % 16], x[e / 16][e % 16 + 1]), bb, o[(d + e) / 2]);
-          }
-        }
-        tc::tc_fence_before();
-        tc::mbar_arrive(&o_empty);
-      }
-      if (failed) break;
+      // ---- the groups' sums: each thread finishes half of its row's dimensions from both O
+      if (!failed && last >= 0)
+        failed = !__all_sync(0xffffffffu, tc::mbar_wait(&pv_done[grp], parity(last, 2), a.status));
+      s_m[grp][r] = ref;
+      s_l[grp][r] = l;
+      if (r == 0) s_v[grp] = vref;
+      tc::tc_fence_before();
+      if (tc::named_barrier_or(1, kSoft, failed)) break;
+      tc::tc_fence_after();
       const int rows = min(kRows, a.T * a.G - s.qb * kRows);
-      if (r < rows) {
+      const bool two = n > 1;                  // (else the other group has nothing)
+      {
+        const int own = it0 & 1;               // the group of the first chunk
+        const float m0 = s_m[own][r], m1 = two ? s_m[1 - own][r] : -INFINITY;
+        float m = fmaxf(m0, m1);
+        if (m == -INFINITY) m = 0.f;           // (nothing seen, or NaN scores alone)
+        const float f0 = m0 == -INFINITY ? 1.f : ex2(m0 - m), f1 = m1 == -INFINITY ? 1.f : ex2(m1 - m);
+        l = s_l[own][r] * f0 + (two ? s_l[1 - own][r] * f1 : 0.f);
         if (r >= s.nq || s.keys == 0) l = 0.f;
-        const float m = l == 0.f ? -INFINITY : ref == -INFINITY ? 0.f : ref;   // (NaN scores: no maximum)
-        if (l != 0.f && s_bad[seg % kFlags][r]) l = __uint_as_float(0x7fc00000u);
+        if (l != 0.f && s_bad[r]) l = __uint_as_float(0x7fc00000u);
+        m = l == 0.f ? -INFINITY : m - kUp;
+        const bool whole = s.c0 == 0 && s.c1 == s.units;
+        const float inv = l == 0.f ? 0.f : whole ? 1.f / l : 1.f;
+        const float g0 = f0 * (F8 ? ex2((float)(s_v[own] - 127)) : 1.f);
+        const float g1 = two ? f1 * (F8 ? ex2((float)(s_v[1 - own] - 127)) : 1.f) : 0.f;
         const Vec x = vector_of(a, s.h, s.qb, r);
-        if (s.c0 == 0 && s.c1 == s.units) {
-          const float inv = l == 0.f ? 0.f : 1.f / l;
-          if (half == 0) store_lse(a, s.b, x, m, l);
-          __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + s.b * a.so[0] + x.t * a.so[1] + x.h * a.so[2] +
-                               half * OD;
-#pragma unroll
-          for (int d = 0; d < OD; d += 8) {
-            uint32_t w[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float2 y = unpair(o[d / 2 + e]);
-              const __nv_bfloat162 z = __floats2bfloat162_rn(l == 0.f ? 0.f : y.x * inv, l == 0.f ? 0.f : y.y * inv);
-              w[e] = *reinterpret_cast<const uint32_t*>(&z);
-            }
-            if (o_aligned) {
-              *reinterpret_cast<uint4*>(out + d) = make_uint4(w[0], w[1], w[2], w[3]);
-            } else {
-#pragma unroll
-              for (int e = 0; e < 8; ++e)
-                out[d + e] = __ushort_as_bfloat16((unsigned short)(w[e / 2] >> (e % 2 * 16)));
-            }
-          }
-        } else {
-          const size_t part = (size_t)blockIdx.x * 2 + (s.c0 == 0);
-          if (half == 0) {
+        const size_t part = (size_t)blockIdx.x * 2 + (s.c0 == 0);
+        if (grp == 0 && r < rows) {
+          if (whole) {
+            store_lse(a, s.b, x, m, l);
+          } else {
             a.part_ml[(part * 2) * kRows + r] = m;
             a.part_ml[(part * 2 + 1) * kRows + r] = l;
           }
-          float4* out = reinterpret_cast<float4*>(a.part_o + (part * kRows + r) * HD + half * OD);
+        }
+        __nv_bfloat16* const out =
+            static_cast<__nv_bfloat16*>(a.out) + s.b * a.so[0] + x.t * a.so[1] + x.h * a.so[2];
+        float* const part_o = a.part_o + (part * kRows + r) * HD;
+#pragma unroll 1
+        for (int d = grp * (HD / 2); d < (grp + 1) * (HD / 2); d += 16) {
+          float o[16];
+          tc::tmem_ld16(t_o + own * kKeys + lanes + d, o);
 #pragma unroll
-          for (int d = 0; d < OD; d += 4) {
-            const float2 y = unpair(o[d / 2]), z = unpair(o[d / 2 + 1]);
-            out[d / 4] = l == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(y.x, y.y, z.x, z.y);
+          for (int e = 0; e < 16; ++e) o[e] *= g0;
+          if (two) {
+            float z[16];
+            tc::tmem_ld16(t_o + (1 - own) * kKeys + lanes + d, z);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[e] = fmaf(z[e], g1, o[e]);
+          }
+#pragma unroll
+          for (int e = 0; e < 16; ++e) o[e] = inv == 0.f ? 0.f : o[e] * inv;
+          if (r < rows) {
+            if (!whole) {
+#pragma unroll
+              for (int e = 0; e < 16; e += 4)
+                *reinterpret_cast<float4*>(part_o + d + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+            } else {
+              uint32_t w[8];
+#pragma unroll
+              for (int e = 0; e < 8; ++e) {
+                const __nv_bfloat162 z = __floats2bfloat162_rn(o[2 * e], o[2 * e + 1]);
+                w[e] = *reinterpret_cast<const uint32_t*>(&z);
+              }
+              if (o_aligned) {
+                *reinterpret_cast<uint4*>(out + d) = make_uint4(w[0], w[1], w[2], w[3]);
+                *reinterpret_cast<uint4*>(out + d + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+              } else {
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                  out[d + e] = __ushort_as_bfloat16((unsigned short)(w[e / 2] >> (e % 2 * 16)));
+              }
+            }
           }
         }
       }
-      unit += s.c1 - s.c0;
+      tc::tc_fence_before();
+      sync();                                  // queries, masks, sums and O are free
+      it0 += n;
+      unit += n;
+    }
+  } else if (F8) {
+    // ------------------------------------------------------------------------- V to fp16
+    // 16 codes at a time, exactly, with the rows' scales; rows that there are not become zeros
+    const int tid = threadIdx.x - kSoft;
+    bool ok = true;
+    for (int i = 0; i < end - begin && ok; ++i) {   // (a unit of the run is a chunk)
+      const int st = i % NST;
+      ok = tc::mbar_wait(&f_full[st], parity(i, NST), a.status) &&
+           tc::mbar_wait(&v_full[st], parity(i, NST), a.status) &&
+           tc::mbar_wait(&pv_done[i & 1], parity(i, 2) ^ 1, a.status);   // (chunk i - 2's: the buffer is free)
+      ok = __all_sync(0xffffffffu, ok);
+      const float* vf = reinterpret_cast<const float*>(sm + C::FACTOR_OFF) + (st * 2 + 1) * kKeys;
+      const uint8_t* from = sm + C::KV_OFF + (st * 2 + 1) * C::TILE;
+      uint8_t* to = sm + C::H_OFF + (i & 1) * C::H_TILE;
+#pragma unroll 4
+      for (int x = tid; x < kKeys * (HD / 16); x += kConv) {
+        const int row = x / (HD / 16), part = x % (HD / 16);
+        const uint4 u = *reinterpret_cast<const uint4*>(from + tc::row_offset(row, part, C::BW));
+        const float f = vf[row];
+        const __half2 f2 = __float2half2_rn(f);
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+        uint32_t h[8];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          __half2 p, q;
+          f8x4_half(f == 0.f ? 0u : w[e], &p, &q);
+          p = __hmul2(p, f2);
+          q = __hmul2(q, f2);
+          h[2 * e] = *reinterpret_cast<const uint32_t*>(&p);
+          h[2 * e + 1] = *reinterpret_cast<const uint32_t*>(&q);
+        }
+        // (the other half first in the second block of 64 dimensions: eight lanes' stores then meet no bank twice)
+        const int flip = part >> 2 & 1;
+        uint8_t* const block = to + part / 4 * C::H_BLOCK;
+        const uint4 lo = make_uint4(h[0], h[1], h[2], h[3]), hi = make_uint4(h[4], h[5], h[6], h[7]);
+        *reinterpret_cast<uint4*>(block + tc::row_offset(row, part % 4 * 2 + flip, 128)) = flip ? hi : lo;
+        *reinterpret_cast<uint4*>(block + tc::row_offset(row, part % 4 * 2 + 1 - flip, 128)) = flip ? lo : hi;
+      }
+      tc::fence_proxy_async();
+      tc::mbar_arrive(&h_full[i & 1]);
+      tc::mbar_arrive(&v_empty[st]);
     }
   }
   tc::tc_fence_before();

@@ -42,6 +42,8 @@ namespace tree {
 namespace {
 
 
+constexpr float kMargin = 8.f;                 // base 2: a sum's reference is raised past it
+constexpr int kPShift = 8;                     // e4m3 probabilities are stored times 2^kPShift <= 448
 constexpr int kSoft = kKeys;                   // softmax threads: one per slot of a chunk
 constexpr int kThreads = kSoft + 64;
 constexpr int kProducer = kSoft / 32, kIssuer = kProducer + 1;   // warps

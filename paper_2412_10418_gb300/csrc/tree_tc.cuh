@@ -9,9 +9,6 @@
 namespace cdsl {
 namespace tree {
 
-constexpr float kMargin = 8.f;                 // base 2: a sum's reference is raised past it
-constexpr int kPShift = 8;                     // e4m3 probabilities are stored times 2^kPShift <= 448
-
 // Position in a sequence of phases: index and parity of the `n`-th use of one of `of` barriers.
 __device__ __forceinline__ uint32_t parity(int n, int of) { return (n / of) & 1; }
 
