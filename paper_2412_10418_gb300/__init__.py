@@ -113,7 +113,7 @@ def _ptr(t) -> Optional[int]:
 
 
 def _check(code: int, ctx=None):
-    if code != 0:
+    if code:
         msg = lib().cdsl_last_error(ctx)
         raise CdslError(code, msg.decode() if msg else "")
 
@@ -318,20 +318,14 @@ def _bad(fn: str, why: str):
 
 def _ints(fn: str, name: str, t, shape, device, dtype=None):
     """A contiguous int32 (or `dtype`) tensor of this shape on this device: its pointer."""
-    if t.dtype is not (dtype or _types.i32) or t.shape != shape or not t.is_contiguous() or t.device != device:
-        _bad(fn, f"{name} must be a contiguous {dtype or _types.i32} tensor {tuple(shape)} on {device}, got "
-                 f"{t.dtype} {tuple(t.shape)} on {t.device}")
-    return t.data_ptr()
+    if t.dtype is (dtype or _types.i32) and t.shape == shape and t.is_contiguous() and t.device == device:
+        return t.data_ptr()
+    _bad(fn, f"{name} must be a contiguous {dtype or _types.i32} tensor {tuple(shape)} on {device}, got "
+             f"{t.dtype} {tuple(t.shape)} on {t.device}")
 
 
-def _optional(fn, name, t, shape, device, dtype=None):
-    return None if t is None else _ints(fn, name, t, shape, device, dtype)
-
-
-def _stream(stream, device):
-    if stream is None:
-        return _types.torch.cuda.current_stream(device).cuda_stream
-    return stream
+def _stream(device):
+    return _types.torch.cuda.current_stream(device).cuda_stream
 
 
 class KvCache:
@@ -372,19 +366,32 @@ class KvCache:
         return KvCache(self.pool, self.scale, page_table)
 
 
-def _rows(fn, cache, name, x, heads, T=None):
-    """[batch, T, heads, head_dim] with a contiguous last dimension: (type code, T)."""
+def _rows(fn, cache, names, x, y, heads):
+    """Two tensors [batch, T, heads, head_dim] of one type with a contiguous last dimension: (type code, T, both
+    tensors' strides)."""
     code = _types.values.get(x.dtype)
     s = x.shape
+    dev = cache.device
     if (code is None or len(s) != 4 or s[0] != cache.batch or s[2] != heads or s[3] != cache.head_dim
-            or (T is not None and s[1] != T) or x.device != cache.device or (x.stride(3) != 1)):
-        _bad(fn, f"{name} must be a float32 or bfloat16 tensor [{cache.batch}, {'T' if T is None else T}, {heads}, "
-                 f"{cache.head_dim}] on {cache.device} with a contiguous last dimension, got {x.dtype} {tuple(s)} "
-                 f"{tuple(x.stride())} on {x.device}")
-    return code, s[1]
+            or y.dtype is not x.dtype or y.shape != s or x.device != dev or y.device != dev):
+        _bad(fn, f"{names} must be float32 or bfloat16 tensors [{cache.batch}, T, {heads}, {cache.head_dim}] of one type "
+                 f"on {dev}, got {x.dtype} {tuple(s)} on {x.device} and {y.dtype} {tuple(y.shape)} on {y.device}")
+    if x.is_contiguous() and y.is_contiguous():   # (by size: a decoding loop repeats a few)
+        st = _contiguous.get(s)
+        if st is None:
+            if len(_contiguous) >= 256:
+                _contiguous.clear()
+            t = heads * cache.head_dim
+            st = _contiguous[s] = _Strides6(*(s[1] * t, t, cache.head_dim) * 2)
+        return code, s[1], st
+    sx, sy = x.stride(), y.stride()
+    if sx[3] != 1 or sy[3] != 1:
+        _bad(fn, f"{names} must have a contiguous last dimension, got strides {tuple(sx)} and {tuple(sy)}")
+    return code, s[1], _Strides6(*sx[:3], *sy[:3])
 
 
 _Strides6 = ctypes.c_int64 * 6
+_contiguous: dict = {}
 _Strides4 = ctypes.c_int64 * 4
 
 
@@ -392,16 +399,12 @@ def cdsl_kv_write(cache: KvCache, layer: int, k, v, start, count=None, status=No
     """Rows k, v [batch, T, kv_heads, head_dim] (float32 or bfloat16, any strides but the last) into slots
     start[b] + i of the layer, i < count[b] (None: all)."""
     fn = "cdsl_kv_write"
-    code, T = _rows(fn, cache, "k", k, cache.n_kv_heads)
-    if v.dtype is not k.dtype:
-        _bad(fn, "k and v must have one type")
-    _rows(fn, cache, "v", v, cache.n_kv_heads, T)
-    st = _Strides6(*k.stride()[:3], *v.stride()[:3])
+    code, T, st = _rows(fn, cache, "k and v", k, v, cache.n_kv_heads)
     _check(lib().cdsl_kv_write(cache._ref, layer, k.data_ptr(), v.data_ptr(), code, T, st,
                                _ints(fn, "start", start, cache._one, cache.device),
-                               _optional(fn, "count", count, cache._one, cache.device),
-                               _optional(fn, "status", status, (1,), cache.device),
-                               _stream(stream, cache.device)))
+                               None if count is None else _ints(fn, "count", count, cache._one, cache.device),
+                               None if status is None else _ints(fn, "status", status, (1,), cache.device),
+                               _stream(cache.device) if stream is None else stream))
 
 
 def cdsl_kv_read(cache: KvCache, layer: int, start, k, v, count=None, status=None, stream=None):
@@ -417,9 +420,9 @@ def cdsl_kv_read(cache: KvCache, layer: int, start, k, v, count=None, status=Non
                  f"{cache.n_kv_heads}, {cache.head_dim}] on {cache.device}")
     _check(lib().cdsl_kv_read(cache._ref, layer, s[0], k.data_ptr(), v.data_ptr(), code, s[2],
                               _ints(fn, "start", start, cache._one, cache.device),
-                              _optional(fn, "count", count, cache._one, cache.device),
-                              _optional(fn, "status", status, (1,), cache.device),
-                              _stream(stream, cache.device)))
+                              None if count is None else _ints(fn, "count", count, cache._one, cache.device),
+                              None if status is None else _ints(fn, "status", status, (1,), cache.device),
+                              _stream(cache.device) if stream is None else stream))
 
 
 def cdsl_kv_commit(cache: KvCache, lens, path, n_path, new_lens=None, status=None, stream=None):
@@ -432,9 +435,9 @@ def cdsl_kv_commit(cache: KvCache, lens, path, n_path, new_lens=None, status=Non
     _check(lib().cdsl_kv_commit(cache._ref, _ints(fn, "lens", lens, cache._one, cache.device),
                                 _ints(fn, "path", path, (cache.batch, T), cache.device),
                                 _ints(fn, "n_path", n_path, cache._one, cache.device), T,
-                                _optional(fn, "new_lens", new_lens, cache._one, cache.device),
-                                _optional(fn, "status", status, (1,), cache.device),
-                                _stream(stream, cache.device)))
+                                None if new_lens is None else _ints(fn, "new_lens", new_lens, cache._one, cache.device),
+                                None if status is None else _ints(fn, "status", status, (1,), cache.device),
+                                _stream(cache.device) if stream is None else stream))
 
 
 def cdsl_tree_mask(parents: Sequence[int]):
@@ -462,23 +465,17 @@ def cdsl_tree_attention(cache: KvCache, layer: int, q, lens, mask, out, workspac
     strides but the last), over its lens[b] cached slots and the tree's own after them, by the ancestor bits of
     mask [batch, T, (T + 31) // 32]."""
     fn = "cdsl_tree_attention"
-    if q.dim() != 4:
-        _bad(fn, "q must be [batch, T, n_heads, head_dim]")
-    H = q.shape[2]
-    code, T = _rows(fn, cache, "q", q, H)
-    if out.dtype is not q.dtype:
-        _bad(fn, "out must have q's type")
-    _rows(fn, cache, "out", out, H, T)
+    H = q.shape[2] if q.dim() == 4 else 0
+    code, T, st = _rows(fn, cache, "q and out", q, out, H)
     dev = cache.device
     if workspace.dtype is not _types.u8 or not workspace.is_contiguous() or workspace.device != dev:
         _bad(fn, f"workspace must be a contiguous uint8 tensor on {dev}")
-    st = _Strides6(*q.stride()[:3], *out.stride()[:3])
     _check(lib().cdsl_tree_attention(
         cache._ref, layer, q.data_ptr(), code, H, T, st, _ints(fn, "lens", lens, cache._one, dev),
-        _optional(fn, "nodes", nodes, cache._one, dev),
+        None if nodes is None else _ints(fn, "nodes", nodes, cache._one, dev),
         _ints(fn, "mask", mask, (cache.batch, T, (T + 31) // 32), dev), scale, max_len, out.data_ptr(),
-        _optional(fn, "lse", lse, (cache.batch, T, H), dev, _types.f32), workspace.data_ptr(), workspace.numel(),
-        _optional(fn, "status", status, (1,), dev), _stream(stream, dev)))
+        None if lse is None else _ints(fn, "lse", lse, (cache.batch, T, H), dev, _types.f32), workspace.data_ptr(), workspace.numel(),
+        None if status is None else _ints(fn, "status", status, (1,), dev), _stream(dev) if stream is None else stream))
 
 
 def cdsl_tree_verify(logits, tokens, parents, u, u_last, path, n_path, emitted, *, draft_logits=None,
@@ -504,10 +501,10 @@ def cdsl_tree_verify(logits, tokens, parents, u, u_last, path, n_path, emitted, 
     _check(lib().cdsl_tree_verify(
         B, T, V, logits.data_ptr(), _ptr(draft_logits), code, _Strides4(st[0], st[1], sd[0], sd[1]),
         _ints(fn, "tokens", tokens, all_, dev), _ints(fn, "parents", parents, all_, dev),
-        _optional(fn, "nodes", nodes, one, dev), _ints(fn, "u", u, all_, dev, ty.f32),
+        None if nodes is None else _ints(fn, "nodes", nodes, one, dev), _ints(fn, "u", u, all_, dev, ty.f32),
         _ints(fn, "u_last", u_last, one, dev, ty.f32), temperature, _ints(fn, "path", path, all_, dev),
         _ints(fn, "n_path", n_path, one, dev), _ints(fn, "emitted", emitted, all_, dev),
-        _optional(fn, "status", status, (1,), dev), _stream(stream, dev)))
+        None if status is None else _ints(fn, "status", status, (1,), dev), _stream(dev) if stream is None else stream))
 
 
 # ------------------------------------------------------------------------------ Engine

@@ -52,10 +52,7 @@ __global__ void __launch_bounds__(kThreads) k_tree_simt(TreeArgs a) {
   pdl_wait();
   pdl_launch_dependents();
   build_plan(a, s_first);
-  if (blockIdx.x == 0) {
-    check_lens(a);
-    for (int b = tid; b <= c.batch; b += kThreads) a.plan[b] = s_first[b];
-  }
+  if (blockIdx.x == 0) check_lens(a);
   const int total = s_first[c.batch], runs = runs_of(a, total);
   if ((int)blockIdx.x >= runs) return;
   const int end = run_begin(blockIdx.x + 1, total, runs);
@@ -199,8 +196,10 @@ __global__ void __launch_bounds__(kThreads) k_tree_simt(TreeArgs a) {
 }
 
 // Joins the parts of the items that several runs share: a warp per query vector, its lanes along
-// head_dim. Grid: (items, blocks of kCombine vectors). Bound by the parts' bytes in L2.
-constexpr int kCombine = 4;
+// head_dim. Grid: (items, blocks of kCombine vectors). It is scheduled beside the pass and works out the item's runs
+// from the lengths before it waits for them; then a vector's (m, l) and its first parts' values are loaded
+// together. Bound by that one round trip to L2, and on large passes by the parts' bytes.
+constexpr int kCombine = 4, kAhead = 8;
 template <typename T, int HD>
 __global__ void __launch_bounds__(32 * kCombine) k_tree_combine(TreeArgs a) {
   constexpr int DPL = HD / 32;
@@ -208,14 +207,35 @@ __global__ void __launch_bounds__(32 * kCombine) k_tree_combine(TreeArgs a) {
   const int item = blockIdx.x;
   const int qb = item % a.QB, h = item / a.QB % a.c.kvh, b = item / a.QB / a.c.kvh;
   const int v = blockIdx.y * kCombine + (threadIdx.x >> 5);
-  pdl_wait();
   const int n = nodes_of(a, b), live = live_blocks(a, n);
-  if (qb >= live || v >= min(a.NQ, a.T * a.G - qb * a.NQ)) return;
-  const int u = item_units(len_of(a, b) + n), total = a.plan[a.c.batch];
-  const int s = a.plan[b] + h * (live * u + a.QB - live) + qb * u;
+  if (qb >= live || v >= min(a.NQ, a.T * a.G - qb * a.NQ)) return pdl_wait();
+  int before = 0, total = 0;                   // units of the sequences before, and of all
+  for (int x = lane; x < a.c.batch; x += 32) {
+    const int w = units_of(a, x);
+    total += w;
+    if (x < b) before += w;
+  }
+  before = __reduce_add_sync(0xffffffffu, before);
+  total = __reduce_add_sync(0xffffffffu, total);
+  const int u = item_units(len_of(a, b) + n);
+  const int s = before + h * (live * u + a.QB - live) + qb * u;
   const int runs = runs_of(a, total), r0 = run_of(s, total, runs), r1 = run_of(s + u - 1, total, runs);
+  pdl_wait();                                  // (no block ends before the pass has)
   if (r0 == r1) return;                        // whole: written
   auto slot = [&](int r) { return (size_t)r * 2 + (r == r0); };
+  struct Values { float x[DPL]; };
+  auto load = [&](int r) {
+    Values z;
+    const float* p = a.part_o + (slot(r) * a.NQ + v) * HD + lane * DPL;
+    if constexpr (DPL == 4) {
+      const float4 t = *reinterpret_cast<const float4*>(p);
+      z.x[0] = t.x; z.x[1] = t.y; z.x[2] = t.z; z.x[3] = t.w;
+    } else {
+      const float2 t = *reinterpret_cast<const float2*>(p);
+      z.x[0] = t.x; z.x[1] = t.y;
+    }
+    return z;
+  };
   float M = -INFINITY, L = 0.f, acc[DPL];
 #pragma unroll
   for (int i = 0; i < DPL; ++i) acc[i] = 0.f;
@@ -226,26 +246,27 @@ __global__ void __launch_bounds__(32 * kCombine) k_tree_combine(TreeArgs a) {
       m = a.part_ml[slot(rb + lane) * 2 * a.NQ + v];
       l = a.part_ml[(slot(rb + lane) * 2 + 1) * a.NQ + v];
     }
+    Values z[kAhead];
+#pragma unroll
+    for (int e = 0; e < kAhead; ++e)
+      if (e < cnt) z[e] = load(rb + e);
     const float Mn = fmaxf(M, warp_max(m));
     const float keep = M == -INFINITY ? 0.f : exp2f(M - Mn);
     const float w = m == -INFINITY ? (l == 0.f ? 0.f : 1.f) : exp2f(m - Mn);   // (l NaN: kept)
     L = L * keep + warp_sum(w * l);
 #pragma unroll
     for (int i = 0; i < DPL; ++i) acc[i] *= keep;
-    for (int r = 0; r < cnt; r += 8) {
-      float x[8][DPL];
+    for (int r = 0; r < cnt; r += kAhead) {
+      if (r > 0)
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
+        for (int e = 0; e < kAhead; ++e)
+          if (r + e < cnt) z[e] = load(rb + r + e);
 #pragma unroll
-        for (int i = 0; i < DPL; ++i)
-          x[e][i] = r + e < cnt
-                        ? a.part_o[(slot(rb + r + e) * a.NQ + v) * HD + lane * DPL + i] : 0.f;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
+      for (int e = 0; e < kAhead; ++e) {
         const float wr = __shfl_sync(0xffffffffu, w, (r + e) & 31);
         if (r + e < cnt)
 #pragma unroll
-          for (int i = 0; i < DPL; ++i) acc[i] = fmaf(wr, x[e][i], acc[i]);
+          for (int i = 0; i < DPL; ++i) acc[i] = fmaf(wr, z[e].x[i], acc[i]);
       }
     }
     M = Mn;
@@ -259,7 +280,7 @@ __global__ void __launch_bounds__(32 * kCombine) k_tree_combine(TreeArgs a) {
 // Sizes of a pass, the same at every length: runs and workspace.
 struct Sizes {
   int NQ, QB, blocks;
-  size_t ml_off, o_off, bytes;
+  size_t o_off, bytes;
 };
 constexpr int kSimtPerSM = 4;                  // resident k_tree_simt blocks per SM
 
@@ -270,8 +291,7 @@ void sizes_of(const Cache& c, bool tc, int H, int T, Sizes* z) {
   z->blocks = kPlanSMs * (!tc ? kSimtPerSM : z->NQ == kRowsBlock ? 1 : tc_blocks_per_sm(c, z->NQ));
   const size_t slots = (size_t)z->blocks * 2 * z->NQ;
   auto up = [](size_t n) { return (n + 255) / 256 * 256; };
-  z->ml_off = up((c.batch + 1) * sizeof(int32_t));
-  z->o_off = up(z->ml_off + slots * 2 * sizeof(float));
+  z->o_off = up(slots * 2 * sizeof(float));
   z->bytes = up(z->o_off + slots * c.hd * sizeof(float));
 }
 
@@ -377,8 +397,7 @@ extern "C" int32_t cdsl_tree_attention(const cdsl_kv_cache* cache, int32_t layer
   a.max_len = max_len;
   a.blocks = (int)std::min<long long>(z.blocks, units);
   char* ws = static_cast<char*>(d_workspace);
-  a.plan = reinterpret_cast<int32_t*>(ws);
-  a.part_ml = reinterpret_cast<float*>(ws + z.ml_off);
+  a.part_ml = reinterpret_cast<float*>(ws);
   a.part_o = reinterpret_cast<float*>(ws + z.o_off);
   a.status = d_status;
   const bool split = chunks > 1;               // one chunk: every item is whole

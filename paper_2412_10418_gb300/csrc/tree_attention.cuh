@@ -33,8 +33,7 @@ struct TreeArgs {
   float scale;                                 // softmax scale * log2(e): scores in base 2
   int max_len;
   int blocks;                                  // launched: runs at most
-  int32_t* plan;                               // workspace: [batch + 1] first unit of each sequence
-  float* part_ml;                              // [blocks][2][2][NQ]: m, l
+  float* part_ml;                              // workspace: [blocks][2][2][NQ]: m, l
   float* part_o;                               // [blocks][2][NQ][hd]
   int32_t* status;
 };
@@ -62,17 +61,18 @@ __device__ __forceinline__ int live_blocks(const TreeArgs& a, int nodes) {
   return (nodes * a.G + a.NQ - 1) / a.NQ;
 }
 
+__device__ __forceinline__ int units_of(const TreeArgs& a, int b) {
+  const int n = nodes_of(a, b), live = live_blocks(a, n);
+  return a.c.kvh * (live * item_units(len_of(a, b) + n) + (a.QB - live));
+}
+
 // first[b], b <= batch: the units before sequence b's. The whole block calls; first is in shared memory.
 __device__ __forceinline__ void build_plan(const TreeArgs& a, int* first) {
   if (threadIdx.x < 32) {
     int sum = 0;
     for (int b0 = 0; b0 < a.c.batch; b0 += 32) {
       const int b = b0 + (int)threadIdx.x;
-      int v = 0;
-      if (b < a.c.batch) {
-        const int n = nodes_of(a, b), live = live_blocks(a, n);
-        v = a.c.kvh * (live * item_units(len_of(a, b) + n) + (a.QB - live));
-      }
+      const int v = b < a.c.batch ? units_of(a, b) : 0;
       int s = v;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {

@@ -120,10 +120,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   build_plan(a, s_first);                      // (ends in a block barrier)
   tc::tc_fence_after();
   const uint32_t tmem = s_tmem;
-  if (blockIdx.x == 0) {
-    check_lens(a);
-    for (int b = threadIdx.x; b <= c.batch; b += kThreads) a.plan[b] = s_first[b];
-  }
+  if (blockIdx.x == 0) check_lens(a);
   const int total = s_first[c.batch], runs = runs_of(a, total);
   const int begin = (int)blockIdx.x < runs ? run_begin(blockIdx.x, total, runs) : 0;
   const int end = (int)blockIdx.x < runs ? run_begin(blockIdx.x + 1, total, runs) : 0;

@@ -128,10 +128,7 @@ __global__ void __launch_bounds__(kThreads, Cfg<HD, NQ, F8>::CTAS)
   tc::tc_fence_after();
   const uint32_t tmem = s_tmem, t_o = tmem + 2 * NQ;
   const uint32_t sbase = tc::smem_u32(sm);
-  if (blockIdx.x == 0) {
-    check_lens(a);
-    for (int b = threadIdx.x; b <= c.batch; b += kThreads) a.plan[b] = s_first[b];
-  }
+  if (blockIdx.x == 0) check_lens(a);
   const int total = s_first[c.batch], runs = runs_of(a, total);
   const int begin = (int)blockIdx.x < runs ? run_begin(blockIdx.x, total, runs) : 0;
   const int end = (int)blockIdx.x < runs ? run_begin(blockIdx.x + 1, total, runs) : 0;

@@ -83,28 +83,34 @@ __device__ __forceinline__ void stage_queries(const TreeArgs& a, const Segment& 
   constexpr int QE = HD / 8;                   // values per thread
   constexpr int KROW = HD * (F8 ? 1 : 2), BW = KROW < 128 ? KROW : 128;
   constexpr uint32_t PLANE = NQ * KROW;
-#pragma unroll 1
-  for (int v0 = 0; v0 < NQ; v0 += NT / 8) {
-    const int v = v0 + tid / 8, part = tid % 8;
-    const Vec x = vector_of(a, s.h, s.qb, v);
-    uint32_t w[QE / 2];
+  constexpr int ROUNDS = NQ * 8 / NT;
+  uint32_t raw[ROUNDS][QE / 2];                // (all loads first: their latency once)
 #pragma unroll
-    for (int i = 0; i < QE / 2; ++i) w[i] = 0u;
+  for (int n = 0; n < ROUNDS; ++n) {
+    const int v = n * (NT / 8) + tid / 8;
+#pragma unroll
+    for (int i = 0; i < QE / 2; ++i) raw[n][i] = 0u;
     if (v < s.nq) {
+      const Vec x = vector_of(a, s.h, s.qb, v);
       const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(a.q) + s.b * a.sq[0] + x.t * a.sq[1] +
-                               x.h * a.sq[2] + part * QE;
+                               x.h * a.sq[2] + tid % 8 * QE;
       if (q_aligned) {
 #pragma unroll
         for (int i = 0; i < QE / 8; ++i) {
           const uint4 u = *reinterpret_cast<const uint4*>(q + 8 * i);
-          w[4 * i] = u.x; w[4 * i + 1] = u.y; w[4 * i + 2] = u.z; w[4 * i + 3] = u.w;
+          raw[n][4 * i] = u.x; raw[n][4 * i + 1] = u.y; raw[n][4 * i + 2] = u.z; raw[n][4 * i + 3] = u.w;
         }
       } else {
 #pragma unroll
         for (int i = 0; i < QE; ++i)
-          w[i / 2] |= (uint32_t)__bfloat16_as_ushort(q[i]) << (i % 2 * 16);
+          raw[n][i / 2] |= (uint32_t)__bfloat16_as_ushort(q[i]) << (i % 2 * 16);
       }
     }
+  }
+#pragma unroll
+  for (int n = 0; n < ROUNDS; ++n) {
+    const int v = n * (NT / 8) + tid / 8, part = tid % 8;
+    const uint32_t (&w)[QE / 2] = raw[n];
     uint32_t top = 0;                      // largest |x|, as bf16 bits
 #pragma unroll
     for (int i = 0; i < QE / 2; ++i) top = max(top, max(w[i] & 0x7fffu, w[i] >> 16 & 0x7fffu));
@@ -151,7 +157,7 @@ __device__ __forceinline__ void stage_queries(const TreeArgs& a, const Segment& 
             bad ? make_uint4(0u, 0u, 0u, 0u) : make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
       }
     }
-    if (part == 0) put(v, x, qs, v < s.nq && bad);
+    if (part == 0) put(v, vector_of(a, s.h, s.qb, v), qs, v < s.nq && bad);
   }
 }
 

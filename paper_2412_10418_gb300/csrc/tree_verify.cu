@@ -1,13 +1,20 @@
 // tree_verify.cu -- cdsl_tree_verify: which drafted path the target takes, and the next token.
 //
-// A block per sequence walks its tree. Only the rows on the way are read: at a node the row's
-// maximum, the sum of its weights, the children's decisions, and where none is taken the token at
-// a position of the weights' running sum. Weights are summed as whole numbers, so that neither the
-// decisions nor the token depend on the order of any sum.
+// Only the rows on the way are read. At a node: the row's maximum, the sum of its weights, the children's
+// decisions, and where none is taken the token at a position of the weights' running sum. Weights are summed as
+// whole numbers, so that neither the decisions nor the token depend on the order of any sum.
+//
+// k_tree_walk: a cluster of up to eight blocks walks a sequence's tree, each with its part of the row in registers
+// (J values a thread). A reduction is one cluster barrier: each warp's value goes to every block's shared
+// memory, where each warp reduces all of them for itself; the children's decisions are then made alike by every
+// thread. Bound by latency: a level is a row's loads, two such reductions and the decisions. Rows of more than
+// the cluster's registers hold (163,840 tokens) take k_tree_verify, a block per sequence that reads a row
+// several times.
 #include <cuda.h>
 
 #include <algorithm>
 
+#include "tc_ptx.cuh"
 #include "tree_host.h"
 
 namespace cdsl {
@@ -239,6 +246,329 @@ __global__ void __launch_bounds__(kThreads) k_tree_verify(VerifyArgs a) {
   }
 }
 
+
+// ------------------------------------------------------------------------------------- the walk in registers
+constexpr int kWalk = 512;             // threads of a block
+constexpr int kWalkWarps = kWalk / 32;
+constexpr int kMaxCluster = 8;
+constexpr int kPrefetch = 4;           // children whose rows are fetched into L2 ahead
+
+// Values of all warps of the cluster, two at a time, two reductions' in turn.
+struct Slots {
+  u64 v[2][2][kMaxCluster * kWalkWarps];
+};
+
+__device__ __forceinline__ u64 shfl_xor(u64 x, int o) { return __shfl_xor_sync(0xffffffffu, x, o); }
+
+// a and b of every thread of the cluster, by op; C: blocks. One cluster barrier. Afterwards s.v[turn][.] holds
+// the warps' values, block by block.
+template <typename Op>
+__device__ __forceinline__ void reduce_cluster(u64& a, u64& b, bool both, Op op, Slots& s, int& turn, int C, int rank) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    a = op(a, shfl_xor(a, o));
+    if (both) b = op(b, shfl_xor(b, o));
+  }
+  turn ^= 1;
+  const int at = rank * kWalkWarps + warp;
+  if (C > 1) {
+    if (lane < C) {
+      const uint32_t to = tc::map_cluster_rank(tc::smem_u32(&s.v[turn][0][at]), lane);
+      asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(to), "l"(a) : "memory");
+      if (both)
+        asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(to + (uint32_t)sizeof(s.v[0][0])), "l"(b) : "memory");
+    }
+    tc::cluster_arrive();
+    tc::cluster_wait();
+  } else {
+    if (lane == 0) {
+      s.v[turn][0][at] = a;
+      if (both) s.v[turn][1][at] = b;
+    }
+    __syncthreads();
+  }
+  a = b = 0;                           // (neutral to both operations: keys and sums are not negative)
+  for (int i = lane; i < C * kWalkWarps; i += 32) {
+    a = op(a, s.v[turn][0][i]);
+    if (both) b = op(b, s.v[turn][1][i]);
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    a = op(a, shfl_xor(a, o));
+    if (both) b = op(b, shfl_xor(b, o));
+  }
+}
+
+template <typename T, int J>
+__global__ void __launch_bounds__(kWalk) k_tree_walk(VerifyArgs a) {
+  __shared__ Slots s_slots;
+  __shared__ int s_tok[kMaxT], s_par[kMaxT];
+  __shared__ float s_u[kMaxT];
+  __shared__ float s_lx[kMaxT], s_qx[kMaxT];   // a node's children's logits, the target's and the draft's
+  __shared__ float s_inv[kMaxT];
+  __shared__ int s_out[kMaxT];
+  __shared__ u64 s_sum[J][kWalkWarps];         // a block's weights by 32 tokens, in their order
+  __shared__ int s_at;
+  __shared__ u64 s_before;
+  const int C = (int)gridDim.x, rank = (int)blockIdx.x, b = blockIdx.y, tid = threadIdx.x, V = a.V;
+  const int lane = tid & 31, warp = tid >> 5;
+  pdl_wait();
+  pdl_launch_dependents();
+  const int n = a.nodes ? min(max(a.nodes[b], 0), a.T) : a.T;
+  for (int i = tid; i < a.T; i += kWalk) {
+    s_tok[i] = a.tokens[(size_t)b * a.T + i];
+    s_par[i] = a.parents[(size_t)b * a.T + i];
+    s_u[i] = a.u[(size_t)b * a.T + i];
+    if (rank == 0) a.path[(size_t)b * a.T + i] = a.emitted[(size_t)b * a.T + i] = -1;
+  }
+  const float u_last = a.u_last[b];
+  const bool greedy = a.inv_t == 0.f, drafts = a.draft != nullptr;
+  const int size = (V + C - 1) / C, base = rank * size, top = min(V, base + size);   // this block's tokens
+  const auto sum = [](u64 x, u64 y) { return x + y; };
+  const auto most = [](u64 x, u64 y) { return x > y ? x : y; };
+  int turn = 0;
+  __syncthreads();
+  if (n == 0) {
+    if (rank == 0 && tid == 0) a.n_path[b] = 0;
+    return;
+  }
+  const T* const rows = static_cast<const T*>(a.logits) + b * a.sl[0];
+  const T* const draft_rows = static_cast<const T*>(a.draft) + b * a.sd[0];
+  auto weight = [&](float l, float m) { return expf(__fmul_rn(__fsub_rn(l, m), a.inv_t)); };
+  auto inverse = [](u64 Z) { return __fdiv_rn(1.f, __fmul_rn(__ull2float_rn(Z), 1.f / kTwo31)); };
+  int cur = 0, m = 0, last = -1;
+  for (;;) {
+    if (rank == 0 && tid == 0) {
+      a.path[(size_t)b * a.T + m] = cur;
+      if (m) a.emitted[(size_t)b * a.T + m - 1] = s_tok[cur];
+    }
+    ++m;
+    // ---- the row, the children's logits, and the likely next rows into L2
+    float l[J], q[J];
+    const T* const row = rows + cur * a.sl[1];
+    const T* const draft_row = draft_rows + cur * a.sd[1];
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      const int v = base + j * kWalk + tid;
+      l[j] = v < top ? to_f32<T>(row[v]) : -INFINITY;
+    }
+    if (drafts)
+#pragma unroll
+      for (int j = 0; j < J; ++j) {
+        const int v = base + j * kWalk + tid;
+        q[j] = v < top ? to_f32<T>(draft_row[v]) : -INFINITY;
+      }
+    if (tid < n && tid > cur && s_par[tid] == cur && (unsigned)s_tok[tid] < (unsigned)V) {
+      s_lx[tid] = to_f32<T>(row[s_tok[tid]]);
+      if (drafts) s_qx[tid] = to_f32<T>(draft_row[s_tok[tid]]);
+    }
+    for (int i = cur + 1, ahead = 0; i < n && ahead < kPrefetch; ++i) {
+      if (s_par[i] != cur) continue;
+      ++ahead;
+      constexpr int kLine = 128 / sizeof(T);
+      for (int v = base + tid * kLine; v < top; v += kWalk * kLine) {
+        asm volatile("prefetch.global.L2 [%0];" ::"l"(rows + i * a.sl[1] + v));
+        if (drafts) asm volatile("prefetch.global.L2 [%0];" ::"l"(draft_rows + i * a.sd[1] + v));
+      }
+    }
+    // ---- maxima (all ones: a row that cannot be drawn from)
+    u64 best = 0, best_q = 0;
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      const int v = base + j * kWalk + tid;
+      if (!(l[j] < INFINITY)) best = ~0ull;
+      else if (l[j] > -INFINITY) best = most(best, argmax_key(l[j] + 0.f, v));
+      if (drafts) {
+        if (!(q[j] < INFINITY)) best_q = ~0ull;
+        else if (q[j] > -INFINITY) best_q = most(best_q, argmax_key(q[j], v));
+      }
+    }
+    reduce_cluster(best, best_q, drafts, most, s_slots, turn, C, rank);
+    if (best == 0 || best == ~0ull || (drafts && (best_q == 0 || best_q == ~0ull))) {
+      if (rank == 0 && tid == 0) set_status(a.status, CDSL_ENONFINITE);
+      break;
+    }
+    int next = -1;
+    if (greedy) {
+      last = argmax_key_index(best);
+      for (int i = cur + 1; i < n && next < 0; ++i) {
+        if (s_par[i] != cur) continue;
+        if (s_tok[i] == last) next = i;
+        else if ((unsigned)s_tok[i] >= (unsigned)V && tid == 0) set_status(a.status, CDSL_ERANGE);
+      }
+      if (next < 0) break;
+      cur = next;
+      __syncthreads();                 // (s_lx of the next node)
+      continue;
+    }
+    // ---- weights, as whole numbers and their sums
+    const float lm = key_value(best), qm = key_value(best_q);
+    uint32_t W[J];
+    u64 Z = 0, Zq = 0;
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      l[j] = weight(l[j], lm);
+      W[j] = units_of(l[j]);
+      Z += W[j];
+      if (drafts) {
+        q[j] = weight(q[j], qm);
+        Zq += units_of(q[j]);
+      }
+    }
+    reduce_cluster(Z, Zq, drafts, sum, s_slots, turn, C, rank);
+    float inv0 = 0.f, invq = 0.f;
+    if (drafts) {                      // the distributions p and q
+      inv0 = inverse(Z);
+      invq = inverse(Zq);
+#pragma unroll
+      for (int j = 0; j < J; ++j) {
+        l[j] = __fmul_rn(l[j], inv0);
+        q[j] = __fmul_rn(q[j], invq);
+      }
+    }
+    int rejected = 0;
+    bool changed = false;              // the weights are no longer those of the last reduction
+    for (int i = cur + 1; i < n && next < 0; ++i) {
+      if (s_par[i] != cur) continue;
+      const int x = s_tok[i];
+      if ((unsigned)x >= (unsigned)V) {
+        if (rank == 0 && tid == 0) set_status(a.status, CDSL_ERANGE);
+        continue;
+      }
+      if (!drafts) {
+        uint32_t w = units_of(weight(s_lx[i], lm));
+        for (int r = 0; r < rejected; ++r)
+          if (s_out[r] == x) w = 0;
+        if (share_of(s_u[i], Z) < w) { next = i; break; }
+        Z -= w;
+        __syncthreads();
+        if (tid == 0) s_out[rejected] = x;
+        ++rejected;
+        __syncthreads();
+        changed = true;
+        const int at = x - base;       // it leaves the distribution
+        if (x >= base && x < top && at % kWalk == tid)
+#pragma unroll
+          for (int j = 0; j < J; ++j)
+            if (j == at / kWalk) W[j] = 0;
+      } else {
+        const float qx = __fmul_rn(weight(s_qx[i], qm), invq);
+        float px = __fmul_rn(weight(s_lx[i], lm), inv0);
+        for (int r = 0; r < rejected; ++r) px = __fmul_rn(fmaxf(__fsub_rn(px, qx), 0.f), s_inv[r]);
+        if (__fmul_rn(s_u[i], qx) < px) { next = i; break; }
+        // the rest of p: it stays p where that is nothing
+        u64 zr = 0, none = 0;
+#pragma unroll
+        for (int j = 0; j < J; ++j) zr += units_of(fmaxf(__fsub_rn(l[j], q[j]), 0.f));
+        reduce_cluster(zr, none, false, sum, s_slots, turn, C, rank);
+        if (zr) {
+          const float inv = inverse(zr);
+          Z = zr;
+          changed = false;
+#pragma unroll
+          for (int j = 0; j < J; ++j) {
+            const float r = fmaxf(__fsub_rn(l[j], q[j]), 0.f);
+            W[j] = units_of(r);
+            l[j] = __fmul_rn(r, inv);
+          }
+          if (tid == 0) s_inv[rejected] = inv;
+          ++rejected;
+          __syncthreads();
+        } else {
+          changed = true;
+        }
+      }
+    }
+    if (next >= 0) {
+      cur = next;
+      __syncthreads();                 // (s_lx, s_out and s_inv of the next node)
+      continue;
+    }
+    // ---- the first token whose running sum passes the draw: the block, the 32 tokens, the token
+    if (changed) {
+      u64 z = 0, none = 0;
+#pragma unroll
+      for (int j = 0; j < J; ++j) z += W[j];
+      reduce_cluster(z, none, false, sum, s_slots, turn, C, rank);
+    }
+    u64 want = share_of(u_last, Z), mine = 0;
+    for (int i = 0; i < rank * kWalkWarps; ++i) want -= s_slots.v[turn][0][i];   // (wraps past 0: not this block's)
+    for (int i = 0; i < kWalkWarps; ++i) mine += s_slots.v[turn][0][rank * kWalkWarps + i];
+    if ((long long)want < 0 || want >= mine) return;
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      u64 z = W[j];
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) z += shfl_xor(z, o);
+      if (lane == 0) s_sum[j][warp] = z;
+    }
+    __syncthreads();
+    if (warp == 0) {                   // J / 2 sums a lane, in order
+      constexpr int PER = J * kWalkWarps / 32;
+      const u64* const mine_s = &s_sum[0][0] + lane * PER;
+      u64 own = 0;
+#pragma unroll
+      for (int i = 0; i < PER; ++i) own += mine_s[i];
+      u64 upto = own;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const u64 t = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += t;
+      }
+      u64 at = upto - own;
+      if (upto > want && at <= want) {
+        int i = 0;
+        while (at + mine_s[i] <= want) at += mine_s[i++];
+        s_at = lane * PER + i;
+        s_before = at;
+      }
+    }
+    __syncthreads();
+    if (warp == s_at % kWalkWarps) {
+      const int jj = s_at / kWalkWarps;
+      uint32_t w = 0;
+#pragma unroll
+      for (int j = 0; j < J; ++j)
+        if (j == jj) w = W[j];
+      u64 upto = w;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const u64 t = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += t;
+      }
+      upto += s_before;
+      if (upto > want && upto - w <= want) {
+        a.n_path[b] = m;
+        a.emitted[(size_t)b * a.T + m - 1] = base + jj * kWalk + tid;
+      }
+    }
+    return;
+  }
+  if (rank == 0 && tid == 0) {
+    a.n_path[b] = m;
+    a.emitted[(size_t)b * a.T + m - 1] = last;
+  }
+}
+
+template <typename T>
+cudaError_t launch_verify(const VerifyArgs& a, int batch, cudaStream_t s) {
+  // As many blocks to a sequence as leave every SM at most one, while a thread has two values to hold at
+  // least; more where the row does not fit otherwise.
+  int C = 1;
+  while (C < kMaxCluster && ((2 * C * batch <= kPlanSMs && 8 * C * kWalk <= 2 * a.V) || a.V > C * kWalk * 40)) C *= 2;
+  const int J = ((a.V + C - 1) / C + kWalk - 1) / kWalk;
+  const dim3 grid(C, batch), block(kWalk);
+  auto go = [&](auto k) {
+    return C == 1 ? launch_pdl(k, grid, block, 0, s, a) : launch_pdl_cluster(k, grid, block, 0, C, s, a);
+  };
+  if (J <= 4) return go(k_tree_walk<T, 4>);
+  if (J <= 8) return go(k_tree_walk<T, 8>);
+  if (J <= 16) return go(k_tree_walk<T, 16>);
+  if (J <= 40) return go(k_tree_walk<T, 40>);
+  return launch_pdl(k_tree_verify<T>, dim3(batch), dim3(kThreads), 0, s, a);
+}
+
 }  // namespace
 }  // namespace tree
 }  // namespace cdsl
@@ -269,6 +599,7 @@ extern "C" int32_t cdsl_tree_verify(int32_t batch, int32_t T, int32_t vocab, con
                   {h_strides[0], h_strides[1]}, {h_strides[2], h_strides[3]}, d_tokens, d_parents, d_nodes,
                   d_u, d_u_last, temperature > 0.f ? 1.f / temperature : 0.f, d_path, d_n_path, d_emitted,
                   d_status};
-  auto k = dtype == CDSL_DTYPE_BF16 ? k_tree_verify<__nv_bfloat16> : k_tree_verify<float>;
-  return ck.launched(launch_pdl(k, dim3(batch), dim3(kThreads), 0, static_cast<cudaStream_t>(stream), a));
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  return ck.launched(dtype == CDSL_DTYPE_BF16 ? launch_verify<__nv_bfloat16>(a, batch, s)
+                                              : launch_verify<float>(a, batch, s));
 }

@@ -423,6 +423,23 @@ def test_verify_matches_64_bits(cdsl, B, T, V, dtype, drafts, temperature):
     assert torch.equal(again[0], path) and torch.equal(again[2], emitted)
 
 
+@pytest.mark.parametrize("B,T,V", [(1, 9, 32000), (2, 3, 163841), (40, 6, 4999), (100, 4, 20500), (160, 3, 700)])
+@pytest.mark.parametrize("drafts", [False, True])
+def test_verify_by_any_number_of_blocks(cdsl, B, T, V, drafts):
+    """Batches and vocabularies that give a sequence eight blocks, two and one, and rows beyond the registers."""
+    logits, draft, tokens, parents, u, u_last = verify_inputs(B, T, V, BF, drafts, 1.0, seed=B + V, spread=5.0)
+    path, n, emitted, st = run_verify(cdsl, logits, draft, tokens, parents, u, u_last, 1.0)
+    assert st == cdsl.CDSL_OK
+    compared = 0
+    for b in range(B):
+        p, e, margin = ref.verify(logits[b], None if draft is None else draft[b], tokens[b].tolist(), parents[b], T,
+                                  u[b].tolist(), float(u_last[b]), 1.0)
+        if margin >= NEAR:
+            compared += 1
+            assert path[b].tolist() == p + [-1] * (T - len(p)) and emitted[b].tolist() == e + [-1] * (T - len(e))
+    assert compared > 0
+
+
 @pytest.mark.parametrize("drafts", [False, True])
 def test_verify_draws_from_the_targets_distribution(cdsl, drafts):
     """The first emitted token over 40,960 walks of one small tree has the target's probabilities: a chi-square
