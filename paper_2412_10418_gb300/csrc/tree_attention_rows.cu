@@ -279,15 +279,12 @@ __global__ void __launch_bounds__(kThreads, 1)
     bool failed = false;
     for (int unit = begin; unit < end;) {
       const Segment s = segment_at(a, s_first, unit, end);
-      stage_queries<HD, kRows, F8, kSoft>(a, s, tid, q_aligned, sm, [&](int v, const Vec&, float qs, bool bad) {
+      stage_queries<HD, kRows, F8, kSoft, true>(a, s, tid, q_aligned, sm, [&](int v, const Vec&, float qs, bool bad) {
         s_qs[v] = v < s.nq ? qs : 0.f;
         s_bad[v] = bad;
       });
       const int t0 = s.qb * kRows / a.G;       // the block's first node
-      for (int i = tid; i < (kRows + 1) * kWords; i += kSoft) {
-        const int t = t0 + i / kWords, w = i % kWords;
-        s_mask[i / kWords][w] = t < s.nodes && w < a.W ? __ldg(a.mask + ((size_t)s.b * a.T + t) * a.W + w) : 0u;
-      }
+      stage_masks<kSoft>(a, s, t0, tid, s_mask);
       tc::fence_proxy_async();
       tc::mbar_arrive(&q_full);
       sync();
@@ -489,8 +486,12 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (r < rows) {
             if (!whole) {
 #pragma unroll
-              for (int e = 0; e < 16; e += 4)
-                *reinterpret_cast<float4*>(part_o + d + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+              for (int e = 0; e < 16; e += 8) {
+                uint32_t w[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) w[j] = __float_as_uint(o[e + j]);
+                store32(part_o + d + e, w);
+              }
             } else {
               uint32_t w[8];
 #pragma unroll

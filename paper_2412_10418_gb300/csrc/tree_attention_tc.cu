@@ -221,16 +221,13 @@ __global__ void __launch_bounds__(kThreads, Cfg<HD, NQ, F8>::CTAS)
     bool failed = false, gone = false;
     for (int unit = begin; unit < end && !gone;) {
       const Segment s = segment_at(a, s_first, unit, end);
-      stage_queries<HD, NQ, F8, kSoft>(a, s, r, q_aligned, sm + C::Q_OFF, [&](int v, const Vec& x, float qs, bool bad) {
+      stage_queries<HD, NQ, F8, kSoft, false>(a, s, r, q_aligned, sm + C::Q_OFF, [&](int v, const Vec& x, float qs, bool bad) {
         s_qs[v] = v < s.nq ? qs : 0.f;
         s_bad[v] = bad;
         s_out[v] = s.b * a.so[0] + x.t * a.so[1] + x.h * a.so[2];
       });
       const int t0 = s.qb * NQ / a.G;          // the block's first node
-      for (int i = r; i < (NQ + 1) * kWords; i += kSoft) {
-        const int t = t0 + i / kWords, w = i % kWords;
-        s_mask[i / kWords][w] = t < s.nodes && w < a.W ? __ldg(a.mask + ((size_t)s.b * a.T + t) * a.W + w) : 0u;
-      }
+      stage_masks<kSoft>(a, s, t0, r, s_mask);
       tc::fence_proxy_async();
       tc::mbar_arrive(&q_full);
       sync();

@@ -76,20 +76,25 @@ __device__ __forceinline__ void f8x4_half(uint32_t four, __half2* a, __half2* b)
 // Queries of a segment's block to shared memory, by NT threads, eight a vector: K-major tiles of NQ rows in
 // blocks of at most 128 bytes. F8: two e4m3 planes of q / 2^e, hi = e4m3(q / 2^e) and lo the rest, e the
 // smallest with which the row's largest value is at most 448; else bf16 as they are. A row that is not finite, and
-// rows past the block's, become zeros. put(v, where, factor of the scores, not finite) once per vector.
-template <int HD, int NQ, bool F8, int NT, typename F>
+// rows past the block's, become zeros. put(v, where, factor of the scores, not finite) once per vector. LIVE: groups
+// of NT / 8 vectors that are all past the block's are left out.
+template <int HD, int NQ, bool F8, int NT, bool LIVE, typename F>
 __device__ __forceinline__ void stage_queries(const TreeArgs& a, const Segment& s, int tid, bool q_aligned,
                                               uint8_t* q_smem, F&& put) {
   constexpr int QE = HD / 8;                   // values per thread
   constexpr int KROW = HD * (F8 ? 1 : 2), BW = KROW < 128 ? KROW : 128;
   constexpr uint32_t PLANE = NQ * KROW;
-  constexpr int ROUNDS = NQ * 8 / NT;
-  uint32_t raw[ROUNDS][QE / 2];                // (all loads first: their latency once)
+  const int rounds = LIVE ? (s.nq + NT / 8 - 1) / (NT / 8) : NQ * 8 / NT;
+  uint32_t next[QE / 2];
+#pragma unroll 1
+  for (int n = -1; n < rounds; ++n) {          // (the next round's loads before this one's work; one copy of the code)
+    uint32_t w[QE / 2];
 #pragma unroll
-  for (int n = 0; n < ROUNDS; ++n) {
-    const int v = n * (NT / 8) + tid / 8;
-#pragma unroll
-    for (int i = 0; i < QE / 2; ++i) raw[n][i] = 0u;
+    for (int i = 0; i < QE / 2; ++i) {
+      w[i] = next[i];
+      next[i] = 0u;
+    }
+    int v = (n + 1) * (NT / 8) + tid / 8;
     if (v < s.nq) {
       const Vec x = vector_of(a, s.h, s.qb, v);
       const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(a.q) + s.b * a.sq[0] + x.t * a.sq[1] +
@@ -98,19 +103,17 @@ __device__ __forceinline__ void stage_queries(const TreeArgs& a, const Segment& 
 #pragma unroll
         for (int i = 0; i < QE / 8; ++i) {
           const uint4 u = *reinterpret_cast<const uint4*>(q + 8 * i);
-          raw[n][4 * i] = u.x; raw[n][4 * i + 1] = u.y; raw[n][4 * i + 2] = u.z; raw[n][4 * i + 3] = u.w;
+          next[4 * i] = u.x; next[4 * i + 1] = u.y; next[4 * i + 2] = u.z; next[4 * i + 3] = u.w;
         }
       } else {
 #pragma unroll
         for (int i = 0; i < QE; ++i)
-          raw[n][i / 2] |= (uint32_t)__bfloat16_as_ushort(q[i]) << (i % 2 * 16);
+          next[i / 2] |= (uint32_t)__bfloat16_as_ushort(q[i]) << (i % 2 * 16);
       }
     }
-  }
-#pragma unroll
-  for (int n = 0; n < ROUNDS; ++n) {
-    const int v = n * (NT / 8) + tid / 8, part = tid % 8;
-    const uint32_t (&w)[QE / 2] = raw[n];
+    if (n < 0) continue;
+    v -= NT / 8;
+    const int part = tid % 8;
     uint32_t top = 0;                      // largest |x|, as bf16 bits
 #pragma unroll
     for (int i = 0; i < QE / 2; ++i) top = max(top, max(w[i] & 0x7fffu, w[i] >> 16 & 0x7fffu));
@@ -159,6 +162,16 @@ __device__ __forceinline__ void stage_queries(const TreeArgs& a, const Segment& 
     }
     if (part == 0) put(v, vector_of(a, s.h, s.qb, v), qs, v < s.nq && bad);
   }
+}
+
+// The masks of the block's nodes to shared memory, s_mask[t - t0], by NT threads; of a part of an item without slots
+// of the tree, none. (Words past a.W stay as they are: no slot has such a node.)
+template <int NT>
+__device__ __forceinline__ void stage_masks(const TreeArgs& a, const Segment& s, int t0, int tid, uint32_t (*s_mask)[kWords]) {
+  if (s.c1 * kKeys <= s.len) return;
+  const int n = (min(s.nodes, t0 + (s.nq + a.G - 1) / a.G + 1) - t0) * a.W;
+  for (int i = tid; i < n; i += NT)
+    s_mask[i / a.W][i % a.W] = __ldg(a.mask + ((size_t)s.b * a.T + t0) * a.W + i);
 }
 
 // The loading warp: K and V chunks of a run's segments into a ring of NST stages (tiles of kKeys rows in blocks
@@ -222,6 +235,13 @@ __device__ __forceinline__ void load_chunks(const TreeArgs& a, const int* first,
     for (int kv = 0; kv < 2; ++kv)
       for (int i = max(0, issued[kv] - NST); i < issued[kv]; ++i)
         tc::mbar_wait(kv ? &v_full[i % NST] : &k_full[i % NST], parity(i, NST), a.status);
+}
+
+// 32 bytes to an address that is a multiple of 32 (a whole sector: two stores of 16 bytes take two).
+__device__ __forceinline__ void store32(void* p, const uint32_t (&v)[8]) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]),
+               "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+               : "memory");
 }
 
 // The tensor map of a layer's rows for load_chunks.
