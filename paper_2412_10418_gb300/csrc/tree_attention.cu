@@ -95,17 +95,24 @@ __global__ void __launch_bounds__(kThreads) k_tree_simt(TreeArgs a) {
         const size_t vrow = row_of(c, a.layer, page, 1, s.h, at);
         s_row[tid] = (uint32_t)(vrow - row_of(c, a.layer, 0, 0, 0, 0));
         const uint4* k = reinterpret_cast<const uint4*>(c.pool + row * HD * (F8 ? 1 : 2));
-#pragma unroll 2
-        for (int i = 0; i < HD / CPL; ++i) {
-          float x[CPL];
-          decode16<F8>(__ldg(k + i), x);
+        constexpr int LOADS = HD / CPL, AHEAD = LOADS < 8 ? LOADS : 8;   // in flight together
+#pragma unroll 1
+        for (int i0 = 0; i0 < LOADS; i0 += AHEAD) {
+          uint4 raw[AHEAD];
 #pragma unroll
-          for (int v = 0; v < SQ; ++v)
+          for (int i = 0; i < AHEAD; ++i) raw[i] = __ldg(k + i0 + i);
 #pragma unroll
-            for (int e = 0; e < CPL; e += 4) {
-              const float4 q = *reinterpret_cast<const float4*>(&s_q[v][i * CPL + e]);
-              t[v] = fmaf(q.x, x[e], fmaf(q.y, x[e + 1], fmaf(q.z, x[e + 2], fmaf(q.w, x[e + 3], t[v]))));
-            }
+          for (int i = 0; i < AHEAD; ++i) {
+            float x[CPL];
+            decode16<F8>(raw[i], x);
+#pragma unroll
+            for (int v = 0; v < SQ; ++v)
+#pragma unroll
+              for (int e = 0; e < CPL; e += 4) {
+                const float4 q = *reinterpret_cast<const float4*>(&s_q[v][(i0 + i) * CPL + e]);
+                t[v] = fmaf(q.x, x[e], fmaf(q.y, x[e + 1], fmaf(q.z, x[e + 2], fmaf(q.w, x[e + 3], t[v]))));
+              }
+          }
         }
         const float ks = scale_value(c.scale[row]);
         vs = scale_value(c.scale[vrow]);
@@ -140,23 +147,27 @@ __global__ void __launch_bounds__(kThreads) k_tree_simt(TreeArgs a) {
       // ---- P V of this thread's dimension (and share of the slots)
       const int d = tid % HD, k0 = tid / HD * (kKeys / SPLIT);
       const int kn = min(s.keys - ch * kKeys, k0 + kKeys / SPLIT);
-      for (int k = k0; k < kn; k += 4) {
-        float x[4];
+      const uint8_t* const pool = c.pool + row_of(c, a.layer, 0, 0, 0, 0) * HD * (F8 ? 1 : 2);
+#pragma unroll 1
+      for (int k = k0; k < kn; k += 16) {      // 16 slots' loads in flight
+        float x[16];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
+        for (int e = 0; e < 16; ++e) {
           const uint32_t row = s_row[k + e];
           x[e] = 0.f;
           if (k + e < kn && row != ~0u) {
-            const uint8_t* v = c.pool + (row_of(c, a.layer, 0, 0, 0, 0) + row) * HD * (F8 ? 1 : 2);
+            const uint8_t* v = pool + (size_t)row * HD * (F8 ? 1 : 2);
             x[e] = F8 ? f8x2_to_f32(__ldg(v + d)).x
                       : __uint_as_float((uint32_t)__ldg(reinterpret_cast<const uint16_t*>(v) + d) << 16);
           }
         }
 #pragma unroll
-        for (int v = 0; v < SQ; ++v) {
-          const float4 p = *reinterpret_cast<const float4*>(&s_p[v][k]);
-          o[v] = fmaf(p.x, x[0], fmaf(p.y, x[1], fmaf(p.z, x[2], fmaf(p.w, x[3], o[v]))));
-        }
+        for (int v = 0; v < SQ; ++v)
+#pragma unroll
+          for (int e = 0; e < 16; e += 4) {
+            const float4 p = *reinterpret_cast<const float4*>(&s_p[v][k + e]);
+            o[v] = fmaf(p.x, x[e], fmaf(p.y, x[e + 1], fmaf(p.z, x[e + 2], fmaf(p.w, x[e + 3], o[v]))));
+          }
       }
       __syncthreads();
     }
