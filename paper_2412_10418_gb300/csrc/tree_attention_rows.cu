@@ -16,13 +16,14 @@
 // the number of vectors. What changes from slot to slot (K's scales, masks) is read from shared memory. That
 // costs the same for 33 vectors as for 128, and reads K and V once for all of them.
 //
-// Two groups of four softmax warps take alternate chunks, each with its own S (which P then overwrites) and O
-// in TMEM, so that one's exponentials run beside the other's maxima and MMAs; they are added up at the end of an
-// item. O is one chain over a group's chunks: fp16's range leaves P exact enough under a reference that is raised
-// only when a maximum passes it by more than 2^kMargin, which after the first chunk is rare, and then the thread
-// multiplies its O. (O started anew in every chunk and was added up in registers before: eight more warps, and a
-// chain of waits through them that held a chunk to 3,500 cycles.) Four warps convert V, one loads, one issues
-// MMAs, one turns scale bytes into factors.
+// Two groups of four softmax warps take alternate chunks, so that one's exponentials run beside the other's
+// maxima; S, which P then overwrites, has three buffers in TMEM, so that neither waits for its next one (with two,
+// and an O for each group, a chunk took 3,100 cycles, of them half waiting). O is one chain over the chunks: fp16's range
+// leaves P exact enough under a reference that is raised only when a maximum passes it by more than 2^kMargin,
+// which after the first chunk is rare; then the thread multiplies its O. A row's reference goes from chunk to chunk, and
+// so from group to group, through shared memory. (O started anew in every chunk and was added up in registers before:
+// eight more warps, and a chain of waits through them that held a chunk to 3,500 cycles.) Four warps convert V, one
+// loads, one issues MMAs, one turns scale bytes into factors.
 #include <cuda.h>
 
 #include <algorithm>
@@ -44,6 +45,7 @@ constexpr int kConvWarp = kSoft / 32, kProducer = kConvWarp + kConv / 32, kIssue
               kScaler = kProducer + 2;         // warps
 constexpr float kMargin = 7.f;                 // base 2: probabilities are at most 2^kMargin of a reference, and
 constexpr float kUp = 7.f;                     // stored times 2^kUp: below fp16's largest
+constexpr int kBuf = 3;                        // S (then P) buffers in TMEM; O has the rest
 constexpr int kVRoom = 6;                      // octaves that V's scales may pass theirs by: 448 * 2^6 in fp16
 
 template <int HD, bool F8>
@@ -80,13 +82,13 @@ __global__ void __launch_bounds__(kThreads, 1)
   int* const s_first = reinterpret_cast<int*>(sm + C::PLAN_OFF);
   __shared__ __align__(8) uint64_t k_full[NST], v_full[NST], k_empty[NST], v_empty[NST];
   __shared__ __align__(8) uint64_t f_full[NST], f_empty[NST], h_full[2];
-  __shared__ __align__(8) uint64_t s_full[2], p_full[2], pv_done[2], q_full, done;
+  __shared__ __align__(8) uint64_t s_full[kBuf], p_full[kBuf], r_full[kBuf], pv_done[2], q_full, done;
   __shared__ uint32_t s_tmem;
   __shared__ __align__(16) uint32_t s_valid[NST][4], s_nan[NST][4];   // slots that there are, whose V is not finite
-  __shared__ int s_vref[NST];                  // V's reference in the chunk
+  __shared__ int s_vref[NST], s_vstep[NST];    // V's reference in the chunk, and that of the chunk before less it
   __shared__ float s_qs[kRows];                // score factors
-  __shared__ float s_m[2][kRows], s_l[2][kRows];   // the groups' references and sums
-  __shared__ int s_v[2];                       // and V references
+  __shared__ int s_v;                          // V's reference at the end
+  __shared__ float s_ref[kRows], s_l[2][kRows];   // the rows' references; the groups' sums
   __shared__ uint8_t s_bad[kRows];             // the query is not finite
   __shared__ uint32_t s_mask[kRows + 1][kWords];
   __shared__ uint32_t s_pieces[NST];
@@ -102,10 +104,15 @@ __global__ void __launch_bounds__(kThreads, 1)
       tc::mbar_init(&f_full[i], 32);
       tc::mbar_init(&f_empty[i], kRows);
     }
-    for (int i = 0; i < 2; ++i) {
-      tc::mbar_init(&h_full[i], kConv);
+    // (P and references by buffers of S: a warp can be at its group's next chunk, two on, before the others have
+    // finished this one, but not at the chunk that takes the same buffer)
+    for (int i = 0; i < kBuf; ++i) {
       tc::mbar_init(&s_full[i], 1);
       tc::mbar_init(&p_full[i], kRows);
+      tc::mbar_init(&r_full[i], kRows);
+    }
+    for (int i = 0; i < 2; ++i) {
+      tc::mbar_init(&h_full[i], kConv);
       tc::mbar_init(&pv_done[i], 1);
     }
     tc::mbar_init(&q_full, kSoft);
@@ -124,7 +131,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int total = s_first[c.batch], runs = runs_of(a, total);
   const int begin = (int)blockIdx.x < runs ? run_begin(blockIdx.x, total, runs) : 0;
   const int end = (int)blockIdx.x < runs ? run_begin(blockIdx.x + 1, total, runs) : 0;
-  const uint32_t t_o = tmem + 2 * kKeys;       // columns: S (then P) of both groups, O of both
+  const uint32_t t_o = tmem + kBuf * kKeys;
 
   if (warp == kProducer) {
     load_chunks<HD, F8, NST>(a, s_first, begin, end, map, sm + C::KV_OFF, sm + C::SCALE_OFF, s_pieces, k_full,
@@ -155,15 +162,15 @@ __global__ void __launch_bounds__(kThreads, 1)
               const uint64_t q = desc_q + ((uint32_t)(p * C::Q_PLANE + nb * kRows * C::BW) / 16 + 2 * x);
               const uint64_t kk = k + (nb * C::BLOCK / 16 + 2 * x);
               const bool add = p < C::QP - 1 || nb + x > 0;
-              if constexpr (F8) tc::umma_f8(tmem + (i & 1) * kKeys, q, kk, idesc_s, add);
-              else tc::umma_bf16(tmem + (i & 1) * kKeys, q, kk, idesc_s, add);
+              if constexpr (F8) tc::umma_f8(tmem + i % kBuf * kKeys, q, kk, idesc_s, add);
+              else tc::umma_bf16(tmem + i % kBuf * kKeys, q, kk, idesc_s, add);
             }
-        tc::umma_commit(&s_full[i & 1]);
+        tc::umma_commit(&s_full[i % kBuf]);
         tc::umma_commit(&k_empty[i % NST]);
         return true;
       };
       auto pv = [&](int i, bool add) {         // P V of chunk i
-        if (!tc::mbar_wait(&p_full[i & 1], parity(i, 2), a.status) ||
+        if (!tc::mbar_wait(&p_full[i % kBuf], parity(i, kBuf), a.status) ||
             !(F8 ? tc::mbar_wait(&h_full[i & 1], parity(i, 2), a.status)
                  : tc::mbar_wait(&v_full[i % NST], parity(i, NST), a.status)))
           return false;
@@ -175,7 +182,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int p = F8 ? 0 : 1; p >= 0; --p)
 #pragma unroll
           for (int k = 0; k < kKeys / 16; ++k)
-            tc::umma_tmem_a(t_o + (i & 1) * kKeys, tmem + (i & 1) * kKeys + k / 2 * 32 + p * 16 + k % 2 * 8, v + k * (16 * 128 / 16), idesc_o,
+            tc::umma_tmem_a(t_o, tmem + i % kBuf * kKeys + k / 2 * 32 + p * 16 + k % 2 * 8, v + k * (16 * 128 / 16), idesc_o,
                             add || (!F8 && p < 1) || k > 0);
         tc::umma_commit(&pv_done[i & 1]);
         if (!F8) tc::umma_commit(&v_empty[i % NST]);
@@ -187,9 +194,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         const Segment s = segment_at(a, s_first, unit, end);
         const int n = s.c1 - s.c0;
         ok = tc::mbar_wait(&q_full, seg & 1, a.status);
-        // S two chunks ahead; it overwrites a P after the P V that reads it, in order
-        for (int i = 0; i < n + 2 && ok; ++i) {
-          if (i >= 2) ok = pv(it + i - 2, i >= 4);
+        // S as far ahead as it has buffers; it overwrites a P after the P V that reads it, in order
+        for (int i = 0; i < n + kBuf && ok; ++i) {
+          if (i >= kBuf) ok = pv(it + i - kBuf, i > kBuf);
           if (ok && i < n) ok = s_mma(it + i);
         }
         it += n;
@@ -224,6 +231,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (e < n && x != 255) vmax = max(vmax, x);
         }
         vmax = __reduce_max_sync(0xffffffffu, vmax);
+        const int before = vref;
         if (vref == 0 || vmax > vref + kVRoom) vref = vmax;
         float kf[4], vf[4];
         uint32_t nan = 0;
@@ -249,7 +257,10 @@ __global__ void __launch_bounds__(kThreads, 1)
           s_valid[st][lane >> 3] = valid;
           s_nan[st][lane >> 3] = nan;
         }
-        if (lane == 0) s_vref[st] = F8 ? vref : 127;
+        if (lane == 0) {
+          s_vref[st] = F8 ? vref : 127;
+          s_vstep[st] = F8 && before ? before - vref : 0;
+        }
         if (F8) {
           __syncwarp();
           if (lane == 0) tc::mbar_arrive(&v_empty[st]);             // (the scale bytes are read)
@@ -274,7 +285,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     auto sync = [] { tc::named_barrier(1, kSoft); };
     const bool q_aligned = (reinterpret_cast<uintptr_t>(a.q) | (a.sq[0] | a.sq[1] | a.sq[2]) * 2) % 16 == 0;
     const bool o_aligned = (reinterpret_cast<uintptr_t>(a.out) | (a.so[0] | a.so[1] | a.so[2]) * 2) % 16 == 0;
-    const uint32_t lanes = (uint32_t)(w4 * 32) << 16, t_s = tmem + grp * kKeys + lanes;
+    const uint32_t lanes = (uint32_t)(w4 * 32) << 16;
     int it0 = 0;
     bool failed = false;
     for (int unit = begin; unit < end;) {
@@ -292,13 +303,14 @@ __global__ void __launch_bounds__(kThreads, 1)
       const bool live = w4 * 32 < s.nq;        // (a warp's: its rows hold vectors)
       const uint32_t* const my_mask = s_mask[r < s.nq ? vector_of(a, s.h, s.qb, r).t - t0 : 0];
       const int n = s.c1 - s.c0;
-      float ref = -INFINITY, l = 0.f;
-      int vref = 0, last = -1;                 // V's reference in O, the group's last chunk
+      float ref = -INFINITY, l = 0.f;          // the row's reference at the group's last chunk, and its sum
+      int vref = 127;                          // V's reference in O
       for (int i = (it0 & 1) ^ grp; i < n && !failed; i += 2) {   // chunks it with it % 2 == grp
         const int it = it0 + i, st = it % NST;
+        const uint32_t t_s = tmem + it % kBuf * kKeys + lanes;
         const float* const kf = reinterpret_cast<const float*>(sm + C::FACTOR_OFF) + st * 2 * kKeys;
         bool ok = tc::mbar_wait(&f_full[st], parity(it, NST), a.status);
-        ok = ok && tc::mbar_wait(&s_full[grp], parity(it, 2), a.status);
+        ok = ok && tc::mbar_wait(&s_full[it % kBuf], parity(it, kBuf), a.status);
         failed = !__all_sync(0xffffffffu, ok);   // (a warp gives up as one)
         tc::tc_fence_after();
         // a chunk with slots of the tree, past the item's, without a page or with a V that is not finite: each row has
@@ -357,23 +369,29 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
           }
           const float top = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
-          // ---- the reference; the group's P V before is done (this S was issued after it)
-          float f = 1.f;
-          const float mq = top * qs;
-          if (top > -INFINITY && !(mq - ref <= kMargin)) {
-            f = ref == -INFINITY ? 1.f : ex2(ref - mq);   // (no reference: the sums are 0)
-            ref = mq;
+          // ---- the row's reference: the chunk before's, raised where the maximum asks for it
+          float was = -INFINITY;
+          if (i > 0) {
+            ok = tc::mbar_wait(&r_full[(it - 1) % kBuf], parity(it - 1, kBuf), a.status);
+            was = s_ref[r];
           }
-          l *= f;
-          if (F8 && last >= 0) f *= ex2((float)(vref - s_vref[st]));
-          if (last >= 0 && __any_sync(0xffffffffu, f != 1.f)) {
+          const float mq = top * qs, now = top > -INFINITY && !(mq - was <= kMargin) ? mq : was;
+          s_ref[r] = now;
+          tc::mbar_arrive(&r_full[it % kBuf]);
+          if (ref != now) l *= ref == -INFINITY ? 1.f : ex2(ref - now);   // (no reference: the sums are 0)
+          ref = now;
+          float f = was == now || was == -INFINITY ? 1.f : ex2(was - now);
+          if (F8) f *= ex2((float)s_vstep[st]);
+          if (i > 0 && __any_sync(0xffffffffu, f != 1.f)) {
+            ok = ok && tc::mbar_wait(&pv_done[1 - grp], parity(it - 1, 2), a.status);
+            tc::tc_fence_after();
 #pragma unroll 1
             for (int d = 0; d < HD; d += 16) {
               float o[16];
-              tc::tmem_ld16(t_o + grp * kKeys + lanes + d, o);
+              tc::tmem_ld16(t_o + lanes + d, o);
 #pragma unroll
               for (int e = 0; e < 16; ++e) o[e] *= f;
-              tc::tmem_st16(t_o + grp * kKeys + lanes + d, o);
+              tc::tmem_st16(t_o + lanes + d, o);
             }
           }
           const float off = ref == -INFINITY ? 0.f : ref - kUp;
@@ -424,38 +442,36 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (live) {
           if (masked) softmax(std::true_type());
           else softmax(std::false_type());
+          failed = !__all_sync(0xffffffffu, ok);
+        } else {
+          tc::mbar_arrive(&r_full[it % kBuf]);
         }
         vref = s_vref[st];
-        last = it;
         tc::tc_fence_before();
-        tc::mbar_arrive(&p_full[grp]);
+        tc::mbar_arrive(&p_full[it % kBuf]);
         tc::mbar_arrive(&f_empty[st]);
       }
-      // ---- the groups' sums: each thread finishes half of its row's dimensions from both O
-      if (!failed && last >= 0)
-        failed = !__all_sync(0xffffffffu, tc::mbar_wait(&pv_done[grp], parity(last, 2), a.status));
-      s_m[grp][r] = ref;
-      s_l[grp][r] = l;
-      if (r == 0) s_v[grp] = vref;
-      tc::tc_fence_before();
+      // ---- the groups' sums: each thread finishes half of its row's dimensions
+      const int last = it0 + n - 1;
+      if (!failed)
+        failed = !__all_sync(0xffffffffu, tc::mbar_wait(&pv_done[last & 1], parity(last, 2), a.status));
       if (tc::named_barrier_or(1, kSoft, failed)) break;
       tc::tc_fence_after();
       const int rows = min(kRows, a.T * a.G - s.qb * kRows);
-      const bool two = n > 1;                  // (else the other group has nothing)
       {
-        const int own = it0 & 1;               // the group of the first chunk
-        const float m0 = s_m[own][r], m1 = two ? s_m[1 - own][r] : -INFINITY;
-        float m = fmaxf(m0, m1);
+        float m = live ? s_ref[r] : -INFINITY;   // the last chunk's
+        if (ref != m) l *= ref == -INFINITY ? 1.f : ex2(ref - m);
+        s_l[grp][r] = l;
+        if (grp == (last & 1) && r == 0) s_v = vref;
+        sync();
+        l = s_l[0][r] + s_l[1][r];
         if (m == -INFINITY) m = 0.f;           // (nothing seen, or NaN scores alone)
-        const float f0 = m0 == -INFINITY ? 1.f : ex2(m0 - m), f1 = m1 == -INFINITY ? 1.f : ex2(m1 - m);
-        l = s_l[own][r] * f0 + (two ? s_l[1 - own][r] * f1 : 0.f);
         if (r >= s.nq || s.keys == 0) l = 0.f;
         if (l != 0.f && s_bad[r]) l = __uint_as_float(0x7fc00000u);
         m = l == 0.f ? -INFINITY : m - kUp;
         const bool whole = s.c0 == 0 && s.c1 == s.units;
         const float inv = l == 0.f ? 0.f : whole ? 1.f / l : 1.f;
-        const float g0 = f0 * (F8 ? ex2((float)(s_v[own] - 127)) : 1.f);
-        const float g1 = two ? f1 * (F8 ? ex2((float)(s_v[1 - own] - 127)) : 1.f) : 0.f;
+        const float unscale = F8 ? ex2((float)(s_v - 127)) : 1.f;
         const Vec x = vector_of(a, s.h, s.qb, r);
         const size_t part = (size_t)blockIdx.x * 2 + (s.c0 == 0);
         if (grp == 0 && r < rows) {
@@ -472,17 +488,9 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll 1
         for (int d = grp * (HD / 2); d < (grp + 1) * (HD / 2); d += 16) {
           float o[16];
-          tc::tmem_ld16(t_o + own * kKeys + lanes + d, o);
+          tc::tmem_ld16(t_o + lanes + d, o);
 #pragma unroll
-          for (int e = 0; e < 16; ++e) o[e] *= g0;
-          if (two) {
-            float z[16];
-            tc::tmem_ld16(t_o + (1 - own) * kKeys + lanes + d, z);
-#pragma unroll
-            for (int e = 0; e < 16; ++e) o[e] = fmaf(z[e], g1, o[e]);
-          }
-#pragma unroll
-          for (int e = 0; e < 16; ++e) o[e] = inv == 0.f ? 0.f : o[e] * inv;
+          for (int e = 0; e < 16; ++e) o[e] = inv == 0.f ? 0.f : o[e] * unscale * inv;
           if (r < rows) {
             if (!whole) {
 #pragma unroll
