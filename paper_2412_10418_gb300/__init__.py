@@ -23,6 +23,7 @@ STATUS = {0: "CDSL_OK", 1: "CDSL_EINVAL", 2: "CDSL_ENOMEM", 3: "CDSL_ECUDA", 4: 
 (CDSL_OK, CDSL_EINVAL, CDSL_ENOMEM, CDSL_ECUDA, CDSL_ETIMEOUT, CDSL_ENONFINITE, CDSL_ESTATE,
  CDSL_ERANGE) = range(8)
 S1, S2_S3, S4 = 1, 2, 4
+TREE_MAX_NODES, TREE_MAX_BATCH, TREE_MAX_VOCAB = 128, 1024, 1 << 20
 
 
 class CdslError(RuntimeError):
