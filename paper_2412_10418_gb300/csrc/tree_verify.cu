@@ -5,14 +5,18 @@
 // whole numbers, so that neither the decisions nor the token depend on the order of any sum.
 //
 // k_tree_walk: a cluster of up to eight blocks walks a sequence's tree, each with its part of the row in registers
-// (J values a thread). A reduction is one cluster barrier: each warp's value goes to every block's shared
-// memory, where each warp reduces all of them for itself; the children's decisions are then made alike by every
-// thread. Bound by latency: a level is a row's loads, two such reductions and the decisions. Rows of more than
-// the cluster's registers hold (163,840 tokens) take k_tree_verify, a block per sequence that reads a row
-// several times.
+// (J values a thread, 16 bytes a load where rows are aligned). A reduction is one cluster barrier: each warp's value
+// goes to every block's shared memory, where each warp reduces all of them for itself; the children's decisions are
+// then made alike by every thread. Bound by latency and, with drafts, by the exponentials: a level of 32,000 bf16
+// tokens with drafts in four blocks is 12,000 cycles (loads 3,400, exponentials 2,900, two reductions of 1,500 each,
+// the decisions 1,600 and more with rejections). 32 sequences of 49 sampled nodes, the longest path 8: 47 us; one of
+// 17 chosen nodes, fp32: 10 us. (A value a load, and keys of 64 bits in the maximum: 18,500 cycles a level, 82 us.) Rows
+// of more than the cluster's registers hold (163,840 tokens) take k_tree_verify, a block per sequence that
+// reads a row several times.
 #include <cuda.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "tc_ptx.cuh"
 #include "tree_host.h"
@@ -258,18 +262,24 @@ struct Slots {
   u64 v[2][2][kMaxCluster * kWalkWarps];
 };
 
-__device__ __forceinline__ u64 shfl_xor(u64 x, int o) { return __shfl_xor_sync(0xffffffffu, x, o); }
+// Over a warp, in two 32-bit reductions each. Sums: of 2^51 at most a lane.
+__device__ __forceinline__ u64 warp_sum(u64 x) {
+  const uint32_t lo = __reduce_add_sync(0xffffffffu, (uint32_t)x & 0xffffffu);
+  return ((u64)__reduce_add_sync(0xffffffffu, (uint32_t)(x >> 24)) << 24) + lo;
+}
+__device__ __forceinline__ u64 warp_most(u64 x) {
+  const uint32_t hi = __reduce_max_sync(0xffffffffu, (uint32_t)(x >> 32));
+  return (u64)hi << 32 | __reduce_max_sync(0xffffffffu, (uint32_t)(x >> 32) == hi ? (uint32_t)x : 0u);
+}
 
-// a and b of every thread of the cluster, by op; C: blocks. One cluster barrier. Afterwards s.v[turn][.] holds
-// the warps' values, block by block.
-template <typename Op>
-__device__ __forceinline__ void reduce_cluster(u64& a, u64& b, bool both, Op op, Slots& s, int& turn, int C, int rank) {
+// a and b of every thread of the cluster, their sums or their maxima; C: blocks. One cluster barrier. Afterwards
+// s.v[turn][.] holds the warps' values, block by block.
+template <bool Sum>
+__device__ __forceinline__ void reduce_cluster(u64& a, u64& b, bool both, Slots& s, int& turn, int C, int rank) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    a = op(a, shfl_xor(a, o));
-    if (both) b = op(b, shfl_xor(b, o));
-  }
+  const auto over_warp = [](u64 x) { return Sum ? warp_sum(x) : warp_most(x); };
+  a = over_warp(a);
+  if (both) b = over_warp(b);
   turn ^= 1;
   const int at = rank * kWalkWarps + warp;
   if (C > 1) {
@@ -290,25 +300,39 @@ __device__ __forceinline__ void reduce_cluster(u64& a, u64& b, bool both, Op op,
   }
   a = b = 0;                           // (neutral to both operations: keys and sums are not negative)
   for (int i = lane; i < C * kWalkWarps; i += 32) {
-    a = op(a, s.v[turn][0][i]);
-    if (both) b = op(b, s.v[turn][1][i]);
+    const u64 x = s.v[turn][0][i], y = both ? s.v[turn][1][i] : 0;
+    a = Sum ? a + x : max(a, x);
+    b = Sum ? b + y : max(b, y);
   }
+  a = over_warp(a);
+  if (both) b = over_warp(b);
+}
+
+// E values from p, in one load.
+template <int E, typename T>
+__device__ __forceinline__ void load_values(const T* p, float* out) {
+  if constexpr (E == 1) {
+    out[0] = to_f32<T>(*p);
+  } else {
+    using Bits = std::conditional_t<E * sizeof(T) == 16, uint4, uint2>;
+    const Bits x = *reinterpret_cast<const Bits*>(p);
+    const T* const v = reinterpret_cast<const T*>(&x);
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    a = op(a, shfl_xor(a, o));
-    if (both) b = op(b, shfl_xor(b, o));
+    for (int e = 0; e < E; ++e) out[e] = to_f32<T>(v[e]);
   }
 }
 
-template <typename T, int J>
+// J values a thread, E of them next to one another: value k is token (k / E * kWalk + tid) * E + k % E of the block's.
+template <typename T, int J, int E>
 __global__ void __launch_bounds__(kWalk) k_tree_walk(VerifyArgs a) {
   __shared__ Slots s_slots;
-  __shared__ int s_tok[kMaxT], s_par[kMaxT];
+  __shared__ int s_tok[kMaxT];
+  __shared__ uint32_t s_child[kMaxT][kMaxT / 32];   // a node's children, by bits
   __shared__ float s_u[kMaxT];
   __shared__ float s_lx[kMaxT], s_qx[kMaxT];   // a node's children's logits, the target's and the draft's
   __shared__ float s_inv[kMaxT];
-  __shared__ int s_out[kMaxT];
-  __shared__ u64 s_sum[J][kWalkWarps];         // a block's weights by 32 tokens, in their order
+  constexpr int kSums = J / E * kWalkWarps;
+  __shared__ u64 s_sum[kSums];                 // a block's weights by 32 E tokens, in their order
   __shared__ int s_at;
   __shared__ u64 s_before;
   const int C = (int)gridDim.x, rank = (int)blockIdx.x, b = blockIdx.y, tid = threadIdx.x, V = a.V;
@@ -316,18 +340,21 @@ __global__ void __launch_bounds__(kWalk) k_tree_walk(VerifyArgs a) {
   pdl_wait();
   pdl_launch_dependents();
   const int n = a.nodes ? min(max(a.nodes[b], 0), a.T) : a.T;
+  if (C > 1) tc::cluster_arrive();     // (before any store to another block's memory: that all have started)
+  for (int i = tid; i < kMaxT * kMaxT / 32; i += kWalk) s_child[0][i] = 0u;
+  __syncthreads();
   for (int i = tid; i < a.T; i += kWalk) {
+    const int parent = a.parents[(size_t)b * a.T + i];
+    if (i > 0 && i < n && parent >= 0 && parent < i) atomicOr(&s_child[parent][i >> 5], 1u << (i & 31));
     s_tok[i] = a.tokens[(size_t)b * a.T + i];
-    s_par[i] = a.parents[(size_t)b * a.T + i];
     s_u[i] = a.u[(size_t)b * a.T + i];
     if (rank == 0) a.path[(size_t)b * a.T + i] = a.emitted[(size_t)b * a.T + i] = -1;
   }
   const float u_last = a.u_last[b];
   const bool greedy = a.inv_t == 0.f, drafts = a.draft != nullptr;
-  const int size = (V + C - 1) / C, base = rank * size, top = min(V, base + size);   // this block's tokens
-  const auto sum = [](u64 x, u64 y) { return x + y; };
-  const auto most = [](u64 x, u64 y) { return x > y ? x : y; };
+  const int size = ((V + C - 1) / C + E - 1) / E * E, base = rank * size, top = min(V, base + size);   // this block's tokens
   int turn = 0;
+  if (C > 1) tc::cluster_wait();
   __syncthreads();
   if (n == 0) {
     if (rank == 0 && tid == 0) a.n_path[b] = 0;
@@ -338,6 +365,11 @@ __global__ void __launch_bounds__(kWalk) k_tree_walk(VerifyArgs a) {
   auto weight = [&](float l, float m) { return expf(__fmul_rn(__fsub_rn(l, m), a.inv_t)); };
   auto inverse = [](u64 Z) { return __fdiv_rn(1.f, __fmul_rn(__ull2float_rn(Z), 1.f / kTwo31)); };
   int cur = 0, m = 0, last = -1;
+  const auto child = [&](int i) {      // the node's first child after i, kMaxT: none
+    for (++i; i < kMaxT; i = (i | 31) + 1)
+      if (const uint32_t x = s_child[cur][i >> 5] >> (i & 31)) return i + __ffs(x) - 1;
+    return kMaxT;
+  };
   for (;;) {
     if (rank == 0 && tid == 0) {
       a.path[(size_t)b * a.T + m] = cur;
@@ -348,24 +380,25 @@ __global__ void __launch_bounds__(kWalk) k_tree_walk(VerifyArgs a) {
     float l[J], q[J];
     const T* const row = rows + cur * a.sl[1];
     const T* const draft_row = draft_rows + cur * a.sd[1];
+    const auto load = [&](const T* from, float (&x)[J]) {
 #pragma unroll
-    for (int j = 0; j < J; ++j) {
-      const int v = base + j * kWalk + tid;
-      l[j] = v < top ? to_f32<T>(row[v]) : -INFINITY;
-    }
-    if (drafts)
+      for (int j = 0; j < J; j += E) {
+        const int v = base + (j / E * kWalk + tid) * E;
+        if (v + E <= top) {
+          load_values<E>(from + v, x + j);
+        } else {
 #pragma unroll
-      for (int j = 0; j < J; ++j) {
-        const int v = base + j * kWalk + tid;
-        q[j] = v < top ? to_f32<T>(draft_row[v]) : -INFINITY;
+          for (int e = 0; e < E; ++e) x[j + e] = v + e < top ? to_f32<T>(from[v + e]) : -INFINITY;
+        }
       }
-    if (tid < n && tid > cur && s_par[tid] == cur && (unsigned)s_tok[tid] < (unsigned)V) {
+    };
+    load(row, l);
+    if (drafts) load(draft_row, q);
+    if (tid < n && s_child[cur][tid >> 5] >> (tid & 31) & 1 && (unsigned)s_tok[tid] < (unsigned)V) {
       s_lx[tid] = to_f32<T>(row[s_tok[tid]]);
       if (drafts) s_qx[tid] = to_f32<T>(draft_row[s_tok[tid]]);
     }
-    for (int i = cur + 1, ahead = 0; i < n && ahead < kPrefetch; ++i) {
-      if (s_par[i] != cur) continue;
-      ++ahead;
+    for (int i = child(cur), ahead = 0; i < kMaxT && ahead < kPrefetch; i = child(i), ++ahead) {
       constexpr int kLine = 128 / sizeof(T);
       for (int v = base + tid * kLine; v < top; v += kWalk * kLine) {
         asm volatile("prefetch.global.L2 [%0];" ::"l"(rows + i * a.sl[1] + v));
@@ -373,18 +406,20 @@ __global__ void __launch_bounds__(kWalk) k_tree_walk(VerifyArgs a) {
       }
     }
     // ---- maxima (all ones: a row that cannot be drawn from)
-    u64 best = 0, best_q = 0;
+    const auto most = [&](const float (&x)[J]) {
+      float m = -INFINITY;
+      int k = 0;
+      bool bad = false;
 #pragma unroll
-    for (int j = 0; j < J; ++j) {
-      const int v = base + j * kWalk + tid;
-      if (!(l[j] < INFINITY)) best = ~0ull;
-      else if (l[j] > -INFINITY) best = most(best, argmax_key(l[j] + 0.f, v));
-      if (drafts) {
-        if (!(q[j] < INFINITY)) best_q = ~0ull;
-        else if (q[j] > -INFINITY) best_q = most(best_q, argmax_key(q[j], v));
+      for (int j = 0; j < J; ++j) {
+        bad |= !(x[j] < INFINITY);
+        k = x[j] > m ? j : k;
+        m = fmaxf(x[j], m);
       }
-    }
-    reduce_cluster(best, best_q, drafts, most, s_slots, turn, C, rank);
+      return bad ? ~0ull : m > -INFINITY ? argmax_key(m + 0.f, base + (k / E * kWalk + tid) * E + k % E) : 0ull;
+    };
+    u64 best = most(l), best_q = drafts ? most(q) : 0ull;
+    reduce_cluster<false>(best, best_q, drafts, s_slots, turn, C, rank);
     if (best == 0 || best == ~0ull || (drafts && (best_q == 0 || best_q == ~0ull))) {
       if (rank == 0 && tid == 0) set_status(a.status, CDSL_ENONFINITE);
       break;
@@ -392,8 +427,7 @@ __global__ void __launch_bounds__(kWalk) k_tree_walk(VerifyArgs a) {
     int next = -1;
     if (greedy) {
       last = argmax_key_index(best);
-      for (int i = cur + 1; i < n && next < 0; ++i) {
-        if (s_par[i] != cur) continue;
+      for (int i = child(cur); i < kMaxT && next < 0; i = child(i)) {
         if (s_tok[i] == last) next = i;
         else if ((unsigned)s_tok[i] >= (unsigned)V && tid == 0) set_status(a.status, CDSL_ERANGE);
       }
@@ -416,7 +450,7 @@ __global__ void __launch_bounds__(kWalk) k_tree_walk(VerifyArgs a) {
         Zq += units_of(q[j]);
       }
     }
-    reduce_cluster(Z, Zq, drafts, sum, s_slots, turn, C, rank);
+    reduce_cluster<true>(Z, Zq, drafts, s_slots, turn, C, rank);
     float inv0 = 0.f, invq = 0.f;
     if (drafts) {                      // the distributions p and q
       inv0 = inverse(Z);
@@ -429,8 +463,7 @@ __global__ void __launch_bounds__(kWalk) k_tree_walk(VerifyArgs a) {
     }
     int rejected = 0;
     bool changed = false;              // the weights are no longer those of the last reduction
-    for (int i = cur + 1; i < n && next < 0; ++i) {
-      if (s_par[i] != cur) continue;
+    for (int i = child(cur); i < kMaxT && next < 0; i = child(i)) {
       const int x = s_tok[i];
       if ((unsigned)x >= (unsigned)V) {
         if (rank == 0 && tid == 0) set_status(a.status, CDSL_ERANGE);
@@ -438,20 +471,16 @@ __global__ void __launch_bounds__(kWalk) k_tree_walk(VerifyArgs a) {
       }
       if (!drafts) {
         uint32_t w = units_of(weight(s_lx[i], lm));
-        for (int r = 0; r < rejected; ++r)
-          if (s_out[r] == x) w = 0;
+        for (int r = child(cur); r < i; r = child(r))   // (a sibling's token has left the distribution)
+          if (s_tok[r] == x) w = 0;
         if (share_of(s_u[i], Z) < w) { next = i; break; }
         Z -= w;
-        __syncthreads();
-        if (tid == 0) s_out[rejected] = x;
-        ++rejected;
-        __syncthreads();
         changed = true;
         const int at = x - base;       // it leaves the distribution
-        if (x >= base && x < top && at % kWalk == tid)
+        if (x >= base && x < top && at / E % kWalk == tid)
 #pragma unroll
           for (int j = 0; j < J; ++j)
-            if (j == at / kWalk) W[j] = 0;
+            if (j == at / E / kWalk * E + at % E) W[j] = 0;
       } else {
         const float qx = __fmul_rn(weight(s_qx[i], qm), invq);
         float px = __fmul_rn(weight(s_lx[i], lm), inv0);
@@ -461,7 +490,7 @@ __global__ void __launch_bounds__(kWalk) k_tree_walk(VerifyArgs a) {
         u64 zr = 0, none = 0;
 #pragma unroll
         for (int j = 0; j < J; ++j) zr += units_of(fmaxf(__fsub_rn(l[j], q[j]), 0.f));
-        reduce_cluster(zr, none, false, sum, s_slots, turn, C, rank);
+        reduce_cluster<true>(zr, none, false, s_slots, turn, C, rank);
         if (zr) {
           const float inv = inverse(zr);
           Z = zr;
@@ -482,7 +511,7 @@ __global__ void __launch_bounds__(kWalk) k_tree_walk(VerifyArgs a) {
     }
     if (next >= 0) {
       cur = next;
-      __syncthreads();                 // (s_lx, s_out and s_inv of the next node)
+      __syncthreads();                 // (s_lx and s_inv of the next node)
       continue;
     }
     // ---- the first token whose running sum passes the draw: the block, the 32 tokens, the token
@@ -490,57 +519,67 @@ __global__ void __launch_bounds__(kWalk) k_tree_walk(VerifyArgs a) {
       u64 z = 0, none = 0;
 #pragma unroll
       for (int j = 0; j < J; ++j) z += W[j];
-      reduce_cluster(z, none, false, sum, s_slots, turn, C, rank);
+      reduce_cluster<true>(z, none, false, s_slots, turn, C, rank);
     }
-    u64 want = share_of(u_last, Z), mine = 0;
-    for (int i = 0; i < rank * kWalkWarps; ++i) want -= s_slots.v[turn][0][i];   // (wraps past 0: not this block's)
-    for (int i = 0; i < kWalkWarps; ++i) mine += s_slots.v[turn][0][rank * kWalkWarps + i];
+    u64 before = 0, mine = 0;
+    for (int i = lane; i < (rank + 1) * kWalkWarps; i += 32)
+      (i < rank * kWalkWarps ? before : mine) += s_slots.v[turn][0][i];
+    mine = warp_sum(mine);
+    const u64 want = share_of(u_last, Z) - warp_sum(before);   // (wraps past 0: not this block's)
     if ((long long)want < 0 || want >= mine) return;
 #pragma unroll
-    for (int j = 0; j < J; ++j) {
-      u64 z = W[j];
+    for (int j = 0; j < J; j += E) {
+      u64 z = 0;
 #pragma unroll
-      for (int o = 16; o > 0; o >>= 1) z += shfl_xor(z, o);
-      if (lane == 0) s_sum[j][warp] = z;
+      for (int e = 0; e < E; ++e) z += W[j + e];
+      z = warp_sum(z);
+      if (lane == 0) s_sum[j / E * kWalkWarps + warp] = z;
     }
     __syncthreads();
-    if (warp == 0) {                   // J / 2 sums a lane, in order
-      constexpr int PER = J * kWalkWarps / 32;
-      const u64* const mine_s = &s_sum[0][0] + lane * PER;
-      u64 own = 0;
-#pragma unroll
-      for (int i = 0; i < PER; ++i) own += mine_s[i];
-      u64 upto = own;
+    const auto scan = [&](u64 x) {     // the sum of the lanes' up to this one
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
-        const u64 t = __shfl_up_sync(0xffffffffu, upto, o);
-        if (lane >= o) upto += t;
+        const u64 t = __shfl_up_sync(0xffffffffu, x, o);
+        if (lane >= o) x += t;
       }
+      return x;
+    };
+    if (warp == 0) {                   // a few sums a lane, in order
+      constexpr int PER = (kSums + 31) / 32;
+      u64 own = 0;
+#pragma unroll
+      for (int i = 0; i < PER; ++i) own += lane * PER + i < kSums ? s_sum[lane * PER + i] : 0;
+      const u64 upto = scan(own);
       u64 at = upto - own;
       if (upto > want && at <= want) {
-        int i = 0;
-        while (at + mine_s[i] <= want) at += mine_s[i++];
-        s_at = lane * PER + i;
+        int i = lane * PER;
+        while (at + s_sum[i] <= want) at += s_sum[i++];
+        s_at = i;
         s_before = at;
       }
     }
     __syncthreads();
     if (warp == s_at % kWalkWarps) {
       const int jj = s_at / kWalkWarps;
-      uint32_t w = 0;
+      uint32_t w[E];
+      u64 own = 0;
 #pragma unroll
-      for (int j = 0; j < J; ++j)
-        if (j == jj) w = W[j];
-      u64 upto = w;
+      for (int e = 0; e < E; ++e) {
+        w[e] = 0;
 #pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const u64 t = __shfl_up_sync(0xffffffffu, upto, o);
-        if (lane >= o) upto += t;
+        for (int j = 0; j < J; j += E)
+          if (j / E == jj) w[e] = W[j + e];
+        own += w[e];
       }
-      upto += s_before;
-      if (upto > want && upto - w <= want) {
+      u64 upto = scan(own) + s_before, at = upto - own;
+      if (upto > want && at <= want) {
+        int v = base + (jj * kWalk + tid) * E;
+#pragma unroll
+        for (int e = 0; e < E - 1; ++e)
+          if ((at += w[e]) <= want) ++v;
+          else at = upto;
         a.n_path[b] = m;
-        a.emitted[(size_t)b * a.T + m - 1] = base + jj * kWalk + tid;
+        a.emitted[(size_t)b * a.T + m - 1] = v;
       }
     }
     return;
@@ -562,10 +601,14 @@ cudaError_t launch_verify(const VerifyArgs& a, int batch, cudaStream_t s) {
   auto go = [&](auto k) {
     return C == 1 ? launch_pdl(k, grid, block, 0, s, a) : launch_pdl_cluster(k, grid, block, 0, C, s, a);
   };
-  if (J <= 4) return go(k_tree_walk<T, 4>);
-  if (J <= 8) return go(k_tree_walk<T, 8>);
-  if (J <= 16) return go(k_tree_walk<T, 16>);
-  if (J <= 40) return go(k_tree_walk<T, 40>);
+  // 16 bytes a load where every row starts at 16
+  constexpr int E = 16 / sizeof(T);
+  const bool vec = (reinterpret_cast<uintptr_t>(a.logits) | reinterpret_cast<uintptr_t>(a.draft)) % 16 == 0 &&
+                   (a.sl[0] | a.sl[1] | (a.draft ? a.sd[0] | a.sd[1] : 0)) % E == 0;
+  if (J <= 4) return vec ? go(k_tree_walk<T, 4, 4>) : go(k_tree_walk<T, 4, 1>);
+  if (J <= 8) return vec ? go(k_tree_walk<T, 8, E>) : go(k_tree_walk<T, 8, 1>);
+  if (J <= 16) return vec ? go(k_tree_walk<T, 16, E>) : go(k_tree_walk<T, 16, 1>);
+  if (J <= 40) return vec ? go(k_tree_walk<T, 40, E>) : go(k_tree_walk<T, 40, 1>);
   return launch_pdl(k_tree_verify<T>, dim3(batch), dim3(kThreads), 0, s, a);
 }
 
