@@ -1,53 +1,61 @@
 // tree_attention.cu -- cdsl_tree_attention: the CUDA-core kernel (fp32 queries), the joining of
 // partial results and the entry points.
 //
-// k_tree_simt: 128 threads. Scores: a thread owns a slot of the chunk, reads its K row 16 bytes at a time
-// and multiplies it by the block's 16 query vectors, which shared memory broadcasts (fp32, scaled by
-// softmax scale * log2 e). Softmax: maxima over the warps, a running maximum and a sum that each thread
-// keeps of its own slots. P V: a thread owns a dimension (head_dim 64: of half the slots) and walks
-// the chunk's V rows. Bound by its fp32 FMAs and shared-memory broadcasts: 2 * 16 * head_dim products a
-// slot.
+// k_tree_simt: a warp has a run. Scores: a lane has four slots of the chunk and all of the block's eight query
+// vectors; it reads its K rows 16 bytes at a time, and shared memory broadcasts the queries (fp32, scaled by
+// softmax scale * log2 e), four vectors at a dimension: a broadcast serves eight FMAs of pairs. Softmax: maxima over the
+// warp, a running maximum, and sums that each lane keeps of its own slots. P V: a lane has hd / 32 dimensions of all
+// vectors and walks the chunk's V rows; a broadcast of a slot's four probabilities serves as many FMAs of pairs again
+// (half where hd is 64). Blocks of one warp have no barrier, and those on an SM cover one another's loads. Bound by its
+// fp32 FMAs where there are many vectors: 38 TFLOP/s, the FMA pipes 58 % busy, for a tree of 24 of 32 heads after
+// 32,768 tokens, 350 us (a slot's scores by a thread, of 16 vectors, by blocks of four warps: 882 us); by latency
+// where there are few: eight trees of 17 of 12 heads after 192 tokens in 19 us with the joining. Sixteen vectors a
+// warp, with half the K and V loads: 344 and 30 us.
 #include <cuda.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "tree_attention.cuh"
 #include "tree_host.h"
+#include "tree_tc.cuh"
 
 namespace cdsl {
 namespace tree {
 namespace {
 
-constexpr int SQ = 16;                         // query vectors per block
-constexpr int kThreads = kKeys;
-constexpr int kWarps = kThreads / 32;
-
-// 16 bytes of codes to floats.
+// Four codes (1 or 2 words) to floats.
 template <bool F8>
-__device__ __forceinline__ void decode16(const uint4& u, float (&x)[F8 ? 16 : 8]) {
-  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if constexpr (F8) {
-      const float2 a = f8x2_to_f32(w[i] & 0xffffu), b = f8x2_to_f32(w[i] >> 16);
-      x[4 * i] = a.x; x[4 * i + 1] = a.y; x[4 * i + 2] = b.x; x[4 * i + 3] = b.y;
-    } else {
-      x[2 * i] = __uint_as_float(w[i] << 16);
-      x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    }
+__device__ __forceinline__ void decode4(uint32_t u, uint32_t w, float (&x)[4]) {
+  if constexpr (F8) {
+    const float2 a = f8x2_to_f32(u & 0xffffu), b = f8x2_to_f32(u >> 16);
+    x[0] = a.x; x[1] = a.y; x[2] = b.x; x[3] = b.y;
+  } else {
+    x[0] = __uint_as_float(u << 16);
+    x[1] = __uint_as_float(u & 0xffff0000u);
+    x[2] = __uint_as_float(w << 16);
+    x[3] = __uint_as_float(w & 0xffff0000u);
   }
 }
 
+constexpr int SQ = 8;                          // query vectors per block
+// Resident warps of an SM, by registers (16 of bf16 rows of 128 spill: 182 us where 12 take 143, four trees of 49 of 40 heads
+// after 1024 tokens; e4m3: 46 us with 16, 59 with 12, a tree of 17 of 32 heads after 4096)
+constexpr int simt_per_sm(int HD, bool F8) { return HD == 128 && !F8 ? 12 : 16; }
+
 template <typename T, int HD, bool F8>
-__global__ void __launch_bounds__(kThreads) k_tree_simt(TreeArgs a) {
+__global__ void __launch_bounds__(32, simt_per_sm(HD, F8)) k_tree_simt(TreeArgs a) {
+  constexpr int EB = F8 ? 1 : 2, CPL = 16 / EB, LOADS = HD / CPL;   // codes in 16 bytes
+  constexpr int DPL = HD / 32;                 // dimensions of a lane
+  constexpr int AHEAD = DPL * EB > 4 ? 8 : 16; // V rows loaded together
+  using VBits = std::conditional_t<DPL * EB == 8, uint2, std::conditional_t<DPL * EB == 4, uint32_t, uint16_t>>;
   extern __shared__ int s_first[];             // [batch + 1]
-  __shared__ __align__(16) float s_q[SQ][HD], s_p[SQ][kKeys];
-  __shared__ float s_max[kWarps][SQ], s_sum[kWarps][SQ];
-  __shared__ uint32_t s_mask[SQ][kWords];
-  __shared__ uint32_t s_row[kKeys];            // V row of each slot of the chunk, ~0: none
-  constexpr int CPL = F8 ? 16 : 8;             // codes per 16 bytes
-  constexpr int SPLIT = kThreads / HD;         // threads per dimension
-  const int tid = threadIdx.x, warp = tid >> 5;
+  constexpr int ROW = SQ + 4;                  // floats (48 or 80 bytes: eight lanes' 16 bytes take all banks)
+  __shared__ __align__(16) float s_q[HD][ROW];
+  __shared__ __align__(16) float s_p[kKeys][ROW];   // slot k in row k % 4 * 32 + k / 4
+  __shared__ float s_m[SQ];
+  __shared__ uint32_t s_mask[SQ][kWords + 1];
+  const int lane = threadIdx.x;
   const Cache& c = a.c;
   pdl_wait();
   pdl_launch_dependents();
@@ -56,149 +64,238 @@ __global__ void __launch_bounds__(kThreads) k_tree_simt(TreeArgs a) {
   const int total = s_first[c.batch], runs = runs_of(a, total);
   if ((int)blockIdx.x >= runs) return;
   const int end = run_begin(blockIdx.x + 1, total, runs);
+  const size_t row0 = row_of(c, a.layer, 0, 0, 0, 0);
   for (int unit = run_begin(blockIdx.x, total, runs); unit < end;) {
     const Segment s = segment_at(a, s_first, unit, end);
-    __syncthreads();                           // (the segment before is done with shared memory)
-    for (int i = tid; i < SQ * HD; i += kThreads) {
-      const int v = i / HD, d = i % HD;
-      float x = 0.f;
-      if (v < s.nq) {
+    __syncwarp();                              // (the segment before is done with shared memory)
+    {
+      float x[SQ][DPL];
+#pragma unroll
+      for (int v = 0; v < SQ; ++v) {
         const Vec w = vector_of(a, s.h, s.qb, v);
-        x = to_f32<T>(static_cast<const T*>(a.q)[s.b * a.sq[0] + w.t * a.sq[1] + w.h * a.sq[2] + d]) * a.scale;
+        const T* const q = static_cast<const T*>(a.q) + s.b * a.sq[0] + w.t * a.sq[1] + w.h * a.sq[2] + lane;
+#pragma unroll
+        for (int i = 0; i < DPL; ++i) x[v][i] = v < s.nq ? to_f32<T>(__ldg(q + i * 32)) * a.scale : 0.f;
       }
-      s_q[v][d] = x;
+#pragma unroll
+      for (int i = 0; i < DPL; ++i)
+#pragma unroll
+        for (int v = 0; v < SQ; v += 4)
+          *reinterpret_cast<float4*>(&s_q[i * 32 + lane][v]) = make_float4(x[v][i], x[v + 1][i], x[v + 2][i], x[v + 3][i]);
     }
-    for (int i = tid; i < SQ * kWords; i += kThreads) {
-      const int v = i / kWords, w = i % kWords;
+    for (int i = lane; i < SQ * (kWords + 1); i += 32) {
+      const int v = i / (kWords + 1), w = i % (kWords + 1);
       s_mask[v][w] = v < s.nq && w < a.W
                          ? __ldg(a.mask + ((size_t)s.b * a.T + vector_of(a, s.h, s.qb, v).t) * a.W + w) : 0u;
     }
-    __syncthreads();
-    float m[SQ], l[SQ], o[SQ];
+    if (lane < SQ) s_m[lane] = -INFINITY;
+    __syncwarp();
+    float l[SQ];
+    uint64_t o[SQ / 2][DPL];                   // of two vectors each
 #pragma unroll
-    for (int v = 0; v < SQ; ++v) { m[v] = -INFINITY; l[v] = o[v] = 0.f; }
+    for (int v = 0; v < SQ; ++v) l[v] = 0.f;
+#pragma unroll
+    for (int v = 0; v < SQ / 2; ++v)
+#pragma unroll
+      for (int i = 0; i < DPL; ++i) o[v][i] = 0ull;
     for (int ch = s.c0; ch < s.c1; ++ch) {
-      const int slot = ch * kKeys + tid;
-      // ---- scores of this thread's slot
-      int page = -1;
-      if (slot < s.keys) {
+      // ---- scores of this lane's slots (four of a page: pages have 16 at least)
+      const int slot = ch * kKeys + 4 * lane;
+      int n = min(max(s.keys - slot, 0), 4), page = -1;   // n: of them that there are
+      if (n > 0) {
         page = page_of(c, s.b, slot);
-        if (page < 0) set_status(a.status, CDSL_ERANGE);
+        if (page < 0) {
+          set_status(a.status, CDSL_ERANGE);
+          n = 0;
+        }
       }
-      float t[SQ], vs = 0.f;
+      const int at = slot & ((1 << c.page_shift) - 1);
+      const size_t row = page >= 0 ? row_of(c, a.layer, page, 0, s.h, at) : row0;
+      const size_t vrow = page >= 0 ? row_of(c, a.layer, page, 1, s.h, at) : row0;
+      const uint32_t ks4 = *reinterpret_cast<const uint32_t*>(c.scale + row);   // (slots past the item's: not used)
+      const uint32_t vs4 = *reinterpret_cast<const uint32_t*>(c.scale + vrow);
+      const uint8_t* const k = c.pool + row * HD * EB;
+      uint64_t t[SQ / 2][4];
 #pragma unroll
-      for (int v = 0; v < SQ; ++v) t[v] = 0.f;
-      s_row[tid] = ~0u;
-      if (page >= 0) {
-        const int at = slot & ((1 << c.page_shift) - 1);
-        const size_t row = row_of(c, a.layer, page, 0, s.h, at);
-        const size_t vrow = row_of(c, a.layer, page, 1, s.h, at);
-        s_row[tid] = (uint32_t)(vrow - row_of(c, a.layer, 0, 0, 0, 0));
-        const uint4* k = reinterpret_cast<const uint4*>(c.pool + row * HD * (F8 ? 1 : 2));
-        constexpr int LOADS = HD / CPL, AHEAD = LOADS < 8 ? LOADS : 8;   // in flight together
+      for (int v = 0; v < SQ / 2; ++v)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) t[v][e] = 0ull;
+      uint4 next[4];
+      auto load_k = [&](int i) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          next[e] = e < n ? __ldg(reinterpret_cast<const uint4*>(k + e * HD * EB) + i) : make_uint4(0u, 0u, 0u, 0u);
+      };
+      load_k(0);
 #pragma unroll 1
-        for (int i0 = 0; i0 < LOADS; i0 += AHEAD) {
-          uint4 raw[AHEAD];
+      for (int i = 0; i < LOADS; ++i) {
+        uint32_t raw[4][4];
 #pragma unroll
-          for (int i = 0; i < AHEAD; ++i) raw[i] = __ldg(k + i0 + i);
+        for (int e = 0; e < 4; ++e) {
+          raw[e][0] = next[e].x; raw[e][1] = next[e].y; raw[e][2] = next[e].z; raw[e][3] = next[e].w;
+        }
+        if (i + 1 < LOADS) load_k(i + 1);
 #pragma unroll
-          for (int i = 0; i < AHEAD; ++i) {
-            float x[CPL];
-            decode16<F8>(raw[i], x);
+        for (int j = 0; j < 4; j += EB) {      // four dimensions
+          float x[4][4];
 #pragma unroll
-            for (int v = 0; v < SQ; ++v)
+          for (int e = 0; e < 4; ++e) decode4<F8>(raw[e][j], raw[e][j + EB - 1], x[e]);
 #pragma unroll
-              for (int e = 0; e < CPL; e += 4) {
-                const float4 q = *reinterpret_cast<const float4*>(&s_q[v][(i0 + i) * CPL + e]);
-                t[v] = fmaf(q.x, x[e], fmaf(q.y, x[e + 1], fmaf(q.z, x[e + 2], fmaf(q.w, x[e + 3], t[v]))));
+          for (int d = 0; d < 4; ++d) {
+            uint64_t xx[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) xx[e] = pair(x[e][d], x[e][d]);
+#pragma unroll
+            for (int v = 0; v < SQ; v += 4) {
+              const ulonglong2 q = *reinterpret_cast<const ulonglong2*>(&s_q[i * CPL + j * 4 / EB + d][v]);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                t[v / 2][e] = fma2(q.x, xx[e], t[v / 2][e]);
+                t[v / 2 + 1][e] = fma2(q.y, xx[e], t[v / 2 + 1][e]);
               }
+            }
           }
         }
-        const float ks = scale_value(c.scale[row]);
-        vs = scale_value(c.scale[vrow]);
-#pragma unroll
-        for (int v = 0; v < SQ; ++v) t[v] *= ks;
       }
-      // ---- masks, maxima
-      const int node = slot - s.len;
-      uint32_t vis = 0;
+      // ---- masks, maxima, probabilities
+      float ks[4], vs[4];
 #pragma unroll
-      for (int v = 0; v < SQ; ++v) {
-        const bool ok = page >= 0 && v < s.nq && (node < 0 || (s_mask[v][node >> 5] >> (node & 31) & 1));
-        vis |= (uint32_t)ok << v;
-        const float wm = warp_max(ok ? t[v] : -INFINITY);
-        if ((tid & 31) == 0) s_max[warp][v] = wm;
+      for (int e = 0; e < 4; ++e) {
+        ks[e] = e < n ? scale_value(ks4 >> (8 * e) & 255) : 1.f;
+        vs[e] = e < n ? scale_value(vs4 >> (8 * e) & 255) : 0.f;
       }
-      __syncthreads();
+      const int node = slot - s.len;           // the tree's node in the first slot
+      const bool masked = __any_sync(0xffffffffu, node > -4 || n < 4);
 #pragma unroll
-      for (int v = 0; v < SQ; ++v) {
-        float mn = m[v];
+      for (int v4 = 0; v4 < SQ; v4 += 4) {
+        float p[4][4];                         // [slot][vector]
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) mn = fmaxf(mn, s_max[w][v]);
-        const float alpha = m[v] == -INFINITY ? 0.f : exp2f(m[v] - mn);
-        m[v] = mn;
-        // NaN scores (a NaN row) survive: they are visible, and fmaxf left them out of the maximum
-        const float p = vis >> v & 1 ? exp2f(t[v] - (mn == -INFINITY ? 0.f : mn)) : 0.f;
-        l[v] = l[v] * alpha + p;
-        o[v] *= alpha;
-        s_p[v][tid] = vis >> v & 1 ? p * vs : 0.f;   // V's scale; what a row sees as NaN stays NaN
+        for (int u = 0; u < 4; ++u) {
+          const int v = v4 + u;
+          uint32_t seen = 15u;
+          if (masked) {
+            if (node >= 0) {
+              const int w = min(node >> 5, kWords - 1);
+              seen = node < 32 * kWords ? __funnelshift_r(s_mask[v][w], s_mask[v][w + 1], node & 31) : 0u;
+            } else if (node > -4) {
+              seen = ((1u << -node) - 1) | s_mask[v][0] << -node;
+            }
+            seen &= (1u << n) - 1;
+            if (v >= s.nq) seen = 0u;
+          }
+          float x[4], top = -INFINITY;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float2 two = unpair(t[v / 2][e]);
+            x[e] = (u % 2 ? two.y : two.x) * ks[e];
+            if (!masked || seen >> e & 1) top = fmaxf(top, x[e]);
+          }
+          const float m = s_m[v], mn = fmaxf(m, warp_fmax(top));
+          float alpha = 1.f;
+          if (mn != m) {                       // (alike in all lanes)
+            alpha = m == -INFINITY ? 0.f : exp2f(m - mn);
+            const uint64_t both = u % 2 ? pair(1.f, alpha) : pair(alpha, 1.f);
+#pragma unroll
+            for (int i = 0; i < DPL; ++i) o[v / 2][i] = mul2(o[v / 2][i], both);
+            l[v] *= alpha;
+            __syncwarp();
+            if (lane == 0) s_m[v] = mn;
+          }
+          // NaN scores (a NaN row) survive: they are visible, and fmaxf left them out of the maximum
+          const float off = mn == -INFINITY ? 0.f : mn;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const bool see = !masked || seen >> e & 1;
+            const float y = see ? exp2f(x[e] - off) : 0.f;
+            l[v] += y;
+            p[e][u] = see ? y * vs[e] : 0.f;   // V's scale; what a row sees as NaN stays NaN
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          *reinterpret_cast<float4*>(&s_p[e * 32 + lane][v4]) = make_float4(p[e][0], p[e][1], p[e][2], p[e][3]);
       }
-      __syncthreads();
-      // ---- P V of this thread's dimension (and share of the slots)
-      const int d = tid % HD, k0 = tid / HD * (kKeys / SPLIT);
-      const int kn = min(s.keys - ch * kKeys, k0 + kKeys / SPLIT);
-      const uint8_t* const pool = c.pool + row_of(c, a.layer, 0, 0, 0, 0) * HD * (F8 ? 1 : 2);
+      __syncwarp();
+      // ---- P V of this lane's dimensions (16 slots of a page at a time)
+      const int kn = min(s.keys - ch * kKeys, kKeys);
+      const uint32_t mine = page >= 0 ? (uint32_t)(vrow - row0) : ~0u;
+      VBits ahead[AHEAD];
+      auto load_v = [&](int k0) {
+        const uint32_t first = __shfl_sync(0xffffffffu, mine, k0 / 4 & 31);
+        const VBits* const v = reinterpret_cast<const VBits*>(c.pool + (row0 + first) * HD * EB) + lane;
+#pragma unroll
+        for (int e = 0; e < AHEAD; ++e)
+          ahead[e] = first != ~0u && k0 + e < kn ? __ldg(v + e * 32) : VBits{};
+      };
+      load_v(0);
 #pragma unroll 1
-      for (int k = k0; k < kn; k += 16) {      // 16 slots' loads in flight
-        float x[16];
+      for (int k0 = 0; k0 < kn; k0 += AHEAD) {
+        VBits raw[AHEAD];
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const uint32_t row = s_row[k + e];
-          x[e] = 0.f;
-          if (k + e < kn && row != ~0u) {
-            const uint8_t* v = pool + (size_t)row * HD * (F8 ? 1 : 2);
-            x[e] = F8 ? f8x2_to_f32(__ldg(v + d)).x
-                      : __uint_as_float((uint32_t)__ldg(reinterpret_cast<const uint16_t*>(v) + d) << 16);
+        for (int e = 0; e < AHEAD; ++e) raw[e] = ahead[e];
+        if (k0 + AHEAD < kn) load_v(k0 + AHEAD);
+#pragma unroll
+        for (int e = 0; e < AHEAD; e += 4) {
+          float x[4][DPL];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            if constexpr (DPL == 4 && F8) {
+              decode4<true>(raw[e + i], 0u, x[i]);
+            } else if constexpr (DPL == 4) {
+              decode4<false>(raw[e + i].x, raw[e + i].y, x[i]);
+            } else if constexpr (F8) {
+              const float2 y = f8x2_to_f32(raw[e + i]);
+              x[i][0] = y.x; x[i][1] = y.y;
+            } else {
+              x[i][0] = __uint_as_float(raw[e + i] << 16);
+              x[i][1] = __uint_as_float(raw[e + i] & 0xffff0000u);
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            uint64_t xx[DPL];
+#pragma unroll
+            for (int d = 0; d < DPL; ++d) xx[d] = pair(x[i][d], x[i][d]);
+#pragma unroll
+            for (int v = 0; v < SQ; v += 4) {
+              const ulonglong2 p = *reinterpret_cast<const ulonglong2*>(&s_p[i * 32 + (k0 + e) / 4][v]);
+#pragma unroll
+              for (int d = 0; d < DPL; ++d) {
+                o[v / 2][d] = fma2(p.x, xx[d], o[v / 2][d]);
+                o[v / 2 + 1][d] = fma2(p.y, xx[d], o[v / 2 + 1][d]);
+              }
+            }
           }
         }
-#pragma unroll
-        for (int v = 0; v < SQ; ++v)
-#pragma unroll
-          for (int e = 0; e < 16; e += 4) {
-            const float4 p = *reinterpret_cast<const float4*>(&s_p[v][k + e]);
-            o[v] = fmaf(p.x, x[e], fmaf(p.y, x[e + 1], fmaf(p.z, x[e + 2], fmaf(p.w, x[e + 3], o[v]))));
-          }
       }
-      __syncthreads();
+      __syncwarp();
     }
-    // ---- the threads' sums, and the halves' outputs of a dimension
-#pragma unroll
-    for (int v = 0; v < SQ; ++v) {
-      const float ws = warp_sum(l[v]);
-      if ((tid & 31) == 0) s_sum[warp][v] = ws;
-      if (SPLIT > 1) s_p[v][tid] = o[v];
-    }
-    __syncthreads();
     const bool whole = s.c0 == 0 && s.c1 == s.units;
     const size_t slot = (size_t)blockIdx.x * 2 + (s.c0 == 0);
     const int live = min(SQ, a.T * a.G - s.qb * SQ);
 #pragma unroll
     for (int v = 0; v < SQ; ++v) {
-      if (v >= live || tid >= HD) break;
-      float sum = 0.f;
+      const bool any = v < s.nq;               // (a vector past the nodes: zeros)
+      const float sum = any ? warp_sum(l[v]) : 0.f, m = any ? s_m[v] : -INFINITY;
+      if (v < live) {
+        float x[DPL];
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) sum += s_sum[w][v];
-      float x = o[v];
-      if (SPLIT > 1) x += s_p[v][tid + HD];
-      if (whole) {
-        const Vec w = vector_of(a, s.h, s.qb, v);
-        store_out<T>(a, s.b, w, tid, sum == 0.f ? 0.f : x / sum);
-        if (tid == 0) store_lse(a, s.b, w, m[v], sum);
-      } else {
-        a.part_o[(slot * SQ + v) * HD + tid] = x;
-        if (tid == 0) {
-          a.part_ml[(slot * 2) * SQ + v] = m[v];
-          a.part_ml[(slot * 2 + 1) * SQ + v] = sum;
+        for (int i = 0; i < DPL; ++i) {
+          const float2 two = unpair(o[v / 2][i]);
+          x[i] = v % 2 ? two.y : two.x;
+        }
+        if (whole) {
+          const Vec w = vector_of(a, s.h, s.qb, v);
+#pragma unroll
+          for (int i = 0; i < DPL; ++i) store_out<T>(a, s.b, w, lane * DPL + i, sum == 0.f ? 0.f : x[i] / sum);
+          if (lane == 0) store_lse(a, s.b, w, m, sum);
+        } else {
+#pragma unroll
+          for (int i = 0; i < DPL; ++i) a.part_o[(slot * SQ + v) * HD + lane * DPL + i] = any ? x[i] : 0.f;
+          if (lane == 0) {
+            a.part_ml[(slot * 2) * SQ + v] = m;
+            a.part_ml[(slot * 2 + 1) * SQ + v] = sum;
+          }
         }
       }
     }
@@ -293,13 +390,11 @@ struct Sizes {
   int NQ, QB, blocks;
   size_t o_off, bytes;
 };
-constexpr int kSimtPerSM = 4;                  // resident k_tree_simt blocks per SM
-
 void sizes_of(const Cache& c, bool tc, int H, int T, Sizes* z) {
   const int vectors = T * (H / c.kvh);
   z->NQ = !tc ? SQ : vectors <= 16 ? 16 : vectors <= 32 ? 32 : kRowsBlock;
   z->QB = (vectors + z->NQ - 1) / z->NQ;
-  z->blocks = kPlanSMs * (!tc ? kSimtPerSM : z->NQ == kRowsBlock ? 1 : tc_blocks_per_sm(c, z->NQ));
+  z->blocks = kPlanSMs * (!tc ? simt_per_sm(c.hd, c.eb == 1) : z->NQ == kRowsBlock ? 1 : tc_blocks_per_sm(c, z->NQ));
   const size_t slots = (size_t)z->blocks * 2 * z->NQ;
   auto up = [](size_t n) { return (n + 255) / 256 * 256; };
   z->o_off = up(slots * 2 * sizeof(float));
@@ -314,7 +409,7 @@ cudaError_t launch_combine(const TreeArgs& a, cudaStream_t s) {
 
 template <typename T, int HD, bool F8>
 cudaError_t launch_simt(const TreeArgs& a, cudaStream_t s) {
-  return launch_pdl(k_tree_simt<T, HD, F8>, dim3(a.blocks), dim3(kThreads), (a.c.batch + 1) * 4, s, a);
+  return launch_pdl(k_tree_simt<T, HD, F8>, dim3(a.blocks), dim3(32), (a.c.batch + 1) * 4, s, a);
 }
 
 cudaError_t launch_pass(const TreeArgs& a, bool tc, bool split, cudaStream_t s) {
