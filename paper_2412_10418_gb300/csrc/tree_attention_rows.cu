@@ -18,12 +18,21 @@
 //
 // Two groups of four softmax warps take alternate chunks, so that one's exponentials run beside the other's
 // maxima; S, which P then overwrites, has three buffers in TMEM, so that neither waits for its next one (with two,
-// and an O for each group, a chunk took 3,100 cycles, of them half waiting). O is one chain over the chunks: fp16's range
+// and an O for each group, half of a chunk's time was waiting). O is one chain over the chunks: fp16's range
 // leaves P exact enough under a reference that is raised only when a maximum passes it by more than 2^kMargin,
 // which after the first chunk is rare; then the thread multiplies its O. A row's reference goes from chunk to chunk, and
 // so from group to group, through shared memory. (O started anew in every chunk and was added up in registers before:
 // eight more warps, and a chain of waits through them that held a chunk to 3,500 cycles.) Four warps convert V, one
-// loads, one issues MMAs, one turns scale bytes into factors.
+// loads, one issues MMAs, one turns scale bytes into factors. A bf16 cache has shared memory for two stages only:
+// there K and the scale bytes are loaded a chunk ahead of V, or S would wait for the V of a chunk before (36 vectors,
+// 8 sequences of 16,384 tokens, 8 heads: 191 -> 123 us; with three stages of e4m3 it loses 5 %).
+//
+// Measured: 8 trees of 25 nodes, 100 vectors a K/V head, up to 32,768 tokens of 8 heads of 128 in e4m3: 155 us,
+// 390 TFLOP/s, 39 % of the copy bandwidth. A chunk takes 3,000 cycles, of which its MMAs need 1,024; a softmax
+// thread spends 1,300 on the maxima, 2,000 on the probabilities, 1,000 on the reference's way through its group and the
+// other, mostly latency of TMEM (166 cycles a load) and of shared memory, which the MMAs' operands, the conversion and
+// the factors together keep busy for 1,900. At 33 vectors (the same chunk's time) 8 sequences of 16,384 take 101 us;
+// two blocks of 32 on tree_attention_tc.cu 114. At 32, 67 there and 94 here.
 #include <cuda.h>
 
 #include <algorithm>
@@ -99,7 +108,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (int i = 0; i < NST; ++i) {
       tc::mbar_init(&k_full[i], 1);
       tc::mbar_init(&v_full[i], 1);
-      tc::mbar_init(&k_empty[i], 1);
+      tc::mbar_init(&k_empty[i], F8 ? 1 : 2);  // (the scale bytes' reader arrives where they came)
       tc::mbar_init(&v_empty[i], F8 ? kConv + 1 : 1);
       tc::mbar_init(&f_full[i], 32);
       tc::mbar_init(&f_empty[i], kRows);
@@ -134,7 +143,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t t_o = tmem + kBuf * kKeys;
 
   if (warp == kProducer) {
-    load_chunks<HD, F8, NST>(a, s_first, begin, end, map, sm + C::KV_OFF, sm + C::SCALE_OFF, s_pieces, k_full,
+    load_chunks<HD, F8, NST, !F8>(a, s_first, begin, end, map, sm + C::KV_OFF, sm + C::SCALE_OFF, s_pieces, k_full,
                              v_full, k_empty, v_empty);
   } else if (warp == kIssuer) {
     if (lane == 0) {
@@ -215,7 +224,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       int vref = 0;
       for (int ch = s.c0; ch < s.c1 && ok; ++ch, ++it) {
         const int st = it % NST;
-        ok = __all_sync(0xffffffffu, tc::mbar_wait(&v_full[st], parity(it, NST), a.status) &&
+        ok = __all_sync(0xffffffffu, tc::mbar_wait(F8 ? &v_full[st] : &k_full[st], parity(it, NST), a.status) &&
                                          tc::mbar_wait(&f_empty[st], parity(it, NST) ^ 1, a.status));
         if (!ok) break;
         // a lane has slots 4 lane .. 4 lane + 3
@@ -261,10 +270,12 @@ __global__ void __launch_bounds__(kThreads, 1)
           s_vref[st] = F8 ? vref : 127;
           s_vstep[st] = F8 && before ? before - vref : 0;
         }
-        if (F8) {
-          __syncwarp();
-          if (lane == 0) tc::mbar_arrive(&v_empty[st]);             // (the scale bytes are read)
-        } else if (n < 4) {                    // nothing of their V rows (page garbage, no copy) may reach the sums
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(F8 ? &v_empty[st] : &k_empty[st]);   // (the scale bytes are read)
+        if (!F8 && __any_sync(0xffffffffu, n < 4))
+          ok = __all_sync(0xffffffffu, tc::mbar_wait(&v_full[st], parity(it, NST), a.status));
+        if (!ok) break;
+        if (!F8 && n < 4) {                    // nothing of their V rows (page garbage, no copy) may reach the sums
 #pragma unroll 1
           for (int e = n; e < 4; ++e) {
             uint8_t* v = sm + C::KV_OFF + (st * 2 + 1) * C::TILE + (4 * lane + e) * C::BW;

@@ -175,9 +175,10 @@ __device__ __forceinline__ void stage_masks(const TreeArgs& a, const Segment& s,
 }
 
 // The loading warp: K and V chunks of a run's segments into a ring of NST stages (tiles of kKeys rows in blocks
-// of at most 128 bytes, swizzled as their rows are wide), a box per page piece, and with V the slots' scale
-// bytes and which pieces there are. Waits are bounded; on expiry it returns with its copies landed.
-template <int HD, bool F8, int NST>
+// of at most 128 bytes, swizzled as their rows are wide), a box per page piece, and the slots' scale bytes and which
+// pieces there are, with V; EARLY: with K, and K a chunk ahead of V, whose stage comes free later. Waits are bounded; on
+// expiry it returns with its copies landed.
+template <int HD, bool F8, int NST, bool EARLY>
 __device__ __forceinline__ void load_chunks(const TreeArgs& a, const int* first, int begin, int end,
                                             const CUtensorMap& map, uint8_t* ring, uint8_t* scales,
                                             uint32_t* s_pieces, uint64_t* k_full, uint64_t* v_full,
@@ -187,48 +188,62 @@ __device__ __forceinline__ void load_chunks(const TreeArgs& a, const int* first,
   const Cache& c = a.c;
   const int lane = threadIdx.x & 31, P = 1 << c.page_shift;
   const int rows = min(P, kKeys), pieces = kKeys / rows;
-  int it = 0, issued[2] = {0, 0};              // chunks, and copies of K and of V
+  struct Chunk {
+    int page, h, at;                           // this lane's piece
+    uint32_t live;
+  };
+  int issued[2] = {0, 0};                      // copies of K and of V
+  auto issue = [&](int kv, int it, const Chunk& x) {
+    const int st = it % NST;
+    uint64_t* full = kv ? &v_full[st] : &k_full[st];
+    if (!__all_sync(0xffffffffu, tc::mbar_wait(kv ? &v_empty[st] : &k_empty[st], parity(it, NST) ^ 1, a.status)))
+      return false;
+    const bool bytes = kv == (EARLY ? 0 : 1);  // both scale bytes too
+    if (lane == 0) {
+      if (bytes) s_pieces[st] = x.live;
+      tc::mbar_expect_tx(full, __popc(x.live) * rows * (KROW + (bytes ? 2 : 0)));
+    }
+    __syncwarp();
+    if (x.page >= 0) {
+      const int y = (int)row_of(c, 0, x.page, kv, x.h, x.at);
+      uint8_t* dst = ring + (st * 2 + kv) * TILE + lane * rows * BW;
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) tc::tma_load_2d(dst + nb * BLOCK, &map, nb * (BW / EB), y, full);
+      if (bytes) {
+        const uint8_t* from = c.scale + row_of(c, a.layer, x.page, 0, x.h, x.at);
+        uint8_t* to = scales + st * 2 * kKeys + lane * rows;
+        tc::bulk_load(to, from, rows, full);
+        tc::bulk_load(to + kKeys, from + ((size_t)c.kvh << c.page_shift), rows, full);
+      }
+    }
+    if (kv) issued[1] = it + 1;
+    else issued[0] = it + 1;
+    return true;
+  };
+  int it = 0;                                  // chunks
   bool ok = true;
+  Chunk before = {};
   for (int unit = begin; unit < end && ok;) {
     const Segment s = segment_at(a, first, unit, end);
     for (int ch = s.c0; ch < s.c1 && ok; ++ch, ++it) {
-      const int st = it % NST;
       const int slot = ch * kKeys + lane * rows;
-      int page = -1;
+      Chunk x = {-1, s.h, slot & (P - 1), 0u};
       if (lane < pieces && slot < s.keys) {
-        page = page_of(c, s.b, slot);
-        if (page < 0) set_status(a.status, CDSL_ERANGE);
+        x.page = page_of(c, s.b, slot);
+        if (x.page < 0) set_status(a.status, CDSL_ERANGE);
       }
-      const uint32_t live = __ballot_sync(0xffffffffu, page >= 0), n = __popc(live) * rows;
-#pragma unroll 1
-      for (int kv = 0; kv < 2; ++kv) {
-        uint64_t* full = kv ? &v_full[st] : &k_full[st];
-        ok = ok && __all_sync(0xffffffffu, tc::mbar_wait(kv ? &v_empty[st] : &k_empty[st], parity(it, NST) ^ 1,
-                                                         a.status));
-        if (!ok) break;
-        if (lane == 0) {
-          if (kv) s_pieces[st] = live;
-          tc::mbar_expect_tx(full, n * (KROW + 2 * kv));
-        }
-        __syncwarp();
-        if (page >= 0) {
-          const int y = (int)row_of(c, 0, page, kv, s.h, slot & (P - 1));
-          uint8_t* dst = ring + (st * 2 + kv) * TILE + lane * rows * BW;
-#pragma unroll
-          for (int nb = 0; nb < NB; ++nb) tc::tma_load_2d(dst + nb * BLOCK, &map, nb * (BW / EB), y, full);
-          if (kv) {                            // both scale bytes
-            const uint8_t* from = c.scale + row_of(c, a.layer, page, 0, s.h, slot & (P - 1));
-            uint8_t* to = scales + st * 2 * kKeys + lane * rows;
-            tc::bulk_load(to, from, rows, full);
-            tc::bulk_load(to + kKeys, from + ((size_t)c.kvh << c.page_shift), rows, full);
-          }
-        }
-        if (kv) issued[1] = it + 1;
-        else issued[0] = it + 1;
+      x.live = __ballot_sync(0xffffffffu, x.page >= 0);
+      ok = issue(0, it, x);
+      if (EARLY) {
+        if (it > 0) ok = ok && issue(1, it - 1, before);
+        before = x;
+      } else {
+        ok = ok && issue(1, it, x);
       }
     }
     unit += s.c1 - s.c0;
   }
+  if (EARLY && it > 0) ok = ok && issue(1, it - 1, before);
   // where a role gave up, nothing may have waited for the copies
   if (!ok)
 #pragma unroll
