@@ -6,7 +6,10 @@
 // a code's value is the same in bf16, fp32 and 64 bits, and the attention folds it into scores and
 // probabilities without a rounding.
 //
-// All three are bound by HBM on large calls and by one launch on a decoding step's few rows.
+// All three are bound by HBM on large calls and by one launch on a decoding step's few rows. A lane of the first
+// two has 16 values, so that a row's few dependent loads (its start, its page, its values) are waited for half as often
+// as with 8: rows of 4 prompts of 1031 tokens, 8 heads of 128, bf16 to e4m3: 8.6 us written (25 MB, 10.1 with 8
+// values), 9.3 us read; a tree of 17 nodes 3.5 us in a graph.
 #include <cuda.h>
 
 #include <algorithm>
@@ -21,7 +24,7 @@ namespace tree {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int EPL = 8;                 // values per lane: a row is head_dim / 8 lanes
+constexpr int EPL = 16;                // values per lane: a row is head_dim / 16 lanes
 
 struct RowsArgs {
   Cache c;
@@ -35,23 +38,37 @@ struct RowsArgs {
 template <typename T>
 __device__ __forceinline__ void load_values(const T* p, bool aligned, float (&x)[EPL]) {
   if (aligned) {
-    if constexpr (sizeof(T) == 2) {
-      const uint4 u = __ldg(reinterpret_cast<const uint4*>(p));
+    constexpr int N = 16 / sizeof(T);  // 16 bytes at a time
+#pragma unroll
+    for (int j = 0; j < EPL; j += N) {
+      const uint4 u = *reinterpret_cast<const uint4*>(p + j);
       const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        x[2 * i] = __uint_as_float(w[i] << 16);
-        x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        if constexpr (N == 8) {
+          x[j + 2 * i] = __uint_as_float(w[i] << 16);
+          x[j + 2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        } else {
+          x[j + i] = __uint_as_float(w[i]);
+        }
       }
-    } else {
-      const float4 a = __ldg(reinterpret_cast<const float4*>(p));
-      const float4 b = __ldg(reinterpret_cast<const float4*>(p) + 1);
-      x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
-      x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
     }
   } else {
 #pragma unroll
     for (int i = 0; i < EPL; ++i) x[i] = to_f32<T>(p[i]);
+  }
+}
+// EPL values as bf16 to an address that is a multiple of 16 bytes; zeros: zeros in their place.
+__device__ __forceinline__ void store_bf16(void* p, const float (&x)[EPL], bool zeros) {
+#pragma unroll
+  for (int j = 0; j < EPL; j += 8) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const __nv_bfloat162 y = __floats2bfloat162_rn(x[j + 2 * i], x[j + 2 * i + 1]);
+      w[i] = zeros ? 0u : *reinterpret_cast<const uint32_t*>(&y);
+    }
+    reinterpret_cast<uint4*>(p)[j / 8] = make_uint4(w[0], w[1], w[2], w[3]);
   }
 }
 
@@ -63,7 +80,7 @@ struct WriteArgs {
   bool aligned;
 };
 
-// Grid: (rows of a sequence over blocks, batch). LPR = head_dim / 8 lanes work on a row.
+// Grid: (rows of a sequence over blocks, batch). LPR = head_dim / 16 lanes work on a row.
 template <typename T, int LPR, bool F8>
 __global__ void __launch_bounds__(kThreads) k_kv_write(WriteArgs a) {
   pdl_wait();
@@ -73,14 +90,14 @@ __global__ void __launch_bounds__(kThreads) k_kv_write(WriteArgs a) {
   const unsigned row = (blockIdx.x * kThreads + threadIdx.x) / LPR;
   const int part = threadIdx.x % LPR;
   const unsigned h = row % c.kvh, kv = row / c.kvh & 1, t = row / c.kvh / 2;
-  const int n = a.r.count ? min(__ldg(a.r.count + b), a.r.T) : a.r.T;
+  const int n = a.r.count ? min(a.r.count[b], a.r.T) : a.r.T;
   if ((int)t >= n) return;             // (a row's lanes return together)
   const T* base = static_cast<const T*>(kv ? a.v : a.k);
   const long long* st = kv ? a.sv : a.sk;
   float x[EPL];
   load_values<T>(base + b * st[0] + t * st[1] + h * st[2] + part * EPL, a.aligned, x);
-  const int page = page_of(c, b, (long long)__ldg(a.r.start + b) + t);
-  const int at = (__ldg(a.r.start + b) + (int)t) & ((1 << c.page_shift) - 1);
+  const int page = page_of(c, b, (long long)a.r.start[b] + t);
+  const int at = (a.r.start[b] + (int)t) & ((1 << c.page_shift) - 1);
   // largest |x| over the row, as bits: they order like the values, and 0x7f800000 on is not finite
   uint32_t top = 0;
 #pragma unroll
@@ -99,25 +116,19 @@ __global__ void __launch_bounds__(kThreads) k_kv_write(WriteArgs a) {
     int e = (int)(top >> 23) - 127 - 8 + ((top & 0x7fffffu) > 0x600000u);
     e = top == 0 || bad ? 0 : max(e, -126);
     const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
-    uint32_t w[2];
+    uint32_t w[EPL / 4];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < EPL / 4; ++i) {
       const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(x[4 * i] * inv, x[4 * i + 1] * inv),
                                                    __NV_SATFINITE, __NV_E4M3);
       const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(x[4 * i + 2] * inv, x[4 * i + 3] * inv),
                                                    __NV_SATFINITE, __NV_E4M3);
       w[i] = bad ? 0u : lo | hi << 16;
     }
-    *reinterpret_cast<uint2*>(c.pool + r * c.hd + part * EPL) = make_uint2(w[0], w[1]);
+    *reinterpret_cast<uint4*>(c.pool + r * c.hd + part * EPL) = make_uint4(w[0], w[1], w[2], w[3]);
     if (part == 0) c.scale[r] = (uint8_t)(bad ? 255 : e + 127);
   } else {
-    uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const __nv_bfloat162 p = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
-      w[i] = bad ? 0u : *reinterpret_cast<const uint32_t*>(&p);
-    }
-    *reinterpret_cast<uint4*>(c.pool + (r * c.hd + part * EPL) * 2) = make_uint4(w[0], w[1], w[2], w[3]);
+    store_bf16(c.pool + (r * c.hd + part * EPL) * 2, x, bad);
     if (part == 0) c.scale[r] = (uint8_t)(bad ? 255 : 127);
   }
 }
@@ -139,51 +150,42 @@ __global__ void __launch_bounds__(kThreads) k_kv_read(ReadArgs a) {
   const int part = threadIdx.x % LPR;
   const unsigned h = row % c.kvh, kv = row / c.kvh & 1, t = row / c.kvh / 2;
   if ((int)t >= a.r.T) return;
-  const int n = a.r.count ? __ldg(a.r.count + b) : a.r.T;
+  const int n = a.r.count ? a.r.count[b] : a.r.T;
   float x[EPL];
 #pragma unroll
   for (int i = 0; i < EPL; ++i) x[i] = 0.f;
   if ((int)t < n) {
-    const int page = page_of(c, b, (long long)__ldg(a.r.start + b) + t);
+    const int page = page_of(c, b, (long long)a.r.start[b] + t);
     if (page < 0) {
       if (part == 0) set_status(a.r.status, CDSL_ERANGE);
     } else {
-      const int at = (__ldg(a.r.start + b) + (int)t) & ((1 << c.page_shift) - 1);
+      const int at = (a.r.start[b] + (int)t) & ((1 << c.page_shift) - 1);
       const size_t r = row_of(c, a.r.layer + layer, page, kv, h, at);
       const float s = scale_value(c.scale[r]);
       if constexpr (F8) {
-        const uint2 u = *reinterpret_cast<const uint2*>(c.pool + r * c.hd + part * EPL);
-        const uint32_t w[4] = {u.x & 0xffffu, u.x >> 16, u.y & 0xffffu, u.y >> 16};
+        const uint4 u = *reinterpret_cast<const uint4*>(c.pool + r * c.hd + part * EPL);
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float2 f = f8x2_to_f32(w[i]);
+        for (int i = 0; i < 8; ++i) {
+          const float2 f = f8x2_to_f32(w[i / 2] >> (16 * (i % 2)) & 0xffffu);
           x[2 * i] = f.x * s;
           x[2 * i + 1] = f.y * s;
         }
       } else {
-        const uint4 u = *reinterpret_cast<const uint4*>(c.pool + (r * c.hd + part * EPL) * 2);
-        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+        load_values(reinterpret_cast<const __nv_bfloat16*>(c.pool) + r * c.hd + part * EPL, true, x);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          x[2 * i] = __uint_as_float(w[i] << 16) * s;
-          x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u) * s;
-        }
+        for (int i = 0; i < EPL; ++i) x[i] *= s;
       }
     }
   }
   T* out = static_cast<T*>(kv ? a.v : a.k) +
            ((((size_t)layer * c.batch + b) * a.r.T + t) * c.kvh + h) * c.hd + part * EPL;
   if constexpr (sizeof(T) == 2) {
-    uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const __nv_bfloat162 p = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
-      w[i] = *reinterpret_cast<const uint32_t*>(&p);
-    }
-    *reinterpret_cast<uint4*>(out) = make_uint4(w[0], w[1], w[2], w[3]);
+    store_bf16(out, x, false);
   } else {
-    *reinterpret_cast<float4*>(out) = make_float4(x[0], x[1], x[2], x[3]);
-    *(reinterpret_cast<float4*>(out) + 1) = make_float4(x[4], x[5], x[6], x[7]);
+#pragma unroll
+    for (int j = 0; j < EPL; j += 4)
+      reinterpret_cast<float4*>(out)[j / 4] = make_float4(x[j], x[j + 1], x[j + 2], x[j + 3]);
   }
 }
 
@@ -202,8 +204,8 @@ constexpr int kMoves = 8;              // rows that a thread holds at a time
 // Grid: (layer, K or V, sequence). A thread moves 16 bytes of a head's row (or its scale byte) for
 // path entries 1, 2, .. in order, kMoves reads before their writes. In order is enough: the path is
 // strictly increasing from 0, so entry i's target i is below the sources of all later entries. Blocks have a thread a
-// part, so that one wave takes a served batch: 40 layers of 16 trees in 19 us, 22 with 256 threads a block; 16 rows in
-// place of 8 a thread, 21.
+// part, so that one wave takes a served batch: 40 layers of 16 trees of 49 nodes in 7.7 us, 3 us less than with 256
+// threads a block; 16 rows in place of 8 a thread, 1.5 us more.
 __global__ void __launch_bounds__(kThreads) k_kv_commit(CommitArgs a) {
   __shared__ int s_from[CDSL_TREE_MAX_NODES], s_to[CDSL_TREE_MAX_NODES];   // page << 8 | place, -1
   pdl_wait();
@@ -253,10 +255,10 @@ template <typename F>
 int by_shape(const Cache& c, int dtype, F&& f) {   // f(element type tag, lanes per row, e4m3?)
   auto g = [&](auto t) {
     if (c.hd == 128)
-      return c.eb == 1 ? f(t, std::integral_constant<int, 16>(), std::true_type())
-                       : f(t, std::integral_constant<int, 16>(), std::false_type());
-    return c.eb == 1 ? f(t, std::integral_constant<int, 8>(), std::true_type())
-                     : f(t, std::integral_constant<int, 8>(), std::false_type());
+      return c.eb == 1 ? f(t, std::integral_constant<int, 8>(), std::true_type())
+                       : f(t, std::integral_constant<int, 8>(), std::false_type());
+    return c.eb == 1 ? f(t, std::integral_constant<int, 4>(), std::true_type())
+                     : f(t, std::integral_constant<int, 4>(), std::false_type());
   };
   return dtype == CDSL_DTYPE_BF16 ? g(__nv_bfloat16()) : g(float());
 }

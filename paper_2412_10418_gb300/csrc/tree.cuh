@@ -27,7 +27,7 @@ __host__ __device__ inline size_t row_of(const Cache& c, int layer, int page, in
 __device__ __forceinline__ int page_of(const Cache& c, int b, long long slot) {
   const long long col = slot >> c.page_shift;
   if (slot < 0 || col >= c.max_pages) return -1;
-  const int page = __ldg(c.table + (size_t)b * c.max_pages + col);
+  const int page = c.table[(size_t)b * c.max_pages + col];
   return (unsigned)page < (unsigned)c.n_pages ? page : -1;
 }
 

@@ -75,7 +75,7 @@ __global__ void __launch_bounds__(32, simt_per_sm(HD, F8)) k_tree_simt(TreeArgs 
         const Vec w = vector_of(a, s.h, s.qb, v);
         const T* const q = static_cast<const T*>(a.q) + s.b * a.sq[0] + w.t * a.sq[1] + w.h * a.sq[2] + lane;
 #pragma unroll
-        for (int i = 0; i < DPL; ++i) x[v][i] = v < s.nq ? to_f32<T>(__ldg(q + i * 32)) * a.scale : 0.f;
+        for (int i = 0; i < DPL; ++i) x[v][i] = v < s.nq ? to_f32<T>(q[i * 32]) * a.scale : 0.f;
       }
 #pragma unroll
       for (int i = 0; i < DPL; ++i)
@@ -86,7 +86,7 @@ __global__ void __launch_bounds__(32, simt_per_sm(HD, F8)) k_tree_simt(TreeArgs 
     for (int i = lane; i < SQ * (kWords + 1); i += 32) {
       const int v = i / (kWords + 1), w = i % (kWords + 1);
       s_mask[v][w] = v < s.nq && w < a.W
-                         ? __ldg(a.mask + ((size_t)s.b * a.T + vector_of(a, s.h, s.qb, v).t) * a.W + w) : 0u;
+                         ? a.mask[((size_t)s.b * a.T + vector_of(a, s.h, s.qb, v).t) * a.W + w] : 0u;
     }
     if (lane < SQ) s_m[lane] = -INFINITY;
     __syncwarp();
@@ -124,7 +124,7 @@ __global__ void __launch_bounds__(32, simt_per_sm(HD, F8)) k_tree_simt(TreeArgs 
       auto load_k = [&](int i) {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          next[e] = e < n ? __ldg(reinterpret_cast<const uint4*>(k + e * HD * EB) + i) : make_uint4(0u, 0u, 0u, 0u);
+          next[e] = e < n ? reinterpret_cast<const uint4*>(k + e * HD * EB)[i] : make_uint4(0u, 0u, 0u, 0u);
       };
       load_k(0);
 #pragma unroll 1
@@ -225,7 +225,7 @@ __global__ void __launch_bounds__(32, simt_per_sm(HD, F8)) k_tree_simt(TreeArgs 
         const VBits* const v = reinterpret_cast<const VBits*>(c.pool + (row0 + first) * HD * EB) + lane;
 #pragma unroll
         for (int e = 0; e < AHEAD; ++e)
-          ahead[e] = first != ~0u && k0 + e < kn ? __ldg(v + e * 32) : VBits{};
+          ahead[e] = first != ~0u && k0 + e < kn ? v[e * 32] : VBits{};
       };
       load_v(0);
 #pragma unroll 1
@@ -306,7 +306,8 @@ __global__ void __launch_bounds__(32, simt_per_sm(HD, F8)) k_tree_simt(TreeArgs 
 // Joins the parts of the items that several runs share: a warp per query vector, its lanes along
 // head_dim. Grid: (items, blocks of kCombine vectors), or (bounds between runs, the same) where there are fewer of
 // them: then the first bound inside an item stands for it. It is scheduled beside the pass and works out the item's runs
-// from the lengths before it waits for them; then a vector's (m, l) and its first parts' values are loaded
+// from the lengths before it waits for the pass (whose blocks let it start after their own wait, so that what wrote the
+// lengths has ended); then a vector's (m, l) and its first parts' values are loaded
 // together. Bound by that one round trip to L2, on large passes by the parts' bytes, and with many short
 // items by its blocks, most without anything to join: 33 trees of 48 of 32 heads after 115 tokens, 528 items, 152 runs:
 // 27 us by items, 16 by bounds.

@@ -49,10 +49,10 @@ __device__ __forceinline__ int run_of(int unit, int total, int runs) {
 }
 
 __device__ __forceinline__ int len_of(const TreeArgs& a, int b) {
-  return min(max(__ldg(a.lens + b), 0), a.max_len);
+  return min(max(a.lens[b], 0), a.max_len);
 }
 __device__ __forceinline__ int nodes_of(const TreeArgs& a, int b) {
-  return a.nodes ? min(max(__ldg(a.nodes + b), 0), a.T) : a.T;
+  return a.nodes ? min(max(a.nodes[b], 0), a.T) : a.T;
 }
 // Units of a block of queries (an item without anything to see has one, which writes its zeros), of those
 // that hold nodes, and how many blocks hold some.
@@ -131,11 +131,6 @@ struct Vec { int t, h; };
 __device__ __forceinline__ Vec vector_of(const TreeArgs& a, int h, int qb, int v) {
   const int x = qb * a.NQ + v;
   return {x / a.G, h * a.G + x % a.G};
-}
-
-// Whether node t's mask has bit `node`.
-__device__ __forceinline__ bool sees(const TreeArgs& a, int b, int t, int node) {
-  return (__ldg(a.mask + ((size_t)b * a.T + t) * a.W + (node >> 5)) >> (node & 31)) & 1;
 }
 
 template <typename T>

@@ -171,7 +171,7 @@ __device__ __forceinline__ void stage_masks(const TreeArgs& a, const Segment& s,
   if (s.c1 * kKeys <= s.len) return;
   const int n = (min(s.nodes, t0 + (s.nq + a.G - 1) / a.G + 1) - t0) * a.W;
   for (int i = tid; i < n; i += NT)
-    s_mask[i / a.W][i % a.W] = __ldg(a.mask + ((size_t)s.b * a.T + t0) * a.W + i);
+    s_mask[i / a.W][i % a.W] = a.mask[((size_t)s.b * a.T + t0) * a.W + i];
 }
 
 // The loading warp: K and V chunks of a run's segments into a ring of NST stages (tiles of kKeys rows in blocks
