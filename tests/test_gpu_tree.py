@@ -1,6 +1,7 @@
 """Tree speculation over a quantised paged cache (include/cdsl_tree.h) against plain 64-bit implementations: the
 cache's write, read and commit, the tree attention, the validation. Pools start full of garbage (NaN codes
 and scales among it), pages are in random order."""
+import copy
 import random
 
 import pytest
@@ -227,6 +228,33 @@ def test_attention_matches_64_bits(cdsl, shape, cache, dtype):
     assert torch.equal(got[0], again[0]) and torch.equal(got[1], again[1])       # sums in a fixed order
     wide = attend(cdsl, c, 1, q, lens, mask, nodes, scale, max_len=c.table.shape[1] * page - T)
     check(c, 1, q, lens, mask, nodes, scale, wide)
+
+
+@pytest.mark.parametrize("cache", [F8, BF], ids=["f8", "bf16"])
+@pytest.mark.parametrize("dtype,B,T", [(BF, 40, 2), (BF, 24, 40), (F32, 20, 128)])
+def test_attention_of_more_items_than_runs(cdsl, cache, dtype, B, T):
+    """Many short sequences: most items are whole, the others are joined from the bounds between runs."""
+    rng = random.Random(B)
+    lens = [rng.choice([0, 1, 120, 127, 200, 300]) for _ in range(B)]
+    nodes = [rng.choice([0, 1, T // 2, T, T]) for _ in range(B)]
+    c, q, mask, _ = problem(cdsl, B, T, 8, 8, 64, 32, lens, cache, dtype, nodes=nodes, seed=B)
+    got = attend(cdsl, c, 1, q, lens, mask, nodes, 0.125)
+    pick = rng.sample(range(B), 5)
+    some = copy.copy(c)
+    some.table = c.table[pick]
+    check(some, 1, q[pick], [lens[b] for b in pick], mask[pick], [nodes[b] for b in pick], 0.125,
+          (got[0][pick], got[1][pick]))
+    each = [attend(cdsl, part, 1, q[b:b + 1], lens[b:b + 1], mask[b:b + 1], nodes[b:b + 1], 0.125)[0]
+            for b, part in ((b, alone(c, b)) for b in range(B))]
+    far = (got[0].float() - torch.cat(each).float()).abs().max()      # other runs: other roundings
+    assert far <= (2.0 ** -6 if dtype is BF else 2.0 ** -14) * got[0].float().abs().max()
+
+
+def alone(c, b):
+    part = copy.copy(c)
+    part.table = c.table[b:b + 1].contiguous()
+    part.c = c.c.at(part.table)
+    return part
 
 
 @pytest.mark.parametrize("cache", [F8, BF], ids=["f8", "bf16"])
@@ -516,3 +544,22 @@ def test_verify_takes_strided_logits(cdsl):
     wide[..., 3:104] = logits.transpose(0, 1)
     got = run_verify(cdsl, wide.cuda()[..., 3:104].transpose(0, 1), None, tokens, parents, u, u_last, 1.0)
     assert torch.equal(got[0], want[0]) and got[1] == want[1] and torch.equal(got[2], want[2])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF], ids=["f32", "bf16"])
+@pytest.mark.parametrize("V", [9, 1001, 20003])
+def test_verify_by_any_alignment(cdsl, dtype, V):
+    """Rows that start at 16 bytes are read 16 bytes at a time, to an end anywhere; others by single values."""
+    logits, draft, tokens, parents, u, u_last = verify_inputs(4, 7, V, dtype, True, 1.0, seed=V, spread=4.0)
+    up = -(-V // 8) * 8
+    want = None
+    for pitch, first in ((V, 0), (up, 0), (up + 16, 8), (up + 8, 1)):
+        wide = [torch.full((4, 7, pitch), float("nan"), dtype=dtype, device="cuda") for _ in range(2)]
+        for w, x in zip(wide, (logits, draft)):
+            w[..., first:first + V] = x.cuda()
+        path, n, emitted, st = run_verify(cdsl, wide[0][..., first:first + V], wide[1][..., first:first + V], tokens, parents,
+                                          u, u_last, 1.0)
+        got = path.tolist(), n, emitted.tolist(), st
+        assert st == cdsl.CDSL_OK and got == (want or got)
+        want = got
+    assert max(want[1]) > 1 and all(0 <= e[m - 1] < V for e, m in zip(want[2], want[1]))
