@@ -49,7 +49,7 @@ __global__ void __launch_bounds__(32, simt_per_sm(HD, F8)) k_tree_simt(TreeArgs 
   constexpr int DPL = HD / 32;                 // dimensions of a lane
   constexpr int AHEAD = DPL * EB > 4 ? 8 : 16; // V rows loaded together
   using VBits = std::conditional_t<DPL * EB == 8, uint2, std::conditional_t<DPL * EB == 4, uint32_t, uint16_t>>;
-  extern __shared__ int s_first[];             // [batch + 1]
+  extern __shared__ int s_first[];             // plan_bytes
   constexpr int ROW = SQ + 4;                  // floats (48 or 80 bytes: eight lanes' 16 bytes take all banks)
   __shared__ __align__(16) float s_q[HD][ROW];
   __shared__ __align__(16) float s_p[kKeys][ROW];   // slot k in row k % 4 * 32 + k / 4
@@ -321,7 +321,7 @@ __global__ void __launch_bounds__(32 * kCombine) k_tree_combine(TreeArgs a) {
   if (!Bounds && (qb >= live_blocks(a, nodes_of(a, b)) || v >= min(a.NQ, a.T * a.G - qb * a.NQ))) return pdl_wait();
   int before = 0, total = 0;                   // units of the sequences before, and of all
   for (int x = lane; x < a.c.batch; x += 32) {
-    const int w = units_of(a, x);
+    const int w = units_of(a, len_of(a, x), nodes_of(a, x));
     total += w;
     if (!Bounds && x < b) before += w;
   }
@@ -333,7 +333,7 @@ __global__ void __launch_bounds__(32 * kCombine) k_tree_combine(TreeArgs a) {
     if (bound >= runs) return pdl_wait();
     x = run_begin(bound, total, runs);
     for (int b0 = 0; b0 < a.c.batch; b0 += 32) {   // the sequence that it lies in
-      const int w = b0 + lane < a.c.batch ? units_of(a, b0 + lane) : 0;
+      const int w = b0 + lane < a.c.batch ? units_of(a, len_of(a, b0 + lane), nodes_of(a, b0 + lane)) : 0;
       int upto = w;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -451,7 +451,7 @@ cudaError_t launch_combine(const TreeArgs& a, cudaStream_t s) {
 
 template <typename T, int HD, bool F8>
 cudaError_t launch_simt(const TreeArgs& a, cudaStream_t s) {
-  return launch_pdl(k_tree_simt<T, HD, F8>, dim3(a.blocks), dim3(32), (a.c.batch + 1) * 4, s, a);
+  return launch_pdl(k_tree_simt<T, HD, F8>, dim3(a.blocks), dim3(32), plan_bytes(a.c.batch), s, a);
 }
 
 cudaError_t launch_pass(const TreeArgs& a, bool tc, bool split, cudaStream_t s) {

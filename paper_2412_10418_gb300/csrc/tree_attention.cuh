@@ -61,25 +61,33 @@ __device__ __forceinline__ int live_blocks(const TreeArgs& a, int nodes) {
   return (nodes * a.G + a.NQ - 1) / a.NQ;
 }
 
-__device__ __forceinline__ int units_of(const TreeArgs& a, int b) {
-  const int n = nodes_of(a, b), live = live_blocks(a, n);
-  return a.c.kvh * (live * item_units(len_of(a, b) + n) + (a.QB - live));
+// of a sequence of `len` cached slots and n nodes
+__device__ __forceinline__ int units_of(const TreeArgs& a, int len, int n) {
+  const int live = live_blocks(a, n);
+  return a.c.kvh * (live * item_units(len + n) + (a.QB - live));
 }
 
-// first[b], b <= batch: the units before sequence b's. The whole block calls; first is in shared memory.
+// first[b], b <= batch: the units before sequence b's; behind them the sequences' lengths and nodes. The whole block
+// calls; first is in shared memory, plan_bytes of it.
+constexpr int plan_bytes(int batch) { return (3 * batch + 1) * 4; }
 __device__ __forceinline__ void build_plan(const TreeArgs& a, int* first) {
   if (threadIdx.x < 32) {
     int sum = 0;
     for (int b0 = 0; b0 < a.c.batch; b0 += 32) {
       const int b = b0 + (int)threadIdx.x;
-      const int v = b < a.c.batch ? units_of(a, b) : 0;
+      const int len = b < a.c.batch ? len_of(a, b) : 0, n = b < a.c.batch ? nodes_of(a, b) : 0;
+      const int v = b < a.c.batch ? units_of(a, len, n) : 0;
       int s = v;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
         const int w = __shfl_up_sync(0xffffffffu, s, o);
         if ((int)threadIdx.x >= o) s += w;
       }
-      if (b < a.c.batch) first[b] = sum + s - v;
+      if (b < a.c.batch) {
+        first[b] = sum + s - v;
+        first[a.c.batch + 1 + b] = len;
+        first[2 * a.c.batch + 1 + b] = n;
+      }
       sum += __shfl_sync(0xffffffffu, s, 31);
     }
     if (threadIdx.x == 0) first[a.c.batch] = sum;
@@ -96,14 +104,15 @@ struct Segment {
 };
 __device__ __forceinline__ Segment segment_at(const TreeArgs& a, const int* first, int unit, int end) {
   int lo = 0, hi = a.c.batch - 1;              // the last sequence whose first unit is not after `unit`
+#pragma unroll 1
   while (lo < hi) {
     const int mid = (lo + hi + 1) / 2;
     if (first[mid] <= unit) lo = mid; else hi = mid - 1;
   }
   Segment s;
   s.b = lo;
-  s.nodes = nodes_of(a, lo);
-  s.len = len_of(a, lo);
+  s.len = first[a.c.batch + 1 + lo];
+  s.nodes = first[2 * a.c.batch + 1 + lo];
   const int live = live_blocks(a, s.nodes), u = item_units(s.len + s.nodes);
   const int per_head = live * u + (a.QB - live);
   const int x = unit - first[lo];

@@ -27,12 +27,17 @@
 // there K and the scale bytes are loaded a chunk ahead of V, or S would wait for the V of a chunk before (36 vectors,
 // 8 sequences of 16,384 tokens, 8 heads: 191 -> 123 us; with three stages of e4m3 it loses 5 %).
 //
-// Measured: 8 trees of 25 nodes, 100 vectors a K/V head, up to 32,768 tokens of 8 heads of 128 in e4m3: 155 us,
-// 390 TFLOP/s, 39 % of the copy bandwidth. A chunk takes 3,000 cycles, of which its MMAs need 1,024; a softmax
-// thread spends 1,300 on the maxima, 2,000 on the probabilities, 1,000 on the reference's way through its group and the
-// other, mostly latency of TMEM (166 cycles a load) and of shared memory, which the MMAs' operands, the conversion and
-// the factors together keep busy for 1,900. At 33 vectors (the same chunk's time) 8 sequences of 16,384 take 101 us;
-// two blocks of 32 on tree_attention_tc.cu 114. At 32, 67 there and 94 here.
+// Between two items the next one's queries and masks are staged as soon as the last S has read this one's, beside
+// the last P V (33 trees of 48 after 115 tokens: 57 -> 53 us).
+//
+// Measured: 8 trees of 25 nodes, 100 vectors a K/V head, up to 32,768 tokens of 8 heads of 128 in e4m3: 150 us,
+// 400 TFLOP/s, 40 % of the copy bandwidth. A chunk takes 3,000 cycles, of which its MMAs need 1,024; a softmax
+// thread spends 1,500 on the maxima, 2,000 on the probabilities and the rest waiting. What holds it is latency (166
+// cycles a TMEM load), shared memory, which operands, conversion and factors keep busy for 1,900, and instruction
+// fetches: the roles together are about as large as the instruction cache, and the same kernel took 150 to 190 us
+// with the sizes of its loops (0.4 to 1.6 million misses a call); the masked maxima are rolled and V's loop
+// unrolled twice for that. At 36 vectors 8 sequences of 16,384 take 99 us, two blocks of 32 on
+// tree_attention_tc.cu 114. At 32, 67 there and 94 here.
 #include <cuda.h>
 
 #include <algorithm>
@@ -78,7 +83,7 @@ struct Cfg {
   // K's scale of each slot, and V's relative to its reference (0: nothing, or not finite)
   static constexpr uint32_t FACTOR_OFF = SCALE_OFF + NST * 2 * kKeys;
   static constexpr uint32_t PLAN_OFF = FACTOR_OFF + NST * 2 * kKeys * 4;
-  static constexpr size_t smem(int batch) { return 1024 + PLAN_OFF + (batch + 1) * 4; }
+  static constexpr size_t smem(int batch) { return 1024 + PLAN_OFF + plan_bytes(batch); }
 };
 
 template <int HD, bool F8>
@@ -95,11 +100,11 @@ __global__ void __launch_bounds__(kThreads, 1)
   __shared__ uint32_t s_tmem;
   __shared__ __align__(16) uint32_t s_valid[NST][4], s_nan[NST][4];   // slots that there are, whose V is not finite
   __shared__ int s_vref[NST], s_vstep[NST];    // V's reference in the chunk, and that of the chunk before less it
-  __shared__ float s_qs[kRows];                // score factors
+  __shared__ float s_qs[2][kRows];             // score factors, of this segment's queries and the next one's
   __shared__ int s_v;                          // V's reference at the end
   __shared__ float s_ref[kRows], s_l[2][kRows];   // the rows' references; the groups' sums
-  __shared__ uint8_t s_bad[kRows];             // the query is not finite
-  __shared__ uint32_t s_mask[kRows + 1][kWords];
+  __shared__ uint8_t s_bad[2][kRows];          // the query is not finite
+  __shared__ uint32_t s_mask[2][kRows + 1][kWords];
   __shared__ uint32_t s_pieces[NST];
   const Cache& c = a.c;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -159,7 +164,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const uint64_t desc_v = F8 ? tc::desc_rows(sbase + C::H_OFF, 128, C::H_BLOCK)
                                  : tc::desc_rows(sbase + C::KV_OFF + C::TILE, C::BW, C::BLOCK);
       auto s_mma = [&](int i) {                // S of chunk i
-        if (!tc::mbar_wait(&k_full[i % NST], parity(i, NST), a.status)) return false;
+        if (!wait_for(&k_full[i % NST], parity(i, NST), a.status)) return false;
         tc::tc_fence_after();
         const uint64_t k = desc_k + (uint32_t)(i % NST) * (2 * C::TILE / 16);
 #pragma unroll 1
@@ -179,9 +184,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         return true;
       };
       auto pv = [&](int i, bool add) {         // P V of chunk i
-        if (!tc::mbar_wait(&p_full[i % kBuf], parity(i, kBuf), a.status) ||
-            !(F8 ? tc::mbar_wait(&h_full[i & 1], parity(i, 2), a.status)
-                 : tc::mbar_wait(&v_full[i % NST], parity(i, NST), a.status)))
+        if (!wait_for(&p_full[i % kBuf], parity(i, kBuf), a.status) ||
+            !(F8 ? wait_for(&h_full[i & 1], parity(i, 2), a.status)
+                 : wait_for(&v_full[i % NST], parity(i, NST), a.status)))
           return false;
         tc::tc_fence_after();
         const uint64_t v = desc_v + (F8 ? (uint32_t)(i & 1) * (C::H_TILE / 16) : (uint32_t)(i % NST) * (2 * C::TILE / 16));
@@ -202,7 +207,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       for (int unit = begin; unit < end && ok; ++seg) {
         const Segment s = segment_at(a, s_first, unit, end);
         const int n = s.c1 - s.c0;
-        ok = tc::mbar_wait(&q_full, seg & 1, a.status);
+        ok = wait_for(&q_full, seg & 1, a.status);
         // S as far ahead as it has buffers; it overwrites a P after the P V that reads it, in order
         for (int i = 0; i < n + kBuf && ok; ++i) {
           if (i >= kBuf) ok = pv(it + i - kBuf, i > kBuf);
@@ -212,7 +217,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         unit += n;
       }
       tc::umma_commit(&done);                  // what was issued completes before the block's memory goes
-      tc::mbar_wait(&done, 0, a.status);
+      wait_for(&done, 0, a.status);
     }
     __syncwarp();
   } else if (warp == kScaler) {
@@ -224,8 +229,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       int vref = 0;
       for (int ch = s.c0; ch < s.c1 && ok; ++ch, ++it) {
         const int st = it % NST;
-        ok = __all_sync(0xffffffffu, tc::mbar_wait(F8 ? &v_full[st] : &k_full[st], parity(it, NST), a.status) &&
-                                         tc::mbar_wait(&f_empty[st], parity(it, NST) ^ 1, a.status));
+        ok = __all_sync(0xffffffffu, wait_for(F8 ? &v_full[st] : &k_full[st], parity(it, NST), a.status) &&
+                                         wait_for(&f_empty[st], parity(it, NST) ^ 1, a.status));
         if (!ok) break;
         // a lane has slots 4 lane .. 4 lane + 3
         const uint8_t* from = sm + C::SCALE_OFF + st * 2 * kKeys + 4 * lane;
@@ -273,7 +278,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         __syncwarp();
         if (lane == 0) tc::mbar_arrive(F8 ? &v_empty[st] : &k_empty[st]);   // (the scale bytes are read)
         if (!F8 && __any_sync(0xffffffffu, n < 4))
-          ok = __all_sync(0xffffffffu, tc::mbar_wait(&v_full[st], parity(it, NST), a.status));
+          ok = __all_sync(0xffffffffu, wait_for(&v_full[st], parity(it, NST), a.status));
         if (!ok) break;
         if (!F8 && n < 4) {                    // nothing of their V rows (page garbage, no copy) may reach the sums
 #pragma unroll 1
@@ -297,22 +302,28 @@ __global__ void __launch_bounds__(kThreads, 1)
     const bool q_aligned = (reinterpret_cast<uintptr_t>(a.q) | (a.sq[0] | a.sq[1] | a.sq[2]) * 2) % 16 == 0;
     const bool o_aligned = (reinterpret_cast<uintptr_t>(a.out) | (a.so[0] | a.so[1] | a.so[2]) * 2) % 16 == 0;
     const uint32_t lanes = (uint32_t)(w4 * 32) << 16;
-    int it0 = 0;
+    int it0 = 0, buf = 0;
     bool failed = false;
-    for (int unit = begin; unit < end;) {
-      const Segment s = segment_at(a, s_first, unit, end);
+    const auto stage = [&](const Segment& s, int to) {   // a segment's queries and masks
       stage_queries<HD, kRows, F8, kSoft, true>(a, s, tid, q_aligned, sm, [&](int v, const Vec&, float qs, bool bad) {
-        s_qs[v] = v < s.nq ? qs : 0.f;
-        s_bad[v] = bad;
+        s_qs[to][v] = v < s.nq ? qs : 0.f;
+        s_bad[to][v] = bad;
       });
-      const int t0 = s.qb * kRows / a.G;       // the block's first node
-      stage_masks<kSoft>(a, s, t0, tid, s_mask);
+      stage_masks<kSoft>(a, s, s.qb * kRows / a.G, tid, s_mask[to]);
       tc::fence_proxy_async();
       tc::mbar_arrive(&q_full);
+    };
+    Segment s;
+    if (begin < end) {
+      s = segment_at(a, s_first, begin, end);
+      stage(s, 0);
       sync();
-      const float qs = s_qs[r];
+    }
+    for (int unit = begin; unit < end; buf ^= 1) {
+      const int t0 = s.qb * kRows / a.G;       // the block's first node
+      const float qs = s_qs[buf][r];
       const bool live = w4 * 32 < s.nq;        // (a warp's: its rows hold vectors)
-      const uint32_t* const my_mask = s_mask[r < s.nq ? vector_of(a, s.h, s.qb, r).t - t0 : 0];
+      const uint32_t* const my_mask = s_mask[buf][r < s.nq ? vector_of(a, s.h, s.qb, r).t - t0 : 0];
       const int n = s.c1 - s.c0;
       float ref = -INFINITY, l = 0.f;          // the row's reference at the group's last chunk, and its sum
       int vref = 127;                          // V's reference in O
@@ -320,8 +331,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int it = it0 + i, st = it % NST;
         const uint32_t t_s = tmem + it % kBuf * kKeys + lanes;
         const float* const kf = reinterpret_cast<const float*>(sm + C::FACTOR_OFF) + st * 2 * kKeys;
-        bool ok = tc::mbar_wait(&f_full[st], parity(it, NST), a.status);
-        ok = ok && tc::mbar_wait(&s_full[it % kBuf], parity(it, kBuf), a.status);
+        bool ok = wait_for(&f_full[st], parity(it, NST), a.status);
+        ok = ok && wait_for(&s_full[it % kBuf], parity(it, kBuf), a.status);
         failed = !__all_sync(0xffffffffu, ok);   // (a warp gives up as one)
         tc::tc_fence_after();
         // a chunk with slots of the tree, past the item's, without a page or with a V that is not finite: each row has
@@ -361,7 +372,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           };
           // ---- the row's maximum
           float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
+#pragma unroll masked ? 1 : 4            // (code for the rare chunks is kept small)
           for (int w = 0; w < 4; ++w) {
             uint32_t x[2][16];
             tc::tmem_ld16_nowait(t_s + 32 * w, x[0]);
@@ -383,7 +394,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           // ---- the row's reference: the chunk before's, raised where the maximum asks for it
           float was = -INFINITY;
           if (i > 0) {
-            ok = tc::mbar_wait(&r_full[(it - 1) % kBuf], parity(it - 1, kBuf), a.status);
+            ok = wait_for(&r_full[(it - 1) % kBuf], parity(it - 1, kBuf), a.status);
             was = s_ref[r];
           }
           const float mq = top * qs, now = top > -INFINITY && !(mq - was <= kMargin) ? mq : was;
@@ -394,7 +405,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           float f = was == now || was == -INFINITY ? 1.f : ex2(was - now);
           if (F8) f *= ex2((float)s_vstep[st]);
           if (i > 0 && __any_sync(0xffffffffu, f != 1.f)) {
-            ok = ok && tc::mbar_wait(&pv_done[1 - grp], parity(it - 1, 2), a.status);
+            ok = ok && wait_for(&pv_done[1 - grp], parity(it - 1, 2), a.status);
             tc::tc_fence_after();
 #pragma unroll 1
             for (int d = 0; d < HD; d += 16) {
@@ -463,12 +474,20 @@ __global__ void __launch_bounds__(kThreads, 1)
         tc::mbar_arrive(&f_empty[st]);
       }
       // ---- the groups' sums: each thread finishes half of its row's dimensions
+      // the next segment's queries, as soon as the last S has read this one's, beside the last P V
       const int last = it0 + n - 1;
+      unit += n;
+      const Segment now = s;
+      if (unit < end) {
+        if (!failed) failed = !__all_sync(0xffffffffu, wait_for(&s_full[last % kBuf], parity(last, kBuf), a.status));
+        s = segment_at(a, s_first, unit, end);
+        if (!failed) stage(s, buf ^ 1);
+      }
       if (!failed)
-        failed = !__all_sync(0xffffffffu, tc::mbar_wait(&pv_done[last & 1], parity(last, 2), a.status));
+        failed = !__all_sync(0xffffffffu, wait_for(&pv_done[last & 1], parity(last, 2), a.status));
       if (tc::named_barrier_or(1, kSoft, failed)) break;
       tc::tc_fence_after();
-      const int rows = min(kRows, a.T * a.G - s.qb * kRows);
+      const int rows = min(kRows, a.T * a.G - now.qb * kRows);
       {
         float m = live ? s_ref[r] : -INFINITY;   // the last chunk's
         if (ref != m) l *= ref == -INFINITY ? 1.f : ex2(ref - m);
@@ -477,24 +496,24 @@ __global__ void __launch_bounds__(kThreads, 1)
         sync();
         l = s_l[0][r] + s_l[1][r];
         if (m == -INFINITY) m = 0.f;           // (nothing seen, or NaN scores alone)
-        if (r >= s.nq || s.keys == 0) l = 0.f;
-        if (l != 0.f && s_bad[r]) l = __uint_as_float(0x7fc00000u);
+        if (r >= now.nq || now.keys == 0) l = 0.f;
+        if (l != 0.f && s_bad[buf][r]) l = __uint_as_float(0x7fc00000u);
         m = l == 0.f ? -INFINITY : m - kUp;
-        const bool whole = s.c0 == 0 && s.c1 == s.units;
+        const bool whole = now.c0 == 0 && now.c1 == now.units;
         const float inv = l == 0.f ? 0.f : whole ? 1.f / l : 1.f;
         const float unscale = F8 ? ex2((float)(s_v - 127)) : 1.f;
-        const Vec x = vector_of(a, s.h, s.qb, r);
-        const size_t part = (size_t)blockIdx.x * 2 + (s.c0 == 0);
+        const Vec x = vector_of(a, now.h, now.qb, r);
+        const size_t part = (size_t)blockIdx.x * 2 + (now.c0 == 0);
         if (grp == 0 && r < rows) {
           if (whole) {
-            store_lse(a, s.b, x, m, l);
+            store_lse(a, now.b, x, m, l);
           } else {
             a.part_ml[(part * 2) * kRows + r] = m;
             a.part_ml[(part * 2 + 1) * kRows + r] = l;
           }
         }
         __nv_bfloat16* const out =
-            static_cast<__nv_bfloat16*>(a.out) + s.b * a.so[0] + x.t * a.so[1] + x.h * a.so[2];
+            static_cast<__nv_bfloat16*>(a.out) + now.b * a.so[0] + x.t * a.so[1] + x.h * a.so[2];
         float* const part_o = a.part_o + (part * kRows + r) * HD;
 #pragma unroll 1
         for (int d = grp * (HD / 2); d < (grp + 1) * (HD / 2); d += 16) {
@@ -533,26 +552,30 @@ __global__ void __launch_bounds__(kThreads, 1)
       tc::tc_fence_before();
       sync();                                  // queries, masks, sums and O are free
       it0 += n;
-      unit += n;
     }
   } else if (F8) {
     // ------------------------------------------------------------------------- V to fp16
     // 16 codes at a time, exactly, with the rows' scales; rows that there are not become zeros
-    const int tid = threadIdx.x - kSoft;
+    constexpr int kRowsAt = kConv / (HD / 16);
+    const int row0 = (threadIdx.x - kSoft) / (HD / 16), part = (threadIdx.x - kSoft) % (HD / 16);
+    // (the other half first in the second block of 64 dimensions: eight lanes' stores then meet no bank twice)
+    const int flip = part >> 2 & 1;
+    const uint32_t to0 = part / 4 * C::H_BLOCK + tc::row_offset(row0, part % 4 * 2 + flip, 128);
+    const uint32_t to1 = part / 4 * C::H_BLOCK + tc::row_offset(row0, part % 4 * 2 + 1 - flip, 128);
     bool ok = true;
     for (int i = 0; i < end - begin && ok; ++i) {   // (a unit of the run is a chunk)
       const int st = i % NST;
-      ok = tc::mbar_wait(&f_full[st], parity(i, NST), a.status) &&
-           tc::mbar_wait(&v_full[st], parity(i, NST), a.status) &&
-           tc::mbar_wait(&pv_done[i & 1], parity(i, 2) ^ 1, a.status);   // (chunk i - 2's: the buffer is free)
+      ok = wait_for(&f_full[st], parity(i, NST), a.status) &&
+           wait_for(&v_full[st], parity(i, NST), a.status) &&
+           wait_for(&pv_done[i & 1], parity(i, 2) ^ 1, a.status);   // (chunk i - 2's: the buffer is free)
       ok = __all_sync(0xffffffffu, ok);
       const float* vf = reinterpret_cast<const float*>(sm + C::FACTOR_OFF) + (st * 2 + 1) * kKeys;
-      const uint8_t* from = sm + C::KV_OFF + (st * 2 + 1) * C::TILE;
+      const uint8_t* from = sm + C::KV_OFF + (st * 2 + 1) * C::TILE + tc::row_offset(row0, part, C::BW);
       uint8_t* to = sm + C::H_OFF + (i & 1) * C::H_TILE;
-#pragma unroll 4
-      for (int x = tid; x < kKeys * (HD / 16); x += kConv) {
-        const int row = x / (HD / 16), part = x % (HD / 16);
-        const uint4 u = *reinterpret_cast<const uint4*>(from + tc::row_offset(row, part, C::BW));
+#pragma unroll 2
+      for (int k = 0; k < kKeys / kRowsAt; ++k) {   // (rows that many apart lie alike in their tiles)
+        const int row = row0 + k * kRowsAt;
+        const uint4 u = *reinterpret_cast<const uint4*>(from + k * kRowsAt * C::BW);
         const float f = vf[row];
         const __half2 f2 = __float2half2_rn(f);
         const uint32_t w[4] = {u.x, u.y, u.z, u.w};
@@ -566,12 +589,9 @@ __global__ void __launch_bounds__(kThreads, 1)
           h[2 * e] = *reinterpret_cast<const uint32_t*>(&p);
           h[2 * e + 1] = *reinterpret_cast<const uint32_t*>(&q);
         }
-        // (the other half first in the second block of 64 dimensions: eight lanes' stores then meet no bank twice)
-        const int flip = part >> 2 & 1;
-        uint8_t* const block = to + part / 4 * C::H_BLOCK;
         const uint4 lo = make_uint4(h[0], h[1], h[2], h[3]), hi = make_uint4(h[4], h[5], h[6], h[7]);
-        *reinterpret_cast<uint4*>(block + tc::row_offset(row, part % 4 * 2 + flip, 128)) = flip ? hi : lo;
-        *reinterpret_cast<uint4*>(block + tc::row_offset(row, part % 4 * 2 + 1 - flip, 128)) = flip ? lo : hi;
+        *reinterpret_cast<uint4*>(to + k * (kRowsAt * 128) + to0) = flip ? hi : lo;
+        *reinterpret_cast<uint4*>(to + k * (kRowsAt * 128) + to1) = flip ? lo : hi;
       }
       tc::fence_proxy_async();
       tc::mbar_arrive(&h_full[i & 1]);

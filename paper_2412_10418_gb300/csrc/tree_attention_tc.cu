@@ -77,7 +77,7 @@ struct Cfg {
   static constexpr uint32_t SCALE_OFF = KV_OFF + NST * 2 * TILE;   // a byte per slot, K and V
   static constexpr uint32_t PLAN_OFF = SCALE_OFF + NST * 2 * kKeys;
   static constexpr uint32_t TMEM = 4 * NQ;                 // S twice, O (a power of two)
-  static constexpr size_t smem(int batch) { return 1024 + PLAN_OFF + (batch + 1) * 4; }
+  static constexpr size_t smem(int batch) { return 1024 + PLAN_OFF + plan_bytes(batch); }
 };
 
 template <int HD, int NQ, bool F8>

@@ -17,6 +17,17 @@ __device__ __forceinline__ float ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+// Waits for the phase of parity `parity` to complete; false (and CDSL_ETIMEOUT latched) if it has not after kTries
+// suspended tries, a second or more. (Tries are counted, not timed: there are some twenty waits in a kernel, and their
+// code in the instruction cache counts.)
+constexpr int kTries = 1 << 19;
+__device__ __forceinline__ bool wait_for(uint64_t* m, uint32_t parity, int32_t* status) {
+#pragma unroll 1
+  for (int i = 0; i < kTries; ++i)
+    if (tc::mbar_try_wait_sleep(m, parity)) return true;
+  set_status(status, CDSL_ETIMEOUT);
+  return false;
+}
 // Pairs of fp32 values in a 64-bit register.
 __device__ __forceinline__ uint64_t pair(float a, float b) {
   uint64_t r;
@@ -192,11 +203,11 @@ __device__ __forceinline__ void load_chunks(const TreeArgs& a, const int* first,
     int page, h, at;                           // this lane's piece
     uint32_t live;
   };
-  int issued[2] = {0, 0};                      // copies of K and of V
+  int issued_k = 0, issued_v = 0;              // copies
   auto issue = [&](int kv, int it, const Chunk& x) {
     const int st = it % NST;
     uint64_t* full = kv ? &v_full[st] : &k_full[st];
-    if (!__all_sync(0xffffffffu, tc::mbar_wait(kv ? &v_empty[st] : &k_empty[st], parity(it, NST) ^ 1, a.status)))
+    if (!__all_sync(0xffffffffu, wait_for(kv ? &v_empty[st] : &k_empty[st], parity(it, NST) ^ 1, a.status)))
       return false;
     const bool bytes = kv == (EARLY ? 0 : 1);  // both scale bytes too
     if (lane == 0) {
@@ -216,15 +227,17 @@ __device__ __forceinline__ void load_chunks(const TreeArgs& a, const int* first,
         tc::bulk_load(to + kKeys, from + ((size_t)c.kvh << c.page_shift), rows, full);
       }
     }
-    if (kv) issued[1] = it + 1;
-    else issued[0] = it + 1;
+    if (kv) issued_v = it + 1;
+    else issued_k = it + 1;
     return true;
   };
   int it = 0;                                  // chunks
   bool ok = true;
   Chunk before = {};
+#pragma unroll 1
   for (int unit = begin; unit < end && ok;) {
     const Segment s = segment_at(a, first, unit, end);
+#pragma unroll 1
     for (int ch = s.c0; ch < s.c1 && ok; ++ch, ++it) {
       const int slot = ch * kKeys + lane * rows;
       Chunk x = {-1, s.h, slot & (P - 1), 0u};
@@ -246,10 +259,11 @@ __device__ __forceinline__ void load_chunks(const TreeArgs& a, const int* first,
   if (EARLY && it > 0) ok = ok && issue(1, it - 1, before);
   // where a role gave up, nothing may have waited for the copies
   if (!ok)
-#pragma unroll
+#pragma unroll 1
     for (int kv = 0; kv < 2; ++kv)
-      for (int i = max(0, issued[kv] - NST); i < issued[kv]; ++i)
-        tc::mbar_wait(kv ? &v_full[i % NST] : &k_full[i % NST], parity(i, NST), a.status);
+#pragma unroll 1
+      for (int n = kv ? issued_v : issued_k, i = max(0, n - NST); i < n; ++i)
+        wait_for(kv ? &v_full[i % NST] : &k_full[i % NST], parity(i, NST), a.status);
 }
 
 // 32 bytes to an address that is a multiple of 32 (a whole sector: two stores of 16 bytes take two).
