@@ -35,9 +35,9 @@
 // thread spends 1,500 on the maxima, 2,000 on the probabilities and the rest waiting. What holds it is latency (166
 // cycles a TMEM load), shared memory, which operands, conversion and factors keep busy for 1,900, and instruction
 // fetches: the roles together are about as large as the instruction cache, and the same kernel took 150 to 190 us
-// with the sizes of its loops (0.4 to 1.6 million misses a call); the masked maxima are rolled and V's loop
-// unrolled twice for that. At 36 vectors 8 sequences of 16,384 take 99 us, two blocks of 32 on
-// tree_attention_tc.cu 114. At 32, 67 there and 94 here.
+// with the sizes of its loops (0.4 to 1.6 million misses a call), which are kept rolled for that. A third group of
+// softmax warps: 177 us. At 36 vectors 8 sequences of 16,384 take 99 us, two blocks of 32 on
+// tree_attention_tc.cu 114. At 32, 67 there and 98 here.
 #include <cuda.h>
 
 #include <algorithm>
@@ -372,7 +372,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           };
           // ---- the row's maximum
           float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll masked ? 1 : 4            // (code for the rare chunks is kept small)
+#pragma unroll 1
           for (int w = 0; w < 4; ++w) {
             uint32_t x[2][16];
             tc::tmem_ld16_nowait(t_s + 32 * w, x[0]);

@@ -24,9 +24,9 @@
 // dimension of O^T. Column maxima come from redux.sync over a warp and shared memory over the warps, the one
 // barrier of a chunk; each warp then works out the columns' factors for itself. Each thread keeps its own
 // slots' share of the sums l. Bound by HBM where a call fills the device: 64 sequences of up to 8,192 tokens, 8 heads of
-// 128 in e4m3, four query heads each, one token: 131 us, 91 % of the copy bandwidth; by latency in small ones: one of
+// 128 in e4m3, four query heads each, one token: 133 us, 90 % of the copy bandwidth; by latency in small ones: one of
 // 512 tokens in 9 us with the joining. The MMA's N is 16 or 32 by the number of vectors: 8 sequences of 16,384, 16
-// vectors: 54.6 us with 16, 64 with 32 (fewer blocks on an SM); 32 vectors: 67 us in one block, 94 as rows.
+// vectors: 54.6 us with 16, 64 with 32 (fewer blocks on an SM); 32 vectors: 67 us in one block, 98 as rows.
 //
 // Waits are bounded (tc::kWaitLimitNs): on expiry CDSL_ETIMEOUT is latched, the role winds down and
 // the block frees its TMEM and exits.
