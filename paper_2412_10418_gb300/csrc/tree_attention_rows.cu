@@ -30,8 +30,8 @@
 // Between two items the next one's queries and masks are staged as soon as the last S has read this one's, beside
 // the last P V (33 trees of 48 after 115 tokens: 57 -> 53 us).
 //
-// Measured: 8 trees of 25 nodes, 100 vectors a K/V head, up to 32,768 tokens of 8 heads of 128 in e4m3: 150 us,
-// 400 TFLOP/s, 40 % of the copy bandwidth. A chunk takes 3,000 cycles, of which its MMAs need 1,024; a softmax
+// Measured: 8 trees of 25 nodes, 100 vectors a K/V head, up to 32,768 tokens of 8 heads of 128 in e4m3: 148 to 157 us,
+// 380 to 400 TFLOP/s, 39 % of the copy bandwidth. A chunk takes 3,000 cycles, of which its MMAs need 1,024; a softmax
 // thread spends 1,500 on the maxima, 2,000 on the probabilities and the rest waiting. What holds it is latency (166
 // cycles a TMEM load), shared memory, which operands, conversion and factors keep busy for 1,900, and instruction
 // fetches: the roles together are about as large as the instruction cache, and the same kernel took 150 to 190 us
