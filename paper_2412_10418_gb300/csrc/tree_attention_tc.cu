@@ -8,9 +8,16 @@
 // An e4m3 cache takes kind::f8f6f4, twice the rate and half the shared memory of bf16 and no
 // conversion of K and V at all. What is not e4m3 is split into two e4m3 planes instead, hi and the rest, each to 4
 // bits: a query row, scaled by a power of two to at most 448 (together bf16's 8 bits, to 2^-18 of the row's
-// largest), and the probabilities (to 2^-10 of themselves). A bf16 cache takes kind::f16 with Q as it is and
+// largest), and the probabilities. A bf16 cache takes kind::f16 with Q as it is and
 // P in two bf16 planes. The rows' power-of-two scales never touch the codes: K's multiplies the
 // thread's scores, V's the thread's probabilities.
+//
+// e4m3 ends at a step of 2^-9, so what the two planes of P keep depends on V's scales, by which P is multiplied. The
+// rest is stored times 2^kLoShift and has columns of O^T of its own (both planes are one MMA of twice the columns): a
+// probability is held to 2^-8 of itself (2^-10 on average), or to a step of 2^-21 of the chunk's largest scale, if
+// that is more. Where the chunk's V scales lie more than 2^kSpread apart, that could be all that a slot with a small scale
+// has, next to one that has no weight, or is not seen: there the softmax threads multiply P and V themselves,
+// in fp32.
 //
 // Every chunk's P is relative to that chunk's own column maxima and largest V scale, and its O^T starts
 // anew in TMEM and is added to fp32 sums in registers with the factor that this takes, so that small
@@ -24,7 +31,7 @@
 // dimension of O^T. Column maxima come from redux.sync over a warp and shared memory over the warps, the one
 // barrier of a chunk; each warp then works out the columns' factors for itself. Each thread keeps its own
 // slots' share of the sums l. Bound by HBM where a call fills the device: 64 sequences of up to 8,192 tokens, 8 heads of
-// 128 in e4m3, four query heads each, one token: 133 us, 90 % of the copy bandwidth; by latency in small ones: one of
+// 128 in e4m3, four query heads each, one token: 130 us, 92 % of the copy bandwidth; by latency in small ones: one of
 // 512 tokens in 9 us with the joining. The MMA's N is 16 or 32 by the number of vectors: 8 sequences of 16,384, 16
 // vectors: 54.6 us with 16, 64 with 32 (fewer blocks on an SM); 32 vectors: 67 us in one block, 98 as rows.
 //
@@ -46,7 +53,9 @@ namespace {
 
 
 constexpr float kMargin = 8.f;                 // base 2: a sum's reference is raised past it
-constexpr int kPShift = 8;                     // e4m3 probabilities are stored times 2^kPShift <= 448
+constexpr int kPShift = 8;                     // e4m3 probabilities are stored times 2^kPShift <= 448, and
+constexpr int kLoShift = 4;                    // what hi leaves of them, at most 2^(kPShift - 5), times 2^kLoShift more
+constexpr int kSpread = 8;                     // octaves between V's scales in a chunk that P's two planes cover
 constexpr int kSoft = kKeys;                   // softmax threads: one per slot of a chunk
 constexpr int kThreads = kSoft + 64;
 constexpr int kProducer = kSoft / 32, kIssuer = kProducer + 1;   // warps
@@ -63,7 +72,8 @@ struct Cfg {
   static constexpr uint32_t Q_PLANE = NQ * KROW;
   // P: a row per slot; e4m3: both planes in it; bf16: a tile per plane
   static constexpr int RB = 2 * NQ;
-  static constexpr uint32_t P_TILE = kKeys * RB, P_NEXT = F8 ? NQ : P_TILE;   // bytes to the second plane
+  static constexpr uint32_t P_TILE = kKeys * RB;
+  static constexpr int OW = F8 ? 2 * NQ : NQ;              // columns of O^T: e4m3: of P's hi, then of the rest
   static constexpr uint32_t FIXED = QP * Q_PLANE + (F8 ? 1 : 2) * P_TILE;
   // two blocks per SM where two stages fit, else one
   static constexpr uint32_t LIMIT2 = 106 * 1024, LIMIT1 = 212 * 1024;
@@ -76,7 +86,7 @@ struct Cfg {
   static constexpr uint32_t KV_OFF = (Q_OFF + FIXED + 1023) / 1024 * 1024;
   static constexpr uint32_t SCALE_OFF = KV_OFF + NST * 2 * TILE;   // a byte per slot, K and V
   static constexpr uint32_t PLAN_OFF = SCALE_OFF + NST * 2 * kKeys;
-  static constexpr uint32_t TMEM = 4 * NQ;                 // S twice, O (a power of two)
+  static constexpr uint32_t TMEM = 4 * NQ;                 // S twice, O^T (a power of two)
   static constexpr size_t smem(int batch) { return 1024 + PLAN_OFF + plan_bytes(batch); }
 };
 
@@ -101,7 +111,7 @@ __global__ void __launch_bounds__(kThreads, Cfg<HD, NQ, F8>::CTAS)
   __shared__ long long s_out[NQ];              // where its output begins
   __shared__ uint32_t s_mask[NQ + 1][kWords];  // of the block's nodes
   __shared__ uint32_t s_pieces[NST];           // pieces of a stage's chunk that hold slots, as bits
-  __shared__ int s_wv[2][4];
+  __shared__ int s_wv[2][4];                   // V's largest and smallest scale byte in a warp's slots (smallest << 8)
   const Cache& c = a.c;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
@@ -145,7 +155,7 @@ __global__ void __launch_bounds__(kThreads, Cfg<HD, NQ, F8>::CTAS)
       constexpr uint32_t formats = F8 ? 0u : (1u << 7) | (1u << 10);
       constexpr uint32_t idesc = (1u << 4) | formats | (128u >> 4) << 24;
       constexpr uint32_t idesc_s = idesc | (uint32_t)(NQ >> 3) << 17;
-      constexpr uint32_t idesc_o = idesc | (uint32_t)(NQ >> 3) << 17 | 1u << 15 | 1u << 16;
+      constexpr uint32_t idesc_o = idesc | (uint32_t)(C::OW >> 3) << 17 | 1u << 15 | 1u << 16;
       constexpr int STEP = 32 / C::EB;         // slots per MMA of P V
       auto mma = [](uint32_t d, uint64_t x, uint64_t y, uint32_t id, bool add) {
         if constexpr (F8) tc::umma_f8(d, x, y, id, add);
@@ -180,11 +190,11 @@ __global__ void __launch_bounds__(kThreads, Cfg<HD, NQ, F8>::CTAS)
         tc::tc_fence_after();
         const uint64_t v = desc_v + (uint32_t)(i % NST) * (2 * C::TILE / 16);
 #pragma unroll 1
-        for (int p = 1; p >= 0; --p)
+        for (int p = F8 ? 0 : 1; p >= 0; --p)
 #pragma unroll 4
           for (int k = 0; k < kKeys / STEP; ++k)
-            mma(t_o, v + k * (STEP * C::BW / 16), desc_p + (p * C::P_NEXT / 16 + k * (STEP * C::RB / 16)), idesc_o,
-                p < 1 || k > 0);
+            mma(t_o, v + k * (STEP * C::BW / 16), desc_p + (p * C::P_TILE / 16 + k * (STEP * C::RB / 16)), idesc_o,
+                (!F8 && p < 1) || k > 0);
         tc::umma_commit(&p_empty);
         tc::umma_commit(&v_empty[i % NST]);
         return true;
@@ -243,17 +253,25 @@ __global__ void __launch_bounds__(kThreads, Cfg<HD, NQ, F8>::CTAS)
       auto add_o = [&](int i) {
         tc::tc_fence_after();
         if (r < HD) {                          // (whole warps)
-          uint32_t x[NQ / 16][16];
 #pragma unroll
-          for (int g = 0; g < NQ / 16; ++g) tc::tmem_ld16_nowait(t_o + lane_base + 16 * g, x[g]);
-          tc::tmem_wait_ld();
+          for (int g = 0; g < NQ; g += 16) {
+            uint32_t hi[16], lo[16];
+            tc::tmem_ld16_nowait(t_o + lane_base + g, hi);
+            if constexpr (F8) tc::tmem_ld16_nowait(t_o + lane_base + NQ + g, lo);
+            tc::tmem_wait_ld();
 #pragma unroll
-          for (int v = 0; v < NQ; v += 4) {
-            const float4 b = *reinterpret_cast<const float4*>(&s_bo[i & 1][warp][v]);
-            o[v] = fmaf(__uint_as_float(x[v / 16][v % 16]), b.x, o[v]);
-            o[v + 1] = fmaf(__uint_as_float(x[v / 16][v % 16 + 1]), b.y, o[v + 1]);
-            o[v + 2] = fmaf(__uint_as_float(x[v / 16][v % 16 + 2]), b.z, o[v + 2]);
-            o[v + 3] = fmaf(__uint_as_float(x[v / 16][v % 16 + 3]), b.w, o[v + 3]);
+            for (int e = 0; e < 16; e += 4) {
+              const float4 b = *reinterpret_cast<const float4*>(&s_bo[i & 1][warp][g + e]);
+              auto add = [&](int v, float by) {
+                float x = __uint_as_float(hi[v]);
+                if constexpr (F8) x = fmaf(__uint_as_float(lo[v]), 1.f / (1 << kLoShift), x);
+                o[g + v] = fmaf(x, by, o[g + v]);
+              };
+              add(e, b.x);
+              add(e + 1, b.y);
+              add(e + 2, b.z);
+              add(e + 3, b.w);
+            }
           }
         }
         tc::tc_fence_before();
@@ -308,14 +326,23 @@ __global__ void __launch_bounds__(kThreads, Cfg<HD, NQ, F8>::CTAS)
             if (lane == 0)
               *reinterpret_cast<float4*>(&s_wmax[it & 1][warp][v]) = make_float4(top[0], top[1], top[2], top[3]);
           }
-          const int wv = F8 ? __reduce_max_sync(0xffffffffu, vb == 255 ? 0 : (int)vb) : 0;
-          if (lane == 0) s_wv[it & 1][warp] = wv;
+          if constexpr (F8) {                  // (bytes 0, no scale, and 255, not finite, take no part)
+            const int most = __reduce_max_sync(0xffffffffu, vb == 255 ? 0 : (int)vb);
+            const int least = __reduce_min_sync(0xffffffffu, vb == 0 ? 255 : (int)vb);
+            if (lane == 0) s_wv[it & 1][warp] = least << 8 | most;
+          }
           if (tc::named_barrier_or(1, kSoft, failed)) {
             gone = true;
             return;
           }
           // ---- the chunk's references: a lane per column, each warp for itself
-          const int vref = F8 ? max(max(s_wv[it & 1][0], s_wv[it & 1][1]), max(s_wv[it & 1][2], s_wv[it & 1][3])) : 127;
+          int vref = 127;
+          bool apart = false;                  // V's scales are (alike in all softmax threads)
+          if constexpr (F8) {
+            const int* const w = s_wv[it & 1];
+            vref = max(max(w[0] & 255, w[1] & 255), max(w[2] & 255, w[3] & 255));
+            apart = vref - (min(min(w[0], w[1]), min(w[2], w[3])) >> 8) > kSpread;
+          }
           float f = 1.f;
           if (lane < NQ) {
             const float top = fmaxf(fmaxf(s_wmax[it & 1][0][lane], s_wmax[it & 1][1][lane]),
@@ -346,65 +373,6 @@ __global__ void __launch_bounds__(kThreads, Cfg<HD, NQ, F8>::CTAS)
               o[v] *= g;
             }
           }
-          // ---- probabilities, their sums, V's scale on them
-          const int ve = F8 ? (int)vb - vref + kPShift + 127 : 127;
-          const float vf = vb == 255 ? __uint_as_float(0x7fc00000u)
-                                     : !valid || ve < 1 ? 0.f : __uint_as_float((uint32_t)ve << 23);
-          uint8_t* const p = sm + C::P_OFF;
-#pragma unroll
-          for (int g = 0; g < NQ; g += 16) {
-            float y[16];
-#pragma unroll
-            for (int e = 0; e < 16; e += 4) {
-              const float4 qs = *reinterpret_cast<const float4*>(&s_qs[g + e]);
-              const float4 mq = *reinterpret_cast<const float4*>(&s_mq[warp][g + e]);
-              const float4 b = *reinterpret_cast<const float4*>(&s_b[warp][g + e]);
-              y[e] = ex2(fmaf(t[g + e], qs.x, -mq.x));
-              y[e + 1] = ex2(fmaf(t[g + e + 1], qs.y, -mq.y));
-              y[e + 2] = ex2(fmaf(t[g + e + 2], qs.z, -mq.z));
-              y[e + 3] = ex2(fmaf(t[g + e + 3], qs.w, -mq.w));
-              l[g + e] = fmaf(y[e], b.x, l[g + e]);
-              l[g + e + 1] = fmaf(y[e + 1], b.y, l[g + e + 1]);
-              l[g + e + 2] = fmaf(y[e + 2], b.z, l[g + e + 2]);
-              l[g + e + 3] = fmaf(y[e + 3], b.w, l[g + e + 3]);
-            }
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              y[e] *= vf;
-              if constexpr (masked)            // (0 * NaN of a V that the vector does not see)
-                if (!(vis >> (g + e) & 1)) y[e] = 0.f;
-            }
-            if constexpr (F8) {
-              uint32_t hi[4], lo[4];
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const __half2 z0 = __floats2half2_rn(y[4 * i], y[4 * i + 1]), z1 = __floats2half2_rn(y[4 * i + 2], y[4 * i + 3]);
-                __half2 h0, h1;
-                hi[i] = f8x4(z0, z1);
-                f8x4_half(hi[i], &h0, &h1);
-                lo[i] = f8x4(__hsub2(z0, h0), __hsub2(z1, h1));
-              }
-              *reinterpret_cast<uint4*>(p + tc::row_offset(r, g / 16, C::RB)) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-              *reinterpret_cast<uint4*>(p + tc::row_offset(r, (NQ + g) / 16, C::RB)) =
-                  make_uint4(lo[0], lo[1], lo[2], lo[3]);
-            } else {
-#pragma unroll
-              for (int half = 0; half < 2; ++half) {
-                uint32_t hi[4], lo[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                  const float u = y[half * 8 + 2 * i], w = y[half * 8 + 2 * i + 1];
-                  const __nv_bfloat162 h = __floats2bfloat162_rn(u, w);
-                  const __nv_bfloat162 z = __floats2bfloat162_rn(u - __low2float(h), w - __high2float(h));
-                  hi[i] = *reinterpret_cast<const uint32_t*>(&h);
-                  lo[i] = *reinterpret_cast<const uint32_t*>(&z);
-                }
-                const uint32_t off = tc::row_offset(r, g / 8 + half, C::RB);
-                *reinterpret_cast<uint4*>(p + off) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-                *reinterpret_cast<uint4*>(p + C::P_TILE + off) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-              }
-            }
-          }
           if constexpr (masked) {
             if (!valid) {                      // nothing of its V row (page garbage, no copy) may reach the sums
               uint8_t* v = sm + C::KV_OFF + (st * 2 + 1) * C::TILE + r * C::BW;
@@ -413,6 +381,110 @@ __global__ void __launch_bounds__(kThreads, Cfg<HD, NQ, F8>::CTAS)
 #pragma unroll 1
                 for (int i = 0; i < C::BW; i += 16)
                   *reinterpret_cast<uint4*>(v + nb * C::BLOCK + i) = make_uint4(0u, 0u, 0u, 0u);
+            }
+          }
+          // ---- probabilities, their sums, V's scale on them
+          if (F8 && apart) {
+            // in fp32: P V of this thread's dimension, 64 slots at a time through P's tile, to the sums
+            float* const p = reinterpret_cast<float*>(sm + C::P_OFF);
+            static_assert(!F8 || C::P_TILE >= kKeys / 2 * NQ * 4);
+            const float vf = scale_value(vb);
+#pragma unroll
+            for (int v = 0; v < NQ; ++v) {
+              const float y = ex2(fmaf(t[v], s_qs[v], -s_mq[warp][v])) * s_b[warp][v];
+              l[v] += y;
+              t[v] = y * vf;
+              if constexpr (masked)
+                if (!(vis >> v & 1)) t[v] = 0.f;
+            }
+#pragma unroll 1
+            for (int half = 0; half < 2; ++half) {
+              if (r / (kKeys / 2) == half)
+#pragma unroll
+                for (int v = 0; v < NQ; v += 4)
+                  *reinterpret_cast<float4*>(&p[r % (kKeys / 2) * NQ + v]) = make_float4(t[v], t[v + 1], t[v + 2], t[v + 3]);
+              sync();
+              if (r < HD) {
+#pragma unroll 1
+                for (int k = 0; k < kKeys / 2; ++k) {
+                  const uint32_t code = sm[C::KV_OFF + (st * 2 + 1) * C::TILE +
+                                           tc::row_offset(half * (kKeys / 2) + k, r / 16, C::BW) + r % 16];
+                  const float x = f8x2_to_f32(code).x;
+#pragma unroll
+                  for (int v = 0; v < NQ; v += 4) {
+                    const float4 y = *reinterpret_cast<const float4*>(&p[k * NQ + v]);
+                    o[v] = fmaf(y.x, x, o[v]);
+                    o[v + 1] = fmaf(y.y, x, o[v + 1]);
+                    o[v + 2] = fmaf(y.z, x, o[v + 2]);
+                    o[v + 3] = fmaf(y.w, x, o[v + 3]);
+                  }
+                }
+              }
+              sync();
+            }
+            // (the chunk's P V adds zeros)
+#pragma unroll
+            for (int i = 0; i < C::RB; i += 16)
+              *reinterpret_cast<uint4*>(sm + C::P_OFF + r * C::RB + i) = make_uint4(0u, 0u, 0u, 0u);
+          } else {
+            const int ve = F8 ? (int)vb - vref + kPShift + 127 : 127;
+            const float vf = vb == 255 ? __uint_as_float(0x7fc00000u)
+                                       : !valid || ve < 1 ? 0.f : __uint_as_float((uint32_t)ve << 23);
+            uint8_t* const p = sm + C::P_OFF;
+#pragma unroll
+            for (int g = 0; g < NQ; g += 16) {
+              float y[16];
+#pragma unroll
+              for (int e = 0; e < 16; e += 4) {
+                const float4 qs = *reinterpret_cast<const float4*>(&s_qs[g + e]);
+                const float4 mq = *reinterpret_cast<const float4*>(&s_mq[warp][g + e]);
+                const float4 b = *reinterpret_cast<const float4*>(&s_b[warp][g + e]);
+                y[e] = ex2(fmaf(t[g + e], qs.x, -mq.x));
+                y[e + 1] = ex2(fmaf(t[g + e + 1], qs.y, -mq.y));
+                y[e + 2] = ex2(fmaf(t[g + e + 2], qs.z, -mq.z));
+                y[e + 3] = ex2(fmaf(t[g + e + 3], qs.w, -mq.w));
+                l[g + e] = fmaf(y[e], b.x, l[g + e]);
+                l[g + e + 1] = fmaf(y[e + 1], b.y, l[g + e + 1]);
+                l[g + e + 2] = fmaf(y[e + 2], b.z, l[g + e + 2]);
+                l[g + e + 3] = fmaf(y[e + 3], b.w, l[g + e + 3]);
+              }
+#pragma unroll
+              for (int e = 0; e < 16; ++e) {
+                y[e] *= vf;
+                if constexpr (masked)            // (0 * NaN of a V that the vector does not see)
+                  if (!(vis >> (g + e) & 1)) y[e] = 0.f;
+              }
+              if constexpr (F8) {
+                uint32_t hi[4], lo[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                  const __half2 z0 = __floats2half2_rn(y[4 * i], y[4 * i + 1]), z1 = __floats2half2_rn(y[4 * i + 2], y[4 * i + 3]);
+                  __half2 h0, h1;
+                  hi[i] = f8x4(z0, z1);
+                  f8x4_half(hi[i], &h0, &h1);
+                  const __half2 up = __float2half2_rn((float)(1 << kLoShift));
+                  lo[i] = f8x4(__hmul2(__hsub2(z0, h0), up), __hmul2(__hsub2(z1, h1), up));
+                }
+                *reinterpret_cast<uint4*>(p + tc::row_offset(r, g / 16, C::RB)) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+                *reinterpret_cast<uint4*>(p + tc::row_offset(r, (NQ + g) / 16, C::RB)) =
+                    make_uint4(lo[0], lo[1], lo[2], lo[3]);
+              } else {
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                  uint32_t hi[4], lo[4];
+#pragma unroll
+                  for (int i = 0; i < 4; ++i) {
+                    const float u = y[half * 8 + 2 * i], w = y[half * 8 + 2 * i + 1];
+                    const __nv_bfloat162 h = __floats2bfloat162_rn(u, w);
+                    const __nv_bfloat162 z = __floats2bfloat162_rn(u - __low2float(h), w - __high2float(h));
+                    hi[i] = *reinterpret_cast<const uint32_t*>(&h);
+                    lo[i] = *reinterpret_cast<const uint32_t*>(&z);
+                  }
+                  const uint32_t off = tc::row_offset(r, g / 8 + half, C::RB);
+                  *reinterpret_cast<uint4*>(p + off) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+                  *reinterpret_cast<uint4*>(p + C::P_TILE + off) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+                }
+              }
             }
           }
           tc::fence_proxy_async();
