@@ -7,9 +7,12 @@
 // S of an e4m3 cache is taken as in tree_attention_tc.cu, from the codes and two e4m3 planes of Q. P V is not:
 // turning a pair of probabilities into two e4m3 planes takes 14 cycles of a quarter of an SM (four
 // conversions at 2 or 4 and a difference, measured), 7 a score, where its exponential takes 4. Here the chunk's V is
-// turned into fp16 once for all rows instead, exactly, with its power-of-two scales multiplied in, and P into
-// fp16 by one conversion a pair: 2^-12 of itself, over 22 octaves below a row's reference. A bf16 cache has Q and V
-// as they are and P in two bf16 planes.
+// turned into fp16 once for all rows instead, with its power-of-two scales multiplied in relative to a reference (the
+// largest of the first chunk, raised when one passes it by more than 2^kVRoom), and P into
+// fp16 by one conversion a pair: 2^-12 of itself, over 22 octaves below a row's reference. That is exact for V's scales
+// down to 2^-kVBelow of the reference; a chunk with a smaller one has V in bf16, exact over fp32's range, and P in two
+// bf16 planes (2^-17), as has a bf16 cache with its V as it is. Chunks with masks do the same: one code
+// for all that is rare.
 //
 // A softmax thread has a vector (a TMEM lane) and walks all the chunk's slots (columns): maximum, reference,
 // probabilities and their sum are its own, no value crosses lanes and no barrier stands in a chunk, whatever
@@ -60,7 +63,8 @@ constexpr int kConvWarp = kSoft / 32, kProducer = kConvWarp + kConv / 32, kIssue
 constexpr float kMargin = 7.f;                 // base 2: probabilities are at most 2^kMargin of a reference, and
 constexpr float kUp = 7.f;                     // stored times 2^kUp: below fp16's largest
 constexpr int kBuf = 3;                        // S (then P) buffers in TMEM; O has the rest
-constexpr int kVRoom = 6;                      // octaves that V's scales may pass theirs by: 448 * 2^6 in fp16
+constexpr int kVRoom = 6;                      // octaves that V's scales may pass their reference by: 448 * 2^6 in fp16,
+constexpr int kVBelow = 15;                    // and lie below it: 2^-9 * 2^-15
 
 template <int HD, bool F8>
 struct Cfg {
@@ -99,6 +103,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   __shared__ __align__(8) uint64_t s_full[kBuf], p_full[kBuf], r_full[kBuf], pv_done[2], q_full, done;
   __shared__ uint32_t s_tmem;
   __shared__ __align__(16) uint32_t s_valid[NST][4], s_nan[NST][4];   // slots that there are, whose V is not finite
+  __shared__ int s_rare[NST], s_h_rare[2];     // a chunk with masks or V's scales far apart: by stages; by V's 16-bit buffers
   __shared__ int s_vref[NST], s_vstep[NST];    // V's reference in the chunk, and that of the chunk before less it
   __shared__ float s_qs[2][kRows];             // score factors, of this segment's queries and the next one's
   __shared__ int s_v;                          // V's reference at the end
@@ -155,9 +160,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       constexpr uint32_t formats = F8 ? 0u : (1u << 7) | (1u << 10);
       constexpr uint32_t idesc = (1u << 4) | formats | (128u >> 4) << 24;
       constexpr uint32_t idesc_s = idesc | (uint32_t)(kKeys >> 3) << 17;
-      // P V in 16 bits: fp16 (format 0) beside an e4m3 cache, else bf16
-      constexpr uint32_t idesc_o = (1u << 4) | (128u >> 4) << 24 | (F8 ? 0u : (1u << 7) | (1u << 10)) |
-                                   (uint32_t)(HD >> 3) << 17 | 1u << 16;
+      // P V in 16 bits: fp16 (format 0) or bf16
+      constexpr uint32_t idesc_half = (1u << 4) | (128u >> 4) << 24 | (uint32_t)(HD >> 3) << 17 | 1u << 16;
+      constexpr uint32_t idesc_bf16 = idesc_half | (1u << 7) | (1u << 10);
       const uint32_t sbase = tc::smem_u32(sm);
       const uint64_t desc_q = tc::desc_rows(sbase, C::BW, 16);
       const uint64_t desc_k = tc::desc_rows(sbase + C::KV_OFF, C::BW, 16);
@@ -192,12 +197,18 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint64_t v = desc_v + (F8 ? (uint32_t)(i & 1) * (C::H_TILE / 16) : (uint32_t)(i % NST) * (2 * C::TILE / 16));
         // 16 slots an MMA: 8 columns of P, 16 rows of 128 bytes of V. P of 32 slots lies in the columns that held
         // their S, bf16 hi then lo.
-#pragma unroll 1
-        for (int p = F8 ? 0 : 1; p >= 0; --p)
+        const auto plane = [&](int p, uint32_t idesc, bool add) {
 #pragma unroll
           for (int k = 0; k < kKeys / 16; ++k)
-            tc::umma_tmem_a(t_o, tmem + i % kBuf * kKeys + k / 2 * 32 + p * 16 + k % 2 * 8, v + k * (16 * 128 / 16), idesc_o,
-                            add || (!F8 && p < 1) || k > 0);
+            tc::umma_tmem_a(t_o, tmem + i % kBuf * kKeys + k / 2 * 32 + p * 16 + k % 2 * 8, v + k * (16 * 128 / 16), idesc,
+                            add || k > 0);
+        };
+        if (F8 && !s_h_rare[i & 1]) {
+          plane(0, idesc_half, add);
+        } else {
+#pragma unroll 1
+          for (int p = 1; p >= 0; --p) plane(p, idesc_bf16, add || p < 1);
+        }
         tc::umma_commit(&pv_done[i & 1]);
         if (!F8) tc::umma_commit(&v_empty[i % NST]);
         return true;
@@ -249,6 +260,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (vref == 0 || vmax > vref + kVRoom) vref = vmax;
         float kf[4], vf[4];
         uint32_t nan = 0;
+        bool rare = n < 4 || slot + 3 >= s.len;   // slots past the item's, without a page or of the tree
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const uint32_t k = kb >> (8 * e) & 255, v = vb >> (8 * e) & 255;
@@ -256,7 +268,9 @@ __global__ void __launch_bounds__(kThreads, 1)
           kf[e] = e < n ? scale_value(k) : 1.f;
           vf[e] = e >= n || v == 255 || x < 1 ? 0.f : __uint_as_float((uint32_t)x << 23);
           nan |= (uint32_t)(e < n && v == 255) << e;
+          rare = rare || (e < n && (v == 255 || (F8 && v > 0 && x < 127 - kVBelow)));
         }
+        rare = __any_sync(0xffffffffu, rare);
         float* to = reinterpret_cast<float*>(sm + C::FACTOR_OFF) + st * 2 * kKeys + 4 * lane;
         *reinterpret_cast<float4*>(to) = make_float4(kf[0], kf[1], kf[2], kf[3]);
         if (F8) *reinterpret_cast<float4*>(to + kKeys) = make_float4(vf[0], vf[1], vf[2], vf[3]);
@@ -274,6 +288,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (lane == 0) {
           s_vref[st] = F8 ? vref : 127;
           s_vstep[st] = F8 && before ? before - vref : 0;
+          s_rare[st] = rare;
         }
         __syncwarp();
         if (lane == 0) tc::mbar_arrive(F8 ? &v_empty[st] : &k_empty[st]);   // (the scale bytes are read)
@@ -335,13 +350,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         ok = ok && wait_for(&s_full[it % kBuf], parity(it, kBuf), a.status);
         failed = !__all_sync(0xffffffffu, ok);   // (a warp gives up as one)
         tc::tc_fence_after();
-        // a chunk with slots of the tree, past the item's, without a page or with a V that is not finite: each row has
-        // its mask
         const int node0 = (s.c0 + i) * kKeys - s.len;
-        const uint4 valid = *reinterpret_cast<const uint4*>(s_valid[st]);
-        const uint4 nan = *reinterpret_cast<const uint4*>(s_nan[st]);
-        const bool masked = node0 > -kKeys || (valid.x & valid.y & valid.z & valid.w) != ~0u ||
-                            (nan.x | nan.y | nan.z | nan.w) != 0u;
         auto word = [&](int w) -> uint32_t {   // slots 32 w .. 32 w + 31 that this row sees
           const int first = node0 + 32 * w;    // the tree's node in the first of them
           uint32_t x;
@@ -351,8 +360,9 @@ __global__ void __launch_bounds__(kThreads, 1)
           else x = __funnelshift_r(my_mask[first >> 5], first >> 5 < kWords - 1 ? my_mask[(first >> 5) + 1] : 0u, first & 31);
           return r < s.nq ? x & s_valid[st][w] : 0u;
         };
-        // Code of its own for chunks with masks: as one, the compiler selects on every score, masked or not,
-        // which took twice the time.
+        // Code of its own for chunks with slots of the tree, past the item's, without a page or with a V that is not finite,
+        // where each row has its mask (and those with V's scales far apart): as one, the compiler selects on every score,
+        // masked or not, which took twice the time.
         auto softmax = [&](auto masked) {
           // slots 16 g .. as scores times K's scale, in pairs
           auto scores = [&](const uint32_t (&x)[16], int g, uint32_t seen, uint64_t (&t)[8]) {
@@ -442,7 +452,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                   if (m & 1) y.x = __uint_as_float(0x7fc00000u);
                   if (m & 2) y.y = __uint_as_float(0x7fc00000u);
                 }
-                if constexpr (F8) {
+                if constexpr (F8 && !masked) {
                   const __half2 p = __floats2half2_rn(y.x, y.y);
                   hi[e] = *reinterpret_cast<const uint32_t*>(&p);
                 } else {
@@ -454,7 +464,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               }
               const uint32_t to = t_s + 32 * w + h * 8;
               tc::tmem_st_nowait(to, hi);
-              if (!F8) tc::tmem_st_nowait(to + 16, lo);
+              if (!F8 || masked) tc::tmem_st_nowait(to + 16, lo);
             }
           }
           const float2 two = unpair(add);
@@ -462,7 +472,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           tc::tmem_wait_st();
         };
         if (live) {
-          if (masked) softmax(std::true_type());
+          if (s_rare[st]) softmax(std::true_type());
           else softmax(std::false_type());
           failed = !__all_sync(0xffffffffu, ok);
         } else {
@@ -554,8 +564,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       it0 += n;
     }
   } else if (F8) {
-    // ------------------------------------------------------------------------- V to fp16
-    // 16 codes at a time, exactly, with the rows' scales; rows that there are not become zeros
+    // ------------------------------------------------------------------------- V to 16 bits
+    // 16 codes at a time, exactly, with the rows' scales; rows that there are not become zeros. fp16, which two
+    // instructions a pair give; in a rare chunk bf16, in which no scale is too small.
     constexpr int kRowsAt = kConv / (HD / 16);
     const int row0 = (threadIdx.x - kSoft) / (HD / 16), part = (threadIdx.x - kSoft) % (HD / 16);
     // (the other half first in the second block of 64 dimensions: eight lanes' stores then meet no bank twice)
@@ -570,28 +581,52 @@ __global__ void __launch_bounds__(kThreads, 1)
            wait_for(&pv_done[i & 1], parity(i, 2) ^ 1, a.status);   // (chunk i - 2's: the buffer is free)
       ok = __all_sync(0xffffffffu, ok);
       const float* vf = reinterpret_cast<const float*>(sm + C::FACTOR_OFF) + (st * 2 + 1) * kKeys;
+      const bool rare = s_rare[st];
+      if (threadIdx.x == kSoft) s_h_rare[i & 1] = rare;
       const uint8_t* from = sm + C::KV_OFF + (st * 2 + 1) * C::TILE + tc::row_offset(row0, part, C::BW);
       uint8_t* to = sm + C::H_OFF + (i & 1) * C::H_TILE;
-#pragma unroll 2
-      for (int k = 0; k < kKeys / kRowsAt; ++k) {   // (rows that many apart lie alike in their tiles)
-        const int row = row0 + k * kRowsAt;
-        const uint4 u = *reinterpret_cast<const uint4*>(from + k * kRowsAt * C::BW);
-        const float f = vf[row];
-        const __half2 f2 = __float2half2_rn(f);
-        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-        uint32_t h[8];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          __half2 p, q;
-          f8x4_half(f == 0.f ? 0u : w[e], &p, &q);
-          p = __hmul2(p, f2);
-          q = __hmul2(q, f2);
-          h[2 * e] = *reinterpret_cast<const uint32_t*>(&p);
-          h[2 * e + 1] = *reinterpret_cast<const uint32_t*>(&q);
-        }
+      const auto store = [&](int k, const uint32_t (&h)[8]) {   // (rows that many apart lie alike in their tiles)
         const uint4 lo = make_uint4(h[0], h[1], h[2], h[3]), hi = make_uint4(h[4], h[5], h[6], h[7]);
         *reinterpret_cast<uint4*>(to + k * (kRowsAt * 128) + to0) = flip ? hi : lo;
         *reinterpret_cast<uint4*>(to + k * (kRowsAt * 128) + to1) = flip ? lo : hi;
+      };
+      if (!rare) {
+#pragma unroll 2
+        for (int k = 0; k < kKeys / kRowsAt; ++k) {
+          const uint4 u = *reinterpret_cast<const uint4*>(from + k * kRowsAt * C::BW);
+          const float f = vf[row0 + k * kRowsAt];
+          const __half2 f2 = __float2half2_rn(f);
+          const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+          uint32_t h[8];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            __half2 p, q;
+            f8x4_half(w[e], &p, &q);
+            p = __hmul2(p, f2);
+            q = __hmul2(q, f2);
+            h[2 * e] = *reinterpret_cast<const uint32_t*>(&p);
+            h[2 * e + 1] = *reinterpret_cast<const uint32_t*>(&q);
+          }
+          store(k, h);
+        }
+      } else {
+#pragma unroll 1
+        for (int k = 0; k < kKeys / kRowsAt; ++k) {
+          const uint4 u = *reinterpret_cast<const uint4*>(from + k * kRowsAt * C::BW);
+          const float f = vf[row0 + k * kRowsAt];
+          const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+          uint32_t h[8];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            __half2 p, q;
+            f8x4_half(f == 0.f ? 0u : w[e], &p, &q);   // (a row that there is not holds anything)
+            const float2 x = __half22float2(p), y = __half22float2(q);
+            const __nv_bfloat162 a2 = __floats2bfloat162_rn(x.x * f, x.y * f), b2 = __floats2bfloat162_rn(y.x * f, y.y * f);
+            h[2 * e] = *reinterpret_cast<const uint32_t*>(&a2);
+            h[2 * e + 1] = *reinterpret_cast<const uint32_t*>(&b2);
+          }
+          store(k, h);
+        }
       }
       tc::fence_proxy_async();
       tc::mbar_arrive(&h_full[i & 1]);

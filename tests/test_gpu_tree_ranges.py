@@ -68,7 +68,8 @@ def problem(cdsl, T, H, kvh, hd, cache, dtype, size, seed, lens=(700, 260)):
     return c, q.to(dtype).cuda(), k, v * size, lens, mask, [T] * B
 
 
-HEADS = [(1, 2, 2, 128), (1, 8, 2, 64), (8, 8, 2, 128), (8, 4, 2, 64)]   # 1, 4, 32 and 16 vectors a K/V head
+# 1, 4, 32 and 16 vectors a K/V head (slots as the MMA's rows), 36 and 34 (vectors as rows)
+HEADS = [(1, 2, 2, 128), (1, 8, 2, 64), (8, 8, 2, 128), (8, 4, 2, 64), (9, 8, 2, 128), (17, 4, 2, 64)]
 CACHES = pytest.mark.parametrize("cache", [F8, BF], ids=["f8", "bf16"])
 TYPES = pytest.mark.parametrize("dtype", [F32, BF], ids=["q32", "q16"])
 
