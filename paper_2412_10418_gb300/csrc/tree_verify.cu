@@ -132,6 +132,7 @@ __global__ void __launch_bounds__(kThreads) k_tree_verify(VerifyArgs a) {
     const u64 best = row_max(p.p, V, s_red, &bad);
     if (bad) {
       if (tid == 0) set_status(a.status, CDSL_ENONFINITE);
+      last = -1;                       // (greedy: not the row's before)
       break;
     }
     p.top = key_value(best);
@@ -422,6 +423,7 @@ __global__ void __launch_bounds__(kWalk) k_tree_walk(VerifyArgs a) {
     reduce_cluster<false>(best, best_q, drafts, s_slots, turn, C, rank);
     if (best == 0 || best == ~0ull || (drafts && (best_q == 0 || best_q == ~0ull))) {
       if (rank == 0 && tid == 0) set_status(a.status, CDSL_ENONFINITE);
+      last = -1;                       // (greedy: not the row's before)
       break;
     }
     int next = -1;

@@ -1,0 +1,38 @@
+"""Tree validation (include/cdsl_tree.h) at nodes whose rows are not finite, by the kernel
+that keeps a row in registers and by the one for rows beyond them."""
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+from test_gpu_tree import cdsl, run_verify  # noqa: E402,F401
+from tree_reference import BF, F32  # noqa: E402
+
+VOCABS = [300, 5000, 163841]                   # one block, a cluster, beyond the registers
+
+
+@pytest.mark.parametrize("V", VOCABS)
+@pytest.mark.parametrize("dtype", [F32, BF], ids=["f32", "bf16"])
+@pytest.mark.parametrize("bad", ["nan", "+inf", "-inf"])
+def test_greedy_walk_ends_without_a_token_at_a_bad_row(cdsl, V, dtype, bad):
+    """A chain 0-1-2 of the target's best tokens, the row of node 0, 1 or 2 not finite: the nodes before are taken, and
+    no token is drawn. -inf: the whole row."""
+    T = 3
+    logits = torch.zeros((T + 1, T, V), dtype=dtype)
+    best = [V - 1, 11, 7]
+    for i, x in enumerate(best):
+        logits[:, i, x] = 4
+    for b in range(T):
+        if bad == "-inf":
+            logits[b, b] = float("-inf")
+        else:
+            logits[b, b, 5] = float(bad)
+    tokens = torch.tensor([[0, best[0], best[1]]] * (T + 1), dtype=torch.int32)
+    u, u_last = torch.zeros((T + 1, T)), torch.zeros(T + 1)
+    for temperature in (0.0, 0.25):
+        path, n, emitted, st = run_verify(cdsl, logits, None, tokens, [[0, 0, 1]] * (T + 1), u, u_last, temperature)
+        assert st == cdsl.CDSL_ENONFINITE
+        assert n == [1, 2, 3, 3]
+        assert path.tolist() == [[0, -1, -1], [0, 1, -1], [0, 1, 2], [0, 1, 2]]
+        assert emitted[:3].tolist() == [[-1, -1, -1], [best[0], -1, -1], [best[0], best[1], -1]]
+        assert emitted[3, :2].tolist() == best[:2] and (temperature > 0 or int(emitted[3, 2]) == best[2])
