@@ -127,7 +127,7 @@ CDSL_API int32_t cdsl_tree_attention(const cdsl_kv_cache* cache, int32_t layer, 
  *   W_v = floor(2^31 exp((l_v - max l) / temperature)), Z their sum: c is taken when
  *   floor(k Z / 2^24) < W_x, k = floor(2^24 u[b, c]).
  *   Drafts sampled from M_q (d_draft_logits[b, i] the row that node i's children were sampled from,
- *   independently, at the same temperature): c is taken when u[b, c] q(x) < p(x), and if it is not, p
+ *   independently, at the same temperature; not read where node i has none): c is taken when u[b, c] q(x) < p(x), and if it is not, p
  *   becomes max(p - q, 0) over its sum (p stays where that is nothing); W_v = floor(2^31 max(p - q, 0)).
  *   The drawn token is the first v with W_0 + .. + W_v > floor(k Z / 2^24), k = floor(2^24
  *   u_last[b]): both procedures draw from p exactly, to the weights' resolution. Whole numbers make it

@@ -154,7 +154,9 @@ __global__ void __launch_bounds__(kThreads) k_tree_verify(VerifyArgs a) {
     const float inv0 = __fdiv_rn(1.f, __fmul_rn(__ull2float_rn(Z), 1.f / kTwo31));
     Row<T> q = {nullptr, 0.f, a.inv_t};
     float invq = 0.f;
-    if (a.draft) {
+    bool kids = false;                 // (nothing was sampled from the draft's row of a leaf)
+    for (int i = cur + 1; i < n; ++i) kids = kids || s_par[i] == cur;
+    if (a.draft && kids) {
       q.p = static_cast<const T*>(a.draft) + b * a.sd[0] + cur * a.sd[1];
       q.top = key_value(row_max(q.p, V, s_red, &bad));
       if (bad) {
@@ -352,7 +354,7 @@ __global__ void __launch_bounds__(kWalk) k_tree_walk(VerifyArgs a) {
     if (rank == 0) a.path[(size_t)b * a.T + i] = a.emitted[(size_t)b * a.T + i] = -1;
   }
   const float u_last = a.u_last[b];
-  const bool greedy = a.inv_t == 0.f, drafts = a.draft != nullptr;
+  const bool greedy = a.inv_t == 0.f, given = a.draft != nullptr;
   const int size = ((V + C - 1) / C + E - 1) / E * E, base = rank * size, top = min(V, base + size);   // this block's tokens
   int turn = 0;
   if (C > 1) tc::cluster_wait();
@@ -377,6 +379,8 @@ __global__ void __launch_bounds__(kWalk) k_tree_walk(VerifyArgs a) {
       if (m) a.emitted[(size_t)b * a.T + m - 1] = s_tok[cur];
     }
     ++m;
+    bool drafts = false;               // (nothing was sampled from the draft's row of a leaf)
+    if (given) drafts = (s_child[cur][0] | s_child[cur][1] | s_child[cur][2] | s_child[cur][3]) != 0u;
     // ---- the row, the children's logits, and the likely next rows into L2
     float l[J], q[J];
     const T* const row = rows + cur * a.sl[1];

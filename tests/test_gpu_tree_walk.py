@@ -1,4 +1,4 @@
-"""Tree validation (include/cdsl_tree.h) at nodes whose rows are not finite, by the kernel
+"""Tree validation (include/cdsl_tree.h) at nodes whose rows are not finite and at nodes without children, by the kernel
 that keeps a row in registers and by the one for rows beyond them."""
 import pytest
 
@@ -36,3 +36,30 @@ def test_greedy_walk_ends_without_a_token_at_a_bad_row(cdsl, V, dtype, bad):
         assert path.tolist() == [[0, -1, -1], [0, 1, -1], [0, 1, 2], [0, 1, 2]]
         assert emitted[:3].tolist() == [[-1, -1, -1], [best[0], -1, -1], [best[0], best[1], -1]]
         assert emitted[3, :2].tolist() == best[:2] and (temperature > 0 or int(emitted[3, 2]) == best[2])
+
+
+@pytest.mark.parametrize("V", VOCABS)
+@pytest.mark.parametrize("dtype", [F32, BF], ids=["f32", "bf16"])
+@pytest.mark.parametrize("left", ["nan", "+inf", "-inf"])
+def test_draft_rows_of_leaves_do_not_matter(cdsl, V, dtype, left):
+    """The draft's row of a node without children was never sampled from: whatever is in it, the target's row alone
+    decides the draw there. Sequences: a chain taken to its leaf; a chain of which `nodes` leaves out the last, so that
+    node 1 is the leaf; the root alone; a node whose only child names a later parent."""
+    B, T = 4, 3
+    g = torch.Generator().manual_seed(V)
+    logits = torch.randn((B, T, V), generator=g).to(dtype)
+    draft = torch.randn((B, T, V), generator=g).to(dtype)
+    tokens = torch.randint(0, V, (B, T), generator=g, dtype=torch.int32)
+    parents = [[0, 0, 1]] * 3 + [[0, 0, 2]]
+    nodes = [3, 2, 1, 3]
+    u, u_last = torch.zeros((B, T)), torch.rand(B, generator=g)     # (u = 0 takes every child that has a weight)
+    want = run_verify(cdsl, logits, draft, tokens, parents, u, u_last, 1.0, nodes)
+    assert want[3] == cdsl.CDSL_OK and want[1] == [3, 2, 1, 2]
+    for b, i in ((0, 2), (1, 1), (2, 0), (3, 1)):
+        if left == "-inf":
+            draft[b, i] = float("-inf")
+        else:
+            draft[b, i, 3] = float(left)
+    got = run_verify(cdsl, logits, draft, tokens, parents, u, u_last, 1.0, nodes)
+    assert got[3] == cdsl.CDSL_OK and got[1] == want[1]
+    assert torch.equal(got[0], want[0]) and torch.equal(got[2], want[2])
