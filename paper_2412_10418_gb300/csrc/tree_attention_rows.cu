@@ -84,7 +84,7 @@ struct Cfg {
   static constexpr int NST = FIT > 4 ? 4 : FIT;
   static_assert(NST >= 2, "stages");
   static constexpr uint32_t SCALE_OFF = KV_OFF + NST * 2 * TILE;
-  // K's scale of each slot, and V's relative to its reference (0: nothing, or not finite)
+  // K's scale of each slot, and V's, e4m3: relative to its reference (0: nothing, or not finite)
   static constexpr uint32_t FACTOR_OFF = SCALE_OFF + NST * 2 * kKeys;
   static constexpr uint32_t PLAN_OFF = FACTOR_OFF + NST * 2 * kKeys * 4;
   static constexpr size_t smem(int batch) { return 1024 + PLAN_OFF + plan_bytes(batch); }
@@ -103,7 +103,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   __shared__ __align__(8) uint64_t s_full[kBuf], p_full[kBuf], r_full[kBuf], pv_done[2], q_full, done;
   __shared__ uint32_t s_tmem;
   __shared__ __align__(16) uint32_t s_valid[NST][4], s_nan[NST][4];   // slots that there are, whose V is not finite
-  __shared__ int s_rare[NST], s_h_rare[2];     // a chunk with masks or V's scales far apart: by stages; by V's 16-bit buffers
+  __shared__ int s_rare[NST], s_h_rare[2];     // a chunk with masks, V's scales far apart (bf16: not 1): by stages; V's buffers
   __shared__ int s_vref[NST], s_vstep[NST];    // V's reference in the chunk, and that of the chunk before less it
   __shared__ float s_qs[2][kRows];             // score factors, of this segment's queries and the next one's
   __shared__ int s_v;                          // V's reference at the end
@@ -264,16 +264,16 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const uint32_t k = kb >> (8 * e) & 255, v = vb >> (8 * e) & 255;
-          const int x = (int)v - vref + 127;
+          const int x = F8 ? (int)v - vref + 127 : (int)v;
           kf[e] = e < n ? scale_value(k) : 1.f;
           vf[e] = e >= n || v == 255 || x < 1 ? 0.f : __uint_as_float((uint32_t)x << 23);
           nan |= (uint32_t)(e < n && v == 255) << e;
-          rare = rare || (e < n && (v == 255 || (F8 && v > 0 && x < 127 - kVBelow)));
+          rare = rare || (e < n && (v == 255 || (F8 ? v > 0 && x < 127 - kVBelow : v != 127)));
         }
         rare = __any_sync(0xffffffffu, rare);
         float* to = reinterpret_cast<float*>(sm + C::FACTOR_OFF) + st * 2 * kKeys + 4 * lane;
         *reinterpret_cast<float4*>(to) = make_float4(kf[0], kf[1], kf[2], kf[3]);
-        if (F8) *reinterpret_cast<float4*>(to + kKeys) = make_float4(vf[0], vf[1], vf[2], vf[3]);
+        *reinterpret_cast<float4*>(to + kKeys) = make_float4(vf[0], vf[1], vf[2], vf[3]);
         uint32_t valid = ((1u << n) - 1) << (4 * (lane & 7));       // eight lanes a word
         nan <<= 4 * (lane & 7);
 #pragma unroll
@@ -447,6 +447,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const float2 z = unpair(fma2(t[e], qs2, off2));
                 float2 y = make_float2(ex2(z.x), ex2(z.y));
                 add = add2(add, pair(y.x, y.y));
+                if constexpr (masked && !F8) {   // (V as it is: its scales, 1 in other chunks)
+                  const float2 f = *reinterpret_cast<const float2*>(kf + kKeys + 16 * (2 * w + h) + 2 * e);
+                  y = make_float2(y.x * f.x, y.y * f.y);
+                }
                 if constexpr (masked) {        // a V that is not finite: NaN in the rows that see it
                   const uint32_t m = (seen & s_nan[st][w]) >> (16 * h + 2 * e);
                   if (m & 1) y.x = __uint_as_float(0x7fc00000u);

@@ -427,7 +427,7 @@ __global__ void __launch_bounds__(kThreads, Cfg<HD, NQ, F8>::CTAS)
             for (int i = 0; i < C::RB; i += 16)
               *reinterpret_cast<uint4*>(sm + C::P_OFF + r * C::RB + i) = make_uint4(0u, 0u, 0u, 0u);
           } else {
-            const int ve = F8 ? (int)vb - vref + kPShift + 127 : 127;
+            const int ve = F8 ? (int)vb - vref + kPShift + 127 : (int)vb;
             const float vf = vb == 255 ? __uint_as_float(0x7fc00000u)
                                        : !valid || ve < 1 ? 0.f : __uint_as_float((uint32_t)ve << 23);
             uint8_t* const p = sm + C::P_OFF;

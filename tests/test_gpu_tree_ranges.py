@@ -126,3 +126,21 @@ def test_a_small_value_with_most_of_the_weight(cdsl, T, H, kvh, hd, cache, dtype
     k[:, 0, :, 0] = hd ** 0.5
     cdsl.cdsl_kv_write(c.c, 1, k.to(BF).cuda(), v.to(BF).cuda(), ints(0, 0))
     check(c, 1, q, lens, mask, nodes, hd ** -0.5, attend(cdsl, c, 1, q, lens, mask, nodes, hd ** -0.5)[0])
+
+
+@pytest.mark.parametrize("T,H,kvh,hd", HEADS, ids=[str(i) for i in range(len(HEADS))])
+@TYPES
+@pytest.mark.parametrize("low,high", [(127, 127), (124, 131), (60, 190)])
+def test_scale_bytes_of_a_bf16_cache(cdsl, T, H, kvh, hd, dtype, low, high):
+    """A caller's own bf16 rows: values are code * 2^(byte - 127) for every kernel, as for cdsl_kv_read. (K's bytes stay
+    within 2^4, or one key takes all the weight.)"""
+    c, q, k, v, lens, mask, nodes = problem(cdsl, T, H, kvh, hd, BF, dtype, 1.0, 2)
+    cdsl.cdsl_kv_write(c.c, 1, k.to(BF).cuda(), v.to(BF).cuda(), ints(0, 0))
+    g = torch.Generator().manual_seed(3)
+    for kv, (a, b) in enumerate(((max(low, 123), min(high, 128)), (low, high))):
+        c.c.scale[1, :, kv] = torch.randint(a, b + 1, c.c.scale[1, :, kv].shape, generator=g, dtype=torch.uint8).cuda()
+    check(c, 1, q, lens, mask, nodes, hd ** -0.5, attend(cdsl, c, 1, q, lens, mask, nodes, hd ** -0.5)[0])
+    out = [torch.empty((1, 2, 200, kvh, hd), device="cuda") for _ in range(2)]
+    cdsl.cdsl_kv_read(c.c, 1, ints(30, 60), *out)
+    for b, first in enumerate((30, 60)):
+        assert all(torch.equal(x[0, b].double(), y) for x, y in zip(out, c.values(1, b, first, 200)))
