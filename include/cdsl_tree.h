@@ -39,8 +39,8 @@ enum { CDSL_TREE_MAX_NODES = 128, CDSL_TREE_MAX_BATCH = 1024, CDSL_TREE_MAX_VOCA
  *   d_pool   [n_layers][n_pages][2 (K, V)][n_kv_heads][page_size][head_dim], e4m3 or bfloat16, 16-byte
  *            aligned
  *   d_scale  [n_layers][n_pages][2][n_kv_heads][page_size] bytes, 16-byte aligned: row (token and head) values are
- *            code * 2^(byte - 127). Byte 255: the row held a value that is not finite; its codes are
- *            zeros and it stands for NaN.
+ *            code * 2^(byte - 127). Byte 255: the row held a value that is not finite (in the cache's type); its
+ *            codes are zeros and it stands for NaN. (A caller's own codes are finite.)
  *   d_page_table [batch][max_pages]: the page of slots [i * page_size, (i + 1) * page_size) of each
  *            sequence, any page ids in any order; entries beyond the cached slots are not read.
  * The pool needs no initial values. page_size: a power of two, 16..256. head_dim: 64 or 128. */

@@ -109,7 +109,7 @@ __global__ void __launch_bounds__(kThreads) k_kv_write(WriteArgs a) {
     if (part == 0) set_status(a.r.status, CDSL_ERANGE);
     return;
   }
-  const bool bad = top >= 0x7f800000u;
+  const bool bad = top >= (F8 ? 0x7f800000u : 0x7f7f8000u);   // (not finite, or bf16 rounds it to infinity)
   const size_t r = row_of(c, a.r.layer, page, kv, h, at);
   if constexpr (F8) {
     // smallest E with top <= 448 * 2^E = 1.75 * 2^(E + 8)

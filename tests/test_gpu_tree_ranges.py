@@ -144,3 +144,27 @@ def test_scale_bytes_of_a_bf16_cache(cdsl, T, H, kvh, hd, dtype, low, high):
     cdsl.cdsl_kv_read(c.c, 1, ints(30, 60), *out)
     for b, first in enumerate((30, 60)):
         assert all(torch.equal(x[0, b].double(), y) for x, y in zip(out, c.values(1, b, first, 200)))
+
+
+@CACHES
+@pytest.mark.parametrize("T", [8, 40], ids=["slots", "rows"])
+@TYPES
+def test_values_that_the_cache_rounds_to_infinity(cdsl, cache, T, dtype):
+    """fp32 values above bf16's largest by half a step and more: a bf16 row with one holds a value that is not finite, and what
+    a node does not see of it does not reach the node. The largest that rounds down stays, and e4m3 holds all of them."""
+    B, kvh, hd, lens = 1, 2, 64, [130]
+    c, q, k, v, _, mask, nodes = problem(cdsl, T, 2, kvh, hd, cache, dtype, 1.0, 4, lens)
+    big = torch.tensor([0x7F7F7FFF, 0x7F7F8000, 0x7F7FFFFF], dtype=torch.int32).view(F32)   # to bf16: its largest, inf, inf
+    n = lens[0]
+    v[0, n + 2, 0, 3], v[0, n + 3, 0, 4], v[0, n + 4, 0, 5] = big[0], -big[1], big[2]
+    cdsl.cdsl_kv_write(c.c, 1, k.cuda(), v.cuda(), ints(0))
+    rows = c.values(1, 0, n + 2, 3)[1]
+    bad = torch.isnan(rows).all(-1)
+    assert bad.tolist() == [[False, False]] + [[cache is BF, False]] * 2
+    assert torch.isfinite(rows[~bad]).all()
+    got = attend(cdsl, c, 1, q, lens, mask, nodes, hd ** -0.5)[0]
+    want = torch.ones(T, dtype=torch.bool, device="cuda")
+    want[[2, 3, 4]] = False
+    assert torch.isfinite(got[0, want]).all()
+    if cache is BF:
+        assert torch.isnan(got[0, 3:5, 0]).all() and torch.isfinite(got[0, 3:5, 1]).all()
