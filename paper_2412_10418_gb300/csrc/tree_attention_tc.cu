@@ -556,9 +556,8 @@ cudaError_t launch(const TreeArgs& a, cudaStream_t s) {
   CUtensorMap map;
   if (encode_cache_map<HD, F8>(a, &map)) return cudaErrorInvalidValue;
   auto k = k_tree_tc<HD, NQ, F8>;
-  static const cudaError_t set =
-      cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::smem(CDSL_TREE_MAX_BATCH));
-  if (set != cudaSuccess) return set;
+  static OncePerDevice once;
+  if (const cudaError_t e = allow_shared(once, k, C::smem(CDSL_TREE_MAX_BATCH))) return e;
   return launch_pdl(k, dim3(a.blocks), dim3(kThreads), C::smem(a.c.batch), s, a, map);
 }
 

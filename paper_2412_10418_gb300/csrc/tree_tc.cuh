@@ -4,6 +4,7 @@
 #include <algorithm>
 
 #include "kernels.h"
+#include "once.h"
 #include "tree_attention.cuh"
 
 namespace cdsl {
@@ -271,6 +272,14 @@ __device__ __forceinline__ void store32(void* p, const uint32_t (&v)[8]) {
   asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]),
                "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
                : "memory");
+}
+
+// Dynamic shared memory beyond 48 KB for `kernel` on the current device; once: the kernel's.
+template <typename K>
+cudaError_t allow_shared(OncePerDevice& once, K kernel, size_t bytes) {
+  int device = 0;
+  if (const cudaError_t e = cudaGetDevice(&device)) return e;
+  return once(device, [&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes); });
 }
 
 // The tensor map of a layer's rows for load_chunks.
