@@ -282,8 +282,9 @@ def cdsl_destroy(ctx):
 
 # ------------------------------------------------------------------------------ tree speculation
 # The C ABI sees pointers, sizes and strides; types, shapes, layouts and devices are checked here, and
-# anything the calls cannot take raises CdslError(CDSL_EINVAL) before a call. `stream` is a cudaStream_t
-# as an integer, None the current torch stream. Semantics: include/cdsl_tree.h.
+# anything the calls cannot take raises CdslError(CDSL_EINVAL) before a call, tensors of a device that is not the
+# current one among it. `stream` is a cudaStream_t as an integer, None the current torch stream. Semantics:
+# include/cdsl_tree.h.
 
 class _KvCacheC(ctypes.Structure):
     _fields_ = [("d_pool", _P), ("d_scale", _P), ("d_page_table", _P), ("n_layers", _I), ("n_pages", _I),
@@ -300,6 +301,7 @@ class _Types:
         self.torch = torch
         self.i32, self.f32, self.bf16, self.u8 = torch.int32, torch.float32, torch.bfloat16, torch.uint8
         self.values = {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16}
+        self.devices = None                    # how many (asked at the first launch)
         self.caches = {torch.float8_e4m3fn: DTYPE_F8E4M3, torch.bfloat16: DTYPE_BF16}
 
 
@@ -325,8 +327,15 @@ def _ints(fn: str, name: str, t, shape, device, dtype=None):
              f"{t.dtype} {tuple(t.shape)} on {t.device}")
 
 
-def _stream(device):
-    return _types.torch.cuda.current_stream(device).cuda_stream
+def _stream(fn: str, device, stream):
+    """The stream of a launch (None: the current one). Launches go to the current device, which must be the tensors'.
+    (Asking which it is takes 1 to 2 us a call; with one device there is no other.)"""
+    cuda = _types.torch.cuda
+    if _types.devices is None:
+        _types.devices = cuda.device_count()
+    if _types.devices > 1 and cuda.current_device() != device.index:
+        _bad(fn, f"the tensors are on {device}, the current device is cuda:{cuda.current_device()}")
+    return cuda.current_stream(device).cuda_stream if stream is None else stream
 
 
 class KvCache:
@@ -405,7 +414,7 @@ def cdsl_kv_write(cache: KvCache, layer: int, k, v, start, count=None, status=No
                                _ints(fn, "start", start, cache._one, cache.device),
                                None if count is None else _ints(fn, "count", count, cache._one, cache.device),
                                None if status is None else _ints(fn, "status", status, (1,), cache.device),
-                               _stream(cache.device) if stream is None else stream))
+                               _stream(fn, cache.device, stream)))
 
 
 def cdsl_kv_read(cache: KvCache, layer: int, start, k, v, count=None, status=None, stream=None):
@@ -423,7 +432,7 @@ def cdsl_kv_read(cache: KvCache, layer: int, start, k, v, count=None, status=Non
                               _ints(fn, "start", start, cache._one, cache.device),
                               None if count is None else _ints(fn, "count", count, cache._one, cache.device),
                               None if status is None else _ints(fn, "status", status, (1,), cache.device),
-                              _stream(cache.device) if stream is None else stream))
+                              _stream(fn, cache.device, stream)))
 
 
 def cdsl_kv_commit(cache: KvCache, lens, path, n_path, new_lens=None, status=None, stream=None):
@@ -438,7 +447,7 @@ def cdsl_kv_commit(cache: KvCache, lens, path, n_path, new_lens=None, status=Non
                                 _ints(fn, "n_path", n_path, cache._one, cache.device), T,
                                 None if new_lens is None else _ints(fn, "new_lens", new_lens, cache._one, cache.device),
                                 None if status is None else _ints(fn, "status", status, (1,), cache.device),
-                                _stream(cache.device) if stream is None else stream))
+                                _stream(fn, cache.device, stream)))
 
 
 def cdsl_tree_mask(parents: Sequence[int]):
@@ -476,7 +485,7 @@ def cdsl_tree_attention(cache: KvCache, layer: int, q, lens, mask, out, workspac
         None if nodes is None else _ints(fn, "nodes", nodes, cache._one, dev),
         _ints(fn, "mask", mask, (cache.batch, T, (T + 31) // 32), dev), scale, max_len, out.data_ptr(),
         None if lse is None else _ints(fn, "lse", lse, (cache.batch, T, H), dev, _types.f32), workspace.data_ptr(), workspace.numel(),
-        None if status is None else _ints(fn, "status", status, (1,), dev), _stream(dev) if stream is None else stream))
+        None if status is None else _ints(fn, "status", status, (1,), dev), _stream(fn, dev, stream)))
 
 
 def cdsl_tree_verify(logits, tokens, parents, u, u_last, path, n_path, emitted, *, draft_logits=None,
@@ -505,7 +514,7 @@ def cdsl_tree_verify(logits, tokens, parents, u, u_last, path, n_path, emitted, 
         None if nodes is None else _ints(fn, "nodes", nodes, one, dev), _ints(fn, "u", u, all_, dev, ty.f32),
         _ints(fn, "u_last", u_last, one, dev, ty.f32), temperature, _ints(fn, "path", path, all_, dev),
         _ints(fn, "n_path", n_path, one, dev), _ints(fn, "emitted", emitted, all_, dev),
-        None if status is None else _ints(fn, "status", status, (1,), dev), _stream(dev) if stream is None else stream))
+        None if status is None else _ints(fn, "status", status, (1,), dev), _stream(fn, dev, stream)))
 
 
 # ------------------------------------------------------------------------------ Engine
