@@ -101,7 +101,8 @@ CDSL_API int32_t cdsl_tree_attention_workspace(const cdsl_kv_cache* cache, int32
  * ([batch, T, (T + 31) / 32] words, as cdsl_tree_mask writes them; any bits are allowed) is set. A node
  * that sees nothing, and nodes t >= d_nodes[b], give zeros (lse -inf). T = 1 is plain decoding.
  *   d_q, d_out [batch, T, n_heads, head_dim] of `dtype` (CDSL_DTYPE_F32 or CDSL_DTYPE_BF16);
- *   h_strides[6]: elements between sequences, tokens and heads of q, then of out. d_lse
+ *   h_strides[6]: elements between sequences, tokens and heads of q, then of out (whose places must not coincide: a 0
+ *   between two of them is refused). d_lse
  *   [batch, T, n_heads] float32 or NULL: log of the sum of exp(scale * q . k_j).
  *   max_len: an upper bound of d_lens (0 .. max_pages * page_size - T); a length outside 0 .. max_len
  *   latches CDSL_ERANGE and counts as the nearer bound. It sets the launch size alone, so a captured

@@ -525,6 +525,9 @@ extern "C" int32_t cdsl_tree_attention(const cdsl_kv_cache* cache, int32_t layer
     return ck.fail("max_len must be 0 .. max_pages * page_size - T");
   const int eb = dtype == CDSL_DTYPE_BF16 ? 2 : 4;
   if (!ck.aligned(d_q, eb) || !ck.aligned(d_out, eb)) return ck.fail("q and out must be aligned to their type");
+  const int64_t* const so = h_strides + 3;
+  if ((c.batch > 1 && so[0] == 0) || (T > 1 && so[1] == 0) || (n_heads > 1 && so[2] == 0))
+    return ck.fail("out must not have a stride of 0 between sequences, tokens or heads");
   const bool tc = dtype == CDSL_DTYPE_BF16;
   Sizes z;
   sizes_of(c, tc, n_heads, T, &z);
