@@ -11,8 +11,7 @@
 // largest of the first chunk, raised when one passes it by more than 2^kVRoom), and P into
 // fp16 by one conversion a pair: 2^-12 of itself, over 22 octaves below a row's reference. That is exact for V's scales
 // down to 2^-kVBelow of the reference; a chunk with a smaller one has V in bf16, exact over fp32's range, and P in two
-// bf16 planes (2^-17), as has a bf16 cache with its V as it is. Chunks with masks do the same: one code
-// for all that is rare.
+// bf16 planes (2^-17), as has a bf16 cache with its V as it is.
 //
 // A softmax thread has a vector (a TMEM lane) and walks all the chunk's slots (columns): maximum, reference,
 // probabilities and their sum are its own, no value crosses lanes and no barrier stands in a chunk, whatever
@@ -103,7 +102,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   __shared__ __align__(8) uint64_t s_full[kBuf], p_full[kBuf], r_full[kBuf], pv_done[2], q_full, done;
   __shared__ uint32_t s_tmem;
   __shared__ __align__(16) uint32_t s_valid[NST][4], s_nan[NST][4];   // slots that there are, whose V is not finite
-  __shared__ int s_rare[NST], s_h_rare[2];     // a chunk with masks, V's scales far apart (bf16: not 1): by stages; V's buffers
+  __shared__ int s_kind[NST], s_h_far[2];      // a chunk's: bit 0 has masks, 1 V's scales far apart (bf16: not 1); V's buffers'
   __shared__ int s_vref[NST], s_vstep[NST];    // V's reference in the chunk, and that of the chunk before less it
   __shared__ float s_qs[2][kRows];             // score factors, of this segment's queries and the next one's
   __shared__ int s_v;                          // V's reference at the end
@@ -189,10 +188,11 @@ __global__ void __launch_bounds__(kThreads, 1)
         return true;
       };
       auto pv = [&](int i, bool add) {         // P V of chunk i
-        if (!wait_for(&p_full[i % kBuf], parity(i, kBuf), a.status) ||
-            !(F8 ? wait_for(&h_full[i & 1], parity(i, 2), a.status)
+        if (!(F8 ? wait_for(&h_full[i & 1], parity(i, 2), a.status)
                  : wait_for(&v_full[i % NST], parity(i, NST), a.status)))
           return false;
+        const bool planes = !F8 || s_h_far[i & 1];
+        if (!wait_for(&p_full[i % kBuf], parity(i, kBuf), a.status)) return false;
         tc::tc_fence_after();
         const uint64_t v = desc_v + (F8 ? (uint32_t)(i & 1) * (C::H_TILE / 16) : (uint32_t)(i % NST) * (2 * C::TILE / 16));
         // 16 slots an MMA: 8 columns of P, 16 rows of 128 bytes of V. P of 32 slots lies in the columns that held
@@ -203,7 +203,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             tc::umma_tmem_a(t_o, tmem + i % kBuf * kKeys + k / 2 * 32 + p * 16 + k % 2 * 8, v + k * (16 * 128 / 16), idesc,
                             add || k > 0);
         };
-        if (F8 && !s_h_rare[i & 1]) {
+        if (!planes) {
           plane(0, idesc_half, add);
         } else {
 #pragma unroll 1
@@ -260,7 +260,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (vref == 0 || vmax > vref + kVRoom) vref = vmax;
         float kf[4], vf[4];
         uint32_t nan = 0;
-        bool rare = n < 4 || slot + 3 >= s.len;   // slots past the item's, without a page or of the tree
+        bool far = false, masks = n < 4 || slot + 3 >= s.len;   // slots past the item's, without a page or of the tree
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const uint32_t k = kb >> (8 * e) & 255, v = vb >> (8 * e) & 255;
@@ -268,9 +268,11 @@ __global__ void __launch_bounds__(kThreads, 1)
           kf[e] = e < n ? scale_value(k) : 1.f;
           vf[e] = e >= n || v == 255 || x < 1 ? 0.f : __uint_as_float((uint32_t)x << 23);
           nan |= (uint32_t)(e < n && v == 255) << e;
-          rare = rare || (e < n && (v == 255 || (F8 ? v > 0 && x < 127 - kVBelow : v != 127)));
+          masks = masks || (e < n && v == 255);
+          far = far || (e < n && v != 255 && (F8 ? v > 0 && x < 127 - kVBelow : v != 127));
         }
-        rare = __any_sync(0xffffffffu, rare);
+        far = __any_sync(0xffffffffu, far);
+        masks = __any_sync(0xffffffffu, masks);
         float* to = reinterpret_cast<float*>(sm + C::FACTOR_OFF) + st * 2 * kKeys + 4 * lane;
         *reinterpret_cast<float4*>(to) = make_float4(kf[0], kf[1], kf[2], kf[3]);
         *reinterpret_cast<float4*>(to + kKeys) = make_float4(vf[0], vf[1], vf[2], vf[3]);
@@ -288,7 +290,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (lane == 0) {
           s_vref[st] = F8 ? vref : 127;
           s_vstep[st] = F8 && before ? before - vref : 0;
-          s_rare[st] = rare;
+          s_kind[st] = masks | far << 1;
         }
         __syncwarp();
         if (lane == 0) tc::mbar_arrive(F8 ? &v_empty[st] : &k_empty[st]);   // (the scale bytes are read)
@@ -361,9 +363,9 @@ __global__ void __launch_bounds__(kThreads, 1)
           return r < s.nq ? x & s_valid[st][w] : 0u;
         };
         // Code of its own for chunks with slots of the tree, past the item's, without a page or with a V that is not finite,
-        // where each row has its mask (and those with V's scales far apart): as one, the compiler selects on every score,
-        // masked or not, which took twice the time.
-        auto softmax = [&](auto masked) {
+        // where each row has its mask: as one, the compiler selects on every score, masked or not, which took twice
+        // the time; and for those with V's scales far apart.
+        auto softmax = [&](auto masked, auto far) {
           // slots 16 g .. as scores times K's scale, in pairs
           auto scores = [&](const uint32_t (&x)[16], int g, uint32_t seen, uint64_t (&t)[8]) {
 #pragma unroll
@@ -447,7 +449,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const float2 z = unpair(fma2(t[e], qs2, off2));
                 float2 y = make_float2(ex2(z.x), ex2(z.y));
                 add = add2(add, pair(y.x, y.y));
-                if constexpr (masked && !F8) {   // (V as it is: its scales, 1 in other chunks)
+                if constexpr (far && !F8) {      // (V as it is: its scales, 1 in other chunks)
                   const float2 f = *reinterpret_cast<const float2*>(kf + kKeys + 16 * (2 * w + h) + 2 * e);
                   y = make_float2(y.x * f.x, y.y * f.y);
                 }
@@ -456,7 +458,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                   if (m & 1) y.x = __uint_as_float(0x7fc00000u);
                   if (m & 2) y.y = __uint_as_float(0x7fc00000u);
                 }
-                if constexpr (F8 && !masked) {
+                if constexpr (F8 && !far) {
                   const __half2 p = __floats2half2_rn(y.x, y.y);
                   hi[e] = *reinterpret_cast<const uint32_t*>(&p);
                 } else {
@@ -468,7 +470,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               }
               const uint32_t to = t_s + 32 * w + h * 8;
               tc::tmem_st_nowait(to, hi);
-              if (!F8 || masked) tc::tmem_st_nowait(to + 16, lo);
+              if (!F8 || far) tc::tmem_st_nowait(to + 16, lo);
             }
           }
           const float2 two = unpair(add);
@@ -476,8 +478,10 @@ __global__ void __launch_bounds__(kThreads, 1)
           tc::tmem_wait_st();
         };
         if (live) {
-          if (s_rare[st]) softmax(std::true_type());
-          else softmax(std::false_type());
+          const int kind = s_kind[st];
+          if (kind == 0) softmax(std::false_type(), std::false_type());
+          else if (kind == 1) softmax(std::true_type(), std::false_type());
+          else softmax(std::true_type(), std::true_type());
           failed = !__all_sync(0xffffffffu, ok);
         } else {
           tc::mbar_arrive(&r_full[it % kBuf]);
@@ -570,7 +574,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   } else if (F8) {
     // ------------------------------------------------------------------------- V to 16 bits
     // 16 codes at a time, exactly, with the rows' scales; rows that there are not become zeros. fp16, which two
-    // instructions a pair give; in a rare chunk bf16, in which no scale is too small.
+    // instructions a pair give; where V's scales are far apart bf16, in which no scale is too small.
     constexpr int kRowsAt = kConv / (HD / 16);
     const int row0 = (threadIdx.x - kSoft) / (HD / 16), part = (threadIdx.x - kSoft) % (HD / 16);
     // (the other half first in the second block of 64 dimensions: eight lanes' stores then meet no bank twice)
@@ -585,8 +589,8 @@ __global__ void __launch_bounds__(kThreads, 1)
            wait_for(&pv_done[i & 1], parity(i, 2) ^ 1, a.status);   // (chunk i - 2's: the buffer is free)
       ok = __all_sync(0xffffffffu, ok);
       const float* vf = reinterpret_cast<const float*>(sm + C::FACTOR_OFF) + (st * 2 + 1) * kKeys;
-      const bool rare = s_rare[st];
-      if (threadIdx.x == kSoft) s_h_rare[i & 1] = rare;
+      const bool far = s_kind[st] >> 1;
+      if (threadIdx.x == kSoft) s_h_far[i & 1] = far;
       const uint8_t* from = sm + C::KV_OFF + (st * 2 + 1) * C::TILE + tc::row_offset(row0, part, C::BW);
       uint8_t* to = sm + C::H_OFF + (i & 1) * C::H_TILE;
       const auto store = [&](int k, const uint32_t (&h)[8]) {   // (rows that many apart lie alike in their tiles)
@@ -594,7 +598,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         *reinterpret_cast<uint4*>(to + k * (kRowsAt * 128) + to0) = flip ? hi : lo;
         *reinterpret_cast<uint4*>(to + k * (kRowsAt * 128) + to1) = flip ? lo : hi;
       };
-      if (!rare) {
+      if (!far) {
 #pragma unroll 2
         for (int k = 0; k < kKeys / kRowsAt; ++k) {
           const uint4 u = *reinterpret_cast<const uint4*>(from + k * kRowsAt * C::BW);
@@ -605,7 +609,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             __half2 p, q;
-            f8x4_half(w[e], &p, &q);
+            f8x4_half(f == 0.f ? 0u : w[e], &p, &q);   // (a row that there is not holds anything)
             p = __hmul2(p, f2);
             q = __hmul2(q, f2);
             h[2 * e] = *reinterpret_cast<const uint32_t*>(&p);
@@ -623,7 +627,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             __half2 p, q;
-            f8x4_half(f == 0.f ? 0u : w[e], &p, &q);   // (a row that there is not holds anything)
+            f8x4_half(f == 0.f ? 0u : w[e], &p, &q);
             const float2 x = __half22float2(p), y = __half22float2(q);
             const __nv_bfloat162 a2 = __floats2bfloat162_rn(x.x * f, x.y * f), b2 = __floats2bfloat162_rn(y.x * f, y.y * f);
             h[2 * e] = *reinterpret_cast<const uint32_t*>(&a2);
