@@ -350,10 +350,10 @@ __global__ void __launch_bounds__(kWalk) k_tree_walk(VerifyArgs a) {
     const int parent = a.parents[(size_t)b * a.T + i];
     if (i > 0 && i < n && parent >= 0 && parent < i) atomicOr(&s_child[parent][i >> 5], 1u << (i & 31));
     s_tok[i] = a.tokens[(size_t)b * a.T + i];
-    s_u[i] = a.u[(size_t)b * a.T + i];
+    if (a.inv_t != 0.f) s_u[i] = a.u[(size_t)b * a.T + i];
     if (rank == 0) a.path[(size_t)b * a.T + i] = a.emitted[(size_t)b * a.T + i] = -1;
   }
-  const float u_last = a.u_last[b];
+  const float u_last = a.inv_t != 0.f ? a.u_last[b] : 0.f;
   const bool greedy = a.inv_t == 0.f, given = a.draft != nullptr;
   const int size = ((V + C - 1) / C + E - 1) / E * E, base = rank * size, top = min(V, base + size);   // this block's tokens
   int turn = 0;
