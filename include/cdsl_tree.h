@@ -20,8 +20,10 @@
  * before anything is launched, with the message in cdsl_last_error(NULL). What only the device can
  * see (an index in device memory that is out of range, a logits row without a finite value) is
  * latched as a cdsl_status in *d_status, first error wins, if d_status is not NULL; the caller sets
- * it to 0. Calls can be captured into CUDA graphs, and calls on different streams may overlap unless
- * they share a workspace or one writes what another reads.
+ * it to 0. CDSL_ETIMEOUT there means that a wait inside a kernel of cdsl_tree_attention has run out,
+ * after a second or more, and that its output is not complete. Calls can be captured into CUDA graphs,
+ * and calls on different streams may overlap unless they share a workspace or one writes what another
+ * reads.
  */
 #ifndef CDSL_TREE_H
 #define CDSL_TREE_H
@@ -67,8 +69,9 @@ CDSL_API int32_t cdsl_kv_write(const cdsl_kv_cache* cache, int32_t layer, const 
 
 /* Read slots d_start[b] + i, i < d_count[b] (NULL: all T), of layers layer .. layer + n_layers - 1
  * back as values: d_k, d_v [n_layers, batch, T, n_kv_heads, head_dim] contiguous, 16-byte aligned,
- * of `dtype` (exact in either type for an e4m3 cache). Rows i >= d_count[b], and rows whose slot or
- * page is out of range (which latches CDSL_ERANGE), are zeros. */
+ * of `dtype` (exact in either type for an e4m3 cache, but for values above the type's largest or below
+ * its smallest). Rows i >= d_count[b], and rows whose slot or page is out of range (which latches
+ * CDSL_ERANGE), are zeros. */
 CDSL_API int32_t cdsl_kv_read(const cdsl_kv_cache* cache, int32_t layer, int32_t n_layers, void* d_k,
                               void* d_v, int32_t dtype, int32_t T, const int32_t* d_start,
                               const int32_t* d_count, int32_t* d_status, void* stream);
@@ -108,8 +111,12 @@ CDSL_API int32_t cdsl_tree_attention_workspace(const cdsl_kv_cache* cache, int32
  *   latches CDSL_ERANGE and counts as the nearer bound. It sets the launch size alone, so a captured
  *   call may be replayed while the lengths stay below it. Pages out of range latch CDSL_ERANGE and
  *   their slots count as not visible.
- * bfloat16 queries run on the tensor cores with fp32 sums and softmax; float32 ones on the CUDA
- * cores in fp32. d_workspace: cdsl_tree_attention_workspace bytes, 256-byte aligned, in any state; it
+ * bfloat16 queries run on the tensor cores with fp32 sums and softmax. Over an e4m3 cache queries are
+ * held to 2^-18 of a row's largest value and probabilities to 2^-8 of themselves (2^-10 on average) for
+ * up to 32 query vectors per K/V head, to 2^-12 for more; small V rows count beside large ones by their
+ * scales, which for that are to be the smallest ones, as cdsl_kv_write makes them. Over a bfloat16 cache
+ * probabilities are held to 2^-17. float32 queries run on the CUDA cores in fp32.
+ * d_workspace: cdsl_tree_attention_workspace bytes, 256-byte aligned, in any state; it
  * holds nothing between calls. */
 CDSL_API int32_t cdsl_tree_attention(const cdsl_kv_cache* cache, int32_t layer, const void* d_q,
                                      int32_t dtype, int32_t n_heads, int32_t T,

@@ -27,19 +27,23 @@
 // eight more warps, and a chain of waits through them that held a chunk to 3,500 cycles.) Four warps convert V, one
 // loads, one issues MMAs, one turns scale bytes into factors. A bf16 cache has shared memory for two stages only:
 // there K and the scale bytes are loaded a chunk ahead of V, or S would wait for the V of a chunk before (36 vectors,
-// 8 sequences of 16,384 tokens, 8 heads: 191 -> 123 us; with three stages of e4m3 it loses 5 %).
+// 8 sequences of 16,384 tokens, 8 heads: 191 -> 123 us, 125 now; with three stages of e4m3 it loses 5 %).
 //
 // Between two items the next one's queries and masks are staged as soon as the last S has read this one's, beside
-// the last P V (33 trees of 48 after 115 tokens: 57 -> 53 us).
+// the last P V (33 trees of 48 after 115 tokens: 7 % less).
 //
-// Measured: 8 trees of 25 nodes, 100 vectors a K/V head, up to 32,768 tokens of 8 heads of 128 in e4m3: 148 to 157 us,
-// 380 to 400 TFLOP/s, 39 % of the copy bandwidth. A chunk takes 3,000 cycles, of which its MMAs need 1,024; a softmax
+// Measured: 8 trees of 25 nodes, 100 vectors a K/V head, up to 32,768 tokens of 8 heads of 128 in e4m3: 146 to 155 us,
+// 385 to 415 TFLOP/s, 40 % of the copy bandwidth (16,384 tokens each 111 us; with V's scales far apart in every chunk 174). A chunk takes 3,000 cycles, of which its MMAs need 1,024; a softmax
 // thread spends 1,500 on the maxima, 2,000 on the probabilities and the rest waiting. What holds it is latency (166
 // cycles a TMEM load), shared memory, which operands, conversion and factors keep busy for 1,900, and instruction
 // fetches: the roles together are about as large as the instruction cache, and the same kernel took 150 to 190 us
 // with the sizes of its loops (0.4 to 1.6 million misses a call), which are kept rolled for that. A third group of
-// softmax warps: 177 us. At 36 vectors 8 sequences of 16,384 take 99 us, two blocks of 32 on
-// tree_attention_tc.cu 114. At 32, 67 there and 98 here.
+// softmax warps: 177 us. At 36 vectors 8 sequences of 16,384 take 99.5 us, two blocks of 32 on
+// tree_attention_tc.cu 117. At 32, 70 there and 92 here. A block has 128 rows whatever it holds: 8 trees of 32 nodes of four
+// heads each after 4096 tokens take 50.5 us, of 33 nodes, whose 132 vectors take two blocks, 75.
+//
+// Waits are bounded by a number of tries (wait_for): on expiry CDSL_ETIMEOUT is latched, the role winds down and the block
+// frees its TMEM and exits.
 #include <cuda.h>
 
 #include <algorithm>

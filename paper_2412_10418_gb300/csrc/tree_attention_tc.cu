@@ -17,7 +17,7 @@
 // probability is held to 2^-8 of itself (2^-10 on average), or to a step of 2^-21 of the chunk's largest scale, if
 // that is more. Where the chunk's V scales lie more than 2^kSpread apart, that could be all that a slot with a small scale
 // has, next to one that has no weight, or is not seen: there the softmax threads multiply P and V themselves,
-// in fp32.
+// in fp32 (the call below with every chunk so: 710 us).
 //
 // Every chunk's P is relative to that chunk's own column maxima and largest V scale, and its O^T starts
 // anew in TMEM and is added to fp32 sums in registers with the factor that this takes, so that small
@@ -31,12 +31,12 @@
 // dimension of O^T. Column maxima come from redux.sync over a warp and shared memory over the warps, the one
 // barrier of a chunk; each warp then works out the columns' factors for itself. Each thread keeps its own
 // slots' share of the sums l. Bound by HBM where a call fills the device: 64 sequences of up to 8,192 tokens, 8 heads of
-// 128 in e4m3, four query heads each, one token: 130 us, 92 % of the copy bandwidth; by latency in small ones: one of
-// 512 tokens in 9 us with the joining. The MMA's N is 16 or 32 by the number of vectors: 8 sequences of 16,384, 16
-// vectors: 54.6 us with 16, 64 with 32 (fewer blocks on an SM); 32 vectors: 67 us in one block, 98 as rows.
+// 128 in e4m3, four query heads each, one token: 130 to 137 us by inputs, 87 to 92 % of the copy bandwidth; by latency in
+// small ones: one of 512 tokens in 9 us with the joining. The MMA's N is 16 or 32 by the number of vectors: 8 sequences of
+// 16,384, 16 vectors: 54 us with 16, 67 with 32 (fewer blocks on an SM); 32 vectors: 70 us in one block, 92 as rows.
 //
-// Waits are bounded (tc::kWaitLimitNs): on expiry CDSL_ETIMEOUT is latched, the role winds down and
-// the block frees its TMEM and exits.
+// Waits are bounded (by tc::kWaitLimitNs, the loading warp's by a number of tries): on expiry CDSL_ETIMEOUT is latched, the
+// role winds down and the block frees its TMEM and exits.
 #include <cuda.h>
 
 #include <algorithm>

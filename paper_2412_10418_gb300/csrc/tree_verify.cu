@@ -10,9 +10,11 @@
 // then made alike by every thread. Bound by latency and, with drafts, by the exponentials: a level of 32,000 bf16
 // tokens with drafts in four blocks is 12,000 cycles (loads 3,400, exponentials 2,900, two reductions of 1,500 each,
 // the decisions 1,600 and more with rejections). 32 sequences of 49 sampled nodes, the longest path 8: 47 us; one of
-// 17 chosen nodes, fp32: 10 us. (A value a load, and keys of 64 bits in the maximum: 18,500 cycles a level, 82 us.) Rows
+// 17 chosen nodes, fp32: 10 us. (A value a load, and keys of 64 bits in the maximum: 18,500 cycles a level, 82 us.) A
+// block of more than 8,192 tokens has up to 40 values a thread, which do not fit its 128 registers (350 bytes of stack): 64
+// sequences of 16 nodes and 32,000 tokens with drafts, two blocks each, 109 us, 32 sequences 33; 8 of 17 and 128,256 tokens 81. Rows
 // of more than the cluster's registers hold (163,840 tokens) take k_tree_verify, a block per sequence that
-// reads a row several times.
+// reads a row several times: one sequence of 262,144 tokens, a root without a taken child, 301 us, of 163,840 tokens 14.
 #include <cuda.h>
 
 #include <algorithm>
