@@ -168,3 +168,92 @@ def test_values_that_the_cache_rounds_to_infinity(cdsl, cache, T, dtype):
     assert torch.isfinite(got[0, want]).all()
     if cache is BF:
         assert torch.isnan(got[0, 3:5, 0]).all() and torch.isfinite(got[0, 3:5, 1]).all()
+
+
+MIXED = [  # B, T, H, kvh, hd, page: 1, 8, 24, 32, 40 and 128 vectors a K/V head, and 2 blocks of rows
+    (6, 1, 4, 4, 128, 16), (5, 2, 8, 2, 64, 64), (6, 6, 8, 2, 128, 256), (5, 32, 3, 3, 64, 16), (5, 10, 8, 2, 128, 32),
+    (4, 128, 1, 1, 64, 128), (4, 33, 8, 2, 128, 64)]
+
+
+@pytest.mark.parametrize("shape", MIXED, ids=[str(i) for i in range(len(MIXED))])
+@CACHES
+@TYPES
+@pytest.mark.parametrize("tail", [1.0, 4.0, 12.0])
+def test_heavy_tails_with_all_that_is_rare(cdsl, shape, cache, dtype, tail):
+    """Values whose sizes are spread by e^tail from row to row, so that chunks with scales far apart and others take turns
+    in an item, together with ragged trees, rows that see nothing, a node whose V and one whose K is not finite, and a page
+    that is out of range. Bits are the same in a second call."""
+    import random
+    B, T, H, kvh, hd, page = shape
+    rng, g = random.Random(T), torch.Generator().manual_seed(T)
+    lens = [rng.choice([0, 1, 127, 128, 129, 300, 700, 1000]) for _ in range(B - 1)] + [1000]
+    nodes = [rng.randint((T + 1) // 2, T) for _ in range(B)]
+    n = max(lens) + T
+    c = ref.Cache(B, n, kvh, hd, page, cache, layers=2, seed=T)
+    k, v = (torch.randn((B, n, kvh, hd), generator=g) for _ in range(2))
+    v = v * torch.where(torch.rand((B, n, kvh, 1), generator=g) < 0.02, (torch.randn((B, n, kvh, 1), generator=g) * tail).exp(), 1.0)
+    v[B - 1, :256] *= 2.0 ** -20               # (whole chunks of small values, then of large ones)
+    bad_v, bad_k = lens[0] + nodes[0] - 1, lens[1] + nodes[1] - 1
+    v[0, bad_v, 0, 3], k[1, bad_k, 0, 5] = float("inf"), float("nan")
+    cdsl.cdsl_kv_write(c.c, 1, k.to(BF).cuda(), v.to(BF).cuda(), ints(*[0] * B), ints(*[a + b for a, b in zip(lens, nodes)]))
+    mask = torch.stack([cdsl.cdsl_tree_mask(ref.tree("random", T, rng))[0] for _ in range(B)])
+    if T > 2:
+        mask[2, 1] = 0
+    q = torch.randn((B, T, H, hd), generator=g).to(dtype).cuda()
+    scale = hd ** -0.5
+    got = attend(cdsl, c, 1, q, lens, mask, nodes, scale)[0]
+    assert torch.equal(torch.nan_to_num(got, 7.0), torch.nan_to_num(attend(cdsl, c, 1, q, lens, mask, nodes, scale)[0], 7.0))
+    G = H // kvh
+    for b in range(B):
+        sees = [ref.bits_of(mask, b, t, nodes[b]) for t in range(nodes[b])]
+        blind = torch.tensor([lens[b] + sum(s) == 0 for s in sees], device="cuda")
+        at = {0: bad_v, 1: bad_k}.get(b, -1) - lens[b]
+        nan = torch.tensor([at >= 0 and s[at] == 1 for s in sees], device="cuda")
+        assert (got[b, nodes[b]:] == 0).all() and (got[b, :nodes[b]][blind] == 0).all()
+        assert torch.isnan(got[b, :nodes[b]][nan][:, :G]).all()
+        rest = ~blind & ~nan
+        if b < 2 and G < H:                    # (other heads' rows are finite)
+            assert torch.isfinite(got[b, :nodes[b]][:, G:]).all()
+        if rest.any():
+            t = torch.nonzero(rest)[:, 0].cpu()
+            part = c.values(1, b, 0, lens[b] + nodes[b])
+            check_rows(c, b, part, q[b, t], [sees[i] for i in t.tolist()], lens[b], scale, got[b, t])
+    lost = c.table.clone()
+    lost[B - 1, 0] = 1 << 22
+    out, ws = torch.empty_like(q), torch.empty(cdsl.cdsl_tree_attention_workspace(c.c, T, H), dtype=torch.uint8, device="cuda")
+    st = torch.zeros(1, dtype=torch.int32, device="cuda")
+    cdsl.cdsl_tree_attention(c.c.at(lost), 1, q, ints(*lens), mask.cuda(), out, ws, scale=scale, max_len=max(lens),
+                             nodes=ints(*nodes), status=st)
+    assert int(st) == cdsl.CDSL_ERANGE
+    b, t = B - 1, nodes[B - 1]
+    part = [x[page:] for x in c.values(1, b, 0, lens[b] + t)]
+    check_rows(c, b, part, q[b, :t], [ref.bits_of(mask, b, i, t) for i in range(t)], lens[b] - page, scale, out[b, :t])
+
+
+def check_rows(c, b, kv, q, sees, n, scale, got):
+    """Rows of one sequence that see its first n slots and some of the rest; as in check()."""
+    G = q.shape[1] // kv[0].shape[1]
+    finite = torch.isfinite(kv[0]).all(-1) & torch.isfinite(kv[1]).all(-1)
+    k, v = (torch.where(finite[..., None], x, 0.0).repeat_interleave(G, 1) for x in kv)
+    see = torch.tensor([[1] * n + s for s in sees], dtype=torch.bool, device="cuda")
+    qd = q.double()
+    x = torch.einsum("thd,nhd->thn", qd, k) * scale
+    p = torch.softmax(x.masked_fill(~see[:, None], float("-inf")), -1)
+    out, size = (torch.einsum("thn,nhd->thd", p, y) for y in (v, v.abs()))
+    s_abs = (torch.einsum("thd,nhd->thn", qd.abs(), k.abs()) * scale).amax(-1, keepdim=True)
+    keys = k.shape[0]
+    dw = 2 * (q.shape[2] + 4) * 2.0 ** -24 * s_abs + (keys + 16) * 2.0 ** -24
+    e = dw * size
+    if q.dtype is BF:
+        e = (dw + 2 * 2.0 ** -13 * s_abs + 2.0 ** -8) * size + 2.0 ** -8 * out.abs()
+        if c.c.pool.dtype is F8:               # per chunk of 128 slots: scales within 2^8 of its smallest
+            vmax = v.abs().amax(-1)            # [keys, heads]; a scale is at most vmax / 224
+            for first in range(0, keys, 128):
+                part = vmax[first:first + 128]
+                small = torch.where(part > 0, part, float("inf")).amin(0)
+                top = torch.minimum(part.amax(0), small * 2 ** 9) / 224
+                step = p[..., first:first + 128].amax(-1) * 448 * top
+                e = e + (6 / 12 ** 0.5 * part.shape[0] ** 0.5 * 2.0 ** -21 * step)[..., None]
+    d = (got.double() - out).abs()
+    assert torch.isfinite(got).all()
+    assert (d <= e).all(), float((d / e).max())
