@@ -3,10 +3,11 @@
  *
  * The CDSL step (cdsl.h) drafts k chains and keeps fp32 K/V of its own. These calls serve a program
  * that runs its own model and drafts a tree of tokens (Sec. 2.2's speculative decoding with several
- * candidates per position): the cache in 8 or 16 bits, the attention of the tree over it, the
- * validation of the drafts by M_p with the random numbers given (Sec. 3.2.2), and the move of the
- * taken path's K/V to their places. One decoding step is, for every layer, cdsl_kv_write and
- * cdsl_tree_attention, then cdsl_tree_verify and cdsl_kv_commit:
+ * candidates per position): rotary positions, the cache in 4, 8 or 16 bits, the attention of the tree over
+ * it, the validation of the drafts by M_p with the random numbers given (Sec. 3.2.2), and the move of the
+ * taken path's K/V to their places. One decoding step is, for every layer, cdsl_rope, cdsl_kv_write and
+ * cdsl_tree_attention, then cdsl_tree_verify and cdsl_kv_commit; between steps cdsl_kv_resize, cdsl_kv_fork and
+ * cdsl_kv_compact say which sequence has which pages:
  *
  *   nodes      0 .. n_b - 1 of sequence b; node 0 is the newest token, whose K/V are not yet cached;
  *              every other node is a drafted token whose parent has a smaller index
@@ -34,8 +35,8 @@
 extern "C" {
 #endif
 
-enum { CDSL_DTYPE_F8E4M3 = 2 };          /* of a cache only */
-enum { CDSL_TREE_MAX_NODES = 128, CDSL_TREE_MAX_BATCH = 1024, CDSL_TREE_MAX_VOCAB = 1 << 20 };
+enum { CDSL_DTYPE_F8E4M3 = 2, CDSL_DTYPE_I4 = 3 };   /* of a cache only */
+enum { CDSL_TREE_MAX_NODES = 128, CDSL_TREE_MAX_BATCH = 1024, CDSL_TREE_MAX_VOCAB = 1 << 20, CDSL_ROPE_MAX_DIM = 1024 };
 
 /* A paged cache of `batch` sequences, all memory the caller's.
  *   d_pool   [n_layers][n_pages][2 (K, V)][n_kv_heads][page_size][head_dim], e4m3 or bfloat16, 16-byte
@@ -43,6 +44,12 @@ enum { CDSL_TREE_MAX_NODES = 128, CDSL_TREE_MAX_BATCH = 1024, CDSL_TREE_MAX_VOCA
  *   d_scale  [n_layers][n_pages][2][n_kv_heads][page_size] bytes, 16-byte aligned: row (token and head) values are
  *            code * 2^(byte - 127). Byte 255: the row held a value that is not finite (in the cache's type); its
  *            codes are zeros and it stands for NaN. (A caller's own codes are finite.)
+ *   CDSL_DTYPE_I4: d_pool [..][page_size][head_dim / 2] bytes, d_scale [..][page_size][head_dim / 32] bfloat16, one
+ *            for each group of 32 values. A byte is two codes, two's complement, the first in the low half; a row's
+ *            groups take turns, four codes each: with G = head_dim / 32, code (j G + g) 4 + i is value 32 g + 4 j + i,
+ *            and the value code * scale of g. A row with a scale that is not finite stands for NaN. (A caller's own
+ *            codes are -7 .. 7 and scales have 4 significant bits, 2^-120 to 2^117, as cdsl_kv_write makes
+ *            them; others may be rounded to bfloat16 on their way through the attention.)
  *   d_page_table [batch][max_pages]: the page of slots [i * page_size, (i + 1) * page_size) of each
  *            sequence, any page ids in any order; entries beyond the cached slots are not read.
  * The pool needs no initial values. page_size: a power of two, 16..256. head_dim: 64 or 128. */
@@ -51,7 +58,7 @@ typedef struct cdsl_kv_cache {
   uint8_t* d_scale;
   const int32_t* d_page_table;
   int32_t n_layers, n_pages, n_kv_heads, page_size, head_dim;
-  int32_t dtype;                          /* CDSL_DTYPE_F8E4M3 or CDSL_DTYPE_BF16 */
+  int32_t dtype;                          /* CDSL_DTYPE_F8E4M3, CDSL_DTYPE_BF16 or CDSL_DTYPE_I4 */
   int32_t batch, max_pages;
 } cdsl_kv_cache;
 
@@ -60,7 +67,9 @@ typedef struct cdsl_kv_cache {
  * elements between sequences, tokens and heads of k, then of v (a head's values are contiguous).
  * e4m3: the scale is the smallest power of two (2^-126 at least) with which the row's largest
  * absolute value is at most 448, 1 for a row of zeros; codes are value / scale rounded to nearest
- * even. bfloat16: rounded to nearest even, scale 1. A slot beyond the page table, or a page id
+ * even. bfloat16: rounded to nearest even, scale 1. 4 bits: a group's scale is its largest absolute value / 7 in float32,
+ * rounded to 4 significant bits (nearest even), 2^-120 at least; codes are value / scale rounded to nearest even. A row
+ * with a value that is not finite, or of 2^120 or more, becomes NaN. A slot beyond the page table, or a page id
  * outside [0, n_pages), latches CDSL_ERANGE and its rows are not written. */
 CDSL_API int32_t cdsl_kv_write(const cdsl_kv_cache* cache, int32_t layer, const void* d_k,
                                const void* d_v, int32_t dtype, int32_t T, const int64_t* h_strides,
@@ -69,8 +78,8 @@ CDSL_API int32_t cdsl_kv_write(const cdsl_kv_cache* cache, int32_t layer, const 
 
 /* Read slots d_start[b] + i, i < d_count[b] (NULL: all T), of layers layer .. layer + n_layers - 1
  * back as values: d_k, d_v [n_layers, batch, T, n_kv_heads, head_dim] contiguous, 16-byte aligned,
- * of `dtype` (exact in either type for an e4m3 cache, but for values above the type's largest or below
- * its smallest). Rows i >= d_count[b], and rows whose slot or page is out of range (which latches
+ * of `dtype` (exact in either type for an e4m3 or 4-bit cache, but for values above the type's largest or
+ * below its smallest). Rows i >= d_count[b], and rows whose slot or page is out of range (which latches
  * CDSL_ERANGE), are zeros. */
 CDSL_API int32_t cdsl_kv_read(const cdsl_kv_cache* cache, int32_t layer, int32_t n_layers, void* d_k,
                               void* d_v, int32_t dtype, int32_t T, const int32_t* d_start,
@@ -115,7 +124,8 @@ CDSL_API int32_t cdsl_tree_attention_workspace(const cdsl_kv_cache* cache, int32
  * held to 2^-18 of a row's largest value and probabilities to 2^-8 of themselves (2^-10 on average) for
  * up to 32 query vectors per K/V head, to 2^-12 for more; small V rows count beside large ones by their
  * scales, which for that are to be the smallest ones, as cdsl_kv_write makes them. Over a bfloat16 cache
- * probabilities are held to 2^-17. float32 queries run on the CUDA cores in fp32.
+ * probabilities are held to 2^-17. float32 queries run on the CUDA cores in fp32. Over a 4-bit cache everything is in
+ * fp32.
  * d_workspace: cdsl_tree_attention_workspace bytes, 256-byte aligned, in any state; it
  * holds nothing between calls. */
 CDSL_API int32_t cdsl_tree_attention(const cdsl_kv_cache* cache, int32_t layer, const void* d_q,
@@ -124,6 +134,65 @@ CDSL_API int32_t cdsl_tree_attention(const cdsl_kv_cache* cache, int32_t layer, 
                                      const int32_t* d_nodes, const uint32_t* d_mask, float scale,
                                      int32_t max_len, void* d_out, float* d_lse, void* d_workspace,
                                      size_t workspace_bytes, int32_t* d_status, void* stream);
+
+/* Which sequence has which pages. A program that deals pages out keeps, next to its page table, d_refs [n_pages]:
+ * how many entries of its tables hold each page (0: free). The three calls below make a new table and new counts from
+ * old ones, on the device and in order of nothing but their indexes: free pages are dealt lowest first. Table entries
+ * of -1 hold nothing; others outside [0, n_pages) latch CDSL_ERANGE and count as -1. Holders beyond the table (a prefix
+ * that is kept, another table of the pool) are counts that the caller has added. A count that falls below 0 latches
+ * CDSL_EINVAL. d_workspace: cdsl_kv_pages_workspace bytes, 256-byte aligned, in any state; it holds nothing between
+ * calls. new_batch there: of the new table, the largest of those that are to use it. */
+CDSL_API int32_t cdsl_kv_pages_workspace(const cdsl_kv_cache* cache, int32_t new_batch, size_t* bytes);
+
+/* The cache's sequences become others: new sequence i, i < new_batch (1 .. 1024), goes on from the d_lens[d_src[i]] cached
+ * tokens of sequence d_src[i]. Whole pages are shared. The last page, if it is partly filled, stays with the first of
+ * a sequence's successors, if no other entry holds it; others get a copy of its rows, of every layer, in a free page. The
+ * old sequences' pages are given back, those past their length and those of sequences without successors among them
+ * (before the copies' pages are dealt). d_new_table [new_batch, max_pages] (-1 behind the pages), d_new_lens
+ * [new_batch] and d_new_refs [n_pages] are other memory than what is read. A length outside 0 .. max_pages * page_size
+ * latches CDSL_ERANGE and counts as the nearer bound; a d_src outside the batch latches it and gives an empty
+ * sequence. Without a free page left, CDSL_ENOMEM is latched and the sequence ends with its last whole page. */
+CDSL_API int32_t cdsl_kv_fork(const cdsl_kv_cache* cache, const int32_t* d_refs, const int32_t* d_src,
+                              const int32_t* d_lens, int32_t new_batch, int32_t* d_new_table, int32_t* d_new_lens,
+                              int32_t* d_new_refs, void* d_workspace, size_t workspace_bytes, int32_t* d_status,
+                              void* stream);
+
+/* Sequence b gets the pages of its first d_slots[b] slots: entries behind them are given back (0: all), then missing ones
+ * get free pages, in order of sequences and columns. Where there are none left, CDSL_ENOMEM is latched and entries stay -1. A
+ * d_slots[b] outside 0 .. max_pages * page_size latches CDSL_ERANGE and counts as the nearer bound. d_new_table [batch,
+ * max_pages] and d_new_refs [n_pages] may be the cache's table and d_refs themselves. */
+CDSL_API int32_t cdsl_kv_resize(const cdsl_kv_cache* cache, const int32_t* d_refs, const int32_t* d_slots,
+                                int32_t* d_new_table, int32_t* d_new_refs, void* d_workspace, size_t workspace_bytes,
+                                int32_t* d_status, void* stream);
+
+/* The pages in use (d_refs > 0) move to the front of the pool, in every layer: with n of them, *d_n_live = n, the k-th in use
+ * from n on goes to the k-th free one below n. d_page_map [n_pages]: each page's new place, -1 of free ones (for other
+ * tables of the pool); d_new_table and d_new_refs, which may be the cache's table and d_refs themselves, are the table and
+ * the counts after it. Pages from n on may then be cut off. */
+CDSL_API int32_t cdsl_kv_compact(const cdsl_kv_cache* cache, const int32_t* d_refs, int32_t* d_new_table,
+                                 int32_t* d_new_refs, int32_t* d_page_map, int32_t* d_n_live, void* d_workspace,
+                                 size_t workspace_bytes, int32_t* d_status, void* stream);
+
+/* Rotary positions. Host helper: the frequencies of rot / 2 pairs as fractions of a turn in 64 bits, h_turns [rot / 2], for
+ * cdsl_rope on the device: f_i = theta^(-2 i / rot) radians a position. Scaled for long contexts (factor != 1): by parts,
+ * g = clamp((original_len f_i / 2 pi - low) / (high - low), 0, 1) of a frequency stays and 1 - g of it is divided by
+ * factor, so that dimensions that turn more than `high` times over the original length stay as they are and those that
+ * turn less than `low` times go factor times slower. rot: even, 2 .. 1024. */
+CDSL_API int32_t cdsl_rope_turns(int32_t rot, double theta, double factor, int32_t original_len, double low, double high,
+                                 uint64_t* h_turns);
+
+/* Each head's first rot dimensions turn with the token's position d_start[b] + d_offset[b, t] (d_offset [batch, T], as
+ * cdsl_tree_mask's depths; NULL: t), exactly so for any positions:
+ *   (x_i, x_j) -> magnitude * (x_i cos - x_j sin, x_j cos + x_i sin),  j = i + rot / 2; interleaved: 2 i and 2 i + 1
+ * and the rest of the head stays. inverse: the other way (sin negated, magnitude as it is), which turns the outputs'
+ * gradients into the inputs'. q, and k (NULL: none), [batch, T, heads, head_dim] of `dtype` (CDSL_DTYPE_F32 or
+ * CDSL_DTYPE_BF16), computed in fp32; h_strides[12]: elements between sequences, tokens and heads of q, q's output, k and
+ * k's output (a head's values are contiguous). An output may be its input. d_turns: rot / 2 words of
+ * cdsl_rope_turns. head_dim: 2 .. 1024. */
+CDSL_API int32_t cdsl_rope(const uint64_t* d_turns, int32_t rot, int32_t interleaved, int32_t inverse, float magnitude,
+                           int32_t dtype, int32_t batch, int32_t T, int32_t head_dim, const void* d_q, void* d_q_out,
+                           int32_t n_heads, const void* d_k, void* d_k_out, int32_t n_kv_heads, const int64_t* h_strides,
+                           const int32_t* d_start, const int32_t* d_offset, void* stream);
 
 /* Validation of each sequence's tree by M_p (Sec. 3.2.2): walk from node 0 to a child that M_p takes,
  * and so on; at the node where no child is taken (or there is none) draw the next token. Row

@@ -17,7 +17,7 @@ from typing import List, Optional, Sequence
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libcdsl_gb300.so")
 
-DTYPE_F32, DTYPE_BF16, DTYPE_F8E4M3 = 0, 1, 2   # (e4m3: of a KvCache)
+DTYPE_F32, DTYPE_BF16, DTYPE_F8E4M3, DTYPE_I4 = 0, 1, 2, 3   # (e4m3 and 4 bits: of a KvCache)
 STATUS = {0: "CDSL_OK", 1: "CDSL_EINVAL", 2: "CDSL_ENOMEM", 3: "CDSL_ECUDA", 4: "CDSL_ETIMEOUT",
           5: "CDSL_ENONFINITE", 6: "CDSL_ESTATE", 7: "CDSL_ERANGE"}
 (CDSL_OK, CDSL_EINVAL, CDSL_ENOMEM, CDSL_ECUDA, CDSL_ETIMEOUT, CDSL_ENONFINITE, CDSL_ESTATE,
@@ -81,6 +81,12 @@ EXPORTS = {
                                  ctypes.c_size_t, _P, _P]),
     "cdsl_tree_verify": (_I, [_I, _I, _I, _P, _P, _I, _P, _P, _P, _P, _P, _P, ctypes.c_float, _P, _P, _P,
                               _P, _P]),
+    "cdsl_kv_pages_workspace": (_I, [_P, _I, _P]),
+    "cdsl_kv_fork": (_I, [_P, _P, _P, _P, _I, _P, _P, _P, _P, ctypes.c_size_t, _P, _P]),
+    "cdsl_kv_resize": (_I, [_P, _P, _P, _P, _P, _P, ctypes.c_size_t, _P, _P]),
+    "cdsl_kv_compact": (_I, [_P, _P, _P, _P, _P, _P, _P, ctypes.c_size_t, _P, _P]),
+    "cdsl_rope_turns": (_I, [_I, ctypes.c_double, ctypes.c_double, _I, ctypes.c_double, ctypes.c_double, _P]),
+    "cdsl_rope": (_I, [_P, _I, _I, _I, ctypes.c_float, _I, _I, _I, _I, _P, _P, _I, _P, _P, _I, _P, _P, _P, _P]),
     "cdsl_last_error": (ctypes.c_char_p, [_P]),
     "cdsl_destroy": (None, [_P]),
 }
@@ -300,9 +306,10 @@ class _Types:
 
         self.torch = torch
         self.i32, self.f32, self.bf16, self.u8 = torch.int32, torch.float32, torch.bfloat16, torch.uint8
+        self.i64 = torch.int64
         self.values = {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16}
         self.devices = None                    # how many (asked at the first launch)
-        self.caches = {torch.float8_e4m3fn: DTYPE_F8E4M3, torch.bfloat16: DTYPE_BF16}
+        self.caches = {torch.float8_e4m3fn: DTYPE_F8E4M3, torch.bfloat16: DTYPE_BF16, torch.uint8: DTYPE_I4}
 
 
 _types: Optional[_Types] = None
@@ -339,10 +346,10 @@ def _stream(fn: str, device, stream):
 
 
 class KvCache:
-    """A paged K/V cache in e4m3 or bfloat16: ``pool`` [layers, pages, 2, kv_heads, page_size, head_dim] of
+    """A paged K/V cache in e4m3, bfloat16 or 4 bits: ``pool`` [layers, pages, 2, kv_heads, page_size, head_dim] of
     torch.float8_e4m3fn or torch.bfloat16, ``scale`` [layers, pages, 2, kv_heads, page_size] uint8 (a row's
     values are code * 2^(byte - 127)) and ``page_table`` [batch, max_pages] int32, all contiguous on one CUDA
-    device. The tensors are the caller's; the object keeps them referenced. ``cache.at(page_table)`` is
+    device. In 4 bits: ``pool`` [.., head_dim / 2] uint8 and ``scale`` [.., page_size, head_dim / 32] bfloat16. The tensors are the caller's; the object keeps them referenced. ``cache.at(page_table)`` is
     the same pool under another table (another set of sequences)."""
 
     def __init__(self, pool, scale, page_table):
@@ -351,23 +358,34 @@ class KvCache:
             _bad("KvCache", "pool must be on a CUDA device")
         if pool.dim() != 6 or pool.shape[2] != 2 or not pool.is_contiguous() or pool.dtype not in ty.caches:
             _bad("KvCache", "pool must be a contiguous float8_e4m3fn or bfloat16 tensor [layers, pages, 2, "
-                            "kv_heads, page_size, head_dim]")
+                            "kv_heads, page_size, head_dim], or uint8 of head_dim / 2 bytes")
         L, N, _, H, P, D = pool.shape
-        _ints("KvCache", "scale", scale, pool.shape[:5], pool.device, ty.u8)
+        if pool.dtype is ty.u8:
+            D *= 2
+            _ints("KvCache", "scale", scale, pool.shape[:5] + (D // 32,), pool.device, ty.bf16)
+        else:
+            _ints("KvCache", "scale", scale, pool.shape[:5], pool.device, ty.u8)
         if page_table.dim() != 2:
             _bad("KvCache", "page_table must be [batch, max_pages]")
         _ints("KvCache", "page_table", page_table, page_table.shape, pool.device)
         self.pool, self.scale, self.page_table, self.device = pool, scale, page_table, pool.device
         self.batch, self.n_layers, self.n_kv_heads, self.head_dim = page_table.shape[0], L, H, D
+        self.n_pages, self.max_pages = N, page_table.shape[1]
         self._c = _KvCacheC(pool.data_ptr(), scale.data_ptr(), page_table.data_ptr(), L, N, H, P, D,
                             ty.caches[pool.dtype], page_table.shape[0], page_table.shape[1])
         self._ref = ctypes.addressof(self._c)
-        self._one = ty.torch.Size((self.batch,))
+        self._one, self._pages = ty.torch.Size((self.batch,)), ty.torch.Size((N,))
 
     @classmethod
     def empty(cls, n_layers, n_pages, n_kv_heads, page_size, head_dim, page_table, dtype=None):
-        """A cache with memory of its own (dtype: torch.float8_e4m3fn, the default, or torch.bfloat16)."""
+        """A cache with memory of its own (dtype: torch.float8_e4m3fn, the default, torch.bfloat16, or torch.uint8 for 4
+        bits)."""
         t = _torch().torch
+        if dtype is t.uint8:
+            shape = (n_layers, n_pages, 2, n_kv_heads, page_size)
+            dev = page_table.device
+            return cls(t.empty(shape + (head_dim // 2,), dtype=t.uint8, device=dev),
+                       t.empty(shape + (head_dim // 32,), dtype=t.bfloat16, device=dev), page_table)
         pool = t.empty((n_layers, n_pages, 2, n_kv_heads, page_size, head_dim), dtype=dtype or t.float8_e4m3fn,
                        device=page_table.device)
         return cls(pool, t.empty(pool.shape[:5], dtype=t.uint8, device=page_table.device), page_table)
@@ -448,6 +466,108 @@ def cdsl_kv_commit(cache: KvCache, lens, path, n_path, new_lens=None, status=Non
                                 None if new_lens is None else _ints(fn, "new_lens", new_lens, cache._one, cache.device),
                                 None if status is None else _ints(fn, "status", status, (1,), cache.device),
                                 _stream(fn, cache.device, stream)))
+
+
+def cdsl_kv_pages_workspace(cache: KvCache, new_batch: Optional[int] = None) -> int:
+    """Bytes of workspace that cdsl_kv_fork to new_batch sequences (None: as many as the cache has), cdsl_kv_resize and
+    cdsl_kv_compact need."""
+    n = ctypes.c_size_t(0)
+    _check(lib().cdsl_kv_pages_workspace(cache._ref, cache.batch if new_batch is None else new_batch, ctypes.byref(n)))
+    return n.value
+
+
+def _workspace(fn, workspace, dev):
+    if workspace.dtype is not _types.u8 or not workspace.is_contiguous() or workspace.device != dev:
+        _bad(fn, f"workspace must be a contiguous uint8 tensor on {dev}")
+    return workspace.data_ptr(), workspace.numel()
+
+
+def cdsl_kv_fork(cache: KvCache, refs, src, lens, new_table, new_lens, new_refs, workspace, status=None, stream=None):
+    """New sequence i goes on from the lens[src[i]] cached tokens of the cache's sequence src[i]: new_table [new_batch,
+    max_pages], new_lens [new_batch] and the pages' numbers of holders new_refs [n_pages] from refs [n_pages]; partly filled last
+    pages are copied for all successors of a sequence but the first. All int32. ``cache.at(new_table)`` is the cache after
+    it."""
+    fn = "cdsl_kv_fork"
+    if src.dim() != 1:
+        _bad(fn, "src must be [new_batch]")
+    new, dev = src.shape[0], cache.device
+    _check(lib().cdsl_kv_fork(
+        cache._ref, _ints(fn, "refs", refs, cache._pages, dev), _ints(fn, "src", src, (new,), dev),
+        _ints(fn, "lens", lens, cache._one, dev), new, _ints(fn, "new_table", new_table, (new, cache.max_pages), dev),
+        _ints(fn, "new_lens", new_lens, (new,), dev), _ints(fn, "new_refs", new_refs, cache._pages, dev),
+        *_workspace(fn, workspace, dev), None if status is None else _ints(fn, "status", status, (1,), dev),
+        _stream(fn, dev, stream)))
+
+
+def cdsl_kv_resize(cache: KvCache, refs, slots, new_table, new_refs, workspace, status=None, stream=None):
+    """Sequence b has the pages of its first slots[b] slots afterwards: those behind are given back, missing ones dealt
+    from the free ones (refs 0), lowest first. new_table and new_refs may be cache.page_table and refs."""
+    fn = "cdsl_kv_resize"
+    dev = cache.device
+    _check(lib().cdsl_kv_resize(
+        cache._ref, _ints(fn, "refs", refs, cache._pages, dev), _ints(fn, "slots", slots, cache._one, dev),
+        _ints(fn, "new_table", new_table, cache.page_table.shape, dev), _ints(fn, "new_refs", new_refs, cache._pages, dev),
+        *_workspace(fn, workspace, dev), None if status is None else _ints(fn, "status", status, (1,), dev),
+        _stream(fn, dev, stream)))
+
+
+def cdsl_kv_compact(cache: KvCache, refs, new_table, new_refs, page_map, n_live, workspace, status=None, stream=None):
+    """The pages in use (refs > 0) move to the front of the pool, in every layer: n_live [1] how many there are, page_map
+    [n_pages] each page's new place (-1: free). new_table and new_refs may be cache.page_table and refs."""
+    fn = "cdsl_kv_compact"
+    dev = cache.device
+    _check(lib().cdsl_kv_compact(
+        cache._ref, _ints(fn, "refs", refs, cache._pages, dev),
+        _ints(fn, "new_table", new_table, cache.page_table.shape, dev), _ints(fn, "new_refs", new_refs, cache._pages, dev),
+        _ints(fn, "page_map", page_map, cache._pages, dev), _ints(fn, "n_live", n_live, (1,), dev),
+        *_workspace(fn, workspace, dev), None if status is None else _ints(fn, "status", status, (1,), dev),
+        _stream(fn, dev, stream)))
+
+
+class Rope:
+    """Rotary positions of heads' first `rot` dimensions, for cdsl_rope. Pairs are i and i + rot / 2, or 2 i and 2 i + 1
+    (`interleaved`). `factor` != 1 scales positions by parts for contexts longer than `original_len`: dimensions that turn
+    fewer than `low` times over it go `factor` times slower, those that turn more than `high` times as before;
+    `magnitude` multiplies what is turned."""
+
+    def __init__(self, rot: int, *, theta: float = 10000.0, interleaved: bool = False, factor: float = 1.0,
+                 original_len: int = 0, low: float = 1.0, high: float = 32.0, magnitude: float = 1.0, device="cuda"):
+        t = _torch().torch
+        turns = t.zeros(max(1, rot // 2), dtype=t.int64)
+        _check(lib().cdsl_rope_turns(rot, theta, factor, original_len, low, high, turns.data_ptr()))
+        if not 0.0 < magnitude < float("inf"):
+            _bad("Rope", "magnitude must be positive and finite")
+        self.rot, self.interleaved, self.magnitude = rot, int(bool(interleaved)), magnitude
+        self.turns = turns.to(device)
+        self._ptr = self.turns.data_ptr()
+
+
+def cdsl_rope(rope: Rope, q, q_out, start, *, k=None, k_out=None, offset=None, inverse: bool = False, stream=None):
+    """q (and k) [batch, T, heads, head_dim] turned by their positions start[b] + offset[b, t] (offset None: t) into q_out
+    (and k_out), which may be the same tensors; any strides but the last. inverse: turned back, which takes gradients of the
+    outputs to those of the inputs."""
+    fn = "cdsl_rope"
+    code = _torch().values.get(q.dtype)
+    dev = rope.turns.device
+    tensors = (q, q_out) if k is None else (q, q_out, k, k_out)
+    if (k is None) != (k_out is None):
+        _bad(fn, "k and k_out go together")
+    if code is None or q.dim() != 4:
+        _bad(fn, "q must be a float32 or bfloat16 tensor [batch, T, heads, head_dim]")
+    B, T, H, D = q.shape
+    strides = []
+    for i, x in enumerate(tensors):
+        s, st = x.shape, x.stride()
+        if (x.dtype is not q.dtype or x.device != dev or len(s) != 4 or s[0] != B or s[1] != T or s[3] != D
+                or s != tensors[i // 2 * 2].shape or st[3] != 1):
+            _bad(fn, f"q, k and their outputs must be of one type on {dev}, [{B}, {T}, heads, {D}] with a contiguous last "
+                     f"dimension, got {x.dtype} {tuple(s)} with strides {tuple(st)} on {x.device}")
+        strides += st[:3]
+    _check(lib().cdsl_rope(
+        rope._ptr, rope.rot, rope.interleaved, int(bool(inverse)), rope.magnitude, code, B, T, D, q.data_ptr(),
+        q_out.data_ptr(), H, _ptr(k), _ptr(k_out), 0 if k is None else k.shape[2], (ctypes.c_int64 * 12)(*strides),
+        _ints(fn, "start", start, (B,), dev), None if offset is None else _ints(fn, "offset", offset, (B, T), dev),
+        _stream(fn, dev, stream)))
 
 
 def cdsl_tree_mask(parents: Sequence[int]):

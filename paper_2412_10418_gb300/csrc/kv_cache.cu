@@ -6,6 +6,11 @@
 // a code's value is the same in bf16, fp32 and 64 bits, and the attention folds it into scores and
 // probabilities without a rounding.
 //
+// Codes of 4 bits are whole numbers, -7 .. 7, which have no steps of their own to follow small values with: 32 values
+// share a scale, and it is not a power of two but the group's largest over 7, kept to 4 significant bits. With the code's
+// three that makes 7 bits, so a value is exact in bf16 all the same. (A bf16 scale as it comes has 8 bits, and every
+// product with a code would be rounded on its way to a tensor core.) 4.5 bits a value.
+//
 // All three are bound by HBM on large calls and by one launch on a decoding step's few rows. A lane of the first
 // two has 16 values, so that a row's few dependent loads (its start, its page, its values) are waited for half as often
 // as with 8: rows of 4 prompts of 1031 tokens, 8 heads of 128, bf16 to e4m3: 8.6 us written (25 MB, 10.1 with 8
@@ -80,8 +85,57 @@ struct WriteArgs {
   bool aligned;
 };
 
+// The codes of a lane's 16 values of an I4 row (half a group), with the group's scale. bad: the row is not finite.
+// The scale is top / 7 to 4 significant bits, nearest, ties to even; 2^-120 at least. Codes are x / scale, nearest, ties
+// to even: a product with the reciprocal can miss by one where it lies near a tie, which the exact remainder shows.
+__device__ __forceinline__ void quantise4(const float (&x)[EPL], uint32_t top, bool bad, uint32_t (&codes)[2], uint32_t* scale) {
+  uint32_t s = __float_as_uint(__fdiv_rn(__uint_as_float(top), 7.f));
+  s = (s + 0x7ffffu + (s >> 20 & 1)) & 0xfff00000u;
+  const float step = fmaxf(__uint_as_float(s), 0x1p-120f), inv = __frcp_rn(step), half = step * 0.5f;
+  codes[0] = codes[1] = 0u;
+#pragma unroll
+  for (int i = 0; i < EPL; ++i) {
+    const float y = fmaf(x[i], inv, 12582912.f);   // 1.5 * 2^23: the low bits are the whole number
+    const float rem = fmaf(12582912.f - y, step, x[i]);
+    int c = __float_as_int(y);
+    const float away = fabsf(rem);
+    if (away > half || (away == half && (c & 1))) c += rem > 0.f ? 1 : -1;
+    codes[i / 8] |= (uint32_t)(c & 15) << (i % 8 * 4);
+  }
+  if (bad) codes[0] = codes[1] = 0u;
+  *scale = bad ? 0x7fc0u : __float_as_uint(step) >> 16;
+}
+// Pieces of 16 bits (four codes) of an I4 row change lanes: a lane's 16 values are the pieces (j, g), j = 4 (part % 2) ..,
+// g = part / 2, of which its 8 bytes of the row hold the numbers 4 part .. 4 part + 3, number j * G + g.
+template <int LPR>
+__device__ __forceinline__ void values_to_row(unsigned lanes, int part, uint32_t (&w)[2]) {
+  constexpr int G = LPR / 2;
+  uint32_t out[2] = {0u, 0u};
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    const int h = 4 * part + t, j = h / G, g = h % G;
+    const uint32_t lo = __shfl_sync(lanes, w[0], 2 * g + j / 4, LPR), hi = __shfl_sync(lanes, w[1], 2 * g + j / 4, LPR);
+    out[t / 2] |= ((j % 4 / 2 ? hi : lo) >> (j % 2 * 16) & 0xffffu) << (t % 2 * 16);
+  }
+  w[0] = out[0];
+  w[1] = out[1];
+}
+template <int LPR>
+__device__ __forceinline__ void row_to_values(unsigned lanes, int part, uint32_t (&w)[2]) {
+  constexpr int G = LPR / 2;
+  uint32_t out[2] = {0u, 0u};
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    const int h = (4 * (part % 2) + t) * G + part / 2;
+    const uint32_t lo = __shfl_sync(lanes, w[0], h / 4, LPR), hi = __shfl_sync(lanes, w[1], h / 4, LPR);
+    out[t / 2] |= ((h % 4 / 2 ? hi : lo) >> (h % 2 * 16) & 0xffffu) << (t % 2 * 16);
+  }
+  w[0] = out[0];
+  w[1] = out[1];
+}
+
 // Grid: (rows of a sequence over blocks, batch). LPR = head_dim / 16 lanes work on a row.
-template <typename T, int LPR, bool F8>
+template <typename T, int LPR, int FORMAT>
 __global__ void __launch_bounds__(kThreads) k_kv_write(WriteArgs a) {
   pdl_wait();
   pdl_launch_dependents();
@@ -103,15 +157,23 @@ __global__ void __launch_bounds__(kThreads) k_kv_write(WriteArgs a) {
 #pragma unroll
   for (int i = 0; i < EPL; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
   const unsigned lanes = ((1u << LPR) - 1) << ((threadIdx.x & 31) / LPR * LPR);   // of this row
+  const uint32_t group = FORMAT == kI4 ? max(top, __shfl_xor_sync(lanes, top, 1)) : 0u;
 #pragma unroll
   for (int o = LPR / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(lanes, top, o));
   if (page < 0) {
     if (part == 0) set_status(a.r.status, CDSL_ERANGE);
     return;
   }
-  const bool bad = top >= (F8 ? 0x7f800000u : 0x7f7f8000u);   // (not finite, or bf16 rounds it to infinity)
+  // (not finite; bf16: or rounded to infinity; I4: or 2^120 and more, beyond which codes times 8 would not fit)
+  const bool bad = top >= (FORMAT == kF8 ? 0x7f800000u : FORMAT == kBF16 ? 0x7f7f8000u : 0x7b800000u);
   const size_t r = row_of(c, a.r.layer, page, kv, h, at);
-  if constexpr (F8) {
+  if constexpr (FORMAT == kI4) {
+    uint32_t w[2], s;
+    quantise4(x, group, bad, w, &s);
+    values_to_row<LPR>(lanes, part, w);
+    *reinterpret_cast<uint2*>(c.pool + r * c.row + part * 8) = make_uint2(w[0], w[1]);
+    if (part % 2 == 0) reinterpret_cast<uint16_t*>(c.scale + r * c.srow)[part / 2] = (uint16_t)s;
+  } else if constexpr (FORMAT == kF8) {
     // smallest E with top <= 448 * 2^E = 1.75 * 2^(E + 8)
     int e = (int)(top >> 23) - 127 - 8 + ((top & 0x7fffffu) > 0x600000u);
     e = top == 0 || bad ? 0 : max(e, -126);
@@ -140,7 +202,7 @@ struct ReadArgs {
 };
 
 // Grid: (rows of a sequence over blocks, batch, layers).
-template <typename T, int LPR, bool F8>
+template <typename T, int LPR, int FORMAT>
 __global__ void __launch_bounds__(kThreads) k_kv_read(ReadArgs a) {
   pdl_wait();
   pdl_launch_dependents();
@@ -161,8 +223,25 @@ __global__ void __launch_bounds__(kThreads) k_kv_read(ReadArgs a) {
     } else {
       const int at = (a.r.start[b] + (int)t) & ((1 << c.page_shift) - 1);
       const size_t r = row_of(c, a.r.layer + layer, page, kv, h, at);
-      const float s = scale_value(c.scale[r]);
-      if constexpr (F8) {
+      if constexpr (FORMAT == kI4) {
+        const unsigned lanes = ((1u << LPR) - 1) << ((threadIdx.x & 31) / LPR * LPR);
+        const uint2 u = *reinterpret_cast<const uint2*>(c.pool + r * c.row + part * 8);
+        uint32_t w[2] = {u.x, u.y};
+        row_to_values<LPR>(lanes, part, w);
+        // (one scale that is not finite: the row's all count as NaN)
+        const uint32_t* const sp = reinterpret_cast<const uint32_t*>(c.scale + r * c.srow);
+        const uint2 all = make_uint2(sp[0], LPR == 8 ? sp[LPR / 8] : 0u);
+        const float s = i4_not_finite(all, LPR / 2) ? __uint_as_float(0x7fc00000u)
+                                                    : bf16_at(part / 4 ? all.y : all.x, part / 2 & 1);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float y[4];
+          i4x4_to_f32(w[i / 2] >> (i % 2 * 16), s, y);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[4 * i + e] = y[e];
+        }
+      } else if constexpr (FORMAT == kF8) {
+        const float s = scale_value(c.scale[r]);
         const uint4 u = *reinterpret_cast<const uint4*>(c.pool + r * c.hd + part * EPL);
         const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
@@ -172,6 +251,7 @@ __global__ void __launch_bounds__(kThreads) k_kv_read(ReadArgs a) {
           x[2 * i + 1] = f.y * s;
         }
       } else {
+        const float s = scale_value(c.scale[r]);
         load_values(reinterpret_cast<const __nv_bfloat16*>(c.pool) + r * c.hd + part * EPL, true, x);
 #pragma unroll
         for (int i = 0; i < EPL; ++i) x[i] *= s;
@@ -201,7 +281,7 @@ struct CommitArgs {
 
 constexpr int kMoves = 8;              // rows that a thread holds at a time
 
-// Grid: (layer, K or V, sequence). A thread moves 16 bytes of a head's row (or its scale byte) for
+// Grid: (layer, K or V, sequence). A thread moves 16 bytes of a head's row (or its scales) for
 // path entries 1, 2, .. in order, kMoves reads before their writes. In order is enough: the path is
 // strictly increasing from 0, so entry i's target i is below the sources of all later entries. Blocks have a thread a
 // part, so that one wave takes a served batch: 40 layers of 16 trees of 49 nodes in 7.7 us, 3 us less than with 256
@@ -244,21 +324,23 @@ __global__ void __launch_bounds__(kThreads) k_kv_commit(CommitArgs a) {
         if (i0 + i < n && s_from[i0 + i] != s_to[i0 + i]) base[row(s_to[i0 + i], head) * pitch] = x[i];
     }
   };
-  const int per = c.hd * c.eb / 16, codes = c.kvh * per;   // 16-byte parts of a row, of all heads
+  const int per = c.row / 16, codes = c.kvh * per;   // 16-byte parts of a row, of all heads
   for (int q = threadIdx.x; q < codes + c.kvh; q += blockDim.x) {
     if (q < codes) move(reinterpret_cast<uint4*>(c.pool) + q % per, per, q / per);
-    else move(c.scale, 1, q - codes);
+    else if (c.srow == 1) move(c.scale, 1, q - codes);
+    else if (c.srow == 4) move(reinterpret_cast<uint32_t*>(c.scale), 1, q - codes);
+    else move(reinterpret_cast<uint2*>(c.scale), 1, q - codes);
   }
 }
 
 template <typename F>
-int by_shape(const Cache& c, int dtype, F&& f) {   // f(element type tag, lanes per row, e4m3?)
+int by_shape(const Cache& c, int dtype, F&& f) {   // f(element type tag, lanes per row, format)
+  auto h = [&](auto t, auto lpr) {
+    if (c.format == kI4) return f(t, lpr, std::integral_constant<int, kI4>());
+    return c.format == kF8 ? f(t, lpr, std::integral_constant<int, kF8>()) : f(t, lpr, std::integral_constant<int, kBF16>());
+  };
   auto g = [&](auto t) {
-    if (c.hd == 128)
-      return c.eb == 1 ? f(t, std::integral_constant<int, 8>(), std::true_type())
-                       : f(t, std::integral_constant<int, 8>(), std::false_type());
-    return c.eb == 1 ? f(t, std::integral_constant<int, 4>(), std::true_type())
-                     : f(t, std::integral_constant<int, 4>(), std::false_type());
+    return c.hd == 128 ? h(t, std::integral_constant<int, 8>()) : h(t, std::integral_constant<int, 4>());
   };
   return dtype == CDSL_DTYPE_BF16 ? g(__nv_bfloat16()) : g(float());
 }
@@ -298,8 +380,8 @@ extern "C" int32_t cdsl_kv_write(const cdsl_kv_cache* cache, int32_t layer, cons
     if (a.sk[i] * eb % 16 || a.sv[i] * eb % 16) a.aligned = false;
   }
   const dim3 grid(row_blocks(c, T), c.batch);
-  return by_shape(c, dtype, [&](auto t, auto lpr, auto f8) {
-    return ck.launched(launch_pdl(k_kv_write<decltype(t), lpr(), f8()>, grid, dim3(kThreads), 0,
+  return by_shape(c, dtype, [&](auto t, auto lpr, auto format) {
+    return ck.launched(launch_pdl(k_kv_write<decltype(t), lpr(), format()>, grid, dim3(kThreads), 0,
                                   static_cast<cudaStream_t>(stream), a));
   });
 }
@@ -318,8 +400,8 @@ extern "C" int32_t cdsl_kv_read(const cdsl_kv_cache* cache, int32_t layer, int32
   a.k = d_k;
   a.v = d_v;
   const dim3 grid(row_blocks(c, T), c.batch, n_layers);
-  return by_shape(c, dtype, [&](auto t, auto lpr, auto f8) {
-    return ck.launched(launch_pdl(k_kv_read<decltype(t), lpr(), f8()>, grid, dim3(kThreads), 0,
+  return by_shape(c, dtype, [&](auto t, auto lpr, auto format) {
+    return ck.launched(launch_pdl(k_kv_read<decltype(t), lpr(), format()>, grid, dim3(kThreads), 0,
                                   static_cast<cudaStream_t>(stream), a));
   });
 }
@@ -333,7 +415,7 @@ extern "C" int32_t cdsl_kv_commit(const cdsl_kv_cache* cache, const int32_t* d_l
   if (!d_lens || !d_path || !d_n_path) return ck.fail("a required pointer is NULL");
   if (d_new_lens == d_lens) return ck.fail("d_new_lens must not be d_lens");
   const CommitArgs a = {c, d_lens, d_path, d_n_path, T, d_new_lens, d_status};
-  const int parts = c.kvh * (c.hd * c.eb / 16 + 1);   // a token's, scales last: a thread each
+  const int parts = c.kvh * (c.row / 16 + 1);   // a token's, scales last: a thread each
   return ck.launched(launch_pdl(k_kv_commit, dim3(c.n_layers, 2, c.batch), dim3(std::min(kThreads, (parts + 31) / 32 * 32)), 0,
                                 static_cast<cudaStream_t>(stream), a));
 }

@@ -23,6 +23,7 @@ constexpr float kLn2 = 0.693147180559945309f;
 struct TreeArgs {
   Cache c;
   int layer, T, H, G, W, NQ, QB;               // W: mask words; QB: query blocks per head
+  int dtype;                                   // of q and out
   const void* q;
   void* out;
   float* lse;

@@ -664,8 +664,8 @@ cudaError_t launch(const TreeArgs& a, cudaStream_t s) {
 }  // namespace
 
 cudaError_t launch_tree_rows(const TreeArgs& a, cudaStream_t s) {
-  if (a.c.hd == 128) return a.c.eb == 1 ? launch<128, true>(a, s) : launch<128, false>(a, s);
-  return a.c.eb == 1 ? launch<64, true>(a, s) : launch<64, false>(a, s);
+  if (a.c.hd == 128) return a.c.format == kF8 ? launch<128, true>(a, s) : launch<128, false>(a, s);
+  return a.c.format == kF8 ? launch<64, true>(a, s) : launch<64, false>(a, s);
 }
 
 }  // namespace tree

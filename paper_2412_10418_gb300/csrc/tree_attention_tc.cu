@@ -570,15 +570,15 @@ auto by_query_block(int NQ, F&& f) {
 
 int tc_blocks_per_sm(const Cache& c, int NQ) {
   return by_query_block(NQ, [&](auto n) {
-    if (c.hd == 128) return c.eb == 1 ? Cfg<128, n(), true>::CTAS : Cfg<128, n(), false>::CTAS;
-    return c.eb == 1 ? Cfg<64, n(), true>::CTAS : Cfg<64, n(), false>::CTAS;
+    if (c.hd == 128) return c.format == kF8 ? Cfg<128, n(), true>::CTAS : Cfg<128, n(), false>::CTAS;
+    return c.format == kF8 ? Cfg<64, n(), true>::CTAS : Cfg<64, n(), false>::CTAS;
   });
 }
 
 cudaError_t launch_tree_tc(const TreeArgs& a, cudaStream_t s) {
   return by_query_block(a.NQ, [&](auto n) {
-    if (a.c.hd == 128) return a.c.eb == 1 ? launch<128, n(), true>(a, s) : launch<128, n(), false>(a, s);
-    return a.c.eb == 1 ? launch<64, n(), true>(a, s) : launch<64, n(), false>(a, s);
+    if (a.c.hd == 128) return a.c.format == kF8 ? launch<128, n(), true>(a, s) : launch<128, n(), false>(a, s);
+    return a.c.format == kF8 ? launch<64, n(), true>(a, s) : launch<64, n(), false>(a, s);
   });
 }
 

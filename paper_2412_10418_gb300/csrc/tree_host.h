@@ -40,8 +40,8 @@ struct Check {
     if (k->head_dim != 64 && k->head_dim != 128) return no("head_dim must be 64 or 128");
     if (k->page_size < 16 || k->page_size > 256 || (k->page_size & (k->page_size - 1)))
       return no("page_size must be a power of two, 16..256");
-    if (k->dtype != CDSL_DTYPE_F8E4M3 && k->dtype != CDSL_DTYPE_BF16)
-      return no("the cache's dtype must be e4m3 or bfloat16");
+    if (k->dtype != CDSL_DTYPE_F8E4M3 && k->dtype != CDSL_DTYPE_BF16 && k->dtype != CDSL_DTYPE_I4)
+      return no("the cache's dtype must be e4m3, bfloat16 or 4 bits");
     if (k->n_layers < 1 || k->n_layers > 65535 || k->n_pages < 1 || k->n_kv_heads < 1 || k->max_pages < 1 ||
         k->batch < 1 || k->batch > CDSL_TREE_MAX_BATCH)
       return no("cache sizes: need n_layers, n_pages, n_kv_heads, max_pages >= 1, 1 <= batch <= 1024");
@@ -52,8 +52,11 @@ struct Check {
                 "1024 heads)");
     int shift = 4;
     while ((1 << shift) < k->page_size) ++shift;
+    const int f = k->dtype == CDSL_DTYPE_I4 ? kI4 : k->dtype == CDSL_DTYPE_BF16 ? kBF16 : kF8;
     *c = {static_cast<uint8_t*>(k->d_pool), k->d_scale, k->d_page_table, k->n_layers, k->n_pages,
-          k->n_kv_heads, shift, k->head_dim, k->dtype == CDSL_DTYPE_BF16 ? 2 : 1, k->batch, k->max_pages};
+          k->n_kv_heads, shift, k->head_dim, k->batch, k->max_pages, f,
+          f == kI4 ? k->head_dim / 2 : f == kBF16 ? k->head_dim * 2 : k->head_dim,
+          f == kI4 ? k->head_dim / kGroup * 2 : 1};
     return true;
   }
   bool layers(const Cache& c, int layer, int n) const {
