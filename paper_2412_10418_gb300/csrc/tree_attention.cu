@@ -485,15 +485,24 @@ struct Sizes {
   int NQ, QB, blocks;
   size_t o_off, bytes;
 };
-void sizes_of(const Cache& c, bool tc, int H, int T, Sizes* z) {
-  const int vectors = T * (H / c.kvh);
-  z->NQ = !tc ? SQ : vectors <= 16 ? 16 : vectors <= 32 ? 32 : kRowsBlock;
-  z->QB = (vectors + z->NQ - 1) / z->NQ;
-  z->blocks = kPlanSMs * (!tc ? simt_per_sm(c.hd, c.format) : z->NQ == kRowsBlock ? 1 : tc_blocks_per_sm(c, z->NQ));
+void bytes_of(const Cache& c, Sizes* z) {
   const size_t slots = (size_t)z->blocks * 2 * z->NQ;
   auto up = [](size_t n) { return (n + 255) / 256 * 256; };
   z->o_off = up(slots * 2 * sizeof(float));
   z->bytes = up(z->o_off + slots * c.hd * sizeof(float));
+}
+void sizes_of(const Cache& c, bool tc, int H, int T, Sizes* z) {   // tc: bf16 queries
+  const int vectors = T * (H / c.kvh);
+  if (c.format == kI4) {
+    z->NQ = vectors <= 8 || !tc ? 8 : 16;
+    z->QB = (vectors + z->NQ - 1) / z->NQ;
+    z->blocks = kPlanSMs * i4_blocks_per_sm(c, z->NQ, !tc);
+    return bytes_of(c, z);
+  }
+  z->NQ = !tc ? SQ : vectors <= 16 ? 16 : vectors <= 32 ? 32 : kRowsBlock;
+  z->QB = (vectors + z->NQ - 1) / z->NQ;
+  z->blocks = kPlanSMs * (!tc ? simt_per_sm(c.hd, c.format) : z->NQ == kRowsBlock ? 1 : tc_blocks_per_sm(c, z->NQ));
+  bytes_of(c, z);
 }
 
 template <typename T, int HD>
@@ -512,9 +521,7 @@ cudaError_t launch_simt(const TreeArgs& a, cudaStream_t s) {
 cudaError_t launch_pass(const TreeArgs& a, bool tc, bool split, cudaStream_t s) {
   const bool d128 = a.c.hd == 128, f8 = a.c.format == kF8, bf16 = a.dtype == CDSL_DTYPE_BF16;
   cudaError_t e;
-  if (a.c.format == kI4)
-    e = bf16 ? (d128 ? launch_simt<__nv_bfloat16, 128, kI4>(a, s) : launch_simt<__nv_bfloat16, 64, kI4>(a, s))
-             : (d128 ? launch_simt<float, 128, kI4>(a, s) : launch_simt<float, 64, kI4>(a, s));
+  if (a.c.format == kI4) e = launch_tree_i4(a, s);
   else if (tc) e = a.NQ == kRowsBlock ? launch_tree_rows(a, s) : launch_tree_tc(a, s);
   else if (d128) e = f8 ? launch_simt<float, 128, kF8>(a, s) : launch_simt<float, 128, kBF16>(a, s);
   else e = f8 ? launch_simt<float, 64, kF8>(a, s) : launch_simt<float, 64, kBF16>(a, s);
@@ -560,7 +567,7 @@ extern "C" int32_t cdsl_tree_attention_workspace(const cdsl_kv_cache* cache, int
   if (!bytes) return ck.fail("bytes is NULL");
   Sizes z[2];
   sizes_of(c, false, n_heads, T, &z[0]);
-  sizes_of(c, c.format != kI4, n_heads, T, &z[1]);
+  sizes_of(c, true, n_heads, T, &z[1]);
   *bytes = std::max(z[0].bytes, z[1].bytes);
   return CDSL_OK;
 }
@@ -586,7 +593,7 @@ extern "C" int32_t cdsl_tree_attention(const cdsl_kv_cache* cache, int32_t layer
   const int64_t* const so = h_strides + 3;
   if ((c.batch > 1 && so[0] == 0) || (T > 1 && so[1] == 0) || (n_heads > 1 && so[2] == 0))
     return ck.fail("out must not have a stride of 0 between sequences, tokens or heads");
-  const bool tc = dtype == CDSL_DTYPE_BF16 && c.format != kI4;
+  const bool tc = dtype == CDSL_DTYPE_BF16;
   Sizes z;
   sizes_of(c, tc, n_heads, T, &z);
   if (!ck.aligned(d_workspace, 256) || workspace_bytes < z.bytes)

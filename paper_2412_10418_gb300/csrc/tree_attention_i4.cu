@@ -1,0 +1,561 @@
+// tree_attention_i4.cu -- cdsl_tree_attention over a 4-bit cache, few query vectors per K/V head.
+//
+// A row of 128 values is 72 bytes, so that what bounds a large pass is less the bytes than the work on each of them:
+// 1.8 us of HBM bring an SM 300,000 codes. Slots are the MMA's M as in tree_attention_tc.cu, but codes go from
+// shared memory to registers, become 16-bit operands there and are multiplied there (mma.sync m16n8k16); through shared memory
+// to tcgen05 they would be written and read once more, in 16 bits four times their size, which alone takes longer than
+// HBM does. A row's groups take turns by four values, so that one 8- or 16-byte load gives a lane the fragments of all
+// groups.
+//
+//   S^T = K Q^T    K's operand is a code plus 8 as the bits of an fp16 number below 2^-14, one instruction for two of
+//                  them: (word & 0x000f000f) ^ 0x00080008 = (code + 8) 2^-24, the next four bits 2^-20. What the 8
+//                  adds, -8 times the sum of the group's q, is what the accumulators start from. Groups are summed
+//                  apart and multiplied by their scales in fp32. q is held in fp16 planes under a power of two that takes the
+//                  row's largest to 2^14 or more: exact down to 2^-31 of it from bf16 (one plane) or float32 (three).
+//   O^T = V^T P^T  V's operand is the value in bf16, exact (a code's 3 bits by a scale's 4): bits 3 .. 6 of
+//                  128 + 8 (code + 8), then one fma of two by (scale / 8, -24 scale). P is the sum of two bf16
+//                  planes (2^-16 of itself; three for float32 queries, 2^-24): fp32's range, whatever lies next to what.
+//
+// Each stretch of 64 slots starts its sums O^T at zero and is added to fp32 registers, so that no sum is a long chain of a tensor
+// core's truncating additions. A warp has a run of its own and no barrier but its own; its K and V come by bulk copies, the next
+// stretch's K while this one's softmax and P V run, and V beside the next scores.
+//
+// Waits are bounded by a number of tries (wait_for): on expiry CDSL_ETIMEOUT is latched and the warp exits once its copies
+// have landed or been given up on as well.
+#include <cuda.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "kernels.h"
+#include "once.h"
+#include "tree_attention.cuh"
+#include "tree_tc.cuh"
+
+namespace cdsl {
+namespace tree {
+namespace {
+
+constexpr int kStretch = 64;                   // slots at a time
+constexpr int kTiles = kStretch / 16;
+constexpr int kPitch = kStretch + 4;           // floats of a vector's probabilities
+
+template <int HD, int NQ, bool F32>
+struct Cfg {
+  static constexpr int G = HD / kGroup, RB = HD / 2, SB = 2 * G;   // groups; bytes of a row's codes and scales
+  static constexpr int NT = NQ / 8;                                // vectors by eights
+  static constexpr int QP = F32 ? 3 : 1, PP = F32 ? 3 : 2;         // planes of q and p
+  static constexpr uint32_t CODES = kStretch * RB, SCALES = kStretch * SB;
+  static constexpr uint32_t V_OFF = CODES + SCALES;
+  static constexpr uint32_t P_OFF = 2 * V_OFF;
+  static constexpr uint32_t MASK_OFF = P_OFF + NQ * kPitch * 4;
+  static constexpr uint32_t PLAN_OFF = MASK_OFF + NQ * (kWords + 1) * 4;
+  static constexpr int WARPS = F32 || NQ == 16 ? 8 : HD == 128 ? 12 : 16;   // of an SM, by registers
+  static constexpr size_t smem(int batch) { return PLAN_OFF + plan_bytes(batch); }
+};
+
+__device__ __forceinline__ uint32_t prmt(uint32_t a, uint32_t b, uint32_t sel) { return __byte_perm(a, b, sel); }
+// The pieces (16 bits, four codes) of group g (even: the low one) of two words.
+__device__ __forceinline__ uint32_t both(uint32_t a, uint32_t b, int g) { return prmt(a, b, g & 1 ? 0x7632 : 0x5410); }
+
+__device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t fma_bf16x2(uint32_t a, uint32_t b, uint32_t c) {
+  uint32_t d;
+  asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
+  return d;
+}
+__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+// (a, b) as two bf16, a low.
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ uint32_t pack_f16(float a, float b) {
+  const __half2 h = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+// Code i of both pieces in x, times their scales: s8 = (scale / 8) and m24 = (-24 scale) of the two.
+template <int I>
+__device__ __forceinline__ uint32_t value_bf16(uint32_t x, uint32_t s8, uint32_t m24) {
+  const uint32_t t = I == 0 ? x << 3 : x >> (4 * I - 3);
+  return fma_bf16x2((t & 0x00780078u) ^ 0x43404340u, s8, m24);
+}
+
+// A stretch of a segment: where it is, and the lane's page of it (pieces of a page or of 64 slots; lanes past them: -1).
+struct Stretch {
+  int slot, n;                                 // first slot, slots that there are
+  int page;
+  uint32_t live;                               // pieces that have a page
+};
+
+template <int HD, int NQ, bool F32>
+__global__ void __launch_bounds__(32, Cfg<HD, NQ, F32>::WARPS) k_tree_i4(TreeArgs a) {
+  using C = Cfg<HD, NQ, F32>;
+  using T = std::conditional_t<F32, float, __nv_bfloat16>;
+  constexpr int G = C::G, NT = C::NT, QP = C::QP, PP = C::PP;
+  extern __shared__ __align__(128) uint8_t sm[];
+  __shared__ __align__(8) uint64_t full[2];    // K, V
+  __shared__ Segment s_seg[2];                 // this segment and the next (registers are dear)
+  float* const s_p = reinterpret_cast<float*>(sm + C::P_OFF);
+  uint32_t* const s_mask = reinterpret_cast<uint32_t*>(sm + C::MASK_OFF);
+  int* const s_first = reinterpret_cast<int*>(sm + C::PLAN_OFF);
+  const Cache& c = a.c;
+  const int lane = threadIdx.x, r = lane >> 2, q4 = lane & 3;   // fragments' row (or column) and quarter
+  if (lane == 0) {
+    tc::mbar_init(&full[0], 1);
+    tc::mbar_init(&full[1], 1);
+    tc::fence_mbar_init();
+  }
+  pdl_wait();
+  pdl_launch_dependents();
+  build_plan(a, s_first);                      // (ends in a block barrier)
+  if (blockIdx.x == 0) check_lens(a);
+  const int total = s_first[c.batch], runs = runs_of(a, total);
+  if ((int)blockIdx.x >= runs) return;
+  const int end = run_begin(blockIdx.x + 1, total, runs);
+  const float fa = a.scale * 0x1p10f;          // of all scores: 2^24 of the codes, 2^-14 of the queries
+  const int P = 1 << c.page_shift, rows = min(P, kStretch), shift = min(c.page_shift, 6);
+
+  // a stretch's pages, and its copies; K's and V's are the same rows of the page's two halves
+  auto locate = [&](const Segment& s, int slot) {
+    Stretch x = {slot, min(kStretch, min(s.keys, s.c1 * kKeys) - slot), -1, 0u};
+    const int mine = slot + lane * rows;
+    if (lane < kStretch / rows && lane * rows < x.n) {
+      x.page = page_of(c, s.b, mine);
+      if (x.page < 0) set_status(a.status, CDSL_ERANGE);
+    }
+    x.live = __ballot_sync(0xffffffffu, x.page >= 0);
+    return x;
+  };
+  auto load = [&](const Segment& s, const Stretch& x, int kv) {
+    if (lane == 0) tc::mbar_expect_tx(&full[kv], __popc(x.live) * rows * (C::RB + C::SB));
+    __syncwarp();
+    if (x.page >= 0) {
+      const size_t row = row_of(c, a.layer, x.page, kv, s.h, (x.slot + lane * rows) & (P - 1));
+      uint8_t* const to = sm + kv * C::V_OFF;
+      tc::bulk_load(to + lane * rows * C::RB, c.pool + row * C::RB, rows * C::RB, &full[kv]);
+      tc::bulk_load(to + C::CODES + lane * rows * C::SB, c.scale + row * C::SB, rows * C::SB, &full[kv]);
+    }
+  };
+
+  int it = 0;                                  // stretches
+  int unit = run_begin(blockIdx.x, total, runs), turn = 0;
+  if (lane == 0) s_seg[0] = segment_at(a, s_first, unit, end);
+  __syncwarp();
+  Stretch x = {};
+  bool loaded = false;                         // x is the segment's first stretch and on its way
+#pragma unroll 1
+  for (; unit < end; turn ^= 1) {
+    const Segment& s = s_seg[turn];
+    const Segment& next = s_seg[turn ^ 1];
+    if (!loaded && s.keys > 0) {
+      x = locate(s, s.c0 * kKeys);
+      load(s, x, 0);
+      load(s, x, 1);
+    }
+    loaded = false;
+    unit += s.c1 - s.c0;
+    __syncwarp();                              // (the segment before is done with shared memory)
+    if (lane == 0 && unit < end) s_seg[turn ^ 1] = segment_at(a, s_first, unit, end);
+    for (int i = lane; i < NQ * (kWords + 1); i += 32) {
+      const int v = i / (kWords + 1), w = i % (kWords + 1);
+      s_mask[i] = v < s.nq && w < a.W ? a.mask[((size_t)s.b * a.T + vector_of(a, s.h, s.qb, v).t) * a.W + w] : 0u;
+    }
+    // ---- queries: this lane has dimensions 32 g + 8 q4 .. of vectors r (+ 8) as the MMA's columns
+    uint32_t qf[NT][QP][G][4];                 // of both steps of a group
+    float from[NT][G][2];                      // what the accumulators of vectors 2 q4, 2 q4 + 1 (+ 8) start from
+    float fb[NT][2];                           // and their scores' factors
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const int v = 8 * n + r;
+      const bool any = v < s.nq;
+      const Vec w = vector_of(a, s.h, s.qb, any ? v : 0);
+      const T* const q = static_cast<const T*>(a.q) + s.b * a.sq[0] + w.t * a.sq[1] + w.h * a.sq[2] + 8 * q4;
+      float y[G][8];
+      uint32_t top = 0;
+#pragma unroll
+      for (int g = 0; g < G; ++g)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          y[g][e] = any ? to_f32<T>(q[g * kGroup + e]) : 0.f;
+          top = max(top, __float_as_uint(y[g][e]) & 0x7fffffffu);
+        }
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      const int e2 = max((int)(top >> 23) - 127, -100);          // (a row that is not finite: 128)
+      // (to 2^14 .. 2^15: up to twice that could round to infinity)
+      const float up = top >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : exp2f((float)(14 - e2));
+      const float f = any ? exp2f((float)e2) : 0.f;
+      float sum[G];
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+        sum[g] = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[g][e] *= e & 1 ? up * 0.0625f : up;   // (the second and fourth of four: codes 2^4 higher)
+#pragma unroll
+        for (int p = 0; p < QP; ++p)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t two = pack_f16(y[g][i], y[g][4 + i]);
+            const float2 z = __half22float2(*reinterpret_cast<const __half2*>(&two));
+            qf[n][p][g][i] = two;
+            sum[g] += (z.x + z.y) * (i & 1 ? 16.f : 1.f);
+            y[g][i] -= z.x;
+            y[g][4 + i] -= z.y;
+          }
+        sum[g] += __shfl_xor_sync(0xffffffffu, sum[g], 1);
+        sum[g] += __shfl_xor_sync(0xffffffffu, sum[g], 2);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) from[n][g][e] = __shfl_sync(0xffffffffu, sum[g], 4 * (2 * q4 + e)) * -0x1p-21f;
+      }
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        fb[n][e] = __shfl_sync(0xffffffffu, f, 4 * (2 * q4 + e));
+      }
+    }
+    __syncwarp();                              // (the masks)
+
+    float o[G][2][NT][4];                      // dimensions 32 g + 4 r + 2 half (+ 1) of vectors 2 q4, 2 q4 + 1 (+ 8)
+    float m[NT][2], l[NT][2];                  // the vectors' maxima so far, and this lane's slots' share of their sums
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        m[n][e] = -INFINITY;
+        l[n][e] = 0.f;
+      }
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[g][h][n][e] = 0.f;
+
+    const int last = min(s.keys, s.c1 * kKeys);
+#pragma unroll 1
+    for (int slot = s.c0 * kKeys; slot < last; slot += kStretch, ++it) {
+      // ---- scores of slots 16 tile + r, + 8 and vectors 2 q4, + 1
+      if (!__all_sync(0xffffffffu, wait_for(&full[0], it & 1, a.status))) {
+        wait_for(&full[1], it & 1, a.status);
+        return;
+      }
+      const uint32_t* const k_scales = reinterpret_cast<const uint32_t*>(sm + C::CODES);
+      float t[kTiles][NT][4];
+#pragma unroll
+      for (int i = 0; i < kTiles; ++i) {
+        uint32_t w[2][G], sc[2][G / 2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int row = 16 * i + r + 8 * h;
+          if constexpr (G == 4) {
+            const uint4 u = *reinterpret_cast<const uint4*>(sm + row * C::RB + 16 * q4);
+            w[h][0] = u.x; w[h][1] = u.y; w[h][2] = u.z; w[h][3] = u.w;
+            const uint2 z = *reinterpret_cast<const uint2*>(k_scales + row * 2);
+            sc[h][0] = z.x; sc[h][1] = z.y;
+          } else {
+            const uint2 u = *reinterpret_cast<const uint2*>(sm + row * C::RB + 8 * q4);
+            w[h][0] = u.x; w[h][1] = u.y;
+            sc[h][0] = k_scales[row];
+          }
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) t[i][n][e] = 0.f;
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+          const uint32_t x0 = both(w[0][g / 2], w[0][G / 2 + g / 2], g), x1 = both(w[1][g / 2], w[1][G / 2 + g / 2], g);
+          const uint32_t y0 = x0 >> 8, y1 = x1 >> 8;
+          const uint32_t lo[4] = {(x0 & 0x000f000fu) ^ 0x00080008u, (x1 & 0x000f000fu) ^ 0x00080008u,
+                                  (x0 & 0x00f000f0u) ^ 0x00800080u, (x1 & 0x00f000f0u) ^ 0x00800080u};
+          const uint32_t hi[4] = {(y0 & 0x000f000fu) ^ 0x00080008u, (y1 & 0x000f000fu) ^ 0x00080008u,
+                                  (y0 & 0x00f000f0u) ^ 0x00800080u, (y1 & 0x00f000f0u) ^ 0x00800080u};
+          const float s0 = bf16_at(sc[0][g / 2], g & 1), s1 = bf16_at(sc[1][g / 2], g & 1);
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            float d[4] = {from[n][g][0], from[n][g][1], from[n][g][0], from[n][g][1]};
+#pragma unroll
+            for (int p = QP - 1; p >= 0; --p) {
+              mma_f16(d, lo, qf[n][p][g][0], qf[n][p][g][1]);
+              mma_f16(d, hi, qf[n][p][g][2], qf[n][p][g][3]);
+            }
+            t[i][n][0] = fmaf(d[0], s0, t[i][n][0]);
+            t[i][n][1] = fmaf(d[1], s0, t[i][n][1]);
+            t[i][n][2] = fmaf(d[2], s1, t[i][n][2]);
+            t[i][n][3] = fmaf(d[3], s1, t[i][n][3]);
+          }
+        }
+      }
+      // rows whose scales are not finite (a lane looks at two of K's; of V's below), as bits
+      auto not_finite = [&](const uint8_t* scales, int row) {
+        const uint32_t* const z = reinterpret_cast<const uint32_t*>(scales) + row * (G / 2);
+        return i4_not_finite(make_uint2(z[0], G == 4 ? z[G / 4] : 0u), G);
+      };
+      const uint32_t kb0 = __ballot_sync(0xffffffffu, not_finite(sm + C::CODES, lane));
+      const uint32_t kb1 = __ballot_sync(0xffffffffu, not_finite(sm + C::CODES, lane + 32));
+      // ---- the next K
+      const Stretch now = x;
+      const bool more = slot + kStretch < last, beyond = !more && unit < end && next.keys > 0;
+      if (more || beyond) {
+        x = locate(more ? s : next, more ? slot + kStretch : next.c0 * kKeys);
+        load(more ? s : next, x, 0);           // (every lane has read this one: the ballots)
+      }
+      if (!__all_sync(0xffffffffu, wait_for(&full[1], it & 1, a.status))) {
+        if (more || beyond) wait_for(&full[0], (it + 1) & 1, a.status);
+        return;
+      }
+      const uint8_t* const v_scales = sm + C::V_OFF + C::CODES;
+      const uint32_t vb0 = __ballot_sync(0xffffffffu, not_finite(v_scales, lane));
+      const uint32_t vb1 = __ballot_sync(0xffffffffu, not_finite(v_scales, lane + 32));
+      // slots that there are, as bits
+      uint64_t valid = now.n >= 64 ? ~0ull : (1ull << now.n) - 1;
+      const uint32_t pieces = shift == 6 ? 1u : shift == 5 ? 3u : 15u;
+      if (now.live != pieces)
+#pragma unroll 1
+        for (int i = 0; i < kStretch >> shift; ++i)
+          if (!(now.live >> i & 1)) valid &= ~((shift == 6 ? ~0ull : (1ull << rows) - 1) << (i << shift));
+      // Code of its own for stretches with slots of the tree, past the item's, without a page or with a row that is not
+      // finite: as one, every score has selects.
+      const bool masked = valid != ~0ull || slot + kStretch > s.len || (kb0 | kb1 | vb0 | vb1) != 0;
+      const uint64_t v_bad = (uint64_t)vb1 << 32 | vb0, k_bad = (uint64_t)kb1 << 32 | kb0;
+      // ---- maxima, probabilities, sums
+      auto softmax = [&](auto general) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          uint64_t seen[2] = {~0ull, ~0ull};
+          if constexpr (general) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const int v = 8 * n + 2 * q4 + e;
+              const int first = slot - s.len;  // the tree's node in the first slot
+              const uint32_t* const w = s_mask + v * (kWords + 1);
+              uint64_t z = 0;
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                const int f = first + 32 * h;
+                uint32_t y;
+                if (f <= -32) y = ~0u;
+                else if (f < 0) y = ((1u << -f) - 1) | w[0] << -f;
+                else if (f >= 32 * kWords) y = 0u;
+                else y = __funnelshift_r(w[f >> 5], w[(f >> 5) + 1], f & 31);
+                z |= (uint64_t)y << (32 * h);
+              }
+              seen[e] = v < s.nq ? z & valid : 0ull;
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              t[i][n][e] *= fa;
+              if constexpr (general)
+                if (k_bad >> (16 * i + r + 8 * (e >> 1)) & 1) t[i][n][e] = __uint_as_float(0x7fc00000u);
+            }
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            float top = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+              for (int h = 0; h < 2; ++h)
+                if (!general || seen[e] >> (16 * i + r + 8 * h) & 1) top = fmaxf(top, t[i][n][2 * h + e]);
+#pragma unroll
+            for (int d = 4; d < 32; d *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+            // (a vector past the block's has the factor 0)
+            const float mq = top == -INFINITY ? top : top * fb[n][e];
+            const float mn = fmaxf(m[n][e], mq);
+            const float alpha = m[n][e] == -INFINITY ? 0.f : ex2(m[n][e] - mn);
+            m[n][e] = mn;
+            const float off = mn == -INFINITY ? 0.f : mn;
+            float sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                float y = ex2(fmaf(t[i][n][2 * h + e], fb[n][e], -off));
+                if constexpr (general) {
+                  const int at = 16 * i + r + 8 * h;
+                  if (!(seen[e] >> at & 1)) y = 0.f;
+                  sum += y;
+                  if (y != 0.f && v_bad >> at & 1) y = __uint_as_float(0x7fc00000u);
+                } else {
+                  sum += y;
+                }
+                s_p[(8 * n + 2 * q4 + e) * kPitch + 16 * i + r + 8 * h] = y;
+              }
+            l[n][e] = fmaf(l[n][e], alpha, sum);
+#pragma unroll
+            for (int g = 0; g < G; ++g)
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                o[g][h][n][e] *= alpha;
+                o[g][h][n][2 + e] *= alpha;
+              }
+          }
+        }
+      };
+      if (masked) softmax(std::true_type());
+      else softmax(std::false_type());
+      __syncwarp();
+      // ---- O^T += V^T P^T: slots 16 tile + 4 q4 .. + 3 are the MMA's k
+      uint32_t pf[NT][kTiles][PP][2];
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i) {
+          const float4 y = *reinterpret_cast<const float4*>(s_p + (8 * n + r) * kPitch + 16 * i + 4 * q4);
+          float z[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+          for (int p = 0; p < PP; ++p)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const uint32_t two = pack_bf16(z[2 * h], z[2 * h + 1]);
+              pf[n][i][p][h] = two;
+              if (p + 1 < PP) {
+                z[2 * h] -= __uint_as_float(two << 16);
+                z[2 * h + 1] -= __uint_as_float(two & 0xffff0000u);
+              }
+            }
+        }
+      const uint64_t gone = masked ? ~valid | v_bad : 0ull;   // rows of V that count as zeros
+      constexpr int AT_ONCE = NT == 1 && G > 2 ? 2 : NT == 1 ? 2 : 1;   // groups
+#pragma unroll
+      for (int g0 = 0; g0 < G; g0 += AT_ONCE) {
+        float d[AT_ONCE][2][NT][4];
+#pragma unroll
+        for (int g = 0; g < AT_ONCE; ++g)
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) d[g][h][n][e] = 0.f;
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i) {
+          const int row = 16 * i + 4 * q4;
+          uint32_t w[4], sc[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            w[e] = *reinterpret_cast<const uint32_t*>(sm + C::V_OFF + (row + e) * C::RB + r * (C::RB / 8) + g0 / 2 * 4);
+            sc[e] = reinterpret_cast<const uint32_t*>(v_scales)[(row + e) * (G / 2) + g0 / 2];
+            if (masked && gone >> (row + e) & 1) sc[e] = 0u;
+          }
+#pragma unroll
+          for (int g = 0; g < AT_ONCE; ++g) {
+            const uint32_t x01 = both(w[0], w[1], g0 + g), x23 = both(w[2], w[3], g0 + g);
+            const uint32_t s01 = both(sc[0], sc[1], g0 + g), s23 = both(sc[2], sc[3], g0 + g);
+            const uint32_t a8 = mul_bf16x2(s01, 0x3e003e00u), am = mul_bf16x2(s01, 0xc1c0c1c0u);   // 1 / 8, -24
+            const uint32_t b8 = mul_bf16x2(s23, 0x3e003e00u), bm = mul_bf16x2(s23, 0xc1c0c1c0u);
+            const uint32_t va[2][4] = {{value_bf16<0>(x01, a8, am), value_bf16<1>(x01, a8, am), value_bf16<0>(x23, b8, bm),
+                                        value_bf16<1>(x23, b8, bm)},
+                                       {value_bf16<2>(x01, a8, am), value_bf16<3>(x01, a8, am), value_bf16<2>(x23, b8, bm),
+                                        value_bf16<3>(x23, b8, bm)}};
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+              for (int p = PP - 1; p >= 0; --p)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) mma_bf16(d[g][h][n], va[h], pf[n][i][p][0], pf[n][i][p][1]);
+          }
+        }
+#pragma unroll
+        for (int g = 0; g < AT_ONCE; ++g)
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) o[g0 + g][h][n][e] += d[g][h][n][e];
+      }
+      __syncwarp();                            // (V and P are read)
+      if (more || beyond) load(more ? s : next, x, 1);
+      loaded = beyond;
+    }
+    // ---- the item's (or its part's) sums
+    const bool whole = s.c0 == 0 && s.c1 == s.units;
+    const size_t part = (size_t)blockIdx.x * 2 + (s.c0 == 0);
+    const int live = min(NQ, a.T * a.G - s.qb * NQ);
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int v = 8 * n + 2 * q4 + e;
+        float sum = l[n][e];
+#pragma unroll
+        for (int d = 4; d < 32; d *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+        if (v >= s.nq) sum = 0.f;              // (a vector past the nodes: zeros)
+        float top = sum == 0.f ? -INFINITY : m[n][e] == -INFINITY ? 0.f : m[n][e];   // (NaN scores: no maximum)
+        const float inv = sum == 0.f ? 0.f : whole ? 1.f / sum : 1.f;
+        if (v < live) {
+          const Vec w = vector_of(a, s.h, s.qb, v);
+#pragma unroll
+          for (int g = 0; g < G; ++g) {
+            const int d = g * kGroup + 4 * r;
+            float y[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[i] = inv == 0.f ? 0.f : o[g][i / 2][n][i % 2 * 2 + e] * inv;
+            if (whole) {
+#pragma unroll
+              for (int i = 0; i < 4; ++i) store_out<T>(a, s.b, w, d + i, y[i]);
+            } else {
+              *reinterpret_cast<float4*>(a.part_o + (part * NQ + v) * HD + d) = make_float4(y[0], y[1], y[2], y[3]);
+            }
+          }
+          if (r == 0) {
+            if (whole) {
+              store_lse(a, s.b, w, top, sum);
+            } else {
+              a.part_ml[(part * 2) * NQ + v] = top;
+              a.part_ml[(part * 2 + 1) * NQ + v] = sum;
+            }
+          }
+        }
+      }
+  }
+}
+
+template <int HD, int NQ, bool F32>
+cudaError_t launch(const TreeArgs& a, cudaStream_t s) {
+  using C = Cfg<HD, NQ, F32>;
+  const auto k = k_tree_i4<HD, NQ, F32>;
+  static OncePerDevice once;
+  if (const cudaError_t e = allow_shared(once, k, C::smem(CDSL_TREE_MAX_BATCH))) return e;
+  return launch_pdl(k, dim3(a.blocks), dim3(32), C::smem(a.c.batch), s, a);
+}
+
+template <typename F>
+auto by_shape(const Cache& c, int NQ, bool f32, F&& f) {   // f(Cfg's parameters as constants)
+  using std::bool_constant;
+  using std::integral_constant;
+  auto g = [&](auto hd, auto nq) { return f32 ? f(hd, nq, bool_constant<true>()) : f(hd, nq, bool_constant<false>()); };
+  auto h = [&](auto hd) { return NQ == 8 ? g(hd, integral_constant<int, 8>()) : f(hd, integral_constant<int, 16>(), bool_constant<false>()); };
+  return c.hd == 128 ? h(integral_constant<int, 128>()) : h(integral_constant<int, 64>());
+}
+
+}  // namespace
+
+int i4_blocks_per_sm(const Cache& c, int NQ, bool f32) {
+  return by_shape(c, NQ, f32, [](auto hd, auto nq, auto f) { return Cfg<hd(), nq(), f()>::WARPS; });
+}
+
+cudaError_t launch_tree_i4(const TreeArgs& a, cudaStream_t s) {
+  return by_shape(a.c, a.NQ, a.dtype == CDSL_DTYPE_F32, [&](auto hd, auto nq, auto f) { return launch<hd(), nq(), f()>(a, s); });
+}
+
+}  // namespace tree
+}  // namespace cdsl
