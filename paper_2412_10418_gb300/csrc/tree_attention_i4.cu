@@ -58,15 +58,18 @@ __device__ __forceinline__ uint32_t prmt(uint32_t a, uint32_t b, uint32_t sel) {
 // The pieces (16 bits, four codes) of group g (even: the low one) of two words.
 __device__ __forceinline__ uint32_t both(uint32_t a, uint32_t b, int g) { return prmt(a, b, g & 1 ? 0x7632 : 0x5410); }
 
-__device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+// d = a b + (c0, c1, c2, c3) (d itself would have to be set first)
+__device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, float c0, float c1,
+                                        float c2, float c3) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %11, %12, %13};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
 }
-__device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+__device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, float c0, float c1,
+                                         float c2, float c3) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %11, %12, %13};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
 }
 __device__ __forceinline__ uint32_t fma_bf16x2(uint32_t a, uint32_t b, uint32_t c) {
   uint32_t d;
@@ -274,10 +277,6 @@ __global__ void __launch_bounds__(32, Cfg<HD, NQ, F32>::WARPS) k_tree_i4(TreeArg
           }
         }
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) t[i][n][e] = 0.f;
-#pragma unroll
         for (int g = 0; g < G; ++g) {
           const uint32_t x0 = both(w[0][g / 2], w[0][G / 2 + g / 2], g), x1 = both(w[1][g / 2], w[1][G / 2 + g / 2], g);
           const uint32_t y0 = x0 >> 8, y1 = x1 >> 8;
@@ -288,40 +287,52 @@ __global__ void __launch_bounds__(32, Cfg<HD, NQ, F32>::WARPS) k_tree_i4(TreeArg
           const float s0 = bf16_at(sc[0][g / 2], g & 1), s1 = bf16_at(sc[1][g / 2], g & 1);
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
-            float d[4] = {from[n][g][0], from[n][g][1], from[n][g][0], from[n][g][1]};
+            float d[4];
+            mma_f16(d, lo, qf[n][QP - 1][g][0], qf[n][QP - 1][g][1], from[n][g][0], from[n][g][1], from[n][g][0], from[n][g][1]);
+            mma_f16(d, hi, qf[n][QP - 1][g][2], qf[n][QP - 1][g][3], d[0], d[1], d[2], d[3]);
 #pragma unroll
-            for (int p = QP - 1; p >= 0; --p) {
-              mma_f16(d, lo, qf[n][p][g][0], qf[n][p][g][1]);
-              mma_f16(d, hi, qf[n][p][g][2], qf[n][p][g][3]);
+            for (int p = QP - 2; p >= 0; --p) {
+              mma_f16(d, lo, qf[n][p][g][0], qf[n][p][g][1], d[0], d[1], d[2], d[3]);
+              mma_f16(d, hi, qf[n][p][g][2], qf[n][p][g][3], d[0], d[1], d[2], d[3]);
             }
-            t[i][n][0] = fmaf(d[0], s0, t[i][n][0]);
-            t[i][n][1] = fmaf(d[1], s0, t[i][n][1]);
-            t[i][n][2] = fmaf(d[2], s1, t[i][n][2]);
-            t[i][n][3] = fmaf(d[3], s1, t[i][n][3]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              t[i][n][e] = g == 0 ? d[e] * (e < 2 ? s0 : s1) : fmaf(d[e], e < 2 ? s0 : s1, t[i][n][e]);
           }
         }
       }
-      // rows whose scales are not finite (a lane looks at two of K's; of V's below), as bits
-      auto not_finite = [&](const uint8_t* scales, int row) {
-        const uint32_t* const z = reinterpret_cast<const uint32_t*>(scales) + row * (G / 2);
-        return i4_not_finite(make_uint2(z[0], G == 4 ? z[G / 4] : 0u), G);
+      // Is a scale of the lane's rows, lane and lane + 32, not finite? (Bits 7 .. 14 of one all set: 0x80 carries into bit 15.)
+      auto not_finite = [&](const uint8_t* scales) {
+        uint32_t any = 0;
+#pragma unroll
+        for (int i = 0; i < kStretch * C::SB / 4; i += 32)
+          any |= (reinterpret_cast<const uint32_t*>(scales)[i + lane] & 0x7f807f80u) + 0x00800080u;
+        return (any & 0x80008000u) != 0;
       };
-      const uint32_t kb0 = __ballot_sync(0xffffffffu, not_finite(sm + C::CODES, lane));
-      const uint32_t kb1 = __ballot_sync(0xffffffffu, not_finite(sm + C::CODES, lane + 32));
+      const auto rows_not_finite = [&](const uint8_t* scales) {   // as bits
+        uint64_t bits = 0;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const uint32_t* const z = reinterpret_cast<const uint32_t*>(scales) + (lane + 32 * h) * (G / 2);
+          bits |= (uint64_t)__ballot_sync(0xffffffffu, i4_not_finite(make_uint2(z[0], G == 4 ? z[G / 4] : 0u), G)) << (32 * h);
+        }
+        return bits;
+      };
+      uint64_t k_bad = 0, v_bad = 0;
+      if (__any_sync(0xffffffffu, not_finite(sm + C::CODES))) k_bad = rows_not_finite(sm + C::CODES);   // (K has been read)
       // ---- the next K
       const Stretch now = x;
       const bool more = slot + kStretch < last, beyond = !more && unit < end && next.keys > 0;
       if (more || beyond) {
         x = locate(more ? s : next, more ? slot + kStretch : next.c0 * kKeys);
-        load(more ? s : next, x, 0);           // (every lane has read this one: the ballots)
+        load(more ? s : next, x, 0);
       }
       if (!__all_sync(0xffffffffu, wait_for(&full[1], it & 1, a.status))) {
         if (more || beyond) wait_for(&full[0], (it + 1) & 1, a.status);
         return;
       }
-      const uint8_t* const v_scales = sm + C::V_OFF + C::CODES;
-      const uint32_t vb0 = __ballot_sync(0xffffffffu, not_finite(v_scales, lane));
-      const uint32_t vb1 = __ballot_sync(0xffffffffu, not_finite(v_scales, lane + 32));
+      uint8_t* const v_scales = sm + C::V_OFF + C::CODES;
+      if (__any_sync(0xffffffffu, not_finite(v_scales))) v_bad = rows_not_finite(v_scales);
       // slots that there are, as bits
       uint64_t valid = now.n >= 64 ? ~0ull : (1ull << now.n) - 1;
       const uint32_t pieces = shift == 6 ? 1u : shift == 5 ? 3u : 15u;
@@ -331,8 +342,7 @@ __global__ void __launch_bounds__(32, Cfg<HD, NQ, F32>::WARPS) k_tree_i4(TreeArg
           if (!(now.live >> i & 1)) valid &= ~((shift == 6 ? ~0ull : (1ull << rows) - 1) << (i << shift));
       // Code of its own for stretches with slots of the tree, past the item's, without a page or with a row that is not
       // finite: as one, every score has selects.
-      const bool masked = valid != ~0ull || slot + kStretch > s.len || (kb0 | kb1 | vb0 | vb1) != 0;
-      const uint64_t v_bad = (uint64_t)vb1 << 32 | vb0, k_bad = (uint64_t)kb1 << 32 | kb0;
+      const bool masked = valid != ~0ull || slot + kStretch > s.len || (k_bad | v_bad) != 0;
       // ---- maxima, probabilities, sums
       auto softmax = [&](auto general) {
 #pragma unroll
@@ -409,8 +419,18 @@ __global__ void __launch_bounds__(32, Cfg<HD, NQ, F32>::WARPS) k_tree_i4(TreeArg
           }
         }
       };
-      if (masked) softmax(std::true_type());
-      else softmax(std::false_type());
+      if (masked) {
+        softmax(std::true_type());
+        const uint64_t gone = ~valid | v_bad;  // nothing of these rows of V may reach the sums
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          if (gone >> (lane + 32 * h) & 1)
+#pragma unroll
+            for (int i = 0; i < G / 2; ++i) reinterpret_cast<uint32_t*>(v_scales)[(lane + 32 * h) * (G / 2) + i] = 0u;
+        tc::fence_proxy_async();               // (before the copy that follows them)
+      } else {
+        softmax(std::false_type());
+      }
       __syncwarp();
       // ---- O^T += V^T P^T: slots 16 tile + 4 q4 .. + 3 are the MMA's k
       uint32_t pf[NT][kTiles][PP][2];
@@ -432,19 +452,10 @@ __global__ void __launch_bounds__(32, Cfg<HD, NQ, F32>::WARPS) k_tree_i4(TreeArg
               }
             }
         }
-      const uint64_t gone = masked ? ~valid | v_bad : 0ull;   // rows of V that count as zeros
       constexpr int AT_ONCE = NT == 1 && G > 2 ? 2 : NT == 1 ? 2 : 1;   // groups
 #pragma unroll
       for (int g0 = 0; g0 < G; g0 += AT_ONCE) {
         float d[AT_ONCE][2][NT][4];
-#pragma unroll
-        for (int g = 0; g < AT_ONCE; ++g)
-#pragma unroll
-          for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-              for (int e = 0; e < 4; ++e) d[g][h][n][e] = 0.f;
 #pragma unroll
         for (int i = 0; i < kTiles; ++i) {
           const int row = 16 * i + 4 * q4;
@@ -453,7 +464,6 @@ __global__ void __launch_bounds__(32, Cfg<HD, NQ, F32>::WARPS) k_tree_i4(TreeArg
           for (int e = 0; e < 4; ++e) {
             w[e] = *reinterpret_cast<const uint32_t*>(sm + C::V_OFF + (row + e) * C::RB + r * (C::RB / 8) + g0 / 2 * 4);
             sc[e] = reinterpret_cast<const uint32_t*>(v_scales)[(row + e) * (G / 2) + g0 / 2];
-            if (masked && gone >> (row + e) & 1) sc[e] = 0u;
           }
 #pragma unroll
           for (int g = 0; g < AT_ONCE; ++g) {
@@ -470,7 +480,11 @@ __global__ void __launch_bounds__(32, Cfg<HD, NQ, F32>::WARPS) k_tree_i4(TreeArg
 #pragma unroll
               for (int p = PP - 1; p >= 0; --p)
 #pragma unroll
-                for (int h = 0; h < 2; ++h) mma_bf16(d[g][h][n], va[h], pf[n][i][p][0], pf[n][i][p][1]);
+                for (int h = 0; h < 2; ++h) {
+                  float (&z)[4] = d[g][h][n];
+                  if (i == 0 && p == PP - 1) mma_bf16(z, va[h], pf[n][i][p][0], pf[n][i][p][1], 0.f, 0.f, 0.f, 0.f);
+                  else mma_bf16(z, va[h], pf[n][i][p][0], pf[n][i][p][1], z[0], z[1], z[2], z[3]);
+                }
           }
         }
 #pragma unroll
