@@ -9,15 +9,18 @@
 //
 //   S^T = K Q^T    K's operand is a code plus 8 as the bits of an fp16 number below 2^-14, one instruction for two of
 //                  them: (word & 0x000f000f) ^ 0x00080008 = (code + 8) 2^-24, the next four bits 2^-20. What the 8
-//                  adds, -8 times the sum of the group's q, is what the accumulators start from. Groups are summed
+//                  adds, -8 times the sum of the group's q, is what the accumulators start from (float32 queries: the
+//                  codes themselves, an fma more, as those sums are larger and so are their roundings). Groups are summed
 //                  apart and multiplied by their scales in fp32. q is held in fp16 planes under a power of two that takes the
 //                  row's largest to 2^14 or more: exact down to 2^-31 of it from bf16 (one plane) or float32 (three).
 //   O^T = V^T P^T  V's operand is the value in bf16, exact (a code's 3 bits by a scale's 4): bits 3 .. 6 of
 //                  128 + 8 (code + 8), then one fma of two by (scale / 8, -24 scale). P is the sum of two bf16
 //                  planes (2^-16 of itself; three for float32 queries, 2^-24): fp32's range, whatever lies next to what.
 //
-// Each stretch of 64 slots starts its sums O^T at zero and is added to fp32 registers, so that no sum is a long chain of a tensor
-// core's truncating additions. A warp has a run of its own and no barrier but its own; its K and V come by bulk copies, the next
+// Scores go through shared memory once, to where a lane has 16 slots of one vector: maxima take two exchanges there, and
+// probabilities are P's fragments as they are. O^T is one chain over kChain stretches of 64 slots and is then added to fp32
+// sums (in the workspace: few passes are as long), as a tensor core's additions truncate; its reference is the running
+// maximum, and few stretches raise it. (float32 queries: every product is added up in fp32.) A warp has a run of its own and no barrier but its own; its K and V come by bulk copies, the next
 // stretch's K while this one's softmax and P V run, and V beside the next scores.
 //
 // Waits are bounded by a number of tries (wait_for): on expiry CDSL_ETIMEOUT is latched and the warp exits once its copies
@@ -38,7 +41,8 @@ namespace {
 
 constexpr int kStretch = 64;                   // slots at a time
 constexpr int kTiles = kStretch / 16;
-constexpr int kPitch = kStretch + 4;           // floats of a vector's probabilities
+constexpr int kPitch = kStretch + 4;           // floats of a vector's scores
+constexpr int kChain = 64;                     // stretches of O^T's chain (512 products: 2^-15 of it at worst)
 
 template <int HD, int NQ, bool F32>
 struct Cfg {
@@ -48,9 +52,11 @@ struct Cfg {
   static constexpr uint32_t CODES = kStretch * RB, SCALES = kStretch * SB;
   static constexpr uint32_t V_OFF = CODES + SCALES;
   static constexpr uint32_t P_OFF = 2 * V_OFF;
-  static constexpr uint32_t MASK_OFF = P_OFF + NQ * kPitch * 4;
+  // scores, then P's fragments: PP planes of two words for each tile and lane
+  static constexpr uint32_t S_BYTES = NQ * kPitch * 4, F_BYTES = NT * kTiles * 32 * PP * 8;
+  static constexpr uint32_t MASK_OFF = P_OFF + (S_BYTES > F_BYTES ? S_BYTES : F_BYTES);
   static constexpr uint32_t PLAN_OFF = MASK_OFF + NQ * (kWords + 1) * 4;
-  static constexpr int WARPS = F32 || NQ == 16 ? 8 : HD == 128 ? 12 : 16;   // of an SM, by registers
+  static constexpr int WARPS = F32 || NQ == 16 ? 12 : 16;          // of an SM, by registers
   static constexpr size_t smem(int batch) { return PLAN_OFF + plan_bytes(batch); }
 };
 
@@ -90,19 +96,30 @@ __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
   const __half2 h = __floats2half2_rn(a, b);
   return *reinterpret_cast<const uint32_t*>(&h);
 }
+// (x & mask) ^ c in one instruction, of which only one operand may be a constant: masks come from registers.
+__device__ __forceinline__ uint32_t and_xor(uint32_t x, uint32_t mask, uint32_t c) {
+  uint32_t d;
+  asm("lop3.b32 %0, %1, %2, %3, 0x6a;" : "=r"(d) : "r"(x), "r"(mask), "r"(c));
+  return d;
+}
+// The codes in bits BIT .. BIT + 3 of both halves of x (mask: those) as fp16: themselves, or (code + 8) 2^(BIT - 24).
+template <bool EXACT, int BIT>
+__device__ __forceinline__ uint32_t code_f16(uint32_t x, uint32_t mask) {
+  constexpr uint32_t eights = 0x00080008u << BIT;
+  if constexpr (!EXACT) return and_xor(x, mask, eights);
+  uint32_t d;                                  // of 1024 + (code + 8) 2^BIT
+  asm("fma.rn.f16x2 %0, %1, %2, %3;"
+      : "=r"(d)
+      : "r"(and_xor(x, mask, 0x64006400u | eights)), "r"(BIT ? 0x2c002c00u : 0x3c003c00u),
+        "r"(BIT ? 0xd480d480u : 0xe408e408u));   // times 1 / 16, less 72; less 1032
+  return d;
+}
 // Code i of both pieces in x, times their scales: s8 = (scale / 8) and m24 = (-24 scale) of the two.
 template <int I>
-__device__ __forceinline__ uint32_t value_bf16(uint32_t x, uint32_t s8, uint32_t m24) {
+__device__ __forceinline__ uint32_t value_bf16(uint32_t x, uint32_t mask, uint32_t s8, uint32_t m24) {
   const uint32_t t = I == 0 ? x << 3 : x >> (4 * I - 3);
-  return fma_bf16x2((t & 0x00780078u) ^ 0x43404340u, s8, m24);
+  return fma_bf16x2(and_xor(t, mask, 0x43404340u), s8, m24);
 }
-
-// A stretch of a segment: where it is, and the lane's page of it (pieces of a page or of 64 slots; lanes past them: -1).
-struct Stretch {
-  int slot, n;                                 // first slot, slots that there are
-  int page;
-  uint32_t live;                               // pieces that have a page
-};
 
 template <int HD, int NQ, bool F32>
 __global__ void __launch_bounds__(32, Cfg<HD, NQ, F32>::WARPS) k_tree_i4(TreeArgs a) {
@@ -111,6 +128,7 @@ __global__ void __launch_bounds__(32, Cfg<HD, NQ, F32>::WARPS) k_tree_i4(TreeArg
   constexpr int G = C::G, NT = C::NT, QP = C::QP, PP = C::PP;
   extern __shared__ __align__(128) uint8_t sm[];
   __shared__ __align__(8) uint64_t full[2];    // K, V
+  __shared__ uint32_t s_masks[4];
   __shared__ Segment s_seg[2];                 // this segment and the next (registers are dear)
   float* const s_p = reinterpret_cast<float*>(sm + C::P_OFF);
   uint32_t* const s_mask = reinterpret_cast<uint32_t*>(sm + C::MASK_OFF);
@@ -129,25 +147,45 @@ __global__ void __launch_bounds__(32, Cfg<HD, NQ, F32>::WARPS) k_tree_i4(TreeArg
   const int total = s_first[c.batch], runs = runs_of(a, total);
   if ((int)blockIdx.x >= runs) return;
   const int end = run_begin(blockIdx.x + 1, total, runs);
-  const float fa = a.scale * 0x1p10f;          // of all scores: 2^24 of the codes, 2^-14 of the queries
+  const float fa = a.scale * (F32 ? 0x1p-14f : 0x1p10f);   // of all scores: 2^-14 of the queries, 2^24 of the codes
+  // (through shared memory, or the compiler knows them as constants and takes two instructions)
+  if (lane < 3) s_masks[lane] = lane == 0 ? 0x000f000fu : lane == 1 ? 0x00f000f0u : 0x00780078u;
+  __syncwarp();
+  const volatile uint32_t* const masks = s_masks;
+  const uint32_t k0 = masks[0], k4 = masks[1], kv = masks[2];
   const int P = 1 << c.page_shift, rows = min(P, kStretch), shift = min(c.page_shift, 6);
 
-  // a stretch's pages, and its copies; K's and V's are the same rows of the page's two halves
-  auto locate = [&](const Segment& s, int slot) {
-    Stretch x = {slot, min(kStretch, min(s.keys, s.c1 * kKeys) - slot), -1, 0u};
-    const int mine = slot + lane * rows;
-    if (lane < kStretch / rows && lane * rows < x.n) {
-      x.page = page_of(c, s.b, mine);
-      if (x.page < 0) set_status(a.status, CDSL_ERANGE);
+  // The copies of a stretch: its pieces (of a page, or of 64 slots) by a lane each. Pages come 32 pieces at a time, or each
+  // copy would wait for its page first.
+  const int per = kStretch >> shift;           // pieces of a stretch
+  int pages = -1, window = 0;                  // this lane's piece of the window, and the window's first slot
+  struct Stretch {
+    int page;
+    uint32_t live;                             // pieces that have a page
+  };
+  auto look = [&](const Segment& s, int slot) {
+    window = slot;
+    const int mine = slot + (lane << shift);
+    pages = -1;
+    if (mine < min(s.keys, s.c1 * kKeys)) {
+      pages = page_of(c, s.b, mine);
+      if (pages < 0) set_status(a.status, CDSL_ERANGE);
     }
+  };
+  auto locate = [&](const Segment& s, int slot) {
+    if ((slot - window) >> shift >= 32) look(s, slot);
+    Stretch x;
+    x.page = __shfl_sync(0xffffffffu, pages, ((slot - window) >> shift) + lane & 31);
+    if (lane >= per) x.page = -1;
     x.live = __ballot_sync(0xffffffffu, x.page >= 0);
     return x;
   };
-  auto load = [&](const Segment& s, const Stretch& x, int kv) {
+  const size_t page_rows = (size_t)2 * c.kvh << c.page_shift, layer_row = row_of(c, a.layer, 0, 0, 0, 0);
+  auto load = [&](const Segment& s, int slot, const Stretch& x, int kv) {
     if (lane == 0) tc::mbar_expect_tx(&full[kv], __popc(x.live) * rows * (C::RB + C::SB));
     __syncwarp();
     if (x.page >= 0) {
-      const size_t row = row_of(c, a.layer, x.page, kv, s.h, (x.slot + lane * rows) & (P - 1));
+      const size_t row = layer_row + x.page * page_rows + ((kv * c.kvh + s.h) << c.page_shift) + ((slot + (lane << shift)) & (P - 1));
       uint8_t* const to = sm + kv * C::V_OFF;
       tc::bulk_load(to + lane * rows * C::RB, c.pool + row * C::RB, rows * C::RB, &full[kv]);
       tc::bulk_load(to + C::CODES + lane * rows * C::SB, c.scale + row * C::SB, rows * C::SB, &full[kv]);
@@ -165,9 +203,10 @@ __global__ void __launch_bounds__(32, Cfg<HD, NQ, F32>::WARPS) k_tree_i4(TreeArg
     const Segment& s = s_seg[turn];
     const Segment& next = s_seg[turn ^ 1];
     if (!loaded && s.keys > 0) {
+      look(s, s.c0 * kKeys);
       x = locate(s, s.c0 * kKeys);
-      load(s, x, 0);
-      load(s, x, 1);
+      load(s, s.c0 * kKeys, x, 0);
+      load(s, s.c0 * kKeys, x, 1);
     }
     loaded = false;
     unit += s.c1 - s.c0;
@@ -180,7 +219,7 @@ __global__ void __launch_bounds__(32, Cfg<HD, NQ, F32>::WARPS) k_tree_i4(TreeArg
     // ---- queries: this lane has dimensions 32 g + 8 q4 .. of vectors r (+ 8) as the MMA's columns
     uint32_t qf[NT][QP][G][4];                 // of both steps of a group
     float from[NT][G][2];                      // what the accumulators of vectors 2 q4, 2 q4 + 1 (+ 8) start from
-    float fb[NT][2];                           // and their scores' factors
+    float fb[NT];                              // factors of the scores of vectors r (+ 8)
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       const int v = 8 * n + r;
@@ -201,13 +240,12 @@ __global__ void __launch_bounds__(32, Cfg<HD, NQ, F32>::WARPS) k_tree_i4(TreeArg
       const int e2 = max((int)(top >> 23) - 127, -100);          // (a row that is not finite: 128)
       // (to 2^14 .. 2^15: up to twice that could round to infinity)
       const float up = top >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : exp2f((float)(14 - e2));
-      const float f = any ? exp2f((float)e2) : 0.f;
       float sum[G];
 #pragma unroll
       for (int g = 0; g < G; ++g) {
         sum[g] = 0.f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[g][e] *= e & 1 ? up * 0.0625f : up;   // (the second and fourth of four: codes 2^4 higher)
+        for (int e = 0; e < 8; ++e) y[g][e] *= !F32 && e & 1 ? up * 0.0625f : up;   // (the second and fourth of four: codes 2^4 higher)
 #pragma unroll
         for (int p = 0; p < QP; ++p)
 #pragma unroll
@@ -222,45 +260,74 @@ __global__ void __launch_bounds__(32, Cfg<HD, NQ, F32>::WARPS) k_tree_i4(TreeArg
         sum[g] += __shfl_xor_sync(0xffffffffu, sum[g], 1);
         sum[g] += __shfl_xor_sync(0xffffffffu, sum[g], 2);
 #pragma unroll
-        for (int e = 0; e < 2; ++e) from[n][g][e] = __shfl_sync(0xffffffffu, sum[g], 4 * (2 * q4 + e)) * -0x1p-21f;
+        for (int e = 0; e < 2; ++e) from[n][g][e] = F32 ? 0.f : __shfl_sync(0xffffffffu, sum[g], 4 * (2 * q4 + e)) * -0x1p-21f;
       }
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        fb[n][e] = __shfl_sync(0xffffffffu, f, 4 * (2 * q4 + e));
-      }
+      fb[n] = any ? exp2f((float)e2) : 0.f;
     }
     __syncwarp();                              // (the masks)
 
     float o[G][2][NT][4];                      // dimensions 32 g + 4 r + 2 half (+ 1) of vectors 2 q4, 2 q4 + 1 (+ 8)
-    float m[NT][2], l[NT][2];                  // the vectors' maxima so far, and this lane's slots' share of their sums
+    float m[NT], l[NT];                        // of vectors r (+ 8): the maxima so far, and this lane's slots' share of the sums
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
+    for (int n = 0; n < NT; ++n) {
+      m[n] = -INFINITY;
+      l[n] = 0.f;
+    }
+    const auto clear = [&] {
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        m[n][e] = -INFINITY;
-        l[n][e] = 0.f;
+      for (int g = 0; g < G; ++g)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[g][h][n][e] = 0.f;
+    };
+    clear();
+    const size_t part = (size_t)blockIdx.x * 2 + (s.c0 == 0);
+    // The sums behind O^T's chain: in the part's place in the workspace, relative to the maxima m_then. (A whole item's is
+    // free while the run is at it: it ends before the run's last part begins.)
+    bool chained = false;
+    float m_then[NT];
+    const auto add_chain = [&] {               // o += the sums
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        const float f = m_then[n] == -INFINITY ? 0.f : ex2(m_then[n] - m[n]);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const float by = __shfl_sync(0xffffffffu, f, 4 * (2 * q4 + e));
+          const float* const from = a.part_o + (part * NQ + 8 * n + 2 * q4 + e) * HD + 4 * r;
+#pragma unroll
+          for (int g = 0; g < G; ++g) {
+            const float4 y = *reinterpret_cast<const float4*>(from + g * kGroup);
+            o[g][0][n][e] = fmaf(y.x, by, o[g][0][n][e]);
+            o[g][0][n][2 + e] = fmaf(y.y, by, o[g][0][n][2 + e]);
+            o[g][1][n][e] = fmaf(y.z, by, o[g][1][n][e]);
+            o[g][1][n][2 + e] = fmaf(y.w, by, o[g][1][n][2 + e]);
+          }
+        }
       }
+    };
+    const auto put = [&](int n, int e, float by) {   // o to the part's place
+      float* const to = a.part_o + (part * NQ + 8 * n + 2 * q4 + e) * HD + 4 * r;
 #pragma unroll
-    for (int g = 0; g < G; ++g)
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) o[g][h][n][e] = 0.f;
+      for (int g = 0; g < G; ++g)
+        *reinterpret_cast<float4*>(to + g * kGroup) =
+            make_float4(o[g][0][n][e] * by, o[g][0][n][2 + e] * by, o[g][1][n][e] * by, o[g][1][n][2 + e] * by);
+    };
 
     const int last = min(s.keys, s.c1 * kKeys);
 #pragma unroll 1
-    for (int slot = s.c0 * kKeys; slot < last; slot += kStretch, ++it) {
+    for (int slot = s.c0 * kKeys, links = 0; slot < last; slot += kStretch, ++it) {
       // ---- scores of slots 16 tile + r, + 8 and vectors 2 q4, + 1
       if (!__all_sync(0xffffffffu, wait_for(&full[0], it & 1, a.status))) {
         wait_for(&full[1], it & 1, a.status);
         return;
       }
       const uint32_t* const k_scales = reinterpret_cast<const uint32_t*>(sm + C::CODES);
-      float t[kTiles][NT][4];
-#pragma unroll
+#pragma unroll 1
       for (int i = 0; i < kTiles; ++i) {
+        float t[NT][4];
         uint32_t w[2][G], sc[2][G / 2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -280,10 +347,8 @@ __global__ void __launch_bounds__(32, Cfg<HD, NQ, F32>::WARPS) k_tree_i4(TreeArg
         for (int g = 0; g < G; ++g) {
           const uint32_t x0 = both(w[0][g / 2], w[0][G / 2 + g / 2], g), x1 = both(w[1][g / 2], w[1][G / 2 + g / 2], g);
           const uint32_t y0 = x0 >> 8, y1 = x1 >> 8;
-          const uint32_t lo[4] = {(x0 & 0x000f000fu) ^ 0x00080008u, (x1 & 0x000f000fu) ^ 0x00080008u,
-                                  (x0 & 0x00f000f0u) ^ 0x00800080u, (x1 & 0x00f000f0u) ^ 0x00800080u};
-          const uint32_t hi[4] = {(y0 & 0x000f000fu) ^ 0x00080008u, (y1 & 0x000f000fu) ^ 0x00080008u,
-                                  (y0 & 0x00f000f0u) ^ 0x00800080u, (y1 & 0x00f000f0u) ^ 0x00800080u};
+          const uint32_t lo[4] = {code_f16<F32, 0>(x0, k0), code_f16<F32, 0>(x1, k0), code_f16<F32, 4>(x0, k4), code_f16<F32, 4>(x1, k4)};
+          const uint32_t hi[4] = {code_f16<F32, 0>(y0, k0), code_f16<F32, 0>(y1, k0), code_f16<F32, 4>(y0, k4), code_f16<F32, 4>(y1, k4)};
           const float s0 = bf16_at(sc[0][g / 2], g & 1), s1 = bf16_at(sc[1][g / 2], g & 1);
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
@@ -297,126 +362,130 @@ __global__ void __launch_bounds__(32, Cfg<HD, NQ, F32>::WARPS) k_tree_i4(TreeArg
             }
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-              t[i][n][e] = g == 0 ? d[e] * (e < 2 ? s0 : s1) : fmaf(d[e], e < 2 ? s0 : s1, t[i][n][e]);
+              t[n][e] = g == 0 ? d[e] * (e < 2 ? s0 : s1) : fmaf(d[e], e < 2 ? s0 : s1, t[n][e]);
           }
         }
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s_p[(8 * n + 2 * q4 + (e & 1)) * kPitch + 16 * i + r + 8 * (e >> 1)] = t[n][e];
       }
-      // Is a scale of the lane's rows, lane and lane + 32, not finite? (Bits 7 .. 14 of one all set: 0x80 carries into bit 15.)
-      auto not_finite = [&](const uint8_t* scales) {
-        uint32_t any = 0;
-#pragma unroll
-        for (int i = 0; i < kStretch * C::SB / 4; i += 32)
-          any |= (reinterpret_cast<const uint32_t*>(scales)[i + lane] & 0x7f807f80u) + 0x00800080u;
-        return (any & 0x80008000u) != 0;
-      };
-      const auto rows_not_finite = [&](const uint8_t* scales) {   // as bits
-        uint64_t bits = 0;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const uint32_t* const z = reinterpret_cast<const uint32_t*>(scales) + (lane + 32 * h) * (G / 2);
-          bits |= (uint64_t)__ballot_sync(0xffffffffu, i4_not_finite(make_uint2(z[0], G == 4 ? z[G / 4] : 0u), G)) << (32 * h);
-        }
-        return bits;
-      };
-      uint64_t k_bad = 0, v_bad = 0;
-      if (__any_sync(0xffffffffu, not_finite(sm + C::CODES))) k_bad = rows_not_finite(sm + C::CODES);   // (K has been read)
+      __syncwarp();                            // (K has been read; the scores)
       // ---- the next K
-      const Stretch now = x;
+      const uint32_t live_now = x.live;
+      const int there = last - slot;           // slots that there are, if fewer than 64
       const bool more = slot + kStretch < last, beyond = !more && unit < end && next.keys > 0;
+      const Segment& after = more ? s : next;
+      const int to = more ? slot + kStretch : next.c0 * kKeys;
       if (more || beyond) {
-        x = locate(more ? s : next, more ? slot + kStretch : next.c0 * kKeys);
-        load(more ? s : next, x, 0);
+        if (beyond) look(after, to);
+        x = locate(after, to);
+        load(after, to, x, 0);
       }
       if (!__all_sync(0xffffffffu, wait_for(&full[1], it & 1, a.status))) {
         if (more || beyond) wait_for(&full[0], (it + 1) & 1, a.status);
         return;
       }
       uint8_t* const v_scales = sm + C::V_OFF + C::CODES;
-      if (__any_sync(0xffffffffu, not_finite(v_scales))) v_bad = rows_not_finite(v_scales);
+      // rows of V whose scales are not finite, as bits. (Of one that is not, bits 7 .. 14 are all set: 0x80 carries into bit
+      // 15. K's need no look: the scores are NaN.)
+      uint64_t v_bad = 0;
+      uint32_t odd = 0;
+      if (lane < kStretch * C::SB / 16) {
+        const uint4 u = reinterpret_cast<const uint4*>(v_scales)[lane];
+        odd = ((u.x & 0x7f807f80u) + 0x00800080u) | ((u.y & 0x7f807f80u) + 0x00800080u) |
+              ((u.z & 0x7f807f80u) + 0x00800080u) | ((u.w & 0x7f807f80u) + 0x00800080u);
+      }
+      if (__any_sync(0xffffffffu, (odd & 0x80008000u) != 0))
+#pragma unroll 1
+        for (int h = 0; h < 2; ++h) {
+          const uint32_t* const z = reinterpret_cast<const uint32_t*>(v_scales) + (lane + 32 * h) * (G / 2);
+          v_bad |= (uint64_t)__ballot_sync(0xffffffffu, i4_not_finite(make_uint2(z[0], G == 4 ? z[G / 4] : 0u), G)) << (32 * h);
+        }
       // slots that there are, as bits
-      uint64_t valid = now.n >= 64 ? ~0ull : (1ull << now.n) - 1;
+      uint64_t valid = there >= 64 ? ~0ull : (1ull << there) - 1;
       const uint32_t pieces = shift == 6 ? 1u : shift == 5 ? 3u : 15u;
-      if (now.live != pieces)
+      if (live_now != pieces)
 #pragma unroll 1
         for (int i = 0; i < kStretch >> shift; ++i)
-          if (!(now.live >> i & 1)) valid &= ~((shift == 6 ? ~0ull : (1ull << rows) - 1) << (i << shift));
+          if (!(live_now >> i & 1)) valid &= ~((shift == 6 ? ~0ull : (1ull << rows) - 1) << (i << shift));
       // Code of its own for stretches with slots of the tree, past the item's, without a page or with a row that is not
       // finite: as one, every score has selects.
-      const bool masked = valid != ~0ull || slot + kStretch > s.len || (k_bad | v_bad) != 0;
-      // ---- maxima, probabilities, sums
+      const bool masked = valid != ~0ull || slot + kStretch > s.len || v_bad != 0;
+      // ---- maxima, probabilities, sums: slots 16 tile + 4 q4 .. + 3 of vector r (+ 8)
+      uint32_t pf[NT][kTiles][PP][2];
+      bool raised = false;
+      float alpha[NT];
       auto softmax = [&](auto general) {
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-          uint64_t seen[2] = {~0ull, ~0ull};
+          const int v = 8 * n + r;
+          uint64_t seen = ~0ull;
           if constexpr (general) {
+            const uint32_t* const w = s_mask + v * (kWords + 1);
+            seen = 0;
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const int v = 8 * n + 2 * q4 + e;
-              const int first = slot - s.len;  // the tree's node in the first slot
-              const uint32_t* const w = s_mask + v * (kWords + 1);
-              uint64_t z = 0;
-#pragma unroll
-              for (int h = 0; h < 2; ++h) {
-                const int f = first + 32 * h;
-                uint32_t y;
-                if (f <= -32) y = ~0u;
-                else if (f < 0) y = ((1u << -f) - 1) | w[0] << -f;
-                else if (f >= 32 * kWords) y = 0u;
-                else y = __funnelshift_r(w[f >> 5], w[(f >> 5) + 1], f & 31);
-                z |= (uint64_t)y << (32 * h);
-              }
-              seen[e] = v < s.nq ? z & valid : 0ull;
+            for (int h = 0; h < 2; ++h) {
+              const int f = slot - s.len + 32 * h;   // the tree's node in the first slot
+              uint32_t y;
+              if (f <= -32) y = ~0u;
+              else if (f < 0) y = ((1u << -f) - 1) | w[0] << -f;
+              else if (f >= 32 * kWords) y = 0u;
+              else y = __funnelshift_r(w[f >> 5], w[(f >> 5) + 1], f & 31);
+              seen |= (uint64_t)y << (32 * h);
             }
+            seen = v < s.nq ? (seen & valid) >> (4 * q4) : 0ull;
           }
+          float t[kTiles][4], top = -INFINITY;
 #pragma unroll
-          for (int i = 0; i < kTiles; ++i)
+          for (int i = 0; i < kTiles; ++i) {
+            const float4 y = *reinterpret_cast<const float4*>(s_p + v * kPitch + 16 * i + 4 * q4);
+            t[i][0] = y.x; t[i][1] = y.y; t[i][2] = y.z; t[i][3] = y.w;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              t[i][n][e] *= fa;
-              if constexpr (general)
-                if (k_bad >> (16 * i + r + 8 * (e >> 1)) & 1) t[i][n][e] = __uint_as_float(0x7fc00000u);
+              t[i][e] *= fa;
+              if constexpr (general) {
+                if (!(seen >> (16 * i + e) & 1)) continue;
+              }
+              top = fmaxf(top, t[i][e]);
+            }
+          }
+          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+          const float mq = top == -INFINITY ? top : top * fb[n];
+          const float was = m[n], mn = fmaxf(was, mq);
+          alpha[n] = was == mn ? 1.f : was == -INFINITY ? 0.f : ex2(was - mn);
+          raised = raised || was != mn;
+          m[n] = mn;
+          const float off = mn == -INFINITY ? 0.f : mn;
+          float sum = 0.f;
+#pragma unroll
+          for (int i = 0; i < kTiles; ++i) {
+            float y[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              y[e] = ex2(fmaf(t[i][e], fb[n], -off));
+              if constexpr (general) {
+                if (!(seen >> (16 * i + e) & 1)) y[e] = 0.f;
+                sum += y[e];
+                if (y[e] != 0.f && v_bad >> (4 * q4) >> (16 * i + e) & 1) y[e] = __uint_as_float(0x7fc00000u);
+              } else {
+                sum += y[e];
+              }
             }
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            float top = -INFINITY;
-#pragma unroll
-            for (int i = 0; i < kTiles; ++i)
-#pragma unroll
-              for (int h = 0; h < 2; ++h)
-                if (!general || seen[e] >> (16 * i + r + 8 * h) & 1) top = fmaxf(top, t[i][n][2 * h + e]);
-#pragma unroll
-            for (int d = 4; d < 32; d *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-            // (a vector past the block's has the factor 0)
-            const float mq = top == -INFINITY ? top : top * fb[n][e];
-            const float mn = fmaxf(m[n][e], mq);
-            const float alpha = m[n][e] == -INFINITY ? 0.f : ex2(m[n][e] - mn);
-            m[n][e] = mn;
-            const float off = mn == -INFINITY ? 0.f : mn;
-            float sum = 0.f;
-#pragma unroll
-            for (int i = 0; i < kTiles; ++i)
+            for (int p = 0; p < PP; ++p)
 #pragma unroll
               for (int h = 0; h < 2; ++h) {
-                float y = ex2(fmaf(t[i][n][2 * h + e], fb[n][e], -off));
-                if constexpr (general) {
-                  const int at = 16 * i + r + 8 * h;
-                  if (!(seen[e] >> at & 1)) y = 0.f;
-                  sum += y;
-                  if (y != 0.f && v_bad >> at & 1) y = __uint_as_float(0x7fc00000u);
-                } else {
-                  sum += y;
+                const uint32_t two = pack_bf16(y[2 * h], y[2 * h + 1]);
+                pf[n][i][p][h] = two;
+                if (p + 1 < PP) {
+                  y[2 * h] -= __uint_as_float(two << 16);
+                  y[2 * h + 1] -= __uint_as_float(two & 0xffff0000u);
                 }
-                s_p[(8 * n + 2 * q4 + e) * kPitch + 16 * i + r + 8 * h] = y;
-              }
-            l[n][e] = fmaf(l[n][e], alpha, sum);
-#pragma unroll
-            for (int g = 0; g < G; ++g)
-#pragma unroll
-              for (int h = 0; h < 2; ++h) {
-                o[g][h][n][e] *= alpha;
-                o[g][h][n][2 + e] *= alpha;
               }
           }
+          l[n] = fmaf(l[n], alpha[n], sum);
         }
       };
       if (masked) {
@@ -431,115 +500,151 @@ __global__ void __launch_bounds__(32, Cfg<HD, NQ, F32>::WARPS) k_tree_i4(TreeArg
       } else {
         softmax(std::false_type());
       }
-      __syncwarp();
-      // ---- O^T += V^T P^T: slots 16 tile + 4 q4 .. + 3 are the MMA's k
-      uint32_t pf[NT][kTiles][PP][2];
+      if (__any_sync(0xffffffffu, raised)) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const float by = __shfl_sync(0xffffffffu, alpha[n], 4 * (2 * q4 + e));
+#pragma unroll
+            for (int g = 0; g < G; ++g)
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                o[g][h][n][e] *= by;
+                o[g][h][n][2 + e] *= by;
+              }
+          }
+      }
+      __syncwarp();                            // (scores are read, V's scales are as they should be)
+      uint32_t* const s_f = reinterpret_cast<uint32_t*>(s_p) + lane * (2 * PP);   // (of this lane alone)
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int i = 0; i < kTiles; ++i) {
-          const float4 y = *reinterpret_cast<const float4*>(s_p + (8 * n + r) * kPitch + 16 * i + 4 * q4);
-          float z[4] = {y.x, y.y, y.z, y.w};
+          uint32_t* const to = s_f + (n * kTiles + i) * (64 * PP);
+          if constexpr (PP == 2) {
+            *reinterpret_cast<uint4*>(to) = make_uint4(pf[n][i][0][0], pf[n][i][0][1], pf[n][i][1][0], pf[n][i][1][1]);
+          } else {
 #pragma unroll
-          for (int p = 0; p < PP; ++p)
+            for (int p = 0; p < PP; ++p) *reinterpret_cast<uint2*>(to + 2 * p) = make_uint2(pf[n][i][p][0], pf[n][i][p][1]);
+          }
+        }
+      // ---- O^T += V^T P^T: slots 16 tile + 4 q4 .. + 3 are the MMA's k
+#pragma unroll 1
+      for (int i = 0; i < kTiles; ++i) {
+        uint32_t b[NT][PP][2];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              const uint32_t two = pack_bf16(z[2 * h], z[2 * h + 1]);
-              pf[n][i][p][h] = two;
-              if (p + 1 < PP) {
-                z[2 * h] -= __uint_as_float(two << 16);
-                z[2 * h + 1] -= __uint_as_float(two & 0xffff0000u);
-              }
+        for (int n = 0; n < NT; ++n) {
+          const uint32_t* const from = s_f + (n * kTiles + i) * (64 * PP);
+          if constexpr (PP == 2) {
+            const uint4 u = *reinterpret_cast<const uint4*>(from);
+            b[n][0][0] = u.x; b[n][0][1] = u.y; b[n][1][0] = u.z; b[n][1][1] = u.w;
+          } else {
+#pragma unroll
+            for (int p = 0; p < PP; ++p) {
+              const uint2 u = *reinterpret_cast<const uint2*>(from + 2 * p);
+              b[n][p][0] = u.x; b[n][p][1] = u.y;
             }
-        }
-      constexpr int AT_ONCE = NT == 1 && G > 2 ? 2 : NT == 1 ? 2 : 1;   // groups
-#pragma unroll
-      for (int g0 = 0; g0 < G; g0 += AT_ONCE) {
-        float d[AT_ONCE][2][NT][4];
-#pragma unroll
-        for (int i = 0; i < kTiles; ++i) {
-          const int row = 16 * i + 4 * q4;
-          uint32_t w[4], sc[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            w[e] = *reinterpret_cast<const uint32_t*>(sm + C::V_OFF + (row + e) * C::RB + r * (C::RB / 8) + g0 / 2 * 4);
-            sc[e] = reinterpret_cast<const uint32_t*>(v_scales)[(row + e) * (G / 2) + g0 / 2];
           }
+        }
+        uint32_t w[4][G / 2], sc[4][G / 2];
 #pragma unroll
-          for (int g = 0; g < AT_ONCE; ++g) {
-            const uint32_t x01 = both(w[0], w[1], g0 + g), x23 = both(w[2], w[3], g0 + g);
-            const uint32_t s01 = both(sc[0], sc[1], g0 + g), s23 = both(sc[2], sc[3], g0 + g);
-            const uint32_t a8 = mul_bf16x2(s01, 0x3e003e00u), am = mul_bf16x2(s01, 0xc1c0c1c0u);   // 1 / 8, -24
-            const uint32_t b8 = mul_bf16x2(s23, 0x3e003e00u), bm = mul_bf16x2(s23, 0xc1c0c1c0u);
-            const uint32_t va[2][4] = {{value_bf16<0>(x01, a8, am), value_bf16<1>(x01, a8, am), value_bf16<0>(x23, b8, bm),
-                                        value_bf16<1>(x23, b8, bm)},
-                                       {value_bf16<2>(x01, a8, am), value_bf16<3>(x01, a8, am), value_bf16<2>(x23, b8, bm),
-                                        value_bf16<3>(x23, b8, bm)}};
+        for (int e = 0; e < 4; ++e) {
+          const int row = 16 * i + 4 * q4 + e;
+          const uint8_t* const from = sm + C::V_OFF + row * C::RB + r * (C::RB / 8);
+          if constexpr (G == 4) {
+            const uint2 u = *reinterpret_cast<const uint2*>(from), z = reinterpret_cast<const uint2*>(v_scales)[row];
+            w[e][0] = u.x; w[e][1] = u.y;
+            sc[e][0] = z.x; sc[e][1] = z.y;
+          } else {
+            w[e][0] = *reinterpret_cast<const uint32_t*>(from);
+            sc[e][0] = reinterpret_cast<const uint32_t*>(v_scales)[row];
+          }
+        }
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
+        for (int g = 0; g < G; ++g) {
+          const uint32_t x01 = both(w[0][g / 2], w[1][g / 2], g), x23 = both(w[2][g / 2], w[3][g / 2], g);
+          const uint32_t s01 = both(sc[0][g / 2], sc[1][g / 2], g), s23 = both(sc[2][g / 2], sc[3][g / 2], g);
+          const uint32_t a8 = mul_bf16x2(s01, 0x3e003e00u), am = mul_bf16x2(s01, 0xc1c0c1c0u);   // 1 / 8, -24
+          const uint32_t b8 = mul_bf16x2(s23, 0x3e003e00u), bm = mul_bf16x2(s23, 0xc1c0c1c0u);
+          const uint32_t va[2][4] = {{value_bf16<0>(x01, kv, a8, am), value_bf16<1>(x01, kv, a8, am), value_bf16<0>(x23, kv, b8, bm),
+                                      value_bf16<1>(x23, kv, b8, bm)},
+                                     {value_bf16<2>(x01, kv, a8, am), value_bf16<3>(x01, kv, a8, am), value_bf16<2>(x23, kv, b8, bm),
+                                      value_bf16<3>(x23, kv, b8, bm)}};
 #pragma unroll
-              for (int p = PP - 1; p >= 0; --p)
+          for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                  float (&z)[4] = d[g][h][n];
-                  if (i == 0 && p == PP - 1) mma_bf16(z, va[h], pf[n][i][p][0], pf[n][i][p][1], 0.f, 0.f, 0.f, 0.f);
-                  else mma_bf16(z, va[h], pf[n][i][p][0], pf[n][i][p][1], z[0], z[1], z[2], z[3]);
+            for (int p = PP - 1; p >= 0; --p)
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                float (&z)[4] = o[g][h][n];
+                if constexpr (F32) {           // (rounded sums: a plane of 16 slots at a time)
+                  float d[4];
+                  mma_bf16(d, va[h], b[n][p][0], b[n][p][1], 0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                  for (int e = 0; e < 4; ++e) z[e] += d[e];
+                } else {
+                  mma_bf16(z, va[h], b[n][p][0], b[n][p][1], z[0], z[1], z[2], z[3]);
                 }
-          }
+              }
         }
-#pragma unroll
-        for (int g = 0; g < AT_ONCE; ++g)
-#pragma unroll
-          for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-              for (int e = 0; e < 4; ++e) o[g0 + g][h][n][e] += d[g][h][n][e];
       }
       __syncwarp();                            // (V and P are read)
-      if (more || beyond) load(more ? s : next, x, 1);
+      if (more || beyond) load(after, to, x, 1);
       loaded = beyond;
+      if (!F32 && ++links == kChain && more) {
+        if (chained) add_chain();
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          put(n, 0, 1.f);
+          put(n, 1, 1.f);
+          m_then[n] = m[n];
+        }
+        chained = true;
+        links = 0;
+        clear();
+      }
     }
     // ---- the item's (or its part's) sums
+    if (chained) add_chain();
     const bool whole = s.c0 == 0 && s.c1 == s.units;
-    const size_t part = (size_t)blockIdx.x * 2 + (s.c0 == 0);
     const int live = min(NQ, a.T * a.G - s.qb * NQ);
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int v = 8 * n + 2 * q4 + e;
-        float sum = l[n][e];
-#pragma unroll
-        for (int d = 4; d < 32; d *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-        if (v >= s.nq) sum = 0.f;              // (a vector past the nodes: zeros)
-        float top = sum == 0.f ? -INFINITY : m[n][e] == -INFINITY ? 0.f : m[n][e];   // (NaN scores: no maximum)
-        const float inv = sum == 0.f ? 0.f : whole ? 1.f / sum : 1.f;
-        if (v < live) {
-          const Vec w = vector_of(a, s.h, s.qb, v);
-#pragma unroll
-          for (int g = 0; g < G; ++g) {
-            const int d = g * kGroup + 4 * r;
-            float y[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) y[i] = inv == 0.f ? 0.f : o[g][i / 2][n][i % 2 * 2 + e] * inv;
-            if (whole) {
-#pragma unroll
-              for (int i = 0; i < 4; ++i) store_out<T>(a, s.b, w, d + i, y[i]);
-            } else {
-              *reinterpret_cast<float4*>(a.part_o + (part * NQ + v) * HD + d) = make_float4(y[0], y[1], y[2], y[3]);
-            }
-          }
-          if (r == 0) {
-            if (whole) {
-              store_lse(a, s.b, w, top, sum);
-            } else {
-              a.part_ml[(part * 2) * NQ + v] = top;
-              a.part_ml[(part * 2 + 1) * NQ + v] = sum;
-            }
-          }
+    for (int n = 0; n < NT; ++n) {
+      const int v = 8 * n + r;
+      float sum = l[n];
+      sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+      sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+      if (v >= s.nq) sum = 0.f;                // (a vector past the nodes: zeros)
+      const float top = sum == 0.f ? -INFINITY : m[n] == -INFINITY ? 0.f : m[n];   // (NaN scores: no maximum)
+      const float inv = sum == 0.f ? 0.f : whole ? 1.f / sum : 1.f;
+      if (q4 == 0 && v < live) {
+        if (whole) {
+          store_lse(a, s.b, vector_of(a, s.h, s.qb, v), top, sum);
+        } else {
+          a.part_ml[(part * 2) * NQ + v] = top;
+          a.part_ml[(part * 2 + 1) * NQ + v] = sum;
         }
       }
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int to = 8 * n + 2 * q4 + e;
+        const float by = __shfl_sync(0xffffffffu, inv, 4 * (2 * q4 + e));
+        if (to >= live) continue;
+        if (by == 0.f)
+#pragma unroll
+          for (int g = 0; g < G; ++g) o[g][0][n][e] = o[g][0][n][2 + e] = o[g][1][n][e] = o[g][1][n][2 + e] = 0.f;
+        if (!whole) {
+          put(n, e, by);
+          continue;
+        }
+        const Vec w = vector_of(a, s.h, s.qb, to);
+#pragma unroll
+        for (int g = 0; g < G; ++g)
+#pragma unroll
+          for (int d = 0; d < 4; ++d) store_out<T>(a, s.b, w, g * kGroup + 4 * r + d, o[g][d / 2][n][d % 2 * 2 + e] * by);
+      }
+    }
   }
 }
 
