@@ -411,7 +411,7 @@ __global__ void __launch_bounds__(32 * kCombine) k_tree_combine(TreeArgs a) {
   } else {
     before = __reduce_add_sync(0xffffffffu, before);
   }
-  const int n = nodes_of(a, b), live = live_blocks(a, n), u = item_units(len_of(a, b) + n);
+  const int n = nodes_of(a, b), live = live_blocks(a, n), u = item_units(a, len_of(a, b) + n);
   const int per_head = live * u + a.QB - live;
   if (Bounds) {
     h = x / per_head;
@@ -599,12 +599,15 @@ extern "C" int32_t cdsl_tree_attention(const cdsl_kv_cache* cache, int32_t layer
   if (!ck.aligned(d_workspace, 256) || workspace_bytes < z.bytes)
     return ck.fail("the workspace must be 256-byte aligned and hold cdsl_tree_attention_workspace bytes",
                    workspace_bytes < z.bytes ? CDSL_ENOMEM : CDSL_EINVAL);
-  const long long chunks = ((long long)max_len + T + kKeys - 1) / kKeys;
+  const int unit_shift = c.format == kI4 ? 6 : 7;
+  static_assert(kKeys == 1 << 7);
+  const long long chunks = ((long long)max_len + T + (1 << unit_shift) - 1) >> unit_shift;
   const long long units = chunks * c.batch * c.kvh * z.QB;   // at most
-  if (units >= (1LL << 31)) return ck.fail("the pass is beyond the limit (2^31 chunks of 128 slots)");
+  if (units >= (1LL << 31)) return ck.fail("the pass is beyond the limit (2^31 chunks of 128 slots, 64 in 4 bits)");
   TreeArgs a = {};
   a.c = c;
   a.dtype = dtype;
+  a.unit_shift = unit_shift;
   a.layer = layer; a.T = T; a.H = n_heads; a.G = n_heads / c.kvh; a.W = (T + 31) / 32;
   a.NQ = z.NQ; a.QB = z.QB;
   a.q = d_q; a.out = d_out; a.lse = d_lse;

@@ -2,7 +2,7 @@
 // that its kernels share.
 //
 // Work: an item is (sequence, K/V head, block of NQ query vectors), its units the chunks of kKeys
-// slots that its queries may see. The units of all items, in order, are cut into as many equal runs as
+// slots (a 4-bit cache: half of them) that its queries may see. The units of all items, in order, are cut into as many equal runs as
 // there are blocks, so that ragged lengths and any batch keep every block equally long at work. A
 // run covers parts of at most two items and any number of whole ones. A whole item's output is written
 // at once; of a part the block leaves (m, l, o) in the workspace, and k_tree_combine adds the parts
@@ -24,6 +24,7 @@ struct TreeArgs {
   Cache c;
   int layer, T, H, G, W, NQ, QB;               // W: mask words; QB: query blocks per head
   int dtype;                                   // of q and out
+  int unit_shift;                              // log2 of a unit's slots
   const void* q;
   void* out;
   float* lse;
@@ -57,7 +58,9 @@ __device__ __forceinline__ int nodes_of(const TreeArgs& a, int b) {
 }
 // Units of a block of queries (an item without anything to see has one, which writes its zeros), of those
 // that hold nodes, and how many blocks hold some.
-__device__ __forceinline__ int item_units(int keys) { return max(1, (keys + kKeys - 1) / kKeys); }
+__device__ __forceinline__ int item_units(const TreeArgs& a, int keys) {
+  return max(1, (keys + (1 << a.unit_shift) - 1) >> a.unit_shift);
+}
 __device__ __forceinline__ int live_blocks(const TreeArgs& a, int nodes) {
   return (nodes * a.G + a.NQ - 1) / a.NQ;
 }
@@ -65,7 +68,7 @@ __device__ __forceinline__ int live_blocks(const TreeArgs& a, int nodes) {
 // of a sequence of `len` cached slots and n nodes
 __device__ __forceinline__ int units_of(const TreeArgs& a, int len, int n) {
   const int live = live_blocks(a, n);
-  return a.c.kvh * (live * item_units(len + n) + (a.QB - live));
+  return a.c.kvh * (live * item_units(a, len + n) + (a.QB - live));
 }
 
 // first[b], b <= batch: the units before sequence b's; behind them the sequences' lengths and nodes. The whole block
@@ -100,7 +103,7 @@ __device__ __forceinline__ void build_plan(const TreeArgs& a, int* first) {
 struct Segment {
   int b, h, qb;
   int len, nodes, keys;     // cached slots, tree slots after them, both (0 of an item without queries)
-  int c0, c1, units;        // chunks [c0, c1) of the item's
+  int c0, c1, units;        // units [c0, c1) of the item's
   int nq;                   // its query vectors (0 without any)
 };
 __device__ __forceinline__ Segment segment_at(const TreeArgs& a, const int* first, int unit, int end) {
@@ -114,7 +117,7 @@ __device__ __forceinline__ Segment segment_at(const TreeArgs& a, const int* firs
   s.b = lo;
   s.len = first[a.c.batch + 1 + lo];
   s.nodes = first[2 * a.c.batch + 1 + lo];
-  const int live = live_blocks(a, s.nodes), u = item_units(s.len + s.nodes);
+  const int live = live_blocks(a, s.nodes), u = item_units(a, s.len + s.nodes);
   const int per_head = live * u + (a.QB - live);
   const int x = unit - first[lo];
   s.h = x / per_head;

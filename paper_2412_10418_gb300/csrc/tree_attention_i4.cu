@@ -39,7 +39,7 @@ namespace cdsl {
 namespace tree {
 namespace {
 
-constexpr int kStretch = 64;                   // slots at a time
+constexpr int kStretch = 64;                   // slots at a time: a unit
 constexpr int kTiles = kStretch / 16;
 constexpr int kPitch = kStretch + 4;           // floats of a vector's scores
 constexpr int kChain = 64;                     // stretches of O^T's chain (512 products: 2^-15 of it at worst)
@@ -51,7 +51,8 @@ struct Cfg {
   static constexpr int QP = F32 ? 3 : 1, PP = F32 ? 3 : 2;         // planes of q and p
   static constexpr uint32_t CODES = kStretch * RB, SCALES = kStretch * SB;
   static constexpr uint32_t V_OFF = CODES + SCALES;
-  static constexpr uint32_t P_OFF = 2 * V_OFF;
+  static constexpr uint32_t F_OFF = 2 * V_OFF;                     // V's scales / 8 by pairs of slots
+  static constexpr uint32_t P_OFF = F_OFF + SCALES;
   // scores, then P's fragments: PP planes of two words for each tile and lane
   static constexpr uint32_t S_BYTES = NQ * kPitch * 4, F_BYTES = NT * kTiles * 32 * PP * 8;
   static constexpr uint32_t MASK_OFF = P_OFF + (S_BYTES > F_BYTES ? S_BYTES : F_BYTES);
@@ -167,7 +168,7 @@ __global__ void __launch_bounds__(32, Cfg<HD, NQ, F32>::WARPS) k_tree_i4(TreeArg
     window = slot;
     const int mine = slot + (lane << shift);
     pages = -1;
-    if (mine < min(s.keys, s.c1 * kKeys)) {
+    if (mine < min(s.keys, s.c1 * kStretch)) {
       pages = page_of(c, s.b, mine);
       if (pages < 0) set_status(a.status, CDSL_ERANGE);
     }
@@ -203,10 +204,10 @@ __global__ void __launch_bounds__(32, Cfg<HD, NQ, F32>::WARPS) k_tree_i4(TreeArg
     const Segment& s = s_seg[turn];
     const Segment& next = s_seg[turn ^ 1];
     if (!loaded && s.keys > 0) {
-      look(s, s.c0 * kKeys);
-      x = locate(s, s.c0 * kKeys);
-      load(s, s.c0 * kKeys, x, 0);
-      load(s, s.c0 * kKeys, x, 1);
+      look(s, s.c0 * kStretch);
+      x = locate(s, s.c0 * kStretch);
+      load(s, s.c0 * kStretch, x, 0);
+      load(s, s.c0 * kStretch, x, 1);
     }
     loaded = false;
     unit += s.c1 - s.c0;
@@ -316,9 +317,9 @@ __global__ void __launch_bounds__(32, Cfg<HD, NQ, F32>::WARPS) k_tree_i4(TreeArg
             make_float4(o[g][0][n][e] * by, o[g][0][n][2 + e] * by, o[g][1][n][e] * by, o[g][1][n][2 + e] * by);
     };
 
-    const int last = min(s.keys, s.c1 * kKeys);
+    const int last = min(s.keys, s.c1 * kStretch);
 #pragma unroll 1
-    for (int slot = s.c0 * kKeys, links = 0; slot < last; slot += kStretch, ++it) {
+    for (int slot = s.c0 * kStretch, links = 0; slot < last; slot += kStretch, ++it) {
       // ---- scores of slots 16 tile + r, + 8 and vectors 2 q4, + 1
       if (!__all_sync(0xffffffffu, wait_for(&full[0], it & 1, a.status))) {
         wait_for(&full[1], it & 1, a.status);
@@ -376,7 +377,7 @@ __global__ void __launch_bounds__(32, Cfg<HD, NQ, F32>::WARPS) k_tree_i4(TreeArg
       const int there = last - slot;           // slots that there are, if fewer than 64
       const bool more = slot + kStretch < last, beyond = !more && unit < end && next.keys > 0;
       const Segment& after = more ? s : next;
-      const int to = more ? slot + kStretch : next.c0 * kKeys;
+      const int to = more ? slot + kStretch : next.c0 * kStretch;
       if (more || beyond) {
         if (beyond) look(after, to);
         x = locate(after, to);
@@ -387,21 +388,28 @@ __global__ void __launch_bounds__(32, Cfg<HD, NQ, F32>::WARPS) k_tree_i4(TreeArg
         return;
       }
       uint8_t* const v_scales = sm + C::V_OFF + C::CODES;
-      // rows of V whose scales are not finite, as bits. (Of one that is not, bits 7 .. 14 are all set: 0x80 carries into bit
+      // V's scales of slots 2 lane, 2 lane + 1. (Of one that is not finite, bits 7 .. 14 are all set: 0x80 carries into bit
       // 15. K's need no look: the scores are NaN.)
-      uint64_t v_bad = 0;
-      uint32_t odd = 0;
-      if (lane < kStretch * C::SB / 16) {
+      uint32_t even[G / 2], odd[G / 2];
+      if constexpr (G == 4) {
         const uint4 u = reinterpret_cast<const uint4*>(v_scales)[lane];
-        odd = ((u.x & 0x7f807f80u) + 0x00800080u) | ((u.y & 0x7f807f80u) + 0x00800080u) |
-              ((u.z & 0x7f807f80u) + 0x00800080u) | ((u.w & 0x7f807f80u) + 0x00800080u);
+        even[0] = u.x; even[1] = u.y; odd[0] = u.z; odd[1] = u.w;
+      } else {
+        const uint2 u = reinterpret_cast<const uint2*>(v_scales)[lane];
+        even[0] = u.x; odd[0] = u.y;
       }
-      if (__any_sync(0xffffffffu, (odd & 0x80008000u) != 0))
-#pragma unroll 1
-        for (int h = 0; h < 2; ++h) {
-          const uint32_t* const z = reinterpret_cast<const uint32_t*>(v_scales) + (lane + 32 * h) * (G / 2);
-          v_bad |= (uint64_t)__ballot_sync(0xffffffffu, i4_not_finite(make_uint2(z[0], G == 4 ? z[G / 4] : 0u), G)) << (32 * h);
-        }
+      uint32_t even_bad = 0, odd_bad = 0;
+#pragma unroll
+      for (int i = 0; i < G / 2; ++i) {
+        even_bad |= (even[i] & 0x7f807f80u) + 0x00800080u;
+        odd_bad |= (odd[i] & 0x7f807f80u) + 0x00800080u;
+      }
+      // rows that are not finite, as bits of the even and of the odd slots
+      uint32_t v_bad[2] = {0u, 0u};
+      if (__any_sync(0xffffffffu, ((even_bad | odd_bad) & 0x80008000u) != 0)) {
+        v_bad[0] = __ballot_sync(0xffffffffu, (even_bad & 0x80008000u) != 0);
+        v_bad[1] = __ballot_sync(0xffffffffu, (odd_bad & 0x80008000u) != 0);
+      }
       // slots that there are, as bits
       uint64_t valid = there >= 64 ? ~0ull : (1ull << there) - 1;
       const uint32_t pieces = shift == 6 ? 1u : shift == 5 ? 3u : 15u;
@@ -411,7 +419,7 @@ __global__ void __launch_bounds__(32, Cfg<HD, NQ, F32>::WARPS) k_tree_i4(TreeArg
           if (!(live_now >> i & 1)) valid &= ~((shift == 6 ? ~0ull : (1ull << rows) - 1) << (i << shift));
       // Code of its own for stretches with slots of the tree, past the item's, without a page or with a row that is not
       // finite: as one, every score has selects.
-      const bool masked = valid != ~0ull || slot + kStretch > s.len || v_bad != 0;
+      const bool masked = valid != ~0ull || slot + kStretch > s.len || (v_bad[0] | v_bad[1]) != 0;
       // ---- maxima, probabilities, sums: slots 16 tile + 4 q4 .. + 3 of vector r (+ 8)
       uint32_t pf[NT][kTiles][PP][2];
       bool raised = false;
@@ -468,7 +476,7 @@ __global__ void __launch_bounds__(32, Cfg<HD, NQ, F32>::WARPS) k_tree_i4(TreeArg
               if constexpr (general) {
                 if (!(seen >> (16 * i + e) & 1)) y[e] = 0.f;
                 sum += y[e];
-                if (y[e] != 0.f && v_bad >> (4 * q4) >> (16 * i + e) & 1) y[e] = __uint_as_float(0x7fc00000u);
+                if (y[e] != 0.f && v_bad[e & 1] >> (8 * i + 2 * q4 + e / 2) & 1) y[e] = __uint_as_float(0x7fc00000u);
               } else {
                 sum += y[e];
               }
@@ -490,15 +498,23 @@ __global__ void __launch_bounds__(32, Cfg<HD, NQ, F32>::WARPS) k_tree_i4(TreeArg
       };
       if (masked) {
         softmax(std::true_type());
-        const uint64_t gone = ~valid | v_bad;  // nothing of these rows of V may reach the sums
+        // nothing of a slot that is not there, or whose V is not finite, may reach the sums
+        const bool e0 = valid >> (2 * lane) & 1 && !(v_bad[0] >> lane & 1), e1 = valid >> (2 * lane + 1) & 1 && !(v_bad[1] >> lane & 1);
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-          if (gone >> (lane + 32 * h) & 1)
-#pragma unroll
-            for (int i = 0; i < G / 2; ++i) reinterpret_cast<uint32_t*>(v_scales)[(lane + 32 * h) * (G / 2) + i] = 0u;
-        tc::fence_proxy_async();               // (before the copy that follows them)
+        for (int i = 0; i < G / 2; ++i) {
+          if (!e0) even[i] = 0u;
+          if (!e1) odd[i] = 0u;
+        }
       } else {
         softmax(std::false_type());
+      }
+      {
+        uint32_t f[G];
+#pragma unroll
+        for (int g = 0; g < G; ++g) f[g] = mul_bf16x2(both(even[g / 2], odd[g / 2], g), 0x3e003e00u);   // 1 / 8
+        uint8_t* const to = sm + C::F_OFF + lane * (4 * G);
+        if constexpr (G == 4) *reinterpret_cast<uint4*>(to) = make_uint4(f[0], f[1], f[2], f[3]);
+        else *reinterpret_cast<uint2*>(to) = make_uint2(f[0], f[1]);
       }
       if (__any_sync(0xffffffffu, raised)) {
 #pragma unroll
@@ -515,7 +531,7 @@ __global__ void __launch_bounds__(32, Cfg<HD, NQ, F32>::WARPS) k_tree_i4(TreeArg
               }
           }
       }
-      __syncwarp();                            // (scores are read, V's scales are as they should be)
+      __syncwarp();                            // (scores are read, V's scales are written)
       uint32_t* const s_f = reinterpret_cast<uint32_t*>(s_p) + lane * (2 * PP);   // (of this lane alone)
 #pragma unroll
       for (int n = 0; n < NT; ++n)
@@ -547,26 +563,32 @@ __global__ void __launch_bounds__(32, Cfg<HD, NQ, F32>::WARPS) k_tree_i4(TreeArg
             }
           }
         }
-        uint32_t w[4][G / 2], sc[4][G / 2];
+        uint32_t w[4][G / 2], f[2][G];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const int row = 16 * i + 4 * q4 + e;
-          const uint8_t* const from = sm + C::V_OFF + row * C::RB + r * (C::RB / 8);
+          const uint8_t* const from = sm + C::V_OFF + (16 * i + 4 * q4 + e) * C::RB + r * (C::RB / 8);
           if constexpr (G == 4) {
-            const uint2 u = *reinterpret_cast<const uint2*>(from), z = reinterpret_cast<const uint2*>(v_scales)[row];
+            const uint2 u = *reinterpret_cast<const uint2*>(from);
             w[e][0] = u.x; w[e][1] = u.y;
-            sc[e][0] = z.x; sc[e][1] = z.y;
           } else {
             w[e][0] = *reinterpret_cast<const uint32_t*>(from);
-            sc[e][0] = reinterpret_cast<const uint32_t*>(v_scales)[row];
+          }
+        }
+        {
+          const uint4* const from = reinterpret_cast<const uint4*>(sm + C::F_OFF + (8 * i + 2 * q4) * (4 * G));
+          const uint4 u = from[0];
+          if constexpr (G == 4) {
+            const uint4 z = from[1];
+            f[0][0] = u.x; f[0][1] = u.y; f[0][2] = u.z; f[0][3] = u.w;
+            f[1][0] = z.x; f[1][1] = z.y; f[1][2] = z.z; f[1][3] = z.w;
+          } else {
+            f[0][0] = u.x; f[0][1] = u.y; f[1][0] = u.z; f[1][1] = u.w;
           }
         }
 #pragma unroll
         for (int g = 0; g < G; ++g) {
           const uint32_t x01 = both(w[0][g / 2], w[1][g / 2], g), x23 = both(w[2][g / 2], w[3][g / 2], g);
-          const uint32_t s01 = both(sc[0][g / 2], sc[1][g / 2], g), s23 = both(sc[2][g / 2], sc[3][g / 2], g);
-          const uint32_t a8 = mul_bf16x2(s01, 0x3e003e00u), am = mul_bf16x2(s01, 0xc1c0c1c0u);   // 1 / 8, -24
-          const uint32_t b8 = mul_bf16x2(s23, 0x3e003e00u), bm = mul_bf16x2(s23, 0xc1c0c1c0u);
+          const uint32_t a8 = f[0][g], am = mul_bf16x2(a8, 0xc340c340u), b8 = f[1][g], bm = mul_bf16x2(b8, 0xc340c340u);   // -192
           const uint32_t va[2][4] = {{value_bf16<0>(x01, kv, a8, am), value_bf16<1>(x01, kv, a8, am), value_bf16<0>(x23, kv, b8, bm),
                                       value_bf16<1>(x23, kv, b8, bm)},
                                      {value_bf16<2>(x01, kv, a8, am), value_bf16<3>(x01, kv, a8, am), value_bf16<2>(x23, kv, b8, bm),
