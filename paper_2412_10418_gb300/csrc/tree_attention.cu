@@ -25,9 +25,9 @@ namespace tree {
 namespace {
 
 // Four codes (1 or 2 words) to floats.
-template <int FORMAT>
+template <bool F8>
 __device__ __forceinline__ void decode4(uint32_t u, uint32_t w, float (&x)[4]) {
-  if constexpr (FORMAT == kF8) {
+  if constexpr (F8) {
     const float2 a = f8x2_to_f32(u & 0xffffu), b = f8x2_to_f32(u >> 16);
     x[0] = a.x; x[1] = a.y; x[2] = b.x; x[3] = b.y;
   } else {
@@ -41,18 +41,14 @@ __device__ __forceinline__ void decode4(uint32_t u, uint32_t w, float (&x)[4]) {
 constexpr int SQ = 8;                          // query vectors per block
 // Resident warps of an SM, by registers (16 of bf16 rows of 128 spill: 182 us where 12 take 143, four trees of 49 of 40 heads
 // after 1024 tokens; e4m3: 46 us with 16, 59 with 12, a tree of 17 of 32 heads after 4096)
-constexpr int simt_per_sm(int HD, int format) { return HD == 128 && format != kF8 ? 12 : 16; }
+constexpr int simt_per_sm(int HD, bool F8) { return HD == 128 && !F8 ? 12 : 16; }
 
-template <typename T, int HD, int FORMAT>
-__global__ void __launch_bounds__(32, simt_per_sm(HD, FORMAT)) k_tree_simt(TreeArgs a) {
-  constexpr bool F8 = FORMAT == kF8, I4 = FORMAT == kI4;
-  constexpr int EB = FORMAT == kBF16 ? 2 : 1, CPL = 16 / EB;   // codes in 16 bytes
-  constexpr int ROW_BYTES = I4 ? HD / 2 : HD * EB, LOADS = ROW_BYTES / 16;
-  constexpr int G = HD / kGroup;               // I4: scales of a row
+template <typename T, int HD, bool F8>
+__global__ void __launch_bounds__(32, simt_per_sm(HD, F8)) k_tree_simt(TreeArgs a) {
+  constexpr int EB = F8 ? 1 : 2, CPL = 16 / EB, LOADS = HD / CPL;   // codes in 16 bytes
   constexpr int DPL = HD / 32;                 // dimensions of a lane
-  constexpr int AHEAD = DPL * EB > 4 || I4 ? 8 : 16; // V rows loaded together
-  using VBits = std::conditional_t<I4, std::conditional_t<DPL == 4, uint16_t, uint8_t>, std::conditional_t<
-      DPL * EB == 8, uint2, std::conditional_t<DPL * EB == 4, uint32_t, uint16_t>>>;
+  constexpr int AHEAD = DPL * EB > 4 ? 8 : 16; // V rows loaded together
+  using VBits = std::conditional_t<DPL * EB == 8, uint2, std::conditional_t<DPL * EB == 4, uint32_t, uint16_t>>;
   extern __shared__ int s_first[];             // plan_bytes
   constexpr int ROW = SQ + 4;                  // floats (48 or 80 bytes: eight lanes' 16 bytes take all banks)
   __shared__ __align__(16) float s_q[HD][ROW];
@@ -116,26 +112,9 @@ __global__ void __launch_bounds__(32, simt_per_sm(HD, FORMAT)) k_tree_simt(TreeA
       const int at = slot & ((1 << c.page_shift) - 1);
       const size_t row = page >= 0 ? row_of(c, a.layer, page, 0, s.h, at) : row0;
       const size_t vrow = page >= 0 ? row_of(c, a.layer, page, 1, s.h, at) : row0;
-      uint32_t ks4 = 0u, vs4 = 0u;             // (slots past the item's: not used)
-      uint2 kg[I4 ? 4 : 1], vg[I4 ? 4 : 1];    // I4: the slots' scales
-      if constexpr (I4) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const uint8_t* const ks = c.scale + (row + e) * (2 * G), * const vs = c.scale + (vrow + e) * (2 * G);
-          if constexpr (G == 4) {
-            kg[e] = *reinterpret_cast<const uint2*>(ks);
-            vg[e] = *reinterpret_cast<const uint2*>(vs);
-          } else {
-            kg[e] = make_uint2(*reinterpret_cast<const uint32_t*>(ks), 0u);
-            vg[e] = make_uint2(*reinterpret_cast<const uint32_t*>(vs), 0u);
-          }
-          if (i4_not_finite(kg[e], G)) kg[e] = make_uint2(0x7fc07fc0u, 0x7fc07fc0u);
-        }
-      } else {
-        ks4 = *reinterpret_cast<const uint32_t*>(c.scale + row);
-        vs4 = *reinterpret_cast<const uint32_t*>(c.scale + vrow);
-      }
-      const uint8_t* const k = c.pool + row * ROW_BYTES;
+      const uint32_t ks4 = *reinterpret_cast<const uint32_t*>(c.scale + row);   // (slots past the item's: not used)
+      const uint32_t vs4 = *reinterpret_cast<const uint32_t*>(c.scale + vrow);
+      const uint8_t* const k = c.pool + row * HD * EB;
       uint64_t t[SQ / 2][4];
 #pragma unroll
       for (int v = 0; v < SQ / 2; ++v)
@@ -145,7 +124,7 @@ __global__ void __launch_bounds__(32, simt_per_sm(HD, FORMAT)) k_tree_simt(TreeA
       auto load_k = [&](int i) {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          next[e] = e < n ? reinterpret_cast<const uint4*>(k + e * ROW_BYTES)[i] : make_uint4(0u, 0u, 0u, 0u);
+          next[e] = e < n ? reinterpret_cast<const uint4*>(k + e * HD * EB)[i] : make_uint4(0u, 0u, 0u, 0u);
       };
       load_k(0);
 #pragma unroll 1
@@ -157,18 +136,10 @@ __global__ void __launch_bounds__(32, simt_per_sm(HD, FORMAT)) k_tree_simt(TreeA
         }
         if (i + 1 < LOADS) load_k(i + 1);
 #pragma unroll
-        for (int j = 0; j < (I4 ? 8 : 4); j += EB) {      // four dimensions
+        for (int j = 0; j < 4; j += EB) {      // four dimensions
           float x[4][4];
-          int d0 = i * CPL + j * 4 / EB;
-          if constexpr (I4) {                  // (a piece of 16 bits)
-            d0 = j % G * kGroup + (8 * i + j) / G * 4;
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              i4x4_to_f32(raw[e][j / 2] >> (j % 2 * 16), bf16_at(j % G / 2 ? kg[e].y : kg[e].x, j % 2), x[e]);
-          } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) decode4<FORMAT>(raw[e][j], raw[e][j + EB - 1], x[e]);
-          }
+          for (int e = 0; e < 4; ++e) decode4<F8>(raw[e][j], raw[e][j + EB - 1], x[e]);
 #pragma unroll
           for (int d = 0; d < 4; ++d) {
             uint64_t xx[4];
@@ -176,7 +147,7 @@ __global__ void __launch_bounds__(32, simt_per_sm(HD, FORMAT)) k_tree_simt(TreeA
             for (int e = 0; e < 4; ++e) xx[e] = pair(x[e][d], x[e][d]);
 #pragma unroll
             for (int v = 0; v < SQ; v += 4) {
-              const ulonglong2 q = *reinterpret_cast<const ulonglong2*>(&s_q[d0 + d][v]);
+              const ulonglong2 q = *reinterpret_cast<const ulonglong2*>(&s_q[i * CPL + j * 4 / EB + d][v]);
 #pragma unroll
               for (int e = 0; e < 4; ++e) {
                 t[v / 2][e] = fma2(q.x, xx[e], t[v / 2][e]);
@@ -190,13 +161,8 @@ __global__ void __launch_bounds__(32, simt_per_sm(HD, FORMAT)) k_tree_simt(TreeA
       float ks[4], vs[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        if constexpr (I4) {                    // (the scales are in the values; a row that is not finite: NaN)
-          ks[e] = 1.f;
-          vs[e] = i4_not_finite(vg[e], G) ? __uint_as_float(0x7fc00000u) : 1.f;
-        } else {
-          ks[e] = e < n ? scale_value(ks4 >> (8 * e) & 255) : 1.f;
-          vs[e] = e < n ? scale_value(vs4 >> (8 * e) & 255) : 0.f;
-        }
+        ks[e] = e < n ? scale_value(ks4 >> (8 * e) & 255) : 1.f;
+        vs[e] = e < n ? scale_value(vs4 >> (8 * e) & 255) : 0.f;
       }
       const int node = slot - s.len;           // the tree's node in the first slot
       const bool masked = __any_sync(0xffffffffu, node > -4 || n < 4);
@@ -254,18 +220,12 @@ __global__ void __launch_bounds__(32, simt_per_sm(HD, FORMAT)) k_tree_simt(TreeA
       const int kn = min(s.keys - ch * kKeys, kKeys);
       const uint32_t mine = page >= 0 ? (uint32_t)(vrow - row0) : ~0u;
       VBits ahead[AHEAD];
-      uint16_t scale_ahead[I4 ? AHEAD : 1];
       auto load_v = [&](int k0) {
         const uint32_t first = __shfl_sync(0xffffffffu, mine, k0 / 4 & 31);
-        const VBits* const v = reinterpret_cast<const VBits*>(c.pool + (row0 + first) * ROW_BYTES) + lane;
+        const VBits* const v = reinterpret_cast<const VBits*>(c.pool + (row0 + first) * HD * EB) + lane;
 #pragma unroll
         for (int e = 0; e < AHEAD; ++e)
           ahead[e] = first != ~0u && k0 + e < kn ? v[e * 32] : VBits{};
-        if constexpr (I4) {                    // of the group that the lane's values are in
-          const uint16_t* const s = reinterpret_cast<const uint16_t*>(c.scale) + (row0 + first) * G + (DPL == 4 ? lane : lane / 2) % G;
-#pragma unroll
-          for (int e = 0; e < AHEAD; ++e) scale_ahead[e] = first != ~0u && k0 + e < kn ? s[e * G] : (uint16_t)0;
-        }
       };
       load_v(0);
 #pragma unroll 1
@@ -273,26 +233,16 @@ __global__ void __launch_bounds__(32, simt_per_sm(HD, FORMAT)) k_tree_simt(TreeA
         VBits raw[AHEAD];
 #pragma unroll
         for (int e = 0; e < AHEAD; ++e) raw[e] = ahead[e];
-        float vf[I4 ? AHEAD : 1];
-        if constexpr (I4)
-#pragma unroll
-          for (int e = 0; e < AHEAD; ++e)      // (not finite: 0, and the probability is NaN)
-            vf[e] = (scale_ahead[e] & 0x7f80u) == 0x7f80u ? 0.f : __uint_as_float((uint32_t)scale_ahead[e] << 16);
         if (k0 + AHEAD < kn) load_v(k0 + AHEAD);
 #pragma unroll
         for (int e = 0; e < AHEAD; e += 4) {
           float x[4][DPL];
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            if constexpr (I4) {
-              float y[4];
-              i4x4_to_f32(raw[e + i], vf[e + i], y);
-#pragma unroll
-              for (int d = 0; d < DPL; ++d) x[i][d] = y[d];
-            } else if constexpr (DPL == 4 && F8) {
-              decode4<kF8>(raw[e + i], 0u, x[i]);
+            if constexpr (DPL == 4 && F8) {
+              decode4<true>(raw[e + i], 0u, x[i]);
             } else if constexpr (DPL == 4) {
-              decode4<kBF16>(raw[e + i].x, raw[e + i].y, x[i]);
+              decode4<false>(raw[e + i].x, raw[e + i].y, x[i]);
             } else if constexpr (F8) {
               const float2 y = f8x2_to_f32(raw[e + i]);
               x[i][0] = y.x; x[i][1] = y.y;
@@ -323,11 +273,6 @@ __global__ void __launch_bounds__(32, simt_per_sm(HD, FORMAT)) k_tree_simt(TreeA
     const bool whole = s.c0 == 0 && s.c1 == s.units;
     const size_t slot = (size_t)blockIdx.x * 2 + (s.c0 == 0);
     const int live = min(SQ, a.T * a.G - s.qb * SQ);
-    int d0 = lane * DPL;                       // this lane's first dimension
-    if constexpr (I4) {
-      const int piece = DPL == 4 ? lane : lane / 2;
-      d0 = piece % G * kGroup + piece / G * 4 + (DPL == 4 ? 0 : lane % 2 * 2);
-    }
 #pragma unroll
     for (int v = 0; v < SQ; ++v) {
       const bool any = v < s.nq;               // (a vector past the nodes: zeros)
@@ -342,11 +287,11 @@ __global__ void __launch_bounds__(32, simt_per_sm(HD, FORMAT)) k_tree_simt(TreeA
         if (whole) {
           const Vec w = vector_of(a, s.h, s.qb, v);
 #pragma unroll
-          for (int i = 0; i < DPL; ++i) store_out<T>(a, s.b, w, d0 + i, sum == 0.f ? 0.f : x[i] / sum);
+          for (int i = 0; i < DPL; ++i) store_out<T>(a, s.b, w, lane * DPL + i, sum == 0.f ? 0.f : x[i] / sum);
           if (lane == 0) store_lse(a, s.b, w, m, sum);
         } else {
 #pragma unroll
-          for (int i = 0; i < DPL; ++i) a.part_o[(slot * SQ + v) * HD + d0 + i] = any ? x[i] : 0.f;
+          for (int i = 0; i < DPL; ++i) a.part_o[(slot * SQ + v) * HD + lane * DPL + i] = any ? x[i] : 0.f;
           if (lane == 0) {
             a.part_ml[(slot * 2) * SQ + v] = m;
             a.part_ml[(slot * 2 + 1) * SQ + v] = sum;
@@ -494,14 +439,14 @@ void bytes_of(const Cache& c, Sizes* z) {
 void sizes_of(const Cache& c, bool tc, int H, int T, Sizes* z) {   // tc: bf16 queries
   const int vectors = T * (H / c.kvh);
   if (c.format == kI4) {
-    z->NQ = vectors <= 8 || !tc ? 8 : 16;
+    z->NQ = vectors <= 8 || !tc ? 8 : vectors <= 16 ? 16 : kRowsBlock;
     z->QB = (vectors + z->NQ - 1) / z->NQ;
-    z->blocks = kPlanSMs * i4_blocks_per_sm(c, z->NQ, !tc);
+    z->blocks = kPlanSMs * (z->NQ == kRowsBlock ? 1 : i4_blocks_per_sm(c, z->NQ, !tc));
     return bytes_of(c, z);
   }
   z->NQ = !tc ? SQ : vectors <= 16 ? 16 : vectors <= 32 ? 32 : kRowsBlock;
   z->QB = (vectors + z->NQ - 1) / z->NQ;
-  z->blocks = kPlanSMs * (!tc ? simt_per_sm(c.hd, c.format) : z->NQ == kRowsBlock ? 1 : tc_blocks_per_sm(c, z->NQ));
+  z->blocks = kPlanSMs * (!tc ? simt_per_sm(c.hd, c.format == kF8) : z->NQ == kRowsBlock ? 1 : tc_blocks_per_sm(c, z->NQ));
   bytes_of(c, z);
 }
 
@@ -513,18 +458,18 @@ cudaError_t launch_combine(const TreeArgs& a, cudaStream_t s) {
                     dim3(32 * kCombine), 0, s, a);
 }
 
-template <typename T, int HD, int FORMAT>
+template <typename T, int HD, bool F8>
 cudaError_t launch_simt(const TreeArgs& a, cudaStream_t s) {
-  return launch_pdl(k_tree_simt<T, HD, FORMAT>, dim3(a.blocks), dim3(32), plan_bytes(a.c.batch), s, a);
+  return launch_pdl(k_tree_simt<T, HD, F8>, dim3(a.blocks), dim3(32), plan_bytes(a.c.batch), s, a);
 }
 
 cudaError_t launch_pass(const TreeArgs& a, bool tc, bool split, cudaStream_t s) {
   const bool d128 = a.c.hd == 128, f8 = a.c.format == kF8, bf16 = a.dtype == CDSL_DTYPE_BF16;
   cudaError_t e;
-  if (a.c.format == kI4) e = launch_tree_i4(a, s);
+  if (a.c.format == kI4 && a.NQ < kRowsBlock) e = launch_tree_i4(a, s);
   else if (tc) e = a.NQ == kRowsBlock ? launch_tree_rows(a, s) : launch_tree_tc(a, s);
-  else if (d128) e = f8 ? launch_simt<float, 128, kF8>(a, s) : launch_simt<float, 128, kBF16>(a, s);
-  else e = f8 ? launch_simt<float, 64, kF8>(a, s) : launch_simt<float, 64, kBF16>(a, s);
+  else if (d128) e = f8 ? launch_simt<float, 128, true>(a, s) : launch_simt<float, 128, false>(a, s);
+  else e = f8 ? launch_simt<float, 64, true>(a, s) : launch_simt<float, 64, false>(a, s);
   if (e != cudaSuccess || !split) return e;
   if (bf16) return d128 ? launch_combine<__nv_bfloat16, 128>(a, s) : launch_combine<__nv_bfloat16, 64>(a, s);
   return d128 ? launch_combine<float, 128>(a, s) : launch_combine<float, 64>(a, s);
@@ -599,7 +544,7 @@ extern "C" int32_t cdsl_tree_attention(const cdsl_kv_cache* cache, int32_t layer
   if (!ck.aligned(d_workspace, 256) || workspace_bytes < z.bytes)
     return ck.fail("the workspace must be 256-byte aligned and hold cdsl_tree_attention_workspace bytes",
                    workspace_bytes < z.bytes ? CDSL_ENOMEM : CDSL_EINVAL);
-  const int unit_shift = c.format == kI4 ? 6 : 7;
+  const int unit_shift = c.format == kI4 && z.NQ < kRowsBlock ? 6 : 7;
   static_assert(kKeys == 1 << 7);
   const long long chunks = ((long long)max_len + T + (1 << unit_shift) - 1) >> unit_shift;
   const long long units = chunks * c.batch * c.kvh * z.QB;   // at most

@@ -68,10 +68,13 @@ constexpr float kUp = 7.f;                     // stored times 2^kUp: below fp16
 constexpr int kBuf = 3;                        // S (then P) buffers in TMEM; O has the rest
 constexpr int kVRoom = 6;                      // octaves that V's scales may pass their reference by: 448 * 2^6 in fp16,
 constexpr int kVBelow = 15;                    // and lie below it: 2^-9 * 2^-15
+constexpr int kVBelow4 = 17;                   // 4 bits: a scale / 16 has its last bit at 2^-24 then
 
-template <int HD, bool F8>
+template <int HD, int FORMAT>
 struct Cfg {
-  static constexpr int EB = F8 ? 1 : 2;
+  static constexpr bool F8 = FORMAT == kF8, I4 = FORMAT == kI4;
+  static constexpr bool TURNED = FORMAT != kBF16;          // V is turned into 16 bits
+  static constexpr int EB = F8 ? 1 : 2;                    // I4: of K's tile
   static constexpr int KROW = HD * EB;                     // bytes of a K or V row
   static constexpr int BW = KROW < 128 ? KROW : 128;       // of it per tile block
   static constexpr int NB = KROW / BW;
@@ -79,24 +82,108 @@ struct Cfg {
   static constexpr uint32_t TILE = NB * BLOCK;             // K or V of a chunk
   static constexpr int QP = F8 ? 2 : 1;
   static constexpr uint32_t Q_PLANE = kRows * KROW;
-  // e4m3: V of two chunks in fp16, in blocks of 64 dimensions
-  static constexpr uint32_t H_BLOCK = kKeys * 128, H_TILE = F8 ? HD / 64 * H_BLOCK : 0;
+  // e4m3 and 4 bits: V of two chunks in fp16, in blocks of 64 dimensions
+  static constexpr uint32_t H_BLOCK = kKeys * 128, H_TILE = TURNED ? HD / 64 * H_BLOCK : 0;
   static constexpr uint32_t H_OFF = QP * Q_PLANE;
-  static constexpr uint32_t KV_OFF = H_OFF + 2 * H_TILE;
-  static constexpr int FIT = (208 * 1024 - KV_OFF) / (2 * TILE);
+  // 4 bits: K of two chunks in bf16
+  static constexpr uint32_t KT_OFF = H_OFF + 2 * H_TILE;
+  static constexpr uint32_t KV_OFF = KT_OFF + (I4 ? 2 * TILE : 0);
+  // the ring: K's and V's rows; 4 bits: with their scales
+  static constexpr int RB = HD / 2, SB = HD / kGroup * 2;
+  static constexpr uint32_t PACKED = kKeys * (RB + SB), HALF = I4 ? PACKED : TILE;
+  static constexpr int FIT = (208 * 1024 - KV_OFF) / (2 * HALF);
   static constexpr int NST = FIT > 4 ? 4 : FIT;
   static_assert(NST >= 2, "stages");
-  static constexpr uint32_t SCALE_OFF = KV_OFF + NST * 2 * TILE;
+  static constexpr uint32_t SCALE_OFF = KV_OFF + NST * 2 * HALF;
   // K's scale of each slot, and V's, e4m3: relative to its reference (0: nothing, or not finite)
-  static constexpr uint32_t FACTOR_OFF = SCALE_OFF + NST * 2 * kKeys;
-  static constexpr uint32_t PLAN_OFF = FACTOR_OFF + NST * 2 * kKeys * 4;
+  static constexpr uint32_t FACTOR_OFF = SCALE_OFF + (I4 ? 0 : NST * 2 * kKeys);
+  static constexpr uint32_t PLAN_OFF = FACTOR_OFF + (I4 ? 0 : NST * 2 * kKeys * 4);
   static constexpr size_t smem(int batch) { return 1024 + PLAN_OFF + plan_bytes(batch); }
 };
 
-template <int HD, bool F8>
+// The loading warp of a 4-bit cache: load_chunks with plain bulk copies, a page piece's codes and scales each, scales behind
+// the codes.
+template <int HD, int NST>
+__device__ __forceinline__ void load_packed(const TreeArgs& a, const int* first, int begin, int end, uint8_t* ring,
+                                            uint32_t* s_pieces, uint64_t* k_full, uint64_t* v_full, uint64_t* k_empty,
+                                            uint64_t* v_empty) {
+  using C = Cfg<HD, kI4>;
+  const Cache& c = a.c;
+  const int lane = threadIdx.x & 31, P = 1 << c.page_shift;
+  const int rows = min(P, kKeys), pieces = kKeys / rows;
+  int issued[2] = {0, 0}, it = 0;
+  bool ok = true;
+#pragma unroll 1
+  for (int unit = begin; unit < end && ok;) {
+    const Segment s = segment_at(a, first, unit, end);
+#pragma unroll 1
+    for (int ch = s.c0; ch < s.c1 && ok; ++ch, ++it) {
+      const int slot = ch * kKeys + lane * rows, st = it % NST;
+      int page = -1;
+      if (lane < pieces && slot < s.keys) {
+        page = page_of(c, s.b, slot);
+        if (page < 0) set_status(a.status, CDSL_ERANGE);
+      }
+      const uint32_t live = __ballot_sync(0xffffffffu, page >= 0);
+#pragma unroll
+      for (int kv = 0; kv < 2 && ok; ++kv) {
+        uint64_t* const full = kv ? &v_full[st] : &k_full[st];
+        ok = __all_sync(0xffffffffu, wait_for(kv ? &v_empty[st] : &k_empty[st], parity(it, NST) ^ 1, a.status));
+        if (!ok) break;
+        if (lane == 0) {
+          if (kv) s_pieces[st] = live;
+          tc::mbar_expect_tx(full, __popc(live) * rows * (C::RB + C::SB));
+        }
+        __syncwarp();
+        if (page >= 0) {
+          const size_t row = row_of(c, a.layer, page, kv, s.h, slot & (P - 1));
+          uint8_t* const to = ring + (st * 2 + kv) * C::PACKED;
+          tc::bulk_load(to + lane * rows * C::RB, c.pool + row * C::RB, rows * C::RB, full);
+          tc::bulk_load(to + kKeys * C::RB + lane * rows * C::SB, c.scale + row * C::SB, rows * C::SB, full);
+        }
+        issued[kv] = it + 1;
+      }
+    }
+    unit += s.c1 - s.c0;
+  }
+  // where a role gave up, nothing may have waited for the copies
+  if (!ok)
+#pragma unroll
+    for (int kv = 0; kv < 2; ++kv)
+#pragma unroll 1
+      for (int n = issued[kv], i = max(0, n - NST); i < n; ++i)
+        wait_for(kv ? &v_full[i % NST] : &k_full[i % NST], parity(i, NST), a.status);
+}
+
+// Code I of both halves of a word of codes (low half: one group's, high half: the next one's) times their scales: in bf16 as
+// (128 + 8 u) scale / 8 - 24 scale, u = code + 8, and in fp16 as (1024 + 16 u) scale / 16 - 72 scale. Exact.
+template <int I>
+__device__ __forceinline__ uint32_t word_bf16(uint32_t w, uint32_t s8, uint32_t m24) {
+  const uint32_t t = I == 0 ? w << 3 : w >> (4 * I - 3);
+  const uint32_t x = (t & 0x00780078u) ^ 0x43404340u;
+  uint32_t d;
+  asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(x), "r"(s8), "r"(m24));
+  return d;
+}
+template <int I>
+__device__ __forceinline__ uint32_t word_f16(uint32_t w, uint32_t s16, uint32_t m72) {
+  const uint32_t t = I == 0 ? w << 4 : w >> (4 * I - 4);
+  const uint32_t x = (t & 0x00f000f0u) ^ 0x64806480u;
+  uint32_t d;
+  asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(x), "r"(s16), "r"(m72));
+  return d;
+}
+__device__ __forceinline__ uint32_t times_bf16(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+
+template <int HD, int FORMAT>
 __global__ void __launch_bounds__(kThreads, 1)
     k_tree_rows(TreeArgs a, const __grid_constant__ CUtensorMap map) {
-  using C = Cfg<HD, F8>;
+  using C = Cfg<HD, FORMAT>;
+  constexpr bool F8 = C::F8, I4 = C::I4, TURNED = C::TURNED;
   constexpr int NST = C::NST;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* const sm = smem_raw + ((1024 - (tc::smem_u32(smem_raw) & 1023)) & 1023);
@@ -104,6 +191,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   __shared__ __align__(8) uint64_t k_full[NST], v_full[NST], k_empty[NST], v_empty[NST];
   __shared__ __align__(8) uint64_t f_full[NST], f_empty[NST], h_full[2];
   __shared__ __align__(8) uint64_t s_full[kBuf], p_full[kBuf], r_full[kBuf], pv_done[2], q_full, done;
+  __shared__ __align__(8) uint64_t kt_full[2], kt_empty[2];   // 4 bits: K's tiles
   __shared__ uint32_t s_tmem;
   __shared__ __align__(16) uint32_t s_valid[NST][4], s_nan[NST][4];   // slots that there are, whose V is not finite
   __shared__ int s_kind[NST], s_h_far[2];      // a chunk's: bit 0 has masks, 1 V's scales far apart (bf16: not 1); V's buffers'
@@ -121,8 +209,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (int i = 0; i < NST; ++i) {
       tc::mbar_init(&k_full[i], 1);
       tc::mbar_init(&v_full[i], 1);
-      tc::mbar_init(&k_empty[i], F8 ? 1 : 2);  // (the scale bytes' reader arrives where they came)
-      tc::mbar_init(&v_empty[i], F8 ? kConv + 1 : 1);
+      tc::mbar_init(&k_empty[i], I4 ? kConv : F8 ? 1 : 2);   // (the scale bytes' reader arrives where they came)
+      tc::mbar_init(&v_empty[i], TURNED ? kConv + 1 : 1);
       tc::mbar_init(&f_full[i], 32);
       tc::mbar_init(&f_empty[i], kRows);
     }
@@ -135,6 +223,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     for (int i = 0; i < 2; ++i) {
       tc::mbar_init(&h_full[i], kConv);
+      tc::mbar_init(&kt_full[i], kConv);
+      tc::mbar_init(&kt_empty[i], 1);
       tc::mbar_init(&pv_done[i], 1);
     }
     tc::mbar_init(&q_full, kSoft);
@@ -142,7 +232,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     tc::fence_mbar_init();
   }
   if (warp == kIssuer) tc::tmem_alloc(&s_tmem, 512);
-  if (warp == kProducer && lane == 0) tc::tma_prefetch_map(&map);
+  if (!I4 && warp == kProducer && lane == 0) tc::tma_prefetch_map(&map);
   pdl_wait();
   pdl_launch_dependents();
   tc::tc_fence_before();
@@ -156,8 +246,11 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t t_o = tmem + kBuf * kKeys;
 
   if (warp == kProducer) {
-    load_chunks<HD, F8, NST, !F8>(a, s_first, begin, end, map, sm + C::KV_OFF, sm + C::SCALE_OFF, s_pieces, k_full,
-                             v_full, k_empty, v_empty);
+    if constexpr (I4)
+      load_packed<HD, NST>(a, s_first, begin, end, sm + C::KV_OFF, s_pieces, k_full, v_full, k_empty, v_empty);
+    else
+      load_chunks<HD, F8, NST, !F8>(a, s_first, begin, end, map, sm + C::KV_OFF, sm + C::SCALE_OFF, s_pieces, k_full,
+                                    v_full, k_empty, v_empty);
   } else if (warp == kIssuer) {
     if (lane == 0) {
       constexpr uint32_t formats = F8 ? 0u : (1u << 7) | (1u << 10);
@@ -168,13 +261,14 @@ __global__ void __launch_bounds__(kThreads, 1)
       constexpr uint32_t idesc_bf16 = idesc_half | (1u << 7) | (1u << 10);
       const uint32_t sbase = tc::smem_u32(sm);
       const uint64_t desc_q = tc::desc_rows(sbase, C::BW, 16);
-      const uint64_t desc_k = tc::desc_rows(sbase + C::KV_OFF, C::BW, 16);
-      const uint64_t desc_v = F8 ? tc::desc_rows(sbase + C::H_OFF, 128, C::H_BLOCK)
+      const uint64_t desc_k = tc::desc_rows(sbase + (I4 ? C::KT_OFF : C::KV_OFF), C::BW, 16);
+      const uint64_t desc_v = TURNED ? tc::desc_rows(sbase + C::H_OFF, 128, C::H_BLOCK)
                                  : tc::desc_rows(sbase + C::KV_OFF + C::TILE, C::BW, C::BLOCK);
       auto s_mma = [&](int i) {                // S of chunk i
-        if (!wait_for(&k_full[i % NST], parity(i, NST), a.status)) return false;
+        if (!(I4 ? wait_for(&kt_full[i & 1], parity(i, 2), a.status) : wait_for(&k_full[i % NST], parity(i, NST), a.status)))
+          return false;
         tc::tc_fence_after();
-        const uint64_t k = desc_k + (uint32_t)(i % NST) * (2 * C::TILE / 16);
+        const uint64_t k = desc_k + (I4 ? (uint32_t)(i & 1) * (C::TILE / 16) : (uint32_t)(i % NST) * (2 * C::TILE / 16));
 #pragma unroll 1
         for (int p = C::QP - 1; p >= 0; --p)
 #pragma unroll 1
@@ -188,17 +282,17 @@ __global__ void __launch_bounds__(kThreads, 1)
               else tc::umma_bf16(tmem + i % kBuf * kKeys, q, kk, idesc_s, add);
             }
         tc::umma_commit(&s_full[i % kBuf]);
-        tc::umma_commit(&k_empty[i % NST]);
+        tc::umma_commit(I4 ? &kt_empty[i & 1] : &k_empty[i % NST]);
         return true;
       };
       auto pv = [&](int i, bool add) {         // P V of chunk i
-        if (!(F8 ? wait_for(&h_full[i & 1], parity(i, 2), a.status)
+        if (!(TURNED ? wait_for(&h_full[i & 1], parity(i, 2), a.status)
                  : wait_for(&v_full[i % NST], parity(i, NST), a.status)))
           return false;
-        const bool planes = !F8 || s_h_far[i & 1];
+        const bool planes = !TURNED || s_h_far[i & 1];
         if (!wait_for(&p_full[i % kBuf], parity(i, kBuf), a.status)) return false;
         tc::tc_fence_after();
-        const uint64_t v = desc_v + (F8 ? (uint32_t)(i & 1) * (C::H_TILE / 16) : (uint32_t)(i % NST) * (2 * C::TILE / 16));
+        const uint64_t v = desc_v + (TURNED ? (uint32_t)(i & 1) * (C::H_TILE / 16) : (uint32_t)(i % NST) * (2 * C::TILE / 16));
         // 16 slots an MMA: 8 columns of P, 16 rows of 128 bytes of V. P of 32 slots lies in the columns that held
         // their S, bf16 hi then lo.
         const auto plane = [&](int p, uint32_t idesc, bool add) {
@@ -214,7 +308,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           for (int p = 1; p >= 0; --p) plane(p, idesc_bf16, add || p < 1);
         }
         tc::umma_commit(&pv_done[i & 1]);
-        if (!F8) tc::umma_commit(&v_empty[i % NST]);
+        if (!TURNED) tc::umma_commit(&v_empty[i % NST]);
         return true;
       };
       bool ok = true;
@@ -244,15 +338,45 @@ __global__ void __launch_bounds__(kThreads, 1)
       int vref = 0;
       for (int ch = s.c0; ch < s.c1 && ok; ++ch, ++it) {
         const int st = it % NST;
-        ok = __all_sync(0xffffffffu, wait_for(F8 ? &v_full[st] : &k_full[st], parity(it, NST), a.status) &&
+        ok = __all_sync(0xffffffffu, wait_for(TURNED ? &v_full[st] : &k_full[st], parity(it, NST), a.status) &&
                                          wait_for(&f_empty[st], parity(it, NST) ^ 1, a.status));
         if (!ok) break;
         // a lane has slots 4 lane .. 4 lane + 3
-        const uint8_t* from = sm + C::SCALE_OFF + st * 2 * kKeys + 4 * lane;
-        const uint32_t kb = *reinterpret_cast<const uint32_t*>(from), vb = *reinterpret_cast<const uint32_t*>(from + kKeys);
         const int slot = ch * kKeys + 4 * lane;
         const bool piece = s_pieces[st] >> (4 * lane >> min(c.page_shift, 7)) & 1;
         const int n = piece ? min(max(s.keys - slot, 0), 4) : 0;   // of them that there are
+        const int before = vref;
+        float kf[4], vf[4];
+        uint32_t nan = 0;
+        bool far = false, masks = n < 4 || slot + 3 >= s.len;   // slots past the item's, without a page or of the tree
+        if constexpr (I4) {
+          // exponents of a row's scales, the largest and the smallest (the converting warps take the scales themselves)
+          constexpr int G2 = HD / kGroup / 2;
+          const uint32_t* const from = reinterpret_cast<const uint32_t*>(sm + C::KV_OFF + (st * 2 + 1) * C::PACKED + kKeys * C::RB) + 4 * lane * G2;
+          int most[4], least[4], vmax = 0;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            most[e] = 0;
+            least[e] = 255;
+#pragma unroll
+            for (int i = 0; i < G2; ++i) {
+              const int lo = from[e * G2 + i] >> 7 & 255, hi = from[e * G2 + i] >> 23 & 255;
+              most[e] = max(most[e], max(lo, hi));
+              least[e] = min(least[e], min(lo, hi));
+            }
+            if (e < n && most[e] != 255) vmax = max(vmax, most[e]);
+          }
+          vmax = __reduce_max_sync(0xffffffffu, vmax);
+          if (vref == 0 || vmax > vref + kVRoom) vref = vmax;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            nan |= (uint32_t)(e < n && most[e] == 255) << e;
+            masks = masks || (e < n && most[e] == 255);
+            far = far || (e < n && most[e] != 255 && least[e] < vref - kVBelow4);
+          }
+        } else {
+        const uint8_t* from = sm + C::SCALE_OFF + st * 2 * kKeys + 4 * lane;
+        const uint32_t kb = *reinterpret_cast<const uint32_t*>(from), vb = *reinterpret_cast<const uint32_t*>(from + kKeys);
         int vmax = 0;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -260,11 +384,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (e < n && x != 255) vmax = max(vmax, x);
         }
         vmax = __reduce_max_sync(0xffffffffu, vmax);
-        const int before = vref;
         if (vref == 0 || vmax > vref + kVRoom) vref = vmax;
-        float kf[4], vf[4];
-        uint32_t nan = 0;
-        bool far = false, masks = n < 4 || slot + 3 >= s.len;   // slots past the item's, without a page or of the tree
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const uint32_t k = kb >> (8 * e) & 255, v = vb >> (8 * e) & 255;
@@ -275,11 +395,14 @@ __global__ void __launch_bounds__(kThreads, 1)
           masks = masks || (e < n && v == 255);
           far = far || (e < n && v != 255 && (F8 ? v > 0 && x < 127 - kVBelow : v != 127));
         }
+        }
         far = __any_sync(0xffffffffu, far);
         masks = __any_sync(0xffffffffu, masks);
-        float* to = reinterpret_cast<float*>(sm + C::FACTOR_OFF) + st * 2 * kKeys + 4 * lane;
-        *reinterpret_cast<float4*>(to) = make_float4(kf[0], kf[1], kf[2], kf[3]);
-        *reinterpret_cast<float4*>(to + kKeys) = make_float4(vf[0], vf[1], vf[2], vf[3]);
+        if constexpr (!I4) {
+          float* to = reinterpret_cast<float*>(sm + C::FACTOR_OFF) + st * 2 * kKeys + 4 * lane;
+          *reinterpret_cast<float4*>(to) = make_float4(kf[0], kf[1], kf[2], kf[3]);
+          *reinterpret_cast<float4*>(to + kKeys) = make_float4(vf[0], vf[1], vf[2], vf[3]);
+        }
         uint32_t valid = ((1u << n) - 1) << (4 * (lane & 7));       // eight lanes a word
         nan <<= 4 * (lane & 7);
 #pragma unroll
@@ -292,16 +415,16 @@ __global__ void __launch_bounds__(kThreads, 1)
           s_nan[st][lane >> 3] = nan;
         }
         if (lane == 0) {
-          s_vref[st] = F8 ? vref : 127;
-          s_vstep[st] = F8 && before ? before - vref : 0;
+          s_vref[st] = TURNED ? vref : 127;
+          s_vstep[st] = TURNED && before ? before - vref : 0;
           s_kind[st] = masks | far << 1;
         }
         __syncwarp();
-        if (lane == 0) tc::mbar_arrive(F8 ? &v_empty[st] : &k_empty[st]);   // (the scale bytes are read)
-        if (!F8 && __any_sync(0xffffffffu, n < 4))
+        if (lane == 0) tc::mbar_arrive(TURNED ? &v_empty[st] : &k_empty[st]);   // (the scale bytes are read)
+        if (!TURNED && __any_sync(0xffffffffu, n < 4))
           ok = __all_sync(0xffffffffu, wait_for(&v_full[st], parity(it, NST), a.status));
         if (!ok) break;
-        if (!F8 && n < 4) {                    // nothing of their V rows (page garbage, no copy) may reach the sums
+        if (!TURNED && n < 4) {                    // nothing of their V rows (page garbage, no copy) may reach the sums
 #pragma unroll 1
           for (int e = n; e < 4; ++e) {
             uint8_t* v = sm + C::KV_OFF + (st * 2 + 1) * C::TILE + (4 * lane + e) * C::BW;
@@ -326,7 +449,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     int it0 = 0, buf = 0;
     bool failed = false;
     const auto stage = [&](const Segment& s, int to) {   // a segment's queries and masks
-      stage_queries<HD, kRows, F8, kSoft, true>(a, s, tid, q_aligned, sm, [&](int v, const Vec&, float qs, bool bad) {
+      stage_queries<HD, kRows, F8, kSoft, true, I4>(a, s, tid, q_aligned, sm, [&](int v, const Vec&, float qs, bool bad) {
         s_qs[to][v] = v < s.nq ? qs : 0.f;
         s_bad[to][v] = bad;
       });
@@ -374,6 +497,11 @@ __global__ void __launch_bounds__(kThreads, 1)
           auto scores = [&](const uint32_t (&x)[16], int g, uint32_t seen, uint64_t (&t)[8]) {
 #pragma unroll
             for (int e = 0; e < 8; e += 2) {
+              if constexpr (I4) {              // (K's tile has the scales)
+                t[e] = pair(x[2 * e], x[2 * e + 1]);
+                t[e + 1] = pair(x[2 * e + 2], x[2 * e + 3]);
+                continue;
+              }
               const ulonglong2 k = *reinterpret_cast<const ulonglong2*>(kf + 16 * g + 2 * e);
               t[e] = mul2(pair(x[2 * e], x[2 * e + 1]), k.x);
               t[e + 1] = mul2(pair(x[2 * e + 2], x[2 * e + 3]), k.y);
@@ -419,7 +547,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (ref != now) l *= ref == -INFINITY ? 1.f : ex2(ref - now);   // (no reference: the sums are 0)
           ref = now;
           float f = was == now || was == -INFINITY ? 1.f : ex2(was - now);
-          if (F8) f *= ex2((float)s_vstep[st]);
+          if (TURNED) f *= ex2((float)s_vstep[st]);
           if (i > 0 && __any_sync(0xffffffffu, f != 1.f)) {
             ok = ok && wait_for(&pv_done[1 - grp], parity(it - 1, 2), a.status);
             tc::tc_fence_after();
@@ -453,7 +581,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const float2 z = unpair(fma2(t[e], qs2, off2));
                 float2 y = make_float2(ex2(z.x), ex2(z.y));
                 add = add2(add, pair(y.x, y.y));
-                if constexpr (far && !F8) {      // (V as it is: its scales, 1 in other chunks)
+                if constexpr (far && !TURNED) {      // (V as it is: its scales, 1 in other chunks)
                   const float2 f = *reinterpret_cast<const float2*>(kf + kKeys + 16 * (2 * w + h) + 2 * e);
                   y = make_float2(y.x * f.x, y.y * f.y);
                 }
@@ -462,7 +590,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                   if (m & 1) y.x = __uint_as_float(0x7fc00000u);
                   if (m & 2) y.y = __uint_as_float(0x7fc00000u);
                 }
-                if constexpr (F8 && !far) {
+                if constexpr (TURNED && !far) {
                   const __half2 p = __floats2half2_rn(y.x, y.y);
                   hi[e] = *reinterpret_cast<const uint32_t*>(&p);
                 } else {
@@ -474,7 +602,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               }
               const uint32_t to = t_s + 32 * w + h * 8;
               tc::tmem_st_nowait(to, hi);
-              if (!F8 || far) tc::tmem_st_nowait(to + 16, lo);
+              if (!TURNED || far) tc::tmem_st_nowait(to + 16, lo);
             }
           }
           const float2 two = unpair(add);
@@ -523,7 +651,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         m = l == 0.f ? -INFINITY : m - kUp;
         const bool whole = now.c0 == 0 && now.c1 == now.units;
         const float inv = l == 0.f ? 0.f : whole ? 1.f / l : 1.f;
-        const float unscale = F8 ? ex2((float)(s_v - 127)) : 1.f;
+        const float unscale = TURNED ? ex2((float)(s_v - 127)) : 1.f;
         const Vec x = vector_of(a, now.h, now.qb, r);
         const size_t part = (size_t)blockIdx.x * 2 + (now.c0 == 0);
         if (grp == 0 && r < rows) {
@@ -543,7 +671,31 @@ __global__ void __launch_bounds__(kThreads, 1)
           tc::tmem_ld16(t_o + lanes + d, o);
 #pragma unroll
           for (int e = 0; e < 16; ++e) o[e] = inv == 0.f ? 0.f : o[e] * unscale * inv;
-          if (r < rows) {
+          if (I4 && r < rows) {
+            // (columns d + 8 w + 2 i + h are dimension 4 j + i of one of two groups)
+            constexpr int PAIRS = HD / kGroup / 2;
+#pragma unroll
+            for (int w = 0; w < 2; ++w)
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                const int W = d / 8 + w, to = (W % PAIRS * 2 + h) * kGroup + W / PAIRS * 4;
+                const float y[4] = {o[8 * w + h], o[8 * w + 2 + h], o[8 * w + 4 + h], o[8 * w + 6 + h]};
+                if (!whole) {
+                  *reinterpret_cast<float4*>(part_o + to) = make_float4(y[0], y[1], y[2], y[3]);
+                } else {
+                  const __nv_bfloat162 z0 = __floats2bfloat162_rn(y[0], y[1]), z1 = __floats2bfloat162_rn(y[2], y[3]);
+                  if (o_aligned) {
+                    *reinterpret_cast<uint2*>(out + to) =
+                        make_uint2(*reinterpret_cast<const uint32_t*>(&z0), *reinterpret_cast<const uint32_t*>(&z1));
+                  } else {
+                    out[to] = z0.x;
+                    out[to + 1] = z0.y;
+                    out[to + 2] = z1.x;
+                    out[to + 3] = z1.y;
+                  }
+                }
+              }
+          } else if (r < rows) {
             if (!whole) {
 #pragma unroll
               for (int e = 0; e < 16; e += 8) {
@@ -575,7 +727,109 @@ __global__ void __launch_bounds__(kThreads, 1)
       sync();                                  // queries, masks, sums and O are free
       it0 += n;
     }
-  } else if (F8) {
+  } else if constexpr (I4) {
+    // ------------------------------------------------------------------------- K to bf16, V to 16 bits
+    // 16 bytes of a row at a time, 8 values of every group, a word (one of each of two groups in turn) to 16 bytes of a
+    // tile; exactly, with the scales. K is a chunk ahead, so that its scores are there when V's are asked for.
+    constexpr int G2 = HD / kGroup / 2, PER = C::RB / 16, kRowsAt = kConv / PER;
+    const int row0 = (threadIdx.x - kSoft) / PER, part = (threadIdx.x - kSoft) % PER;
+    // (words 2, 3 first in the second block of 64 dimensions: eight lanes' stores then meet no bank twice)
+    const int flip = part >> 1 & 1;
+    uint32_t to[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int W = 4 * part + (i ^ flip << 1);
+      to[i] = W / 8 * C::H_BLOCK + tc::row_offset(row0, W % 8, 128);
+    }
+    static_assert(C::BLOCK == C::H_BLOCK && C::BW == 128);
+    const auto words = [&](const uint8_t* half, int k, uint32_t (&w)[4], uint32_t (&sc)[G2]) {
+      const int row = row0 + k * kRowsAt;
+      const uint4 u = *reinterpret_cast<const uint4*>(half + row * C::RB + part * 16);
+      w[0] = flip ? u.z : u.x; w[1] = flip ? u.w : u.y; w[2] = flip ? u.x : u.z; w[3] = flip ? u.y : u.w;
+      const uint8_t* const z = half + kKeys * C::RB + row * C::SB;
+      if constexpr (G2 == 2) {
+        const uint2 y = *reinterpret_cast<const uint2*>(z);
+        sc[0] = y.x; sc[1] = y.y;
+      } else {
+        sc[0] = *reinterpret_cast<const uint32_t*>(z);
+      }
+    };
+    const auto bf16_words = [&](uint8_t* tile, const uint32_t (&w)[4], const uint32_t (&sc)[G2]) {
+      uint32_t s8[G2], m24[G2];
+#pragma unroll
+      for (int i = 0; i < G2; ++i) {
+        s8[i] = times_bf16(sc[i], 0x3e003e00u);                  // 1 / 8
+        m24[i] = times_bf16(s8[i], 0xc340c340u);                 // -192
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<uint4*>(tile + to[i]) =
+            make_uint4(word_bf16<0>(w[i], s8[i % G2], m24[i % G2]), word_bf16<1>(w[i], s8[i % G2], m24[i % G2]),
+                       word_bf16<2>(w[i], s8[i % G2], m24[i % G2]), word_bf16<3>(w[i], s8[i % G2], m24[i % G2]));
+    };
+    const auto turn_k = [&](int i) {
+      const int st = i % NST;
+      if (!__all_sync(0xffffffffu, wait_for(&k_full[st], parity(i, NST), a.status) &&
+                                       wait_for(&kt_empty[i & 1], parity(i, 2) ^ 1, a.status)))
+        return false;
+      const uint8_t* const from = sm + C::KV_OFF + st * 2 * C::PACKED;
+#pragma unroll 2
+      for (int k = 0; k < kKeys / kRowsAt; ++k) {
+        uint32_t w[4], sc[G2];
+        words(from, k, w, sc);
+        bf16_words(sm + C::KT_OFF + (i & 1) * C::TILE + k * (kRowsAt * 128), w, sc);
+      }
+      tc::fence_proxy_async();
+      tc::mbar_arrive(&kt_full[i & 1]);
+      tc::mbar_arrive(&k_empty[st]);
+      return true;
+    };
+    const int n = end - begin;
+    bool ok = n == 0 || turn_k(0);
+    for (int i = 0; i < n && ok; ++i) {
+      if (i + 1 < n && !(ok = turn_k(i + 1))) break;
+      const int st = i % NST;
+      ok = wait_for(&f_full[st], parity(i, NST), a.status) && wait_for(&v_full[st], parity(i, NST), a.status) &&
+           wait_for(&pv_done[i & 1], parity(i, 2) ^ 1, a.status);   // (chunk i - 2's: the buffer is free)
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+      const bool far = s_kind[st] >> 1;
+      if (threadIdx.x == kSoft) s_h_far[i & 1] = far;
+      const uint8_t* const from = sm + C::KV_OFF + (st * 2 + 1) * C::PACKED;
+      uint8_t* const tile = sm + C::H_OFF + (i & 1) * C::H_TILE;
+      const uint32_t rel = (uint32_t)max(254 - s_vref[st], 1) * 0x00800080u;   // 2^-reference
+#pragma unroll 2
+      for (int k = 0; k < kKeys / kRowsAt; ++k) {
+        const int row = row0 + k * kRowsAt;
+        uint32_t w[4], sc[G2];
+        words(from, k, w, sc);
+        const bool there = (s_valid[st][row >> 5] & ~s_nan[st][row >> 5]) >> (row & 31) & 1;
+#pragma unroll
+        for (int e = 0; e < G2; ++e) sc[e] = there ? times_bf16(sc[e], rel) : 0u;
+        uint8_t* const at = tile + k * (kRowsAt * 128);
+        if (!far) {
+          uint32_t s16[G2], m72[G2];
+#pragma unroll
+          for (int e = 0; e < G2; ++e) {
+            const __half2 f = __floats2half2_rn(bf16_at(sc[e], 0), bf16_at(sc[e], 1));
+            const __half2 x = __hmul2(f, __float2half2_rn(0.0625f)), y = __hmul2(f, __float2half2_rn(-72.f));
+            s16[e] = *reinterpret_cast<const uint32_t*>(&x);
+            m72[e] = *reinterpret_cast<const uint32_t*>(&y);
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            *reinterpret_cast<uint4*>(at + to[e]) =
+                make_uint4(word_f16<0>(w[e], s16[e % G2], m72[e % G2]), word_f16<1>(w[e], s16[e % G2], m72[e % G2]),
+                           word_f16<2>(w[e], s16[e % G2], m72[e % G2]), word_f16<3>(w[e], s16[e % G2], m72[e % G2]));
+        } else {
+          bf16_words(at, w, sc);
+        }
+      }
+      tc::fence_proxy_async();
+      tc::mbar_arrive(&h_full[i & 1]);
+      tc::mbar_arrive(&v_empty[st]);
+    }
+  } else if constexpr (F8) {
     // ------------------------------------------------------------------------- V to 16 bits
     // 16 codes at a time, exactly, with the rows' scales; rows that there are not become zeros. fp16, which two
     // instructions a pair give; where V's scales are far apart bf16, in which no scale is too small.
@@ -650,12 +904,13 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (warp == kIssuer) tc::tmem_dealloc(tmem, 512);
 }
 
-template <int HD, bool F8>
+template <int HD, int FORMAT>
 cudaError_t launch(const TreeArgs& a, cudaStream_t s) {
-  using C = Cfg<HD, F8>;
-  CUtensorMap map;
-  if (encode_cache_map<HD, F8>(a, &map)) return cudaErrorInvalidValue;
-  auto k = k_tree_rows<HD, F8>;
+  using C = Cfg<HD, FORMAT>;
+  CUtensorMap map = {};
+  if constexpr (!C::I4)
+    if (encode_cache_map<HD, C::F8>(a, &map)) return cudaErrorInvalidValue;
+  auto k = k_tree_rows<HD, FORMAT>;
   static OncePerDevice once;
   if (const cudaError_t e = allow_shared(once, k, C::smem(CDSL_TREE_MAX_BATCH))) return e;
   return launch_pdl(k, dim3(a.blocks), dim3(kThreads), C::smem(a.c.batch), s, a, map);
@@ -664,8 +919,9 @@ cudaError_t launch(const TreeArgs& a, cudaStream_t s) {
 }  // namespace
 
 cudaError_t launch_tree_rows(const TreeArgs& a, cudaStream_t s) {
-  if (a.c.hd == 128) return a.c.format == kF8 ? launch<128, true>(a, s) : launch<128, false>(a, s);
-  return a.c.format == kF8 ? launch<64, true>(a, s) : launch<64, false>(a, s);
+  if (a.c.format == kI4) return a.c.hd == 128 ? launch<128, kI4>(a, s) : launch<64, kI4>(a, s);
+  if (a.c.hd == 128) return a.c.format == kF8 ? launch<128, kF8>(a, s) : launch<128, kBF16>(a, s);
+  return a.c.format == kF8 ? launch<64, kF8>(a, s) : launch<64, kBF16>(a, s);
 }
 
 }  // namespace tree

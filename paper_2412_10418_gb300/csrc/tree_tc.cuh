@@ -89,8 +89,9 @@ __device__ __forceinline__ void f8x4_half(uint32_t four, __half2* a, __half2* b)
 // blocks of at most 128 bytes. F8: two e4m3 planes of q / 2^e, hi = e4m3(q / 2^e) and lo the rest, e the
 // smallest with which the row's largest value is at most 448; else bf16 as they are. A row that is not finite, and
 // rows past the block's, become zeros. put(v, where, factor of the scores, not finite) once per vector. LIVE: groups
-// of NT / 8 vectors that are all past the block's are left out.
-template <int HD, int NQ, bool F8, int NT, bool LIVE, typename F>
+// of NT / 8 vectors that are all past the block's are left out. I4: bf16 with a row's dimensions in the order in which a
+// 4-bit cache's words give them: 16 bytes W are those of codes 8 W .., one of each of two groups in turn.
+template <int HD, int NQ, bool F8, int NT, bool LIVE, bool I4 = false, typename F>
 __device__ __forceinline__ void stage_queries(const TreeArgs& a, const Segment& s, int tid, bool q_aligned,
                                               uint8_t* q_smem, F&& put) {
   constexpr int QE = HD / 8;                   // values per thread
@@ -110,8 +111,28 @@ __device__ __forceinline__ void stage_queries(const TreeArgs& a, const Segment& 
     if (v < s.nq) {
       const Vec x = vector_of(a, s.h, s.qb, v);
       const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(a.q) + s.b * a.sq[0] + x.t * a.sq[1] +
-                               x.h * a.sq[2] + tid % 8 * QE;
-      if (q_aligned) {
+                               x.h * a.sq[2] + (I4 ? 0 : tid % 8 * QE);
+      if constexpr (I4) {
+        constexpr int PAIRS = HD / kGroup / 2; // of groups
+#pragma unroll
+        for (int i = 0; i < QE / 8; ++i) {
+          const int W = tid % 8 * (QE / 8) + i;
+          const __nv_bfloat16* const lo = q + W % PAIRS * 2 * kGroup + W / PAIRS * 4;
+          uint32_t l[2], h[2];                 // four dimensions of each group
+          if (q_aligned) {
+            const uint2 u = *reinterpret_cast<const uint2*>(lo), z = *reinterpret_cast<const uint2*>(lo + kGroup);
+            l[0] = u.x; l[1] = u.y; h[0] = z.x; h[1] = z.y;
+          } else {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              l[e] = __bfloat16_as_ushort(lo[2 * e]) | (uint32_t)__bfloat16_as_ushort(lo[2 * e + 1]) << 16;
+              h[e] = __bfloat16_as_ushort(lo[kGroup + 2 * e]) | (uint32_t)__bfloat16_as_ushort(lo[kGroup + 2 * e + 1]) << 16;
+            }
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) next[4 * i + e] = __byte_perm(l[e / 2], h[e / 2], e % 2 ? 0x7632 : 0x5410);
+        }
+      } else if (q_aligned) {
 #pragma unroll
         for (int i = 0; i < QE / 8; ++i) {
           const uint4 u = *reinterpret_cast<const uint4*>(q + 8 * i);
