@@ -181,18 +181,28 @@ CDSL_API int32_t cdsl_kv_compact(const cdsl_kv_cache* cache, const int32_t* d_re
 CDSL_API int32_t cdsl_rope_turns(int32_t rot, double theta, double factor, int32_t original_len, double low, double high,
                                  uint64_t* h_turns);
 
+typedef struct cdsl_rope_cfg {
+  const uint64_t* d_turns;                /* rot / 2 words of cdsl_rope_turns, on the device */
+  int32_t rot;
+  int32_t interleaved;                    /* pairs: 0: i and i + rot / 2; else 2 i and 2 i + 1 */
+  float magnitude;
+} cdsl_rope_cfg;
+/* q and k [batch, T, heads, head_dim] (2 .. 1024) of dtype CDSL_DTYPE_F32 or CDSL_DTYPE_BF16; strides: elements between
+ * sequences, tokens and heads of q, q's output, k and k's output (a head's values are contiguous). */
+typedef struct cdsl_rope_rows {
+  int32_t dtype, batch, T, head_dim, n_heads, n_kv_heads;
+  int64_t strides[12];
+} cdsl_rope_rows;
+
 /* Each head's first rot dimensions turn with the token's position d_start[b] + d_offset[b, t] (d_offset [batch, T], as
  * cdsl_tree_mask's depths; NULL: t), exactly so for any positions:
- *   (x_i, x_j) -> magnitude * (x_i cos - x_j sin, x_j cos + x_i sin),  j = i + rot / 2; interleaved: 2 i and 2 i + 1
- * and the rest of the head stays. inverse: the other way (sin negated, magnitude as it is), which turns the outputs'
- * gradients into the inputs'. q, and k (NULL: none), [batch, T, heads, head_dim] of `dtype` (CDSL_DTYPE_F32 or
- * CDSL_DTYPE_BF16), computed in fp32; h_strides[12]: elements between sequences, tokens and heads of q, q's output, k and
- * k's output (a head's values are contiguous). An output may be its input. d_turns: rot / 2 words of
- * cdsl_rope_turns. head_dim: 2 .. 1024. */
-CDSL_API int32_t cdsl_rope(const uint64_t* d_turns, int32_t rot, int32_t interleaved, int32_t inverse, float magnitude,
-                           int32_t dtype, int32_t batch, int32_t T, int32_t head_dim, const void* d_q, void* d_q_out,
-                           int32_t n_heads, const void* d_k, void* d_k_out, int32_t n_kv_heads, const int64_t* h_strides,
-                           const int32_t* d_start, const int32_t* d_offset, void* stream);
+ *   (x_i, x_j) -> magnitude * (x_i cos - x_j sin, x_j cos + x_i sin)
+ * and the rest of the head stays; computed in fp32. inverse: the other way (sin negated, magnitude as it is), which turns
+ * the outputs' gradients into the inputs'. k may be NULL (with its output: none). An output may be its input. Both
+ * structures are read before the call returns. */
+CDSL_API int32_t cdsl_rope(const cdsl_rope_cfg* rope, int32_t inverse, const cdsl_rope_rows* rows, const void* d_q,
+                           void* d_q_out, const void* d_k, void* d_k_out, const int32_t* d_start,
+                           const int32_t* d_offset, void* stream);
 
 /* Validation of each sequence's tree by M_p (Sec. 3.2.2): walk from node 0 to a child that M_p takes,
  * and so on; at the node where no child is taken (or there is none) draw the next token. Row

@@ -86,7 +86,7 @@ EXPORTS = {
     "cdsl_kv_resize": (_I, [_P, _P, _P, _P, _P, _P, ctypes.c_size_t, _P, _P]),
     "cdsl_kv_compact": (_I, [_P, _P, _P, _P, _P, _P, _P, ctypes.c_size_t, _P, _P]),
     "cdsl_rope_turns": (_I, [_I, ctypes.c_double, ctypes.c_double, _I, ctypes.c_double, ctypes.c_double, _P]),
-    "cdsl_rope": (_I, [_P, _I, _I, _I, ctypes.c_float, _I, _I, _I, _I, _P, _P, _I, _P, _P, _I, _P, _P, _P, _P]),
+    "cdsl_rope": (_I, [_P, _I, _P, _P, _P, _P, _P, _P, _P, _P]),
     "cdsl_last_error": (ctypes.c_char_p, [_P]),
     "cdsl_destroy": (None, [_P]),
 }
@@ -539,7 +539,21 @@ class Rope:
             _bad("Rope", "magnitude must be positive and finite")
         self.rot, self.interleaved, self.magnitude = rot, int(bool(interleaved)), magnitude
         self.turns = turns.to(device)
-        self._ptr = self.turns.data_ptr()
+        self.device = self.turns.device
+        self._c = _RopeC(self.turns.data_ptr(), rot, self.interleaved, magnitude)
+        self._ref = ctypes.addressof(self._c)
+
+
+class _RopeC(ctypes.Structure):
+    _fields_ = [("d_turns", _P), ("rot", _I), ("interleaved", _I), ("magnitude", ctypes.c_float)]
+
+
+class _RopeRows(ctypes.Structure):
+    _fields_ = [("dtype", _I), ("batch", _I), ("T", _I), ("head_dim", _I), ("n_heads", _I), ("n_kv_heads", _I),
+                ("strides", ctypes.c_int64 * 12)]
+
+
+_rope_rows: dict = {}
 
 
 def cdsl_rope(rope: Rope, q, q_out, start, *, k=None, k_out=None, offset=None, inverse: bool = False, stream=None):
@@ -547,27 +561,40 @@ def cdsl_rope(rope: Rope, q, q_out, start, *, k=None, k_out=None, offset=None, i
     (and k_out), which may be the same tensors; any strides but the last. inverse: turned back, which takes gradients of the
     outputs to those of the inputs."""
     fn = "cdsl_rope"
-    code = _torch().values.get(q.dtype)
-    dev = rope.turns.device
-    tensors = (q, q_out) if k is None else (q, q_out, k, k_out)
-    if (k is None) != (k_out is None):
-        _bad(fn, "k and k_out go together")
-    if code is None or q.dim() != 4:
-        _bad(fn, "q must be a float32 or bfloat16 tensor [batch, T, heads, head_dim]")
-    B, T, H, D = q.shape
-    strides = []
-    for i, x in enumerate(tensors):
-        s, st = x.shape, x.stride()
-        if (x.dtype is not q.dtype or x.device != dev or len(s) != 4 or s[0] != B or s[1] != T or s[3] != D
-                or s != tensors[i // 2 * 2].shape or st[3] != 1):
-            _bad(fn, f"q, k and their outputs must be of one type on {dev}, [{B}, {T}, heads, {D}] with a contiguous last "
-                     f"dimension, got {x.dtype} {tuple(s)} with strides {tuple(st)} on {x.device}")
-        strides += st[:3]
+    dt, s, dev = q.dtype, q.shape, rope.device
+    code = _types.values.get(dt)
+    ok = (code is not None and len(s) == 4 and q_out.dtype is dt and q_out.shape == s and q.device == dev
+          and q_out.device == dev and (k is None) is (k_out is None))
+    sk = None
+    if ok and k is not None:
+        sk = k.shape
+        ok = (len(sk) == 4 and sk[0] == s[0] and sk[1] == s[1] and sk[3] == s[3] and k.dtype is dt and k_out.dtype is dt
+              and k_out.shape == sk and k.device == dev and k_out.device == dev)
+    if not ok:
+        _bad(fn, f"q, k (with k_out, or neither) and their outputs must be float32 or bfloat16 tensors [batch, T, heads, "
+                 f"head_dim] of one type on {dev}, got " +
+                 ", ".join(f"{x.dtype} {tuple(x.shape)} on {x.device}" for x in (q, q_out, k, k_out) if x is not None))
+    B, T, H, D = s
+    if q.is_contiguous() and q_out.is_contiguous() and (k is None or k.is_contiguous() and k_out.is_contiguous()):
+        key = (dt, s, sk)                      # (a decoding loop repeats a few)
+        rows = _rope_rows.get(key)
+        if rows is None:
+            if len(_rope_rows) >= 256:
+                _rope_rows.clear()
+            K = 0 if k is None else sk[2]
+            rows = _rope_rows[key] = _RopeRows(code, B, T, D, H, K, (ctypes.c_int64 * 12)(
+                *(T * H * D, H * D, D) * 2, *(T * K * D, K * D, D) * 2))
+    else:
+        tensors = (q, q_out) if k is None else (q, q_out, k, k_out)
+        strides = [x.stride() for x in tensors]
+        if any(st[3] != 1 for st in strides):
+            _bad(fn, f"q, k and their outputs must have a contiguous last dimension, got strides {strides}")
+        rows = _RopeRows(code, B, T, D, H, 0 if k is None else sk[2],
+                         (ctypes.c_int64 * 12)(*(n for st in strides for n in st[:3])))
     _check(lib().cdsl_rope(
-        rope._ptr, rope.rot, rope.interleaved, int(bool(inverse)), rope.magnitude, code, B, T, D, q.data_ptr(),
-        q_out.data_ptr(), H, _ptr(k), _ptr(k_out), 0 if k is None else k.shape[2], (ctypes.c_int64 * 12)(*strides),
-        _ints(fn, "start", start, (B,), dev), None if offset is None else _ints(fn, "offset", offset, (B, T), dev),
-        _stream(fn, dev, stream)))
+        rope._ref, inverse, ctypes.addressof(rows), q.data_ptr(), q_out.data_ptr(), None if k is None else k.data_ptr(),
+        None if k is None else k_out.data_ptr(), _ints(fn, "start", start, (B,), dev),
+        None if offset is None else _ints(fn, "offset", offset, (B, T), dev), _stream(fn, dev, stream)))
 
 
 def cdsl_tree_mask(parents: Sequence[int]):

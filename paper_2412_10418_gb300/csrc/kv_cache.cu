@@ -85,57 +85,8 @@ struct WriteArgs {
   bool aligned;
 };
 
-// The codes of a lane's 16 values of an I4 row (half a group), with the group's scale. bad: the row is not finite.
-// The scale is top / 7 to 4 significant bits, nearest, ties to even; 2^-120 at least. Codes are x / scale, nearest, ties
-// to even: a product with the reciprocal can miss by one where it lies near a tie, which the exact remainder shows.
-__device__ __forceinline__ void quantise4(const float (&x)[EPL], uint32_t top, bool bad, uint32_t (&codes)[2], uint32_t* scale) {
-  uint32_t s = __float_as_uint(__fdiv_rn(__uint_as_float(top), 7.f));
-  s = (s + 0x7ffffu + (s >> 20 & 1)) & 0xfff00000u;
-  const float step = fmaxf(__uint_as_float(s), 0x1p-120f), inv = __frcp_rn(step), half = step * 0.5f;
-  codes[0] = codes[1] = 0u;
-#pragma unroll
-  for (int i = 0; i < EPL; ++i) {
-    const float y = fmaf(x[i], inv, 12582912.f);   // 1.5 * 2^23: the low bits are the whole number
-    const float rem = fmaf(12582912.f - y, step, x[i]);
-    int c = __float_as_int(y);
-    const float away = fabsf(rem);
-    if (away > half || (away == half && (c & 1))) c += rem > 0.f ? 1 : -1;
-    codes[i / 8] |= (uint32_t)(c & 15) << (i % 8 * 4);
-  }
-  if (bad) codes[0] = codes[1] = 0u;
-  *scale = bad ? 0x7fc0u : __float_as_uint(step) >> 16;
-}
-// Pieces of 16 bits (four codes) of an I4 row change lanes: a lane's 16 values are the pieces (j, g), j = 4 (part % 2) ..,
-// g = part / 2, of which its 8 bytes of the row hold the numbers 4 part .. 4 part + 3, number j * G + g.
-template <int LPR>
-__device__ __forceinline__ void values_to_row(unsigned lanes, int part, uint32_t (&w)[2]) {
-  constexpr int G = LPR / 2;
-  uint32_t out[2] = {0u, 0u};
-#pragma unroll
-  for (int t = 0; t < 4; ++t) {
-    const int h = 4 * part + t, j = h / G, g = h % G;
-    const uint32_t lo = __shfl_sync(lanes, w[0], 2 * g + j / 4, LPR), hi = __shfl_sync(lanes, w[1], 2 * g + j / 4, LPR);
-    out[t / 2] |= ((j % 4 / 2 ? hi : lo) >> (j % 2 * 16) & 0xffffu) << (t % 2 * 16);
-  }
-  w[0] = out[0];
-  w[1] = out[1];
-}
-template <int LPR>
-__device__ __forceinline__ void row_to_values(unsigned lanes, int part, uint32_t (&w)[2]) {
-  constexpr int G = LPR / 2;
-  uint32_t out[2] = {0u, 0u};
-#pragma unroll
-  for (int t = 0; t < 4; ++t) {
-    const int h = (4 * (part % 2) + t) * G + part / 2;
-    const uint32_t lo = __shfl_sync(lanes, w[0], h / 4, LPR), hi = __shfl_sync(lanes, w[1], h / 4, LPR);
-    out[t / 2] |= ((h % 4 / 2 ? hi : lo) >> (h % 2 * 16) & 0xffffu) << (t % 2 * 16);
-  }
-  w[0] = out[0];
-  w[1] = out[1];
-}
-
 // Grid: (rows of a sequence over blocks, batch). LPR = head_dim / 16 lanes work on a row.
-template <typename T, int LPR, int FORMAT>
+template <typename T, int LPR, bool F8>
 __global__ void __launch_bounds__(kThreads) k_kv_write(WriteArgs a) {
   pdl_wait();
   pdl_launch_dependents();
@@ -157,23 +108,15 @@ __global__ void __launch_bounds__(kThreads) k_kv_write(WriteArgs a) {
 #pragma unroll
   for (int i = 0; i < EPL; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
   const unsigned lanes = ((1u << LPR) - 1) << ((threadIdx.x & 31) / LPR * LPR);   // of this row
-  const uint32_t group = FORMAT == kI4 ? max(top, __shfl_xor_sync(lanes, top, 1)) : 0u;
 #pragma unroll
   for (int o = LPR / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(lanes, top, o));
   if (page < 0) {
     if (part == 0) set_status(a.r.status, CDSL_ERANGE);
     return;
   }
-  // (not finite; bf16: or rounded to infinity; I4: or 2^120 and more, beyond which codes times 8 would not fit)
-  const bool bad = top >= (FORMAT == kF8 ? 0x7f800000u : FORMAT == kBF16 ? 0x7f7f8000u : 0x7b800000u);
+  const bool bad = top >= (F8 ? 0x7f800000u : 0x7f7f8000u);   // (not finite, or bf16 rounds it to infinity)
   const size_t r = row_of(c, a.r.layer, page, kv, h, at);
-  if constexpr (FORMAT == kI4) {
-    uint32_t w[2], s;
-    quantise4(x, group, bad, w, &s);
-    values_to_row<LPR>(lanes, part, w);
-    *reinterpret_cast<uint2*>(c.pool + r * c.row + part * 8) = make_uint2(w[0], w[1]);
-    if (part % 2 == 0) reinterpret_cast<uint16_t*>(c.scale + r * c.srow)[part / 2] = (uint16_t)s;
-  } else if constexpr (FORMAT == kF8) {
+  if constexpr (F8) {
     // smallest E with top <= 448 * 2^E = 1.75 * 2^(E + 8)
     int e = (int)(top >> 23) - 127 - 8 + ((top & 0x7fffffu) > 0x600000u);
     e = top == 0 || bad ? 0 : max(e, -126);
@@ -202,7 +145,7 @@ struct ReadArgs {
 };
 
 // Grid: (rows of a sequence over blocks, batch, layers).
-template <typename T, int LPR, int FORMAT>
+template <typename T, int LPR, bool F8>
 __global__ void __launch_bounds__(kThreads) k_kv_read(ReadArgs a) {
   pdl_wait();
   pdl_launch_dependents();
@@ -223,25 +166,8 @@ __global__ void __launch_bounds__(kThreads) k_kv_read(ReadArgs a) {
     } else {
       const int at = (a.r.start[b] + (int)t) & ((1 << c.page_shift) - 1);
       const size_t r = row_of(c, a.r.layer + layer, page, kv, h, at);
-      if constexpr (FORMAT == kI4) {
-        const unsigned lanes = ((1u << LPR) - 1) << ((threadIdx.x & 31) / LPR * LPR);
-        const uint2 u = *reinterpret_cast<const uint2*>(c.pool + r * c.row + part * 8);
-        uint32_t w[2] = {u.x, u.y};
-        row_to_values<LPR>(lanes, part, w);
-        // (one scale that is not finite: the row's all count as NaN)
-        const uint32_t* const sp = reinterpret_cast<const uint32_t*>(c.scale + r * c.srow);
-        const uint2 all = make_uint2(sp[0], LPR == 8 ? sp[LPR / 8] : 0u);
-        const float s = i4_not_finite(all, LPR / 2) ? __uint_as_float(0x7fc00000u)
-                                                    : bf16_at(part / 4 ? all.y : all.x, part / 2 & 1);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float y[4];
-          i4x4_to_f32(w[i / 2] >> (i % 2 * 16), s, y);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) x[4 * i + e] = y[e];
-        }
-      } else if constexpr (FORMAT == kF8) {
-        const float s = scale_value(c.scale[r]);
+      const float s = scale_value(c.scale[r]);
+      if constexpr (F8) {
         const uint4 u = *reinterpret_cast<const uint4*>(c.pool + r * c.hd + part * EPL);
         const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
@@ -251,7 +177,6 @@ __global__ void __launch_bounds__(kThreads) k_kv_read(ReadArgs a) {
           x[2 * i + 1] = f.y * s;
         }
       } else {
-        const float s = scale_value(c.scale[r]);
         load_values(reinterpret_cast<const __nv_bfloat16*>(c.pool) + r * c.hd + part * EPL, true, x);
 #pragma unroll
         for (int i = 0; i < EPL; ++i) x[i] *= s;
@@ -266,6 +191,207 @@ __global__ void __launch_bounds__(kThreads) k_kv_read(ReadArgs a) {
 #pragma unroll
     for (int j = 0; j < EPL; j += 4)
       reinterpret_cast<float4*>(out)[j / 4] = make_float4(x[j], x[j + 1], x[j + 2], x[j + 3]);
+  }
+}
+
+// ---- 4 bits. A lane has 8 bytes of a row, 16 codes: pieces of four of one group each. Its values are 8 or 16 bytes of each
+// group (pieces 4 part .. of number j * G + g: G = 4: dimensions 32 g + 4 part .., G = 2: 32 g + 8 part ..), so that a row's
+// lanes take whole sectors and no value changes lanes.
+
+__device__ __forceinline__ float rcp(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// Codes of 8 values, x[i] / step rounded to nearest, ties to even, as nibbles; step has 4 significant bits. A product with
+// the reciprocal is off by 2^-20 at most, which only a quotient on or next to a tie notices. Of bfloat16 values (8 bits)
+// one that is not a tie is 2^-11 away from it: rounded to 2^-15 first, ties are ties. Of float32 values the remainder
+// decides where it is close.
+template <typename T>
+__device__ __forceinline__ uint32_t codes_of(const float (&x)[8], const float (&steps)[2]) {   // of four values each
+  const float invs[2] = {rcp(steps[0]), rcp(steps[1])};
+  int c[8];
+  if constexpr (sizeof(T) == 2) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) c[i] = __float_as_int(fmaf(x[i], invs[i / 4], 384.f) + (12582912.f - 384.f));   // 1.5 * 2^8, 1.5 * 2^23
+  } else {
+    bool close = false;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float y = fmaf(x[i], invs[i / 4], 12582912.f);
+      close = close || fabsf(fmaf(12582912.f - y, steps[i / 4], x[i])) > steps[i / 4] * 0.4999f;
+      c[i] = __float_as_int(y);
+    }
+    if (close)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float rem = fmaf(12582912.f - __int_as_float(c[i]), steps[i / 4], x[i]), away = fabsf(rem), half = steps[i / 4] * 0.5f;
+        if (away > half || (away == half && (c[i] & 1))) c[i] += rem > 0.f ? 1 : -1;
+      }
+  }
+  // sum of (c_i + 8) 16^i, the constants' own bits taken off (modulo 2^32), then two's complement
+  uint32_t all = 0;
+#pragma unroll
+  for (int i = 7; i >= 0; --i) all = all * 16 + (uint32_t)c[i];
+  return (all + 0x88888888u - 0x4b400000u * 0x11111111u) ^ 0x88888888u;
+}
+
+// Grid: (rows of a sequence over blocks, batch). LPR = head_dim / 16 lanes work on a row.
+template <typename T, int LPR>
+__global__ void __launch_bounds__(kThreads) k_kv_write4(WriteArgs a) {
+  constexpr int G = LPR / 2, N = 16 / G;       // values of a group
+  pdl_wait();
+  pdl_launch_dependents();
+  const Cache& c = a.r.c;
+  const int b = blockIdx.y;
+  const unsigned row = (blockIdx.x * kThreads + threadIdx.x) / LPR;
+  const int part = threadIdx.x % LPR;
+  const unsigned h = row % c.kvh, kv = row / c.kvh & 1, t = row / c.kvh / 2;
+  const int n = a.r.count ? min(a.r.count[b], a.r.T) : a.r.T;
+  if ((int)t >= n) return;             // (a row's lanes return together)
+  const long long* st = kv ? a.sv : a.sk;
+  const T* const from = static_cast<const T*>(kv ? a.v : a.k) + b * st[0] + t * st[1] + h * st[2] + part * N;
+  float x[G][N];
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+    const T* const p = from + g * kGroup;
+    if (a.aligned) {
+      constexpr int W = N * sizeof(T) / 8;     // 8 bytes at a time
+#pragma unroll
+      for (int i = 0; i < W; ++i) {
+        const uint2 u = reinterpret_cast<const uint2*>(p)[i];
+        if constexpr (sizeof(T) == 2) {
+          x[g][4 * i] = bf16_at(u.x, 0); x[g][4 * i + 1] = bf16_at(u.x, 1);
+          x[g][4 * i + 2] = bf16_at(u.y, 0); x[g][4 * i + 3] = bf16_at(u.y, 1);
+        } else {
+          x[g][2 * i] = __uint_as_float(u.x); x[g][2 * i + 1] = __uint_as_float(u.y);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) x[g][i] = to_f32<T>(p[i]);
+    }
+  }
+  const int page = page_of(c, b, (long long)a.r.start[b] + t);
+  const int at = (a.r.start[b] + (int)t) & ((1 << c.page_shift) - 1);
+  // the groups' largest |x| as bits (they order like the values): lane part gets group part % G's
+  uint32_t top[G];
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+    top[g] = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) top[g] = max(top[g], __float_as_uint(x[g][i]) & 0x7fffffffu);
+  }
+  const unsigned lanes = ((1u << LPR) - 1) << ((threadIdx.x & 31) / LPR * LPR);   // of this row
+  uint32_t mine;
+  if constexpr (G == 4) {
+    uint32_t two[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {              // bit 1 of the lane keeps groups 2, 3
+      const uint32_t keep = part & 2 ? top[2 + i] : top[i], give = part & 2 ? top[i] : top[2 + i];
+      two[i] = max(keep, __shfl_xor_sync(lanes, give, 2));
+    }
+    const uint32_t keep = part & 1 ? two[1] : two[0], give = part & 1 ? two[0] : two[1];
+    mine = max(keep, __shfl_xor_sync(lanes, give, 1));
+    mine = max(mine, __shfl_xor_sync(lanes, mine, 4));
+  } else {
+    const uint32_t keep = part & 1 ? top[1] : top[0], give = part & 1 ? top[0] : top[1];
+    mine = max(keep, __shfl_xor_sync(lanes, give, 1));
+    mine = max(mine, __shfl_xor_sync(lanes, mine, 2));
+  }
+  // its scale: top / 7 to 4 significant bits, nearest, ties to even; 2^-120 at least. (Not finite, or 2^120 and more, beyond
+  // which codes times 8 would not fit: NaN.)
+  uint32_t s = __float_as_uint(__fdiv_rn(__uint_as_float(mine), 7.f));
+  s = max((s + 0x7ffffu + (s >> 20 & 1)) & 0xfff00000u, 0x03800000u);
+  if (mine >= 0x7b800000u) s = 0x7fc00000u;
+  float step[G];
+  bool bad = false;
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+    step[g] = __uint_as_float(__shfl_sync(lanes, s, g, LPR));
+    bad = bad || step[g] != step[g];
+  }
+  if (page < 0) {
+    if (part == 0) set_status(a.r.status, CDSL_ERANGE);
+    return;
+  }
+  const size_t r = row_of(c, a.r.layer, page, kv, h, at);
+  // pieces in the order of their numbers: the groups of 4 j, then of the next j
+  uint32_t w[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    float y[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = x[(2 * i + e / 4) % G][(2 * i + e / 4) / G * 4 + e % 4];
+    const float steps[2] = {step[2 * i % G], step[(2 * i + 1) % G]};
+    w[i] = bad ? 0u : codes_of<T>(y, steps);
+  }
+  *reinterpret_cast<uint2*>(c.pool + r * c.row + part * 8) = make_uint2(w[0], w[1]);
+  if (part < G) reinterpret_cast<uint16_t*>(c.scale + r * c.srow)[part] = (uint16_t)(bad ? 0x7fc0u : s >> 16);
+}
+
+// Grid: (rows of a sequence over blocks, batch, layers).
+template <typename T, int LPR>
+__global__ void __launch_bounds__(kThreads) k_kv_read4(ReadArgs a) {
+  constexpr int G = LPR / 2, N = 16 / G;       // values of a group
+  pdl_wait();
+  pdl_launch_dependents();
+  const Cache& c = a.r.c;
+  const int b = blockIdx.y, layer = blockIdx.z;
+  const unsigned row = (blockIdx.x * kThreads + threadIdx.x) / LPR;
+  const int part = threadIdx.x % LPR;
+  const unsigned h = row % c.kvh, kv = row / c.kvh & 1, t = row / c.kvh / 2;
+  if ((int)t >= a.r.T) return;
+  const int n = a.r.count ? a.r.count[b] : a.r.T;
+  uint2 u = make_uint2(0u, 0u);                // codes
+  uint32_t s[G / 2];                           // scales
+#pragma unroll
+  for (int i = 0; i < G / 2; ++i) s[i] = 0u;
+  if ((int)t < n) {
+    const int page = page_of(c, b, (long long)a.r.start[b] + t);
+    if (page < 0) {
+      if (part == 0) set_status(a.r.status, CDSL_ERANGE);
+    } else {
+      const int at = (a.r.start[b] + (int)t) & ((1 << c.page_shift) - 1);
+      const size_t r = row_of(c, a.r.layer + layer, page, kv, h, at);
+      u = *reinterpret_cast<const uint2*>(c.pool + r * c.row + part * 8);
+      const uint32_t* const sp = reinterpret_cast<const uint32_t*>(c.scale + r * c.srow);
+#pragma unroll
+      for (int i = 0; i < G / 2; ++i) s[i] = sp[i];
+      // (one scale that is not finite: the row's all count as NaN)
+      if (i4_not_finite(make_uint2(s[0], s[G / 2 - 1]), G))
+#pragma unroll
+        for (int i = 0; i < G / 2; ++i) s[i] = 0x7fc07fc0u;
+    }
+  }
+  T* const out = static_cast<T*>(kv ? a.v : a.k) +
+                 ((((size_t)layer * c.batch + b) * a.r.T + t) * c.kvh + h) * c.hd + part * N;
+  const uint32_t w[2] = {u.x, u.y};
+  float x[G][N];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {                // pieces
+    const int g = i % G;
+    float y[4];
+    i4x4_to_f32(w[i / 2] >> (i % 2 * 16), bf16_at(s[g / 2], g % 2), y);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[g][i / G * 4 + e] = y[e];
+  }
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int i = 0; i < N; i += 4)
+        *reinterpret_cast<float4*>(out + g * kGroup + i) = make_float4(x[g][i], x[g][i + 1], x[g][i + 2], x[g][i + 3]);
+    } else {
+      uint32_t two[N / 2];
+#pragma unroll
+      for (int i = 0; i < N / 2; ++i) {
+        const __nv_bfloat162 z = __floats2bfloat162_rn(x[g][2 * i], x[g][2 * i + 1]);
+        two[i] = *reinterpret_cast<const uint32_t*>(&z);
+      }
+      if constexpr (N == 4) *reinterpret_cast<uint2*>(out + g * kGroup) = make_uint2(two[0], two[1]);
+      else *reinterpret_cast<uint4*>(out + g * kGroup) = make_uint4(two[0], two[1], two[2], two[3]);
+    }
   }
 }
 
@@ -334,13 +460,13 @@ __global__ void __launch_bounds__(kThreads) k_kv_commit(CommitArgs a) {
 }
 
 template <typename F>
-int by_shape(const Cache& c, int dtype, F&& f) {   // f(element type tag, lanes per row, format)
-  auto h = [&](auto t, auto lpr) {
-    if (c.format == kI4) return f(t, lpr, std::integral_constant<int, kI4>());
-    return c.format == kF8 ? f(t, lpr, std::integral_constant<int, kF8>()) : f(t, lpr, std::integral_constant<int, kBF16>());
-  };
+int by_shape(const Cache& c, int dtype, F&& f) {   // f(element type tag, lanes per row, e4m3?)
   auto g = [&](auto t) {
-    return c.hd == 128 ? h(t, std::integral_constant<int, 8>()) : h(t, std::integral_constant<int, 4>());
+    if (c.hd == 128)
+      return c.format == kF8 ? f(t, std::integral_constant<int, 8>(), std::true_type())
+                       : f(t, std::integral_constant<int, 8>(), std::false_type());
+    return c.format == kF8 ? f(t, std::integral_constant<int, 4>(), std::true_type())
+                     : f(t, std::integral_constant<int, 4>(), std::false_type());
   };
   return dtype == CDSL_DTYPE_BF16 ? g(__nv_bfloat16()) : g(float());
 }
@@ -380,9 +506,9 @@ extern "C" int32_t cdsl_kv_write(const cdsl_kv_cache* cache, int32_t layer, cons
     if (a.sk[i] * eb % 16 || a.sv[i] * eb % 16) a.aligned = false;
   }
   const dim3 grid(row_blocks(c, T), c.batch);
-  return by_shape(c, dtype, [&](auto t, auto lpr, auto format) {
-    return ck.launched(launch_pdl(k_kv_write<decltype(t), lpr(), format()>, grid, dim3(kThreads), 0,
-                                  static_cast<cudaStream_t>(stream), a));
+  return by_shape(c, dtype, [&](auto t, auto lpr, auto f8) {
+    const auto k = c.format == kI4 ? k_kv_write4<decltype(t), lpr()> : k_kv_write<decltype(t), lpr(), f8()>;
+    return ck.launched(launch_pdl(k, grid, dim3(kThreads), 0, static_cast<cudaStream_t>(stream), a));
   });
 }
 
@@ -400,9 +526,9 @@ extern "C" int32_t cdsl_kv_read(const cdsl_kv_cache* cache, int32_t layer, int32
   a.k = d_k;
   a.v = d_v;
   const dim3 grid(row_blocks(c, T), c.batch, n_layers);
-  return by_shape(c, dtype, [&](auto t, auto lpr, auto format) {
-    return ck.launched(launch_pdl(k_kv_read<decltype(t), lpr(), format()>, grid, dim3(kThreads), 0,
-                                  static_cast<cudaStream_t>(stream), a));
+  return by_shape(c, dtype, [&](auto t, auto lpr, auto f8) {
+    const auto k = c.format == kI4 ? k_kv_read4<decltype(t), lpr()> : k_kv_read<decltype(t), lpr(), f8()>;
+    return ck.launched(launch_pdl(k, grid, dim3(kThreads), 0, static_cast<cudaStream_t>(stream), a));
   });
 }
 

@@ -5,8 +5,11 @@
 // in turns, as 64-bit fractions of one: pos * turns modulo 2^64 is the fraction exactly, with no range to reduce.
 // Its nearest quarter is taken off in whole numbers and the rest, at most an eighth of a turn, goes through sincospif.
 //
-// Bound by HBM on large calls, where the sines, once for all heads of a token, go beside the loads, and by the launch on
-// a decoding step's.
+// Bound by HBM on large calls and by the launch on a decoding step's: 4 x 4093 tokens of 48 heads of 128 in bf16, 96 of them
+// turned, and their gradients (two calls, 805 MB): 129 us, 92 % of the copy bandwidth; one token 2.6 us in a graph. What counts
+// there is instructions, of which 16 bytes have room for some fifty: a token by a block, with the sines through shared memory
+// and each address worked out, took 167 us; heads' addresses worked out in a warp's loop 235; this with blocks of 256
+// threads 150, of 128 without a bound on registers 135 (90 of them), eight heads loaded together 179.
 #include <cuda.h>
 
 #include <algorithm>
@@ -14,17 +17,19 @@
 
 #include "kernels.h"
 #include "tree_host.h"
+#include "tree_tc.cuh"
 
 namespace cdsl {
 namespace tree {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 128, kBlocks = 6;     // of an SM, by registers
 
 struct RopeArgs {
   const uint64_t* turns;
   int half;                            // pairs
-  int hd, T, heads[2];                 // of q, k (0: none)
+  int hd, batch, T, heads[2];          // of q, k (0: none)
+  int slices;
   float magnitude, sign;               // sign: of the sine
   const void* x[2];
   void* y[2];
@@ -33,85 +38,139 @@ struct RopeArgs {
   const int32_t* offset;
 };
 
-// A pair, turned; written out, so that every variant rounds alike.
-__device__ __forceinline__ float2 turn(float p, float q, float2 cs) {
-  return make_float2(fmaf(p, cs.x, -__fmul_rn(q, cs.y)), fmaf(q, cs.x, __fmul_rn(p, cs.y)));
+// Pairs (p, q), turned, by twos: the products of every variant are these, so that all round alike.
+__device__ __forceinline__ void turn(uint64_t& p, uint64_t& q, uint64_t cos2, uint64_t sin2, uint64_t minus2) {
+  const uint64_t z = fma2(p, cos2, mul2(q, minus2));
+  q = fma2(q, cos2, mul2(p, sin2));
+  p = z;
 }
 
 // V values of a head.
 template <typename T, int V> struct alignas(sizeof(T) * V) Values { T x[V]; };
 
-// Grid: (tokens, batch). A thread has V values of a head: both sides of V pairs (halves: V values of each; neighbours: V / 2
-// pairs), or V values that are not turned.
+// A warp has a token's heads, or a share of them: `slices` warps a token. A lane has the same part of every head it
+// turns, V values (halves: V of both sides; neighbours: V / 2 pairs, of single values a pair) or V that are not turned, so
+// that it needs its sines once, in registers; a head's parts are side by side in the lanes, several heads' where a head
+// has fewer than 32. kAhead heads are loaded together.
+constexpr int kAhead = 4;
 template <typename T, int V, bool PAIRS>
-__global__ void __launch_bounds__(kThreads) k_rope(RopeArgs a) {
-  extern __shared__ float2 s_cs[];             // cosine and sine, times the magnitude
+__global__ void __launch_bounds__(kThreads, kBlocks) k_rope(const __grid_constant__ RopeArgs a) {
+  constexpr int STEP = PAIRS && V == 1 ? 2 : V;          // values of a turned part's first side
+  constexpr int ANGLES = PAIRS ? STEP / 2 : V;
+  using Vec = Values<T, STEP>;
   pdl_wait();
   pdl_launch_dependents();
-  const int t = blockIdx.x, b = blockIdx.y;
+  const int lane = threadIdx.x & 31;
+  const long long warp = (long long)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
+  const long long token = warp / a.slices;
+  if (token >= (long long)a.batch * a.T) return;
+  const int slice = (int)(warp % a.slices), b = (int)(token / a.T), t = (int)(token % a.T);
+  const int turned = PAIRS ? 2 * a.half / STEP : a.half / V, per = turned + (a.hd - 2 * a.half) / V;   // parts of a head
+  const int together = max(1, 32 / per), sub = per < 32 ? lane / per : 0;   // heads that a warp has at once
+  const int heads = a.heads[0] + a.heads[1], share = (heads + a.slices - 1) / a.slices;
+  const int end = min(heads, (slice + 1) * share);
   const long long pos = (long long)a.start[b] + (a.offset ? a.offset[(size_t)b * a.T + t] : t);
-  for (int i = threadIdx.x; i < a.half; i += kThreads) {
-    const uint64_t turn = (uint64_t)pos * a.turns[i];
-    const uint32_t top = (uint32_t)(turn >> 32);
-    const uint32_t quarter = (top + (1u << 29)) >> 30;           // the nearest (4: 0)
-    const float rest = (float)(int32_t)(top - (quarter << 30)) * 0x1p-31f;   // of half a turn
-    float s, c;
-    sincospif(rest, &s, &c);
-    const float cs = quarter & 1 ? -s : c, sn = quarter & 1 ? c : s;
-    const float flip = quarter & 2 ? -a.magnitude : a.magnitude;
-    s_cs[i] = make_float2(cs * flip, sn * flip * a.sign);
-  }
-  __syncthreads();
-  using Vec = Values<T, V>;
-  const int turned = PAIRS ? 2 * a.half / V : a.half / V, per = turned + (a.hd - 2 * a.half) / V;   // parts of a head
-  const int all = (a.heads[0] + a.heads[1]) * per;
-  for (int i = threadIdx.x; i < all; i += kThreads) {
-    int h = i / per;
-    const int part = i - h * per, w = h >= a.heads[0];
-    if (w) h -= a.heads[0];
-    const T* const x = static_cast<const T*>(a.x[w]) + b * a.sx[w][0] + t * a.sx[w][1] + h * a.sx[w][2];
-    T* const y = static_cast<T*>(a.y[w]) + b * a.sy[w][0] + t * a.sy[w][1] + h * a.sy[w][2];
-    if (part >= turned) {
-      const int d = 2 * a.half + (part - turned) * V;
-      *reinterpret_cast<Vec*>(y + d) = *reinterpret_cast<const Vec*>(x + d);
-    } else if constexpr (PAIRS && V > 1) {
-      const int d = part * V;
-      Vec u = *reinterpret_cast<const Vec*>(x + d);
+#pragma unroll 1
+  for (int p0 = 0; p0 < per; p0 += 32) {
+    const int part = per < 32 ? lane % per : p0 + lane;
+    if (part >= per || sub >= together) continue;
+    const bool turns = part < turned;
+    const int d = turns ? part * STEP : 2 * a.half + (part - turned) * V;   // the part's first value
+    float2 cs[ANGLES];
+    if (turns) {
 #pragma unroll
-      for (int e = 0; e < V; e += 2) {
-        const float2 cs = s_cs[(d + e) / 2];
-        const float2 z = turn(to_f32<T>(u.x[e]), to_f32<T>(u.x[e + 1]), cs);
-        u.x[e] = from_f32<T>(z.x);
-        u.x[e + 1] = from_f32<T>(z.y);
+      for (int i = 0; i < ANGLES; ++i) {
+        const uint64_t turn = (uint64_t)pos * a.turns[PAIRS ? d / 2 + i : d + i];
+        const uint32_t top = (uint32_t)(turn >> 32);
+        const uint32_t quarter = (top + (1u << 29)) >> 30;           // the nearest (4: 0)
+        const float rest = (float)(int32_t)(top - (quarter << 30)) * 0x1p-31f;   // of half a turn
+        float s, c;
+        sincospif(rest, &s, &c);
+        const float x = quarter & 1 ? -s : c, y = quarter & 1 ? c : s;
+        const float flip = quarter & 2 ? -a.magnitude : a.magnitude;
+        cs[i] = make_float2(x * flip, y * flip * a.sign);
       }
-      *reinterpret_cast<Vec*>(y + d) = u;
-    } else if constexpr (PAIRS) {              // (one value at a time: the thread of a pair's first has both)
-      if (part % 2) continue;
-      const float2 cs = s_cs[part / 2];
-      const float2 z = turn(to_f32<T>(x[part]), to_f32<T>(x[part + 1]), cs);
-      y[part] = from_f32<T>(z.x);
-      y[part + 1] = from_f32<T>(z.y);
-    } else {
-      const int d = part * V;
-      Vec u = *reinterpret_cast<const Vec*>(x + d), v = *reinterpret_cast<const Vec*>(x + a.half + d);
+    }
+    uint64_t c2[(ANGLES + 1) / 2], s2[(ANGLES + 1) / 2], m2[(ANGLES + 1) / 2];   // of two angles
 #pragma unroll
-      for (int e = 0; e < V; ++e) {
-        const float2 cs = s_cs[d + e];
-        const float2 z = turn(to_f32<T>(u.x[e]), to_f32<T>(v.x[e]), cs);
-        u.x[e] = from_f32<T>(z.x);
-        v.x[e] = from_f32<T>(z.y);
+    for (int i = 0; i < (ANGLES + 1) / 2; ++i) {
+      const float2 x = cs[2 * i], y = cs[min(2 * i + 1, ANGLES - 1)];
+      c2[i] = pair(x.x, y.x);
+      s2[i] = pair(x.y, y.y);
+      m2[i] = pair(-x.y, -y.y);
+    }
+    const auto turn_part = [&](Vec& u, Vec& v) {
+#pragma unroll
+      for (int i = 0; i < ANGLES; i += 2) {
+        const int j = min(i + 1, ANGLES - 1);
+        T& p0 = u.x[PAIRS ? 2 * i : i], & p1 = u.x[PAIRS ? 2 * j : j];
+        T& q0 = PAIRS ? u.x[PAIRS ? 2 * i + 1 : 0] : v.x[PAIRS ? 0 : i], & q1 = PAIRS ? u.x[PAIRS ? 2 * j + 1 : 0] : v.x[PAIRS ? 0 : j];
+        uint64_t p = pair(to_f32<T>(p0), to_f32<T>(p1)), q = pair(to_f32<T>(q0), to_f32<T>(q1));
+        turn(p, q, c2[i / 2], s2[i / 2], m2[i / 2]);
+        const float2 y = unpair(p), z = unpair(q);
+        p1 = from_f32<T>(y.y);
+        q1 = from_f32<T>(z.y);
+        p0 = from_f32<T>(y.x);
+        q0 = from_f32<T>(z.x);
       }
-      *reinterpret_cast<Vec*>(y + d) = u;
-      *reinterpret_cast<Vec*>(y + a.half + d) = v;
+    };
+#pragma unroll 1
+    for (int w = 0; w < 2; ++w) {              // q, k
+      const int first = w ? max(slice * share - a.heads[0], 0) : slice * share;
+      const int last = w ? end - a.heads[0] : min(end, a.heads[0]);
+      int h = first + sub;
+      if (h >= last) continue;
+      const T* x = static_cast<const T*>(a.x[w]) + b * a.sx[w][0] + t * a.sx[w][1] + h * a.sx[w][2] + d;
+      T* y = static_cast<T*>(a.y[w]) + b * a.sy[w][0] + t * a.sy[w][1] + h * a.sy[w][2] + d;
+      const long long dx = together * a.sx[w][2], dy = together * a.sy[w][2];
+      const auto load = [&](Vec& u, Vec& v) {
+        if constexpr (STEP == V) {
+          u = *reinterpret_cast<const Vec*>(x);
+          if (!PAIRS && turns) v = *reinterpret_cast<const Vec*>(x + a.half);
+        } else {                               // (single values need not be aligned in twos)
+          u.x[0] = x[0];
+          if (turns) u.x[1] = x[1];
+        }
+        x += dx;
+      };
+      const auto store = [&](Vec& u, Vec& v) {
+        if (turns) turn_part(u, v);
+        if constexpr (STEP == V) {
+          *reinterpret_cast<Vec*>(y) = u;
+          if (!PAIRS && turns) *reinterpret_cast<Vec*>(y + a.half) = v;
+        } else {
+          y[0] = u.x[0];
+          if (turns) y[1] = u.x[1];
+        }
+        y += dy;
+      };
+#pragma unroll 1
+      for (; h + (kAhead - 1) * together < last; h += kAhead * together) {
+        Vec u[kAhead], v[kAhead];
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e) load(u[e], v[e]);
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e) store(u[e], v[e]);
+      }
+#pragma unroll 1
+      for (; h < last; h += together) {
+        Vec u, v;
+        load(u, v);
+        store(u, v);
+      }
     }
   }
 }
 
 template <typename T>
-cudaError_t launch(const RopeArgs& a, int batch, bool pairs, bool wide, cudaStream_t s) {
+cudaError_t launch(RopeArgs& a, bool pairs, bool wide, cudaStream_t s) {
   constexpr int V = 16 / sizeof(T);
   const auto k = pairs ? (wide ? k_rope<T, V, true> : k_rope<T, 1, true>) : (wide ? k_rope<T, V, false> : k_rope<T, 1, false>);
-  return launch_pdl(k, dim3(a.T, batch), dim3(kThreads), a.half * sizeof(float2), s, a);
+  // a token's heads among warps where tokens alone do not fill the device
+  const long long tokens = (long long)a.batch * a.T, want = (long long)kPlanSMs * 16;
+  a.slices = (int)std::min<long long>(a.heads[0] + a.heads[1], (want + tokens - 1) / tokens);
+  const long long blocks = (tokens * a.slices + kThreads / 32 - 1) / (kThreads / 32);
+  return launch_pdl(k, dim3((unsigned)blocks), dim3(kThreads), 0, s, a);
 }
 
 }  // namespace
@@ -145,50 +204,53 @@ extern "C" int32_t cdsl_rope_turns(int32_t rot, double theta, double factor, int
   return CDSL_OK;
 }
 
-extern "C" int32_t cdsl_rope(const uint64_t* d_turns, int32_t rot, int32_t interleaved, int32_t inverse, float magnitude,
-                             int32_t dtype, int32_t batch, int32_t T, int32_t head_dim, const void* d_q, void* d_q_out,
-                             int32_t n_heads, const void* d_k, void* d_k_out, int32_t n_kv_heads, const int64_t* h_strides,
-                             const int32_t* d_start, const int32_t* d_offset, void* stream) {
+extern "C" int32_t cdsl_rope(const cdsl_rope_cfg* rope, int32_t inverse, const cdsl_rope_rows* rows, const void* d_q,
+                             void* d_q_out, const void* d_k, void* d_k_out, const int32_t* d_start, const int32_t* d_offset,
+                             void* stream) {
   Check ck("cdsl_rope");
-  if (!ck.value_type(dtype)) return CDSL_EINVAL;
-  if (!d_turns || !d_q || !d_q_out || !h_strides || !d_start) return ck.fail("a required pointer is NULL");
+  if (!rope || !rows || !rope->d_turns || !d_q || !d_q_out || !d_start) return ck.fail("a required pointer is NULL");
+  const cdsl_rope_rows& z = *rows;
+  if (!ck.value_type(z.dtype)) return CDSL_EINVAL;
   if (!d_k != !d_k_out) return ck.fail("k and k's output go together");
-  if (head_dim < 2 || head_dim > CDSL_ROPE_MAX_DIM) return ck.fail("head_dim must be 2 .. 1024");
-  if (rot < 2 || rot % 2 || rot > head_dim) return ck.fail("rot must be even, 2 .. head_dim");
-  if (batch < 1 || batch > 65535 || T < 1 || n_heads < 1 || n_heads > (1 << 16) || (d_k && (n_kv_heads < 1 || n_kv_heads > (1 << 16))))
-    return ck.fail("sizes: need 1 <= batch <= 65535, T >= 1, 1 .. 65536 heads");
-  if (!(magnitude > 0.f) || !std::isfinite(magnitude)) return ck.fail("magnitude must be positive and finite");
-  const int eb = dtype == CDSL_DTYPE_BF16 ? 2 : 4, V = 16 / eb;
+  if (z.head_dim < 2 || z.head_dim > CDSL_ROPE_MAX_DIM) return ck.fail("head_dim must be 2 .. 1024");
+  if (rope->rot < 2 || rope->rot % 2 || rope->rot > z.head_dim) return ck.fail("rot must be even, 2 .. head_dim");
+  if (z.batch < 1 || z.T < 1 || (long long)z.batch * z.T > (1 << 26) || z.n_heads < 1 || z.n_heads > (1 << 16) ||
+      (d_k && (z.n_kv_heads < 1 || z.n_kv_heads > (1 << 16))))
+    return ck.fail("sizes: need batch, T >= 1, at most 2^26 tokens, 1 .. 65536 heads");
+  if (!(rope->magnitude > 0.f) || !std::isfinite(rope->magnitude)) return ck.fail("magnitude must be positive and finite");
+  const int eb = z.dtype == CDSL_DTYPE_BF16 ? 2 : 4, V = 16 / eb;
   RopeArgs a = {};
-  a.turns = d_turns;
-  a.half = rot / 2;
-  a.hd = head_dim;
-  a.T = T;
-  a.heads[0] = n_heads;
-  a.heads[1] = d_k ? n_kv_heads : 0;
-  a.magnitude = magnitude;
+  a.turns = rope->d_turns;
+  a.half = rope->rot / 2;
+  a.hd = z.head_dim;
+  a.batch = z.batch;
+  a.T = z.T;
+  a.heads[0] = z.n_heads;
+  a.heads[1] = d_k ? z.n_kv_heads : 0;
+  a.magnitude = rope->magnitude;
   a.sign = inverse ? -1.f : 1.f;
   a.x[0] = d_q; a.x[1] = d_k;
   a.y[0] = d_q_out; a.y[1] = d_k_out;
   a.start = d_start;
   a.offset = d_offset;
   // 16 bytes at a time where every part of a head begins at a multiple of them
-  bool wide = (interleaved ? rot : a.half) % V == 0 && (head_dim - rot) % V == 0;
+  bool wide = (rope->interleaved ? rope->rot : a.half) % V == 0 && (z.head_dim - rope->rot) % V == 0;
   for (int w = 0; w < (d_k ? 2 : 1); ++w) {
     if (!ck.aligned(a.x[w], eb) || !ck.aligned(a.y[w], eb)) return ck.fail("tensors must be aligned to their type");
     wide = wide && ck.aligned(a.x[w], 16) && ck.aligned(a.y[w], 16);
     for (int i = 0; i < 3; ++i) {
-      a.sx[w][i] = h_strides[6 * w + i];
-      a.sy[w][i] = h_strides[6 * w + 3 + i];
+      a.sx[w][i] = z.strides[6 * w + i];
+      a.sy[w][i] = z.strides[6 * w + 3 + i];
       if (a.sx[w][i] % V || a.sy[w][i] % V) wide = false;
     }
     const long long* const so = a.sy[w];
-    if ((batch > 1 && so[0] == 0) || (T > 1 && so[1] == 0) || (a.heads[w] > 1 && so[2] == 0))
+    if ((z.batch > 1 && so[0] == 0) || (z.T > 1 && so[1] == 0) || (a.heads[w] > 1 && so[2] == 0))
       return ck.fail("an output must not have a stride of 0 between sequences, tokens or heads");
     if (a.x[w] == a.y[w] && !std::equal(a.sx[w], a.sx[w] + 3, a.sy[w]))
       return ck.fail("an output in its input's place must have its strides");
   }
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
-  return ck.launched(dtype == CDSL_DTYPE_BF16 ? launch<__nv_bfloat16>(a, batch, interleaved, wide, s)
-                                              : launch<float>(a, batch, interleaved, wide, s));
+  const bool pairs = rope->interleaved != 0;
+  return ck.launched(z.dtype == CDSL_DTYPE_BF16 ? launch<__nv_bfloat16>(a, pairs, wide, s)
+                                                : launch<float>(a, pairs, wide, s));
 }

@@ -71,16 +71,20 @@ def test_the_pages_workspace(cdsl):
 
 
 def test_bad_ropes_are_refused(cdsl):
-    st = (ctypes.c_int64 * 12)(*[16384, 4096, 128] * 4)
+    st = [16384, 4096, 128] * 4
 
-    def rope(turns=PTR, rot=128, m=1.0, dtype=1, B=2, T=4, hd=128, q=PTR, qo=PTR, H=32, k=PTR, ko=PTR, kvh=8, st=st, start=PTR):
-        return cdsl.lib().cdsl_rope(turns, rot, 0, 0, m, dtype, B, T, hd, q, qo, H, k, ko, kvh, st, start, None, None)
+    def rope(turns=PTR, rot=128, m=1.0, dtype=1, B=2, T=4, hd=128, q=PTR, qo=PTR, H=32, k=PTR, ko=PTR, kvh=8, st=st, start=PTR,
+             none=()):
+        c = cdsl._RopeC(turns, rot, 0, m)
+        rows = cdsl._RopeRows(dtype, B, T, hd, H, kvh, (ctypes.c_int64 * 12)(*st))
+        return cdsl.lib().cdsl_rope(None if "rope" in none else ctypes.addressof(c), 0,
+                                    None if "rows" in none else ctypes.addressof(rows), q, qo, k, ko, start, None, None)
 
-    zero = (ctypes.c_int64 * 12)(*[16384, 4096, 128] * 3, 16384, 0, 128)
-    other = (ctypes.c_int64 * 12)(16384, 4096, 128, 16384, 128, 512, *[16384, 4096, 128] * 2)
+    zero = [16384, 4096, 128] * 3 + [16384, 0, 128]
+    other = [16384, 4096, 128, 16384, 128, 512] + [16384, 4096, 128] * 2
     for kw in (dict(turns=None), dict(rot=0), dict(rot=3), dict(rot=130), dict(m=0.0), dict(m=math.nan), dict(m=math.inf),
-               dict(dtype=2), dict(B=0), dict(B=65536), dict(T=0), dict(hd=1), dict(hd=1025), dict(q=None), dict(qo=None),
-               dict(H=0), dict(k=None), dict(ko=None), dict(kvh=0), dict(st=None), dict(start=None), dict(q=PTR + 1),
+               dict(dtype=2), dict(B=0), dict(B=1 << 14, T=1 << 13), dict(T=0), dict(hd=1), dict(hd=1025), dict(q=None), dict(qo=None),
+               dict(H=0), dict(k=None), dict(ko=None), dict(kvh=0), dict(none=("rope",)), dict(none=("rows",)), dict(start=None), dict(q=PTR + 1),
                dict(ko=PTR + 1), dict(st=zero, ko=PTR + 4096), dict(st=other)):
         assert rope(**kw) == cdsl.CDSL_EINVAL, kw
         assert "cdsl_rope" in cdsl.cdsl_last_error(None)
