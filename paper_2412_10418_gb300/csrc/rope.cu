@@ -6,10 +6,11 @@
 // Its nearest quarter is taken off in whole numbers and the rest, at most an eighth of a turn, goes through sincospif.
 //
 // Bound by HBM on large calls and by the launch on a decoding step's: 4 x 4093 tokens of 48 heads of 128 in bf16, 96 of them
-// turned, and their gradients (two calls, 805 MB): 129 us, 92 % of the copy bandwidth; one token 2.6 us in a graph. What counts
-// there is instructions, of which 16 bytes have room for some fifty: a token by a block, with the sines through shared memory
-// and each address worked out, took 167 us; heads' addresses worked out in a warp's loop 235; this with blocks of 256
-// threads 150, of 128 without a bound on registers 135 (90 of them), eight heads loaded together 179.
+// turned, and their gradients (two calls, 805 MB): 132 us as neighbours, 145 as halves, 90 and 82 % of the copy bandwidth; one
+// token 2.6 us in a graph. What counts there is instructions, of which 16 bytes have room for some fifty: a token by a
+// block, with the sines through shared memory and each address worked out, took 167 us; heads' addresses worked out in a
+// warp's loop 235; blocks of 256 threads 150; eight heads loaded together 179; halves by 16 bytes of each side, with as
+// many angles in registers, 240.
 #include <cuda.h>
 
 #include <algorithm>
@@ -23,6 +24,7 @@ namespace cdsl {
 namespace tree {
 namespace {
 
+constexpr int kHalves = 4;                     // values of each side (8 of bf16 are as many angles, and take their registers)
 constexpr int kThreads = 128, kBlocks = 6;     // of an SM, by registers
 
 struct RopeArgs {
@@ -51,12 +53,12 @@ template <typename T, int V> struct alignas(sizeof(T) * V) Values { T x[V]; };
 // A warp has a token's heads, or a share of them: `slices` warps a token. A lane has the same part of every head it
 // turns, V values (halves: V of both sides; neighbours: V / 2 pairs, of single values a pair) or V that are not turned, so
 // that it needs its sines once, in registers; a head's parts are side by side in the lanes, several heads' where a head
-// has fewer than 32. kAhead heads are loaded together.
-constexpr int kAhead = 4;
+// has fewer than 32. four heads are loaded together.
 template <typename T, int V, bool PAIRS>
 __global__ void __launch_bounds__(kThreads, kBlocks) k_rope(const __grid_constant__ RopeArgs a) {
   constexpr int STEP = PAIRS && V == 1 ? 2 : V;          // values of a turned part's first side
   constexpr int ANGLES = PAIRS ? STEP / 2 : V;
+  constexpr int AHEAD = 4;
   using Vec = Values<T, STEP>;
   pdl_wait();
   pdl_launch_dependents();
@@ -65,7 +67,9 @@ __global__ void __launch_bounds__(kThreads, kBlocks) k_rope(const __grid_constan
   const long long token = warp / a.slices;
   if (token >= (long long)a.batch * a.T) return;
   const int slice = (int)(warp % a.slices), b = (int)(token / a.T), t = (int)(token % a.T);
-  const int turned = PAIRS ? 2 * a.half / STEP : a.half / V, per = turned + (a.hd - 2 * a.half) / V;   // parts of a head
+  // parts of a head (halves: what is not turned goes by two sides as well, of which the second may be one shorter)
+  const int turned = PAIRS ? 2 * a.half / STEP : a.half / V, rest = a.hd - 2 * a.half, side = PAIRS ? 0 : (rest + 1) / 2;
+  const int per = turned + (PAIRS ? rest : side) / V;
   const int together = max(1, 32 / per), sub = per < 32 ? lane / per : 0;   // heads that a warp has at once
   const int heads = a.heads[0] + a.heads[1], share = (heads + a.slices - 1) / a.slices;
   const int end = min(heads, (slice + 1) * share);
@@ -76,6 +80,8 @@ __global__ void __launch_bounds__(kThreads, kBlocks) k_rope(const __grid_constan
     if (part >= per || sub >= together) continue;
     const bool turns = part < turned;
     const int d = turns ? part * STEP : 2 * a.half + (part - turned) * V;   // the part's first value
+    const int other = turns ? a.half : side;   // halves: the second side, from the first
+    const bool both = !PAIRS && (turns || d + side + V <= a.hd);
     float2 cs[ANGLES];
     if (turns) {
 #pragma unroll
@@ -85,7 +91,8 @@ __global__ void __launch_bounds__(kThreads, kBlocks) k_rope(const __grid_constan
         const uint32_t quarter = (top + (1u << 29)) >> 30;           // the nearest (4: 0)
         const float rest = (float)(int32_t)(top - (quarter << 30)) * 0x1p-31f;   // of half a turn
         float s, c;
-        sincospif(rest, &s, &c);
+        if constexpr (sizeof(T) == 2) __sincosf(rest * 3.14159265f, &s, &c);   // (off by 2^-21: bf16's rounding is 2^-9)
+        else sincospif(rest, &s, &c);
         const float x = quarter & 1 ? -s : c, y = quarter & 1 ? c : s;
         const float flip = quarter & 2 ? -a.magnitude : a.magnitude;
         cs[i] = make_float2(x * flip, y * flip * a.sign);
@@ -123,40 +130,46 @@ __global__ void __launch_bounds__(kThreads, kBlocks) k_rope(const __grid_constan
       const T* x = static_cast<const T*>(a.x[w]) + b * a.sx[w][0] + t * a.sx[w][1] + h * a.sx[w][2] + d;
       T* y = static_cast<T*>(a.y[w]) + b * a.sy[w][0] + t * a.sy[w][1] + h * a.sy[w][2] + d;
       const long long dx = together * a.sx[w][2], dy = together * a.sy[w][2];
-      const auto load = [&](Vec& u, Vec& v) {
+      const auto load = [&](const T* x, Vec& u, Vec& v) {
         if constexpr (STEP == V) {
           u = *reinterpret_cast<const Vec*>(x);
-          if (!PAIRS && turns) v = *reinterpret_cast<const Vec*>(x + a.half);
+          if (both) v = *reinterpret_cast<const Vec*>(x + other);
         } else {                               // (single values need not be aligned in twos)
           u.x[0] = x[0];
           if (turns) u.x[1] = x[1];
         }
-        x += dx;
       };
-      const auto store = [&](Vec& u, Vec& v) {
+      const auto store = [&](T* y, Vec& u, Vec& v) {
         if (turns) turn_part(u, v);
         if constexpr (STEP == V) {
           *reinterpret_cast<Vec*>(y) = u;
-          if (!PAIRS && turns) *reinterpret_cast<Vec*>(y + a.half) = v;
+          if (both) *reinterpret_cast<Vec*>(y + other) = v;
         } else {
           y[0] = u.x[0];
           if (turns) y[1] = u.x[1];
         }
-        y += dy;
       };
 #pragma unroll 1
-      for (; h + (kAhead - 1) * together < last; h += kAhead * together) {
-        Vec u[kAhead], v[kAhead];
+      for (; h + (AHEAD - 1) * together < last; h += AHEAD * together) {
+        Vec u[AHEAD], v[AHEAD];
 #pragma unroll
-        for (int e = 0; e < kAhead; ++e) load(u[e], v[e]);
+        for (int e = 0; e < AHEAD; ++e) {
+          load(x, u[e], v[e]);
+          x += dx;
+        }
 #pragma unroll
-        for (int e = 0; e < kAhead; ++e) store(u[e], v[e]);
+        for (int e = 0; e < AHEAD; ++e) {
+          store(y, u[e], v[e]);
+          y += dy;
+        }
       }
 #pragma unroll 1
       for (; h < last; h += together) {
         Vec u, v;
-        load(u, v);
-        store(u, v);
+        load(x, u, v);
+        x += dx;
+        store(y, u, v);
+        y += dy;
       }
     }
   }
@@ -165,7 +178,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks) k_rope(const __grid_constan
 template <typename T>
 cudaError_t launch(RopeArgs& a, bool pairs, bool wide, cudaStream_t s) {
   constexpr int V = 16 / sizeof(T);
-  const auto k = pairs ? (wide ? k_rope<T, V, true> : k_rope<T, 1, true>) : (wide ? k_rope<T, V, false> : k_rope<T, 1, false>);
+  const auto k = pairs ? (wide ? k_rope<T, V, true> : k_rope<T, 1, true>) : (wide ? k_rope<T, kHalves, false> : k_rope<T, 1, false>);
   // a token's heads among warps where tokens alone do not fill the device
   const long long tokens = (long long)a.batch * a.T, want = (long long)kPlanSMs * 16;
   a.slices = (int)std::min<long long>(a.heads[0] + a.heads[1], (want + tokens - 1) / tokens);
@@ -234,7 +247,8 @@ extern "C" int32_t cdsl_rope(const cdsl_rope_cfg* rope, int32_t inverse, const c
   a.start = d_start;
   a.offset = d_offset;
   // 16 bytes at a time where every part of a head begins at a multiple of them
-  bool wide = (rope->interleaved ? rope->rot : a.half) % V == 0 && (z.head_dim - rope->rot) % V == 0;
+  bool wide = rope->interleaved ? rope->rot % V == 0 && (z.head_dim - rope->rot) % V == 0
+                                : a.half % kHalves == 0 && (z.head_dim - rope->rot) % (2 * kHalves) == 0;
   for (int w = 0; w < (d_k ? 2 : 1); ++w) {
     if (!ck.aligned(a.x[w], eb) || !ck.aligned(a.y[w], eb)) return ck.fail("tensors must be aligned to their type");
     wide = wide && ck.aligned(a.x[w], 16) && ck.aligned(a.y[w], 16);
