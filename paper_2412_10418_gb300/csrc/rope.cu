@@ -53,7 +53,7 @@ template <typename T, int V> struct alignas(sizeof(T) * V) Values { T x[V]; };
 // A warp has a token's heads, or a share of them: `slices` warps a token. A lane has the same part of every head it
 // turns, V values (halves: V of both sides; neighbours: V / 2 pairs, of single values a pair) or V that are not turned, so
 // that it needs its sines once, in registers; a head's parts are side by side in the lanes, several heads' where a head
-// has fewer than 32. four heads are loaded together.
+// has fewer than 32. Four heads are loaded together.
 template <typename T, int V, bool PAIRS>
 __global__ void __launch_bounds__(kThreads, kBlocks) k_rope(const __grid_constant__ RopeArgs a) {
   constexpr int STEP = PAIRS && V == 1 ? 2 : V;          // values of a turned part's first side

@@ -59,10 +59,8 @@ namespace {
 
 constexpr int kRows = 128;                     // query vectors per block
 constexpr int kSoft = 2 * kRows;               // softmax threads: two groups
-constexpr int kConv = 128;                     // threads that convert V
-constexpr int kThreads = kSoft + kConv + 96;
-constexpr int kConvWarp = kSoft / 32, kProducer = kConvWarp + kConv / 32, kIssuer = kProducer + 1,
-              kScaler = kProducer + 2;         // warps
+constexpr int kConv = 128;                     // threads that convert V, and as many K of 4 bits
+constexpr int kConvWarp = kSoft / 32;          // warps: softmax, conversion, loading, MMAs, scales
 constexpr float kMargin = 7.f;                 // base 2: probabilities are at most 2^kMargin of a reference, and
 constexpr float kUp = 7.f;                     // stored times 2^kUp: below fp16's largest
 constexpr int kBuf = 3;                        // S (then P) buffers in TMEM; O has the rest
@@ -74,6 +72,8 @@ template <int HD, int FORMAT>
 struct Cfg {
   static constexpr bool F8 = FORMAT == kF8, I4 = FORMAT == kI4;
   static constexpr bool TURNED = FORMAT != kBF16;          // V is turned into 16 bits
+  static constexpr int CONV = I4 ? 2 * kConv : kConv, THREADS = kSoft + CONV + 96;
+  static constexpr int PRODUCER = kConvWarp + CONV / 32, ISSUER = PRODUCER + 1, SCALER = PRODUCER + 2;   // warps
   static constexpr int EB = F8 ? 1 : 2;                    // I4: of K's tile
   static constexpr int KROW = HD * EB;                     // bytes of a K or V row
   static constexpr int BW = KROW < 128 ? KROW : 128;       // of it per tile block
@@ -95,9 +95,11 @@ struct Cfg {
   static constexpr int NST = FIT > 4 ? 4 : FIT;
   static_assert(NST >= 2, "stages");
   static constexpr uint32_t SCALE_OFF = KV_OFF + NST * 2 * HALF;
-  // K's scale of each slot, and V's, e4m3: relative to its reference (0: nothing, or not finite)
+  // K's scale of each slot, and V's, e4m3: relative to its reference (0: nothing, or not finite). 4 bits: V's by two groups,
+  // the two factors of its fma (0: the same)
   static constexpr uint32_t FACTOR_OFF = SCALE_OFF + (I4 ? 0 : NST * 2 * kKeys);
-  static constexpr uint32_t PLAN_OFF = FACTOR_OFF + (I4 ? 0 : NST * 2 * kKeys * 4);
+  static constexpr uint32_t FACTORS = I4 ? kKeys * HD / kGroup * 4 : 2 * kKeys * 4;
+  static constexpr uint32_t PLAN_OFF = FACTOR_OFF + NST * FACTORS;
   static constexpr size_t smem(int batch) { return 1024 + PLAN_OFF + plan_bytes(batch); }
 };
 
@@ -155,20 +157,26 @@ __device__ __forceinline__ void load_packed(const TreeArgs& a, const int* first,
         wait_for(kv ? &v_full[i % NST] : &k_full[i % NST], parity(i, NST), a.status);
 }
 
+// (x & mask) ^ c in one instruction, of which only one operand may be a constant: masks come from registers.
+__device__ __forceinline__ uint32_t and_xor(uint32_t x, uint32_t mask, uint32_t c) {
+  uint32_t d;
+  asm("lop3.b32 %0, %1, %2, %3, 0x6a;" : "=r"(d) : "r"(x), "r"(mask), "r"(c));
+  return d;
+}
 // Code I of both halves of a word of codes (low half: one group's, high half: the next one's) times their scales: in bf16 as
 // (128 + 8 u) scale / 8 - 24 scale, u = code + 8, and in fp16 as (1024 + 16 u) scale / 16 - 72 scale. Exact.
 template <int I>
-__device__ __forceinline__ uint32_t word_bf16(uint32_t w, uint32_t s8, uint32_t m24) {
+__device__ __forceinline__ uint32_t word_bf16(uint32_t w, uint32_t mask, uint32_t s8, uint32_t m24) {   // mask 0x00780078
   const uint32_t t = I == 0 ? w << 3 : w >> (4 * I - 3);
-  const uint32_t x = (t & 0x00780078u) ^ 0x43404340u;
+  const uint32_t x = and_xor(t, mask, 0x43404340u);
   uint32_t d;
   asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(x), "r"(s8), "r"(m24));
   return d;
 }
 template <int I>
-__device__ __forceinline__ uint32_t word_f16(uint32_t w, uint32_t s16, uint32_t m72) {
+__device__ __forceinline__ uint32_t word_f16(uint32_t w, uint32_t mask, uint32_t s16, uint32_t m72) {   // mask 0x00f000f0
   const uint32_t t = I == 0 ? w << 4 : w >> (4 * I - 4);
-  const uint32_t x = (t & 0x00f000f0u) ^ 0x64806480u;
+  const uint32_t x = and_xor(t, mask, 0x64806480u);
   uint32_t d;
   asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(x), "r"(s16), "r"(m72));
   return d;
@@ -180,11 +188,11 @@ __device__ __forceinline__ uint32_t times_bf16(uint32_t a, uint32_t b) {
 }
 
 template <int HD, int FORMAT>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__((Cfg<HD, FORMAT>::THREADS), 1)
     k_tree_rows(TreeArgs a, const __grid_constant__ CUtensorMap map) {
   using C = Cfg<HD, FORMAT>;
   constexpr bool F8 = C::F8, I4 = C::I4, TURNED = C::TURNED;
-  constexpr int NST = C::NST;
+  constexpr int NST = C::NST, kProducer = C::PRODUCER, kIssuer = C::ISSUER, kScaler = C::SCALER;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* const sm = smem_raw + ((1024 - (tc::smem_u32(smem_raw) & 1023)) & 1023);
   int* const s_first = reinterpret_cast<int*>(sm + C::PLAN_OFF);
@@ -201,11 +209,13 @@ __global__ void __launch_bounds__(kThreads, 1)
   __shared__ float s_ref[kRows], s_l[2][kRows];   // the rows' references; the groups' sums
   __shared__ uint8_t s_bad[2][kRows];          // the query is not finite
   __shared__ uint32_t s_mask[2][kRows + 1][kWords];
-  __shared__ uint32_t s_pieces[NST];
+  __shared__ uint32_t s_pieces[NST], s_masks[2];
   const Cache& c = a.c;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
+    s_masks[0] = 0x00780078u;
+    s_masks[1] = 0x00f000f0u;
     for (int i = 0; i < NST; ++i) {
       tc::mbar_init(&k_full[i], 1);
       tc::mbar_init(&v_full[i], 1);
@@ -397,6 +407,29 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         }
         far = __any_sync(0xffffffffu, far);
+        if constexpr (I4) {
+          constexpr int G2 = HD / kGroup / 2;
+          const uint32_t* const from = reinterpret_cast<const uint32_t*>(sm + C::KV_OFF + (st * 2 + 1) * C::PACKED + kKeys * C::RB) + 4 * lane * G2;
+          uint32_t* const to = reinterpret_cast<uint32_t*>(sm + C::FACTOR_OFF + st * C::FACTORS) + 8 * lane * G2;
+          const uint32_t rel = (uint32_t)max(254 - vref, 1) * 0x00800080u;   // 2^-reference
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int i = 0; i < G2; ++i) {
+              const uint32_t f = e < n && !(nan >> e & 1) ? times_bf16(from[e * G2 + i], rel) : 0u;
+              uint32_t x, y;
+              if (far) {
+                x = times_bf16(f, 0x3e003e00u);                  // 1 / 8
+                y = times_bf16(x, 0xc340c340u);                  // -192
+              } else {
+                const __half2 h = __floats2half2_rn(bf16_at(f, 0), bf16_at(f, 1));
+                const __half2 a16 = __hmul2(h, __float2half2_rn(0.0625f)), m72 = __hmul2(h, __float2half2_rn(-72.f));
+                x = *reinterpret_cast<const uint32_t*>(&a16);
+                y = *reinterpret_cast<const uint32_t*>(&m72);
+              }
+              *reinterpret_cast<uint2*>(to + 2 * (e * G2 + i)) = make_uint2(x, y);
+            }
+        }
         masks = __any_sync(0xffffffffu, masks);
         if constexpr (!I4) {
           float* to = reinterpret_cast<float*>(sm + C::FACTOR_OFF) + st * 2 * kKeys + 4 * lane;
@@ -730,9 +763,9 @@ __global__ void __launch_bounds__(kThreads, 1)
   } else if constexpr (I4) {
     // ------------------------------------------------------------------------- K to bf16, V to 16 bits
     // 16 bytes of a row at a time, 8 values of every group, a word (one of each of two groups in turn) to 16 bytes of a
-    // tile; exactly, with the scales. K is a chunk ahead, so that its scores are there when V's are asked for.
+    // tile; exactly, with the scales. Four warps have K, four V.
     constexpr int G2 = HD / kGroup / 2, PER = C::RB / 16, kRowsAt = kConv / PER;
-    const int row0 = (threadIdx.x - kSoft) / PER, part = (threadIdx.x - kSoft) % PER;
+    const int tid = (threadIdx.x - kSoft) % kConv, row0 = tid / PER, part = tid % PER;
     // (words 2, 3 first in the second block of 64 dimensions: eight lanes' stores then meet no bank twice)
     const int flip = part >> 1 & 1;
     uint32_t to[4];
@@ -742,30 +775,19 @@ __global__ void __launch_bounds__(kThreads, 1)
       to[i] = W / 8 * C::H_BLOCK + tc::row_offset(row0, W % 8, 128);
     }
     static_assert(C::BLOCK == C::H_BLOCK && C::BW == 128);
-    const auto words = [&](const uint8_t* half, int k, uint32_t (&w)[4], uint32_t (&sc)[G2]) {
-      const int row = row0 + k * kRowsAt;
-      const uint4 u = *reinterpret_cast<const uint4*>(half + row * C::RB + part * 16);
+    // (through shared memory, or the compiler knows them as constants and takes two instructions)
+    const volatile uint32_t* const masks = s_masks;
+    const uint32_t mb = masks[0], mh = masks[1];
+    const auto words = [&](const uint8_t* half, int k, uint32_t (&w)[4]) {
+      const uint4 u = *reinterpret_cast<const uint4*>(half + (row0 + k * kRowsAt) * C::RB + part * 16);
       w[0] = flip ? u.z : u.x; w[1] = flip ? u.w : u.y; w[2] = flip ? u.x : u.z; w[3] = flip ? u.y : u.w;
-      const uint8_t* const z = half + kKeys * C::RB + row * C::SB;
-      if constexpr (G2 == 2) {
-        const uint2 y = *reinterpret_cast<const uint2*>(z);
-        sc[0] = y.x; sc[1] = y.y;
-      } else {
-        sc[0] = *reinterpret_cast<const uint32_t*>(z);
-      }
     };
-    const auto bf16_words = [&](uint8_t* tile, const uint32_t (&w)[4], const uint32_t (&sc)[G2]) {
-      uint32_t s8[G2], m24[G2];
-#pragma unroll
-      for (int i = 0; i < G2; ++i) {
-        s8[i] = times_bf16(sc[i], 0x3e003e00u);                  // 1 / 8
-        m24[i] = times_bf16(s8[i], 0xc340c340u);                 // -192
-      }
+    const auto bf16_words = [&](uint8_t* tile, const uint32_t (&w)[4], const uint32_t (&s8)[G2], const uint32_t (&m24)[G2]) {
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         *reinterpret_cast<uint4*>(tile + to[i]) =
-            make_uint4(word_bf16<0>(w[i], s8[i % G2], m24[i % G2]), word_bf16<1>(w[i], s8[i % G2], m24[i % G2]),
-                       word_bf16<2>(w[i], s8[i % G2], m24[i % G2]), word_bf16<3>(w[i], s8[i % G2], m24[i % G2]));
+            make_uint4(word_bf16<0>(w[i], mb, s8[i % G2], m24[i % G2]), word_bf16<1>(w[i], mb, s8[i % G2], m24[i % G2]),
+                       word_bf16<2>(w[i], mb, s8[i % G2], m24[i % G2]), word_bf16<3>(w[i], mb, s8[i % G2], m24[i % G2]));
     };
     const auto turn_k = [&](int i) {
       const int st = i % NST;
@@ -773,11 +795,17 @@ __global__ void __launch_bounds__(kThreads, 1)
                                        wait_for(&kt_empty[i & 1], parity(i, 2) ^ 1, a.status)))
         return false;
       const uint8_t* const from = sm + C::KV_OFF + st * 2 * C::PACKED;
-#pragma unroll 2
+#pragma unroll 1
       for (int k = 0; k < kKeys / kRowsAt; ++k) {
-        uint32_t w[4], sc[G2];
-        words(from, k, w, sc);
-        bf16_words(sm + C::KT_OFF + (i & 1) * C::TILE + k * (kRowsAt * 128), w, sc);
+        uint32_t w[4], s8[G2], m24[G2];
+        words(from, k, w);
+        const uint32_t* const z = reinterpret_cast<const uint32_t*>(from + kKeys * C::RB + (row0 + k * kRowsAt) * C::SB);
+#pragma unroll
+        for (int e = 0; e < G2; ++e) {
+          s8[e] = times_bf16(z[e], 0x3e003e00u);                 // 1 / 8
+          m24[e] = times_bf16(s8[e], 0xc340c340u);               // -192
+        }
+        bf16_words(sm + C::KT_OFF + (i & 1) * C::TILE + k * (kRowsAt * 128), w, s8, m24);
       }
       tc::fence_proxy_async();
       tc::mbar_arrive(&kt_full[i & 1]);
@@ -785,9 +813,12 @@ __global__ void __launch_bounds__(kThreads, 1)
       return true;
     };
     const int n = end - begin;
-    bool ok = n == 0 || turn_k(0);
+    bool ok = true;
+    if (warp >= kConvWarp + kConv / 32) {      // K
+      for (int i = 0; i < n && ok; ++i) ok = turn_k(i);
+      ok = false;
+    }
     for (int i = 0; i < n && ok; ++i) {
-      if (i + 1 < n && !(ok = turn_k(i + 1))) break;
       const int st = i % NST;
       ok = wait_for(&f_full[st], parity(i, NST), a.status) && wait_for(&v_full[st], parity(i, NST), a.status) &&
            wait_for(&pv_done[i & 1], parity(i, 2) ^ 1, a.status);   // (chunk i - 2's: the buffer is free)
@@ -797,33 +828,29 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (threadIdx.x == kSoft) s_h_far[i & 1] = far;
       const uint8_t* const from = sm + C::KV_OFF + (st * 2 + 1) * C::PACKED;
       uint8_t* const tile = sm + C::H_OFF + (i & 1) * C::H_TILE;
-      const uint32_t rel = (uint32_t)max(254 - s_vref[st], 1) * 0x00800080u;   // 2^-reference
-#pragma unroll 2
+      const uint32_t* const factors = reinterpret_cast<const uint32_t*>(sm + C::FACTOR_OFF + st * C::FACTORS);
+#pragma unroll 1
       for (int k = 0; k < kKeys / kRowsAt; ++k) {
-        const int row = row0 + k * kRowsAt;
-        uint32_t w[4], sc[G2];
-        words(from, k, w, sc);
-        const bool there = (s_valid[st][row >> 5] & ~s_nan[st][row >> 5]) >> (row & 31) & 1;
-#pragma unroll
-        for (int e = 0; e < G2; ++e) sc[e] = there ? times_bf16(sc[e], rel) : 0u;
-        uint8_t* const at = tile + k * (kRowsAt * 128);
-        if (!far) {
-          uint32_t s16[G2], m72[G2];
-#pragma unroll
-          for (int e = 0; e < G2; ++e) {
-            const __half2 f = __floats2half2_rn(bf16_at(sc[e], 0), bf16_at(sc[e], 1));
-            const __half2 x = __hmul2(f, __float2half2_rn(0.0625f)), y = __hmul2(f, __float2half2_rn(-72.f));
-            s16[e] = *reinterpret_cast<const uint32_t*>(&x);
-            m72[e] = *reinterpret_cast<const uint32_t*>(&y);
-          }
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            *reinterpret_cast<uint4*>(at + to[e]) =
-                make_uint4(word_f16<0>(w[e], s16[e % G2], m72[e % G2]), word_f16<1>(w[e], s16[e % G2], m72[e % G2]),
-                           word_f16<2>(w[e], s16[e % G2], m72[e % G2]), word_f16<3>(w[e], s16[e % G2], m72[e % G2]));
+        uint32_t w[4], x[G2], y[G2];
+        words(from, k, w);
+        const uint32_t* const z = factors + (row0 + k * kRowsAt) * (2 * G2);
+        if constexpr (G2 == 2) {
+          const uint4 u = *reinterpret_cast<const uint4*>(z);
+          x[0] = u.x; y[0] = u.y; x[1] = u.z; y[1] = u.w;
         } else {
-          bf16_words(at, w, sc);
+          const uint2 u = *reinterpret_cast<const uint2*>(z);
+          x[0] = u.x; y[0] = u.y;
         }
+        uint8_t* const at = tile + k * (kRowsAt * 128);
+        if (far) {
+          bf16_words(at, w, x, y);
+          continue;
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          *reinterpret_cast<uint4*>(at + to[e]) =
+              make_uint4(word_f16<0>(w[e], mh, x[e % G2], y[e % G2]), word_f16<1>(w[e], mh, x[e % G2], y[e % G2]),
+                         word_f16<2>(w[e], mh, x[e % G2], y[e % G2]), word_f16<3>(w[e], mh, x[e % G2], y[e % G2]));
       }
       tc::fence_proxy_async();
       tc::mbar_arrive(&h_full[i & 1]);
@@ -857,7 +884,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         *reinterpret_cast<uint4*>(to + k * (kRowsAt * 128) + to1) = flip ? lo : hi;
       };
       if (!far) {
-#pragma unroll 2
+#pragma unroll 1
         for (int k = 0; k < kKeys / kRowsAt; ++k) {
           const uint4 u = *reinterpret_cast<const uint4*>(from + k * kRowsAt * C::BW);
           const float f = vf[row0 + k * kRowsAt];
@@ -913,7 +940,7 @@ cudaError_t launch(const TreeArgs& a, cudaStream_t s) {
   auto k = k_tree_rows<HD, FORMAT>;
   static OncePerDevice once;
   if (const cudaError_t e = allow_shared(once, k, C::smem(CDSL_TREE_MAX_BATCH))) return e;
-  return launch_pdl(k, dim3(a.blocks), dim3(kThreads), C::smem(a.c.batch), s, a, map);
+  return launch_pdl(k, dim3(a.blocks), dim3(C::THREADS), C::smem(a.c.batch), s, a, map);
 }
 
 }  // namespace
