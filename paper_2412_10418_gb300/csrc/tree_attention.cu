@@ -425,6 +425,94 @@ __global__ void __launch_bounds__(32 * kCombine) k_tree_combine(TreeArgs a) {
   if (lane == 0) store_lse(a, b, w, M, L);
 }
 
+// The same for items that many runs share (a 4-bit cache's, of a warp each): a block per vector, whose warps take parts in
+// turn and join what they have through shared memory.
+constexpr int kWide = 8;                       // warps
+template <typename T, int HD>
+__global__ void __launch_bounds__(32 * kWide) k_tree_combine_wide(TreeArgs a) {
+  constexpr int DPL = HD / 32;
+  __shared__ float s_m[kWide], s_l[kWide], s_o[kWide][HD];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int v = blockIdx.y, qb = blockIdx.x % a.QB, h = blockIdx.x / a.QB % a.c.kvh, b = blockIdx.x / a.QB / a.c.kvh;
+  const int n = nodes_of(a, b), live = live_blocks(a, n), u = item_units(a, len_of(a, b) + n);
+  if (qb >= live || v >= min(a.NQ, a.T * a.G - qb * a.NQ)) return pdl_wait();
+  int before = 0, total = 0;                   // units of the sequences before, and of all
+  for (int x = lane; x < a.c.batch; x += 32) {
+    const int w = units_of(a, len_of(a, x), nodes_of(a, x));
+    total += w;
+    if (x < b) before += w;
+  }
+  total = __reduce_add_sync(0xffffffffu, total);
+  before = __reduce_add_sync(0xffffffffu, before);
+  const int runs = runs_of(a, total), s = before + h * (live * u + a.QB - live) + qb * u;
+  const int r0 = run_of(s, total, runs), r1 = run_of(s + u - 1, total, runs);
+  pdl_wait();                                  // (no block ends before the pass has)
+  if (r0 == r1) return;                        // whole: written
+  auto slot = [&](int r) { return (size_t)r * 2 + (r == r0); };
+  float M = -INFINITY, L = 0.f, acc[DPL];
+#pragma unroll
+  for (int i = 0; i < DPL; ++i) acc[i] = 0.f;
+  for (int rb = r0 + warp; rb <= r1; rb += 32 * kWide) {   // 32 of the warp's parts: a lane has one's (m, l)
+    const int mine = rb + lane * kWide, cnt = min(32, (r1 - rb) / kWide + 1);
+    float m = -INFINITY, l = 0.f;
+    if (mine <= r1) {
+      m = a.part_ml[slot(mine) * 2 * a.NQ + v];
+      l = a.part_ml[(slot(mine) * 2 + 1) * a.NQ + v];
+    }
+    const float Mn = fmaxf(M, warp_max(m));
+    const float keep = M == -INFINITY ? 0.f : exp2f(M - Mn);
+    const float w = m == -INFINITY ? (l == 0.f ? 0.f : 1.f) : exp2f(m - Mn);   // (l NaN: kept)
+    L = L * keep + warp_sum(w * l);
+#pragma unroll
+    for (int i = 0; i < DPL; ++i) acc[i] *= keep;
+    for (int r = 0; r < cnt; r += kAhead) {
+      float z[kAhead][DPL];
+#pragma unroll
+      for (int e = 0; e < kAhead; ++e)
+        if (r + e < cnt) {
+          const float* const p = a.part_o + (slot(rb + (r + e) * kWide) * a.NQ + v) * HD + lane * DPL;
+          if constexpr (DPL == 4) {
+            const float4 t = *reinterpret_cast<const float4*>(p);
+            z[e][0] = t.x; z[e][1] = t.y; z[e][2] = t.z; z[e][3] = t.w;
+          } else {
+            const float2 t = *reinterpret_cast<const float2*>(p);
+            z[e][0] = t.x; z[e][1] = t.y;
+          }
+        }
+#pragma unroll
+      for (int e = 0; e < kAhead; ++e) {
+        const float wr = __shfl_sync(0xffffffffu, w, (r + e) & 31);
+        if (r + e < cnt)
+#pragma unroll
+          for (int i = 0; i < DPL; ++i) acc[i] = fmaf(wr, z[e][i], acc[i]);
+      }
+    }
+    M = Mn;
+  }
+  if (lane == 0) {
+    s_m[warp] = M;
+    s_l[warp] = L;
+  }
+#pragma unroll
+  for (int i = 0; i < DPL; ++i) s_o[warp][lane * DPL + i] = acc[i];
+  __syncthreads();
+  float top = -INFINITY;
+#pragma unroll
+  for (int w = 0; w < kWide; ++w) top = fmaxf(top, s_m[w]);
+  const Vec x = vector_of(a, h, qb, v);
+  for (int d = threadIdx.x; d < HD; d += 32 * kWide) {
+    float sum = 0.f, o = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWide; ++w) {
+      const float f = s_m[w] == -INFINITY ? (s_l[w] == 0.f ? 0.f : 1.f) : exp2f(s_m[w] - top);
+      sum = fmaf(f, s_l[w], sum);
+      o = fmaf(f, s_o[w][d], o);
+    }
+    store_out<T>(a, b, x, d, sum == 0.f ? 0.f : o / sum);
+    if (d == 0) store_lse(a, b, x, top, sum);
+  }
+}
+
 // Sizes of a pass, the same at every length: runs and workspace.
 struct Sizes {
   int NQ, QB, blocks;
@@ -453,6 +541,8 @@ void sizes_of(const Cache& c, bool tc, int H, int T, Sizes* z) {   // tc: bf16 q
 template <typename T, int HD>
 cudaError_t launch_combine(const TreeArgs& a, cudaStream_t s) {
   const int items = a.c.batch * a.c.kvh * a.QB, bounds = std::max(a.blocks - 1, 1);
+  if (a.c.format == kI4 && a.NQ < kRowsBlock && a.blocks >= kWide * items)   // (parts of an item, about)
+    return launch_pdl(k_tree_combine_wide<T, HD>, dim3(items, std::min(a.NQ, a.T * a.G)), dim3(32 * kWide), 0, s, a);
   const dim3 grid(std::min(items, bounds), (std::min(a.NQ, a.T * a.G) + kCombine - 1) / kCombine);
   return launch_pdl(bounds < items ? k_tree_combine<T, HD, true> : k_tree_combine<T, HD, false>, grid,
                     dim3(32 * kCombine), 0, s, a);
