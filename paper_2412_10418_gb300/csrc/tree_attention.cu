@@ -541,7 +541,7 @@ void sizes_of(const Cache& c, bool tc, int H, int T, Sizes* z) {   // tc: bf16 q
 template <typename T, int HD>
 cudaError_t launch_combine(const TreeArgs& a, cudaStream_t s) {
   const int items = a.c.batch * a.c.kvh * a.QB, bounds = std::max(a.blocks - 1, 1);
-  if (a.c.format == kI4 && a.NQ < kRowsBlock && a.blocks >= kWide * items)   // (parts of an item, about)
+  if (a.c.format == kI4 && a.NQ < kRowsBlock && a.blocks >= 32 * items)   // (parts of an item, about)
     return launch_pdl(k_tree_combine_wide<T, HD>, dim3(items, std::min(a.NQ, a.T * a.G)), dim3(32 * kWide), 0, s, a);
   const dim3 grid(std::min(items, bounds), (std::min(a.NQ, a.T * a.G) + kCombine - 1) / kCombine);
   return launch_pdl(bounds < items ? k_tree_combine<T, HD, true> : k_tree_combine<T, HD, false>, grid,

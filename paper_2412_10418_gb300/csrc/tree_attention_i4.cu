@@ -57,7 +57,8 @@ struct Cfg {
   static constexpr uint32_t S_BYTES = NQ * kPitch * 4, F_BYTES = NT * kTiles * 32 * PP * 8;
   static constexpr uint32_t MASK_OFF = P_OFF + (S_BYTES > F_BYTES ? S_BYTES : F_BYTES);
   static constexpr uint32_t PLAN_OFF = MASK_OFF + NQ * (kWords + 1) * 4;
-  static constexpr int WARPS = F32 || NQ == 16 ? 12 : 16;          // of an SM, by registers
+  static constexpr int WARPS = F32 || NQ == 16 ? 8 : 12;           // of an SM, by registers
+  static constexpr int K_TILES = NT == 2 ? 2 : 4, V_TILES = NT == 2 ? 1 : 2;   // side by side
   static constexpr size_t smem(int batch) { return PLAN_OFF + plan_bytes(batch); }
 };
 
@@ -326,7 +327,7 @@ __global__ void __launch_bounds__(32, Cfg<HD, NQ, F32>::WARPS) k_tree_i4(TreeArg
         return;
       }
       const uint32_t* const k_scales = reinterpret_cast<const uint32_t*>(sm + C::CODES);
-#pragma unroll 1
+#pragma unroll C::K_TILES
       for (int i = 0; i < kTiles; ++i) {
         float t[NT][4];
         uint32_t w[2][G], sc[2][G / 2];
@@ -546,7 +547,7 @@ __global__ void __launch_bounds__(32, Cfg<HD, NQ, F32>::WARPS) k_tree_i4(TreeArg
           }
         }
       // ---- O^T += V^T P^T: slots 16 tile + 4 q4 .. + 3 are the MMA's k
-#pragma unroll 1
+#pragma unroll C::V_TILES
       for (int i = 0; i < kTiles; ++i) {
         uint32_t b[NT][PP][2];
 #pragma unroll
