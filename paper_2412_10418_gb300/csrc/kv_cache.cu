@@ -330,67 +330,82 @@ __global__ void __launch_bounds__(kThreads) k_kv_write4(WriteArgs a) {
   if (part < G) reinterpret_cast<uint16_t*>(c.scale + r * c.srow)[part] = (uint16_t)(bad ? 0x7fc0u : s >> 16);
 }
 
-// Grid: (rows of a sequence over blocks, batch, layers).
+// Grid: (rows of a sequence over blocks, batch, layers or fewer): a thread has its row of every gridDim.z-th layer, kLayers
+// of them at a time: where it lies takes three dependent loads, which a layer of one's own would wait for each time.
+constexpr int kLayers = 4;
 template <typename T, int LPR>
-__global__ void __launch_bounds__(kThreads) k_kv_read4(ReadArgs a) {
+__global__ void __launch_bounds__(kThreads) k_kv_read4(ReadArgs a, int n_layers) {
   constexpr int G = LPR / 2, N = 16 / G;       // values of a group
   pdl_wait();
   pdl_launch_dependents();
   const Cache& c = a.r.c;
-  const int b = blockIdx.y, layer = blockIdx.z;
+  const int b = blockIdx.y;
   const unsigned row = (blockIdx.x * kThreads + threadIdx.x) / LPR;
   const int part = threadIdx.x % LPR;
   const unsigned h = row % c.kvh, kv = row / c.kvh & 1, t = row / c.kvh / 2;
   if ((int)t >= a.r.T) return;
   const int n = a.r.count ? a.r.count[b] : a.r.T;
-  uint2 u = make_uint2(0u, 0u);                // codes
-  uint32_t s[G / 2];                           // scales
-#pragma unroll
-  for (int i = 0; i < G / 2; ++i) s[i] = 0u;
+  int page = -1;
   if ((int)t < n) {
-    const int page = page_of(c, b, (long long)a.r.start[b] + t);
-    if (page < 0) {
-      if (part == 0) set_status(a.r.status, CDSL_ERANGE);
-    } else {
-      const int at = (a.r.start[b] + (int)t) & ((1 << c.page_shift) - 1);
-      const size_t r = row_of(c, a.r.layer + layer, page, kv, h, at);
-      u = *reinterpret_cast<const uint2*>(c.pool + r * c.row + part * 8);
-      const uint32_t* const sp = reinterpret_cast<const uint32_t*>(c.scale + r * c.srow);
-#pragma unroll
-      for (int i = 0; i < G / 2; ++i) s[i] = sp[i];
-      // (one scale that is not finite: the row's all count as NaN)
-      if (i4_not_finite(make_uint2(s[0], s[G / 2 - 1]), G))
-#pragma unroll
-        for (int i = 0; i < G / 2; ++i) s[i] = 0x7fc07fc0u;
-    }
+    page = page_of(c, b, (long long)a.r.start[b] + t);
+    if (page < 0 && part == 0) set_status(a.r.status, CDSL_ERANGE);
   }
-  T* const out = static_cast<T*>(kv ? a.v : a.k) +
-                 ((((size_t)layer * c.batch + b) * a.r.T + t) * c.kvh + h) * c.hd + part * N;
-  const uint32_t w[2] = {u.x, u.y};
-  float x[G][N];
+  const int at = (a.r.start[b] + (int)t) & ((1 << c.page_shift) - 1);
+#pragma unroll 1
+  for (int l0 = blockIdx.z; l0 < n_layers; l0 += kLayers * gridDim.z) {
+    uint2 u[kLayers];                          // codes
+    uint32_t s[kLayers][G / 2];                // scales
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {                // pieces
-    const int g = i % G;
-    float y[4];
-    i4x4_to_f32(w[i / 2] >> (i % 2 * 16), bf16_at(s[g / 2], g % 2), y);
+    for (int l = 0; l < kLayers; ++l) {
+      const int layer = l0 + l * gridDim.z;
+      u[l] = make_uint2(0u, 0u);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) x[g][i / G * 4 + e] = y[e];
-  }
+      for (int i = 0; i < G / 2; ++i) s[l][i] = 0u;
+      if (page >= 0 && layer < n_layers) {
+        const size_t r = row_of(c, a.r.layer + layer, page, kv, h, at);
+        u[l] = *reinterpret_cast<const uint2*>(c.pool + r * c.row + part * 8);
+        const uint32_t* const sp = reinterpret_cast<const uint32_t*>(c.scale + r * c.srow);
 #pragma unroll
-  for (int g = 0; g < G; ++g) {
-    if constexpr (sizeof(T) == 4) {
-#pragma unroll
-      for (int i = 0; i < N; i += 4)
-        *reinterpret_cast<float4*>(out + g * kGroup + i) = make_float4(x[g][i], x[g][i + 1], x[g][i + 2], x[g][i + 3]);
-    } else {
-      uint32_t two[N / 2];
-#pragma unroll
-      for (int i = 0; i < N / 2; ++i) {
-        const __nv_bfloat162 z = __floats2bfloat162_rn(x[g][2 * i], x[g][2 * i + 1]);
-        two[i] = *reinterpret_cast<const uint32_t*>(&z);
+        for (int i = 0; i < G / 2; ++i) s[l][i] = sp[i];
       }
-      if constexpr (N == 4) *reinterpret_cast<uint2*>(out + g * kGroup) = make_uint2(two[0], two[1]);
-      else *reinterpret_cast<uint4*>(out + g * kGroup) = make_uint4(two[0], two[1], two[2], two[3]);
+    }
+#pragma unroll
+    for (int l = 0; l < kLayers; ++l) {
+      const int layer = l0 + l * gridDim.z;
+      if (layer >= n_layers) break;
+      // (one scale that is not finite: the row's all count as NaN)
+      if (i4_not_finite(make_uint2(s[l][0], s[l][G / 2 - 1]), G))
+#pragma unroll
+        for (int i = 0; i < G / 2; ++i) s[l][i] = 0x7fc07fc0u;
+      T* const out = static_cast<T*>(kv ? a.v : a.k) +
+                     ((((size_t)layer * c.batch + b) * a.r.T + t) * c.kvh + h) * c.hd + part * N;
+      const uint32_t w[2] = {u[l].x, u[l].y};
+      float x[G][N];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {            // pieces
+        const int g = i % G;
+        float y[4];
+        i4x4_to_f32(w[i / 2] >> (i % 2 * 16), bf16_at(s[l][g / 2], g % 2), y);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[g][i / G * 4 + e] = y[e];
+      }
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+          for (int i = 0; i < N; i += 4)
+            *reinterpret_cast<float4*>(out + g * kGroup + i) = make_float4(x[g][i], x[g][i + 1], x[g][i + 2], x[g][i + 3]);
+        } else {
+          uint32_t two[N / 2];
+#pragma unroll
+          for (int i = 0; i < N / 2; ++i) {
+            const __nv_bfloat162 z = __floats2bfloat162_rn(x[g][2 * i], x[g][2 * i + 1]);
+            two[i] = *reinterpret_cast<const uint32_t*>(&z);
+          }
+          if constexpr (N == 4) *reinterpret_cast<uint2*>(out + g * kGroup) = make_uint2(two[0], two[1]);
+          else *reinterpret_cast<uint4*>(out + g * kGroup) = make_uint4(two[0], two[1], two[2], two[3]);
+        }
+      }
     }
   }
 }
@@ -527,8 +542,14 @@ extern "C" int32_t cdsl_kv_read(const cdsl_kv_cache* cache, int32_t layer, int32
   a.v = d_v;
   const dim3 grid(row_blocks(c, T), c.batch, n_layers);
   return by_shape(c, dtype, [&](auto t, auto lpr, auto f8) {
-    const auto k = c.format == kI4 ? k_kv_read4<decltype(t), lpr()> : k_kv_read<decltype(t), lpr(), f8()>;
-    return ck.launched(launch_pdl(k, grid, dim3(kThreads), 0, static_cast<cudaStream_t>(stream), a));
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (c.format == kI4) {
+      // (several layers a thread where there are blocks enough)
+      const long long each = (long long)grid.x * grid.y, want = (long long)kPlanSMs * 16;
+      const int z = (int)std::min<long long>(n_layers, std::max<long long>((n_layers + 2 * kLayers - 1) / (2 * kLayers), (want + each - 1) / each));
+      return ck.launched(launch_pdl(k_kv_read4<decltype(t), lpr()>, dim3(grid.x, grid.y, z), dim3(kThreads), 0, s, a, n_layers));
+    }
+    return ck.launched(launch_pdl(k_kv_read<decltype(t), lpr(), f8()>, grid, dim3(kThreads), 0, s, a));
   });
 }
 
