@@ -3,7 +3,7 @@
 A decoding step of `TreeDecoder`, for every sequence of the batch:
 
 1. M_q drafts a tree of tokens, level by level: the children of a node are M_q's most likely tokens after it.
-2. M_p runs once over the tree: per layer `cdsl_kv_write` and `cdsl_tree_attention`.
+2. M_p runs once over the tree: per layer `cdsl_rope`, `cdsl_kv_write` and `cdsl_tree_attention`.
 3. `cdsl_tree_verify` walks the tree by M_p's distributions and draws the token after the path.
 4. `cdsl_kv_commit` moves the path's K/V in both caches to their places.
 
@@ -27,16 +27,6 @@ import paper_2412_10418_gb300 as cdsl  # noqa: E402
 import synth  # noqa: E402
 
 
-def rope(x, pos, theta):
-    """x [B, T, heads, hd] turned by the angles of positions pos [B, T]; dimension i goes with i + hd / 2."""
-    half = x.shape[-1] // 2
-    freq = theta ** (-torch.arange(half, device=x.device, dtype=torch.float32) / half)
-    ang = pos[..., None, None].float() * freq
-    cos, sin = ang.cos(), ang.sin()
-    a, b = x[..., :half].float(), x[..., half:].float()
-    return torch.cat([a * cos - b * sin, b * cos + a * sin], -1).to(x.dtype)
-
-
 class Model:
     """A decoder whose K/V live in a paged cache of its own, `slots` tokens for each of `batch` sequences."""
 
@@ -48,20 +38,20 @@ class Model:
         self.cache = cdsl.KvCache.empty(shape.n_layers, batch * pages, shape.n_kv_heads, page_size, shape.head_dim, table,
                                         cache_dtype)
         self.max_len = pages * page_size - cdsl.TREE_MAX_NODES
+        self.rope = cdsl.Rope(shape.head_dim, theta=shape.rope_theta, device=dev)
         self.work = torch.empty(cdsl.cdsl_tree_attention_workspace(self.cache, cdsl.TREE_MAX_NODES, shape.n_heads),
                                 dtype=torch.uint8, device=dev)
 
     def forward(self, tokens, lens, depth, mask, nodes=None, head=True, status=None):
-        """Nodes tokens [B, T] at positions lens + depth: their K/V into slots lens .. lens + T - 1, and the logits of
+        """Nodes tokens [B, T] at positions lens + depth [B, T]: their K/V into slots lens .. lens + T - 1, and the logits of
         the tokens after them [B, T, vocab]."""
         s, w = self.shape, self.w
         B, T = tokens.shape
-        pos = lens[:, None] + depth
         h = F.embedding(tokens.clamp(0, s.vocab - 1), w["embed"])
         for l in range(s.n_layers):
             a = self.norm(h, w[f"l{l}.attn_norm"])
             q, k, v = (F.linear(a, w[f"l{l}.w{x}"]).view(B, T, -1, s.head_dim) for x in "qkv")
-            q, k = rope(q, pos, s.rope_theta), rope(k, pos, s.rope_theta)
+            cdsl.cdsl_rope(self.rope, q, q, lens, k=k, k_out=k, offset=depth)
             cdsl.cdsl_kv_write(self.cache, l, k, v, lens, count=nodes, status=status)
             out = torch.empty_like(q)
             cdsl.cdsl_tree_attention(self.cache, l, q, lens, mask, out, self.work, scale=s.head_dim ** -0.5,
@@ -93,7 +83,7 @@ class TreeDecoder:
         self.T, self.levels, self.widths = len(parents), levels, widths
         mask, depth = cdsl.cdsl_tree_mask(parents)
         self.mask = mask.to(dev).expand(B, -1, -1).contiguous()
-        self.depth = depth.to(dev)
+        self.depth = depth.to(dev).expand(B, -1).contiguous()
         self.parents = torch.tensor(parents, dtype=torch.int32, device=dev).expand(B, -1).contiguous()
         self.known = [torch.full((B,), l[-1] + 1, dtype=torch.int32, device=dev) for l in levels]
         self.tokens = torch.zeros((B, self.T), dtype=torch.int32, device=dev)
@@ -115,7 +105,7 @@ class TreeDecoder:
             part = prompts[:, first:min(n - 1, first + cdsl.TREE_MAX_NODES)].contiguous()
             T = part.shape[1]
             mask, depth = cdsl.cdsl_tree_mask([max(0, i - 1) for i in range(T)])
-            mask, depth = mask.to(part.device).expand(B, -1, -1).contiguous(), depth.to(part.device)
+            mask, depth = (x.to(part.device).expand(B, *x.shape).contiguous() for x in (mask, depth))
             nodes = (lengths - 1 - first).clamp(0, T).int()
             for m in (self.target, self.draft):
                 m.forward(part, self.lens, depth, mask, nodes, head=False, status=self.status)
@@ -154,6 +144,9 @@ class TreeDecoder:
         self.tokens[:, 0] = self.emitted.gather(1, (self.n_path - 1).clamp(min=0).long()[:, None])[:, 0]
 
 
+CACHES = {"e4m3": torch.float8_e4m3fn, "bf16": torch.bfloat16, "4-bit": torch.uint8}
+
+
 def build(workload, widths, slots, self_draft=False, cache_dtype=None, **kw):
     """A decoder of a `synth` workload's models; self_draft: M_p drafts for itself."""
     target = synth.model_weights(workload, "target", device="cuda")
@@ -172,11 +165,13 @@ def main():
     p.add_argument("--widths", default="3,2,1,1", help="children of the nodes at each depth")
     p.add_argument("--temperature", type=float, default=0.0)
     p.add_argument("--new", type=int, default=64, help="tokens to decode per sequence")
+    p.add_argument("--cache", default="e4m3", choices=sorted(CACHES), help="the caches' type")
     p.add_argument("--self-draft", action="store_true", help="the target drafts for itself")
     a = p.parse_args()
     wl = synth.WORKLOADS[a.workload]
     widths = tuple(int(x) for x in a.widths.split(",") if x)
-    d = build(wl, widths, wl.prompt_len + a.new + 2 * cdsl.TREE_MAX_NODES, a.self_draft, temperature=a.temperature)
+    d = build(wl, widths, wl.prompt_len + a.new + 2 * cdsl.TREE_MAX_NODES, a.self_draft, CACHES[a.cache],
+              temperature=a.temperature)
     prompts = torch.from_numpy(synth.prompts(wl)).cuda()
     d.prefill(prompts, torch.full((wl.batch,), wl.prompt_len, dtype=torch.int32, device="cuda"))
     out = [[] for _ in range(wl.batch)]
