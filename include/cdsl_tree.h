@@ -139,8 +139,8 @@ CDSL_API int32_t cdsl_tree_attention(const cdsl_kv_cache* cache, int32_t layer, 
  * how many entries of its tables hold each page (0: free). The three calls below make a new table and new counts from
  * old ones, on the device and in order of nothing but their indexes: free pages are dealt lowest first. Table entries
  * of -1 hold nothing; others outside [0, n_pages) latch CDSL_ERANGE and count as -1. Holders beyond the table (a prefix
- * that is kept, another table of the pool) are counts that the caller has added. A count that falls below 0 latches
- * CDSL_EINVAL. d_workspace: cdsl_kv_pages_workspace bytes, 256-byte aligned, in any state; it holds nothing between
+ * that is kept, another table of the pool) are counts that the caller has added. Counts that are below the table's own
+ * entries latch CDSL_EINVAL. d_workspace: cdsl_kv_pages_workspace bytes, 256-byte aligned, in any state; it holds nothing between
  * calls. new_batch there: of the new table, the largest of those that are to use it. */
 CDSL_API int32_t cdsl_kv_pages_workspace(const cdsl_kv_cache* cache, int32_t new_batch, size_t* bytes);
 

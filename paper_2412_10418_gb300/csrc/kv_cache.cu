@@ -427,7 +427,8 @@ constexpr int kMoves = 8;              // rows that a thread holds at a time
 // strictly increasing from 0, so entry i's target i is below the sources of all later entries. Blocks have a thread a
 // part, so that one wave takes a served batch: 40 layers of 16 trees of 49 nodes in 7.7 us, 3 us less than with 256
 // threads a block; 16 rows in place of 8 a thread, 1.5 us more.
-__global__ void __launch_bounds__(kThreads) k_kv_commit(CommitArgs a) {
+template <typename S>
+__global__ void __launch_bounds__(kThreads) k_kv_commit(CommitArgs a) {   // S: a row's scales
   __shared__ int s_from[CDSL_TREE_MAX_NODES], s_to[CDSL_TREE_MAX_NODES];   // page << 8 | place, -1
   pdl_wait();
   pdl_launch_dependents();
@@ -468,9 +469,7 @@ __global__ void __launch_bounds__(kThreads) k_kv_commit(CommitArgs a) {
   const int per = c.row / 16, codes = c.kvh * per;   // 16-byte parts of a row, of all heads
   for (int q = threadIdx.x; q < codes + c.kvh; q += blockDim.x) {
     if (q < codes) move(reinterpret_cast<uint4*>(c.pool) + q % per, per, q / per);
-    else if (c.srow == 1) move(c.scale, 1, q - codes);
-    else if (c.srow == 4) move(reinterpret_cast<uint32_t*>(c.scale), 1, q - codes);
-    else move(reinterpret_cast<uint2*>(c.scale), 1, q - codes);
+    else move(reinterpret_cast<S*>(c.scale), 1, q - codes);
   }
 }
 
@@ -563,6 +562,7 @@ extern "C" int32_t cdsl_kv_commit(const cdsl_kv_cache* cache, const int32_t* d_l
   if (d_new_lens == d_lens) return ck.fail("d_new_lens must not be d_lens");
   const CommitArgs a = {c, d_lens, d_path, d_n_path, T, d_new_lens, d_status};
   const int parts = c.kvh * (c.row / 16 + 1);   // a token's, scales last: a thread each
-  return ck.launched(launch_pdl(k_kv_commit, dim3(c.n_layers, 2, c.batch), dim3(std::min(kThreads, (parts + 31) / 32 * 32)), 0,
+  const auto k = c.srow == 1 ? k_kv_commit<uint8_t> : c.srow == 4 ? k_kv_commit<uint32_t> : k_kv_commit<uint2>;
+  return ck.launched(launch_pdl(k, dim3(c.n_layers, 2, c.batch), dim3(std::min(kThreads, (parts + 31) / 32 * 32)), 0,
                                 static_cast<cudaStream_t>(stream), a));
 }

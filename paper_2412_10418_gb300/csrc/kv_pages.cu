@@ -215,6 +215,8 @@ __global__ void __launch_bounds__(kPlan) k_resize(PagesArgs a) {
     } else if (!is) {
       ++missing;
       page = -2;
+    } else if (__ldcg(a.new_refs + page) < 1) {
+      set_status(a.status, CDSL_EINVAL);       // (this entry holds it)
     }
     a.new_table[i] = page;
   }
@@ -279,7 +281,9 @@ __global__ void __launch_bounds__(kPlan) k_compact_plan(PagesArgs a) {
   for (long long i = tid; i < (long long)c.batch * c.max_pages; i += kPlan) {
     const int page = c.table[i];
     if (!is_page(c, page) && page != -1) set_status(a.status, CDSL_ERANGE);
-    a.new_table[i] = is_page(c, page) ? a.page_map[page] : -1;
+    const int to = is_page(c, page) ? a.page_map[page] : -1;
+    if (to < 0 && is_page(c, page)) set_status(a.status, CDSL_EINVAL);   // (an entry of a page that nobody holds)
+    a.new_table[i] = to;
   }
   if (tid == 0) {
     *a.n_moves = movers;

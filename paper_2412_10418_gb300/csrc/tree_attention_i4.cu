@@ -389,15 +389,16 @@ __global__ void __launch_bounds__(32, Cfg<HD, NQ, F32>::WARPS) k_tree_i4(TreeArg
         return;
       }
       uint8_t* const v_scales = sm + C::V_OFF + C::CODES;
-      // V's scales of slots 2 lane, 2 lane + 1. (Of one that is not finite, bits 7 .. 14 are all set: 0x80 carries into bit
+      // V's scales of the slots of a pair of the MMA's k, s0 and s0 + 4. (Of one that is not finite, bits 7 .. 14 are all set: 0x80 carries into bit
       // 15. K's need no look: the scores are NaN.)
+      const int s0 = 16 * (lane >> 3) + 8 * (lane >> 2 & 1) + (lane & 3);
       uint32_t even[G / 2], odd[G / 2];
       if constexpr (G == 4) {
-        const uint4 u = reinterpret_cast<const uint4*>(v_scales)[lane];
-        even[0] = u.x; even[1] = u.y; odd[0] = u.z; odd[1] = u.w;
+        const uint2 u = reinterpret_cast<const uint2*>(v_scales)[s0], z = reinterpret_cast<const uint2*>(v_scales)[s0 + 4];
+        even[0] = u.x; even[1] = u.y; odd[0] = z.x; odd[1] = z.y;
       } else {
-        const uint2 u = reinterpret_cast<const uint2*>(v_scales)[lane];
-        even[0] = u.x; odd[0] = u.y;
+        even[0] = reinterpret_cast<const uint32_t*>(v_scales)[s0];
+        odd[0] = reinterpret_cast<const uint32_t*>(v_scales)[s0 + 4];
       }
       uint32_t even_bad = 0, odd_bad = 0;
 #pragma unroll
@@ -405,7 +406,7 @@ __global__ void __launch_bounds__(32, Cfg<HD, NQ, F32>::WARPS) k_tree_i4(TreeArg
         even_bad |= (even[i] & 0x7f807f80u) + 0x00800080u;
         odd_bad |= (odd[i] & 0x7f807f80u) + 0x00800080u;
       }
-      // rows that are not finite, as bits of the even and of the odd slots
+      // rows that are not finite, as bits of the lanes' first and second slots
       uint32_t v_bad[2] = {0u, 0u};
       if (__any_sync(0xffffffffu, ((even_bad | odd_bad) & 0x80008000u) != 0)) {
         v_bad[0] = __ballot_sync(0xffffffffu, (even_bad & 0x80008000u) != 0);
@@ -421,7 +422,7 @@ __global__ void __launch_bounds__(32, Cfg<HD, NQ, F32>::WARPS) k_tree_i4(TreeArg
       // Code of its own for stretches with slots of the tree, past the item's, without a page or with a row that is not
       // finite: as one, every score has selects.
       const bool masked = valid != ~0ull || slot + kStretch > s.len || (v_bad[0] | v_bad[1]) != 0;
-      // ---- maxima, probabilities, sums: slots 16 tile + 4 q4 .. + 3 of vector r (+ 8)
+      // ---- maxima, probabilities, sums: slots 16 tile + q4, + 4, + 8, + 12 of vector r (+ 8)
       uint32_t pf[NT][kTiles][PP][2];
       bool raised = false;
       float alpha[NT];
@@ -443,18 +444,16 @@ __global__ void __launch_bounds__(32, Cfg<HD, NQ, F32>::WARPS) k_tree_i4(TreeArg
               else y = __funnelshift_r(w[f >> 5], w[(f >> 5) + 1], f & 31);
               seen |= (uint64_t)y << (32 * h);
             }
-            seen = v < s.nq ? (seen & valid) >> (4 * q4) : 0ull;
+            seen = v < s.nq ? (seen & valid) >> q4 : 0ull;
           }
           float t[kTiles][4], top = -INFINITY;
 #pragma unroll
           for (int i = 0; i < kTiles; ++i) {
-            const float4 y = *reinterpret_cast<const float4*>(s_p + v * kPitch + 16 * i + 4 * q4);
-            t[i][0] = y.x; t[i][1] = y.y; t[i][2] = y.z; t[i][3] = y.w;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              t[i][e] *= fa;
+              t[i][e] = s_p[v * kPitch + 16 * i + 4 * e + q4] * fa;
               if constexpr (general) {
-                if (!(seen >> (16 * i + e) & 1)) continue;
+                if (!(seen >> (16 * i + 4 * e) & 1)) continue;
               }
               top = fmaxf(top, t[i][e]);
             }
@@ -475,9 +474,9 @@ __global__ void __launch_bounds__(32, Cfg<HD, NQ, F32>::WARPS) k_tree_i4(TreeArg
             for (int e = 0; e < 4; ++e) {
               y[e] = ex2(fmaf(t[i][e], fb[n], -off));
               if constexpr (general) {
-                if (!(seen >> (16 * i + e) & 1)) y[e] = 0.f;
+                if (!(seen >> (16 * i + 4 * e) & 1)) y[e] = 0.f;
                 sum += y[e];
-                if (y[e] != 0.f && v_bad[e & 1] >> (8 * i + 2 * q4 + e / 2) & 1) y[e] = __uint_as_float(0x7fc00000u);
+                if (y[e] != 0.f && v_bad[e & 1] >> (8 * i + 4 * (e >> 1) + q4) & 1) y[e] = __uint_as_float(0x7fc00000u);
               } else {
                 sum += y[e];
               }
@@ -500,7 +499,7 @@ __global__ void __launch_bounds__(32, Cfg<HD, NQ, F32>::WARPS) k_tree_i4(TreeArg
       if (masked) {
         softmax(std::true_type());
         // nothing of a slot that is not there, or whose V is not finite, may reach the sums
-        const bool e0 = valid >> (2 * lane) & 1 && !(v_bad[0] >> lane & 1), e1 = valid >> (2 * lane + 1) & 1 && !(v_bad[1] >> lane & 1);
+        const bool e0 = valid >> s0 & 1 && !(v_bad[0] >> lane & 1), e1 = valid >> (s0 + 4) & 1 && !(v_bad[1] >> lane & 1);
 #pragma unroll
         for (int i = 0; i < G / 2; ++i) {
           if (!e0) even[i] = 0u;
@@ -513,7 +512,7 @@ __global__ void __launch_bounds__(32, Cfg<HD, NQ, F32>::WARPS) k_tree_i4(TreeArg
         uint32_t f[G];
 #pragma unroll
         for (int g = 0; g < G; ++g) f[g] = mul_bf16x2(both(even[g / 2], odd[g / 2], g), 0x3e003e00u);   // 1 / 8
-        uint8_t* const to = sm + C::F_OFF + lane * (4 * G);
+        uint8_t* const to = sm + C::F_OFF + ((lane & 0x18) + 2 * (lane & 3) + (lane >> 2 & 1)) * (4 * G);   // [tile][q4][half]
         if constexpr (G == 4) *reinterpret_cast<uint4*>(to) = make_uint4(f[0], f[1], f[2], f[3]);
         else *reinterpret_cast<uint2*>(to) = make_uint2(f[0], f[1]);
       }
@@ -546,7 +545,7 @@ __global__ void __launch_bounds__(32, Cfg<HD, NQ, F32>::WARPS) k_tree_i4(TreeArg
             for (int p = 0; p < PP; ++p) *reinterpret_cast<uint2*>(to + 2 * p) = make_uint2(pf[n][i][p][0], pf[n][i][p][1]);
           }
         }
-      // ---- O^T += V^T P^T: slots 16 tile + 4 q4 .. + 3 are the MMA's k
+      // ---- O^T += V^T P^T: slots 16 tile + q4, + 4, + 8, + 12 are the lane's k (so that four lanes' rows lie next to one another)
 #pragma unroll C::V_TILES
       for (int i = 0; i < kTiles; ++i) {
         uint32_t b[NT][PP][2];
@@ -567,7 +566,7 @@ __global__ void __launch_bounds__(32, Cfg<HD, NQ, F32>::WARPS) k_tree_i4(TreeArg
         uint32_t w[4][G / 2], f[2][G];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const uint8_t* const from = sm + C::V_OFF + (16 * i + 4 * q4 + e) * C::RB + r * (C::RB / 8);
+          const uint8_t* const from = sm + C::V_OFF + (16 * i + 4 * e + q4) * C::RB + r * (C::RB / 8);
           if constexpr (G == 4) {
             const uint2 u = *reinterpret_cast<const uint2*>(from);
             w[e][0] = u.x; w[e][1] = u.y;

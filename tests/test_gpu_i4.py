@@ -272,6 +272,40 @@ def test_small_values_keep_their_weights_beside_huge_ones(cdsl, dtype, T):
 
 
 @DTYPES
+@pytest.mark.parametrize("B,kvh,G,hd,n", [(1, 1, 4, 128, 9000), (1, 2, 1, 64, 6001), (2, 1, 12, 64, 5000), (1, 1, 16, 128, 4097)])
+def test_attention_of_few_long_sequences(cdsl, dtype, B, kvh, G, hd, n):
+    """Items of many runs, which blocks of several warps join."""
+    lens = [n] + [n // 3] * (B - 1)
+    c, q, mask, nodes = problem(cdsl, B, 1, kvh * G, kvh, hd, 64, lens, dtype, seed=n)
+    got = attend(cdsl, c, 1, q, lens, mask, nodes, hd ** -0.5)
+    check(c, 1, q, lens, mask, nodes, hd ** -0.5, got)
+    again = attend(cdsl, c, 1, q, lens, mask, nodes, hd ** -0.5)
+    assert torch.equal(got[0], again[0]) and torch.equal(got[1], again[1])
+
+
+@DTYPES
+@pytest.mark.parametrize("T", [1, 3])
+def test_attention_of_runs_of_thousands_of_slots(cdsl, dtype, T):
+    """64 sequences over the same 16,384 slots: a run has more slots than one chain of sums takes; their sizes rise with the
+    slots, so that what comes first does not vanish beside the rest, and scores rise and fall."""
+    n, H, kvh, hd, B = 16384, 32, 8, 64, 64
+    one, q, mask, _ = problem(cdsl, 1, T, H, kvh, hd, 64, [n], dtype, kind="chain", seed=1)
+    g = torch.Generator().manual_seed(2)
+    k, v = (torch.randn((1, n + T, kvh, hd), generator=g) for _ in range(2))
+    v *= torch.linspace(3, 1, n + T)[None, :, None, None]
+    k *= torch.linspace(0.5, 1.5, n + T)[None, :, None, None]
+    cdsl.cdsl_kv_write(one.c, 1, k.cuda(), v.cuda(), ints(0))
+    many = copy.copy(one)
+    many.table = one.table.expand(B, -1).contiguous()
+    many.c = one.c.at(many.table)
+    lens, nodes = [n - 7 * b for b in range(B)], [T] * B
+    qs, masks = torch.cat([q * (1 + b / 64) for b in range(B)]), mask.expand(B, -1, -1)
+    got = attend(cdsl, many, 1, qs, lens, masks, nodes, 0.125)
+    for b in (0, 31, 63):
+        check(one, 1, qs[b:b + 1], lens[b:b + 1], mask, [T], 0.125, (got[0][b:b + 1], got[1][b:b + 1]))
+
+
+@DTYPES
 def test_attention_takes_strides_streams_and_graphs(cdsl, dtype):
     """Queries as a slice of a fused projection, off 16 bytes too; output in another order; a stream that is not the
     tensors' own; a captured call replayed at other lengths, two graphs with one workspace one after the other."""

@@ -255,6 +255,26 @@ def test_compact(cdsl, dtype, kvh, hd, page, B, cols, gone):
     assert [own.page_table.tolist(), r.tolist()] == [want[0], want[1]]
 
 
+def test_counts_below_the_tables_are_latched(cdsl):
+    """An entry of a page that the counts call free: by every call, and nothing outside the outputs is written."""
+    c = pool(cdsl, U8, 1, 6, 1, 16, 64, tensor([[0, 1], [2, -1]]))
+    before = raw(c)
+    ws = workspace(cdsl, c)
+    outs = [torch.full(s, 77, dtype=torch.int32, device="cuda") for s in ((2, 2), (6,), (6,), (1,))]
+    for refs in ([1, 0, 1, 0, 0, 0], [1, -1, 1, 0, 0, 0]):
+        st = status()
+        cdsl.cdsl_kv_resize(c, ints(*refs), ints(32, 16), *outs[:2], ws, status=st)
+        assert int(st) == cdsl.CDSL_EINVAL and outs[0].tolist() == [[0, 1], [2, -1]]
+        st.zero_()
+        cdsl.cdsl_kv_resize(c, ints(*refs), ints(0, 0), *outs[:2], ws, status=st)
+        assert int(st) == cdsl.CDSL_EINVAL
+        st.zero_()
+        cdsl.cdsl_kv_compact(c, ints(*refs), *outs, ws, status=st)
+        assert int(st) == cdsl.CDSL_EINVAL and int(outs[3]) == 2 and outs[0].tolist() == [[0, -1], [1, -1]]
+        c = pool(cdsl, U8, 1, 6, 1, 16, 64, tensor([[0, 1], [2, -1]]))
+        assert all(torch.equal(x, y) for x, y in zip(before, raw(c)))
+
+
 def test_page_calls_in_graphs_and_on_other_streams(cdsl):
     """Captured once and replayed with other lengths and successors, on a side stream too."""
     rng, P = random.Random(5), 16
