@@ -41,6 +41,7 @@ namespace {
 
 constexpr int kStretch = 64;                   // slots at a time: a unit
 constexpr int kTiles = kStretch / 16;
+constexpr int kWarps = 4;                      // of a block: one to each of an SM's four schedulers
 constexpr int kPitch = kStretch + 4;           // floats of a vector's scores
 constexpr int kChain = 64;                     // stretches of O^T's chain (512 products: 2^-15 of it at worst)
 
@@ -56,7 +57,8 @@ struct Cfg {
   // scores, then P's fragments: PP planes of two words for each tile and lane
   static constexpr uint32_t S_BYTES = NQ * kPitch * 4, F_BYTES = NT * kTiles * 32 * PP * 8;
   static constexpr uint32_t MASK_OFF = P_OFF + (S_BYTES > F_BYTES ? S_BYTES : F_BYTES);
-  static constexpr uint32_t PLAN_OFF = MASK_OFF + NQ * (kWords + 1) * 4;
+  static constexpr uint32_t WARP_BYTES = (MASK_OFF + NQ * (kWords + 1) * 4 + 127) / 128 * 128;
+  static constexpr uint32_t PLAN_OFF = kWarps * WARP_BYTES;
   static constexpr int WARPS = F32 || NQ == 16 ? 8 : 12;           // of an SM, by registers
   static constexpr int K_TILES = NT == 2 ? 2 : 4, V_TILES = NT == 2 ? 1 : 2;   // side by side
   static constexpr size_t smem(int batch) { return PLAN_OFF + plan_bytes(batch); }
@@ -124,35 +126,38 @@ __device__ __forceinline__ uint32_t value_bf16(uint32_t x, uint32_t mask, uint32
 }
 
 template <int HD, int NQ, bool F32>
-__global__ void __launch_bounds__(32, Cfg<HD, NQ, F32>::WARPS) k_tree_i4(TreeArgs a) {
+__global__ void __launch_bounds__(32 * kWarps, Cfg<HD, NQ, F32>::WARPS / kWarps) k_tree_i4(TreeArgs a) {
   using C = Cfg<HD, NQ, F32>;
   using T = std::conditional_t<F32, float, __nv_bfloat16>;
   constexpr int G = C::G, NT = C::NT, QP = C::QP, PP = C::PP;
-  extern __shared__ __align__(128) uint8_t sm[];
-  __shared__ __align__(8) uint64_t full[2];    // K, V
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ __align__(8) uint64_t s_full[kWarps][2];   // K, V
   __shared__ uint32_t s_masks[4];
-  __shared__ Segment s_seg[2];                 // this segment and the next (registers are dear)
+  __shared__ Segment s_segs[kWarps][2];        // this segment and the next (registers are dear)
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, run = blockIdx.x * kWarps + warp;
+  uint8_t* const sm = smem + warp * C::WARP_BYTES;
+  uint64_t* const full = s_full[warp];
+  Segment* const s_seg = s_segs[warp];
   float* const s_p = reinterpret_cast<float*>(sm + C::P_OFF);
   uint32_t* const s_mask = reinterpret_cast<uint32_t*>(sm + C::MASK_OFF);
-  int* const s_first = reinterpret_cast<int*>(sm + C::PLAN_OFF);
+  int* const s_first = reinterpret_cast<int*>(smem + C::PLAN_OFF);
   const Cache& c = a.c;
-  const int lane = threadIdx.x, r = lane >> 2, q4 = lane & 3;   // fragments' row (or column) and quarter
+  const int r = lane >> 2, q4 = lane & 3;   // fragments' row (or column) and quarter
   if (lane == 0) {
     tc::mbar_init(&full[0], 1);
     tc::mbar_init(&full[1], 1);
     tc::fence_mbar_init();
   }
+  if (threadIdx.x < 3) s_masks[lane] = lane == 0 ? 0x000f000fu : lane == 1 ? 0x00f000f0u : 0x00780078u;
   pdl_wait();
   pdl_launch_dependents();
   build_plan(a, s_first);                      // (ends in a block barrier)
   if (blockIdx.x == 0) check_lens(a);
   const int total = s_first[c.batch], runs = runs_of(a, total);
-  if ((int)blockIdx.x >= runs) return;
-  const int end = run_begin(blockIdx.x + 1, total, runs);
+  if (run >= runs) return;
+  const int end = run_begin(run + 1, total, runs);
   const float fa = a.scale * (F32 ? 0x1p-14f : 0x1p10f);   // of all scores: 2^-14 of the queries, 2^24 of the codes
   // (through shared memory, or the compiler knows them as constants and takes two instructions)
-  if (lane < 3) s_masks[lane] = lane == 0 ? 0x000f000fu : lane == 1 ? 0x00f000f0u : 0x00780078u;
-  __syncwarp();
   const volatile uint32_t* const masks = s_masks;
   const uint32_t k0 = masks[0], k4 = masks[1], kv = masks[2];
   const int P = 1 << c.page_shift, rows = min(P, kStretch), shift = min(c.page_shift, 6);
@@ -195,7 +200,7 @@ __global__ void __launch_bounds__(32, Cfg<HD, NQ, F32>::WARPS) k_tree_i4(TreeArg
   };
 
   int it = 0;                                  // stretches
-  int unit = run_begin(blockIdx.x, total, runs), turn = 0;
+  int unit = run_begin(run, total, runs), turn = 0;
   if (lane == 0) s_seg[0] = segment_at(a, s_first, unit, end);
   __syncwarp();
   Stretch x = {};
@@ -286,7 +291,7 @@ __global__ void __launch_bounds__(32, Cfg<HD, NQ, F32>::WARPS) k_tree_i4(TreeArg
             for (int e = 0; e < 4; ++e) o[g][h][n][e] = 0.f;
     };
     clear();
-    const size_t part = (size_t)blockIdx.x * 2 + (s.c0 == 0);
+    const size_t part = (size_t)run * 2 + (s.c0 == 0);
     // The sums behind O^T's chain: in the part's place in the workspace, relative to the maxima m_then. (A whole item's is
     // free while the run is at it: it ends before the run's last part begins.)
     bool chained = false;
@@ -676,7 +681,7 @@ cudaError_t launch(const TreeArgs& a, cudaStream_t s) {
   const auto k = k_tree_i4<HD, NQ, F32>;
   static OncePerDevice once;
   if (const cudaError_t e = allow_shared(once, k, C::smem(CDSL_TREE_MAX_BATCH))) return e;
-  return launch_pdl(k, dim3(a.blocks), dim3(32), C::smem(a.c.batch), s, a);
+  return launch_pdl(k, dim3((a.blocks + kWarps - 1) / kWarps), dim3(32 * kWarps), C::smem(a.c.batch), s, a);
 }
 
 template <typename F>
