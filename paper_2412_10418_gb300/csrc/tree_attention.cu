@@ -527,7 +527,7 @@ void bytes_of(const Cache& c, Sizes* z) {
 void sizes_of(const Cache& c, bool tc, int H, int T, Sizes* z) {   // tc: bf16 queries
   const int vectors = T * (H / c.kvh);
   if (c.format == kI4) {
-    z->NQ = vectors <= 8 || !tc ? 8 : vectors <= 16 ? 16 : kRowsBlock;
+    z->NQ = !tc ? 8 : vectors <= 4 ? 4 : vectors <= 8 ? 8 : vectors <= 16 ? 16 : kRowsBlock;
     z->QB = (vectors + z->NQ - 1) / z->NQ;
     z->blocks = kPlanSMs * (z->NQ == kRowsBlock ? 1 : i4_blocks_per_sm(c, z->NQ, !tc));
     return bytes_of(c, z);

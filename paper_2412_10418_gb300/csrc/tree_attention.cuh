@@ -167,7 +167,7 @@ constexpr int kRowsBlock = 128;
 int tc_blocks_per_sm(const Cache& c, int NQ);
 cudaError_t launch_tree_tc(const TreeArgs& a, cudaStream_t s);
 cudaError_t launch_tree_rows(const TreeArgs& a, cudaStream_t s);
-// A 4-bit cache's (tree_attention_i4.cu): slots as M, 8 query vectors per block, or 16 of bf16.
+// A 4-bit cache's (tree_attention_i4.cu): slots as M, 8 query vectors per block, or 4 or 16 of bf16.
 int i4_blocks_per_sm(const Cache& c, int NQ, bool f32);
 cudaError_t launch_tree_i4(const TreeArgs& a, cudaStream_t s);
 

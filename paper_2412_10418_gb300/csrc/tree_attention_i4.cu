@@ -48,14 +48,16 @@ constexpr int kChain = 64;                     // stretches of O^T's chain (512 
 template <int HD, int NQ, bool F32>
 struct Cfg {
   static constexpr int G = HD / kGroup, RB = HD / 2, SB = 2 * G;   // groups; bytes of a row's codes and scales
-  static constexpr int NT = NQ / 8;                                // vectors by eights
-  static constexpr int QP = F32 ? 3 : 1, PP = F32 ? 3 : 2;         // planes of q and p
+  static constexpr int NT = NQ == 16 ? 2 : 1;                      // the MMA's columns by eights
+  // four vectors: each has two columns, of P's two planes, which one MMA then takes for two
+  static constexpr bool TWICE = NQ == 4;
+  static constexpr int QP = F32 ? 3 : 1, PP = F32 ? 3 : TWICE ? 1 : 2;   // planes of q, and of p in a column
   static constexpr uint32_t CODES = kStretch * RB, SCALES = kStretch * SB;
   static constexpr uint32_t V_OFF = CODES + SCALES;
   static constexpr uint32_t F_OFF = 2 * V_OFF;                     // V's scales / 8 by pairs of slots
   static constexpr uint32_t P_OFF = F_OFF + SCALES;
   // scores, then P's fragments: PP planes of two words for each tile and lane
-  static constexpr uint32_t S_BYTES = NQ * kPitch * 4, F_BYTES = NT * kTiles * 32 * PP * 8;
+  static constexpr uint32_t S_BYTES = 8 * NT * kPitch * 4, F_BYTES = NT * kTiles * 32 * PP * 8;
   static constexpr uint32_t MASK_OFF = P_OFF + (S_BYTES > F_BYTES ? S_BYTES : F_BYTES);
   static constexpr uint32_t WARP_BYTES = (MASK_OFF + NQ * (kWords + 1) * 4 + 127) / 128 * 128;
   static constexpr uint32_t PLAN_OFF = kWarps * WARP_BYTES;
@@ -130,6 +132,7 @@ __global__ void __launch_bounds__(32 * kWarps, Cfg<HD, NQ, F32>::WARPS / kWarps)
   using C = Cfg<HD, NQ, F32>;
   using T = std::conditional_t<F32, float, __nv_bfloat16>;
   constexpr int G = C::G, NT = C::NT, QP = C::QP, PP = C::PP;
+  constexpr bool TWICE = C::TWICE;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ __align__(8) uint64_t s_full[kWarps][2];   // K, V
   __shared__ uint32_t s_masks[4];
@@ -229,7 +232,7 @@ __global__ void __launch_bounds__(32 * kWarps, Cfg<HD, NQ, F32>::WARPS / kWarps)
     float fb[NT];                              // factors of the scores of vectors r (+ 8)
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      const int v = 8 * n + r;
+      const int v = TWICE ? r & 3 : 8 * n + r;
       const bool any = v < s.nq;
       const Vec w = vector_of(a, s.h, s.qb, any ? v : 0);
       const T* const q = static_cast<const T*>(a.q) + s.b * a.sq[0] + w.t * a.sq[1] + w.h * a.sq[2] + 8 * q4;
@@ -303,6 +306,7 @@ __global__ void __launch_bounds__(32 * kWarps, Cfg<HD, NQ, F32>::WARPS / kWarps)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           const float by = __shfl_sync(0xffffffffu, f, 4 * (2 * q4 + e));
+          if (TWICE && q4 >= 2) continue;      // (put wrote the planes' sum)
           const float* const from = a.part_o + (part * NQ + 8 * n + 2 * q4 + e) * HD + 4 * r;
 #pragma unroll
           for (int g = 0; g < G; ++g) {
@@ -315,7 +319,17 @@ __global__ void __launch_bounds__(32 * kWarps, Cfg<HD, NQ, F32>::WARPS / kWarps)
         }
       }
     };
+    const auto one_plane = [&] {               // o of a vector's two columns together in the first
+      if constexpr (TWICE)
+#pragma unroll
+        for (int g = 0; g < G; ++g)
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[g][h][0][e] += __shfl_xor_sync(0xffffffffu, o[g][h][0][e], 2);
+    };
     const auto put = [&](int n, int e, float by) {   // o to the part's place
+      if (TWICE && q4 >= 2) return;
       float* const to = a.part_o + (part * NQ + 8 * n + 2 * q4 + e) * HD + 4 * r;
 #pragma unroll
       for (int g = 0; g < G; ++g)
@@ -434,7 +448,7 @@ __global__ void __launch_bounds__(32 * kWarps, Cfg<HD, NQ, F32>::WARPS / kWarps)
       auto softmax = [&](auto general) {
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-          const int v = 8 * n + r;
+          const int v = TWICE ? r & 3 : 8 * n + r;
           uint64_t seen = ~0ull;
           if constexpr (general) {
             const uint32_t* const w = s_mask + v * (kWords + 1);
@@ -490,7 +504,11 @@ __global__ void __launch_bounds__(32 * kWarps, Cfg<HD, NQ, F32>::WARPS / kWarps)
             for (int p = 0; p < PP; ++p)
 #pragma unroll
               for (int h = 0; h < 2; ++h) {
-                const uint32_t two = pack_bf16(y[2 * h], y[2 * h + 1]);
+                uint32_t two = pack_bf16(y[2 * h], y[2 * h + 1]);
+                if constexpr (TWICE) {
+                  const uint32_t rest = pack_bf16(y[2 * h] - __uint_as_float(two << 16), y[2 * h + 1] - __uint_as_float(two & 0xffff0000u));
+                  if (r >= 4) two = rest;
+                }
                 pf[n][i][p][h] = two;
                 if (p + 1 < PP) {
                   y[2 * h] -= __uint_as_float(two << 16);
@@ -543,7 +561,9 @@ __global__ void __launch_bounds__(32 * kWarps, Cfg<HD, NQ, F32>::WARPS / kWarps)
 #pragma unroll
         for (int i = 0; i < kTiles; ++i) {
           uint32_t* const to = s_f + (n * kTiles + i) * (64 * PP);
-          if constexpr (PP == 2) {
+          if constexpr (PP == 1) {
+            *reinterpret_cast<uint2*>(to) = make_uint2(pf[n][i][0][0], pf[n][i][0][1]);
+          } else if constexpr (PP == 2) {
             *reinterpret_cast<uint4*>(to) = make_uint4(pf[n][i][0][0], pf[n][i][0][1], pf[n][i][1][0], pf[n][i][1][1]);
           } else {
 #pragma unroll
@@ -621,6 +641,7 @@ __global__ void __launch_bounds__(32 * kWarps, Cfg<HD, NQ, F32>::WARPS / kWarps)
       loaded = beyond;
       if (!F32 && ++links == kChain && more) {
         if (chained) add_chain();
+        one_plane();
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
           put(n, 0, 1.f);
@@ -634,6 +655,7 @@ __global__ void __launch_bounds__(32 * kWarps, Cfg<HD, NQ, F32>::WARPS / kWarps)
     }
     // ---- the item's (or its part's) sums
     if (chained) add_chain();
+    one_plane();
     const bool whole = s.c0 == 0 && s.c1 == s.units;
     const int live = min(NQ, a.T * a.G - s.qb * NQ);
 #pragma unroll
@@ -689,7 +711,10 @@ auto by_shape(const Cache& c, int NQ, bool f32, F&& f) {   // f(Cfg's parameters
   using std::bool_constant;
   using std::integral_constant;
   auto g = [&](auto hd, auto nq) { return f32 ? f(hd, nq, bool_constant<true>()) : f(hd, nq, bool_constant<false>()); };
-  auto h = [&](auto hd) { return NQ == 8 ? g(hd, integral_constant<int, 8>()) : f(hd, integral_constant<int, 16>(), bool_constant<false>()); };
+  auto h = [&](auto hd) {
+    if (NQ == 8) return g(hd, integral_constant<int, 8>());
+    return NQ == 4 ? f(hd, integral_constant<int, 4>(), bool_constant<false>()) : f(hd, integral_constant<int, 16>(), bool_constant<false>());
+  };
   return c.hd == 128 ? h(integral_constant<int, 128>()) : h(integral_constant<int, 64>());
 }
 
