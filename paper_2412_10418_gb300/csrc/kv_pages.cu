@@ -293,7 +293,7 @@ __global__ void __launch_bounds__(kPlan) k_compact_plan(PagesArgs a) {
 
 // Copies the listed pages' rows in every layer. A warp has a part of at most kPart bytes of one head's codes or of its
 // scales, kAhead loads before their stores. Sources and targets are apart: a target was free, a source was not.
-constexpr int kAhead = 8, kPart = kAhead * 32 * 16;
+constexpr int kAhead = 8, kPart = 2 * kAhead * 32 * 16;
 __global__ void __launch_bounds__(kCopy) k_copy_pages(Cache c, const int* n_moves, const Move* moves) {
   pdl_wait();
   pdl_launch_dependents();
@@ -331,7 +331,7 @@ __global__ void __launch_bounds__(kCopy) k_copy_pages(Cache c, const int* n_move
 cudaError_t launch_copies(const Cache& c, const PagesArgs& a, long long most, cudaStream_t s) {
   const long long parts = ((c.row << c.page_shift) + kPart - 1) / kPart + 1;
   const long long warps = most * c.n_layers * 2 * c.kvh * parts;
-  const int blocks = (int)std::min<long long>((warps + kCopy / 32 - 1) / (kCopy / 32), kPlanSMs * 8);
+  const int blocks = (int)std::min<long long>((warps + kCopy / 32 - 1) / (kCopy / 32), kPlanSMs * 16);
   return launch_pdl(k_copy_pages, dim3(blocks), dim3(kCopy), 0, s, c, (const int*)a.n_moves, (const Move*)a.moves);
 }
 
