@@ -124,8 +124,9 @@ CDSL_API int32_t cdsl_tree_attention_workspace(const cdsl_kv_cache* cache, int32
  * held to 2^-18 of a row's largest value and probabilities to 2^-8 of themselves (2^-10 on average) for
  * up to 32 query vectors per K/V head, to 2^-12 for more; small V rows count beside large ones by their
  * scales, which for that are to be the smallest ones, as cdsl_kv_write makes them. Over a bfloat16 cache
- * probabilities are held to 2^-17. float32 queries run on the CUDA cores in fp32. Over a 4-bit cache everything is in
- * fp32.
+ * probabilities are held to 2^-17. float32 queries run on the CUDA cores in fp32. Over a 4-bit cache both run on the
+ * tensor cores: bfloat16 queries hold probabilities to 2^-16 for up to 16 query vectors per K/V head, to 2^-12 for more,
+ * float32 ones to 2^-23, and queries to 2^-35 of a row's largest value.
  * d_workspace: cdsl_tree_attention_workspace bytes, 256-byte aligned, in any state; it
  * holds nothing between calls. */
 CDSL_API int32_t cdsl_tree_attention(const cdsl_kv_cache* cache, int32_t layer, const void* d_q,

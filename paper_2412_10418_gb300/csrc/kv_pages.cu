@@ -4,8 +4,9 @@
 // and counts from old ones, so that nothing depends on the order of threads: the counts are sums of whole numbers, and
 // free pages are dealt lowest first, in order of sequences and columns. One block plans, as a decoding step's tables
 // are small and all of it hangs on prefix sums over the pages; the rows to be copied are a list for a second kernel,
-// over the whole device, whose blocks are scheduled beside the plan. Bound by the latency of the plan on small calls and by
-// HBM where many layers' pages move.
+// over the whole device, whose blocks are scheduled beside the plan. Bound by the latency of the plan on small calls (a fork of
+// 32 beams 7.7 us, a resize 5, a compaction's plan 5 to 6, by ncu) and by HBM where many layers' pages move: a third of a pool
+// in 8 layers, 700 MB, 113 us, 91 % of the copy bandwidth with the plan apart (118 to 120 as calls; parts of 4 KB a warp 124).
 #include <cuda.h>
 
 #include <algorithm>
@@ -291,8 +292,8 @@ __global__ void __launch_bounds__(kPlan) k_compact_plan(PagesArgs a) {
   }
 }
 
-// Copies the listed pages' rows in every layer. A warp has a part of at most kPart bytes of one head's codes or of its
-// scales, kAhead loads before their stores. Sources and targets are apart: a target was free, a source was not.
+// Copies the listed pages' rows in every layer. A warp has a part of at most kPart bytes of one head's codes or its scales,
+// kAhead loads before their stores. Sources and targets are apart: a target was free, a source was not.
 constexpr int kAhead = 8, kPart = 2 * kAhead * 32 * 16;
 __global__ void __launch_bounds__(kCopy) k_copy_pages(Cache c, const int* n_moves, const Move* moves) {
   pdl_wait();

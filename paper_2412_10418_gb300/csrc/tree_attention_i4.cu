@@ -1,7 +1,8 @@
-// tree_attention_i4.cu -- cdsl_tree_attention over a 4-bit cache, few query vectors per K/V head.
+// tree_attention_i4.cu -- cdsl_tree_attention over a 4-bit cache: float32 queries, and bf16 ones of at most 16 query
+// vectors per K/V head (more: tree_attention_rows.cu).
 //
 // A row of 128 values is 72 bytes, so that what bounds a large pass is less the bytes than the work on each of them:
-// 1.8 us of HBM bring an SM 300,000 codes. Slots are the MMA's M as in tree_attention_tc.cu, but codes go from
+// in the time in which HBM brings an SM two chunks of 64 slots its four schedulers issue 3,000 instructions, for 32,768 codes. Slots are the MMA's M as in tree_attention_tc.cu, but codes go from
 // shared memory to registers, become 16-bit operands there and are multiplied there (mma.sync m16n8k16); through shared memory
 // to tcgen05 they would be written and read once more, in 16 bits four times their size, which alone takes longer than
 // HBM does. A row's groups take turns by four values, so that one 8- or 16-byte load gives a lane the fragments of all
@@ -12,16 +13,28 @@
 //                  adds, -8 times the sum of the group's q, is what the accumulators start from (float32 queries: the
 //                  codes themselves, an fma more, as those sums are larger and so are their roundings). Groups are summed
 //                  apart and multiplied by their scales in fp32. q is held in fp16 planes under a power of two that takes the
-//                  row's largest to 2^14 or more: exact down to 2^-31 of it from bf16 (one plane) or float32 (three).
+//                  row's largest to 2^14 or more: exact down to 2^-27 of it from bf16 (one plane), to 2^-35 of it from float32 (three).
 //   O^T = V^T P^T  V's operand is the value in bf16, exact (a code's 3 bits by a scale's 4): bits 3 .. 6 of
 //                  128 + 8 (code + 8), then one fma of two by (scale / 8, -24 scale). P is the sum of two bf16
 //                  planes (2^-16 of itself; three for float32 queries, 2^-24): fp32's range, whatever lies next to what.
+//                  Up to four vectors have two of the MMA's eight columns each, of P's two planes: one product for both.
 //
 // Scores go through shared memory once, to where a lane has 16 slots of one vector: maxima take two exchanges there, and
 // probabilities are P's fragments as they are. O^T is one chain over kChain stretches of 64 slots and is then added to fp32
 // sums (in the workspace: few passes are as long), as a tensor core's additions truncate; its reference is the running
-// maximum, and few stretches raise it. (float32 queries: every product is added up in fp32.) A warp has a run of its own and no barrier but its own; its K and V come by bulk copies, the next
-// stretch's K while this one's softmax and P V run, and V beside the next scores.
+// maximum, and few stretches raise it. (float32 queries: every product is added up in fp32.) A warp has a run of its own and
+// no barrier but its own; its K and V come by bulk copies, the next stretch's K while this one's softmax and P V run, and V
+// beside the next scores.
+//
+// Measured, 32 heads over 8 of 128: 64 sequences of up to 8192 tokens, one token (453 MB): 111 us, 60 % of the copy
+// bandwidth; 8 sequences of 16,384, 4 / 8 / 16 vectors: 48 / 50 / 70 us; one of 512 tokens 8.6 us in a graph with the joining. Bound by
+// instructions: 2,900 a chunk of 128 slots, 2.2 a cycle and SM, half of the integer pipe's rate (masks, shifts, byte moves) and
+// a third of the tensor cores'. Steps on the way (us, the large case): by the CUDA cores 505; codes turned as above, K's
+// and V's rows by a warp of 64 slots 181; no selects on V's scales 148; scores through shared memory and loops rolled, masks as one
+// instruction, pages 32 at a time 126; V's scales by pairs once, units of 64 slots 121; 12 warps an SM with two to four
+// tiles side by side, in place of 16 with one, 115; blocks of four warps, one to a scheduler, 111 with four vectors twice.
+// Right shifts as high halves of products, on the FMA pipe: 132 for 122. V's rows four slots apart in a lane, so that
+// four lanes' meet half as many banks twice: no difference.
 //
 // Waits are bounded by a number of tries (wait_for): on expiry CDSL_ETIMEOUT is latched and the warp exits once its copies
 // have landed or been given up on as well.
@@ -61,7 +74,8 @@ struct Cfg {
   static constexpr uint32_t MASK_OFF = P_OFF + (S_BYTES > F_BYTES ? S_BYTES : F_BYTES);
   static constexpr uint32_t WARP_BYTES = (MASK_OFF + NQ * (kWords + 1) * 4 + 127) / 128 * 128;
   static constexpr uint32_t PLAN_OFF = kWarps * WARP_BYTES;
-  static constexpr int WARPS = F32 || NQ == 16 ? 8 : 12;           // of an SM, by registers
+  // of an SM, by registers (16 of 128 registers: 117 us for 111; NQ 16 with 12: 93 for 72, float32 34 for 30)
+  static constexpr int WARPS = F32 || NQ == 16 ? 8 : 12;
   static constexpr int K_TILES = NT == 2 ? 2 : 4, V_TILES = NT == 2 ? 1 : 2;   // side by side
   static constexpr size_t smem(int batch) { return PLAN_OFF + plan_bytes(batch); }
 };
@@ -83,16 +97,6 @@ __device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], 
       : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
 }
-__device__ __forceinline__ uint32_t fma_bf16x2(uint32_t a, uint32_t b, uint32_t c) {
-  uint32_t d;
-  asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
-  return d;
-}
-__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
-  uint32_t d;
-  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
-  return d;
-}
 // (a, b) as two bf16, a low.
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
   const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
@@ -101,12 +105,6 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
 __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
   const __half2 h = __floats2half2_rn(a, b);
   return *reinterpret_cast<const uint32_t*>(&h);
-}
-// (x & mask) ^ c in one instruction, of which only one operand may be a constant: masks come from registers.
-__device__ __forceinline__ uint32_t and_xor(uint32_t x, uint32_t mask, uint32_t c) {
-  uint32_t d;
-  asm("lop3.b32 %0, %1, %2, %3, 0x6a;" : "=r"(d) : "r"(x), "r"(mask), "r"(c));
-  return d;
 }
 // The codes in bits BIT .. BIT + 3 of both halves of x (mask: those) as fp16: themselves, or (code + 8) 2^(BIT - 24).
 template <bool EXACT, int BIT>
@@ -119,12 +117,6 @@ __device__ __forceinline__ uint32_t code_f16(uint32_t x, uint32_t mask) {
       : "r"(and_xor(x, mask, 0x64006400u | eights)), "r"(BIT ? 0x2c002c00u : 0x3c003c00u),
         "r"(BIT ? 0xd480d480u : 0xe408e408u));   // times 1 / 16, less 72; less 1032
   return d;
-}
-// Code i of both pieces in x, times their scales: s8 = (scale / 8) and m24 = (-24 scale) of the two.
-template <int I>
-__device__ __forceinline__ uint32_t value_bf16(uint32_t x, uint32_t mask, uint32_t s8, uint32_t m24) {
-  const uint32_t t = I == 0 ? x << 3 : x >> (4 * I - 3);
-  return fma_bf16x2(and_xor(t, mask, 0x43404340u), s8, m24);
 }
 
 template <int HD, int NQ, bool F32>

@@ -1,5 +1,5 @@
 // tree_attention_rows.cu -- cdsl_tree_attention of bf16 queries with more than 32 query vectors per K/V
-// head, on the 5th-generation tensor cores: query vectors are the MMA's M = 128 rows.
+// head (a 4-bit cache: more than 16), on the 5th-generation tensor cores: query vectors are the MMA's M = 128 rows.
 //
 //   S = Q K^T   M = 128 vectors, N = 128 slots, K = head_dim    Q and K tiles K-major in shared memory
 //   O = P V     M = 128 vectors, N = head_dim, K = 128 slots    P in TMEM over S, V tile MN-major as it lands
@@ -41,6 +41,16 @@
 // softmax warps: 177 us. At 36 vectors 8 sequences of 16,384 take 99.5 us, two blocks of 32 on
 // tree_attention_tc.cu 117. At 32, 70 there and 92 here. A block has 128 rows whatever it holds: 8 trees of 32 nodes of four
 // heads each after 4096 tokens take 50.5 us, of 33 nodes, whose 132 vectors take two blocks, 75.
+//
+// A 4-bit cache's rows land packed, and eight warps turn them into tiles with their scales multiplied in: K into bf16, in which
+// a value is exact (4 bits of scale by 3 of code), with Q as it is; V as e4m3's is, into fp16 under a reference, exact from
+// 2^kVRoom above it to 2^-kVBelow4 below, and into bf16 in chunks with smaller scales. A tile's dimensions are in the order in
+// which a row's words give them (one of each of two groups in turn), so that a word is 16 bytes of it and takes no byte moves; Q is
+// staged, and O written, in that order. V's factors come from the scaling warp. Measured: 8 trees of 25 nodes after up to 32,768
+// tokens (243 MB): 161 to 165 us where e4m3 takes 159 on the same boxes; 8 sequences of 16,384 of 20 to 36 vectors 107 to 110
+// (of 16: 107 here, 70 by tree_attention_i4.cu). Without the conversion's work, its barriers left, it takes 125: what that
+// adds is instruction fetches as much as work. Both conversions by four warps 174 to 185; the loops unrolled twice 173, four
+// times 236; each value's factors worked out where it is turned 164.
 //
 // Waits are bounded by a number of tries (wait_for): on expiry CDSL_ETIMEOUT is latched, the role winds down and the block
 // frees its TMEM and exits.
@@ -157,33 +167,14 @@ __device__ __forceinline__ void load_packed(const TreeArgs& a, const int* first,
         wait_for(kv ? &v_full[i % NST] : &k_full[i % NST], parity(i, NST), a.status);
 }
 
-// (x & mask) ^ c in one instruction, of which only one operand may be a constant: masks come from registers.
-__device__ __forceinline__ uint32_t and_xor(uint32_t x, uint32_t mask, uint32_t c) {
-  uint32_t d;
-  asm("lop3.b32 %0, %1, %2, %3, 0x6a;" : "=r"(d) : "r"(x), "r"(mask), "r"(c));
-  return d;
-}
-// Code I of both halves of a word of codes (low half: one group's, high half: the next one's) times their scales: in bf16 as
-// (128 + 8 u) scale / 8 - 24 scale, u = code + 8, and in fp16 as (1024 + 16 u) scale / 16 - 72 scale. Exact.
+// 4-bit code I of both halves of w, times their scales, exactly: (1024 + 16 (code + 8)) scale / 16 - 72 scale in fp16, of mask =
+// 0x00f000f0.
 template <int I>
-__device__ __forceinline__ uint32_t word_bf16(uint32_t w, uint32_t mask, uint32_t s8, uint32_t m24) {   // mask 0x00780078
-  const uint32_t t = I == 0 ? w << 3 : w >> (4 * I - 3);
-  const uint32_t x = and_xor(t, mask, 0x43404340u);
-  uint32_t d;
-  asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(x), "r"(s8), "r"(m24));
-  return d;
-}
-template <int I>
-__device__ __forceinline__ uint32_t word_f16(uint32_t w, uint32_t mask, uint32_t s16, uint32_t m72) {   // mask 0x00f000f0
+__device__ __forceinline__ uint32_t value_f16(uint32_t w, uint32_t mask, uint32_t s16, uint32_t m72) {
   const uint32_t t = I == 0 ? w << 4 : w >> (4 * I - 4);
   const uint32_t x = and_xor(t, mask, 0x64806480u);
   uint32_t d;
   asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(x), "r"(s16), "r"(m72));
-  return d;
-}
-__device__ __forceinline__ uint32_t times_bf16(uint32_t a, uint32_t b) {
-  uint32_t d;
-  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
   return d;
 }
 
@@ -416,11 +407,11 @@ __global__ void __launch_bounds__((Cfg<HD, FORMAT>::THREADS), 1)
           for (int e = 0; e < 4; ++e)
 #pragma unroll
             for (int i = 0; i < G2; ++i) {
-              const uint32_t f = e < n && !(nan >> e & 1) ? times_bf16(from[e * G2 + i], rel) : 0u;
+              const uint32_t f = e < n && !(nan >> e & 1) ? mul_bf16x2(from[e * G2 + i], rel) : 0u;
               uint32_t x, y;
               if (far) {
-                x = times_bf16(f, 0x3e003e00u);                  // 1 / 8
-                y = times_bf16(x, 0xc340c340u);                  // -192
+                x = mul_bf16x2(f, 0x3e003e00u);                  // 1 / 8
+                y = mul_bf16x2(x, 0xc340c340u);                  // -192
               } else {
                 const __half2 h = __floats2half2_rn(bf16_at(f, 0), bf16_at(f, 1));
                 const __half2 a16 = __hmul2(h, __float2half2_rn(0.0625f)), m72 = __hmul2(h, __float2half2_rn(-72.f));
@@ -786,8 +777,8 @@ __global__ void __launch_bounds__((Cfg<HD, FORMAT>::THREADS), 1)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         *reinterpret_cast<uint4*>(tile + to[i]) =
-            make_uint4(word_bf16<0>(w[i], mb, s8[i % G2], m24[i % G2]), word_bf16<1>(w[i], mb, s8[i % G2], m24[i % G2]),
-                       word_bf16<2>(w[i], mb, s8[i % G2], m24[i % G2]), word_bf16<3>(w[i], mb, s8[i % G2], m24[i % G2]));
+            make_uint4(value_bf16<0>(w[i], mb, s8[i % G2], m24[i % G2]), value_bf16<1>(w[i], mb, s8[i % G2], m24[i % G2]),
+                       value_bf16<2>(w[i], mb, s8[i % G2], m24[i % G2]), value_bf16<3>(w[i], mb, s8[i % G2], m24[i % G2]));
     };
     const auto turn_k = [&](int i) {
       const int st = i % NST;
@@ -802,8 +793,8 @@ __global__ void __launch_bounds__((Cfg<HD, FORMAT>::THREADS), 1)
         const uint32_t* const z = reinterpret_cast<const uint32_t*>(from + kKeys * C::RB + (row0 + k * kRowsAt) * C::SB);
 #pragma unroll
         for (int e = 0; e < G2; ++e) {
-          s8[e] = times_bf16(z[e], 0x3e003e00u);                 // 1 / 8
-          m24[e] = times_bf16(s8[e], 0xc340c340u);               // -192
+          s8[e] = mul_bf16x2(z[e], 0x3e003e00u);                 // 1 / 8
+          m24[e] = mul_bf16x2(s8[e], 0xc340c340u);               // -192
         }
         bf16_words(sm + C::KT_OFF + (i & 1) * C::TILE + k * (kRowsAt * 128), w, s8, m24);
       }
@@ -849,8 +840,8 @@ __global__ void __launch_bounds__((Cfg<HD, FORMAT>::THREADS), 1)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
           *reinterpret_cast<uint4*>(at + to[e]) =
-              make_uint4(word_f16<0>(w[e], mh, x[e % G2], y[e % G2]), word_f16<1>(w[e], mh, x[e % G2], y[e % G2]),
-                         word_f16<2>(w[e], mh, x[e % G2], y[e % G2]), word_f16<3>(w[e], mh, x[e % G2], y[e % G2]));
+              make_uint4(value_f16<0>(w[e], mh, x[e % G2], y[e % G2]), value_f16<1>(w[e], mh, x[e % G2], y[e % G2]),
+                         value_f16<2>(w[e], mh, x[e % G2], y[e % G2]), value_f16<3>(w[e], mh, x[e % G2], y[e % G2]));
       }
       tc::fence_proxy_async();
       tc::mbar_arrive(&h_full[i & 1]);

@@ -85,6 +85,30 @@ __device__ __forceinline__ void f8x4_half(uint32_t four, __half2* a, __half2* b)
       : "=r"(*reinterpret_cast<uint32_t*>(a)), "=r"(*reinterpret_cast<uint32_t*>(b))
       : "r"(four));
 }
+// (x & mask) ^ c in one instruction, of which only one operand may be a constant: masks come from registers.
+__device__ __forceinline__ uint32_t and_xor(uint32_t x, uint32_t mask, uint32_t c) {
+  uint32_t d;
+  asm("lop3.b32 %0, %1, %2, %3, 0x6a;" : "=r"(d) : "r"(x), "r"(mask), "r"(c));
+  return d;
+}
+__device__ __forceinline__ uint32_t fma_bf16x2(uint32_t a, uint32_t b, uint32_t c) {
+  uint32_t d;
+  asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
+  return d;
+}
+__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+// 4-bit code I of both halves of x, times their scales, exactly: (128 + 8 (code + 8)) scale / 8 - 24 scale in bf16, of
+// mask = 0x00780078, s8 = (scale / 8) and m24 = (-24 scale) of the two.
+template <int I>
+__device__ __forceinline__ uint32_t value_bf16(uint32_t x, uint32_t mask, uint32_t s8, uint32_t m24) {
+  const uint32_t t = I == 0 ? x << 3 : x >> (4 * I - 3);
+  return fma_bf16x2(and_xor(t, mask, 0x43404340u), s8, m24);
+}
+
 // Queries of a segment's block to shared memory, by NT threads, eight a vector: K-major tiles of NQ rows in
 // blocks of at most 128 bytes. F8: two e4m3 planes of q / 2^e, hi = e4m3(q / 2^e) and lo the rest, e the
 // smallest with which the row's largest value is at most 448; else bf16 as they are. A row that is not finite, and
