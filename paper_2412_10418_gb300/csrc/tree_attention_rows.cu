@@ -43,8 +43,8 @@
 // heads each after 4096 tokens take 50.5 us, of 33 nodes, whose 132 vectors take two blocks, 75.
 //
 // A 4-bit cache's rows land packed, and eight warps turn them into tiles with their scales multiplied in: K into bf16, in which
-// a value is exact (4 bits of scale by 3 of code), with Q as it is; V as e4m3's is, into fp16 under a reference, exact from
-// 2^kVRoom above it to 2^-kVBelow4 below, and into bf16 in chunks with smaller scales. A tile's dimensions are in the order in
+// a value is exact (4 bits of scale by 3 of code), with Q as it is; V as e4m3's is, into fp16 under a reference from
+// 2^kVRoom4 above it to 2^-kVBelow4 below, and into bf16 in chunks with smaller scales. A tile's dimensions are in the order in
 // which a row's words give them (one of each of two groups in turn), so that a word is 16 bytes of it and takes no byte moves; Q is
 // staged, and O written, in that order. V's factors come from the scaling warp. Measured: 8 trees of 25 nodes after up to 32,768
 // tokens (243 MB): 161 to 165 us where e4m3 takes 159 on the same boxes; 8 sequences of 16,384 of 20 to 36 vectors 107 to 110
@@ -76,7 +76,9 @@ constexpr float kUp = 7.f;                     // stored times 2^kUp: below fp16
 constexpr int kBuf = 3;                        // S (then P) buffers in TMEM; O has the rest
 constexpr int kVRoom = 6;                      // octaves that V's scales may pass their reference by: 448 * 2^6 in fp16,
 constexpr int kVBelow = 15;                    // and lie below it: 2^-9 * 2^-15
-constexpr int kVBelow4 = 17;                   // 4 bits: a scale / 16 has its last bit at 2^-24 then
+// 4 bits: scales / 16 would have their last bit at 2^-24 from 17 below on, but a probability of less than 2^-32 is nothing in
+// fp16: with scales 16 octaves apart at most, it leaves out 2^-16 of what the row has.
+constexpr int kVRoom4 = 4, kVBelow4 = 12;
 
 template <int HD, int FORMAT>
 struct Cfg {
@@ -368,7 +370,7 @@ __global__ void __launch_bounds__((Cfg<HD, FORMAT>::THREADS), 1)
             if (e < n && most[e] != 255) vmax = max(vmax, most[e]);
           }
           vmax = __reduce_max_sync(0xffffffffu, vmax);
-          if (vref == 0 || vmax > vref + kVRoom) vref = vmax;
+          if (vref == 0 || vmax > vref + kVRoom4) vref = vmax;
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             nan |= (uint32_t)(e < n && most[e] == 255) << e;
