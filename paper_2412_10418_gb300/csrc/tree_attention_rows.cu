@@ -180,6 +180,45 @@ __device__ __forceinline__ uint32_t value_f16(uint32_t w, uint32_t mask, uint32_
   return d;
 }
 
+// MMAs of a warp that is at one place, of which an elected lane issues them: the operands, which the compiler knows to be the
+// warp's (shuffled from one lane), stay in uniform registers. Issued by a lane on a branch of its own each took 80 cycles, 120
+// beside the other roles, where a tensor core takes 64.
+template <bool F8>
+__device__ __forceinline__ void warp_umma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t add) {
+  if constexpr (F8)
+    asm volatile(
+        "{\n\t.reg .pred p, e;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "elect.sync _|e, 0xffffffff;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(add)
+        : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .pred p, e;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "elect.sync _|e, 0xffffffff;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(add)
+        : "memory");
+}
+__device__ __forceinline__ void warp_umma_tmem_a(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t add) {
+  asm volatile(
+      "{\n\t.reg .pred p, e;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "elect.sync _|e, 0xffffffff;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+      "r"(a), "l"(b), "r"(idesc), "r"(add)
+      : "memory");
+}
+__device__ __forceinline__ void warp_commit(uint64_t* mbar) {
+  asm volatile(
+      "{\n\t.reg .pred e;\n\t"
+      "elect.sync _|e, 0xffffffff;\n\t"
+      "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(tc::smem_u32(mbar))
+      : "memory");
+}
+
 template <int HD, int FORMAT>
 __global__ void __launch_bounds__((Cfg<HD, FORMAT>::THREADS), 1)
     k_tree_rows(TreeArgs a, const __grid_constant__ CUtensorMap map) {
@@ -204,7 +243,7 @@ __global__ void __launch_bounds__((Cfg<HD, FORMAT>::THREADS), 1)
   __shared__ uint32_t s_mask[2][kRows + 1][kWords];
   __shared__ uint32_t s_pieces[NST], s_masks[2];
   const Cache& c = a.c;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;   // (the warp's, to the compiler)
 
   if (threadIdx.x == 0) {
     s_masks[0] = 0x00780078u;
@@ -255,83 +294,84 @@ __global__ void __launch_bounds__((Cfg<HD, FORMAT>::THREADS), 1)
       load_chunks<HD, F8, NST, !F8>(a, s_first, begin, end, map, sm + C::KV_OFF, sm + C::SCALE_OFF, s_pieces, k_full,
                                     v_full, k_empty, v_empty);
   } else if (warp == kIssuer) {
-    if (lane == 0) {
-      constexpr uint32_t formats = F8 ? 0u : (1u << 7) | (1u << 10);
-      constexpr uint32_t idesc = (1u << 4) | formats | (128u >> 4) << 24;
-      constexpr uint32_t idesc_s = idesc | (uint32_t)(kKeys >> 3) << 17;
-      // P V in 16 bits: fp16 (format 0) or bf16
-      constexpr uint32_t idesc_half = (1u << 4) | (128u >> 4) << 24 | (uint32_t)(HD >> 3) << 17 | 1u << 16;
-      constexpr uint32_t idesc_bf16 = idesc_half | (1u << 7) | (1u << 10);
-      const uint32_t sbase = tc::smem_u32(sm);
-      const uint64_t desc_q = tc::desc_rows(sbase, C::BW, 16);
-      const uint64_t desc_k = tc::desc_rows(sbase + (I4 ? C::KT_OFF : C::KV_OFF), C::BW, 16);
-      const uint64_t desc_v = TURNED ? tc::desc_rows(sbase + C::H_OFF, 128, C::H_BLOCK)
-                                 : tc::desc_rows(sbase + C::KV_OFF + C::TILE, C::BW, C::BLOCK);
-      auto s_mma = [&](int i) {                // S of chunk i
-        if (!(I4 ? wait_for(&kt_full[i & 1], parity(i, 2), a.status) : wait_for(&k_full[i % NST], parity(i, NST), a.status)))
-          return false;
-        tc::tc_fence_after();
-        const uint64_t k = desc_k + (I4 ? (uint32_t)(i & 1) * (C::TILE / 16) : (uint32_t)(i % NST) * (2 * C::TILE / 16));
+    // (the whole warp is here: see warp_umma)
+    const auto uniform = [](uint32_t x) { return __shfl_sync(0xffffffffu, x, 0); };
+    const uint32_t tmem = uniform(s_tmem), t_o = tmem + kBuf * kKeys;
+    constexpr uint32_t formats = F8 ? 0u : (1u << 7) | (1u << 10);
+    constexpr uint32_t idesc = (1u << 4) | formats | (128u >> 4) << 24;
+    constexpr uint32_t idesc_s = idesc | (uint32_t)(kKeys >> 3) << 17;
+    // P V in 16 bits: fp16 (format 0) or bf16
+    constexpr uint32_t idesc_half = (1u << 4) | (128u >> 4) << 24 | (uint32_t)(HD >> 3) << 17 | 1u << 16;
+    constexpr uint32_t idesc_bf16 = idesc_half | (1u << 7) | (1u << 10);
+    const uint32_t sbase = uniform(tc::smem_u32(sm));
+    const uint64_t desc_q = tc::desc_rows(sbase, C::BW, 16);
+    const uint64_t desc_k = tc::desc_rows(sbase + (I4 ? C::KT_OFF : C::KV_OFF), C::BW, 16);
+    const uint64_t desc_v = TURNED ? tc::desc_rows(sbase + C::H_OFF, 128, C::H_BLOCK)
+                               : tc::desc_rows(sbase + C::KV_OFF + C::TILE, C::BW, C::BLOCK);
+    auto s_mma = [&](int i) {                // S of chunk i
+      if (!__all_sync(0xffffffffu, I4 ? wait_for(&kt_full[i & 1], parity(i, 2), a.status)
+                                      : wait_for(&k_full[i % NST], parity(i, NST), a.status)))
+        return false;
+      tc::tc_fence_after();
+      const uint64_t k = desc_k + (I4 ? (uint32_t)(i & 1) * (C::TILE / 16) : (uint32_t)(i % NST) * (2 * C::TILE / 16));
 #pragma unroll 1
-        for (int p = C::QP - 1; p >= 0; --p)
+      for (int p = C::QP - 1; p >= 0; --p)
 #pragma unroll 1
-          for (int nb = 0; nb < C::NB; ++nb)
+        for (int nb = 0; nb < C::NB; ++nb)
 #pragma unroll
-            for (int x = 0; x < C::BW / 32; ++x) {
-              const uint64_t q = desc_q + ((uint32_t)(p * C::Q_PLANE + nb * kRows * C::BW) / 16 + 2 * x);
-              const uint64_t kk = k + (nb * C::BLOCK / 16 + 2 * x);
-              const bool add = p < C::QP - 1 || nb + x > 0;
-              if constexpr (F8) tc::umma_f8(tmem + i % kBuf * kKeys, q, kk, idesc_s, add);
-              else tc::umma_bf16(tmem + i % kBuf * kKeys, q, kk, idesc_s, add);
-            }
-        tc::umma_commit(&s_full[i % kBuf]);
-        tc::umma_commit(I4 ? &kt_empty[i & 1] : &k_empty[i % NST]);
-        return true;
-      };
-      auto pv = [&](int i, bool add) {         // P V of chunk i
-        if (!(TURNED ? wait_for(&h_full[i & 1], parity(i, 2), a.status)
-                 : wait_for(&v_full[i % NST], parity(i, NST), a.status)))
-          return false;
-        const bool planes = !TURNED || s_h_far[i & 1];
-        if (!wait_for(&p_full[i % kBuf], parity(i, kBuf), a.status)) return false;
-        tc::tc_fence_after();
-        const uint64_t v = desc_v + (TURNED ? (uint32_t)(i & 1) * (C::H_TILE / 16) : (uint32_t)(i % NST) * (2 * C::TILE / 16));
-        // 16 slots an MMA: 8 columns of P, 16 rows of 128 bytes of V. P of 32 slots lies in the columns that held
-        // their S, bf16 hi then lo.
-        const auto plane = [&](int p, uint32_t idesc, bool add) {
+          for (int x = 0; x < C::BW / 32; ++x) {
+            const uint64_t q = desc_q + ((uint32_t)(p * C::Q_PLANE + nb * kRows * C::BW) / 16 + 2 * x);
+            const uint64_t kk = k + (nb * C::BLOCK / 16 + 2 * x);
+            const bool add = p < C::QP - 1 || nb + x > 0;
+            warp_umma<F8>(tmem + i % kBuf * kKeys, q, kk, idesc_s, add);
+          }
+      warp_commit(&s_full[i % kBuf]);
+      warp_commit(I4 ? &kt_empty[i & 1] : &k_empty[i % NST]);
+      return true;
+    };
+    auto pv = [&](int i, bool add) {         // P V of chunk i
+      if (!__all_sync(0xffffffffu, TURNED ? wait_for(&h_full[i & 1], parity(i, 2), a.status)
+                                          : wait_for(&v_full[i % NST], parity(i, NST), a.status)))
+        return false;
+      const bool planes = !TURNED || uniform(s_h_far[i & 1]);
+      if (!__all_sync(0xffffffffu, wait_for(&p_full[i % kBuf], parity(i, kBuf), a.status))) return false;
+      tc::tc_fence_after();
+      const uint64_t v = desc_v + (TURNED ? (uint32_t)(i & 1) * (C::H_TILE / 16) : (uint32_t)(i % NST) * (2 * C::TILE / 16));
+      // 16 slots an MMA: 8 columns of P, 16 rows of 128 bytes of V. P of 32 slots lies in the columns that held
+      // their S, bf16 hi then lo.
+      const auto plane = [&](int p, uint32_t idesc, bool add) {
 #pragma unroll
-          for (int k = 0; k < kKeys / 16; ++k)
-            tc::umma_tmem_a(t_o, tmem + i % kBuf * kKeys + k / 2 * 32 + p * 16 + k % 2 * 8, v + k * (16 * 128 / 16), idesc,
-                            add || k > 0);
-        };
-        if (!planes) {
-          plane(0, idesc_half, add);
-        } else {
-#pragma unroll 1
-          for (int p = 1; p >= 0; --p) plane(p, idesc_bf16, add || p < 1);
-        }
-        tc::umma_commit(&pv_done[i & 1]);
-        if (!TURNED) tc::umma_commit(&v_empty[i % NST]);
-        return true;
+        for (int k = 0; k < kKeys / 16; ++k)
+          warp_umma_tmem_a(t_o, tmem + i % kBuf * kKeys + k / 2 * 32 + p * 16 + k % 2 * 8, v + k * (16 * 128 / 16), idesc,
+                          add || k > 0);
       };
-      bool ok = true;
-      int it = 0, seg = 0;                     // chunks of the segments before
-      for (int unit = begin; unit < end && ok; ++seg) {
-        const Segment s = segment_at(a, s_first, unit, end);
-        const int n = s.c1 - s.c0;
-        ok = wait_for(&q_full, seg & 1, a.status);
-        // S as far ahead as it has buffers; it overwrites a P after the P V that reads it, in order
-        for (int i = 0; i < n + kBuf && ok; ++i) {
-          if (i >= kBuf) ok = pv(it + i - kBuf, i > kBuf);
-          if (ok && i < n) ok = s_mma(it + i);
-        }
-        it += n;
-        unit += n;
+      if (!planes) {
+        plane(0, idesc_half, add);
+      } else {
+#pragma unroll 1
+        for (int p = 1; p >= 0; --p) plane(p, idesc_bf16, add || p < 1);
       }
-      tc::umma_commit(&done);                  // what was issued completes before the block's memory goes
-      wait_for(&done, 0, a.status);
+      warp_commit(&pv_done[i & 1]);
+      if (!TURNED) warp_commit(&v_empty[i % NST]);
+      return true;
+    };
+    bool ok = true;
+    int it = 0, seg = 0;                     // chunks of the segments before
+    const int last = (int)uniform(end);
+    for (int unit = (int)uniform(begin); unit < last && ok; ++seg) {
+      const Segment s = segment_at(a, s_first, unit, last);
+      const int n = (int)uniform(s.c1 - s.c0);
+      ok = __all_sync(0xffffffffu, wait_for(&q_full, seg & 1, a.status));
+      // S as far ahead as it has buffers; it overwrites a P after the P V that reads it, in order
+      for (int i = 0; i < n + kBuf && ok; ++i) {
+        if (i >= kBuf) ok = pv(it + i - kBuf, i > kBuf);
+        if (ok && i < n) ok = s_mma(it + i);
+      }
+      it += n;
+      unit += n;
     }
-    __syncwarp();
+    warp_commit(&done);                  // what was issued completes before the block's memory goes
+    wait_for(&done, 0, a.status);
   } else if (warp == kScaler) {
     // ------------------------------------------------------------------------- scale bytes to factors
     int it = 0;
