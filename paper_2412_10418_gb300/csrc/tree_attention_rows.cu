@@ -76,9 +76,9 @@ constexpr float kUp = 7.f;                     // stored times 2^kUp: below fp16
 constexpr int kBuf = 3;                        // S (then P) buffers in TMEM; O has the rest
 constexpr int kVRoom = 6;                      // octaves that V's scales may pass their reference by: 448 * 2^6 in fp16,
 constexpr int kVBelow = 15;                    // and lie below it: 2^-9 * 2^-15
-// 4 bits: scales / 16 would have their last bit at 2^-24 from 17 below on, but a probability of less than 2^-32 is nothing in
-// fp16: with scales 16 octaves apart at most, it leaves out 2^-16 of what the row has.
-constexpr int kVRoom4 = 4, kVBelow4 = 12;
+// 4 bits: a probability of less than 2^-32 is nothing in fp16: with scales 16 octaves apart at most, it leaves out 2^-16 of what
+// the row has. V is held 2^kVUp4 larger: a factor that is 2^-4 of a scale is a normal fp16 number down to 14 below.
+constexpr int kVRoom4 = 4, kVBelow4 = 12, kVUp4 = 4;
 
 template <int HD, int FORMAT>
 struct Cfg {
@@ -384,6 +384,80 @@ __global__ void __launch_bounds__((Cfg<HD, FORMAT>::THREADS), 1)
         ok = __all_sync(0xffffffffu, wait_for(TURNED ? &v_full[st] : &k_full[st], parity(it, NST), a.status) &&
                                          wait_for(&f_empty[st], parity(it, NST) ^ 1, a.status));
         if (!ok) break;
+        if constexpr (I4) {
+          // a lane has slots lane, lane + 32 ..: their scales, two groups a word, of whose exponents (bits 7 .. 14; all set: not
+          // finite, to which 0x80 carries into bit 15) it takes the largest and the smallest (a negative scale's: below 0)
+          constexpr int G2 = HD / kGroup / 2;
+          const uint32_t* const from = reinterpret_cast<const uint32_t*>(sm + C::KV_OFF + (st * 2 + 1) * C::PACKED + kKeys * C::RB);
+          const uint32_t pieces = s_pieces[st];
+          const int before = vref;
+          uint32_t z[4][G2], most = 0u, least = 0x7fff7fffu;
+          bool there[4], nan[4], masks = false;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int row = 32 * e + lane, slot = ch * kKeys + row;
+#pragma unroll
+            for (int i = 0; i < G2; ++i) z[e][i] = from[row * G2 + i];
+            const uint32_t x = z[e][0] & 0x7f807f80u, y = z[e][G2 - 1] & 0x7f807f80u;
+            there[e] = slot < s.keys && pieces >> (row >> min(c.page_shift, 7)) & 1;
+            nan[e] = there[e] && (((x + 0x00800080u) | (y + 0x00800080u)) & 0x80008000u) != 0;
+            masks = masks || !there[e] || slot >= s.len || nan[e];
+            if (there[e] && !nan[e]) {
+              most = __vmaxu2(most, __vmaxu2(x, y));
+              least = __vmins2(least, __vmins2(z[e][0], z[e][G2 - 1]));
+            }
+          }
+          const int vmax = __reduce_max_sync(0xffffffffu, max(most >> 23, most >> 7 & 0xff));
+          const int vmin = __reduce_min_sync(0xffffffffu, min((int)least >> 23, (int)(least << 16) >> 23));
+          masks = __any_sync(0xffffffffu, masks);
+          if (vref == 0 || vmax > vref + kVRoom4) vref = vmax;
+          const bool far = vmin < max(vref - kVBelow4, 1);
+          uint32_t* const to = reinterpret_cast<uint32_t*>(sm + C::FACTOR_OFF + st * C::FACTORS) + lane * (2 * G2);
+          const auto put = [&](auto factors) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              uint32_t y[2 * G2];
+#pragma unroll
+              for (int i = 0; i < G2; ++i) factors(z[e][i], there[e] && !nan[e], &y[2 * i]);
+              if constexpr (G2 == 2) *reinterpret_cast<uint4*>(to + e * (64 * G2)) = make_uint4(y[0], y[1], y[2], y[3]);
+              else *reinterpret_cast<uint2*>(to + e * (64 * G2)) = make_uint2(y[0], y[1]);
+            }
+          };
+          if (far) {
+            const uint32_t rel = (uint32_t)min(max(254 + kVUp4 - vref, 1), 254) * 0x00800080u;   // 2^(kVUp4 - reference)
+            put([&](uint32_t x, bool some, uint32_t* y) {
+              y[0] = some ? mul_bf16x2(mul_bf16x2(x, rel), 0x3e003e00u) : 0u;   // 1 / 8
+              y[1] = mul_bf16x2(y[0], 0xc340c340u);                             // -192
+            });
+          } else {
+            // bf16 to fp16, 2^-4 of it: the exponents moved (3 at least is left of one, so that no half borrows of the other), then
+            // all bits by three
+            const uint32_t move = (uint32_t)(vref - 15) * (128u * 0x00010001u);
+            put([&](uint32_t x, bool some, uint32_t* y) {
+              y[0] = some ? (x - move) * 8u : 0u;
+              const __half2 h = __hmul2(*reinterpret_cast<const __half2*>(&y[0]), __float2half2_rn(-1152.f));
+              y[1] = *reinterpret_cast<const uint32_t*>(&h);
+            });
+          }
+          if (masks || far)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const uint32_t v = __ballot_sync(0xffffffffu, there[e]), w = __ballot_sync(0xffffffffu, nan[e]);
+              if (lane == e) {
+                s_valid[st][e] = v;
+                s_nan[st][e] = w;
+              }
+            }
+          if (lane == 0) {
+            s_vref[st] = vref;
+            s_vstep[st] = before ? before - vref : 0;
+            s_kind[st] = masks | far << 1;
+          }
+          __syncwarp();
+          if (lane == 0) tc::mbar_arrive(&v_empty[st]);   // (the scales are read)
+          tc::mbar_arrive(&f_full[st]);
+          continue;
+        }
         // a lane has slots 4 lane .. 4 lane + 3
         const int slot = ch * kKeys + 4 * lane;
         const bool piece = s_pieces[st] >> (4 * lane >> min(c.page_shift, 7)) & 1;
@@ -392,32 +466,6 @@ __global__ void __launch_bounds__((Cfg<HD, FORMAT>::THREADS), 1)
         float kf[4], vf[4];
         uint32_t nan = 0;
         bool far = false, masks = n < 4 || slot + 3 >= s.len;   // slots past the item's, without a page or of the tree
-        if constexpr (I4) {
-          // exponents of a row's scales, the largest and the smallest (the converting warps take the scales themselves)
-          constexpr int G2 = HD / kGroup / 2;
-          const uint32_t* const from = reinterpret_cast<const uint32_t*>(sm + C::KV_OFF + (st * 2 + 1) * C::PACKED + kKeys * C::RB) + 4 * lane * G2;
-          int most[4], least[4], vmax = 0;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            most[e] = 0;
-            least[e] = 255;
-#pragma unroll
-            for (int i = 0; i < G2; ++i) {
-              const int lo = from[e * G2 + i] >> 7 & 255, hi = from[e * G2 + i] >> 23 & 255;
-              most[e] = max(most[e], max(lo, hi));
-              least[e] = min(least[e], min(lo, hi));
-            }
-            if (e < n && most[e] != 255) vmax = max(vmax, most[e]);
-          }
-          vmax = __reduce_max_sync(0xffffffffu, vmax);
-          if (vref == 0 || vmax > vref + kVRoom4) vref = vmax;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            nan |= (uint32_t)(e < n && most[e] == 255) << e;
-            masks = masks || (e < n && most[e] == 255);
-            far = far || (e < n && most[e] != 255 && least[e] < vref - kVBelow4);
-          }
-        } else {
         const uint8_t* from = sm + C::SCALE_OFF + st * 2 * kKeys + 4 * lane;
         const uint32_t kb = *reinterpret_cast<const uint32_t*>(from), vb = *reinterpret_cast<const uint32_t*>(from + kKeys);
         int vmax = 0;
@@ -438,31 +486,7 @@ __global__ void __launch_bounds__((Cfg<HD, FORMAT>::THREADS), 1)
           masks = masks || (e < n && v == 255);
           far = far || (e < n && v != 255 && (F8 ? v > 0 && x < 127 - kVBelow : v != 127));
         }
-        }
         far = __any_sync(0xffffffffu, far);
-        if constexpr (I4) {
-          constexpr int G2 = HD / kGroup / 2;
-          const uint32_t* const from = reinterpret_cast<const uint32_t*>(sm + C::KV_OFF + (st * 2 + 1) * C::PACKED + kKeys * C::RB) + 4 * lane * G2;
-          uint32_t* const to = reinterpret_cast<uint32_t*>(sm + C::FACTOR_OFF + st * C::FACTORS) + 8 * lane * G2;
-          const uint32_t rel = (uint32_t)max(254 - vref, 1) * 0x00800080u;   // 2^-reference
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-#pragma unroll
-            for (int i = 0; i < G2; ++i) {
-              const uint32_t f = e < n && !(nan >> e & 1) ? mul_bf16x2(from[e * G2 + i], rel) : 0u;
-              uint32_t x, y;
-              if (far) {
-                x = mul_bf16x2(f, 0x3e003e00u);                  // 1 / 8
-                y = mul_bf16x2(x, 0xc340c340u);                  // -192
-              } else {
-                const __half2 h = __floats2half2_rn(bf16_at(f, 0), bf16_at(f, 1));
-                const __half2 a16 = __hmul2(h, __float2half2_rn(0.0625f)), m72 = __hmul2(h, __float2half2_rn(-72.f));
-                x = *reinterpret_cast<const uint32_t*>(&a16);
-                y = *reinterpret_cast<const uint32_t*>(&m72);
-              }
-              *reinterpret_cast<uint2*>(to + 2 * (e * G2 + i)) = make_uint2(x, y);
-            }
-        }
         masks = __any_sync(0xffffffffu, masks);
         if constexpr (!I4) {
           float* to = reinterpret_cast<float*>(sm + C::FACTOR_OFF) + st * 2 * kKeys + 4 * lane;
@@ -717,7 +741,7 @@ __global__ void __launch_bounds__((Cfg<HD, FORMAT>::THREADS), 1)
         m = l == 0.f ? -INFINITY : m - kUp;
         const bool whole = now.c0 == 0 && now.c1 == now.units;
         const float inv = l == 0.f ? 0.f : whole ? 1.f / l : 1.f;
-        const float unscale = TURNED ? ex2((float)(s_v - 127)) : 1.f;
+        const float unscale = TURNED ? ex2((float)(s_v - 127 - (I4 ? kVUp4 : 0))) : 1.f;
         const Vec x = vector_of(a, now.h, now.qb, r);
         const size_t part = (size_t)blockIdx.x * 2 + (now.c0 == 0);
         if (grp == 0 && r < rows) {
