@@ -33,8 +33,9 @@
 // the last P V (33 trees of 48 after 115 tokens: 7 % less).
 //
 // Measured: 8 trees of 25 nodes, 100 vectors a K/V head, up to 32,768 tokens of 8 heads of 128 in e4m3: 146 to 155 us,
-// 385 to 415 TFLOP/s, 40 % of the copy bandwidth (16,384 tokens each 111 us; with V's scales far apart in every chunk 174). A chunk takes 3,000 cycles, of which its MMAs need 1,024; a softmax
-// thread spends 1,500 on the maxima, 2,000 on the probabilities and the rest waiting. What holds it is latency (166
+// 385 to 415 TFLOP/s, 40 % of the copy bandwidth (16,384 tokens each 111 us; with V's scales far apart in every chunk 174; calls
+// one after another 159, and 152 since MMAs are issued by an elected lane, see warp_umma). A chunk takes 3,000 cycles, of which its
+// MMAs need 1,024; a softmax thread spends 1,500 on the maxima, 2,000 on the probabilities and the rest waiting. What holds it is latency (166
 // cycles a TMEM load), shared memory, which operands, conversion and factors keep busy for 1,900, and instruction
 // fetches: the roles together are about as large as the instruction cache, and the same kernel took 150 to 190 us
 // with the sizes of its loops (0.4 to 1.6 million misses a call), which are kept rolled for that. A third group of
@@ -47,10 +48,11 @@
 // 2^kVRoom4 above it to 2^-kVBelow4 below, and into bf16 in chunks with smaller scales. A tile's dimensions are in the order in
 // which a row's words give them (one of each of two groups in turn), so that a word is 16 bytes of it and takes no byte moves; Q is
 // staged, and O written, in that order. V's factors come from the scaling warp. Measured: 8 trees of 25 nodes after up to 32,768
-// tokens (243 MB): 161 to 165 us where e4m3 takes 159 on the same boxes; 8 sequences of 16,384 of 20 to 36 vectors 107 to 110
-// (of 16: 107 here, 70 by tree_attention_i4.cu). Without the conversion's work, its barriers left, it takes 125: what that
-// adds is instruction fetches as much as work. Both conversions by four warps 174 to 185; the loops unrolled twice 173, four
-// times 236; each value's factors worked out where it is turned 164.
+// tokens (243 MB): 155 us among other calls, 163 one after another, where e4m3 takes 152; 8 sequences of 16,384 of 20 / 36 / 100
+// vectors 98 / 102 / 116 (of 16: 70 by tree_attention_i4.cu). Of the 98, conversions are some 20, softmax 15, an empty
+// pipeline 60 (20 of them whatever the length). Steps and trials, the trees among other calls: both conversions by four warps 174,
+// loops unrolled twice 184, four times 236; eight warps 164; factors by the scaling warp 161; and one after another, from 174
+// there: MMAs by an elected lane 172, factors by integer moves 167, stages loaded as they become free 163.
 //
 // Waits are bounded by a number of tries (wait_for): on expiry CDSL_ETIMEOUT is latched, the role winds down and the block
 // frees its TMEM and exits.
