@@ -141,7 +141,8 @@ CDSL_API int32_t cdsl_tree_attention(const cdsl_kv_cache* cache, int32_t layer, 
  * old ones, on the device and in order of nothing but their indexes: free pages are dealt lowest first. Table entries
  * of -1 hold nothing; others outside [0, n_pages) latch CDSL_ERANGE and count as -1. Holders beyond the table (a prefix
  * that is kept, another table of the pool) are counts that the caller has added. Counts that are below the table's own
- * entries latch CDSL_EINVAL. d_workspace: cdsl_kv_pages_workspace bytes, 256-byte aligned, in any state; it holds nothing between
+ * entries (or below 0) latch CDSL_EINVAL: such a page counts as held by the entries alone, so that none that an entry keeps is
+ * dealt out (cdsl_kv_compact, which deals none out, goes by the counts: entries of a page with 0 become -1). d_workspace: cdsl_kv_pages_workspace bytes, 256-byte aligned, in any state; it holds nothing between
  * calls. new_batch there: of the new table, the largest of those that are to use it. */
 CDSL_API int32_t cdsl_kv_pages_workspace(const cdsl_kv_cache* cache, int32_t new_batch, size_t* bytes);
 

@@ -41,6 +41,7 @@ struct PagesArgs {
   int* n_moves;
   Move* moves;
   int32_t* free_pages;
+  int32_t* entries;                            // compact: of each page, in the free pages' place
 };
 
 // Sum of x over the block's threads before this one, and over all.
@@ -100,9 +101,37 @@ __device__ int find_free(const int32_t* refs, int n_pages, int want, int32_t* to
 
 __device__ __forceinline__ bool is_page(const Cache& c, int page) { return (unsigned)page < (unsigned)c.n_pages; }
 
-// A holder gives page p up (a count below 0: the counts were not the table's).
-__device__ __forceinline__ void give_up(const PagesArgs& a, int p) {
-  if (atomicSub(a.new_refs + p, 1) < 1) set_status(a.status, CDSL_EINVAL);
+// The counts without the table's entries, to new_refs (the holders beyond it), and whether one of them is below 0, to the whole
+// block: then the counts are not the table's, which settle() latches, and has them count from 0. Every entry is taken off
+// before any is kept, so that nothing depends on which thread comes first.
+__device__ bool take_off(const PagesArgs& a) {
+  constexpr int AHEAD = 4;                     // entries whose counts are waited for together
+  const Cache& c = a.c;
+  const int tid = threadIdx.x;
+  bool low = false;
+  for (int p = tid; p < c.n_pages; p += kPlan) {
+    const int r = a.refs[p];
+    low = low || r < 0;
+    if (a.new_refs != a.refs) a.new_refs[p] = r;
+  }
+  __syncthreads();
+  const long long n = (long long)c.batch * c.max_pages;
+  for (long long i0 = tid; i0 < n; i0 += AHEAD * kPlan) {
+    int page[AHEAD], had[AHEAD];
+#pragma unroll
+    for (int e = 0; e < AHEAD; ++e) page[e] = i0 + e * kPlan < n ? c.table[i0 + e * kPlan] : -1;
+#pragma unroll
+    for (int e = 0; e < AHEAD; ++e) had[e] = is_page(c, page[e]) ? atomicSub(a.new_refs + page[e], 1) : 1;
+#pragma unroll
+    for (int e = 0; e < AHEAD; ++e) low = low || had[e] < 1;
+  }
+  return __syncthreads_or(low);
+}
+__device__ void settle(const PagesArgs& a) {
+  if (threadIdx.x == 0) set_status(a.status, CDSL_EINVAL);
+  for (int p = threadIdx.x; p < a.c.n_pages; p += kPlan)
+    if (__ldcg(a.new_refs + p) < 0) a.new_refs[p] = 0;
+  __syncthreads();
 }
 
 __global__ void __launch_bounds__(kPlan) k_fork_plan(PagesArgs a) {
@@ -112,12 +141,8 @@ __global__ void __launch_bounds__(kPlan) k_fork_plan(PagesArgs a) {
   const int tid = threadIdx.x, P = 1 << c.page_shift;
   pdl_wait();
   pdl_launch_dependents();
-  for (int p = tid; p < c.n_pages; p += kPlan) a.new_refs[p] = a.refs[p];
   for (int b = tid; b < c.batch; b += kPlan) s_first[b] = INT_MAX;
   __syncthreads();
-  // every old sequence gives its pages up
-  for (int i = tid; i < c.batch * c.max_pages; i += kPlan)
-    if (is_page(c, c.table[i])) give_up(a, c.table[i]);
   // a new sequence per thread
   int parent = -1, len = 0;
   if (tid < a.new_batch) {
@@ -135,20 +160,20 @@ __global__ void __launch_bounds__(kPlan) k_fork_plan(PagesArgs a) {
       atomicMin(&s_first[parent], tid);
     }
   }
-  __syncthreads();
+  // every old sequence gives its pages up
+  const bool low = take_off(a);
   // its last page, if partly filled, is the first child's if nobody else has it, and copied for others
   const int full = len >> c.page_shift, rest = len & (P - 1);
-  int part = -1;
-  bool copies = false;
-  if (rest) {
-    part = c.table[(size_t)parent * c.max_pages + full];
-    if (!is_page(c, part)) {
-      set_status(a.status, CDSL_ERANGE);
-      part = -1;
-    } else {
-      copies = s_first[parent] != tid || a.refs[part] != 1;
-      atomicAdd(a.new_refs + part, 1);         // (kept; or, until the free pages are dealt, read from)
-    }
+  int part = rest ? c.table[(size_t)parent * c.max_pages + full] : -1;
+  const bool is = is_page(c, part);
+  // (one entry, and the count that belongs to it)
+  const bool copies = is && (s_first[parent] != tid || a.refs[part] != 1 || __ldcg(a.new_refs + part) != 0);
+  __syncthreads();
+  if (low) settle(a);
+  if (is) atomicAdd(a.new_refs + part, 1);     // (kept; or, until the free pages are dealt, read from)
+  if (rest && !is) {
+    set_status(a.status, CDSL_ERANGE);
+    part = -1;
   }
   // whole pages are shared
   for (long long i = tid; i < (long long)a.new_batch * c.max_pages; i += kPlan) {
@@ -194,9 +219,6 @@ __global__ void __launch_bounds__(kPlan) k_resize(PagesArgs a) {
   const int tid = threadIdx.x;
   pdl_wait();
   pdl_launch_dependents();
-  if (a.new_refs != a.refs)
-    for (int p = tid; p < c.n_pages; p += kPlan) a.new_refs[p] = a.refs[p];
-  __syncthreads();
   const long long n = (long long)c.batch * c.max_pages;
   const auto columns = [&](int b) {            // that sequence b is to have
     const long long most = (long long)c.max_pages << c.page_shift;
@@ -205,19 +227,19 @@ __global__ void __launch_bounds__(kPlan) k_resize(PagesArgs a) {
   };
   for (int b = tid; b < c.batch; b += kPlan)
     if (a.lens[b] < 0 || a.lens[b] > (long long)c.max_pages << c.page_shift) set_status(a.status, CDSL_ERANGE);
+  if (take_off(a)) settle(a);
   int missing = 0;
-  for (long long i = tid; i < n; i += kPlan) {
+  for (long long i = tid; i < n; i += kPlan) { // (in its place each entry is read before it is written)
     int page = c.table[i];
     const bool is = is_page(c, page);
     if (!is && page != -1) set_status(a.status, CDSL_ERANGE);
     if (i % c.max_pages >= columns((int)(i / c.max_pages))) {
-      if (is) give_up(a, page);
       page = -1;
-    } else if (!is) {
+    } else if (is) {
+      atomicAdd(a.new_refs + page, 1);         // (kept)
+    } else {
       ++missing;
       page = -2;
-    } else if (__ldcg(a.new_refs + page) < 1) {
-      set_status(a.status, CDSL_EINVAL);       // (this entry holds it)
     }
     a.new_table[i] = page;
   }
@@ -246,10 +268,12 @@ __global__ void __launch_bounds__(kPlan) k_compact_plan(PagesArgs a) {
   pdl_wait();
   pdl_launch_dependents();
   int mine = 0, live;
+  bool low = false;                            // counts that are not the table's
   for (int p = tid; p < c.n_pages; p += kPlan) {
     const int r = a.refs[p];
-    if (r < 0) set_status(a.status, CDSL_EINVAL);
+    low = low || r < 0;
     mine += r > 0;
+    a.entries[p] = 0;
   }
   scan(mine, &live);
   // the k-th hole below `live`, and the k-th page in use from there on, belong together
@@ -257,7 +281,7 @@ __global__ void __launch_bounds__(kPlan) k_compact_plan(PagesArgs a) {
   for (int p0 = 0; p0 < c.n_pages; p0 += kPlan) {
     const int p = p0 + tid;
     const int r = p < c.n_pages ? a.refs[p] : 0;
-    const bool low = p < live, hole = low && r <= 0, mover = !low && r > 0;
+    const bool front = p < live, hole = front && r <= 0, mover = !front && r > 0;
     int h, m;
     const int hk = holes + scan(hole, &h), mk = movers + scan(mover, &m);
     if (hole) a.moves[hk].to = p;
@@ -281,11 +305,13 @@ __global__ void __launch_bounds__(kPlan) k_compact_plan(PagesArgs a) {
   __syncthreads();
   for (long long i = tid; i < (long long)c.batch * c.max_pages; i += kPlan) {
     const int page = c.table[i];
-    if (!is_page(c, page) && page != -1) set_status(a.status, CDSL_ERANGE);
-    const int to = is_page(c, page) ? a.page_map[page] : -1;
-    if (to < 0 && is_page(c, page)) set_status(a.status, CDSL_EINVAL);   // (an entry of a page that nobody holds)
+    const bool is = is_page(c, page);
+    if (!is && page != -1) set_status(a.status, CDSL_ERANGE);
+    const int to = is ? a.page_map[page] : -1; // (-1 of a page whose count is 0)
+    if (is) low = low || atomicAdd(a.entries + page, 1) >= (to < 0 ? 0 : a.new_refs[to]);
     a.new_table[i] = to;
   }
+  if (__syncthreads_or(low) && tid == 0) set_status(a.status, CDSL_EINVAL);
   if (tid == 0) {
     *a.n_moves = movers;
     *a.n_live = live;
@@ -336,7 +362,7 @@ cudaError_t launch_copies(const Cache& c, const PagesArgs& a, long long most, cu
   return launch_pdl(k_copy_pages, dim3(blocks), dim3(kCopy), 0, s, c, (const int*)a.n_moves, (const Move*)a.moves);
 }
 
-// Workspace: the moves' number, the moves, the free pages.
+// Workspace: the moves' number, the moves, the free pages (or the entries of each).
 struct Sizes { size_t moves, free_pages, bytes; };
 Sizes sizes_of(const Cache& c, int new_batch) {
   auto up = [](size_t n) { return (n + 255) / 256 * 256; };
@@ -357,7 +383,7 @@ bool workspace(const Check& ck, PagesArgs* a, int new_batch, void* ws, size_t by
   char* const p = static_cast<char*>(ws);
   a->n_moves = reinterpret_cast<int*>(p);
   a->moves = reinterpret_cast<Move*>(p + z.moves);
-  a->free_pages = reinterpret_cast<int32_t*>(p + z.free_pages);
+  a->free_pages = a->entries = reinterpret_cast<int32_t*>(p + z.free_pages);
   return true;
 }
 
