@@ -139,11 +139,13 @@ CDSL_API int32_t cdsl_tree_attention(const cdsl_kv_cache* cache, int32_t layer, 
 /* Which sequence has which pages. A program that deals pages out keeps, next to its page table, d_refs [n_pages]:
  * how many entries of its tables hold each page (0: free). The three calls below make a new table and new counts from
  * old ones, on the device and in order of nothing but their indexes: free pages are dealt lowest first. Table entries
- * of -1 hold nothing; others outside [0, n_pages) latch CDSL_ERANGE and count as -1. Holders beyond the table (a prefix
- * that is kept, another table of the pool) are counts that the caller has added. Counts that are below the table's own
- * entries (or below 0) latch CDSL_EINVAL: such a page counts as held by the entries alone, so that none that an entry keeps is
- * dealt out (cdsl_kv_compact, which deals none out, goes by the counts: entries of a page with 0 become -1). d_workspace: cdsl_kv_pages_workspace bytes, 256-byte aligned, in any state; it holds nothing between
- * calls. new_batch there: of the new table, the largest of those that are to use it. */
+ * of -1 hold nothing; others outside [0, n_pages) latch CDSL_ERANGE and count as -1 (cdsl_kv_fork does so where a new sequence
+ * was to have the entry, for -1 too; entries that nobody goes on with are given back if they are pages). Holders beyond the
+ * table (a prefix that is kept, another table of the pool) are counts that the caller has added. Counts that are below the
+ * table's own entries (or below 0) latch CDSL_EINVAL: such a page counts as held by the entries alone, so that none that an
+ * entry keeps is dealt out (cdsl_kv_compact, which deals none out, goes by the counts: entries of a page with 0 become -1).
+ * d_workspace: cdsl_kv_pages_workspace bytes, 256-byte aligned, in any state; it holds nothing between calls. new_batch
+ * there: of the new table, the largest of those that are to use it. */
 CDSL_API int32_t cdsl_kv_pages_workspace(const cdsl_kv_cache* cache, int32_t new_batch, size_t* bytes);
 
 /* The cache's sequences become others: new sequence i, i < new_batch (1 .. 1024), goes on from the d_lens[d_src[i]] cached

@@ -136,3 +136,22 @@ def test_one_count_too_low_among_many(cdsl, B, cols):
         st, out = status(), [torch.full(s, 77, dtype=torch.int32, device="cuda") for s in ((B, cols), (n,), (n,), (1,))]
         cdsl.cdsl_kv_compact(c, ints(*refs), *out, workspace(cdsl, c), status=st)
         assert int(st) == want and out[0].tolist() == plain_compact(table, refs)[0]
+
+
+def test_fork_latches_the_entries_that_a_successor_was_to_have(cdsl):
+    """Pages that are not, whole or partly filled, inside the length; none behind it or of a sequence without successors."""
+    P, n = 16, 8
+    refs = [1, 1, 1, 1, 0, 0, 0, 0]
+
+    def fork(table, src, lens):
+        c = pool(cdsl, U8, 1, n, 1, P, 64, tensor(table))
+        st, out = status(), [torch.full(s, 77, dtype=torch.int32, device="cuda") for s in ((len(src), 3), (len(src),), (n,))]
+        cdsl.cdsl_kv_fork(c, ints(*refs), ints(*src), ints(*lens), *out, workspace(cdsl, c, len(src)), status=st)
+        return [int(st)] + [x.tolist() for x in out]
+
+    keeps = [cdsl.CDSL_OK, [[0, 1, -1]], [20], [1, 1, 0, 0, 0, 0, 0, 0]]
+    assert fork([[0, 1, 99], [2, 3, -1]], [0], [20, 0]) == keeps          # behind the length
+    assert fork([[0, 1, -1], [2, 3, -7]], [0], [20, 48]) == keeps         # without successors
+    for bad in (-1, 8, -(1 << 31)):
+        assert fork([[0, bad, 1], [2, 3, -1]], [0], [40, 0]) == [cdsl.CDSL_ERANGE, [[0, -1, 1]], [40], [1, 1, 0, 0, 0, 0, 0, 0]]
+        assert fork([[0, 1, bad], [2, 3, -1]], [0], [40, 0]) == [cdsl.CDSL_ERANGE, [[0, 1, -1]], [32], [1, 1, 0, 0, 0, 0, 0, 0]]
