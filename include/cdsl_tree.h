@@ -161,10 +161,12 @@ CDSL_API int32_t cdsl_kv_fork(const cdsl_kv_cache* cache, const int32_t* d_refs,
                               int32_t* d_new_refs, void* d_workspace, size_t workspace_bytes, int32_t* d_status,
                               void* stream);
 
-/* Sequence b gets the pages of its first d_slots[b] slots: entries behind them are given back (0: all), then missing ones
- * get free pages, in order of sequences and columns. Where there are none left, CDSL_ENOMEM is latched and entries stay -1. A
- * d_slots[b] outside 0 .. max_pages * page_size latches CDSL_ERANGE and counts as the nearer bound. d_new_table [batch,
- * max_pages] and d_new_refs [n_pages] may be the cache's table and d_refs themselves. */
+/* Sequence b gets the pages of its first d_slots[b] slots: entries behind them are given back (0: all), then missing ones get
+ * free pages, in order of sequences and columns. Where there are none left, CDSL_ENOMEM is latched and entries stay -1. A
+ * d_slots[b] outside 0 .. max_pages * page_size latches CDSL_ERANGE and counts as the nearer bound. The page in which the last of
+ * the slots lies stays, whoever else holds it, and what is then written behind them changes the other holders' rows too: a
+ * sequence that goes back to a length inside a page that it shares is to be forked with that length, which copies
+ * the page's rows. d_new_table [batch, max_pages] and d_new_refs [n_pages] may be the cache's table and d_refs themselves. */
 CDSL_API int32_t cdsl_kv_resize(const cdsl_kv_cache* cache, const int32_t* d_refs, const int32_t* d_slots,
                                 int32_t* d_new_table, int32_t* d_new_refs, void* d_workspace, size_t workspace_bytes,
                                 int32_t* d_status, void* stream);

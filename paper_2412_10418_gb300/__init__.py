@@ -501,7 +501,8 @@ def cdsl_kv_fork(cache: KvCache, refs, src, lens, new_table, new_lens, new_refs,
 
 def cdsl_kv_resize(cache: KvCache, refs, slots, new_table, new_refs, workspace, status=None, stream=None):
     """Sequence b has the pages of its first slots[b] slots afterwards: those behind are given back, missing ones dealt
-    from the free ones (refs 0), lowest first. new_table and new_refs may be cache.page_table and refs."""
+    from the free ones (refs 0), lowest first. A page that the last slot lies in stays even if others hold it: to go back to
+    a length inside a shared page, fork with that length. new_table and new_refs may be cache.page_table and refs."""
     fn = "cdsl_kv_resize"
     dev = cache.device
     _check(lib().cdsl_kv_resize(

@@ -155,3 +155,26 @@ def test_fork_latches_the_entries_that_a_successor_was_to_have(cdsl):
     for bad in (-1, 8, -(1 << 31)):
         assert fork([[0, bad, 1], [2, 3, -1]], [0], [40, 0]) == [cdsl.CDSL_ERANGE, [[0, -1, 1]], [40], [1, 1, 0, 0, 0, 0, 0, 0]]
         assert fork([[0, 1, bad], [2, 3, -1]], [0], [40, 0]) == [cdsl.CDSL_ERANGE, [[0, 1, -1]], [32], [1, 1, 0, 0, 0, 0, 0, 0]]
+
+
+@pytest.mark.parametrize("dtype", [U8, F8, BF])
+def test_going_back_into_a_shared_page_by_a_fork(cdsl, dtype):
+    """Two beams share a prompt's two whole pages; one goes back to 20 of its 32 tokens and writes others: the second beam's
+    rows stay."""
+    P, cols, n = 16, 3, 8
+    cache = pool(cdsl, dtype, 2, n, 2, P, 64, tensor([[0, 1, -1], [0, 1, -1]]))
+    refs = ints(2, 2, 0, 0, 0, 0, 0, 0)
+    before, st = raw(cache), status()
+    out = [torch.full(s, 77, dtype=torch.int32, device="cuda") for s in ((2, cols), (2,), (n,))]
+    cdsl.cdsl_kv_fork(cache, refs, ints(0, 1), ints(20, 32), *out, workspace(cdsl, cache, 2), status=st)
+    assert [x.tolist() for x in out] == [[[0, 2, -1], [0, 1, -1]], [20, 32], [2, 1, 1, 0, 0, 0, 0, 0]]
+    forked = cache.at(out[0])
+    k = torch.ones((2, 8, 2, 64), dtype=BF, device="cuda")
+    for layer in range(2):
+        cdsl.cdsl_kv_write(forked, layer, k, k, out[1], ints(8, 0), status=st)
+    now = raw(cache)
+    for x, y in zip(before, now):
+        assert torch.equal(y[:, :2], x[:, :2])                            # the prompt's pages
+        assert torch.equal(y[:, 2, :, :, :4], x[:, 1, :, :, :4])          # the copied rows
+        assert not torch.equal(y[:, 2, :, :, 4:12], x[:, 1, :, :, 4:12])  # and the new ones
+    assert int(st) == cdsl.CDSL_OK
