@@ -9,9 +9,12 @@
 // conversions at 2 or 4 and a difference, measured), 7 a score, where its exponential takes 4. Here the chunk's V is
 // turned into fp16 once for all rows instead, with its power-of-two scales multiplied in relative to a reference (the
 // largest of the first chunk, raised when one passes it by more than 2^kVRoom), and P into
-// fp16 by one conversion a pair: 2^-12 of itself, over 22 octaves below a row's reference. That is exact for V's scales
-// down to 2^-kVBelow of the reference; a chunk with a smaller one has V in bf16, exact over fp32's range, and P in two
-// bf16 planes (2^-17), as has a bf16 cache with its V as it is.
+// fp16 by one conversion a pair: 2^-12 of itself down to 2^-21 of a row's reference, and 2^-32 of that below, which is nothing
+// beside a V of much the same size. V is exact for scales down to 2^-kVBelow of the reference. From a chunk with a
+// smaller one on, to the end of what the block has of the item, V is in bf16, exact over fp32's range, and P in two bf16 planes
+// (2^-17), as a bf16 cache's are with its V as it is: the slot with that V may be the one whose weight is the reference, and those
+// below 2^-32 of it, chunks later, all that the row has. (Of that chunk alone, as it was: 1,000 tokens of 2^-33 each behind one
+// with a V of 2^-40 counted for nothing.)
 //
 // A softmax thread has a vector (a TMEM lane) and walks all the chunk's slots (columns): maximum, reference,
 // probabilities and their sum are its own, no value crosses lanes and no barrier stands in a chunk, whatever
@@ -78,8 +81,8 @@ constexpr float kUp = 7.f;                     // stored times 2^kUp: below fp16
 constexpr int kBuf = 3;                        // S (then P) buffers in TMEM; O has the rest
 constexpr int kVRoom = 6;                      // octaves that V's scales may pass their reference by: 448 * 2^6 in fp16,
 constexpr int kVBelow = 15;                    // and lie below it: 2^-9 * 2^-15
-// 4 bits: a probability of less than 2^-32 is nothing in fp16: with scales 16 octaves apart at most, it leaves out 2^-16 of what
-// the row has. V is held 2^kVUp4 larger: a factor that is 2^-4 of a scale is a normal fp16 number down to 14 below.
+// (So in fp16 V's scales lie within 21 octaves of one another, 4 bits: 16, and a probability of less than 2^-32, which is nothing
+// there, leaves out 2^-11, or 2^-16, of what the reference's slot gives, each.) V of 4 bits is held 2^kVUp4 larger: a factor that is 2^-4 of a scale is a normal fp16 number down to 14 below.
 constexpr int kVRoom4 = 4, kVBelow4 = 12, kVUp4 = 4;
 
 template <int HD, int FORMAT>
@@ -433,7 +436,7 @@ __global__ void __launch_bounds__((Cfg<HD, FORMAT>::THREADS), 1)
     bool ok = true;
     for (int unit = begin; unit < end && ok;) {
       const Segment s = segment_at(a, s_first, unit, end);
-      int vref = 0;
+      int vref = 0, vlow = 255;                // V's reference, and its smallest exponent so far (e4m3: of the lane's slots)
       for (int ch = s.c0; ch < s.c1 && ok; ++ch, ++it) {
         const int st = it % NST;
         ok = __all_sync(0xffffffffu, wait_for(TURNED ? &v_full[st] : &k_full[st], parity(it, NST), a.status) &&
@@ -463,10 +466,10 @@ __global__ void __launch_bounds__((Cfg<HD, FORMAT>::THREADS), 1)
             }
           }
           const int vmax = __reduce_max_sync(0xffffffffu, max(most >> 23, most >> 7 & 0xff));
-          const int vmin = __reduce_min_sync(0xffffffffu, min((int)least >> 23, (int)(least << 16) >> 23));
+          vlow = min(vlow, __reduce_min_sync(0xffffffffu, min((int)least >> 23, (int)(least << 16) >> 23)));
           masks = __any_sync(0xffffffffu, masks);
           if (vref == 0 || vmax > vref + kVRoom4) vref = vmax;
-          const bool far = vmin < max(vref - kVBelow4, 1);
+          const bool far = vlow < max(vref - kVBelow4, 1);
           uint32_t* const to = reinterpret_cast<uint32_t*>(sm + C::FACTOR_OFF + st * C::FACTORS) + lane * (2 * G2);
           const auto put = [&](auto factors) {
 #pragma unroll
@@ -539,8 +542,10 @@ __global__ void __launch_bounds__((Cfg<HD, FORMAT>::THREADS), 1)
           vf[e] = e >= n || v == 255 || x < 1 ? 0.f : __uint_as_float((uint32_t)x << 23);
           nan |= (uint32_t)(e < n && v == 255) << e;
           masks = masks || (e < n && v == 255);
-          far = far || (e < n && v != 255 && (F8 ? v > 0 && x < 127 - kVBelow : v != 127));
+          if (F8 && e < n && v != 255 && v > 0) vlow = min(vlow, (int)v);
+          far = far || (!F8 && e < n && v != 255 && v != 127);
         }
+        if (F8) far = vlow < vref - kVBelow;
         far = __any_sync(0xffffffffu, far);
         masks = __any_sync(0xffffffffu, masks);
         if constexpr (!I4) {
