@@ -383,7 +383,22 @@ __global__ void __launch_bounds__(32 * kWarps, Cfg<HD, NQ, F32>::WARPS / kWarps)
 #pragma unroll
           for (int e = 0; e < 4; ++e) s_p[(8 * n + 2 * q4 + (e & 1)) * kPitch + 16 * i + r + 8 * (e >> 1)] = t[n][e];
       }
+      // A key with a scale that is not finite: its scores are NaN, which an infinite one alone would not make them (-inf is nothing
+      // to a maximum). A scale times 0, of two slots a lane: 0 or NaN.
+      uint32_t k_bad[2] = {0u, 0u};
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < G / 2; ++i) k_bad[h] = fma_bf16x2(k_scales[(lane + 32 * h) * (G / 2) + i], 0u, k_bad[h]);
       __syncwarp();                            // (K has been read; the scores)
+      if (__any_sync(0xffffffffu, ((k_bad[0] | k_bad[1]) & 0x7fff7fffu) != 0)) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          if (k_bad[h] & 0x7fff7fffu)
+#pragma unroll 1
+            for (int v = 0; v < 8 * NT; ++v) s_p[v * kPitch + lane + 32 * h] = __uint_as_float(0x7fc00000u);
+        __syncwarp();
+      }
       // ---- the next K
       const uint32_t live_now = x.live;
       const int there = last - slot;           // slots that there are, if fewer than 64
@@ -400,8 +415,8 @@ __global__ void __launch_bounds__(32 * kWarps, Cfg<HD, NQ, F32>::WARPS / kWarps)
         return;
       }
       uint8_t* const v_scales = sm + C::V_OFF + C::CODES;
-      // V's scales of the slots of a pair of the MMA's k, s0 and s0 + 4. (Of one that is not finite, bits 7 .. 14 are all set: 0x80 carries into bit
-      // 15. K's need no look: the scores are NaN.)
+      // V's scales of the slots of a pair of the MMA's k, s0 and s0 + 4. (Of one that is not finite, bits 7 .. 14 are all set: 0x80
+      // carries into bit 15.)
       const int s0 = 16 * (lane >> 3) + 8 * (lane >> 2 & 1) + (lane & 3);
       uint32_t even[G / 2], odd[G / 2];
       if constexpr (G == 4) {
