@@ -126,7 +126,9 @@ CDSL_API int32_t cdsl_tree_attention_workspace(const cdsl_kv_cache* cache, int32
  * scales, which for that are to be the smallest ones, as cdsl_kv_write makes them. Over a bfloat16 cache
  * probabilities are held to 2^-17. float32 queries run on the CUDA cores in fp32. Over a 4-bit cache both run on the
  * tensor cores: bfloat16 queries hold probabilities to 2^-16 for up to 16 query vectors per K/V head, to 2^-12 for more,
- * float32 ones to 2^-23, and queries to 2^-35 of a row's largest value. Where 2^-12 is said, a probability below 2^-21 of
+ * float32 ones to 2^-23, and queries to 2^-35 of a row's largest value, or 2^-138. q . k and scores are to be
+ * within float32's range, and those of bfloat16 queries below 2^24 in size, but for up to 16 vectors over a 4-bit cache: from
+ * there on float32 does not tell whole numbers apart, and larger ones may give NaN. Where 2^-12 is said, a probability below 2^-21 of
  * the row's largest is held to 2^-32 of that instead (below it, it may be nothing) while V's scales lie within
  * 2^21 of one another (4 bits: 2^16), and from where they do not to 2^-16 of itself.
  * d_workspace: cdsl_tree_attention_workspace bytes, 256-byte aligned, in any state; it

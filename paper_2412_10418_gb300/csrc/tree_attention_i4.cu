@@ -65,6 +65,8 @@ struct Cfg {
   // four vectors: each has two columns, of P's two planes, which one MMA then takes for two
   static constexpr bool TWICE = NQ == 4;
   static constexpr int QP = F32 ? 3 : 1, PP = F32 ? 3 : TWICE ? 1 : 2;   // planes of q, and of p in a column
+  // of K's scales: 128 products of 2^15 (a query) and 2^120 (a key's value) stay within float32 (codes times 2^-24 do as they are)
+  static constexpr float DOWN = F32 ? 0x1p-15f : 1.f;
   static constexpr uint32_t CODES = kStretch * RB, SCALES = kStretch * SB;
   static constexpr uint32_t V_OFF = CODES + SCALES;
   static constexpr uint32_t F_OFF = 2 * V_OFF;                     // V's scales / 8 by pairs of slots
@@ -151,7 +153,8 @@ __global__ void __launch_bounds__(32 * kWarps, Cfg<HD, NQ, F32>::WARPS / kWarps)
   const int total = s_first[c.batch], runs = runs_of(a, total);
   if (run >= runs) return;
   const int end = run_begin(run + 1, total, runs);
-  const float fa = a.scale * (F32 ? 0x1p-14f : 0x1p10f);   // of all scores: 2^-14 of the queries, 2^24 of the codes
+  // of all scores: 2^-14 of the queries, 2^24 of the codes or 2^15 of their scales (DOWN)
+  const float fa = a.scale * (F32 ? 2.f : 0x1p10f);
   // (through shared memory, or the compiler knows them as constants and takes two instructions)
   const volatile uint32_t* const masks = s_masks;
   const uint32_t k0 = masks[0], k4 = masks[1], kv = masks[2];
@@ -362,7 +365,7 @@ __global__ void __launch_bounds__(32 * kWarps, Cfg<HD, NQ, F32>::WARPS / kWarps)
           const uint32_t y0 = x0 >> 8, y1 = x1 >> 8;
           const uint32_t lo[4] = {code_f16<F32, 0>(x0, k0), code_f16<F32, 0>(x1, k0), code_f16<F32, 4>(x0, k4), code_f16<F32, 4>(x1, k4)};
           const uint32_t hi[4] = {code_f16<F32, 0>(y0, k0), code_f16<F32, 0>(y1, k0), code_f16<F32, 4>(y0, k4), code_f16<F32, 4>(y1, k4)};
-          const float s0 = bf16_at(sc[0][g / 2], g & 1), s1 = bf16_at(sc[1][g / 2], g & 1);
+          const float s0 = bf16_at(sc[0][g / 2], g & 1) * C::DOWN, s1 = bf16_at(sc[1][g / 2], g & 1) * C::DOWN;
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
             float d[4];
@@ -415,8 +418,7 @@ __global__ void __launch_bounds__(32 * kWarps, Cfg<HD, NQ, F32>::WARPS / kWarps)
         return;
       }
       uint8_t* const v_scales = sm + C::V_OFF + C::CODES;
-      // V's scales of the slots of a pair of the MMA's k, s0 and s0 + 4. (Of one that is not finite, bits 7 .. 14 are all set: 0x80
-      // carries into bit 15.)
+      // V's scales of the slots of a pair of the MMA's k, s0 and s0 + 4; and are they finite?
       const int s0 = 16 * (lane >> 3) + 8 * (lane >> 2 & 1) + (lane & 3);
       uint32_t even[G / 2], odd[G / 2];
       if constexpr (G == 4) {
@@ -455,6 +457,9 @@ __global__ void __launch_bounds__(32 * kWarps, Cfg<HD, NQ, F32>::WARPS / kWarps)
       auto softmax = [&](auto general) {
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
+          // (the query's power of two before the maximum where it is small and after it where it is large: no step leaves
+          // float32's range where the score is inside it)
+          const float f1 = fa * fminf(fb[n], 1.f), f2 = fmaxf(fb[n], 1.f);
           const int v = TWICE ? r & 3 : 8 * n + r;
           uint64_t seen = ~0ull;
           if constexpr (general) {
@@ -477,7 +482,7 @@ __global__ void __launch_bounds__(32 * kWarps, Cfg<HD, NQ, F32>::WARPS / kWarps)
           for (int i = 0; i < kTiles; ++i) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              t[i][e] = s_p[v * kPitch + 16 * i + 4 * e + q4] * fa;
+              t[i][e] = s_p[v * kPitch + 16 * i + 4 * e + q4] * f1;
               if constexpr (general) {
                 if (!(seen >> (16 * i + 4 * e) & 1)) continue;
               }
@@ -486,7 +491,7 @@ __global__ void __launch_bounds__(32 * kWarps, Cfg<HD, NQ, F32>::WARPS / kWarps)
           }
           top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
           top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-          const float mq = top == -INFINITY ? top : top * fb[n];
+          const float mq = top == -INFINITY ? top : top * f2;
           const float was = m[n], mn = fmaxf(was, mq);
           alpha[n] = was == mn ? 1.f : was == -INFINITY ? 0.f : ex2(was - mn);
           raised = raised || was != mn;
@@ -498,7 +503,7 @@ __global__ void __launch_bounds__(32 * kWarps, Cfg<HD, NQ, F32>::WARPS / kWarps)
             float y[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              y[e] = ex2(fmaf(t[i][e], fb[n], -off));
+              y[e] = ex2(fmaf(t[i][e], f2, -off));
               if constexpr (general) {
                 if (!(seen >> (16 * i + 4 * e) & 1)) y[e] = 0.f;
                 sum += y[e];
