@@ -386,22 +386,13 @@ __global__ void __launch_bounds__(32 * kWarps, Cfg<HD, NQ, F32>::WARPS / kWarps)
 #pragma unroll
           for (int e = 0; e < 4; ++e) s_p[(8 * n + 2 * q4 + (e & 1)) * kPitch + 16 * i + r + 8 * (e >> 1)] = t[n][e];
       }
-      // A key with a scale that is not finite: its scores are NaN, which an infinite one alone would not make them (-inf is nothing
-      // to a maximum). A scale times 0, of two slots a lane: 0 or NaN.
+      // Scales times 0, of two slots a lane: is one of them not finite?
       uint32_t k_bad[2] = {0u, 0u};
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int i = 0; i < G / 2; ++i) k_bad[h] = fma_bf16x2(k_scales[(lane + 32 * h) * (G / 2) + i], 0u, k_bad[h]);
       __syncwarp();                            // (K has been read; the scores)
-      if (__any_sync(0xffffffffu, ((k_bad[0] | k_bad[1]) & 0x7fff7fffu) != 0)) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-          if (k_bad[h] & 0x7fff7fffu)
-#pragma unroll 1
-            for (int v = 0; v < 8 * NT; ++v) s_p[v * kPitch + lane + 32 * h] = __uint_as_float(0x7fc00000u);
-        __syncwarp();
-      }
       // ---- the next K
       const uint32_t live_now = x.live;
       const int there = last - slot;           // slots that there are, if fewer than 64
@@ -431,14 +422,22 @@ __global__ void __launch_bounds__(32 * kWarps, Cfg<HD, NQ, F32>::WARPS / kWarps)
       uint32_t even_bad = 0, odd_bad = 0;
 #pragma unroll
       for (int i = 0; i < G / 2; ++i) {
-        even_bad |= (even[i] & 0x7f807f80u) + 0x00800080u;
-        odd_bad |= (odd[i] & 0x7f807f80u) + 0x00800080u;
+        even_bad = fma_bf16x2(even[i], 0u, even_bad);
+        odd_bad = fma_bf16x2(odd[i], 0u, odd_bad);
       }
-      // rows that are not finite, as bits of the lanes' first and second slots
+      const auto nan = [](uint32_t x) { return (x & 0x7fff7fffu) != 0; };   // (else 0 or -0)
+      // rows of V that are not finite, as bits of the lanes' first and second slots; of K: their scores become NaN, which an
+      // infinite scale alone would not make them (-inf is nothing to a maximum)
       uint32_t v_bad[2] = {0u, 0u};
-      if (__any_sync(0xffffffffu, ((even_bad | odd_bad) & 0x80008000u) != 0)) {
-        v_bad[0] = __ballot_sync(0xffffffffu, (even_bad & 0x80008000u) != 0);
-        v_bad[1] = __ballot_sync(0xffffffffu, (odd_bad & 0x80008000u) != 0);
+      if (__any_sync(0xffffffffu, nan(even_bad | odd_bad | k_bad[0] | k_bad[1]))) {
+        v_bad[0] = __ballot_sync(0xffffffffu, nan(even_bad));
+        v_bad[1] = __ballot_sync(0xffffffffu, nan(odd_bad));
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          if (nan(k_bad[h]))
+#pragma unroll 1
+            for (int v = 0; v < 8 * NT; ++v) s_p[v * kPitch + lane + 32 * h] = __uint_as_float(0x7fc00000u);
+        __syncwarp();
       }
       // slots that there are, as bits
       uint64_t valid = there >= 64 ? ~0ull : (1ull << there) - 1;
@@ -461,6 +460,9 @@ __global__ void __launch_bounds__(32 * kWarps, Cfg<HD, NQ, F32>::WARPS / kWarps)
           // float32's range where the score is inside it)
           const float f1 = fa * fminf(fb[n], 1.f), f2 = fmaxf(fb[n], 1.f);
           const int v = TWICE ? r & 3 : 8 * n + r;
+          // (the query's power of two before the maximum where it is small and after it where it is large: no step leaves
+          // float32's range where the score is inside it)
+          const float f1 = fa * fminf(fb[n], 1.f), f2 = fmaxf(fb[n], 1.f);
           uint64_t seen = ~0ull;
           if constexpr (general) {
             const uint32_t* const w = s_mask + v * (kWords + 1);
