@@ -456,9 +456,6 @@ __global__ void __launch_bounds__(32 * kWarps, Cfg<HD, NQ, F32>::WARPS / kWarps)
       auto softmax = [&](auto general) {
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-          // (the query's power of two before the maximum where it is small and after it where it is large: no step leaves
-          // float32's range where the score is inside it)
-          const float f1 = fa * fminf(fb[n], 1.f), f2 = fmaxf(fb[n], 1.f);
           const int v = TWICE ? r & 3 : 8 * n + r;
           // (the query's power of two before the maximum where it is small and after it where it is large: no step leaves
           // float32's range where the score is inside it)
