@@ -209,6 +209,7 @@ extern "C" int32_t cdsl_rope_turns(int32_t rot, double theta, double factor, int
       const double kept = std::min(1.0, std::max(0.0, (original_len * f / two_pi - low) / (high - low)));
       f = f * kept + f / factor * (1.0 - kept);
     }
+    if (!std::isfinite(f)) return ck.fail("factor is too small: a frequency over it is not finite");
     double turn = f / two_pi;
     turn -= std::floor(turn);                                    // (a factor below 1: whole turns say nothing)
     const double scaled = std::ldexp(turn, 64);
