@@ -1,4 +1,4 @@
-"""The attention over a 4-bit cache with keys whose scale is not finite: they stand for NaN."""
+"""The attention over a 4-bit cache with keys and values whose scale is not finite: they stand for NaN."""
 import pytest
 
 pytestmark = pytest.mark.gpu
@@ -48,3 +48,20 @@ def test_a_node_whose_keys_scale_is_not_finite(cdsl, T, H, kvh, hd, dtype, value
         mask[b, :, :] = mask[b] & torch.tensor([-1 ^ (1 << (T - 1))], dtype=torch.int64).to(torch.int32)
     one = nodes[0] - 1
     check(c, 1, q[:, :one], lens, mask, [one] * len(lens), hd ** -0.5, got[:, :one])
+
+
+@SHAPES
+@TYPES
+@pytest.mark.parametrize("value", [float("inf"), float("-inf"), float("nan")])
+@pytest.mark.parametrize("slot", [0, 70, 259])
+def test_a_value_whose_scale_is_not_finite(cdsl, T, H, kvh, hd, dtype, value, slot):
+    """V's, alike: NaN in all of the head's dimensions."""
+    c, q, k, v, lens, mask, nodes = problem(cdsl, T, H, kvh, hd, dtype, 1.0, 11)
+    cdsl.cdsl_kv_write(c.c, 1, k.to(BF).cuda(), v.to(BF).cuda(), ints(0, 0))
+    for b, group in ((0, 0), (1, hd // 32 - 1)):
+        p, i = at(c, b, slot)
+        c.c.scale[1, p, 1, 0, i, group] = value
+    got = attend(cdsl, c, 1, q, lens, mask, nodes, hd ** -0.5)[0]
+    G = H // kvh
+    assert torch.isnan(got[:, :, :G]).all()
+    assert torch.isfinite(got[:, :, G:]).all()
