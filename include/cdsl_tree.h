@@ -207,7 +207,7 @@ typedef struct cdsl_rope_rows {
 /* Each head's first rot dimensions turn with the token's position d_start[b] + d_offset[b, t] (d_offset [batch, T], as
  * cdsl_tree_mask's depths; NULL: t), exactly so for any positions:
  *   (x_i, x_j) -> magnitude * (x_i cos - x_j sin, x_j cos + x_i sin)
- * and the rest of the head stays; computed in fp32. inverse: the other way (sin negated, magnitude as it is), which turns
+ * and the rest of the head stays; computed in fp32 (bfloat16: sines and cosines to 2^-21). inverse: the other way (sin negated, magnitude as it is), which turns
  * the outputs' gradients into the inputs'. k may be NULL (with its output: none). An output may be its input. Both
  * structures are read before the call returns. */
 CDSL_API int32_t cdsl_rope(const cdsl_rope_cfg* rope, int32_t inverse, const cdsl_rope_rows* rows, const void* d_q,

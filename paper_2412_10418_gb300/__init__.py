@@ -560,7 +560,8 @@ _rope_rows: dict = {}
 def cdsl_rope(rope: Rope, q, q_out, start, *, k=None, k_out=None, offset=None, inverse: bool = False, stream=None):
     """q (and k) [batch, T, heads, head_dim] turned by their positions start[b] + offset[b, t] (offset None: t) into q_out
     (and k_out), which may be the same tensors; any strides but the last. inverse: turned back, which takes gradients of the
-    outputs to those of the inputs."""
+    outputs to those of the inputs. (Outputs are written as memory: autograd records nothing, and a training program has
+    both directions in a function of its own.)"""
     fn = "cdsl_rope"
     dt, s, dev = q.dtype, q.shape, rope.device
     code = _types.values.get(dt)

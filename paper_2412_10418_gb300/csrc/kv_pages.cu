@@ -5,8 +5,8 @@
 // free pages are dealt lowest first, in order of sequences and columns. One block plans, as a decoding step's tables
 // are small and all of it hangs on prefix sums over the pages; the rows to be copied are a list for a second kernel,
 // over the whole device, whose blocks are scheduled beside the plan. Bound by the latency of the plan on small calls (a fork of
-// 32 beams 7.7 us, a resize 5, a compaction's plan 5 to 6, by ncu) and by HBM where many layers' pages move: a third of a pool
-// in 8 layers, 700 MB, 113 us, 91 % of the copy bandwidth with the plan apart (118 to 120 as calls; parts of 4 KB a warp 124).
+// 32 beams 8.4 us, a resize 5.0 to 5.6, a compaction's plan 5.3 to 6.4, by ncu) and by HBM where many layers' pages move: a third of a pool
+// in 8 layers, 700 MB, 113 us, 91 % of the copy bandwidth with the plan apart (119 to 122 as calls; parts of 4 KB a warp 124).
 #include <cuda.h>
 
 #include <algorithm>

@@ -6,8 +6,8 @@
 // Its nearest quarter is taken off in whole numbers and the rest, at most an eighth of a turn, goes through sincospif.
 //
 // Bound by HBM on large calls and by the launch on a decoding step's: 4 x 4093 tokens of 48 heads of 128 in bf16, 96 of them
-// turned, and their gradients (two calls, 805 MB): 132 us as neighbours, 145 as halves, 90 and 82 % of the copy bandwidth; one
-// token 2.6 us in a graph. What counts there is instructions, of which 16 bytes have room for some fifty: a token by a
+// turned, and their gradients (two calls, 805 MB): 128 us as neighbours, 93 % of the copy bandwidth; halves of whole heads 137, 87 %;
+// one token 2.4 us in a graph. What counts there is instructions, of which 16 bytes have room for some fifty: a token by a
 // block, with the sines through shared memory and each address worked out, took 167 us; heads' addresses worked out in a
 // warp's loop 235; blocks of 256 threads 150; eight heads loaded together 179; halves by 16 bytes of each side, with as
 // many angles in registers, 240.

@@ -1,12 +1,12 @@
 // tree_attention_i4.cu -- cdsl_tree_attention over a 4-bit cache: float32 queries, and bf16 ones of at most 16 query
 // vectors per K/V head (more: tree_attention_rows.cu).
 //
-// A row of 128 values is 72 bytes, so that what bounds a large pass is less the bytes than the work on each of them:
-// in the time in which HBM brings an SM two chunks of 64 slots its four schedulers issue 3,000 instructions, for 32,768 codes. Slots are the MMA's M as in tree_attention_tc.cu, but codes go from
-// shared memory to registers, become 16-bit operands there and are multiplied there (mma.sync m16n8k16); through shared memory
-// to tcgen05 they would be written and read once more, in 16 bits four times their size, which alone takes longer than
-// HBM does. A row's groups take turns by four values, so that one 8- or 16-byte load gives a lane the fragments of all
-// groups.
+// A row of 128 values is 72 bytes, so that what bounds a large pass is less the bytes than the work on each of them: in the
+// time in which HBM brings an SM two chunks of 64 slots its four schedulers issue 3,000 instructions, for 32,768 codes.
+// Slots are the MMA's M as in tree_attention_tc.cu, but codes go from shared memory to registers, become 16-bit operands
+// there and are multiplied there (mma.sync m16n8k16); through shared memory to tcgen05 they would be written and read once
+// more, in 16 bits four times their size, which alone takes longer than HBM does. A row's groups take turns by four
+// values, so that one 8- or 16-byte load gives a lane the fragments of all groups.
 //
 //   S^T = K Q^T    K's operand is a code plus 8 as the bits of an fp16 number below 2^-14, one instruction for two of
 //                  them: (word & 0x000f000f) ^ 0x00080008 = (code + 8) 2^-24, the next four bits 2^-20. What the 8
@@ -26,8 +26,8 @@
 // no barrier but its own; its K and V come by bulk copies, the next stretch's K while this one's softmax and P V run, and V
 // beside the next scores.
 //
-// Measured, 32 heads over 8 of 128: 64 sequences of up to 8192 tokens, one token (453 MB): 111 us, 60 % of the copy
-// bandwidth; 8 sequences of 16,384, 4 / 8 / 16 vectors: 48 / 50 / 70 us; one of 512 tokens 8.6 us in a graph with the joining. Bound by
+// Measured, 32 heads over 8 of 128: 64 sequences of up to 8192 tokens, one token (453 MB): 113 us, 59 % of the copy
+// bandwidth; 8 sequences of 16,384, 4 / 8 / 16 vectors: 47 / 50 / 70 us; one of 512 tokens 8.9 us in a graph with the joining. Bound by
 // instructions: 2,900 a chunk of 128 slots, 2.2 a cycle and SM, half of the integer pipe's rate (masks, shifts, byte moves) and
 // a third of the tensor cores'. Steps on the way (us, the large case): by the CUDA cores 505; codes turned as above, K's
 // and V's rows by a warp of 64 slots 181; no selects on V's scales 148; scores through shared memory and loops rolled, masks as one

@@ -35,12 +35,11 @@
 // Between two items the next one's queries and masks are staged as soon as the last S has read this one's, beside
 // the last P V (33 trees of 48 after 115 tokens: 7 % less).
 //
-// Measured: 8 trees of 25 nodes, 100 vectors a K/V head, up to 32,768 tokens of 8 heads of 128 in e4m3: 146 to 155 us,
-// 385 to 415 TFLOP/s, 40 % of the copy bandwidth (16,384 tokens each 111 us; with V's scales far apart in every chunk 174; calls
-// one after another 159, and 152 since MMAs are issued by an elected lane, see warp_umma). A chunk takes 3,000 cycles, of which its
-// MMAs need 1,024; a softmax thread spends 1,500 on the maxima, 2,000 on the probabilities and the rest waiting. What holds it is latency (166
-// cycles a TMEM load), shared memory, which operands, conversion and factors keep busy for 1,900, and instruction
-// fetches: the roles together are about as large as the instruction cache, and the same kernel took 150 to 190 us
+// Measured: 8 trees of 25 nodes, 100 vectors a K/V head, up to 32,768 tokens of 8 heads of 128 in e4m3: 150 us, 400
+// TFLOP/s, 40 % of the copy bandwidth (16,384 tokens each 111 us; with V's scales far apart from the first chunk on 174). A
+// chunk takes 3,000 cycles, of which its MMAs need 1,024; a softmax thread spends 1,500 on the maxima, 2,000 on the
+// probabilities and the rest waiting. What holds it is latency (166 cycles a TMEM load), shared memory, which operands,
+// conversion and factors keep busy for 1,900, and instruction fetches: the roles together are about as large as the instruction cache, and the same kernel took 150 to 190 us
 // with the sizes of its loops (0.4 to 1.6 million misses a call), which are kept rolled for that. A third group of
 // softmax warps: 177 us. At 36 vectors 8 sequences of 16,384 take 99.5 us, two blocks of 32 on
 // tree_attention_tc.cu 117. At 32, 70 there and 92 here. A block has 128 rows whatever it holds: 8 trees of 32 nodes of four
@@ -48,11 +47,12 @@
 //
 // A 4-bit cache's rows land packed, and eight warps turn them into tiles with their scales multiplied in: K into bf16, in which
 // a value is exact (4 bits of scale by 3 of code), with Q as it is; V as e4m3's is, into fp16 under a reference from
-// 2^kVRoom4 above it to 2^-kVBelow4 below, and into bf16 in chunks with smaller scales. A tile's dimensions are in the order in
+// 2^kVRoom4 above it to 2^-kVBelow4 below, and into bf16 from a chunk with smaller scales on (a group of zeros
+// has 2^-120). A tile's dimensions are in the order in
 // which a row's words give them (one of each of two groups in turn), so that a word is 16 bytes of it and takes no byte moves; Q is
 // staged, and O written, in that order. V's factors come from the scaling warp. Measured: 8 trees of 25 nodes after up to 32,768
-// tokens (243 MB): 155 us among other calls, 163 one after another, where e4m3 takes 152; 8 sequences of 16,384 of 20 / 36 / 100
-// vectors 98 / 102 / 116 (of 16: 70 by tree_attention_i4.cu). Of the 98, conversions are some 20, softmax 15, an empty
+// tokens (243 MB): 152 to 160 us by inputs, where e4m3 takes 150; 8 sequences of 16,384 of 20 / 36 / 100
+// vectors 97 / 102 / 115 (of 16: 70 by tree_attention_i4.cu). Of the 97, conversions are some 20, softmax 15, an empty
 // pipeline 60 (20 of them whatever the length). Steps and trials, the trees among other calls: both conversions by four warps 174,
 // loops unrolled twice 184, four times 236; eight warps 164; factors by the scaling warp 161; and one after another, from 174
 // there: MMAs by an elected lane 172, factors by integer moves 167, stages loaded as they become free 163.
@@ -82,7 +82,8 @@ constexpr int kBuf = 3;                        // S (then P) buffers in TMEM; O 
 constexpr int kVRoom = 6;                      // octaves that V's scales may pass their reference by: 448 * 2^6 in fp16,
 constexpr int kVBelow = 15;                    // and lie below it: 2^-9 * 2^-15
 // (So in fp16 V's scales lie within 21 octaves of one another, 4 bits: 16, and a probability of less than 2^-32, which is nothing
-// there, leaves out 2^-11, or 2^-16, of what the reference's slot gives, each.) V of 4 bits is held 2^kVUp4 larger: a factor that is 2^-4 of a scale is a normal fp16 number down to 14 below.
+// there, leaves out 2^-11, or 2^-16, of what the reference's slot gives, each.) V of 4 bits is held 2^kVUp4 larger: a factor
+// that is 2^-4 of a scale is a normal fp16 number down to 14 below.
 constexpr int kVRoom4 = 4, kVBelow4 = 12, kVUp4 = 4;
 
 template <int HD, int FORMAT>
