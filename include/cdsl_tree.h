@@ -128,8 +128,9 @@ CDSL_API int32_t cdsl_tree_attention_workspace(const cdsl_kv_cache* cache, int32
  * tensor cores: bfloat16 queries hold probabilities to 2^-16 for up to 16 query vectors per K/V head, to 2^-12 for more,
  * float32 ones to 2^-23, and queries to 2^-35 of a row's largest value, or 2^-138. q . k and scores are to be
  * within float32's range, and those of bfloat16 queries below 2^24 in size, but for up to 16 vectors over a 4-bit cache: from
- * there on float32 does not tell whole numbers apart, and larger ones may give NaN. Where 2^-12 is said, a probability below 2^-21 of
- * the row's largest is held to 2^-32 of that instead (below it, it may be nothing) while V's scales lie within
+ * there on float32 does not tell whole numbers apart, and larger ones may give NaN. Where 2^-8 is said, a probability is held
+ * to a step of 2^-21 of the largest in its 128 slots, if that is more, while V's scales there lie within 2^8 of one another.
+ * Where 2^-12 is said, one below 2^-21 of the row's largest is held to 2^-32 of that instead (below it, it may be nothing) while V's scales lie within
  * 2^21 of one another (4 bits: 2^16), and from where they do not to 2^-16 of itself.
  * d_workspace: cdsl_tree_attention_workspace bytes, 256-byte aligned, in any state; it
  * holds nothing between calls. */
